@@ -285,6 +285,100 @@ int acespec_convert_v_cache(const void *src, void *dst, int planes, int capacity
                             acespec_dtype dtype, acespec_v_direction direction,
                             hipStream_t stream);
 
+/* ---- The KV cache in 4 bits -------------------------------------------------------------
+ * Slots are held in blocks of 32.  A group is 32 consecutive head dims of one key, or the 32
+ * slots of a block for one head dim of the values; its elements are e2m1 values (0, 1/2, 1,
+ * 3/2, 2, 3, 4, 6 and their negatives) times one power of two 2^e.  With top the group's
+ * largest magnitude, e = floor(log2 top) - 2, one more if top >= 1.75 * 2^floor(log2 top), and
+ * at least -13; an element is held as the nearest such value (ties to the even code), so it is
+ * off by at most 2^e.  A group with a NaN, an infinity or a magnitude of 57344 or more (fp16
+ * could not hold it) is marked instead, and all 32 elements read as NaN.
+ *  blocks  [n_layers][B][n_kv_heads][capacity / 32] records of 34 * head_dim bytes (17/32
+ *          byte an element).  A record's inner order is that of the attention's matrix
+ *          operands; acespec_quantize_kv and acespec_commit_kv_quant write it,
+ *          acespec_dequantize_kv reads it back.
+ *  tail_k, tail_v  the slots of the last, incomplete block and behind them the tree's rows,
+ *          in the model dtype: [n_layers][B][n_kv_heads][tail_capacity][head_dim] and
+ *          [..][head_dim][tail_capacity], as in acespec_kv_cache.
+ * A session of P = prefix_len[b] slots holds slots [0, P / 32 * 32) in blocks, slot
+ * P / 32 * 32 + i in tail slot i (i < P % 32), and tree row r in tail slot P % 32 + r.
+ * P % 32 = 0 leaves no slot in the tail, and P may be 0. */
+typedef struct {
+  void *blocks;
+  void *tail_k, *tail_v;
+  int capacity;                 /* slots in blocks; a positive multiple of 32             */
+  int tail_capacity;            /* a multiple of 64; at least 31 + N + 1 where a tree of N
+                                   drafted nodes is verified or committed               */
+  const int32_t *prefix_len;    /* [B] DEVICE; at most capacity + 31                     */
+} acespec_kv_quant;
+
+/* Which positions a row at position p attends to, besides the tree mask: with window > 0
+ * those in (p - window, p] and those below sinks (the first tokens, which stay visible);
+ * window 0: all, whatever sinks is.  Positions are not renumbered: keys keep the rotation of
+ * their own position.  A row always sees itself.  A NULL span is {0, 0}. */
+typedef struct {
+  int window;   /* >= 0 */
+  int sinks;    /* >= 0 */
+} acespec_attn_span;
+
+/* Brings a cache to 4 bits (the model's dtype, shapes of ctx): of every session the complete
+ * blocks of slots [0, prefix_len[b]), and the prefix_len[b] % 32 slots behind them copied into
+ * the tail.  prefix_len is kv's; qc's is not read (it may be NULL).
+ *  first [B] DEVICE or NULL: slots below first[b] are taken to be held already, and blocks
+ *          that lie wholly below it are left alone (for prefixes that grew: quantise what was
+ *          appended).
+ *  status [B] DEVICE or NULL: ACESPEC_OK, or ACESPEC_EBADTREE for a session with
+ *          prefix_len[b] outside [0, kv->capacity], beyond qc->capacity + 31, or first[b]
+ *          outside [0, prefix_len[b]]; nothing of such a session is written.
+ * kv->capacity is a multiple of 64; k, v, blocks and the tails are 16-byte aligned and do not
+ * overlap.  Enqueued on stream; ACESPEC_EINVAL before anything is launched for arguments
+ * outside the above. */
+int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
+                        const int32_t *first, int B, int32_t *status, hipStream_t stream);
+
+/* Reads a cache in 4 bits back into one of the model's dtype: slots [first[b] / 32 * 32,
+ * prefix_len[b]) of every session (prefix_len: qc's; kv's is not read).  The elements' values
+ * are exact in bf16 and fp32.  Slots from prefix_len[b] on are left as they were.  first,
+ * status and the rest as above. */
+int acespec_dequantize_kv(acespec_ctx *ctx, const acespec_kv_quant *qc, const acespec_kv_cache *kv,
+                          const int32_t *first, int B, int32_t *status, hipStream_t stream);
+
+/* Tree attention of one layer over a cache in 4 bits: row r of session b, at position
+ * prefix_len[b] + depth(r), attends to the prefix, its ancestors and itself, as far as span
+ * shows them, with scale 1/sqrt(head_dim).
+ *  layer   in [0, n_layers) of ctx's model,
+ *  q, out  [B, N+1, n_heads, head_dim] in the model dtype, q rotated; 16-byte aligned, no
+ *          overlap.  Tail slots prefix_len[b] % 32 + r hold the keys (rotated) and values of the
+ *          tree's rows.  A decode of single tokens is N = 0.
+ *  parent_idx [B, N+1] as in acespec_verify_tree,
+ *  status [B]: ACESPEC_OK or ACESPEC_EBADTREE (parents, or prefix_len outside
+ *          [0, capacity + 31]).
+ * A bf16 model multiplies in fp16 with fp32 sums: queries, and keys and values of the tail,
+ * beyond its range (65504) count as infinite.  A NaN or an infinity among the keys and values
+ * reaches the rows that attend to its slot and no others. */
+int acespec_attention_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, int layer,
+                            const acespec_attn_span *span, const void *q,
+                            const int32_t *parent_idx, int B, int N, void *out, int32_t *status,
+                            hipStream_t stream);
+
+/* acespec_verify_tree, or with q_hat in draft_q's place acespec_verify_tree_scalar_q, over a
+ * cache in 4 bits (exactly one of draft_q and q_hat is given).  The tree's keys and values are
+ * written to its tail in the model dtype and attended to unrounded; nothing is committed. */
+int acespec_verify_tree_quant(acespec_ctx *ctx, const acespec_weights *weights,
+                              const acespec_kv_quant *qc, const acespec_attn_span *span,
+                              const int32_t *tree_tokens, const int32_t *parent_idx,
+                              const float *draft_q, const float *q_hat, const float *uniforms,
+                              int B, int N, const acespec_params *params,
+                              const acespec_outputs *outs, hipStream_t stream);
+
+/* acespec_commit_kv over a cache in 4 bits: the root and the kept rows join the tail's
+ * committed slots, every 32 of which become a block; the rest move to the tail's front.  Tail
+ * slots past them keep stale entries.  Arguments and new_prefix_len as in acespec_commit_kv; a
+ * session is not committed (-1, nothing moved) also where its new blocks do not fit capacity. */
+int acespec_commit_kv_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, const int32_t *path,
+                            const int32_t *path_len, const int32_t *status, int B, int N,
+                            int32_t *new_prefix_len, hipStream_t stream);
+
 /* Message for the last non-OK return on this thread ("" if none). */
 const char *acespec_last_error(void);
 

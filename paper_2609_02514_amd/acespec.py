@@ -22,7 +22,8 @@ EXPORTED = ["acespec_create", "acespec_destroy", "acespec_verify_tree",
             "acespec_verify_tree_scalar_q", "acespec_verify_tail", "acespec_commit_kv",
             "acespec_last_error", "acespec_timing_enable", "acespec_timing_read",
             "acespec_timing_only", "acespec_verify_tail_noalloc", "acespec_pack_weight",
-            "acespec_convert_v_cache"]
+            "acespec_convert_v_cache", "acespec_quantize_kv", "acespec_dequantize_kv",
+            "acespec_attention_quant", "acespec_verify_tree_quant", "acespec_commit_kv_quant"]
 
 
 class ModelDesc(C.Structure):
@@ -49,6 +50,15 @@ class Weights(C.Structure):
 class KVCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("capacity", C.c_int),
                 ("prefix_len", C.c_void_p)]
+
+
+class KVQuant(C.Structure):
+    _fields_ = [("blocks", C.c_void_p), ("tail_k", C.c_void_p), ("tail_v", C.c_void_p),
+                ("capacity", C.c_int), ("tail_capacity", C.c_int), ("prefix_len", C.c_void_p)]
+
+
+class AttnSpan(C.Structure):
+    _fields_ = [("window", C.c_int), ("sinks", C.c_int)]
 
 
 class Params(C.Structure):
@@ -106,6 +116,24 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.acespec_convert_v_cache.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int,
                                             C.c_int, C.c_int, C.c_void_p]
     lib.acespec_convert_v_cache.restype = C.c_int
+    lib.acespec_quantize_kv.argtypes = [C.c_void_p, C.POINTER(KVCache), C.POINTER(KVQuant),
+                                        C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
+    lib.acespec_quantize_kv.restype = C.c_int
+    lib.acespec_dequantize_kv.argtypes = [C.c_void_p, C.POINTER(KVQuant), C.POINTER(KVCache),
+                                          C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
+    lib.acespec_dequantize_kv.restype = C.c_int
+    lib.acespec_attention_quant.argtypes = [C.c_void_p, C.POINTER(KVQuant), C.c_int,
+                                            C.POINTER(AttnSpan), C.c_void_p, C.c_void_p, C.c_int,
+                                            C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.acespec_attention_quant.restype = C.c_int
+    lib.acespec_verify_tree_quant.argtypes = [C.c_void_p, C.POINTER(Weights), C.POINTER(KVQuant),
+                                              C.POINTER(AttnSpan), C.c_void_p, C.c_void_p,
+                                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int,
+                                              C.POINTER(Params), C.POINTER(Outputs), C.c_void_p]
+    lib.acespec_verify_tree_quant.restype = C.c_int
+    lib.acespec_commit_kv_quant.argtypes = [C.c_void_p, C.POINTER(KVQuant), C.c_void_p, C.c_void_p,
+                                            C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
+    lib.acespec_commit_kv_quant.restype = C.c_int
     lib.acespec_last_error.argtypes = []
     lib.acespec_last_error.restype = C.c_char_p
     lib.acespec_timing_enable.argtypes = [C.c_void_p, C.c_int]
@@ -201,6 +229,41 @@ def acespec_convert_v_cache(src: int, dst: int, planes: int, capacity: int, head
                                                  direction, stream))
 
 
+def acespec_quantize_kv(ctx, kv: KVCache, qc: KVQuant, first: Optional[int], B: int,
+                        status: Optional[int], stream: int) -> int:
+    return _check(load().acespec_quantize_kv(ctx, C.byref(kv), C.byref(qc), first, B, status,
+                                             stream))
+
+
+def acespec_dequantize_kv(ctx, qc: KVQuant, kv: KVCache, first: Optional[int], B: int,
+                          status: Optional[int], stream: int) -> int:
+    return _check(load().acespec_dequantize_kv(ctx, C.byref(qc), C.byref(kv), first, B, status,
+                                               stream))
+
+
+def acespec_attention_quant(ctx, qc: KVQuant, layer: int, span: AttnSpan, q: int,
+                            parent_idx: int, B: int, N: int, out: int, status: int,
+                            stream: int) -> int:
+    return _check(load().acespec_attention_quant(ctx, C.byref(qc), layer, C.byref(span), q,
+                                                 parent_idx, B, N, out, status, stream))
+
+
+def acespec_verify_tree_quant(ctx, weights: Weights, qc: KVQuant, span: AttnSpan,
+                              tree_tokens: int, parent_idx: int, draft_q: Optional[int],
+                              q_hat: Optional[int], uniforms: int, B: int, N: int, params: Params,
+                              outputs: Outputs, stream: int) -> int:
+    return _check(load().acespec_verify_tree_quant(ctx, C.byref(weights), C.byref(qc),
+                                                   C.byref(span), tree_tokens, parent_idx,
+                                                   draft_q, q_hat, uniforms, B, N,
+                                                   C.byref(params), C.byref(outputs), stream))
+
+
+def acespec_commit_kv_quant(ctx, qc: KVQuant, path: int, path_len: int, status: Optional[int],
+                            B: int, N: int, new_prefix_len: int, stream: int) -> int:
+    return _check(load().acespec_commit_kv_quant(ctx, C.byref(qc), path, path_len, status, B, N,
+                                                 new_prefix_len, stream))
+
+
 def acespec_timing_enable(ctx, enable: bool) -> None:
     _check(load().acespec_timing_enable(ctx, 1 if enable else 0))
 
@@ -225,6 +288,40 @@ def acespec_timing_read(ctx) -> Dict[str, tuple]:
 
 def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+class QuantCache:
+    """The tensors of a KV cache in 4 bits (acespec_kv_quant): blocks [L, B, Hkv,
+    capacity / 32, 34 hd] uint8, tail_k [L, B, Hkv, tail_capacity, hd] and tail_v [L, B, Hkv,
+    hd, tail_capacity] in the model dtype, prefix_len [B] int32."""
+
+    def __init__(self, blocks, tail_k, tail_v, capacity: int, tail_capacity: int, prefix_len):
+        self.blocks, self.tail_k, self.tail_v = blocks, tail_k, tail_v
+        self.capacity, self.tail_capacity = capacity, tail_capacity
+        self.prefix_len = prefix_len
+        self._struct = None if prefix_len is None else KVQuant(
+            _ptr(blocks), _ptr(tail_k), _ptr(tail_v), capacity, tail_capacity, _ptr(prefix_len))
+
+    @classmethod
+    def alloc(cls, L: int, B: int, Hkv: int, hd: int, capacity: int, max_nodes: int, dtype: str,
+              device="cuda"):
+        """An empty cache of `capacity` slots in blocks, whose tail takes trees of max_nodes
+        drafted nodes."""
+        import torch
+        dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        cap, tail = (capacity + 31) // 32 * 32, (31 + max_nodes + 1 + 63) // 64 * 64
+        return cls(torch.zeros((L, B, Hkv, cap // 32, 34 * hd), dtype=torch.uint8, device=device),
+                   torch.zeros((L, B, Hkv, tail, hd), dtype=dt, device=device),
+                   torch.zeros((L, B, Hkv, hd, tail), dtype=dt, device=device), cap, tail,
+                   torch.zeros(B, dtype=torch.int32, device=device))
+
+    def with_prefix(self, prefix_len) -> "QuantCache":
+        """The same cache under other lengths (a commit's new_prefix_len)."""
+        return QuantCache(self.blocks, self.tail_k, self.tail_v, self.capacity,
+                          self.tail_capacity, prefix_len)
+
+    def struct(self) -> KVQuant:
+        return self._struct
 
 
 class Verifier:
@@ -359,3 +456,92 @@ class Verifier:
                                    _ptr(final_norm), _ptr(hidden), _ptr(draft), _ptr(q),
                                    _ptr(u), R, chain_len, Params(T, top_p, k),
                                    self.outputs_struct(outs), self._stream())
+
+    def _check_quant(self, cache: QuantCache, B: int):
+        """The cache's tensors against this model: a wrong shape, type or stride would be read
+        out of range."""
+        import torch
+        d = self.desc
+        dt = torch.bfloat16 if d.dtype == ACESPEC_BF16 else torch.float32
+        lead = (d.n_layers, B, d.n_kv_heads)
+        want = [("blocks", cache.blocks, lead + (cache.capacity // 32, 34 * d.head_dim), torch.uint8),
+                ("tail_k", cache.tail_k, lead + (cache.tail_capacity, d.head_dim), dt),
+                ("tail_v", cache.tail_v, lead + (d.head_dim, cache.tail_capacity), dt),
+                ("prefix_len", cache.prefix_len, (B,), torch.int32)]
+        self._check_tensors(want)
+
+    @staticmethod
+    def _check_tensors(want):
+        for name, t, shape, dt in want:
+            if tuple(t.shape) != tuple(shape) or t.dtype != dt or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError(f"{name} must be a contiguous {dt} tensor {tuple(shape)} on the "
+                                 f"GPU (got {t.dtype} {tuple(t.shape)} on {t.device})")
+
+    def _check_kv(self, kv_k, kv_v, capacity: int, B: int, more):
+        import torch
+        d = self.desc
+        dt = torch.bfloat16 if d.dtype == ACESPEC_BF16 else torch.float32
+        lead = (d.n_layers, B, d.n_kv_heads)
+        self._check_tensors([("kv_k", kv_k, lead + (capacity, d.head_dim), dt),
+                             ("kv_v", kv_v, lead + (d.head_dim, capacity), dt)]
+                            + [(n, t, (B,), torch.int32) for n, t in more if t is not None])
+
+    def quantize_kv(self, kv_k, kv_v, capacity: int, prefix_len, cache: QuantCache, status=None,
+                    first=None) -> int:
+        """kv's slots [0, prefix_len) brought to 4 bits (acespec_quantize_kv).  The cache's own
+        prefix_len is not touched."""
+        B = prefix_len.shape[0]
+        self._check_kv(kv_k, kv_v, capacity, B, [("prefix_len", prefix_len), ("status", status),
+                                                 ("first", first)])
+        self._check_quant(cache, B)
+        kv = KVCache(_ptr(kv_k), _ptr(kv_v), capacity, _ptr(prefix_len))
+        return acespec_quantize_kv(self.ctx, kv, cache.struct(), _ptr(first), B, _ptr(status),
+                                   self._stream())
+
+    def dequantize_kv(self, cache: QuantCache, kv_k, kv_v, capacity: int, status=None,
+                      first=None) -> int:
+        """Slots [first / 32 * 32, cache.prefix_len) read back into kv (acespec_dequantize_kv)."""
+        B = cache.prefix_len.shape[0]
+        self._check_kv(kv_k, kv_v, capacity, B, [("status", status), ("first", first)])
+        self._check_quant(cache, B)
+        kv = KVCache(_ptr(kv_k), _ptr(kv_v), capacity, None)
+        return acespec_dequantize_kv(self.ctx, cache.struct(), kv, _ptr(first), B, _ptr(status),
+                                     self._stream())
+
+    def attention_quant(self, cache: QuantCache, layer: int, q, parents, out, status,
+                        window: int = 0, sinks: int = 0) -> int:
+        """Tree attention of one layer (acespec_attention_quant): q, out [B, N+1, H, hd]."""
+        import torch
+        d, (B, n1) = self.desc, parents.shape
+        dt = torch.bfloat16 if d.dtype == ACESPEC_BF16 else torch.float32
+        shape = (B, n1, d.n_heads, d.head_dim)
+        self._check_tensors([("q", q, shape, dt), ("out", out, shape, dt),
+                             ("parents", parents, (B, n1), torch.int32),
+                             ("status", status, (B,), torch.int32)])
+        self._check_quant(cache, B)
+        return acespec_attention_quant(self.ctx, cache.struct(), layer, AttnSpan(window, sinks),
+                                       _ptr(q), _ptr(parents), B, n1 - 1, _ptr(out), _ptr(status),
+                                       self._stream())
+
+    def verify_tree_quant(self, wstruct: Weights, cache: QuantCache, tokens, parents, q, u,
+                          T: float, top_p: float, k: int, outs: Dict, window: int = 0,
+                          sinks: int = 0, scalar: bool = False) -> int:
+        """verify_tree over a cache in 4 bits; scalar: q is q_hat [B, N+1]."""
+        B, n1 = tokens.shape
+        self._check_quant(cache, B)
+        return acespec_verify_tree_quant(self.ctx, wstruct, cache.struct(), AttnSpan(window, sinks),
+                                         _ptr(tokens), _ptr(parents), None if scalar else _ptr(q),
+                                         _ptr(q) if scalar else None, _ptr(u), B, n1 - 1,
+                                         Params(T, top_p, k), self.outputs_struct(outs),
+                                         self._stream())
+
+    def commit_kv_quant(self, cache: QuantCache, path, path_len, status, new_prefix_len) -> int:
+        import torch
+        B, n1 = path.shape
+        self._check_quant(cache, B)
+        self._check_tensors([(n, t, s, torch.int32) for n, t, s in (
+            ("path", path, (B, n1)), ("path_len", path_len, (B,)), ("status", status, (B,)),
+            ("new_prefix_len", new_prefix_len, (B,))) if t is not None])
+        return acespec_commit_kv_quant(self.ctx, cache.struct(), _ptr(path), _ptr(path_len),
+                                       _ptr(status), B, n1 - 1, _ptr(new_prefix_len),
+                                       self._stream())

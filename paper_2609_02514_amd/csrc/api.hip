@@ -36,13 +36,13 @@ int fail(int code, const char *fmt, ...) {
 
 enum Kind {
   K_TREE, K_EMBED, K_RMSNORM, K_GEMM_QKV, K_ROPE, K_ATTN, K_GEMM_O, K_GEMM_GATE_UP,
-  K_GEMM_DOWN, K_GEMM_LM, K_VOCAB, K_WALK, K_COMMIT, K_COUNT
+  K_GEMM_DOWN, K_GEMM_LM, K_VOCAB, K_WALK, K_COMMIT, K_QUANTIZE, K_DEQUANTIZE, K_COUNT
 };
 const char *kKindNames[K_COUNT] = {"tree_prep",    "embed",       "rmsnorm",
                                    "gemm_qkv",     "rope_table",  "tree_attention",
                                    "gemm_o",       "gemm_gate_up", "gemm_down",
                                    "gemm_lm_head", "vocab_verify", "path_walk",
-                                   "commit_kv"};
+                                   "commit_kv",    "quantize_kv", "dequantize_kv"};
 
 size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -158,8 +158,24 @@ int check_outputs(const acespec_outputs *o) {
   return ACESPEC_OK;
 }
 
+constexpr int kBlock = 32;   // slots of a block of the cache in 4 bits
+
+size_t quant_layer_bytes(const acespec_model_desc &d, const acespec_kv_quant *qc, int B) {
+  return (size_t)B * d.n_kv_heads * (qc->capacity / kBlock) * 34 * d.head_dim;
+}
+
+// The cache a verify step runs over.  The tree's keys and values go to slots of k and v
+// (capacity cap): behind the prefix, or, over a cache in 4 bits, behind the tail's slots.
+struct CacheView {
+  void *k, *v;
+  int cap;
+  const int32_t *prefix_len;
+  const acespec_kv_quant *quant;   // NULL: k and v hold the prefix too
+  acespec_attn_span span;
+};
+
 template <typename T>
-int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const acespec_kv_cache *kv,
+int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView &kv,
                      const int32_t *tokens, const int32_t *parents, const float *draft_q,
                      const float *q_scalar, const float *uniforms, int B, int N,
                      const acespec_params *p, const acespec_outputs *o, hipStream_t stream) {
@@ -168,15 +184,20 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const acespec_k
   const int n1 = N + 1, R = B * n1;
   const int L = d.n_layers, D = d.d_model, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
   const int F = d.d_ff, V = d.vocab, QKVN = (H + 2 * Hkv) * hd;
-  const int cap = kv->capacity;
+  const int cap = kv.cap;
   A *x_a = (A *)ctx->a, *x_attn = (A *)ctx->attn, *x_q = (A *)ctx->q, *x_h = (A *)ctx->h;
   const GemmAux aux{ctx->gpart, ctx->gpart_cap, ctx->cus,
                    w->layout == ACESPEC_LAYOUT_PACKED ? 1 : 0};
   float *logits = o->logits_out ? o->logits_out : ctx->logits;
   const TreeMeta &meta = ctx->meta;
 
-  RUN(K_TREE, launch_tree_prep(tokens, parents, kv->prefix_len, B, n1, V, cap, meta, o->status,
-                               stream));
+  if (kv.quant)
+    RUN(K_TREE, launch_tree_prep_quant(tokens, parents, kv.prefix_len, B, n1, V,
+                                       kv.quant->capacity, kv.span.window, kv.span.sinks, meta,
+                                       o->status, stream));
+  else
+    RUN(K_TREE, launch_tree_prep(tokens, parents, kv.prefix_len, B, n1, V, cap, meta, o->status,
+                                 stream));
   RUN(K_EMBED, launch_embed<T>((const T *)w->embed, meta.tok, ctx->x, R, D, stream));
   if (L > 0) RUN(K_ROPE, launch_rope_table(meta.pos, ctx->inv_freq, ctx->rot, R, hd / 2, stream));
   const size_t layer_stride = (size_t)B * Hkv * cap * hd;
@@ -187,15 +208,22 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const acespec_k
                      R, D, d.rms_eps, stream)));
   for (int l = 0; l < L; ++l) {
     const acespec_layer_weights &lw = w->layers[l];
-    T *ck = (T *)kv->k + l * layer_stride;
-    T *cv = (T *)kv->v + l * layer_stride;
+    T *ck = (T *)kv.k + l * layer_stride;
+    T *cv = (T *)kv.v + l * layer_stride;
     const RopeOut<T> ro{x_q, ck, cv, ctx->rot, meta.sess_S, n1, H, Hkv, hd, cap};
     RUN(K_GEMM_QKV, (launch_qkv_rope<T, A>(x_a, (const T *)lw.wqkv, R, QKVN, D, ctx->qkv, ro,
                                            meta, B, aux, stream)));
     int nsplit = 1;
-    RUN(K_ATTN, launch_attention<T>(x_q, ck, cv, meta, x_attn, ctx->part_o, ctx->part_ml,
-                                    ctx->part_cap, B, n1, H, Hkv, hd, cap, ctx->cus, stream,
-                                    &nsplit));
+    if (kv.quant)
+      RUN(K_ATTN, launch_attention_quant<T>(
+                      x_q, (const uint8_t *)kv.quant->blocks + l * quant_layer_bytes(d, kv.quant, B),
+                      ck, cv, meta, x_attn, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv,
+                      hd, kv.quant->capacity, cap, kv.span.window, kv.span.sinks, 0, ctx->cus,
+                      stream));
+    else
+      RUN(K_ATTN, launch_attention<T>(x_q, ck, cv, meta, x_attn, ctx->part_o, ctx->part_ml,
+                                      ctx->part_cap, B, n1, H, Hkv, hd, cap, ctx->cus, stream,
+                                      &nsplit));
     RUN(K_GEMM_O, (launch_gemm_resid_norm<T, A>(x_attn, (const T *)lw.wo, R, D, H * hd, ctx->x,
                                                 (const T *)lw.mlp_norm, x_a, d.rms_eps, aux,
                                                 stream)));
@@ -458,9 +486,49 @@ void acespec_destroy(acespec_ctx *c) {
 
 namespace {
 
-// Shared argument checks and dispatch of the two verify_tree entry points (dense draft
-// distributions, or the scalar q-hat of each drafted token).
+bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  return a0 < b0 + nb && b0 < a0 + na;
+}
+
+// A cache in 4 bits for B sessions whose tail takes n1 tree rows behind any prefix (n1 0: no
+// tree).
+int check_quant(const acespec_model_desc &d, const acespec_kv_quant *qc, int B, int n1) {
+  if (!qc) return fail(ACESPEC_EINVAL, "the quantized cache is NULL");
+  if (!qc->blocks || !qc->tail_k || !qc->tail_v || !qc->prefix_len)
+    return fail(ACESPEC_EINVAL, "a pointer of the quantized cache is NULL");
+  if (((uintptr_t)qc->blocks | (uintptr_t)qc->tail_k | (uintptr_t)qc->tail_v) & 15)
+    return fail(ACESPEC_EINVAL, "blocks, tail_k and tail_v must be 16-byte aligned");
+  if (qc->capacity < kBlock || qc->capacity % kBlock != 0 || qc->capacity > 0x7fffff00)
+    return fail(ACESPEC_EINVAL, "capacity must be a positive multiple of 32 (got %d)", qc->capacity);
+  if (qc->tail_capacity < 64 || qc->tail_capacity % 64 != 0 || qc->tail_capacity < kBlock - 1 + n1)
+    return fail(ACESPEC_EINVAL,
+                "tail_capacity must be a multiple of 64 that holds 31 slots and the %d tree rows "
+                "(got %d)", n1, qc->tail_capacity);
+  return ACESPEC_OK;
+}
+
+int check_span(const acespec_attn_span *span, acespec_attn_span *out) {
+  *out = span ? *span : acespec_attn_span{0, 0};
+  if (out->window < 0 || out->sinks < 0)
+    return fail(ACESPEC_EINVAL, "window and sinks must be >= 0 (got %d, %d)", out->window,
+                out->sinks);
+  return ACESPEC_OK;
+}
+
+int check_batch(const acespec_ctx *ctx, int B, int N) {
+  if (B < 1 || B > ctx->max_batch)
+    return fail(ACESPEC_EINVAL, "B must be in [1, %d] (got %d)", ctx->max_batch, B);
+  if (N < 0 || N > ctx->max_nodes)
+    return fail(N > 64 ? ACESPEC_EUNSUPPORTED : ACESPEC_EINVAL,
+                "N must be in [0, %d] (got %d)", ctx->max_nodes, N);
+  return ACESPEC_OK;
+}
+
+// Shared argument checks and dispatch of the verify_tree entry points (dense draft
+// distributions, or the scalar q-hat of each drafted token; over kv, or over qc).
 int verify_tree_checked(acespec_ctx *ctx, const acespec_weights *w, const acespec_kv_cache *kv,
+                        const acespec_kv_quant *qc, const acespec_attn_span *span,
                         const int32_t *tree_tokens, const int32_t *parent_idx,
                         const float *draft_q, const float *q_scalar, const float *uniforms,
                         int B, int N, const acespec_params *p, const acespec_outputs *o,
@@ -469,7 +537,7 @@ int verify_tree_checked(acespec_ctx *ctx, const acespec_weights *w, const acespe
   if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
   const acespec_model_desc &d = ctx->d;
   if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "context has no layers (tail-only model)");
-  if (!w || !kv || !tree_tokens || !parent_idx || !(draft_q || q_scalar) || !uniforms)
+  if (!w || !(kv || qc) || !tree_tokens || !parent_idx || !(draft_q || q_scalar) || !uniforms)
     return fail(ACESPEC_EINVAL, "a required pointer is NULL");
   if (!w->embed || !w->layers || !w->final_norm || !w->lm_head)
     return fail(ACESPEC_EINVAL, "a weight pointer is NULL");
@@ -482,24 +550,31 @@ int verify_tree_checked(acespec_ctx *ctx, const acespec_weights *w, const acespe
     const int rc = check_layout(w->layout, d);
     if (rc) return rc;
   }
-  if (!kv->k || !kv->v || !kv->prefix_len) return fail(ACESPEC_EINVAL, "kv cache pointer NULL");
-  if (B < 1 || B > ctx->max_batch)
-    return fail(ACESPEC_EINVAL, "B must be in [1, %d] (got %d)", ctx->max_batch, B);
-  if (N < 0 || N > ctx->max_nodes)
-    return fail(N > 64 ? ACESPEC_EUNSUPPORTED : ACESPEC_EINVAL,
-                "N must be in [0, %d] (got %d)", ctx->max_nodes, N);
-  if (kv->capacity < N + 1)
-    return fail(ACESPEC_EINVAL, "kv capacity %d cannot hold the %d tree rows", kv->capacity, N + 1);
-  if (kv->capacity % 64 != 0)
-    return fail(ACESPEC_EINVAL, "kv capacity must be a multiple of 64 (got %d)", kv->capacity);
-  int rc = check_params(p, d.vocab);
+  if (kv && (!kv->k || !kv->v || !kv->prefix_len))
+    return fail(ACESPEC_EINVAL, "kv cache pointer NULL");
+  int rc = check_batch(ctx, B, N);
+  if (rc) return rc;
+  CacheView view{};
+  if (qc) {
+    rc = check_quant(d, qc, B, N + 1);
+    if (!rc) rc = check_span(span, &view.span);
+    if (rc) return rc;
+    view = CacheView{qc->tail_k, qc->tail_v, qc->tail_capacity, qc->prefix_len, qc, view.span};
+  } else {
+    if (kv->capacity < N + 1)
+      return fail(ACESPEC_EINVAL, "kv capacity %d cannot hold the %d tree rows", kv->capacity, N + 1);
+    if (kv->capacity % 64 != 0)
+      return fail(ACESPEC_EINVAL, "kv capacity must be a multiple of 64 (got %d)", kv->capacity);
+    view = CacheView{kv->k, kv->v, kv->capacity, kv->prefix_len, nullptr, {0, 0}};
+  }
+  rc = check_params(p, d.vocab);
   if (rc) return rc;
   rc = check_outputs(o);
   if (rc) return rc;
   if (d.dtype == ACESPEC_BF16)
-    return verify_tree_impl<bf16>(ctx, w, kv, tree_tokens, parent_idx, draft_q, q_scalar,
+    return verify_tree_impl<bf16>(ctx, w, view, tree_tokens, parent_idx, draft_q, q_scalar,
                                   uniforms, B, N, p, o, stream);
-  return verify_tree_impl<float>(ctx, w, kv, tree_tokens, parent_idx, draft_q, q_scalar,
+  return verify_tree_impl<float>(ctx, w, view, tree_tokens, parent_idx, draft_q, q_scalar,
                                  uniforms, B, N, p, o, stream);
 }
 
@@ -523,8 +598,8 @@ int acespec_verify_tree(acespec_ctx *ctx, const acespec_weights *w, const acespe
     g_err.clear();
     return fail(ACESPEC_EINVAL, "draft_q is NULL");
   }
-  return verify_tree_checked(ctx, w, kv, tree_tokens, parent_idx, draft_q, nullptr, uniforms, B,
-                             N, p, o, stream);
+  return verify_tree_checked(ctx, w, kv, nullptr, nullptr, tree_tokens, parent_idx, draft_q, nullptr,
+                             uniforms, B, N, p, o, stream);
 }
 
 int acespec_verify_tree_scalar_q(acespec_ctx *ctx, const acespec_weights *w,
@@ -536,8 +611,8 @@ int acespec_verify_tree_scalar_q(acespec_ctx *ctx, const acespec_weights *w,
     g_err.clear();
     return fail(ACESPEC_EINVAL, "q_hat is NULL");
   }
-  return verify_tree_checked(ctx, w, kv, tree_tokens, parent_idx, nullptr, q_hat, uniforms, B,
-                             N, p, o, stream);
+  return verify_tree_checked(ctx, w, kv, nullptr, nullptr, tree_tokens, parent_idx, nullptr, q_hat,
+                             uniforms, B, N, p, o, stream);
 }
 
 int acespec_pack_weight(const void *src, void *dst, int rows, int cols, hipStream_t stream) {
@@ -642,6 +717,170 @@ int acespec_commit_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const int32_
     RUN(K_COMMIT, launch_commit_kv<float>((float *)kv->k, (float *)kv->v, kv->prefix_len, path,
                                           path_len, status, d.n_layers, B, N + 1, d.n_kv_heads,
                                           d.head_dim, kv->capacity, new_prefix_len, stream));
+  return ACESPEC_OK;
+}
+
+int acespec_verify_tree_quant(acespec_ctx *ctx, const acespec_weights *w,
+                              const acespec_kv_quant *qc, const acespec_attn_span *span,
+                              const int32_t *tree_tokens, const int32_t *parent_idx,
+                              const float *draft_q, const float *q_hat, const float *uniforms,
+                              int B, int N, const acespec_params *p, const acespec_outputs *o,
+                              hipStream_t stream) {
+  g_err.clear();
+  if ((draft_q != nullptr) == (q_hat != nullptr))
+    return fail(ACESPEC_EINVAL, "exactly one of draft_q and q_hat must be given");
+  if (!qc) return fail(ACESPEC_EINVAL, "the quantized cache is NULL");
+  return verify_tree_checked(ctx, w, nullptr, qc, span, tree_tokens, parent_idx, draft_q, q_hat,
+                             uniforms, B, N, p, o, stream);
+}
+
+int acespec_attention_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, int layer,
+                            const acespec_attn_span *span, const void *q,
+                            const int32_t *parent_idx, int B, int N, void *out, int32_t *status,
+                            hipStream_t stream) {
+  g_err.clear();
+  if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
+  const acespec_model_desc &d = ctx->d;
+  if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
+  if (!q || !parent_idx || !out || !status) return fail(ACESPEC_EINVAL, "a required pointer is NULL");
+  if (((uintptr_t)q | (uintptr_t)out) & 15)
+    return fail(ACESPEC_EINVAL, "q and out must be 16-byte aligned");
+  if (layer < 0 || layer >= d.n_layers)
+    return fail(ACESPEC_EINVAL, "layer must be in [0, %d) (got %d)", d.n_layers, layer);
+  int rc = check_batch(ctx, B, N);
+  if (!rc) rc = check_quant(d, qc, B, N + 1);
+  acespec_attn_span sp{};
+  if (!rc) rc = check_span(span, &sp);
+  if (rc) return rc;
+  const int n1 = N + 1, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
+  const size_t io = (size_t)B * n1 * H * hd * ctx->esz;
+  if (overlap(q, io, out, io)) return fail(ACESPEC_EINVAL, "q and out overlap");
+  RUN(K_TREE, launch_tree_prep_quant(nullptr, parent_idx, qc->prefix_len, B, n1, 1, qc->capacity,
+                                     sp.window, sp.sinks, ctx->meta, status, stream));
+  const uint8_t *blocks = (const uint8_t *)qc->blocks + layer * quant_layer_bytes(d, qc, B);
+  const size_t tail = (size_t)layer * B * Hkv * qc->tail_capacity * hd;
+  if (d.dtype == ACESPEC_BF16)
+    RUN(K_ATTN, launch_attention_quant<bf16>(
+                    q, blocks, (const bf16 *)qc->tail_k + tail, (const bf16 *)qc->tail_v + tail,
+                    ctx->meta, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
+                    qc->capacity, qc->tail_capacity, sp.window, sp.sinks, 1, ctx->cus, stream));
+  else
+    RUN(K_ATTN, launch_attention_quant<float>(
+                    q, blocks, (const float *)qc->tail_k + tail, (const float *)qc->tail_v + tail,
+                    ctx->meta, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
+                    qc->capacity, qc->tail_capacity, sp.window, sp.sinks, 1, ctx->cus, stream));
+  return ACESPEC_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The arguments that acespec_quantize_kv and acespec_dequantize_kv share; prefix_len is the
+// source's.
+int check_convert(const acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
+                  const int32_t *prefix_len, int B) {
+  if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
+  const acespec_model_desc &d = ctx->d;
+  if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
+  if (!kv || !kv->k || !kv->v || !prefix_len)
+    return fail(ACESPEC_EINVAL, "a pointer of the cache is NULL");
+  if (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15)
+    return fail(ACESPEC_EINVAL, "k and v must be 16-byte aligned");
+  int rc = check_batch(ctx, B, 0);
+  if (rc) return rc;
+  if (kv->capacity < 64 || kv->capacity % 64 != 0)
+    return fail(ACESPEC_EINVAL, "kv capacity must be a positive multiple of 64 (got %d)", kv->capacity);
+  acespec_kv_quant c = qc ? *qc : acespec_kv_quant{};
+  if (qc) c.prefix_len = prefix_len;
+  rc = check_quant(d, qc ? &c : nullptr, B, 0);
+  if (rc) return rc;
+  const size_t planes = (size_t)d.n_layers * B * d.n_kv_heads;
+  if (planes > 0x7fff0000u) return fail(ACESPEC_EINVAL, "%zu planes exceed one launch", planes);
+  const size_t eb = d.dtype == ACESPEC_BF16 ? 2 : 4, n = planes * d.head_dim * eb;
+  const void *held[3] = {qc->blocks, qc->tail_k, qc->tail_v};
+  const size_t sizes[3] = {planes * (qc->capacity / kBlock) * 34 * d.head_dim,
+                           n * qc->tail_capacity, n * qc->tail_capacity};
+  for (int i = 0; i < 3; ++i)
+    if (overlap(kv->k, n * kv->capacity, held[i], sizes[i]) ||
+        overlap(kv->v, n * kv->capacity, held[i], sizes[i]))
+      return fail(ACESPEC_EINVAL, "the cache and the quantized cache overlap");
+  return ACESPEC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
+                        const int32_t *first, int B, int32_t *status, hipStream_t stream) {
+  g_err.clear();
+  const int rc = check_convert(ctx, kv, qc, kv ? kv->prefix_len : nullptr, B);
+  if (rc) return rc;
+  const acespec_model_desc &d = ctx->d;
+  if (d.dtype == ACESPEC_BF16)
+    RUN(K_QUANTIZE, launch_quantize_kv<bf16>((const bf16 *)kv->k, (const bf16 *)kv->v, kv->prefix_len,
+                                             first, (uint8_t *)qc->blocks, (bf16 *)qc->tail_k,
+                                             (bf16 *)qc->tail_v, d.n_layers, B, d.n_kv_heads,
+                                             d.head_dim, kv->capacity, qc->capacity,
+                                             qc->tail_capacity, status, stream));
+  else
+    RUN(K_QUANTIZE, launch_quantize_kv<float>((const float *)kv->k, (const float *)kv->v,
+                                              kv->prefix_len, first, (uint8_t *)qc->blocks,
+                                              (float *)qc->tail_k, (float *)qc->tail_v, d.n_layers,
+                                              B, d.n_kv_heads, d.head_dim, kv->capacity,
+                                              qc->capacity, qc->tail_capacity, status, stream));
+  return ACESPEC_OK;
+}
+
+int acespec_dequantize_kv(acespec_ctx *ctx, const acespec_kv_quant *qc, const acespec_kv_cache *kv,
+                          const int32_t *first, int B, int32_t *status, hipStream_t stream) {
+  g_err.clear();
+  const int rc = check_convert(ctx, kv, qc, qc ? qc->prefix_len : nullptr, B);
+  if (rc) return rc;
+  const acespec_model_desc &d = ctx->d;
+  if (d.dtype == ACESPEC_BF16)
+    RUN(K_DEQUANTIZE, launch_dequantize_kv<bf16>((const uint8_t *)qc->blocks, (const bf16 *)qc->tail_k,
+                                                 (const bf16 *)qc->tail_v, qc->prefix_len, first,
+                                                 (bf16 *)kv->k, (bf16 *)kv->v, d.n_layers, B,
+                                                 d.n_kv_heads, d.head_dim, kv->capacity,
+                                                 qc->capacity, qc->tail_capacity, status, stream));
+  else
+    RUN(K_DEQUANTIZE, launch_dequantize_kv<float>((const uint8_t *)qc->blocks,
+                                                  (const float *)qc->tail_k, (const float *)qc->tail_v,
+                                                  qc->prefix_len, first, (float *)kv->k, (float *)kv->v,
+                                                  d.n_layers, B, d.n_kv_heads, d.head_dim,
+                                                  kv->capacity, qc->capacity, qc->tail_capacity,
+                                                  status, stream));
+  return ACESPEC_OK;
+}
+
+int acespec_commit_kv_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, const int32_t *path,
+                            const int32_t *path_len, const int32_t *status, int B, int N,
+                            int32_t *new_prefix_len, hipStream_t stream) {
+  g_err.clear();
+  if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
+  const acespec_model_desc &d = ctx->d;
+  if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
+  if (!path || !path_len || !new_prefix_len)
+    return fail(ACESPEC_EINVAL, "a required pointer is NULL (only status may be)");
+  int rc = check_batch(ctx, B, N);
+  if (!rc) rc = check_quant(d, qc, B, N + 1);
+  if (rc) return rc;
+  if (overlap(qc->prefix_len, (size_t)B * 4, new_prefix_len, (size_t)B * 4))
+    return fail(ACESPEC_EINVAL,
+                "new_prefix_len overlaps prefix_len: give it its own buffer and copy it over "
+                "after the call");
+  if (d.dtype == ACESPEC_BF16)
+    RUN(K_COMMIT, launch_commit_quant<bf16>((uint8_t *)qc->blocks, (bf16 *)qc->tail_k,
+                                            (bf16 *)qc->tail_v, qc->prefix_len, path, path_len, status,
+                                            d.n_layers, B, N + 1, d.n_kv_heads, d.head_dim,
+                                            qc->capacity, qc->tail_capacity, new_prefix_len, stream));
+  else
+    RUN(K_COMMIT, launch_commit_quant<float>((uint8_t *)qc->blocks, (float *)qc->tail_k,
+                                             (float *)qc->tail_v, qc->prefix_len, path, path_len, status,
+                                             d.n_layers, B, N + 1, d.n_kv_heads, d.head_dim,
+                                             qc->capacity, qc->tail_capacity, new_prefix_len, stream));
   return ACESPEC_OK;
 }
 

@@ -208,6 +208,13 @@ namespace acespec {
 hipError_t launch_tree_prep(const int32_t *tokens, const int32_t *parents,
                             const int32_t *prefix_len, int B, int n1, int V, int capacity,
                             TreeMeta meta, int32_t *status, hipStream_t s);
+// The same for a cache in 4 bits of `capacity` block slots: sess_S is the tail's length
+// (prefix_len % 32, where the tree's rows go), and anc holds only what the window shows.
+// tokens may be NULL (meta.tok is then not written).
+hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
+                                  const int32_t *prefix_len, int B, int n1, int V, int capacity,
+                                  int window, int sinks, TreeMeta meta, int32_t *status,
+                                  hipStream_t s);
 
 template <typename TW>
 hipError_t launch_embed(const TW *embed, const int32_t *tok, float *x, int rows, int d,
@@ -304,6 +311,35 @@ hipError_t launch_attention(const typename ActOf<TW>::type *q, const TW *cache_k
                             typename ActOf<TW>::type *out, float *part_o, float *part_ml,
                             long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                             int capacity, int cus, hipStream_t s, int *nsplit_used);
+
+// One layer's tree attention over the cache in 4 bits: blocks [B][Hkv][capacity / 32] records,
+// the tail tk [B][Hkv][tcap][hd] and tv [B][Hkv][hd][tcap].  window (0: none) and sinks as in
+// acespec_attn_span.  rows_io: q and out are row-major [rows][H hd] in TW; else as in
+// launch_attention.
+template <typename TW>
+hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const TW *tk,
+                                  const TW *tv, const TreeMeta &meta, void *out, float *part_o,
+                                  float *part_ml, long long part_capacity, int B, int n1, int H,
+                                  int Hkv, int hd, int capacity, int tcap, int window, int sinks,
+                                  int rows_io, int cus, hipStream_t s);
+
+// A cache (capacity cap) brought to 4 bits (block slots qcap, tail slots tcap), and back.
+// first[b] (or NULL: 0): slots below it are left as they are, but for those of its block.
+template <typename T>
+hipError_t launch_quantize_kv(const T *k, const T *v, const int32_t *prefix_len,
+                              const int32_t *first, uint8_t *blocks, T *tk, T *tv, int L, int B,
+                              int Hkv, int hd, int cap, int qcap, int tcap, int32_t *status,
+                              hipStream_t s);
+template <typename T>
+hipError_t launch_dequantize_kv(const uint8_t *blocks, const T *tk, const T *tv,
+                                const int32_t *prefix_len, const int32_t *first, T *k, T *v,
+                                int L, int B, int Hkv, int hd, int cap, int qcap, int tcap,
+                                int32_t *status, hipStream_t s);
+template <typename T>
+hipError_t launch_commit_quant(uint8_t *blocks, T *tk, T *tv, const int32_t *prefix_len,
+                               const int32_t *path, const int32_t *path_len,
+                               const int32_t *status, int L, int B, int n1, int Hkv, int hd,
+                               int qcap, int tcap, int32_t *new_len, hipStream_t s);
 
 struct VocabArgs {
   const float *logits;      // [rows, V]

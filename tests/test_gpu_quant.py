@@ -1,0 +1,587 @@
+"""The 4-bit KV cache and the attention over it, through the ABI, against plain forms in 64
+bits (quant_ref)."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import synth
+from oracle import model as om
+from tests import harness as hz
+from tests import quant_ref as qr
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def make(L, B, H, Hkv, hd, dtype, max_nodes, cap):
+    from paper_2609_02514_amd.acespec import QuantCache, Verifier
+    ver = Verifier(L, 64, H, Hkv, hd, 64, 64, dtype, B, max_nodes)
+    return ver, QuantCache.alloc(L, B, Hkv, hd, cap, max_nodes, dtype)
+
+
+def random_cache(L, B, Hkv, cap, hd, dtype, seed, spread=3.0):
+    """A cache whose groups' magnitudes differ by powers of two."""
+    g = torch.Generator().manual_seed(seed)
+    k = torch.randn(L, B, Hkv, cap, hd, generator=g)
+    v = torch.randn(L, B, Hkv, hd, cap, generator=g)
+    k *= torch.exp2(torch.randn(L, B, Hkv, cap, 1, generator=g) * spread)
+    v *= torch.exp2(torch.randn(L, B, Hkv, hd, 1, generator=g) * spread)
+    return k.to(DT[dtype]).cuda(), v.to(DT[dtype]).cuda()
+
+
+def want_cache(k, v, lens, first=None):
+    """The read-back of k, v (float64), NaN where nothing is read back."""
+    wk, wv = torch.full_like(k, 0, dtype=torch.float64), torch.full_like(v, 0, dtype=torch.float64)
+    there_k, there_v = torch.zeros_like(k, dtype=torch.bool), torch.zeros_like(v, dtype=torch.bool)
+    for b, P in enumerate(lens):
+        full, f = P // 32 * 32, (first[b] // 32 * 32 if first else 0)
+        wk[:, b, :, :P], wv[:, b, :, :, :P] = k[:, b, :, :P].double(), v[:, b, :, :, :P].double()
+        wk[:, b, :, :full] = qr.held_keys(k[:, b, :, :full])
+        wv[:, b, :, :, :full] = qr.held_values(v[:, b, :, :, :full])
+        there_k[:, b, :, f:P] = True
+        there_v[:, b, :, :, f:P] = True
+    return wk, wv, there_k, there_v
+
+
+def same(a, b):
+    """Bit for bit, any NaN like any other."""
+    a, b = a.double(), b.double()
+    return bool(((a == b) | (a.isnan() & b.isnan())).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("L, B, Hkv, lens", [
+    (1, 1, 1, [64]), (2, 7, 3, [0, 1, 31, 32, 33, 100, 192]), (1, 2, 1, [128, 5])])
+def test_read_back_is_the_definition(dtype, hd, L, B, Hkv, lens):
+    cap = 192
+    ver, cache = make(L, B, Hkv, Hkv, hd, dtype, 0, cap)
+    k, v = random_cache(L, B, Hkv, cap, hd, dtype, 7 * hd + B)
+    wk, wv, tk, tv = want_cache(k, v, lens)
+    bk, bv = torch.full_like(k, -77.0), torch.full_like(v, -77.0)
+    status = i32([9] * B)
+    hz.log(f"quantize_kv {dtype} hd={hd} lens={lens}")
+    ver.quantize_kv(k, v, cap, i32(lens), cache, status)
+    ver.dequantize_kv(cache.with_prefix(i32(lens)), bk, bv, cap, status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0] * B
+    assert same(torch.where(tk, bk.double(), 0), torch.where(tk, wk, 0))
+    assert same(torch.where(tv, bv.double(), 0), torch.where(tv, wv, 0))
+    assert bool((bk[~tk] == -77).all()) and bool((bv[~tv] == -77).all())   # left as they were
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_borders_of_the_grid_and_of_the_range(dtype, hd):
+    """Ties, the largest element's border, powers of two, zeros of both signs, values below the
+    smallest scale, and groups that hold NaN, inf or what fp16 could not hold."""
+    tops = [6.0, 6.99, 7.0, 7.01, 4.0, 1.0, 1.75, 1.749, 8.0]
+    ties = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -2.5, -5.0, 0.0, -0.0]
+    groups = []
+    for t in tops:
+        for s in (1.0, 2.0 ** -9, 2.0 ** 12 if t < 7 else 2.0 ** 5):
+            groups.append([x * s for x in [t] + ties] + [0.1 * s] * 19)
+    for t in (2.0 ** -13, 2.0 ** -14, 2.0 ** -15, 1.5 * 2.0 ** -14, 2.0 ** -40, 0.0, 49152.0, 57088.0):
+        groups.append([t, -t, t / 2, t / 4] * 8)
+    for bad in (math.nan, math.inf, -math.inf, 57344.0, 3e38, -65536.0):
+        groups.append([1.0] * 15 + [bad] + [0.5] * 16)
+    while len(groups) % (hd // 32) or len(groups) % 32:
+        groups.append([1.0] * 32)
+    x = torch.tensor(groups, dtype=torch.float64).to(DT[dtype])
+    n = len(groups)
+    cap = 64 * ((n * 32 // hd + 63) // 64)
+    k = torch.ones(1, 1, 1, cap, hd, dtype=DT[dtype])
+    k.view(-1, 32)[:n] = x
+    # value rows: group i is block i % (cap / 32) of head dim i / (cap / 32)
+    v = torch.ones(1, 1, 1, hd, cap, dtype=DT[dtype])
+    v.view(-1, 32)[:min(n, hd * cap // 32)] = x[:hd * cap // 32]
+    k, v = k.cuda(), v.cuda()
+    ver, cache = make(1, 1, 1, 1, hd, dtype, 0, cap)
+    bk, bv = torch.zeros_like(k), torch.zeros_like(v)
+    ver.quantize_kv(k, v, cap, i32([cap]), cache)
+    ver.dequantize_kv(cache.with_prefix(i32([cap])), bk, bv, cap)
+    torch.cuda.synchronize()
+    assert same(bk, qr.held_keys(k)) and same(bv, qr.held_values(v))
+
+
+@pytest.mark.parametrize("dtype, hd", [("bf16", 128), ("f32", 64)])
+def test_what_was_appended_and_sessions_that_do_not_fit(dtype, hd):
+    L, B, Hkv, cap = 2, 6, 2, 128
+    ver, cache = make(L, B, Hkv, Hkv, hd, dtype, 0, 64)
+    k, v = random_cache(L, B, Hkv, cap, hd, dtype, 3)
+    lens = [95, 96, 70, 40, 129, -1]      # 96 slots do not fit 64 in blocks and 31 behind them
+    first = [0, 0, 33, 41, 0, 0]          # session 2: from block 1 on; session 3: past its end
+    cache.blocks.fill_(0xEE)
+    before = cache.blocks.clone()
+    status = i32([9] * B)
+    ver.quantize_kv(k, v, cap, i32(lens), cache, status, first=i32(first))
+    torch.cuda.synchronize()
+    assert status.tolist() == [0, -5, 0, -5, -5, -5]
+    for b in (1, 3, 4, 5):
+        assert torch.equal(cache.blocks[:, b], before[:, b])
+        assert bool((cache.tail_k[:, b] == 0).all()) and bool((cache.tail_v[:, b] == 0).all())
+    assert torch.equal(cache.blocks[:, 2, :, 0], before[:, 2, :, 0])     # below first
+    bk, bv = torch.full_like(k, -77.0), torch.full_like(v, -77.0)
+    good = [95, 0, 70, 0, 0, 0]
+    ver.dequantize_kv(cache.with_prefix(i32(good)), bk, bv, cap, status, first=i32([64, 0, 32, 0, 0, 0]))
+    torch.cuda.synchronize()
+    assert status.tolist() == [0] * 6
+    wk, wv, tk, tv = want_cache(k, v, good, [64, 0, 32, 0, 0, 0])
+    assert same(torch.where(tk, bk.double(), 0), torch.where(tk, wk, 0))
+    assert same(torch.where(tv, bv.double(), 0), torch.where(tv, wv, 0))
+    assert bool((bk[~tk] == -77).all()) and bool((bv[~tv] == -77).all())
+
+
+# --------------------------------------------------------------------------------------
+# Attention
+# --------------------------------------------------------------------------------------
+
+
+def random_parents(r, n):
+    return [-1] + [r.randint(max(0, i - 7), i - 1) for i in range(1, n + 1)]
+
+
+def fill(ver, cache, k, v, lens, n1, seed):
+    """The prefix in 4 bits, random tree rows behind it; what each session then attends to
+    (keys, values [L, Hkv, P + n1, hd], float64)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    cache.tail_k.copy_(torch.randn(cache.tail_k.shape, generator=g, device="cuda"))
+    cache.tail_v.copy_(torch.randn(cache.tail_v.shape, generator=g, device="cuda"))
+    tk, tv = cache.tail_k.clone(), cache.tail_v.clone()
+    ver.quantize_kv(k, v, k.shape[3], i32(lens), cache)
+    out = []
+    for b, P in enumerate(lens):
+        t, full = P % 32, P // 32 * 32
+        kk = torch.cat([qr.held_keys(k[:, b, :, :full]), k[:, b, :, full:P].double(),
+                        tk[:, b, :, t:t + n1].double()], 2)
+        vv = torch.cat([qr.held_values(v[:, b, :, :, :full]), v[:, b, :, :, full:P].double(),
+                        tv[:, b, :, :, t:t + n1].double()], 3).transpose(2, 3)
+        out.append((kk, vv))
+    return out
+
+
+def bound(dtype, out, mag, big, hd):
+    """|error| of an attention output, element by element.  Scores are sums of hd products in
+    fp32: each is off by at most (hd + 4) 2^-24 of the sum of magnitudes `big`, as the exponent
+    is by 2^-22 of it (its scale and reference), and a weight relatively by as much (twice: its
+    own and the sum's).  exp2 and the sums of weights and products add 2^-20 of mag = sum p |v|.
+    bf16 model: weights rounded to fp16 (2^-11 of mag, and 2^-24 of an element where they are
+    subnormal, the most at 2^8 references apart), the output to bf16 (2^-8)."""
+    b = mag * (2 * big * ((hd + 4) * 2.0 ** -24 + 2.0 ** -22) + 2.0 ** -20)
+    if dtype == "bf16":
+        b = b + mag * 2.0 ** -11 + 2.0 ** -14
+        b = b + (out.abs() + b) * 2.0 ** -8
+    return b + 1e-30
+
+
+def check_attention(dtype, hd, H, Hkv, lens, N, window, sinks, seed, layer=0, L=1, poison=None):
+    r = random.Random(seed)
+    B, n1 = len(lens), N + 1
+    cap = max(64, (max(lens) + 63) // 64 * 64)
+    ver, cache = make(L, B, H, Hkv, hd, dtype, N, cap)
+    k, v = random_cache(L, B, Hkv, cap, hd, dtype, seed, spread=0.5)
+    kv = fill(ver, cache, k, v, lens, n1, seed + 1)
+    cache = cache.with_prefix(i32(lens))
+    parents = [random_parents(r, N) for _ in range(B)]
+    g = torch.Generator().manual_seed(seed + 2)
+    q = torch.randn(B, n1, H, hd, generator=g).to(DT[dtype]).cuda()
+    if poison:
+        poison(cache, kv, parents)
+    out, status = torch.full_like(q, -77.0), i32([9] * B)
+    hz.log(f"attention_quant {dtype} hd={hd} H={H}/{Hkv} lens={lens} N={N} window={window}/{sinks}")
+    ver.attention_quant(cache, layer, q, i32(parents), out, status, window, sinks)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0] * B
+    worst = 0.0
+    for b, P in enumerate(lens):
+        want, mag, big = qr.attend(q[b], kv[b][0][layer], kv[b][1][layer], P, parents[b], window, sinks)
+        got = out[b].double().cpu()
+        fine = want.isfinite()
+        assert torch.equal(fine, got.isfinite()), (b, fine.logical_xor(got.isfinite()).nonzero()[:5])
+        err = (got - want).abs()[fine] / bound(dtype, want, mag, big, hd)[fine]
+        if err.numel():
+            worst = max(worst, float(err.max()))
+    hz.log(f"  worst error: {worst:.3f} of its bound")
+    assert worst <= 1.0
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("H, Hkv, lens, N", [
+    (1, 1, [0], 0), (1, 1, [1], 0), (4, 1, [0, 31, 32, 33, 64, 95], 0), (8, 2, [5, 200, 97], 16),
+    (4, 4, [130, 63], 8), (14, 2, [257], 33), (16, 2, [64, 31], 64), (6, 2, [1000, 3], 5)])
+def test_attention_against_64_bits(dtype, hd, H, Hkv, lens, N):
+    check_attention(dtype, hd, H, Hkv, lens, N, 0, 0, seed=H * 100 + N + hd)
+
+
+@pytest.mark.parametrize("dtype, hd", [("bf16", 128), ("f32", 64), ("bf16", 64)])
+@pytest.mark.parametrize("window, sinks", [
+    (1, 0), (1, 1), (2, 4), (5, 33), (31, 0), (32, 4), (33, 64), (64, 1000), (100, 4), (5000, 4)])
+def test_windows_and_sinks(dtype, hd, window, sinks):
+    """Windows that end inside a block, inside the tail and inside the tree, sinks that reach
+    into the window and past the prefix."""
+    check_attention(dtype, hd, 4, 2, [0, 3, 40, 161, 256], 12, window, sinks, seed=window + sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_long_session_is_split(dtype):
+    """Few sessions over long caches: splits that are joined, the last ones past the end."""
+    check_attention(dtype, 128, 4, 1, [6000, 17], 3, 0, 0, seed=5)
+    check_attention(dtype, 64, 8, 1, [6001, 4500], 16, 900, 40, seed=6)
+
+
+def test_one_layer_of_several():
+    check_attention("bf16", 128, 4, 2, [70, 33], 4, 0, 0, seed=11, layer=2, L=3)
+
+
+@pytest.mark.parametrize("dtype, hd", [("bf16", 128), ("f32", 64), ("bf16", 64), ("f32", 128)])
+def test_what_a_row_does_not_see_does_not_reach_it(dtype, hd):
+    """NaN and inf in a sibling's key and value, in slots behind the last row, and in prefix
+    groups that a window has passed: rows that do not see them stay as they are."""
+    def poison(cache, kv, parents):
+        B = cache.tail_k.shape[1]
+        for b, P in enumerate([0, 70, 200, 96]):
+            t = P % 32
+            cache.tail_k[:, b, :, t + 9:] = math.nan          # N = 8: past the tree
+            cache.tail_v[:, b, :, :, t + 9:] = math.inf
+            parents[b][:] = [-1, 0, 0, 1, 1, 2, 2, 3, 5]
+            cache.tail_v[:, b, :, 3, t + 4] = math.nan        # a leaf's value, one head dim
+            kv[b][1][:, :, P + 4, 3] = math.nan
+            cache.tail_k[:, b, :, t + 6, 5] = math.inf        # another leaf's key
+            kv[b][0][:, :, P + 6, 5] = math.inf
+            if b == 2:
+                cache.tail_v[:, b, :, 7, t + 1] = math.inf    # an inner row: its subtree sees it
+                kv[b][1][:, :, P + 1, 7] = math.inf
+    check_attention(dtype, hd, 4, 2, [0, 70, 200, 96], 8, 0, 0, seed=21, poison=poison)
+    check_attention(dtype, hd, 4, 2, [0, 70, 200, 96], 8, 3, 1, seed=22, poison=poison)
+
+
+@pytest.mark.parametrize("dtype, hd", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("window", [0, 60, 100, 103])
+def test_marked_groups_reach_the_rows_that_see_them(dtype, hd, window):
+    """A prefix of three blocks and a tail; one key and one value group of a block marked."""
+    L, B, Hkv, H, N, P = 1, 2, 1, 4, 6, 140
+    ver, cache = make(L, B, H, Hkv, hd, dtype, N, 192)
+    k, v = random_cache(L, B, Hkv, 192, hd, dtype, 4, spread=0.5)
+    k[0, 0, 0, 35, 2] = math.nan        # session 0: a key of block 1
+    v[0, 1, 0, 9, 37] = math.inf        # session 1: a value group of block 1, head dim 9
+    kv = fill(ver, cache, k, v, [P, P], N + 1, 5)
+    parents = [-1, 0, 1, 2, 3, 4, 5]    # a chain: each row's window ends one slot further on
+    q = torch.randn(B, N + 1, H, hd, generator=torch.Generator().manual_seed(1)).to(DT[dtype]).cuda()
+    out, status = torch.zeros_like(q), i32([0, 0])
+    ver.attention_quant(cache.with_prefix(i32([P, P])), 0, q, i32([parents] * B), out, status, window, 2)
+    torch.cuda.synchronize()
+    for b in range(B):
+        want, mag, big = qr.attend(q[b], kv[b][0][0], kv[b][1][0], P, parents, window, 2)
+        got, fine = out[b].double().cpu(), want.isfinite()
+        assert torch.equal(fine, got.isfinite())
+        assert bool(((got - want).abs() <= bound(dtype, want, mag, big, hd))[fine].all())
+        assert bool(fine.all()) == (window == 60) or window in (100, 103)
+
+
+def test_equal_scores_far_apart_references_and_large_queries():
+    """Scores of thousands, whose running reference moves from block to block, and queries of
+    zero (all weights equal)."""
+    for scale in (0.0, 60.0):
+        L, B, Hkv, H, N, P, hd = 1, 1, 1, 2, 2, 300, 64
+        for dtype in ("bf16", "f32"):
+            ver, cache = make(L, B, H, Hkv, hd, dtype, N, 320)
+            k, v = random_cache(L, B, Hkv, 320, hd, dtype, 4, spread=1.0)
+            kv = fill(ver, cache, k, v, [P], N + 1, 5)
+            q = (torch.randn(B, N + 1, H, hd, generator=torch.Generator().manual_seed(1)) * scale
+                 ).to(DT[dtype]).cuda()
+            out, status = torch.zeros_like(q), i32([0])
+            ver.attention_quant(cache.with_prefix(i32([P])), 0, q, i32([[-1, 0, 0]]), out, status)
+            torch.cuda.synchronize()
+            want, mag, big = qr.attend(q[0], kv[0][0][0], kv[0][1][0], P, [-1, 0, 0])
+            err = (out[0].double().cpu() - want).abs() / bound(dtype, want, mag, big, hd)
+            assert float(err.max()) <= 1.0
+
+
+def test_malformed_sessions_are_flagged_and_the_others_unharmed():
+    from paper_2609_02514_amd import acespec as A
+    L, H, Hkv, hd, N = 1, 4, 2, 128, 3
+    lens = [50, 64 + 32, -1, 70, 50]       # capacity 64: 95 slots at most
+    good = [-1, 0, 0, 1]
+    parents = [good, good, good, [-1, 0, 2, 1], [0, 0, 0, 0]]
+    ver, cache = make(L, 5, H, Hkv, hd, "bf16", N, 64)
+    k, v = random_cache(L, 5, Hkv, 64, hd, "bf16", 4)
+    q = torch.randn(5, N + 1, H, hd, device="cuda").bfloat16()
+    ver.quantize_kv(k, v, 64, i32([50] * 5), cache)
+    out, status = torch.zeros_like(q), i32([9] * 5)
+    ver.attention_quant(cache.with_prefix(i32(lens)), 0, q, i32(parents), out, status)
+    alone, one = torch.zeros_like(q), i32([9] * 5)
+    ver.attention_quant(cache.with_prefix(i32([50] * 5)), 0, q, i32([good] * 5), alone, one)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0, A.ACESPEC_EBADTREE, A.ACESPEC_EBADTREE, A.ACESPEC_EBADTREE,
+                               A.ACESPEC_EBADTREE]
+    assert torch.equal(out[0], alone[0])
+
+
+# --------------------------------------------------------------------------------------
+# Commit
+# --------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype, hd, N", [("bf16", 64, 1), ("bf16", 128, 16), ("bf16", 128, 64),
+                                          ("f32", 128, 64), ("f32", 64, 7), ("bf16", 64, 33)])
+def test_commit_moves_the_path_and_quantizes_complete_blocks(dtype, hd, N):
+    L, B, Hkv, cap = 2, 9, 3, 160
+    ver, cache = make(L, B, Hkv, Hkv, hd, dtype, N, cap)
+    g = torch.Generator().manual_seed(N * 7 + hd)
+    for t in (cache.tail_k, cache.tail_v):
+        t.copy_(torch.randn(t.shape, generator=g))
+    if N > 16:
+        cache.tail_k[0, 8, 0, 40, 3] = math.nan
+    cache.blocks.fill_(0xEE)
+    lens = [0, 31, 32, 63, 40, 95, 64, 159, 30]
+    plen = [min(N, n) for n in (0, 1, 31, 32, 5, 64, 64, 0, N)]
+    path = torch.full((B, N + 1), -1, dtype=torch.int32)
+    for b, n in enumerate(plen):
+        path[b, :n] = torch.randperm(N, generator=g)[:n].int() + 1
+    status = [0] * B
+    status[4] = -5                          # not committed
+    tk, tv, blocks = cache.tail_k.clone(), cache.tail_v.clone(), cache.blocks.clone()
+    new = i32([-7] * B)
+    hz.log(f"commit_kv_quant {dtype} hd={hd} N={N}")
+    ver.commit_kv_quant(cache.with_prefix(i32(lens)), path.cuda(), i32(plen), i32(status), new)
+    torch.cuda.synchronize()
+    back_k = torch.zeros((L, B, Hkv, 192, hd), dtype=DT[dtype], device="cuda")
+    back_v = torch.zeros((L, B, Hkv, hd, 192), dtype=DT[dtype], device="cuda")
+    want_len = [-1 if s else P + 1 + n for P, n, s in zip(lens, plen, status)]
+    assert new.tolist() == want_len
+    ok = [max(x, 0) for x in want_len]
+    ver.dequantize_kv(cache.with_prefix(i32(ok)), back_k, back_v, 192,
+                      first=i32([min(P, o) for P, o in zip(lens, ok)]))
+    torch.cuda.synchronize()
+    for b, (P, n) in enumerate(zip(lens, plen)):
+        t, base = P % 32, P // 32
+        if status[b]:
+            assert torch.equal(cache.tail_k[:, b], tk[:, b]) and torch.equal(cache.blocks[:, b], blocks[:, b])
+            continue
+        src = list(range(t + 1)) + [t + int(x) for x in path[b, :n]]
+        xk, xv = tk[:, b][:, :, src], tv[:, b][:, :, :, src]
+        full = len(src) // 32 * 32
+        wk = torch.cat([qr.held_keys(xk[:, :, :full]), xk[:, :, full:].double()], 2)
+        wv = torch.cat([qr.held_values(xv[..., :full]), xv[..., full:].double()], 3)
+        lo, hi = base * 32, P + 1 + n
+        assert same(back_k[:, b, :, lo:hi], wk) and same(back_v[:, b, :, :, lo:hi], wv), b
+        left = len(src) - full
+        sk, sv = tk[:, b].clone(), tv[:, b].clone()
+        sk[:, :, :left], sv[:, :, :, :left] = xk[:, :, full:], xv[..., full:]
+        assert same(cache.tail_k[:, b], sk) and same(cache.tail_v[:, b], sv), b
+        rest = blocks[:, b].clone()
+        rest[:, :, base:base + full // 32] = cache.blocks[:, b, :, base:base + full // 32]
+        assert torch.equal(rest, cache.blocks[:, b])     # no other block was written
+
+
+def test_commits_that_are_refused_on_the_device_move_nothing():
+    L, B, Hkv, hd, N = 1, 7, 1, 64, 8
+    ver, cache = make(L, B, Hkv, Hkv, hd, "bf16", N, 64)
+    g = torch.Generator().manual_seed(3)
+    for t in (cache.tail_k, cache.tail_v):
+        t.copy_(torch.randn(t.shape, generator=g))
+    cache.blocks.fill_(0xEE)
+    k0, v0, b0 = cache.tail_k.clone(), cache.tail_v.clone(), cache.blocks.clone()
+    lens = [95, -3, 20, 20, 20, 2 ** 31 - 1, 94]       # 95 + 1 slots complete a block: no room
+    plen = [0, 1, 9, 2, 2, 1, 0]
+    path = torch.full((B, N + 1), 1, dtype=torch.int32)
+    path[3, 1], path[4, 0] = 9, 0                      # rows outside [1, N]
+    new = i32([-7] * B)
+    ver.commit_kv_quant(cache.with_prefix(i32(lens)), path.cuda(), i32(plen), None, new)
+    torch.cuda.synchronize()
+    assert new.tolist() == [-1] * 6 + [95]
+    assert torch.equal(cache.tail_k, k0) and torch.equal(cache.tail_v, v0)
+    assert torch.equal(cache.blocks, b0)
+
+
+# --------------------------------------------------------------------------------------
+# The verify step
+# --------------------------------------------------------------------------------------
+
+
+def workload(dtype, **kw):
+    base = dict(name="quant", dtype=dtype, L=2, d=256, H=4, Hkv=2, hd=64, F=512, V=2048, B=3,
+                S=150, tree="widths_2455", depth=4, q_std=2.5, q_T=0.8, T=0.8, top_p=0.9,
+                top_k=16, ragged=True, seed_base=91)
+    return synth.Workload(**dict(base, **kw))
+
+
+def quantized(ver, w, batch, n):
+    from paper_2609_02514_amd.acespec import QuantCache
+    cache = QuantCache.alloc(w.L, w.B, w.Hkv, w.hd, batch.cap, n, w.dtype)
+    ver.quantize_kv(batch.kv_k, batch.kv_v, batch.cap, batch.prefix_len, cache)
+    return cache.with_prefix(batch.prefix_len)
+
+
+def reference_logits(w, W, k, v, tokens, parents, lens, window, sinks):
+    """k, v: the cache's read-back [L, B, Hkv, cap, hd] / [.., hd, cap]."""
+    F64, dims, z = om.F64Weights(W), om.dims_of(w), []
+    for b, P in enumerate(lens):
+        kp = [om.to_f64(k[l, b, :, :P]) for l in range(w.L)]
+        vp = [om.to_f64(v[l, b, :, :, :P]).transpose(0, 2, 1) for l in range(w.L)]
+        z.append(qr.forward_windowed(F64, dims, kp, vp, tokens[b], parents[b], P, window, sinks))
+    return np.stack(z)
+
+
+@pytest.mark.parametrize("dtype, kw, window, sinks", [
+    ("f32", {}, 0, 0), ("f32", dict(hd=128, d=512), 40, 4), ("bf16", {}, 0, 0),
+    ("bf16", dict(hd=128, d=512, H=8, Hkv=2), 70, 3), ("bf16", dict(S=40), 3, 0),
+    ("bf16", dict(tree="chain_sib", depth=8, sib=7, H=8, Hkv=1), 0, 0)])
+def test_verify_then_commit_then_verify(dtype, kw, window, sinks):
+    """The operators as they are used: a prefix taken over in 4 bits, a verify step, the commit
+    of its path, and the next verify step over the committed cache.  Logits against the 64-bit
+    decoder on the cache's read-back: within 1e-4 (fp32 model) and 2e-2 (bf16) of their largest,
+    the bounds the verify step's own tests use."""
+    from paper_2609_02514_amd.acespec import Verifier
+    w = workload(dtype, **kw)
+    W, batch = synth.make_weights(w, "cuda"), synth.make_batch(w, "cuda")
+    ver = Verifier.for_workload(w)
+    n1 = batch.tokens.shape[1]
+    cache = quantized(ver, w, batch, n1 - 1)
+    outs = ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True)
+    ws, parents = ver.weights_struct(W), batch.parents.tolist()
+    tokens, lens = batch.tokens, batch.prefix_len.tolist()
+    for step in range(3):
+        cap = (max(lens) + 63) // 64 * 64
+        bk = torch.zeros((w.L, w.B, w.Hkv, cap, w.hd), dtype=DT[dtype], device="cuda")
+        bv = torch.zeros((w.L, w.B, w.Hkv, w.hd, cap), dtype=DT[dtype], device="cuda")
+        ver.dequantize_kv(cache, bk, bv, cap)
+        hz.log(f"verify_tree_quant {dtype} step {step} lens={lens}")
+        ver.verify_tree_quant(ws, cache, tokens, batch.parents, batch.q, batch.u, w.T, w.top_p,
+                              w.top_k, outs, window, sinks)
+        torch.cuda.synchronize()
+        assert outs["status"].tolist() == [0] * w.B
+        z = reference_logits(w, W, bk, bv, tokens.tolist(), parents, lens, window, sinks)
+        got = outs["logits_out"].view(w.B, n1, w.V).double().cpu().numpy()
+        err = np.abs(got - z).max() / np.abs(z).max()
+        hz.log(f"  logits off by {err:.2e} of the largest")
+        assert err < (1e-4 if dtype == "f32" else 2e-2)
+        # commit a path of our own (the drafts are seldom accepted), the deepest chain
+        path, chain = torch.full((w.B, n1), -1, dtype=torch.int32), []
+        r = 0
+        while True:
+            kids = [j for j in range(1, n1) if parents[0][j] == r]
+            if not kids:
+                break
+            r = kids[-1]
+            chain.append(r)
+        path[:, :len(chain)] = torch.tensor(chain, dtype=torch.int32)
+        new = i32([0] * w.B)
+        ver.commit_kv_quant(cache, path.cuda(), i32([len(chain)] * w.B), outs["status"], new)
+        torch.cuda.synchronize()
+        lens = [P + 1 + len(chain) for P in lens]
+        assert new.tolist() == lens
+        if max(lens) // 32 * 32 > cache.capacity - 32:
+            break
+        cache = cache.with_prefix(new)
+        tokens = torch.roll(tokens, 1, 1)
+    ver.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scalar_q_and_decisions_over_the_read_back_cache(dtype):
+    """The scalar-q step, and a dense one whose decisions are those of acespec_verify_tree over
+    the read-back cache where the logits agree to the last bits (fp32: few decisions hang on
+    them, none at these seeds)."""
+    from paper_2609_02514_amd.acespec import Verifier
+    w = workload(dtype)
+    W, batch = synth.make_weights(w, "cuda"), synth.make_batch(w, "cuda")
+    ver = Verifier.for_workload(w)
+    n1 = batch.tokens.shape[1]
+    cache = quantized(ver, w, batch, n1 - 1)
+    bk, bv = batch.kv_k.clone(), batch.kv_v.clone()
+    ver.dequantize_kv(cache, bk, bv, batch.cap)
+    a, b = (ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True) for _ in range(2))
+    ws, args = ver.weights_struct(W), (w.T, w.top_p, w.top_k)
+    q_hat = torch.rand(w.B, n1, generator=torch.Generator().manual_seed(2)).cuda()
+    for scalar in (False, True):
+        ver.verify_tree_quant(ws, cache, batch.tokens, batch.parents, q_hat if scalar else batch.q,
+                              batch.u, *args, a, scalar=scalar)
+        call = ver.verify_tree_scalar_q if scalar else ver.verify_tree
+        call(ws, bk, bv, batch.cap, batch.prefix_len, batch.tokens, batch.parents,
+             q_hat if scalar else batch.q, batch.u, *args, b)
+        torch.cuda.synchronize()
+        za, zb = a["logits_out"].double(), b["logits_out"].double()
+        assert float((za - zb).abs().max() / zb.abs().max()) < (1e-4 if dtype == "f32" else 2e-2)
+        assert torch.equal(a["status"], b["status"])
+        if dtype == "f32":
+            for name in ("accept", "acc_prefix_len", "resample_token", "path", "path_len", "next_token"):
+                assert torch.equal(a[name], b[name]), name
+    ver.close()
+
+
+def test_a_marked_group_flags_its_session():
+    from paper_2609_02514_amd import acespec as A
+    w = workload("bf16", ragged=False)
+    W, batch = synth.make_weights(w, "cuda"), synth.make_batch(w, "cuda")
+    batch.kv_v[1, 1, 0, 5, 40] = math.inf
+    ver = A.Verifier.for_workload(w)
+    n1 = batch.tokens.shape[1]
+    cache = quantized(ver, w, batch, n1 - 1)
+    outs = ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True)
+    args = (ver.weights_struct(W), cache, batch.tokens, batch.parents, batch.q, batch.u, w.T,
+            w.top_p, w.top_k, outs)
+    ver.verify_tree_quant(*args)
+    torch.cuda.synchronize()
+    assert outs["status"].tolist() == [0, A.ACESPEC_ENONFINITE, 0]
+    ver.verify_tree_quant(*args, window=60, sinks=32)     # slots 32 .. 63 are out of sight
+    torch.cuda.synchronize()
+    assert outs["status"].tolist() == [0, 0, 0]
+    ver.close()
+
+
+def test_a_captured_step_replays_as_it_ran():
+    """Quantise, verify and commit in one graph, replayed between eager calls of another cache
+    on the same context."""
+    from paper_2609_02514_amd.acespec import Verifier
+    w = workload("bf16", ragged=True)
+    W, batch = synth.make_weights(w, "cuda"), synth.make_batch(w, "cuda")
+    ver = Verifier.for_workload(w)
+    n1 = batch.tokens.shape[1]
+    ws = ver.weights_struct(W)
+    cache, other = quantized(ver, w, batch, n1 - 1), quantized(ver, w, batch, n1 - 1)
+    outs = ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True)
+    outs2 = ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True)
+    new = i32([0] * w.B)
+    path, plen = i32([[1, 3] + [-1] * (n1 - 2)] * w.B), i32([2] * w.B)
+
+    def step(c, o, toks):
+        ver.quantize_kv(batch.kv_k, batch.kv_v, batch.cap, batch.prefix_len, c)
+        ver.verify_tree_quant(ws, c, toks, batch.parents, batch.q, batch.u, w.T, w.top_p, w.top_k,
+                              o, 64, 4)
+        ver.commit_kv_quant(c, path, plen, o["status"], new)
+
+    step(cache, outs, batch.tokens)
+    torch.cuda.synchronize()
+    want = {k: t.clone() for k, t in outs.items()}
+    held = [t.clone() for t in (cache.blocks, cache.tail_k, cache.tail_v, new)]
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step(cache, outs, batch.tokens)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cache, outs, batch.tokens)
+    for i in range(4):
+        for t in outs.values():
+            t.zero_()
+        cache.blocks.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in want:
+            assert torch.equal(outs[k], want[k]), (i, k)
+        for a, b in zip((cache.blocks, cache.tail_k, cache.tail_v, new), held):
+            assert torch.equal(a, b), i
+        step(other, outs2, torch.roll(batch.tokens, 1 + i, 1))
+        torch.cuda.synchronize()
+    ver.close()

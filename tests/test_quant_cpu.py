@@ -1,0 +1,164 @@
+"""What the entry points of the 4-bit KV cache refuse, without a GPU: every check runs before
+anything is enqueued (the pointers below are never dereferenced)."""
+import ctypes as C
+import struct
+
+import pytest
+
+import paper_2609_02514_amd.acespec as A
+
+P = 0x7F0000000000
+
+
+class Ctx:
+    """The head of a context (model, max_batch, max_nodes), all that the checks read."""
+
+    def __init__(self, L=2, H=4, Hkv=2, hd=128, dtype=A.ACESPEC_BF16, max_batch=4, max_nodes=16):
+        self.buf = C.create_string_buffer(8192)
+        desc = A.ModelDesc(L, 64, H, Hkv, hd, 64, 64, 10000.0, 1e-5, dtype)
+        C.memmove(self.buf, C.byref(desc), C.sizeof(desc))
+        struct.pack_into("iii", self.buf, C.sizeof(desc), max_batch, max_nodes,
+                         max_batch * (max_nodes + 1))
+        struct.pack_into("N", self.buf, C.sizeof(desc) + 16, 2)   # bytes per activation
+        self.ptr = C.cast(self.buf, C.c_void_p)
+
+
+def quant(blocks=P, tail_k=P + (1 << 32), tail_v=P + (2 << 32), capacity=128, tail=64,
+          prefix=P + (3 << 32)):
+    return A.KVQuant(blocks, tail_k, tail_v, capacity, tail, prefix)
+
+
+def cache(k=P + (4 << 32), v=P + (5 << 32), capacity=128, prefix=P + (6 << 32)):
+    return A.KVCache(k, v, capacity, prefix)
+
+
+def refused(rc, text, code=A.ACESPEC_EINVAL):
+    assert rc == code and text in A.acespec_last_error(), (rc, A.acespec_last_error())
+
+
+def test_struct_layouts_match_the_header():
+    assert C.sizeof(A.KVQuant) == 40 and A.KVQuant.prefix_len.offset == 32
+    assert C.sizeof(A.AttnSpan) == 8
+
+
+BAD_QUANT = [(dict(blocks=None), "NULL"), (dict(tail_k=None), "NULL"), (dict(tail_v=None), "NULL"),
+             (dict(blocks=P + 8), "aligned"), (dict(tail_v=P + (2 << 32) + 2), "aligned"),
+             (dict(capacity=0), "multiple of 32"), (dict(capacity=48), "multiple of 32"),
+             (dict(capacity=-32), "multiple of 32"), (dict(tail=0), "tail_capacity"),
+             (dict(tail=96), "tail_capacity")]
+
+
+def calls(lib, ctx, qc, kv, N=16, B=4, span=None):
+    """Every entry point on these structures."""
+    ref = lambda s: None if s is None else C.byref(s)
+    outs, params = A.Outputs(*([P] * 12)), A.Params(0.8, 0.9, 8)
+    layers = (A.LayerWeights * 2)(*[A.LayerWeights(P, P, P, P, P, P)] * 2)
+    w = A.Weights(P, layers, P, P, 0)
+    far = P + (7 << 32)
+    yield "quantize", lib.acespec_quantize_kv(ctx, ref(kv), ref(qc), None, B, None, None)
+    yield "dequantize", lib.acespec_dequantize_kv(ctx, ref(qc), ref(kv), None, B, None, None)
+    yield "attention", lib.acespec_attention_quant(ctx, ref(qc), 0, ref(span), far, far, B, N,
+                                                   far + (1 << 30), far, None)
+    yield "verify", lib.acespec_verify_tree_quant(ctx, C.byref(w), ref(qc), ref(span), P, P, P, None,
+                                                  P, B, N, C.byref(params), C.byref(outs), None)
+    yield "commit", lib.acespec_commit_kv_quant(ctx, ref(qc), P, P, None, B, N, far, None)
+
+
+@pytest.mark.parametrize("kw, text", BAD_QUANT)
+def test_a_bad_quantized_cache_is_refused_everywhere(kw, text):
+    ctx = Ctx()
+    for name, rc in calls(A.load(), ctx.ptr, quant(**kw), cache()):
+        refused(rc, text)
+
+
+def test_missing_contexts_caches_and_lengths():
+    lib, ctx = A.load(), Ctx()
+    for name, rc in calls(lib, None, quant(), cache()):
+        refused(rc, "ctx is NULL")
+    for name, rc in calls(lib, ctx.ptr, None, cache()):
+        refused(rc, "NULL")
+    for name, rc in calls(lib, ctx.ptr, quant(prefix=None), cache(prefix=None)):
+        refused(rc, "NULL")
+    for name, rc in calls(lib, Ctx(L=0).ptr, quant(), cache()):
+        refused(rc, "no layers")
+
+
+@pytest.mark.parametrize("B", [0, -1, 5])
+def test_batches_outside_the_context(B):
+    for name, rc in calls(A.load(), Ctx().ptr, quant(), cache(), B=B):
+        refused(rc, "B must be")
+
+
+def test_trees_outside_the_context_and_the_tail():
+    lib = A.load()
+    for N, code in ((-1, A.ACESPEC_EINVAL), (17, A.ACESPEC_EINVAL), (65, A.ACESPEC_EUNSUPPORTED)):
+        for name, rc in calls(lib, Ctx().ptr, quant(), cache(), N=N):
+            if name in ("attention", "verify", "commit"):
+                refused(rc, "N must be", code)
+    for name, rc in calls(lib, Ctx(max_nodes=64).ptr, quant(tail=64), cache(), N=33):
+        if name in ("attention", "verify", "commit"):
+            refused(rc, "34 tree rows")
+
+
+@pytest.mark.parametrize("window, sinks", [(-1, 0), (4, -1), (0, -5)])
+def test_negative_spans(window, sinks):
+    for name, rc in calls(A.load(), Ctx().ptr, quant(), cache(), span=A.AttnSpan(window, sinks)):
+        if name in ("attention", "verify"):
+            refused(rc, "window and sinks")
+
+
+@pytest.mark.parametrize("kw, text", [
+    (dict(k=None), "NULL"), (dict(v=None), "NULL"), (dict(k=P + (4 << 32) + 4), "aligned"),
+    (dict(capacity=96), "multiple of 64"), (dict(capacity=0), "multiple of 64"),
+    (dict(k=P + 64), "overlap"), (dict(v=P + (1 << 32)), "overlap")])
+def test_caches_that_cannot_be_converted(kw, text):
+    for name, rc in calls(A.load(), Ctx().ptr, quant(), cache(**kw)):
+        if name in ("quantize", "dequantize"):
+            refused(rc, text)
+
+
+def test_the_attention_refuses_layers_aliases_and_missing_tensors():
+    lib, ctx, qc = A.load(), Ctx(), quant()
+    q, out = P + (8 << 32), P + (9 << 32)
+
+    def call(layer=0, q=q, parents=P, out=out, status=P):
+        return lib.acespec_attention_quant(ctx.ptr, C.byref(qc), layer, None, q, parents, 4, 16, out,
+                                           status, None)
+
+    refused(call(layer=2), "layer")
+    refused(call(layer=-1), "layer")
+    refused(call(out=q), "overlap")
+    refused(call(out=q + 1024), "overlap")
+    refused(call(q=q + 2), "aligned")
+    for kw in (dict(q=None), dict(parents=None), dict(out=None), dict(status=None)):
+        refused(call(**kw), "NULL")
+
+
+def test_the_verify_step_takes_one_kind_of_draft():
+    lib, ctx, qc = A.load(), Ctx(), quant()
+    outs, params, w = A.Outputs(*([P] * 12)), A.Params(0.8, 0.9, 8), A.Weights()
+    for dense, scalar in ((None, None), (P, P)):
+        rc = lib.acespec_verify_tree_quant(ctx.ptr, C.byref(w), C.byref(qc), None, P, P, dense, scalar,
+                                           P, 4, 16, C.byref(params), C.byref(outs), None)
+        refused(rc, "exactly one")
+
+
+def test_the_commit_needs_its_own_lengths():
+    lib, ctx = A.load(), Ctx()
+    base = P + (3 << 32)
+    for new in (base, base + 8, base - 12):
+        rc = lib.acespec_commit_kv_quant(ctx.ptr, C.byref(quant()), P, P, None, 4, 16, new, None)
+        refused(rc, "overlaps")
+
+
+def test_tensors_of_another_shape_or_type_are_refused_by_the_binding():
+    import torch
+    blocks = torch.zeros(2, 1, 1, 2, 34 * 64, dtype=torch.uint8)
+    k, v = torch.zeros(2, 1, 1, 64, 64), torch.zeros(2, 1, 1, 64, 64)
+    ver = A.Verifier.__new__(A.Verifier)
+    ver.desc, ver.ctx = A.ModelDesc(2, 64, 2, 1, 64, 64, 64, 1e4, 1e-5, A.ACESPEC_F32), None
+    c = A.QuantCache(blocks, k, v, 64, 64, torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(ValueError, match="blocks"):        # right shapes, but not on the GPU
+        ver._check_quant(c, 1)
+    with pytest.raises(ValueError, match="blocks"):
+        ver._check_quant(A.QuantCache(blocks[:1], k, v, 64, 64, c.prefix_len), 1)
