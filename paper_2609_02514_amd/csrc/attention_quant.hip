@@ -4,43 +4,56 @@
 // Row r of a session of P slots sits at position P + depth(r).  It sees the P slots and, of the
 // tree, its ancestors and itself; with a window w > 0 only what is at a position less than w
 // behind its own, or below `sinks`.  Of the P slots the complete blocks of 32 are records, the
-// rest and the tree's rows the tail in the model's type; both go through the same code as blocks
-// of 32 slots.
+// rest and the tree's rows the tail in the model's type, taken as blocks of 32 slots too.
 //
 // Query rows are the G query heads of the kv head times the tree rows (row = tree_row * G +
 // head) in tiles of 16.  The work is divided by slots, not by queries: a wave holds all TPW
 // tiles of its workgroup (as accumulators) and takes blocks of its own, so a block's codes are
-// read once, by one wave, straight into the registers that the matrix instructions read, and
-// are decoded once for all the tiles.  No barrier and no LDS traffic but the queries' fragments.
+// read by one wave, straight into the registers that the matrix instructions read, and serve
+// all the tiles.  No barrier and no LDS traffic but the queries' fragments.
 //  * S^T = K Q^T by 16x16 products: a lane holds 8 scores of ONE query, for 8 consecutive
 //    slots.  Its running reference, exp2 and the probabilities stay in the lane, and these are
-//    its B operand of O^T = V^T P^T.  Head dims are dealt to the products so that a lane's codes
-//    of a key are consecutive (head dims lg * hd/4 ..), the queries' fragments alike.
-//  * A decoded element is e2m1 times a power of two: exact in fp16.  The bf16 model multiplies
-//    in fp16 (v_mfma_f32_16x16x32_f16), the fp32 model in fp32 (v_mfma_f32_16x16x4_f32).
-//  * The reference of a query's exponents moves only when a score exceeds it by more than
-//    2^8 (LAZY_LOG2): a lane compares its own scores, and only then are the four lanes of a query
-//    reduced and the accumulators rescaled.
+//    its B operand of O^T = V^T P^T.
+//  * bf16 model: the keys' codes and scale bytes ARE the operand of the scaled product
+//    (v_mfma_scale_f32_16x16x128_f8f6f4, a scale per 32 elements), so keys are never decoded.
+//    The queries are its e4m3 operand in two pieces, q = hi + lo: hi the nearest e4m3, lo the
+//    nearest to the rest, each with its own scale per 32 head dims.  A bf16 query (8
+//    significant bits) is held exactly, but for what lies 2^22 below its group's largest;
+//    an fp16 one (the verify step's) to 2^-8 of each element.  Values are decoded to fp16
+//    (exactly) and multiplied by fp16 weights (v_mfma_f32_16x16x32_f16), the tail's keys and
+//    values widened to fp16.
+//  * fp32 model: keys and values decoded to fp32 (exactly), v_mfma_f32_16x16x4_f32.
+//  * The reference of a query's exponents moves only when a score exceeds it by about 2^8
+//    (LAZY_LOG2), and only then are the four lanes of a query reduced and the accumulators
+//    rescaled: one rare branch for all tiles, so that one tile's exponents fill the matrix
+//    pipe's time on the others.
 // At the end the waves of a workgroup, and then the splits of a session, are joined by their
 // (maximum, sum) pairs.
 //
 // Not finite: a group of 32 marked so reads as NaN.  NaN and inf reach the rows that see them
-// and no others: where a mask applies, slots with such values are taken one at a time.
+// and no others: where a mask applies, values that are not finite count as 0 in the products and
+// are added at the end, to the rows that see their slots.
 #include "quant.h"
 
 namespace {
 
 constexpr float LAZY_LOG2 = 8.f;
+constexpr float LAZY_SUM = 8 * 256.f;   // of 8 weights none of which exceeds 2^LAZY_LOG2
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int NW = 4;   // waves of a workgroup
+constexpr int NW = 4;     // waves of a workgroup
+constexpr int JOIN = 2;   // tiles joined at a time
+constexpr int SLOW = 3;   // what a masked block costs a wave, in blocks that every row sees whole
 
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 // The operand arithmetic of a model's type: eight elements of a lane.
 template <typename T> struct Ops;
 template <> struct Ops<bf16> {
   typedef f16x8 F8;
   typedef f16 E;
   static AS_DEVICE F8 decode(uint32_t c, float s) { return q4_decode_f16(c, s); }
-  static AS_DEVICE F8 load(const bf16 *p) { return bf16x8_to_f16x8(*(const bf16x8 *)p); }
+  typedef bf16x8 Raw;
+  static AS_DEVICE Raw raw(const bf16 *p) { return *(const bf16x8 *)p; }
+  static AS_DEVICE F8 wide(bf16x8 v) { return bf16x8_to_f16x8(v); }
   static AS_DEVICE f32x4 mma(F8 a, F8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
@@ -49,10 +62,12 @@ template <> struct Ops<float> {
   typedef f32x8 F8;
   typedef float E;
   static AS_DEVICE F8 decode(uint32_t c, float s) { return q4_decode_f32(c, s); }
-  static AS_DEVICE F8 load(const float *p) {
+  typedef F8 Raw;
+  static AS_DEVICE F8 raw(const float *p) {
     const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
     return F8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   }
+  static AS_DEVICE F8 wide(F8 v) { return v; }
   static AS_DEVICE f32x4 mma(F8 a, F8 b, f32x4 c) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
@@ -79,6 +94,16 @@ struct RowView {
   int root;       // whether it sees the root
   uint64_t anc;   // drafted rows
 };
+// Bit j: whether it sees tree row tr0 + j or, where that is negative, position pos0 + j of the
+// prefix (j < 8).
+AS_DEVICE uint32_t visible(const RowView &w, int sinks, int tr0, int pos0) {
+  auto ones = [](int n) { return (1u << min(max(n, 0), 8)) - 1u; };   // the first n of 8
+  const uint32_t prefix = ones(-tr0) & (~ones(w.lo - pos0) | ones(sinks - pos0));
+  uint32_t tree;
+  if (tr0 >= 1) tree = tr0 <= 64 ? (uint32_t)(w.anc >> (tr0 - 1)) : 0u;
+  else tree = tr0 > -8 ? (((uint32_t)w.anc << 1) | (uint32_t)w.root) << -tr0 : 0u;
+  return (prefix | tree) & 255u;
+}
 
 // Eight consecutive elements of a query row, and four of an output row.
 AS_DEVICE f16x8 load_q(const QuantAttnArgs &a, bf16, size_t off) {
@@ -86,7 +111,7 @@ AS_DEVICE f16x8 load_q(const QuantAttnArgs &a, bf16, size_t off) {
   return *(const f16x8 *)((const f16 *)a.q + off);
 }
 AS_DEVICE f32x8 load_q(const QuantAttnArgs &a, float, size_t off) {
-  return Ops<float>::load((const float *)a.q + off);
+  return Ops<float>::raw((const float *)a.q + off);
 }
 AS_DEVICE void store_out(const QuantAttnArgs &a, bf16, int row, int col, int width, f32x4 v) {
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -98,6 +123,18 @@ AS_DEVICE void store_out(const QuantAttnArgs &a, bf16, int row, int col, int wid
     *(f16x4 *)((f16 *)a.out + act_off(row, col, a.B * a.n1, width)) =
         f16x4{(f16)v[0], (f16)v[1], (f16)v[2], (f16)v[3]};
 }
+AS_DEVICE void add_out(const QuantAttnArgs &a, bf16, int row, int col, int width, float v) {
+  if (a.rows_io) {
+    bf16 *p = (bf16 *)a.out + (size_t)row * width + col;
+    *p = (bf16)((float)*p + v);
+  } else {
+    f16 *p = (f16 *)a.out + act_off(row, col, a.B * a.n1, width);
+    *p = (f16)((float)*p + v);
+  }
+}
+AS_DEVICE void add_out(const QuantAttnArgs &a, float, int row, int col, int width, float v) {
+  ((float *)a.out)[(size_t)row * width + col] += v;
+}
 AS_DEVICE void store_out(const QuantAttnArgs &a, float, int row, int col, int width, f32x4 v) {
   *(f32x4 *)((float *)a.out + (size_t)row * width + col) = v;
 }
@@ -105,263 +142,604 @@ AS_DEVICE void store_out(const QuantAttnArgs &a, float, int row, int col, int wi
 AS_DEVICE bool not_finite(f16 v) { return (__builtin_bit_cast(uint16_t, v) & 0x7c00) == 0x7c00; }
 AS_DEVICE bool not_finite(float v) { return abs_bits(v) >= 0x7f800000u; }
 
-template <typename T, int HD, int TPW, int WPS>
-__global__ __launch_bounds__(NW * 64, WPS) void quant_attn_kernel(QuantAttnArgs a) {
+// The queries of a workgroup's tiles as operands of the scores, in LDS.
+//
+// fp32 model: [tile][hd / 32 fragments][lane][8], head dims lg * hd/4 + 8 s .. of query lr.
+template <typename T, int HD, int TPW> struct Queries {
+  float x[TPW][HD / 32][64][8];
+  AS_DEVICE f32x8 plain(int i, int s, int lane) const { return *(const f32x8 *)x[i][s][lane]; }
+  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int G, int g, int row0, int tid) {
+    const int width = a.H * HD;
+    for (int e = tid; e < TPW * 16 * (HD / 8); e += NW * 64) {
+      const int qi = e / (HD / 8), c = e % (HD / 8);     // query of the group, piece of 8 head dims
+      f32x8 v{};
+      if (qbase + qi < QR) {
+        const int r = (qbase + qi) / G, h = g * G + (qbase + qi - r * G);
+        v = load_q(a, T(), (size_t)(row0 + r) * width + h * HD + c * 8);
+      }
+      *(f32x8 *)x[qi >> 4][c % (HD / 32)][c / (HD / 32) * 16 + (qi & 15)] = v;
+    }
+  }
+};
+// bf16 model: e4m3 pieces [tile][piece][half][lane][16 bytes] and their scale bytes
+// [tile][lane].  Element k of the 128 that a product contracts is byte k % 16 of lane group
+// k % 64 / 16 in half k / 64 (measured; an e2m1 operand's is nibble k % 32 of lane group k / 32),
+// its scale that of lane group k / 32.  hd 128: pieces hi and lo, their scales bytes 0 and 1.
+// hd 64: one piece, the first half hi and the second lo (the keys' lane groups 2 and 3 repeat 0
+// and 1, so one product adds both).
+template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
+  static constexpr int NP = HD / 64;
+  u32x4 x[TPW][NP][2][64];
+  f16x8 wide[TPW][HD / 32][64];   // fp16, for the tail: as in the fp32 model
+  uint16_t scale[TPW][64];
+  AS_DEVICE f16x8 plain(int i, int s, int lane) const { return wide[i][s][lane]; }
+  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int G, int g, int row0, int tid) {
+    const int width = a.H * HD;
+    for (int e = tid; e < TPW * 16 * (HD / 32); e += NW * 64) {
+      const int qi = e / (HD / 32), c = e % (HD / 32), lr = qi & 15;   // query, group of 32
+      f16x8 v[4] = {};
+      uint32_t top = 0;
+      if (qbase + qi < QR) {
+        const int r = (qbase + qi) / G, h = g * G + (qbase + qi - r * G);
+        const size_t off = (size_t)(row0 + r) * width + h * HD + c * 32;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) v[s] = load_q(a, T16(), off + s * 8);
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {   // piece 4 c + s of 8 head dims
+        const int piece = 4 * c + s, lg = piece / (HD / 32);
+        wide[qi >> 4][piece % (HD / 32)][lg * 16 + lr] = v[s];
+      }
+      float f[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        f[j] = (float)v[j >> 3][j & 7];
+        top = max(top, abs_bits(f[j]));
+      }
+      // hi: the largest in [128, 256); what it leaves is at most 8, lo holds 16 times that
+      const int ex = max((int)(top >> 23), 30) - 7;      // biased; fp16 queries are 2^-24 or 0
+      const bool bad = top >= 0x7f800000u;               // NaN or inf: every score is NaN
+      const float down = __uint_as_float((uint32_t)(254 - ex) << 23);
+      uint32_t hi[8], lo[8];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = bad ? 0.f : f[4 * w + j] * down;
+        hi[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        hi[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi[w], true);
+        float d[4];
+        d[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 0)) * 16.f;
+        d[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 1)) * 16.f;
+        d[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 2)) * 16.f;
+        d[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 3)) * 16.f;
+        lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(d[0], d[1], 0, false);
+        lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(d[2], d[3], lo[w], true);
+      }
+      const uint32_t sh = bad ? 255u : (uint32_t)ex, sl = bad ? 255u : (uint32_t)(ex - 4);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {   // elements 16 h .. + 16 of the group
+        const u32x4 vh = {hi[4 * h], hi[4 * h + 1], hi[4 * h + 2], hi[4 * h + 3]};
+        const u32x4 vl = {lo[4 * h], lo[4 * h + 1], lo[4 * h + 2], lo[4 * h + 3]};
+        if (HD == 128) {
+          const int l = ((c & 1) * 2 + h) * 16 + lr;
+          x[qi >> 4][0][c >> 1][l] = vh;
+          x[qi >> 4][NP - 1][c >> 1][l] = vl;
+        } else {
+          x[qi >> 4][0][0][(c * 2 + h) * 16 + lr] = vh;
+          x[qi >> 4][0][1][(c * 2 + h) * 16 + lr] = vl;
+        }
+      }
+      if (HD == 128) {
+        scale[qi >> 4][c * 16 + lr] = (uint16_t)(sh | (sl << 8));
+      } else {
+        scale[qi >> 4][c * 16 + lr] = (uint16_t)sh;
+        scale[qi >> 4][c * 16 + lr + 32] = (uint16_t)sl;
+      }
+    }
+  }
+  typedef bf16 T16;
+};
+
+// What a lane holds of a block's keys as operands of the scores.
+template <typename T, int HD> struct Keys {   // fp32 model: decoded
+  u32x4 k[HD / 64];
+  uint32_t ks;
+  AS_DEVICE void load(const uint8_t *rec, int lane) {
+    const int lr = lane & 15, lg = lane >> 4;
+#pragma unroll
+    for (int h = 0; h < HD / 64; ++h) k[h] = *(const u32x4 *)(rec + h * 1024 + lane * 16);
+    ks = *(const uint16_t *)(rec + 32 * HD + (lr * (HD / 32) + (HD == 128 ? lg : lg >> 1)) * 2);
+  }
+  template <int TPW>
+  AS_DEVICE void score(const Queries<T, HD, TPW> &q, int lane, const uint32_t (&)[TPW], f32x4 (&sc)[TPW][2]) const {
+    f32x8 kf[2][HD / 32];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int s = 0; s < HD / 32; ++s)
+        kf[kk][s] = q4_decode_f32(HD == 128 ? k[kk * (HD / 128)][s] : k[0][kk * 2 + s],
+                                  q4_scale((ks >> (8 * kk)) & 255u));
+    dot<TPW>(q, kf, lane, sc);
+  }
+  template <int TPW>
+  static AS_DEVICE void dot(const Queries<T, HD, TPW> &q, const f32x8 (&kf)[2][HD / 32], int lane,
+                            f32x4 (&sc)[TPW][2]) {
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      sc[i][0] = sc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < HD / 32; ++s) {
+        const f32x8 qf = *(const f32x8 *)q.x[i][s][lane];
+        sc[i][0] = Ops<T>::mma(kf[0][s], qf, sc[i][0]);
+        sc[i][1] = Ops<T>::mma(kf[1][s], qf, sc[i][1]);
+      }
+    }
+  }
+};
+template <int HD> struct Keys<bf16, HD> {     // bf16 model: as they are
+  u32x4 k[2];
+  uint32_t ks;
+  AS_DEVICE void load(const uint8_t *rec, int lane) {
+    const int lr = lane & 15, lg = lane >> 4;
+    if constexpr (HD == 128) {
+      k[0] = *(const u32x4 *)(rec + lane * 16);
+      k[1] = *(const u32x4 *)(rec + 1024 + lane * 16);
+      ks = *(const uint16_t *)(rec + 32 * HD + (lr * 4 + lg) * 2);
+    } else {   // both 16-dim halves of group lg % 2, each with both operands' keys
+      k[0] = *(const u32x4 *)(rec + ((lg & 1) * 32 + lr) * 16);
+      k[1] = *(const u32x4 *)(rec + ((lg & 1) * 32 + 16 + lr) * 16);
+      ks = *(const uint16_t *)(rec + 32 * HD + (lr * 2 + (lg & 1)) * 2);
+    }
+  }
+  template <int TPW>
+  AS_DEVICE void score(const Queries<bf16, HD, TPW> &q, int lane, const uint32_t (&qs)[TPW],
+                       f32x4 (&sc)[TPW][2]) const {
+    i32x8 kf[2] = {};
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        kf[kk][j] = (int)(HD == 128 ? k[kk][j] : k[j >> 1][kk * 2 + (j & 1)]);
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      sc[i][0] = sc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < HD / 64; ++p) {
+        const u32x4 b0 = q.x[i][p][0][lane], b1 = q.x[i][p][1][lane];
+        const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3],
+                         (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
+        // operand formats: 4 e2m1 (keys), 0 e4m3 (queries); scale byte kk and p
+        if (p == 0) {
+          sc[i][0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[0], b, sc[i][0], 4, 0, 0, (int)ks, 0, (int)qs[i]);
+          sc[i][1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[1], b, sc[i][1], 4, 0, 1, (int)ks, 0, (int)qs[i]);
+        } else {
+          sc[i][0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[0], b, sc[i][0], 4, 0, 0, (int)ks, 1, (int)qs[i]);
+          sc[i][1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[1], b, sc[i][1], 4, 0, 1, (int)ks, 1, (int)qs[i]);
+        }
+      }
+    }
+  }
+};
+// ... and of its values.
+template <int HD> struct Values {
+  u32x4 v[HD / 64];
+  uint32_t vs[HD / 64];   // byte nb % 4 of word nb / 4
+  AS_DEVICE void load(const uint8_t *rec, int lane) {
+#pragma unroll
+    for (int h = 0; h < HD / 64; ++h) {
+      v[h] = *(const u32x4 *)(rec + 16 * HD + h * 1024 + lane * 16);
+      vs[h] = *(const uint32_t *)(rec + 33 * HD + (lane & 15) * (HD / 16) + h * 4);
+    }
+  }
+  AS_DEVICE float scale(int nb) const { return q4_scale((vs[nb >> 2] >> (8 * (nb & 3))) & 255u); }
+};
+
+template <typename T, int HD, int TPW> struct Shared {
+  union {
+    Queries<T, HD, TPW> q;
+    f32x4 part[TPW < JOIN ? TPW : JOIN][NW][(HD / 16) * (NW - 1) / NW][64];   // accumulators other waves join
+  };
+  RowView view[TPW * 16];
+  float2 ml[NW][TPW * 16];
+};
+
+template <typename T, int HD, int TPW, int LDST>
+AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int item, int split, int qbase) {
   typedef Ops<T> O;
   typedef typename O::F8 F8;
-  constexpr int KS = HD / 32, NB = HD / 16, LD = HD / 4;
-  __shared__ __attribute__((aligned(16))) typename O::E qs[TPW * 16 * HD];  // [tile][s][lane][8]
-  __shared__ RowView view[TPW * 16];
-  __shared__ f32x4 mo[NW * NB * 64];
-  __shared__ float2 ml[NW][TPW * 16];
-
-  // The query groups and the splits of a session's kv head follow each other on one XCD: the
-  // groups read the same records.
-  const int id = xcd_tile(blockIdx.x, gridDim.x);
-  const int grp = id % a.nqg, split = id / a.nqg % a.nsplit, item = id / (a.nqg * a.nsplit);
+  typedef typename O::E E;
+  typedef typename O::Raw Raw;
+  constexpr int NB = HD / 16, LD = HD / 4, OWN = NB / NW;   // OWN: value operands a wave joins
+  Shared<T, HD, TPW> &sm = reinterpret_cast<Shared<T, HD, TPW> &>(smem_);
   const int b = item / a.Hkv, g = item - b * a.Hkv;
-  const int G = a.H / a.Hkv, QR = G * a.n1, qbase = grp * TPW * 16;
+  const int G = a.H / a.Hkv, QR = G * a.n1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lg = lane >> 4;
   const int row0 = b * a.n1, width = a.H * HD;
   const int P = a.pos[row0], t = P & (Q4_SLOTS - 1), full = P / Q4_SLOTS;
-  // Blocks that some row sees: [0, nsink) and [wlo, full), then the tail's.
-  int nsink = 0, wlo = 0;
+
+  // Complete blocks that some row sees: [0, nsink) and [wlo, full).  Those that every row sees
+  // whole are [0, send) and [wend, full); a window cuts [send, nsink) and [wlo, wend).
+  int nsink = 0, wlo = 0, send = 0, wend = 0;
   if (a.window) {
-    const int lo = max(P - a.window + 1, 0);           // the root's window, the furthest back
-    wlo = min(lo / Q4_SLOTS, full);
+    wlo = min(max(P - a.window + 1, 0) / Q4_SLOTS, full);        // the root's window starts first
     nsink = min((int)(((unsigned)a.sinks + Q4_SLOTS - 1) / Q4_SLOTS), wlo);
+    send = min(a.sinks / Q4_SLOTS, nsink);
+    const long long last = (long long)P + a.n1 - a.window;       // the deepest row's at most here
+    wend = min(max((int)((last > 0 ? last : 0) + Q4_SLOTS - 1) / Q4_SLOTS, wlo), full);
   }
-  const int nq = nsink + full - wlo, total = nq + (t + a.n1 + Q4_SLOTS - 1) / Q4_SLOTS;
-  const int per = (total + a.nsplit - 1) / a.nsplit;
-  const int c0 = min(split * per, total), c1 = min(c0 + per, total);
-
-  for (int e = tid; e < TPW * 16 * (HD / 8); e += NW * 64) {
-    const int qi = e / (HD / 8), c = e % (HD / 8);     // query of the group, piece of 8 head dims
-    const int s = c % KS, l = c / KS * 16 + (qi & 15);
-    F8 v{};
-    if (qbase + qi < QR) {
-      const int r = (qbase + qi) / G, h = g * G + (qbase + qi - r * G);
-      v = load_q(a, T(), (size_t)(row0 + r) * width + h * HD + c * 8);
-    }
-    *(F8 *)(qs + (((qi >> 4) * KS + s) * 64 + l) * 8) = v;
-  }
-  for (int e = tid; e < TPW * 16; e += NW * 64) {
-    const int r = min(qbase + e, QR - 1) / G, p = a.pos[row0 + r];
-    view[e].lo = a.window ? p - a.window + 1 : -1;
-    view[e].root = !a.window || p - P < a.window || P < a.sinks;
-    view[e].anc = a.anc[row0 + r];
-  }
-  __syncthreads();
-
-  const float sscale = LOG2E / sqrtf((float)HD), lazy = LAZY_LOG2 / sscale;
-  float m_run[TPW], l_run[TPW];
-  f32x4 o[TPW][NB];
-#pragma unroll
-  for (int i = 0; i < TPW; ++i) {
-    m_run[i] = -INFINITY;
-    l_run[i] = 0.f;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) o[i][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  // The scores of tile i against a block's keys and their step of the online softmax; `vis`
-  // has a bit for each of the lane's 8 slots.
-  auto soft = [&](int i, const F8 (&kf)[2][KS], uint32_t vis, bool masked) -> F8 {
-    f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const F8 qf = *(const F8 *)(qs + ((i * KS + s) * 64 + lane) * 8);
-      sc[0] = O::mma(kf[0][s], qf, sc[0]);
-      sc[1] = O::mma(kf[1][s], qf, sc[1]);
-    }
-    if (masked) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (!((vis >> j) & 1u)) sc[j >> 2][j & 3] = -INFINITY;
-    }
-    float mx = sc[0][0];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j >> 2][j & 3]);
-    if (__ballot(mx > m_run[i] + lazy)) {
-      mx = rows4_max(mx);
-      const float mn = mx > m_run[i] + lazy ? mx : m_run[i];
-      const float alpha = __builtin_amdgcn_exp2f((m_run[i] - (mn == -INFINITY ? 0.f : mn)) * sscale);
-      m_run[i] = mn;
-      l_run[i] *= alpha;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][nb][e] *= alpha;
-    }
-    const float mb = m_run[i] == -INFINITY ? 0.f : m_run[i] * sscale;
-    F8 p;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float v = __builtin_amdgcn_exp2f(fmaf(sc[j >> 2][j & 3], sscale, -mb));
-      l_run[i] += v;
-      p[j] = (typename O::E)v;
-    }
-    return p;
+  // Masked blocks, the tail's first, then the cut ones; then the whole ones.  A masked block
+  // counts as SLOW whole ones in the shares of the splits and of the waves.
+  const int ntail = (t + a.n1 + Q4_SLOTS - 1) / Q4_SLOTS;
+  const int nmask = ntail + nsink - send + wend - wlo, nwhole = send + full - wend;
+  const int per = (nmask * SLOW + nwhole + a.nsplit - 1) / a.nsplit;
+  const int u0 = split * per, u1 = u0 + per;
+  const int m0 = min((u0 + SLOW - 1) / SLOW, nmask), m1 = min((u1 + SLOW - 1) / SLOW, nmask);
+  const int w0 = min(max(u0 - nmask * SLOW, 0), nwhole), w1 = min(max(u1 - nmask * SLOW, 0), nwhole);
+  auto masked_block = [&](int m) {   // m >= ntail: a record
+    m -= ntail;
+    return m < nsink - send ? send + m : wlo + m - (nsink - send);
   };
-  // O^T += V^T P^T for head dims 16 nb .. where rows do not all see the same slots: slots whose
-  // value is not finite go one at a time, to the rows that see them (0 * NaN is NaN).
-  auto weigh = [&](int nb, F8 vf, const F8 (&p)[TPW], const uint32_t (&vis)[TPW]) {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) bad |= (uint32_t)not_finite(vf[j]) << j;
-    if (__ballot(bad != 0)) {
-      for (int js = 0; js < Q4_SLOTS; ++js) {
-        const bool mine = lg == js >> 3;
-        const int je = js & 7;
-        if (!__ballot(mine && ((bad >> je) & 1u))) continue;
-        F8 v1;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v1[j] = mine && j == je ? vf[j] : (typename O::E)0.f;
-          vf[j] = mine && j == je ? (typename O::E)0.f : vf[j];
-        }
-#pragma unroll
-        for (int i = 0; i < TPW; ++i) {
-          F8 p1;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) p1[j] = mine && j == je ? p[i][j] : (typename O::E)0.f;
-          const bool sees = ((uint32_t)__shfl((int)vis[i], (js >> 3) * 16 + lr) >> je) & 1u;
-          const f32x4 n = O::mma(v1, p1, o[i][nb]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[i][nb][e] = sees ? n[e] : o[i][nb][e];
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], o[i][nb]);
+  auto whole_block = [&](int c) { return c < send ? c : wend + c - send; };
+  // Of the split's masked blocks wave w takes every NW-th; the first `odd` waves one more than
+  // the others, which have SLOW rounds of whole blocks to themselves.
+  const int odd = (m1 - m0) % NW;
+  auto whole_of_round = [&](int r) {
+    const int alone = SLOW * (NW - odd);
+    return r < SLOW ? w0 + r * (NW - odd) + wave - odd : w0 + alone + (r - SLOW) * NW + wave;
   };
 
   const uint8_t *rec0 = a.blocks + (size_t)item * a.nblk * q4_bytes(HD);
   const T *tk = (const T *)a.tk + (size_t)item * a.tcap * HD;
   const T *tv = (const T *)a.tv + (size_t)item * HD * a.tcap;
-  auto block_of = [&](int c) { return c < nsink ? c : wlo + c - nsink; };
-  Q4Regs<HD> cur, nxt;
-  if (c0 + wave < min(c1, nq)) q4_load<HD>(cur, rec0 + (size_t)block_of(c0 + wave) * q4_bytes(HD), lane);
-  for (int c = c0 + wave; c < c1; c += NW) {
-    if (c + NW < min(c1, nq)) q4_load<HD>(nxt, rec0 + (size_t)block_of(c + NW) * q4_bytes(HD), lane);
-    const int slot0 = block_of(c) * Q4_SLOTS;
-    F8 kf[2][KS], p[TPW];
-    // Every row sees the whole block unless a window ends in it.
-    if (c < nq && (a.window == 0 || slot0 + Q4_SLOTS <= a.sinks || slot0 >= P + a.n1 - a.window)) {
+  int round = wave < odd ? SLOW : 0, c = whole_of_round(round);
+  auto record = [&](int c) { return rec0 + (size_t)whole_block(min(c, nwhole - 1)) * q4_bytes(HD); };
+  // A wave's first block of the tail is loaded ahead of everything.
+  Raw kt[2][HD / 32], vt[NB];
+  const bool early = m0 + wave < min(m1, ntail);
+  if (early) {
+    const int s0 = (m0 + wave) * Q4_SLOTS;
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+    for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-          kf[kk][s] = O::decode(q4_kword<HD>(cur, kk, s), q4_kscale<HD>(cur, kk));
+      for (int s = 0; s < HD / 32; ++s)
+        kt[kk][s] = O::raw(tk + (size_t)(s0 + q4_key(kk, lr)) * HD + lg * LD + s * 8);
 #pragma unroll
-      for (int i = 0; i < TPW; ++i) p[i] = soft(i, kf, 0, false);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const F8 vf = O::decode(q4_vword<HD>(cur, nb), q4_vscale<HD>(cur, nb));
-#pragma unroll
-        for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], o[i][nb]);
-      }
-    } else {
-      // A block that a window cuts, or one of the tail: slots of the last, incomplete block,
-      // then the tree's rows.
-      const bool tail = c >= nq;
-      const int s0 = tail ? (c - nq) * Q4_SLOTS : 0;       // first slot within the tail
-      const int tr0 = tail ? s0 - t + lg * 8 : -Q4_SLOTS;  // tree row of the lane's first slot
-      const int pos0 = (tail ? full * Q4_SLOTS + s0 : slot0) + lg * 8;
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-          kf[kk][s] = tail ? O::load(tk + (size_t)(s0 + q4_key(kk, lr)) * HD + lg * LD + s * 8)
-                           : O::decode(q4_kword<HD>(cur, kk, s), q4_kscale<HD>(cur, kk));
-      uint32_t vis[TPW];
-#pragma unroll
-      for (int i = 0; i < TPW; ++i) {
-        const RowView w = view[i * 16 + lr];
-        vis[i] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int tr = tr0 + j, slot = pos0 + j;
-          const bool see = tr < 0 ? slot < a.sinks || slot >= w.lo
-                                  : tr == 0 ? w.root != 0 : tr < a.n1 && ((w.anc >> (tr - 1)) & 1ull);
-          vis[i] |= (uint32_t)see << j;
-        }
-        p[i] = soft(i, kf, vis[i], true);
-      }
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        F8 vf;
-        if (tail) {
-          vf = O::load(tv + (size_t)(nb * 16 + lr) * a.tcap + s0 + lg * 8);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (tr0 + j >= a.n1) vf[j] = (typename O::E)0.f;   // never written
-        } else {
-          vf = O::decode(q4_vword<HD>(cur, nb), q4_vscale<HD>(cur, nb));
-        }
-        weigh(nb, vf, p, vis);
-      }
-    }
-    cur = nxt;
+    for (int nb = 0; nb < NB; ++nb)
+      vt[nb] = O::raw(tv + (size_t)(nb * 16 + lr) * a.tcap + s0 + lg * 8);
   }
 
-  // Join the waves: o[i][nb][e] is head dim 16 nb + 4 lg + e of query 16 i + lr.
+  sm.q.fill(a, qbase, QR, G, g, row0, tid);
+  for (int e = tid; e < TPW * 16; e += NW * 64) {
+    const int r = min(qbase + e, QR - 1) / G, p = a.pos[row0 + r];
+    sm.view[e].lo = a.window ? max(p - a.window + 1, 0) : 0;
+    sm.view[e].root = !a.window || p - P < a.window || P < a.sinks;
+    sm.view[e].anc = a.anc[row0 + r];
+  }
+  __syncthreads();
+  uint32_t qs[TPW];   // scale bytes of the queries' pieces
+#pragma unroll
+  for (int i = 0; i < TPW; ++i) {
+    if constexpr (sizeof(T) == 2) qs[i] = sm.q.scale[i][lane];
+    else qs[i] = 0;
+  }
+
+  const float sscale = LOG2E / sqrtf((float)HD), lazy = LAZY_LOG2 / sscale;
+  float m_run[TPW], mb[TPW], l_run[TPW];   // reference, the same as an exponent (0 if none), sum
+  f32x4 o[TPW][NB];
+  // Moves the references that a score exceeds by too much.
+  auto refer = [&](const f32x4 (&sc)[TPW][2]) {
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      float mx = sc[i][0][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[i][j >> 2][j & 3]);
+      if (__ballot(mx > m_run[i] + lazy)) {
+        mx = rows4_max(mx);
+        const float mn = mx > m_run[i] + lazy ? mx : m_run[i];
+        const float alpha = __builtin_amdgcn_exp2f((m_run[i] - (mn == -INFINITY ? 0.f : mn)) * sscale);
+        m_run[i] = mn;
+        mb[i] = mn == -INFINITY ? 0.f : mn * sscale;
+        l_run[i] *= alpha;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][nb][e] *= alpha;
+      }
+    }
+  };
+  // The weights of tile i, in place of its scores; their sum in the lane.
+  auto weights = [&](int i, f32x4 (&sc)[TPW][2]) -> float {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      sc[i][j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(sc[i][j >> 2][j & 3], sscale, -mb[i]));
+    const f32x4 h = f32x4{sc[i][0][0] + sc[i][1][0], sc[i][0][1] + sc[i][1][1],
+                          sc[i][0][2] + sc[i][1][2], sc[i][0][3] + sc[i][1][3]};
+    return (h[0] + h[1]) + (h[2] + h[3]);
+  };
+  auto operand = [&](const f32x4 (&sc)[2]) -> F8 {
+    F8 p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = (E)sc[j >> 2][j & 3];
+    return p;
+  };
+
+  // Masked blocks: those of the tail (slots of the last, incomplete block, then the tree's
+  // rows) and records that a window cuts.
+  bool bad = false;   // one held values that are not finite: left out here, put in at the end
+  auto mask = [&](int i, int tr0, int pos0, f32x4 (&sc)[2]) {
+    const uint32_t vis = visible(sm.view[i * 16 + lr], a.sinks, tr0, pos0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sc[j >> 2][j & 3] = (vis >> j) & 1u ? sc[j >> 2][j & 3] : -INFINITY;
+  };
+  auto clean = [&](F8 vf, int tr0) -> F8 {   // slots behind the last row were never written
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool nf = not_finite(vf[j]), there = tr0 + j < a.n1;
+      bad |= nf && there;
+      vf[j] = nf || !there ? (E)0.f : vf[j];
+    }
+    return vf;
+  };
+  if (early) {   // nothing is summed yet
+    const int s0 = (m0 + wave) * Q4_SLOTS, tr0 = s0 - t + lg * 8;
+    F8 p[TPW];
+    f32x4 sc[TPW][2];
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int s = 0; s < HD / 32; ++s) {
+        const F8 kf = O::wide(kt[kk][s]);
+#pragma unroll
+        for (int i = 0; i < TPW; ++i)
+          sc[i][kk] = O::mma(kf, sm.q.plain(i, s, lane), s ? sc[i][kk] : zero);
+      }
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      mask(i, tr0, full * Q4_SLOTS + s0 + lg * 8, sc[i]);
+      float mx = sc[i][0][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[i][j >> 2][j & 3]);
+      m_run[i] = rows4_max(mx);
+      mb[i] = m_run[i] == -INFINITY ? 0.f : m_run[i] * sscale;
+      l_run[i] = weights(i, sc);
+      p[i] = operand(sc[i]);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const F8 vf = clean(O::wide(vt[nb]), tr0);
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], zero);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      m_run[i] = -INFINITY;
+      mb[i] = l_run[i] = 0.f;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) o[i][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+#pragma unroll 1
+  for (int m = m0 + wave + (early ? NW : 0); m < m1; m += NW) {
+    const bool tail = m < ntail;
+    const int blk = masked_block(m), s0 = m * Q4_SLOTS;   // s0: first slot within the tail
+    const int tr0 = tail ? s0 - t + lg * 8 : -Q4_SLOTS;
+    const int pos0 = (tail ? full * Q4_SLOTS + s0 : blk * Q4_SLOTS) + lg * 8;
+    const uint8_t *rec = rec0 + (size_t)(tail ? 0 : blk) * q4_bytes(HD);
+    f32x4 sc[TPW][2];
+    if (tail) {
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) sc[i][0] = sc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+        for (int s = 0; s < HD / 32; ++s) {
+          const F8 kf = O::wide(O::raw(tk + (size_t)(s0 + q4_key(kk, lr)) * HD + lg * LD + s * 8));
+#pragma unroll
+          for (int i = 0; i < TPW; ++i) sc[i][kk] = O::mma(kf, sm.q.plain(i, s, lane), sc[i][kk]);
+        }
+        SCHED_FENCE();
+      }
+    } else {
+      Keys<T, HD> kc;
+      kc.load(rec, lane);
+      kc.score(sm.q, lane, qs, sc);
+    }
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      mask(i, tr0, pos0, sc[i]);
+      SCHED_FENCE();
+    }
+    refer(sc);
+    F8 p[TPW];
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      l_run[i] += weights(i, sc);
+      p[i] = operand(sc[i]);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      F8 vf;
+      if (tail)
+        vf = O::wide(O::raw(tv + (size_t)(nb * 16 + lr) * a.tcap + s0 + lg * 8));
+      else
+        vf = O::decode(*(const uint32_t *)(rec + 16 * HD + (nb >> 2) * 1024 + lane * 16 + (nb & 3) * 4),
+                       q4_scale(rec[33 * HD + lr * NB + nb]));
+      vf = clean(vf, tr0);
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], o[i][nb]);
+      if (nb % 2) SCHED_FENCE();
+    }
+  }
+  // Whole blocks.  The next block's keys are asked for once the scores have read this one's,
+  // its values once they are multiplied: a wave's loads cross the other half of its work.
+  // A lane does not look for its largest score: a reference that is too low (or, before the
+  // first, -inf) shows in the sum of the weights, and the scores are then computed again.
+#pragma unroll
+  for (int i = 0; i < TPW; ++i)
+    if (m_run[i] == -INFINITY) mb[i] = -INFINITY;
+  Keys<T, HD> key;
+  Values<HD> val;
+  if (c < w1) {
+    key.load(record(c), lane);
+    val.load(record(c), lane);
+  }
+  while (c < w1) {
+    c = whole_of_round(++round);
+    f32x4 sc[TPW][2];
+    float add[TPW];
+    bool over = false;
+    key.score(sm.q, lane, qs, sc);
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      add[i] = weights(i, sc);
+      over |= add[i] > LAZY_SUM;
+    }
+    if (__ballot(over)) {
+      key.score(sm.q, lane, qs, sc);
+      refer(sc);
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) add[i] = weights(i, sc);
+    }
+    key.load(record(c), lane);
+    F8 p[TPW];
+#pragma unroll
+    for (int i = 0; i < TPW; ++i) {
+      l_run[i] += add[i];
+      p[i] = operand(sc[i]);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const F8 vf = O::decode(val.v[nb >> 2][nb & 3], val.scale(nb));
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], o[i][nb]);
+    }
+    val.load(record(c), lane);
+  }
+
+  // Join the waves: o[i][nb][e] is head dim 16 nb + 4 lg + e of query 16 i + lr.  Wave w joins
+  // the operands nb = w OWN .. and hands the others' to their waves.
 #pragma unroll
   for (int i = 0; i < TPW; ++i) {
     const float l = rows4_sum(l_run[i]);
     if (lg == 0)
-      ml[wave][i * 16 + lr] = make_float2(m_run[i] == -INFINITY ? -INFINITY : m_run[i] * sscale, l);
+      sm.ml[wave][i * 16 + lr] = make_float2(m_run[i] == -INFINITY ? -INFINITY : m_run[i] * sscale, l);
   }
-  __syncthreads();
+  const bool any_bad = __syncthreads_or(bad);   // (and the queries are read)
+  float top[TPW], sum[TPW];
 #pragma unroll
   for (int i = 0; i < TPW; ++i) {
-    float M = -INFINITY, L = 0.f;
+    float M = -INFINITY, L = 0.f, f = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w][i * 16 + lr].x);
-    float f = 0.f;
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, sm.ml[w][i * 16 + lr].x);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float2 e = ml[w][i * 16 + lr];
+      const float2 e = sm.ml[w][i * 16 + lr];
       const float fw = e.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(e.x - M);
       L += fw * e.y;
       f = w == wave ? fw : f;
     }
+    top[i] = M;
+    sum[i] = L;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      f32x4 v = o[i][nb];
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] *= f;
-      mo[(wave * NB + nb) * 64 + lane] = v;
-    }
-    __syncthreads();
+      for (int e = 0; e < 4; ++e) o[i][nb][e] *= f;
+  }
+  // (qi: the query, acc: what the other waves handed over, for operand nb)
+  auto finish = [&](int i, int nb, f32x4 acc) {
     const int qi = qbase + i * 16 + lr;
+#pragma unroll
+    for (int w = 0; w < NW - 1; ++w) {
+      const f32x4 v = sm.part[i % JOIN][wave][w * OWN + nb % OWN][lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += v[e];
+    }
     if (qi < QR) {
       const int r = qi / G, h = g * G + (qi - r * G);
+      if (a.nsplit == 1) {
+        const float inv = 1.f / sum[i];                  // every row sees itself
 #pragma unroll
-      for (int x = 0; x < NB / NW; ++x) {
-        const int nb = wave * (NB / NW) + x;
-        f32x4 acc = mo[nb * 64 + lane];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) {
-          const f32x4 v = mo[(w * NB + nb) * 64 + lane];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] += v[e];
-        }
-        if (a.nsplit == 1) {
-          const float inv = 1.f / L;                   // every row sees itself
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] *= inv;
-          store_out(a, T(), row0 + r, h * HD + nb * 16 + lg * 4, width, acc);
-        } else {
-          const size_t q = ((size_t)item * a.nsplit + split) * QR + qi;
-          *(f32x4 *)(a.part_o + q * HD + nb * 16 + lg * 4) = acc;
-          if (nb == 0 && lg == 0) *(float2 *)(a.part_ml + q * 2) = make_float2(M, L);
-        }
+        for (int e = 0; e < 4; ++e) acc[e] *= inv;
+        store_out(a, T(), row0 + r, h * HD + nb * 16 + lg * 4, width, acc);
+      } else {
+        const size_t q = ((size_t)item * a.nsplit + split) * QR + qi;
+        *(f32x4 *)(a.part_o + q * HD + nb * 16 + lg * 4) = acc;
+        if (nb == 0 && lg == 0) *(float2 *)(a.part_ml + q * 2) = make_float2(top[i], sum[i]);
       }
     }
-    if (i + 1 < TPW) __syncthreads();
+  };
+#pragma unroll
+  for (int i = 0; i < TPW; ++i) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+      if (nb / OWN != wave)
+        sm.part[i % JOIN][nb / OWN][(wave - (wave > nb / OWN)) * OWN + nb % OWN][lane] = o[i][nb];
+    if (i % JOIN == JOIN - 1 || i + 1 == TPW) {
+      __syncthreads();
+#pragma unroll
+      for (int j = i / JOIN * JOIN; j <= i; ++j)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          if (nb / OWN == wave) finish(j, nb, o[j][nb]);
+      if (i + 1 < TPW) __syncthreads();
+    }
   }
+  if (!any_bad) return;
+  // Values that are not finite, in the masked blocks of this split (rare): added to the rows
+  // that see their slots, and to no others.
+  __threadfence();
+  __syncthreads();
+#pragma unroll 1
+  for (int x = tid; x < TPW * 16 * HD; x += NW * 64) {
+    const int e = x / HD, d = x % HD, qi = qbase + e;
+    if (qi >= QR) break;
+    const RowView w = sm.view[e];
+    float v = 0.f;
+#pragma unroll 1
+    for (int m = m0; m < m1; ++m) {
+      const bool tail = m < ntail;
+      const int blk = masked_block(m), s0 = m * Q4_SLOTS;
+      const int n = tail ? min(Q4_SLOTS, t + a.n1 - s0) : Q4_SLOTS;
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        if (!(visible(w, a.sinks, tail ? s0 + j - t : -Q4_SLOTS,
+                      tail ? full * Q4_SLOTS + s0 + j : blk * Q4_SLOTS + j) & 1u))
+          continue;
+        const float y = tail ? (float)(E)(float)tv[(size_t)d * a.tcap + s0 + j]
+                             : q4_scale(rec0[(size_t)blk * q4_bytes(HD) + 33 * HD + d % 16 * NB + d / 16]);
+        if (not_finite(y)) v += tail ? y : __builtin_nanf("");
+      }
+    }
+    if (v == 0.f) continue;
+    const int r = qi / G, h = g * G + (qi - r * G);
+    if (a.nsplit == 1) add_out(a, T(), row0 + r, h * HD + d, width, v);
+    else a.part_o[(((size_t)item * a.nsplit + split) * QR + qi) * HD + d] += v;
+  }
+}
+
+// Waves a SIMD holds, by the registers of the accumulators (hd 128: 32 a tile) and of the fp32
+// model's decoded keys.
+template <typename T> constexpr int waves_per_simd(int tpw) {
+  return sizeof(T) == 4 ? 2 : tpw == 1 ? 4 : tpw == 2 ? 3 : 2;
+}
+
+// A workgroup: TPW tiles of a session's kv head (or TPW - 1: the tiles are dealt evenly to nqg
+// groups) over one of nsplit shares of its blocks.
+template <typename T, int HD, int TPW>
+__global__ __launch_bounds__(NW * 64, waves_per_simd<T>(TPW)) void quant_attn_kernel(QuantAttnArgs a) {
+  __shared__ __attribute__((aligned(16))) Shared<T, HD, TPW> sm;
+  // The query groups and the splits of a session's kv head follow each other on one XCD: the
+  // groups read the same records.
+  const int id = xcd_tile(blockIdx.x, gridDim.x);
+  const int grp = id % a.nqg, split = id / a.nqg % a.nsplit, item = id / (a.nqg * a.nsplit);
+  const int tiles = (a.H / a.Hkv * a.n1 + 15) / 16, each = tiles / a.nqg, more = tiles % a.nqg;
+  const int qbase = (grp * each + min(grp, more)) * 16;
+  if (TPW == 1 || each + (grp < more) == TPW) attend<T, HD, TPW, TPW>(a, sm, item, split, qbase);
+  else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW>(a, sm, item, split, qbase);
 }
 
 // Joins the splits: one thread per 4 head dims of a query row.
@@ -398,7 +776,9 @@ __global__ __launch_bounds__(256) void quant_combine_kernel(QuantAttnArgs a, int
 
 template <typename T, int HD>
 void launch_tiles(int tpw, unsigned grid, hipStream_t s, const QuantAttnArgs &a) {
-  auto kernel = tpw == 1 ? quant_attn_kernel<T, HD, 1, 2> : quant_attn_kernel<T, HD, 2, 2>;
+  auto kernel = tpw == 1 ? quant_attn_kernel<T, HD, 1> : quant_attn_kernel<T, HD, 2>;
+  if constexpr (sizeof(T) == 2)
+    if (tpw == 3) kernel = quant_attn_kernel<T, HD, 3>;
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(NW * 64), 0, s, a);
 }
 
@@ -412,20 +792,28 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
                                   long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                                   int capacity, int tcap, int window, int sinks, int rows_io,
                                   int cus, hipStream_t s) {
-  constexpr int MAXT = 2;
-  const int QR = H / Hkv * n1, tiles = (QR + 15) / 16;
-  const int tpw = (tiles + (tiles + MAXT - 1) / MAXT - 1) / ((tiles + MAXT - 1) / MAXT);
-  const int nqg = (tiles + tpw - 1) / tpw, items = B * Hkv;
-  // Splits: two workgroups a CU, and at least two blocks a wave.
+  const int QR = H / Hkv * n1, tiles = (QR + 15) / 16, items = B * Hkv;
+  // Tiles a workgroup: more of them share a block's decoding and its read, fewer make more
+  // workgroups.
+  constexpr int MAXT = sizeof(T) == 2 ? 3 : 2;
+  const long long work = (long long)items * tiles;
+  const int most = work <= 2LL * cus ? 1 : work <= 4LL * cus ? 2 : MAXT;
+  const int nqg = (tiles + most - 1) / most, tpw = (tiles + nqg - 1) / nqg;
+  // Splits, where a CU would have less than two workgroups: as many as it holds at once (three
+  // rounds of the large ones, which leave less idle at the end), of at least 8 blocks a wave.
   const long long seen = window ? (long long)window + n1 + sinks + 2 * Q4_SLOTS : capacity;
   const int blocks_seen = (int)((seen < capacity ? seen : capacity) / Q4_SLOTS) + 3;
-  int nsplit = 2 * cus / (items * nqg);
-  nsplit = nsplit < blocks_seen / (2 * NW) ? nsplit : blocks_seen / (2 * NW);
+  const long long groups = (long long)items * nqg;
+  long long nsplit = 1;
+  if (groups < 2LL * cus) {
+    nsplit = (tpw == 1 ? 4LL : tpw == 2 ? 3LL : 6LL) * cus / groups;
+    nsplit = nsplit < blocks_seen / (8 * NW) ? nsplit : blocks_seen / (8 * NW);
+  }
   if (nsplit < 1) nsplit = 1;
   while (nsplit > 1 && (long long)items * nsplit * QR * hd > part_capacity) --nsplit;
   const QuantAttnArgs a{q, blocks, tk, tv, meta.pos, meta.anc, out, part_o, part_ml, B, n1, H, Hkv,
-                        capacity / Q4_SLOTS, tcap, nsplit, nqg, window, sinks, rows_io};
-  const unsigned grid = (unsigned)(items * nqg * nsplit);
+                        capacity / Q4_SLOTS, tcap, (int)nsplit, nqg, window, sinks, rows_io};
+  const unsigned grid = (unsigned)(groups * nsplit);
   if (hd == 128) launch_tiles<T, 128>(tpw, grid, s, a);
   else launch_tiles<T, 64>(tpw, grid, s, a);
   hipError_t e = hipGetLastError();
