@@ -59,126 +59,184 @@ AS_DEVICE uint32_t q4_group_scale(uint32_t top) {
 }
 AS_DEVICE uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// Eight elements to codes: the nearest, ties to the even code, at most 6.
-AS_DEVICE uint32_t q4_encode(const float *x, float s) {
-  uint32_t c = 0;
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
-  return c;
-}
+// Eight elements as they are stored, the largest of their magnitudes' bits (as fp32), and their
+// codes: the nearest, ties to the even code, at most 6.
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16> {
+  u32x4 w;
+  AS_DEVICE uint32_t top() const {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
+  }
+  AS_DEVICE uint32_t encode(float s) const {
+    const bf16x8 v = __builtin_bit_cast(bf16x8, w);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_shufflevector(v, v, 0, 1), s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_shufflevector(v, v, 2, 3), s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_shufflevector(v, v, 4, 5), s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_shufflevector(v, v, 6, 7), s, 3);
+    return c;
+  }
+  static AS_DEVICE u32x4 decoded(uint32_t c, float s) {   // exact in bf16
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+    return r;
+  }
+  AS_DEVICE void decode(uint32_t c, float s) { w = decoded(c, s); }
+  AS_DEVICE void load(const bf16 *p) { w = *(const u32x4 *)p; }
+  // (of memory that the kernel touches once: past L2 and the MALL)
+  AS_DEVICE void load_once(const bf16 *p) { w = __builtin_nontemporal_load((const u32x4 *)p); }
+  AS_DEVICE void store_once(bf16 *p) const { __builtin_nontemporal_store(w, (u32x4 *)p); }
+  AS_DEVICE void store(bf16 *p) const { *(u32x4 *)p = w; }
+  AS_DEVICE void store_first(bf16 *p, int n) const {   // n < 8 of them
+    if (n & 4) *(uint2 *)p = make_uint2(w[0], w[1]);
+    const uint32_t a = n & 4 ? w[2] : w[0], b = n & 4 ? w[3] : w[1];
+    if (n & 2) *(uint32_t *)(p + (n & 4)) = a;
+    if (n & 1) *(uint16_t *)(p + (n & 6)) = (uint16_t)(n & 2 ? b : a);
+  }
+};
+template <> struct Raw8<float> {
+  u32x4 w[2];
+  AS_DEVICE uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, w[i >> 2][i & 3] & 0x7fffffffu);
+    return m;
+  }
+  AS_DEVICE uint32_t encode(float s) const {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i >> 2][i & 3]);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
+    return c;
+  }
+  AS_DEVICE void decode(uint32_t c, float s) {
+    const f32x8 v = q4_decode_f32(c, s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = __float_as_uint(v[i]);
+  }
+  AS_DEVICE void load(const float *p) { w[0] = *(const u32x4 *)p; w[1] = *(const u32x4 *)(p + 4); }
+  AS_DEVICE void load_once(const float *p) {
+    w[0] = __builtin_nontemporal_load((const u32x4 *)p);
+    w[1] = __builtin_nontemporal_load((const u32x4 *)(p + 4));
+  }
+  AS_DEVICE void store_once(float *p) const {
+    __builtin_nontemporal_store(w[0], (u32x4 *)p);
+    __builtin_nontemporal_store(w[1], (u32x4 *)(p + 4));
+  }
+  AS_DEVICE void store_first(float *p, int n) const {
+    uint32_t *q = (uint32_t *)p;
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (i < n) q[i] = w[i >> 2][i & 3];
+  }
+  AS_DEVICE void store(float *p) const { *(u32x4 *)p = w[0]; *(u32x4 *)(p + 4) = w[1]; }
+};
 
 AS_DEVICE uint32_t max4_u32(uint32_t v) {   // over the lanes l, l^16, l^32, l^48
   v = max(v, (uint32_t)__shfl_xor((int)v, 16));
   return max(v, (uint32_t)__shfl_xor((int)v, 32));
 }
 
-// Eight consecutive elements as floats, and back (16-byte aligned).
-AS_DEVICE void load8(const bf16 *p, float *x) {
-  const bf16x8 v = *(const bf16x8 *)p;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-}
-AS_DEVICE void load8(const float *p, float *x) {
-  const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-AS_DEVICE void store8(bf16 *p, f32x8 x) {
-  bf16x8 v;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (bf16)x[i];
-  *(bf16x8 *)p = v;
-}
-AS_DEVICE void store8(float *p, f32x8 x) {
-  *(f32x4 *)p = f32x4{x[0], x[1], x[2], x[3]};
-  *(f32x4 *)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
-}
-
-// One wave writes a record from 32 slots: keys k[slot * HD + dim], values v[dim * vstride +
-// slot], both 16-byte aligned.
-template <typename T, int HD>
-AS_DEVICE void q4_encode_block(const T *k, const T *v, size_t vstride, uint8_t *rec, int lane) {
-  constexpr int LD = HD / 4, NB = HD / 16;   // head dims a lane holds of a key; value operands
+// One wave writes the key codes and scales of operand kk of a record; load(slot, dim) gives 8
+// head dims of a slot of the block.
+template <typename T, int HD, typename F>
+AS_DEVICE void q4_encode_keys(F &&load, int kk, uint8_t *rec, int lane) {
+  constexpr int LD = HD / 4;   // head dims a lane holds of a key
   const int lr = lane & 15, lg = lane >> 4;
-  uint32_t kc[2][LD / 8];
-  uint32_t ks[2];
+  Raw8<T> x[LD / 8];
+  uint32_t top = 0, c[LD / 8];
 #pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
-    float x[LD];
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < LD / 8; ++j) load8(k + (size_t)q4_key(kk, lr) * HD + lg * LD + j * 8, x + j * 8);
-#pragma unroll
-    for (int j = 0; j < LD; ++j) top = max(top, abs_bits(x[j]));
-    if (HD == 64) top = max(top, (uint32_t)__shfl_xor((int)top, 16));   // two lanes a group
-    ks[kk] = q4_group_scale(top);
-    const float s = q4_scale(ks[kk]);
-#pragma unroll
-    for (int j = 0; j < LD / 8; ++j) kc[kk][j] = ks[kk] == Q4_BAD ? 0u : q4_encode(x + j * 8, s);
+  for (int j = 0; j < LD / 8; ++j) {
+    x[j] = load(q4_key(kk, lr), lg * LD + j * 8);
+    top = max(top, x[j].top());
   }
-  uint32_t vc[NB];
-  uint64_t vs = 0;
+  if (HD == 64) top = max(top, (uint32_t)__shfl_xor((int)top, 16));   // two lanes a group
+  const uint32_t sb = q4_group_scale(top);
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    float x[8];
-    uint32_t top = 0;
-    load8(v + (size_t)(nb * 16 + lr) * vstride + lg * 8, x);
+  for (int j = 0; j < LD / 8; ++j) c[j] = sb == Q4_BAD ? 0u : x[j].encode(q4_scale(sb));
+  if constexpr (HD == 128) {
+    *(u32x4 *)(rec + kk * 1024 + lane * 16) = u32x4{c[0], c[1], c[2], c[3]};
+    rec[32 * HD + (lr * 4 + lg) * 2 + kk] = (uint8_t)sb;
+  } else {
+    *(uint2 *)(rec + lane * 16 + kk * 8) = make_uint2(c[0], c[1]);
+    if ((lg & 1) == 0) rec[32 * HD + (lr * 2 + (lg >> 1)) * 2 + kk] = (uint8_t)sb;
+  }
+}
+// ... and half `h` of its value operands; load(dim, slot) gives 8 slots of a head dim.
+template <typename T, int HD, typename F>
+AS_DEVICE void q4_encode_values(F &&load, int h, uint8_t *rec, int lane) {
+  constexpr int N = HD / 32;   // operands
+  const int lr = lane & 15, lg = lane >> 4;
+  uint32_t c[N], vs = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, abs_bits(x[j]));
-    const uint32_t sb = q4_group_scale(max4_u32(top));
-    vs |= (uint64_t)sb << (8 * nb);
-    vc[nb] = sb == Q4_BAD ? 0u : q4_encode(x, q4_scale(sb));
+  for (int n = 0; n < N; ++n) {
+    const Raw8<T> x = load((h * N + n) * 16 + lr, lg * 8);
+    const uint32_t sb = q4_group_scale(max4_u32(x.top()));
+    vs |= sb << (8 * n);
+    c[n] = sb == Q4_BAD ? 0u : x.encode(q4_scale(sb));
   }
   if constexpr (HD == 128) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-      *(u32x4 *)(rec + kk * 1024 + lane * 16) = u32x4{kc[kk][0], kc[kk][1], kc[kk][2], kc[kk][3]};
-    *(uint16_t *)(rec + 32 * HD + (lr * 4 + lg) * 2) = (uint16_t)(ks[0] | (ks[1] << 8));
-    if (lg == 0) *(uint2 *)(rec + 33 * HD + lr * 8) = make_uint2((uint32_t)vs, (uint32_t)(vs >> 32));
+    *(u32x4 *)(rec + 16 * HD + h * 1024 + lane * 16) = u32x4{c[0], c[1], c[2], c[3]};
+    if (lg == 0) *(uint32_t *)(rec + 33 * HD + lr * 8 + h * 4) = vs;
   } else {
-    *(u32x4 *)(rec + lane * 16) = u32x4{kc[0][0], kc[0][1], kc[1][0], kc[1][1]};
-    if ((lg & 1) == 0)
-      *(uint16_t *)(rec + 32 * HD + (lr * 2 + (lg >> 1)) * 2) = (uint16_t)(ks[0] | (ks[1] << 8));
-    if (lg == 0) *(uint32_t *)(rec + 33 * HD + lr * 4) = (uint32_t)vs;
+    *(uint2 *)(rec + 16 * HD + lane * 16 + h * 8) = make_uint2(c[0], c[1]);
+    if (lg == 0) *(uint16_t *)(rec + 33 * HD + lr * 4 + h * 2) = (uint16_t)vs;
   }
-#pragma unroll
-  for (int h = 0; h < NB / 4; ++h)
-    *(u32x4 *)(rec + 16 * HD + h * 1024 + lane * 16) =
-        u32x4{vc[h * 4], vc[h * 4 + 1], vc[h * 4 + 2], vc[h * 4 + 3]};
 }
 
-// What a lane holds of a record.
-template <int HD> struct Q4Regs {
-  u32x4 k[HD / 64], v[HD / 64];
-  uint32_t ks;           // bytes kk = 0, 1
-  uint32_t vs[HD / 64];  // byte nb % 4 of word nb / 4
+// What a lane holds of a record's operand kk of the keys, or half h of its values: codes (16
+// bytes; head dim 64: 8) and scale bytes.
+template <int HD> struct Q4Part {
+  u32x4 c;
+  uint32_t s;
+  AS_DEVICE void load_keys(const uint8_t *rec, int kk, int lane) {
+    const int lr = lane & 15, lg = lane >> 4;
+    if constexpr (HD == 128) {
+      c = *(const u32x4 *)(rec + kk * 1024 + lane * 16);
+    } else {
+      const uint2 v = *(const uint2 *)(rec + lane * 16 + kk * 8);
+      c = u32x4{v.x, v.y, 0, 0};
+    }
+    s = rec[32 * HD + (lr * (HD / 32) + (HD == 128 ? lg : lg >> 1)) * 2 + kk];
+  }
+  AS_DEVICE void load_values(const uint8_t *rec, int h, int lane) {
+    const int lr = lane & 15;
+    if constexpr (HD == 128) {
+      c = *(const u32x4 *)(rec + 16 * HD + h * 1024 + lane * 16);
+      s = *(const uint32_t *)(rec + 33 * HD + lr * 8 + h * 4);
+    } else {
+      const uint2 v = *(const uint2 *)(rec + 16 * HD + lane * 16 + h * 8);
+      c = u32x4{v.x, v.y, 0, 0};
+      s = *(const uint16_t *)(rec + 33 * HD + lr * 4 + h * 2);
+    }
+  }
+  // store(slot, dim, values) takes 8 head dims of a slot, store(dim, slot, values) 8 slots of
+  // a head dim
+  template <typename T, typename F> AS_DEVICE void decode_keys(F &&store, int kk, int lane) const {
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j) {
+      Raw8<T> x;
+      x.decode(c[j], q4_scale(s));
+      store(q4_key(kk, lane & 15), (lane >> 4) * (HD / 4) + j * 8, x);
+    }
+  }
+  template <typename T, typename F> AS_DEVICE void decode_values(F &&store, int h, int lane) const {
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n) {
+      Raw8<T> x;
+      x.decode(c[n], q4_scale((s >> (8 * n)) & 255u));
+      store((h * (HD / 32) + n) * 16 + (lane & 15), (lane >> 4) * 8, x);
+    }
+  }
 };
-template <int HD> AS_DEVICE void q4_load(Q4Regs<HD> &r, const uint8_t *rec, int lane) {
-  const int lr = lane & 15, lg = lane >> 4;
-#pragma unroll
-  for (int h = 0; h < HD / 64; ++h) {
-    r.k[h] = *(const u32x4 *)(rec + h * 1024 + lane * 16);
-    r.v[h] = *(const u32x4 *)(rec + 16 * HD + h * 1024 + lane * 16);
-  }
-  r.ks = *(const uint16_t *)(rec + 32 * HD + (lr * (HD / 32) + (HD == 128 ? lg : lg >> 1)) * 2);
-  if constexpr (HD == 128) {
-    const uint2 t = *(const uint2 *)(rec + 33 * HD + lr * 8);
-    r.vs[0] = t.x;
-    r.vs[1] = t.y;
-  } else {
-    r.vs[0] = *(const uint32_t *)(rec + 33 * HD + lr * 4);
-  }
-}
-// Word j of the lane's key codes of operand kk: head dims lg * HD/4 + 8 j .. + 8.
-template <int HD> AS_DEVICE uint32_t q4_kword(const Q4Regs<HD> &r, int kk, int j) {
-  return HD == 128 ? r.k[kk * (HD / 128)][j] : r.k[0][kk * 2 + j];
-}
-template <int HD> AS_DEVICE float q4_kscale(const Q4Regs<HD> &r, int kk) {
-  return q4_scale((r.ks >> (8 * kk)) & 255u);
-}
-template <int HD> AS_DEVICE uint32_t q4_vword(const Q4Regs<HD> &r, int nb) { return r.v[nb >> 2][nb & 3]; }
-template <int HD> AS_DEVICE float q4_vscale(const Q4Regs<HD> &r, int nb) {
-  return q4_scale((r.vs[nb >> 2] >> (8 * (nb & 3))) & 255u);
-}
