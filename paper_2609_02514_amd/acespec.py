@@ -6,6 +6,7 @@ library has not been built.
 """
 from __future__ import annotations
 
+import copy
 import ctypes as C
 import os
 from typing import Dict, List, Optional
@@ -293,14 +294,23 @@ def _ptr(t) -> Optional[int]:
 class QuantCache:
     """The tensors of a KV cache in 4 bits (acespec_kv_quant): blocks [L, B, Hkv,
     capacity / 32, 34 hd] uint8, tail_k [L, B, Hkv, tail_capacity, hd] and tail_v [L, B, Hkv,
-    hd, tail_capacity] in the model dtype, prefix_len [B] int32."""
+    hd, tail_capacity] in the model dtype, prefix_len [B] int32, all contiguous on one GPU.
+    Shapes and types are checked here, once; the tensors are the cache's from then on."""
 
     def __init__(self, blocks, tail_k, tail_v, capacity: int, tail_capacity: int, prefix_len):
+        import torch
+        if blocks.dim() != 5 or tail_k.dim() != 5 or tail_k.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("blocks and tail_k must have five dimensions, tail_k in bfloat16 or float32")
+        L, B, Hkv, _, hd = tail_k.shape
+        _check_tensors([("blocks", blocks, (L, B, Hkv, capacity // 32, 34 * hd), torch.uint8),
+                        ("tail_k", tail_k, (L, B, Hkv, tail_capacity, hd), tail_k.dtype),
+                        ("tail_v", tail_v, (L, B, Hkv, hd, tail_capacity), tail_k.dtype),
+                        ("prefix_len", prefix_len, (B,), torch.int32)], blocks.device)
         self.blocks, self.tail_k, self.tail_v = blocks, tail_k, tail_v
-        self.capacity, self.tail_capacity = capacity, tail_capacity
-        self.prefix_len = prefix_len
-        self._struct = None if prefix_len is None else KVQuant(
-            _ptr(blocks), _ptr(tail_k), _ptr(tail_v), capacity, tail_capacity, _ptr(prefix_len))
+        self.capacity, self.tail_capacity, self.prefix_len = capacity, tail_capacity, prefix_len
+        self._fit = (L, B, Hkv, hd, ACESPEC_BF16 if tail_k.dtype == torch.bfloat16 else ACESPEC_F32)
+        self._struct = KVQuant(_ptr(blocks), _ptr(tail_k), _ptr(tail_v), capacity, tail_capacity,
+                               _ptr(prefix_len))
 
     @classmethod
     def alloc(cls, L: int, B: int, Hkv: int, hd: int, capacity: int, max_nodes: int, dtype: str,
@@ -317,11 +327,27 @@ class QuantCache:
 
     def with_prefix(self, prefix_len) -> "QuantCache":
         """The same cache under other lengths (a commit's new_prefix_len)."""
-        return QuantCache(self.blocks, self.tail_k, self.tail_v, self.capacity,
-                          self.tail_capacity, prefix_len)
+        import torch
+        _check_tensors([("prefix_len", prefix_len, self.prefix_len.shape, torch.int32)],
+                       self.blocks.device)
+        other = copy.copy(self)
+        other.prefix_len = prefix_len
+        other._struct = KVQuant.from_buffer_copy(self._struct)
+        other._struct.prefix_len = _ptr(prefix_len)
+        return other
 
     def struct(self) -> KVQuant:
         return self._struct
+
+
+def _check_tensors(want, device=None):
+    """Tensors whose shape, type or stride differ from what the call says would be read out of
+    range."""
+    for name, t, shape, dt in want:
+        if t.shape != shape or t.dtype is not dt or not t.is_contiguous() or not t.is_cuda or (
+                device is not None and t.device != device):
+            raise ValueError(f"{name} must be a contiguous {dt} tensor {tuple(shape)} on the "
+                             f"GPU (got {t.dtype} {tuple(t.shape)} on {t.device})")
 
 
 class Verifier:
@@ -362,7 +388,6 @@ class Verifier:
         are shared with W.  The result carries `packed = True` for weights_struct.
         drop_source: release each row-major matrix of W once it is packed (W's entries
         become None), so that a model only slightly smaller than the device fits."""
-        import copy
         import torch
 
         def pk(t):
@@ -458,33 +483,27 @@ class Verifier:
                                    self.outputs_struct(outs), self._stream())
 
     def _check_quant(self, cache: QuantCache, B: int):
-        """The cache's tensors against this model: a wrong shape, type or stride would be read
-        out of range."""
         import torch
         d = self.desc
-        dt = torch.bfloat16 if d.dtype == ACESPEC_BF16 else torch.float32
-        lead = (d.n_layers, B, d.n_kv_heads)
-        want = [("blocks", cache.blocks, lead + (cache.capacity // 32, 34 * d.head_dim), torch.uint8),
-                ("tail_k", cache.tail_k, lead + (cache.tail_capacity, d.head_dim), dt),
-                ("tail_v", cache.tail_v, lead + (d.head_dim, cache.tail_capacity), dt),
-                ("prefix_len", cache.prefix_len, (B,), torch.int32)]
-        self._check_tensors(want)
+        if cache.blocks.device.index != torch.cuda.current_device():
+            raise ValueError(f"the cache is on {cache.blocks.device}, the current device and stream "
+                             f"are cuda:{torch.cuda.current_device()}'s")
+        if cache._fit != (d.n_layers, B, d.n_kv_heads, d.head_dim, d.dtype):
+            raise ValueError(f"a cache of (layers, sessions, kv heads, head dim, dtype) {cache._fit} "
+                             f"is not this model's and batch's "
+                             f"{(d.n_layers, B, d.n_kv_heads, d.head_dim, d.dtype)}")
 
-    @staticmethod
-    def _check_tensors(want):
-        for name, t, shape, dt in want:
-            if tuple(t.shape) != tuple(shape) or t.dtype != dt or not t.is_contiguous() or not t.is_cuda:
-                raise ValueError(f"{name} must be a contiguous {dt} tensor {tuple(shape)} on the "
-                                 f"GPU (got {t.dtype} {tuple(t.shape)} on {t.device})")
-
-    def _check_kv(self, kv_k, kv_v, capacity: int, B: int, more):
+    def _torch_dtype(self):
         import torch
-        d = self.desc
-        dt = torch.bfloat16 if d.dtype == ACESPEC_BF16 else torch.float32
+        return torch.bfloat16 if self.desc.dtype == ACESPEC_BF16 else torch.float32
+
+    def _check_kv(self, kv_k, kv_v, capacity: int, B: int, more, device):
+        import torch
+        d, dt = self.desc, self._torch_dtype()
         lead = (d.n_layers, B, d.n_kv_heads)
-        self._check_tensors([("kv_k", kv_k, lead + (capacity, d.head_dim), dt),
-                             ("kv_v", kv_v, lead + (d.head_dim, capacity), dt)]
-                            + [(n, t, (B,), torch.int32) for n, t in more if t is not None])
+        _check_tensors([("kv_k", kv_k, lead + (capacity, d.head_dim), dt),
+                        ("kv_v", kv_v, lead + (d.head_dim, capacity), dt)]
+                       + [(n, t, (B,), torch.int32) for n, t in more if t is not None], device)
 
     def quantize_kv(self, kv_k, kv_v, capacity: int, prefix_len, cache: QuantCache, status=None,
                     first=None) -> int:
@@ -492,7 +511,7 @@ class Verifier:
         prefix_len is not touched."""
         B = prefix_len.shape[0]
         self._check_kv(kv_k, kv_v, capacity, B, [("prefix_len", prefix_len), ("status", status),
-                                                 ("first", first)])
+                                                 ("first", first)], cache.blocks.device)
         self._check_quant(cache, B)
         kv = KVCache(_ptr(kv_k), _ptr(kv_v), capacity, _ptr(prefix_len))
         return acespec_quantize_kv(self.ctx, kv, cache.struct(), _ptr(first), B, _ptr(status),
@@ -502,7 +521,8 @@ class Verifier:
                       first=None) -> int:
         """Slots [first / 32 * 32, cache.prefix_len) read back into kv (acespec_dequantize_kv)."""
         B = cache.prefix_len.shape[0]
-        self._check_kv(kv_k, kv_v, capacity, B, [("status", status), ("first", first)])
+        self._check_kv(kv_k, kv_v, capacity, B, [("status", status), ("first", first)],
+                       cache.blocks.device)
         self._check_quant(cache, B)
         kv = KVCache(_ptr(kv_k), _ptr(kv_v), capacity, None)
         return acespec_dequantize_kv(self.ctx, cache.struct(), kv, _ptr(first), B, _ptr(status),
@@ -512,12 +532,11 @@ class Verifier:
                         window: int = 0, sinks: int = 0) -> int:
         """Tree attention of one layer (acespec_attention_quant): q, out [B, N+1, H, hd]."""
         import torch
-        d, (B, n1) = self.desc, parents.shape
-        dt = torch.bfloat16 if d.dtype == ACESPEC_BF16 else torch.float32
+        d, (B, n1), dt = self.desc, parents.shape, self._torch_dtype()
         shape = (B, n1, d.n_heads, d.head_dim)
-        self._check_tensors([("q", q, shape, dt), ("out", out, shape, dt),
-                             ("parents", parents, (B, n1), torch.int32),
-                             ("status", status, (B,), torch.int32)])
+        _check_tensors([("q", q, shape, dt), ("out", out, shape, dt),
+                        ("parents", parents, (B, n1), torch.int32),
+                        ("status", status, (B,), torch.int32)], cache.blocks.device)
         self._check_quant(cache, B)
         return acespec_attention_quant(self.ctx, cache.struct(), layer, AttnSpan(window, sinks),
                                        _ptr(q), _ptr(parents), B, n1 - 1, _ptr(out), _ptr(status),
@@ -539,9 +558,9 @@ class Verifier:
         import torch
         B, n1 = path.shape
         self._check_quant(cache, B)
-        self._check_tensors([(n, t, s, torch.int32) for n, t, s in (
+        _check_tensors([(n, t, s, torch.int32) for n, t, s in (
             ("path", path, (B, n1)), ("path_len", path_len, (B,)), ("status", status, (B,)),
-            ("new_prefix_len", new_prefix_len, (B,))) if t is not None])
+            ("new_prefix_len", new_prefix_len, (B,))) if t is not None], cache.blocks.device)
         return acespec_commit_kv_quant(self.ctx, cache.struct(), _ptr(path), _ptr(path_len),
                                        _ptr(status), B, n1 - 1, _ptr(new_prefix_len),
                                        self._stream())

@@ -153,12 +153,29 @@ def test_the_commit_needs_its_own_lengths():
 
 def test_tensors_of_another_shape_or_type_are_refused_by_the_binding():
     import torch
-    blocks = torch.zeros(2, 1, 1, 2, 34 * 64, dtype=torch.uint8)
+    blocks, prefix = torch.zeros(2, 1, 1, 2, 34 * 64, dtype=torch.uint8), torch.zeros(1, dtype=torch.int32)
     k, v = torch.zeros(2, 1, 1, 64, 64), torch.zeros(2, 1, 1, 64, 64)
+    for bad in ((blocks, k, v, 64, 64, prefix),          # right shapes, but not on the GPU
+                (blocks[:1], k, v, 64, 64, prefix), (blocks, k, v, 96, 64, prefix)):
+        with pytest.raises(ValueError, match="blocks"):
+            A.QuantCache(*bad)
+    with pytest.raises(ValueError, match="five dimensions"):
+        A.QuantCache(blocks[0], k, v, 64, 64, prefix)
+    with pytest.raises(ValueError, match="bfloat16 or float32"):
+        A.QuantCache(blocks, k.half(), v.half(), 64, 64, prefix)
+
+
+def test_a_cache_of_another_device_or_model_is_refused_by_the_binding(monkeypatch):
+    import torch
+    from types import SimpleNamespace
     ver = A.Verifier.__new__(A.Verifier)
     ver.desc, ver.ctx = A.ModelDesc(2, 64, 2, 1, 64, 64, 64, 1e4, 1e-5, A.ACESPEC_F32), None
-    c = A.QuantCache(blocks, k, v, 64, 64, torch.zeros(1, dtype=torch.int32))
-    with pytest.raises(ValueError, match="blocks"):        # right shapes, but not on the GPU
-        ver._check_quant(c, 1)
-    with pytest.raises(ValueError, match="blocks"):
-        ver._check_quant(A.QuantCache(blocks[:1], k, v, 64, 64, c.prefix_len), 1)
+    c = A.QuantCache.__new__(A.QuantCache)
+    c.blocks, c._fit = SimpleNamespace(device=torch.device("cuda:1")), (2, 3, 1, 64, A.ACESPEC_F32)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="cuda:1"):
+        ver._check_quant(c, 3)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    ver._check_quant(c, 3)
+    with pytest.raises(ValueError, match="is not this model's"):
+        ver._check_quant(c, 2)
