@@ -173,42 +173,44 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
   f16x8 wide[TPW][HD / 32][64];   // fp16, for the tail: as in the fp32 model
   uint16_t scale[TPW][64];
   AS_DEVICE f16x8 plain(int i, int s, int lane) const { return wide[i][s][lane]; }
+  AS_DEVICE i32x8 piece(int i, int p, int lane) const {
+    const u32x4 a = x[i][p][0][lane], b = x[i][p][1][lane];
+    return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+  }
   AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int G, int g, int row0, int tid) {
     const int width = a.H * HD;
-    for (int e = tid; e < TPW * 16 * (HD / 32); e += NW * 64) {
-      const int qi = e / (HD / 32), c = e % (HD / 32), lr = qi & 15;   // query, group of 32
-      f16x8 v[4] = {};
-      uint32_t top = 0;
+#pragma unroll
+    for (int e0 = 0; e0 < TPW * 16 * (HD / 8); e0 += NW * 64) {
+      const int e = e0 + tid;
+      if (TPW * 16 * (HD / 8) % (NW * 64) && e >= TPW * 16 * (HD / 8)) break;
+      const int qi = e / (HD / 8), piece = e % (HD / 8), lr = qi & 15, c = piece >> 2;   // c: group
+      f16x8 v = {};
       if (qbase + qi < QR) {
         const int r = (qbase + qi) / G, h = g * G + (qbase + qi - r * G);
-        const size_t off = (size_t)(row0 + r) * width + h * HD + c * 32;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) v[s] = load_q(a, T16(), off + s * 8);
+        v = load_q(a, T16(), (size_t)(row0 + r) * width + h * HD + piece * 8);
       }
+      wide[qi >> 4][piece % (HD / 32)][piece / (HD / 32) * 16 + lr] = v;
+      float f[8];
+      uint32_t top = 0;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {   // piece 4 c + s of 8 head dims
-        const int piece = 4 * c + s, lg = piece / (HD / 32);
-        wide[qi >> 4][piece % (HD / 32)][lg * 16 + lr] = v[s];
-      }
-      float f[32];
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        f[j] = (float)v[j >> 3][j & 7];
+      for (int j = 0; j < 8; ++j) {
+        f[j] = (float)v[j];
         top = max(top, abs_bits(f[j]));
       }
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1));   // four lanes a group
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2));
       // hi: the largest in [128, 256); what it leaves is at most 8, lo holds 16 times that
       const int ex = max((int)(top >> 23), 30) - 7;      // biased; fp16 queries are 2^-24 or 0
       const bool bad = top >= 0x7f800000u;               // NaN or inf: every score is NaN
-      const float down = __uint_as_float((uint32_t)(254 - ex) << 23);
-      uint32_t hi[8], lo[8];
+      const float down = bad ? 0.f : __uint_as_float((uint32_t)(254 - ex) << 23);
+      uint32_t hi[2], lo[2];
 #pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        float y[4];
+      for (int w = 0; w < 2; ++w) {
+        float y[4], d[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = bad ? 0.f : f[4 * w + j] * down;
         hi[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         hi[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi[w], true);
-        float d[4];
         d[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 0)) * 16.f;
         d[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 1)) * 16.f;
         d[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 2)) * 16.f;
@@ -217,69 +219,62 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
         lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(d[2], d[3], lo[w], true);
       }
       const uint32_t sh = bad ? 255u : (uint32_t)ex, sl = bad ? 255u : (uint32_t)(ex - 4);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {   // elements 16 h .. + 16 of the group
-        const u32x4 vh = {hi[4 * h], hi[4 * h + 1], hi[4 * h + 2], hi[4 * h + 3]};
-        const u32x4 vl = {lo[4 * h], lo[4 * h + 1], lo[4 * h + 2], lo[4 * h + 3]};
-        if (HD == 128) {
-          const int l = ((c & 1) * 2 + h) * 16 + lr;
-          x[qi >> 4][0][c >> 1][l] = vh;
-          x[qi >> 4][NP - 1][c >> 1][l] = vl;
-        } else {
-          x[qi >> 4][0][0][(c * 2 + h) * 16 + lr] = vh;
-          x[qi >> 4][0][1][(c * 2 + h) * 16 + lr] = vl;
-        }
-      }
+      const int half = piece >> 1 & 1, at = piece & 1;   // of the group's 32 bytes: which 8
       if (HD == 128) {
-        scale[qi >> 4][c * 16 + lr] = (uint16_t)(sh | (sl << 8));
+        const int l = ((c & 1) * 2 + half) * 16 + lr;
+        ((uint2 *)&x[qi >> 4][0][c >> 1][l])[at] = make_uint2(hi[0], hi[1]);
+        ((uint2 *)&x[qi >> 4][NP - 1][c >> 1][l])[at] = make_uint2(lo[0], lo[1]);
+        if ((piece & 3) == 0) scale[qi >> 4][c * 16 + lr] = (uint16_t)(sh | (sl << 8));
       } else {
-        scale[qi >> 4][c * 16 + lr] = (uint16_t)sh;
-        scale[qi >> 4][c * 16 + lr + 32] = (uint16_t)sl;
+        const int l = (c * 2 + half) * 16 + lr;
+        ((uint2 *)&x[qi >> 4][0][0][l])[at] = make_uint2(hi[0], hi[1]);
+        ((uint2 *)&x[qi >> 4][0][1][l])[at] = make_uint2(lo[0], lo[1]);
+        if ((piece & 3) == 0) {
+          scale[qi >> 4][c * 16 + lr] = (uint16_t)sh;
+          scale[qi >> 4][c * 16 + lr + 32] = (uint16_t)sl;
+        }
       }
     }
   }
   typedef bf16 T16;
 };
 
-// What a lane holds of a block's keys as operands of the scores.
-template <typename T, int HD> struct Keys {   // fp32 model: decoded
+// What a lane holds of a block's keys, and the scores of a tile against them.
+template <typename T, int HD> struct Keys {   // fp32 model
   u32x4 k[HD / 64];
   uint32_t ks;
+  struct Op { f32x8 f[2][HD / 32]; };          // decoded
   AS_DEVICE void load(const uint8_t *rec, int lane) {
     const int lr = lane & 15, lg = lane >> 4;
 #pragma unroll
     for (int h = 0; h < HD / 64; ++h) k[h] = *(const u32x4 *)(rec + h * 1024 + lane * 16);
     ks = *(const uint16_t *)(rec + 32 * HD + (lr * (HD / 32) + (HD == 128 ? lg : lg >> 1)) * 2);
   }
-  template <int TPW>
-  AS_DEVICE void score(const Queries<T, HD, TPW> &q, int lane, const uint32_t (&)[TPW], f32x4 (&sc)[TPW][2]) const {
-    f32x8 kf[2][HD / 32];
+  AS_DEVICE Op operand() const {
+    Op o;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int s = 0; s < HD / 32; ++s)
-        kf[kk][s] = q4_decode_f32(HD == 128 ? k[kk * (HD / 128)][s] : k[0][kk * 2 + s],
-                                  q4_scale((ks >> (8 * kk)) & 255u));
-    dot<TPW>(q, kf, lane, sc);
+        o.f[kk][s] = q4_decode_f32(HD == 128 ? k[kk * (HD / 128)][s] : k[0][kk * 2 + s],
+                                   q4_scale((ks >> (8 * kk)) & 255u));
+    return o;
   }
   template <int TPW>
-  static AS_DEVICE void dot(const Queries<T, HD, TPW> &q, const f32x8 (&kf)[2][HD / 32], int lane,
-                            f32x4 (&sc)[TPW][2]) {
+  static AS_DEVICE void score(const Op &o, const Queries<T, HD, TPW> &q, int i, int lane, f32x4 (&sc)[2]) {
+    sc[0] = sc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-      sc[i][0] = sc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < HD / 32; ++s) {
-        const f32x8 qf = *(const f32x8 *)q.x[i][s][lane];
-        sc[i][0] = Ops<T>::mma(kf[0][s], qf, sc[i][0]);
-        sc[i][1] = Ops<T>::mma(kf[1][s], qf, sc[i][1]);
-      }
+    for (int s = 0; s < HD / 32; ++s) {
+      const f32x8 qf = q.plain(i, s, lane);
+      sc[0] = Ops<T>::mma(o.f[0][s], qf, sc[0]);
+      sc[1] = Ops<T>::mma(o.f[1][s], qf, sc[1]);
     }
   }
 };
 template <int HD> struct Keys<bf16, HD> {     // bf16 model: as they are
   u32x4 k[2];
   uint32_t ks;
+  struct Op { i32x8 f[2]; int ks; };
   AS_DEVICE void load(const uint8_t *rec, int lane) {
     const int lr = lane & 15, lg = lane >> 4;
     if constexpr (HD == 128) {
@@ -292,32 +287,27 @@ template <int HD> struct Keys<bf16, HD> {     // bf16 model: as they are
       ks = *(const uint16_t *)(rec + 32 * HD + (lr * 2 + (lg & 1)) * 2);
     }
   }
-  template <int TPW>
-  AS_DEVICE void score(const Queries<bf16, HD, TPW> &q, int lane, const uint32_t (&qs)[TPW],
-                       f32x4 (&sc)[TPW][2]) const {
-    i32x8 kf[2] = {};
+  AS_DEVICE Op operand() const {
+    Op o = {};
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        kf[kk][j] = (int)(HD == 128 ? k[kk][j] : k[j >> 1][kk * 2 + (j & 1)]);
-#pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-      sc[i][0] = sc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int p = 0; p < HD / 64; ++p) {
-        const u32x4 b0 = q.x[i][p][0][lane], b1 = q.x[i][p][1][lane];
-        const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3],
-                         (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
-        // operand formats: 4 e2m1 (keys), 0 e4m3 (queries); scale byte kk and p
-        if (p == 0) {
-          sc[i][0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[0], b, sc[i][0], 4, 0, 0, (int)ks, 0, (int)qs[i]);
-          sc[i][1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[1], b, sc[i][1], 4, 0, 1, (int)ks, 0, (int)qs[i]);
-        } else {
-          sc[i][0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[0], b, sc[i][0], 4, 0, 0, (int)ks, 1, (int)qs[i]);
-          sc[i][1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf[1], b, sc[i][1], 4, 0, 1, (int)ks, 1, (int)qs[i]);
-        }
-      }
+      for (int j = 0; j < 4; ++j) o.f[kk][j] = (int)(HD == 128 ? k[kk][j] : k[j >> 1][kk * 2 + (j & 1)]);
+    o.ks = (int)ks;
+    return o;
+  }
+  template <int TPW>
+  static AS_DEVICE void score(const Op &o, const Queries<bf16, HD, TPW> &q, int i, int lane, f32x4 (&sc)[2]) {
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const int qs = q.scale[i][lane];
+    // operand formats: 4 e2m1 (keys), 0 e4m3 (queries); scale byte kk of ks, and the piece's
+    const i32x8 a = q.piece(i, 0, lane);
+    sc[0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[0], a, zero, 4, 0, 0, o.ks, 0, qs);
+    sc[1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[1], a, zero, 4, 0, 1, o.ks, 0, qs);
+    if constexpr (HD == 128) {
+      const i32x8 b = q.piece(i, 1, lane);
+      sc[0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[0], b, sc[0], 4, 0, 0, o.ks, 1, qs);
+      sc[1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[1], b, sc[1], 4, 0, 1, o.ks, 1, qs);
     }
   }
 };
@@ -350,6 +340,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   typedef typename O::F8 F8;
   typedef typename O::E E;
   typedef typename O::Raw Raw;
+  typedef Keys<T, HD> K;
   constexpr int NB = HD / 16, LD = HD / 4, OWN = NB / NW;   // OWN: value operands a wave joins
   Shared<T, HD, TPW> &sm = reinterpret_cast<Shared<T, HD, TPW> &>(smem_);
   const int b = item / a.Hkv, g = item - b * a.Hkv;
@@ -410,55 +401,47 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
       vt[nb] = O::raw(tv + (size_t)(nb * 16 + lr) * a.tcap + s0 + lg * 8);
   }
 
+  RowView mine = {};
+  if (tid < TPW * 16) {
+    const int r = min(qbase + tid, QR - 1) / G, p = a.pos[row0 + r];
+    mine.lo = a.window ? max(p - a.window + 1, 0) : 0;
+    mine.root = !a.window || p - P < a.window || P < a.sinks;
+    mine.anc = a.anc[row0 + r];
+  }
   sm.q.fill(a, qbase, QR, G, g, row0, tid);
-  for (int e = tid; e < TPW * 16; e += NW * 64) {
-    const int r = min(qbase + e, QR - 1) / G, p = a.pos[row0 + r];
-    sm.view[e].lo = a.window ? max(p - a.window + 1, 0) : 0;
-    sm.view[e].root = !a.window || p - P < a.window || P < a.sinks;
-    sm.view[e].anc = a.anc[row0 + r];
-  }
+  if (tid < TPW * 16) sm.view[tid] = mine;
   __syncthreads();
-  uint32_t qs[TPW];   // scale bytes of the queries' pieces
-#pragma unroll
-  for (int i = 0; i < TPW; ++i) {
-    if constexpr (sizeof(T) == 2) qs[i] = sm.q.scale[i][lane];
-    else qs[i] = 0;
-  }
 
-  const float sscale = LOG2E / sqrtf((float)HD), lazy = LAZY_LOG2 / sscale;
-  float m_run[TPW], mb[TPW], l_run[TPW];   // reference, the same as an exponent (0 if none), sum
+  const float sscale = LOG2E / sqrtf((float)HD);   // scores -> exponents of 2
+  float mb[TPW], l_run[TPW];   // reference as an exponent (-inf: none yet), sum of weights
   f32x4 o[TPW][NB];
-  // Moves the references that a score exceeds by too much.
-  auto refer = [&](const f32x4 (&sc)[TPW][2]) {
+  // Moves the reference of tile i where one of the scores exceeds it by too much; returns it, or
+  // 0 where there is none.
+  auto refer = [&](int i, const f32x4 (&sc)[2]) -> float {
+    float mx = sc[0][0];
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-      float mx = sc[i][0][0];
+    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j >> 2][j & 3]);
+    mx *= sscale;
+    if (__ballot(mx > mb[i] + LAZY_LOG2)) {
+      mx = rows4_max(mx);
+      const float mn = mx > mb[i] + LAZY_LOG2 ? mx : mb[i];
+      const float alpha = __builtin_amdgcn_exp2f(mb[i] - (mn == -INFINITY ? 0.f : mn));
+      mb[i] = mn;
+      l_run[i] *= alpha;
 #pragma unroll
-      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[i][j >> 2][j & 3]);
-      if (__ballot(mx > m_run[i] + lazy)) {
-        mx = rows4_max(mx);
-        const float mn = mx > m_run[i] + lazy ? mx : m_run[i];
-        const float alpha = __builtin_amdgcn_exp2f((m_run[i] - (mn == -INFINITY ? 0.f : mn)) * sscale);
-        m_run[i] = mn;
-        mb[i] = mn == -INFINITY ? 0.f : mn * sscale;
-        l_run[i] *= alpha;
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[i][nb][e] *= alpha;
-      }
+        for (int e = 0; e < 4; ++e) o[i][nb][e] *= alpha;
     }
+    return mb[i] == -INFINITY ? 0.f : mb[i];
   };
-  // The weights of tile i, in place of its scores; their sum in the lane.
-  auto weights = [&](int i, f32x4 (&sc)[TPW][2]) -> float {
+  // The weights of a tile's scores against reference m, as operands of the values; adds their
+  // sum in the lane.
+  auto weights = [&](f32x4 (&sc)[2], float m, float &sum) -> F8 {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      sc[i][j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(sc[i][j >> 2][j & 3], sscale, -mb[i]));
-    const f32x4 h = f32x4{sc[i][0][0] + sc[i][1][0], sc[i][0][1] + sc[i][1][1],
-                          sc[i][0][2] + sc[i][1][2], sc[i][0][3] + sc[i][1][3]};
-    return (h[0] + h[1]) + (h[2] + h[3]);
-  };
-  auto operand = [&](const f32x4 (&sc)[2]) -> F8 {
+      sc[j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(sc[j >> 2][j & 3], sscale, -m));
+    sum = ((sc[0][0] + sc[1][0]) + (sc[0][1] + sc[1][1])) + ((sc[0][2] + sc[1][2]) + (sc[0][3] + sc[1][3]));
     F8 p;
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] = (E)sc[j >> 2][j & 3];
@@ -484,28 +467,22 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   };
   if (early) {   // nothing is summed yet
     const int s0 = (m0 + wave) * Q4_SLOTS, tr0 = s0 - t + lg * 8;
-    F8 p[TPW];
-    f32x4 sc[TPW][2];
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int s = 0; s < HD / 32; ++s) {
-        const F8 kf = O::wide(kt[kk][s]);
-#pragma unroll
-        for (int i = 0; i < TPW; ++i)
-          sc[i][kk] = O::mma(kf, sm.q.plain(i, s, lane), s ? sc[i][kk] : zero);
-      }
+    F8 p[TPW];
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
-      mask(i, tr0, full * Q4_SLOTS + s0 + lg * 8, sc[i]);
-      float mx = sc[i][0][0];
+      f32x4 sc[2];
 #pragma unroll
-      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[i][j >> 2][j & 3]);
-      m_run[i] = rows4_max(mx);
-      mb[i] = m_run[i] == -INFINITY ? 0.f : m_run[i] * sscale;
-      l_run[i] = weights(i, sc);
-      p[i] = operand(sc[i]);
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int s = 0; s < HD / 32; ++s)
+          sc[kk] = O::mma(O::wide(kt[kk][s]), sm.q.plain(i, s, lane), s ? sc[kk] : zero);
+      mask(i, tr0, full * Q4_SLOTS + s0 + lg * 8, sc);
+      float mx = sc[0][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j >> 2][j & 3]);
+      mb[i] = rows4_max(mx) * sscale;
+      p[i] = weights(sc, mb[i] == -INFINITY ? 0.f : mb[i], l_run[i]);
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -516,8 +493,8 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   } else {
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
-      m_run[i] = -INFINITY;
-      mb[i] = l_run[i] = 0.f;
+      mb[i] = -INFINITY;
+      l_run[i] = 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) o[i][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -529,36 +506,27 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
     const int tr0 = tail ? s0 - t + lg * 8 : -Q4_SLOTS;
     const int pos0 = (tail ? full * Q4_SLOTS + s0 : blk * Q4_SLOTS) + lg * 8;
     const uint8_t *rec = rec0 + (size_t)(tail ? 0 : blk) * q4_bytes(HD);
-    f32x4 sc[TPW][2];
-    if (tail) {
-#pragma unroll
-      for (int i = 0; i < TPW; ++i) sc[i][0] = sc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-#pragma unroll
-        for (int s = 0; s < HD / 32; ++s) {
-          const F8 kf = O::wide(O::raw(tk + (size_t)(s0 + q4_key(kk, lr)) * HD + lg * LD + s * 8));
-#pragma unroll
-          for (int i = 0; i < TPW; ++i) sc[i][kk] = O::mma(kf, sm.q.plain(i, s, lane), sc[i][kk]);
-        }
-        SCHED_FENCE();
-      }
-    } else {
-      Keys<T, HD> kc;
-      kc.load(rec, lane);
-      kc.score(sm.q, lane, qs, sc);
-    }
-#pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-      mask(i, tr0, pos0, sc[i]);
-      SCHED_FENCE();
-    }
-    refer(sc);
     F8 p[TPW];
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
-      l_run[i] += weights(i, sc);
-      p[i] = operand(sc[i]);
+      f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+      if (tail) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int s = 0; s < HD / 32; ++s)
+            sc[kk] = O::mma(O::wide(O::raw(tk + (size_t)(s0 + q4_key(kk, lr)) * HD + lg * LD + s * 8)),
+                            sm.q.plain(i, s, lane), sc[kk]);
+      } else {
+        K kc;
+        kc.load(rec, lane);
+        K::score(kc.operand(), sm.q, i, lane, sc);
+      }
+      mask(i, tr0, pos0, sc);
+      float sum;
+      p[i] = weights(sc, refer(i, sc), sum);
+      l_run[i] += sum;
+      SCHED_FENCE();
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -578,10 +546,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   // its values once they are multiplied: a wave's loads cross the other half of its work.
   // A lane does not look for its largest score: a reference that is too low (or, before the
   // first, -inf) shows in the sum of the weights, and the scores are then computed again.
-#pragma unroll
-  for (int i = 0; i < TPW; ++i)
-    if (m_run[i] == -INFINITY) mb[i] = -INFINITY;
-  Keys<T, HD> key;
+  K key;
   Values<HD> val;
   if (c < w1) {
     key.load(record(c), lane);
@@ -589,28 +554,29 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   }
   while (c < w1) {
     c = whole_of_round(++round);
-    f32x4 sc[TPW][2];
+    F8 p[TPW];
     float add[TPW];
     bool over = false;
-    key.score(sm.q, lane, qs, sc);
+    const typename K::Op kop = key.operand();
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
-      add[i] = weights(i, sc);
+      f32x4 sc[2];
+      K::score(kop, sm.q, i, lane, sc);
+      p[i] = weights(sc, mb[i], add[i]);
       over |= add[i] > LAZY_SUM;
     }
     if (__ballot(over)) {
-      key.score(sm.q, lane, qs, sc);
-      refer(sc);
 #pragma unroll
-      for (int i = 0; i < TPW; ++i) add[i] = weights(i, sc);
+      for (int i = 0; i < TPW; ++i) {
+        f32x4 sc[2];
+        K::score(kop, sm.q, i, lane, sc);
+        p[i] = weights(sc, refer(i, sc), add[i]);
+        SCHED_FENCE();
+      }
     }
     key.load(record(c), lane);
-    F8 p[TPW];
 #pragma unroll
-    for (int i = 0; i < TPW; ++i) {
-      l_run[i] += add[i];
-      p[i] = operand(sc[i]);
-    }
+    for (int i = 0; i < TPW; ++i) l_run[i] += add[i];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const F8 vf = O::decode(val.v[nb >> 2][nb & 3], val.scale(nb));
@@ -626,7 +592,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   for (int i = 0; i < TPW; ++i) {
     const float l = rows4_sum(l_run[i]);
     if (lg == 0)
-      sm.ml[wave][i * 16 + lr] = make_float2(m_run[i] == -INFINITY ? -INFINITY : m_run[i] * sscale, l);
+      sm.ml[wave][i * 16 + lr] = make_float2(mb[i], l);
   }
   const bool any_bad = __syncthreads_or(bad);   // (and the queries are read)
   float top[TPW], sum[TPW];
@@ -724,7 +690,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
 // Waves a SIMD holds, by the registers of the accumulators (hd 128: 32 a tile) and of the fp32
 // model's decoded keys.
 template <typename T> constexpr int waves_per_simd(int tpw) {
-  return sizeof(T) == 4 ? 2 : tpw == 1 ? 4 : tpw == 2 ? 3 : 2;
+  return sizeof(T) == 4 ? 2 : tpw == 1 ? 4 : 3;
 }
 
 // A workgroup: TPW tiles of a session's kv head (or TPW - 1: the tiles are dealt evenly to nqg
@@ -776,9 +742,7 @@ __global__ __launch_bounds__(256) void quant_combine_kernel(QuantAttnArgs a, int
 
 template <typename T, int HD>
 void launch_tiles(int tpw, unsigned grid, hipStream_t s, const QuantAttnArgs &a) {
-  auto kernel = tpw == 1 ? quant_attn_kernel<T, HD, 1> : quant_attn_kernel<T, HD, 2>;
-  if constexpr (sizeof(T) == 2)
-    if (tpw == 3) kernel = quant_attn_kernel<T, HD, 3>;
+  const auto kernel = tpw == 1 ? quant_attn_kernel<T, HD, 1> : quant_attn_kernel<T, HD, 2>;
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(NW * 64), 0, s, a);
 }
 
@@ -793,22 +757,25 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
                                   int capacity, int tcap, int window, int sinks, int rows_io,
                                   int cus, hipStream_t s) {
   const int QR = H / Hkv * n1, tiles = (QR + 15) / 16, items = B * Hkv;
-  // Tiles a workgroup: more of them share a block's decoding and its read, fewer make more
-  // workgroups.
-  constexpr int MAXT = sizeof(T) == 2 ? 3 : 2;
-  const long long work = (long long)items * tiles;
-  const int most = work <= 2LL * cus ? 1 : work <= 4LL * cus ? 2 : MAXT;
-  const int nqg = (tiles + most - 1) / most, tpw = (tiles + nqg - 1) / nqg;
-  // Splits, where a CU would have less than two workgroups: as many as it holds at once (three
-  // rounds of the large ones, which leave less idle at the end), of at least 8 blocks a wave.
   const long long seen = window ? (long long)window + n1 + sinks + 2 * Q4_SLOTS : capacity;
   const int blocks_seen = (int)((seen < capacity ? seen : capacity) / Q4_SLOTS) + 3;
+  // Splits of at least 8 blocks a wave, which pays for their joining.
+  const long long splits = blocks_seen > 8 * NW ? blocks_seen / (8 * NW) : 1;
+  // Tiles a workgroup: two share a block's decoding and its read (70b fan-out: 85 us against 106),
+  // one gives twice the workgroups, for few rows over a short prefix (one session: 15 against 19).
+  // Three were slower than two at head dim 128 (90 against 85) and mixed at 64 (36 against 33 with 5
+  // tiles, 57 against 64 with 17).
+  const long long work = (long long)items * tiles;
+  const int most = work <= 2LL * cus && work * splits <= 4LL * cus ? 1 : 2;
+  const int nqg = (tiles + most - 1) / most, tpw = (tiles + nqg - 1) / nqg;
+  // Splits, where a CU would have less than two workgroups: as many as it holds at once.  A prefix
+  // of 96 blocks a wave or more is read in four parts also by up to three workgroups a CU: small
+  // ones end closer together (16384 slots, 576 workgroups: 169 us against 179).
   const long long groups = (long long)items * nqg;
   long long nsplit = 1;
-  if (groups < 2LL * cus) {
-    nsplit = (tpw == 1 ? 4LL : tpw == 2 ? 3LL : 6LL) * cus / groups;
-    nsplit = nsplit < blocks_seen / (8 * NW) ? nsplit : blocks_seen / (8 * NW);
-  }
+  if (groups < 2LL * cus) nsplit = (tpw == 1 ? 4LL : 3LL) * cus / groups;
+  if (groups < 3LL * cus && nsplit < 4 && blocks_seen / NW >= 96) nsplit = 4;
+  nsplit = nsplit < splits ? nsplit : splits;
   if (nsplit < 1) nsplit = 1;
   while (nsplit > 1 && (long long)items * nsplit * QR * hd > part_capacity) --nsplit;
   const QuantAttnArgs a{q, blocks, tk, tv, meta.pos, meta.anc, out, part_o, part_ml, B, n1, H, Hkv,
