@@ -217,8 +217,8 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
     if (kv.quant)
       RUN(K_ATTN, launch_attention_quant<T>(
                       x_q, (const uint8_t *)kv.quant->blocks + l * quant_layer_bytes(d, kv.quant, B),
-                      ck, cv, meta, x_attn, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv,
-                      hd, kv.quant->capacity, cap, kv.span.window, kv.span.sinks, 0, ctx->cus,
+                      ck, cv, meta, nullptr, nullptr, nullptr, x_attn, ctx->part_o, ctx->part_ml,
+                      ctx->part_cap, B, n1, H, Hkv, hd, kv.quant->capacity, cap, kv.span.window, kv.span.sinks, 0, ctx->cus,
                       stream));
     else
       RUN(K_ATTN, launch_attention<T>(x_q, ck, cv, meta, x_attn, ctx->part_o, ctx->part_ml,
@@ -755,19 +755,17 @@ int acespec_attention_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, int la
   const int n1 = N + 1, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
   const size_t io = (size_t)B * n1 * H * hd * ctx->esz;
   if (overlap(q, io, out, io)) return fail(ACESPEC_EINVAL, "q and out overlap");
-  RUN(K_TREE, launch_tree_prep_quant(nullptr, parent_idx, qc->prefix_len, B, n1, 1, qc->capacity,
-                                     sp.window, sp.sinks, ctx->meta, status, stream));
   const uint8_t *blocks = (const uint8_t *)qc->blocks + layer * quant_layer_bytes(d, qc, B);
   const size_t tail = (size_t)layer * B * Hkv * qc->tail_capacity * hd;
   if (d.dtype == ACESPEC_BF16)
     RUN(K_ATTN, launch_attention_quant<bf16>(
                     q, blocks, (const bf16 *)qc->tail_k + tail, (const bf16 *)qc->tail_v + tail,
-                    ctx->meta, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
+                    TreeMeta{}, parent_idx, qc->prefix_len, status, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
                     qc->capacity, qc->tail_capacity, sp.window, sp.sinks, 1, ctx->cus, stream));
   else
     RUN(K_ATTN, launch_attention_quant<float>(
                     q, blocks, (const float *)qc->tail_k + tail, (const float *)qc->tail_v + tail,
-                    ctx->meta, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
+                    TreeMeta{}, parent_idx, qc->prefix_len, status, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
                     qc->capacity, qc->tail_capacity, sp.window, sp.sinks, 1, ctx->cus, stream));
   return ACESPEC_OK;
 }

@@ -79,8 +79,12 @@ struct QuantAttnArgs {
   const void *q;            // [rows][H hd]: T (rows_io) or the activation type
   const uint8_t *blocks;    // records of the layer
   const void *tk, *tv;      // tail of the layer
+  // The trees: prepared as pos and anc, or else as the caller's parents [rows] and lengths [B],
+  // and status [B] to write.
   const int32_t *pos;       // [rows] P + depth
   const uint64_t *anc;      // [rows] visible drafted rows (bit j - 1)
+  const int32_t *parents, *prefix;
+  int32_t *status;
   void *out;
   float *part_o, *part_ml;
   int B, n1, H, Hkv, nblk, tcap, nsplit, nqg, window, sinks;
@@ -103,6 +107,31 @@ AS_DEVICE uint32_t visible(const RowView &w, int sinks, int tr0, int pos0) {
   if (tr0 >= 1) tree = tr0 <= 64 ? (uint32_t)(w.anc >> (tr0 - 1)) : 0u;
   else tree = tr0 > -8 ? (((uint32_t)w.anc << 1) | (uint32_t)w.root) << -tr0 : 0u;
   return (prefix | tree) & 255u;
+}
+
+// The drafted rows of a session's tree from the caller's parents, in one wave: lane j holds row
+// j + 1, `parent` its parent and rows n1 - 1.  Each row's ancestors are folded in by pointer
+// jumping over shuffles; a malformed tree (`ok` false) becomes a chain.
+struct TreeRow {
+  uint64_t anc;   // visible drafted rows
+  int depth;
+};
+AS_DEVICE TreeRow tree_row(const QuantAttnArgs &a, int lane, int P, int parent, bool ok) {
+  const bool in = lane + 1 < a.n1;
+  int jump = !in ? 0 : ok ? parent : lane;   // the next ancestor's row, 0 (the root): none
+  uint64_t anc = in ? 1ull << lane : 0ull;
+  for (int span = 1; span < a.n1; span *= 2) {
+    const uint64_t up = __shfl((unsigned long long)anc, max(jump - 1, 0));
+    const int next = __shfl(jump, max(jump - 1, 0));
+    if (jump) anc |= up, jump = next;
+  }
+  const int depth = __popcll(anc);
+  if (a.window && __any(depth >= a.window))   // ancestors too far back
+    for (int j = 0; j + 1 < a.n1; ++j) {
+      const int dj = __shfl(depth, j);
+      if (depth - dj >= a.window && P + dj >= a.sinks) anc &= ~(1ull << j);
+    }
+  return {anc, depth};
 }
 
 // Eight consecutive elements of a query row, and four of an output row.
@@ -348,7 +377,11 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lg = lane >> 4;
   const int row0 = b * a.n1, width = a.H * HD;
-  const int P = a.pos[row0], t = P & (Q4_SLOTS - 1), full = P / Q4_SLOTS;
+  const bool own = a.parents != nullptr;
+  const int given = own ? a.prefix[b] : a.pos[row0], most = a.nblk * Q4_SLOTS + Q4_SLOTS - 1;
+  const int parent = own && wave == 0 && lane + 1 < a.n1 ? a.parents[row0 + lane + 1] : 0;
+  const int root = own ? a.parents[row0] : -1;
+  const int P = min(max(given, 0), most), t = P & (Q4_SLOTS - 1), full = P / Q4_SLOTS;
 
   // Complete blocks that some row sees: [0, nsink) and [wlo, full).  Those that every row sees
   // whole are [0, send) and [wend, full); a window cuts [send, nsink) and [wlo, wend).
@@ -402,11 +435,22 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   }
 
   RowView mine = {};
-  if (tid < TPW * 16) {
-    const int r = min(qbase + tid, QR - 1) / G, p = a.pos[row0 + r];
-    mine.lo = a.window ? max(p - a.window + 1, 0) : 0;
-    mine.root = !a.window || p - P < a.window || P < a.sinks;
-    mine.anc = a.anc[row0 + r];
+  if (wave == 0) {
+    const int r = min(qbase + min(lane, TPW * 16 - 1), QR - 1) / G;
+    int depth;
+    if (own) {
+      const bool ok = __all(parent >= 0 && parent <= lane) && root == -1 && given == P;
+      const TreeRow row = tree_row(a, lane, P, parent, ok);
+      mine.anc = __shfl((unsigned long long)row.anc, max(r - 1, 0));
+      depth = __shfl(row.depth, max(r - 1, 0));
+      if (r == 0) mine.anc = depth = 0;
+      if (lane == 0 && qbase == 0 && split == 0 && g == 0) a.status[b] = ok ? ACESPEC_OK : ACESPEC_EBADTREE;
+    } else {
+      mine.anc = a.anc[row0 + r];
+      depth = a.pos[row0 + r] - P;
+    }
+    mine.lo = a.window ? max(P + depth - a.window + 1, 0) : 0;
+    mine.root = !a.window || depth < a.window || P < a.sinks;
   }
   sm.q.fill(a, qbase, QR, G, g, row0, tid);
   if (tid < TPW * 16) sm.view[tid] = mine;
@@ -752,8 +796,9 @@ namespace acespec {
 
 template <typename T>
 hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T *tk, const T *tv,
-                                  const TreeMeta &meta, void *out, float *part_o, float *part_ml,
-                                  long long part_capacity, int B, int n1, int H, int Hkv, int hd,
+                                  const TreeMeta &meta, const int32_t *parents,
+                                  const int32_t *prefix, int32_t *status, void *out, float *part_o,
+                                  float *part_ml, long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                                   int capacity, int tcap, int window, int sinks, int rows_io,
                                   int cus, hipStream_t s) {
   const int QR = H / Hkv * n1, tiles = (QR + 15) / 16, items = B * Hkv;
@@ -778,7 +823,7 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
   nsplit = nsplit < splits ? nsplit : splits;
   if (nsplit < 1) nsplit = 1;
   while (nsplit > 1 && (long long)items * nsplit * QR * hd > part_capacity) --nsplit;
-  const QuantAttnArgs a{q, blocks, tk, tv, meta.pos, meta.anc, out, part_o, part_ml, B, n1, H, Hkv,
+  const QuantAttnArgs a{q, blocks, tk, tv, meta.pos, meta.anc, parents, prefix, status, out, part_o, part_ml, B, n1, H, Hkv,
                         capacity / Q4_SLOTS, tcap, (int)nsplit, nqg, window, sinks, rows_io};
   const unsigned grid = (unsigned)(groups * nsplit);
   if (hd == 128) launch_tiles<T, 128>(tpw, grid, s, a);
@@ -791,12 +836,14 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
 }
 
 template hipError_t launch_attention_quant<float>(const void *, const uint8_t *, const float *,
-                                                  const float *, const TreeMeta &, void *, float *,
-                                                  float *, long long, int, int, int, int, int, int,
+                                                  const float *, const TreeMeta &, const int32_t *,
+                                                  const int32_t *, int32_t *, void *, float *, float *,
+                                                  long long, int, int, int, int, int, int,
                                                   int, int, int, int, int, hipStream_t);
 template hipError_t launch_attention_quant<bf16>(const void *, const uint8_t *, const bf16 *,
-                                                 const bf16 *, const TreeMeta &, void *, float *,
-                                                 float *, long long, int, int, int, int, int, int,
+                                                 const bf16 *, const TreeMeta &, const int32_t *,
+                                                 const int32_t *, int32_t *, void *, float *, float *,
+                                                 long long, int, int, int, int, int, int,
                                                  int, int, int, int, int, hipStream_t);
 
 }  // namespace acespec

@@ -210,7 +210,6 @@ hipError_t launch_tree_prep(const int32_t *tokens, const int32_t *parents,
                             TreeMeta meta, int32_t *status, hipStream_t s);
 // The same for a cache in 4 bits of `capacity` block slots: sess_S is the tail's length
 // (prefix_len % 32, where the tree's rows go), and anc holds only what the window shows.
-// tokens may be NULL (meta.tok is then not written).
 hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
                                   const int32_t *prefix_len, int B, int n1, int V, int capacity,
                                   int window, int sinks, TreeMeta meta, int32_t *status,
@@ -314,11 +313,13 @@ hipError_t launch_attention(const typename ActOf<TW>::type *q, const TW *cache_k
 
 // One layer's tree attention over the cache in 4 bits: blocks [B][Hkv][capacity / 32] records,
 // the tail tk [B][Hkv][tcap][hd] and tv [B][Hkv][hd][tcap].  window (0: none) and sinks as in
-// acespec_attn_span.  rows_io: q and out are row-major [rows][H hd] in TW; else as in
-// launch_attention.
+// acespec_attn_span.  The trees come as meta, or with parents given as these [rows] and the
+// prefix lengths [B], checked and prepared by the kernel itself, which writes status [B].
+// rows_io: q and out are row-major [rows][H hd] in TW; else as in launch_attention.
 template <typename TW>
 hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const TW *tk,
-                                  const TW *tv, const TreeMeta &meta, void *out, float *part_o,
+                                  const TW *tv, const TreeMeta &meta, const int32_t *parents,
+                                  const int32_t *prefix, int32_t *status, void *out, float *part_o,
                                   float *part_ml, long long part_capacity, int B, int n1, int H,
                                   int Hkv, int hd, int capacity, int tcap, int window, int sinks,
                                   int rows_io, int cus, hipStream_t s);

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(TP_THREADS) void tree_prep_kernel(
   const size_t base = (size_t)b * n1;
   const bool in = r < n1;
   const int pr = in ? parents[base + r] : 0;
-  const int tk = in && (!QUANT || tokens) ? tokens[base + r] : 0;
+  const int tk = in ? tokens[base + r] : 0;
   int S = prefix_len[b];
   const bool row_ok = !in || (((r == 0) ? (pr == -1) : (pr >= 0 && pr < r)) && tk >= 0 && tk < V);
   // largest prefix: with QUANT full blocks and a full tail behind them
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(TP_THREADS) void tree_prep_kernel(
       const int j = __builtin_ctzll(rest) + 1, dj = __popcll(s_anc[j]);
       if (depth - dj >= window && S + dj >= sinks) anc &= ~(1ull << (j - 1));
     }
-  if (!QUANT || tokens) meta.tok[base + r] = tk < 0 ? 0 : (tk >= V ? V - 1 : tk);
+  meta.tok[base + r] = tk < 0 ? 0 : (tk >= V ? V - 1 : tk);
   meta.par[base + r] = p;
   meta.depth[base + r] = depth;
   meta.anc[base + r] = anc;
