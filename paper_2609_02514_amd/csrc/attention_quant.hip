@@ -268,15 +268,19 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
   typedef bf16 T16;
 };
 
+// 16 bytes of a record's codes; ONCE: past the caches, as no other workgroup reads them.
+template <bool ONCE> AS_DEVICE u32x4 codes(const uint8_t *p) {
+  return ONCE ? __builtin_nontemporal_load((const u32x4 *)p) : *(const u32x4 *)p;
+}
 // What a lane holds of a block's keys, and the scores of a tile against them.
 template <typename T, int HD> struct Keys {   // fp32 model
   u32x4 k[HD / 64];
   uint32_t ks;
   struct Op { f32x8 f[2][HD / 32]; };          // decoded
-  AS_DEVICE void load(const uint8_t *rec, int lane) {
+  template <bool ONCE> AS_DEVICE void load(const uint8_t *rec, int lane) {
     const int lr = lane & 15, lg = lane >> 4;
 #pragma unroll
-    for (int h = 0; h < HD / 64; ++h) k[h] = *(const u32x4 *)(rec + h * 1024 + lane * 16);
+    for (int h = 0; h < HD / 64; ++h) k[h] = codes<ONCE>(rec + h * 1024 + lane * 16);
     ks = *(const uint16_t *)(rec + 32 * HD + (lr * (HD / 32) + (HD == 128 ? lg : lg >> 1)) * 2);
   }
   AS_DEVICE Op operand() const {
@@ -304,15 +308,15 @@ template <int HD> struct Keys<bf16, HD> {     // bf16 model: as they are
   u32x4 k[2];
   uint32_t ks;
   struct Op { i32x8 f[2]; int ks; };
-  AS_DEVICE void load(const uint8_t *rec, int lane) {
+  template <bool ONCE> AS_DEVICE void load(const uint8_t *rec, int lane) {
     const int lr = lane & 15, lg = lane >> 4;
     if constexpr (HD == 128) {
-      k[0] = *(const u32x4 *)(rec + lane * 16);
-      k[1] = *(const u32x4 *)(rec + 1024 + lane * 16);
+      k[0] = codes<ONCE>(rec + lane * 16);
+      k[1] = codes<ONCE>(rec + 1024 + lane * 16);
       ks = *(const uint16_t *)(rec + 32 * HD + (lr * 4 + lg) * 2);
     } else {   // both 16-dim halves of group lg % 2, each with both operands' keys
-      k[0] = *(const u32x4 *)(rec + ((lg & 1) * 32 + lr) * 16);
-      k[1] = *(const u32x4 *)(rec + ((lg & 1) * 32 + 16 + lr) * 16);
+      k[0] = codes<ONCE>(rec + ((lg & 1) * 32 + lr) * 16);
+      k[1] = codes<ONCE>(rec + ((lg & 1) * 32 + 16 + lr) * 16);
       ks = *(const uint16_t *)(rec + 32 * HD + (lr * 2 + (lg & 1)) * 2);
     }
   }
@@ -344,10 +348,10 @@ template <int HD> struct Keys<bf16, HD> {     // bf16 model: as they are
 template <int HD> struct Values {
   u32x4 v[HD / 64];
   uint32_t vs[HD / 64];   // byte nb % 4 of word nb / 4
-  AS_DEVICE void load(const uint8_t *rec, int lane) {
+  template <bool ONCE> AS_DEVICE void load(const uint8_t *rec, int lane) {
 #pragma unroll
     for (int h = 0; h < HD / 64; ++h) {
-      v[h] = *(const u32x4 *)(rec + 16 * HD + h * 1024 + lane * 16);
+      v[h] = codes<ONCE>(rec + 16 * HD + h * 1024 + lane * 16);
       vs[h] = *(const uint32_t *)(rec + 33 * HD + (lane & 15) * (HD / 16) + h * 4);
     }
   }
@@ -363,7 +367,7 @@ template <typename T, int HD, int TPW> struct Shared {
   float2 ml[NW][TPW * 16];
 };
 
-template <typename T, int HD, int TPW, int LDST>
+template <typename T, int HD, int TPW, int LDST, bool ONCE>
 AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int item, int split, int qbase) {
   typedef Ops<T> O;
   typedef typename O::F8 F8;
@@ -434,6 +438,8 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
       vt[nb] = O::raw(tv + (size_t)(nb * 16 + lr) * a.tcap + s0 + lg * 8);
   }
 
+  K key;
+  if (c < w1) key.template load<ONCE>(record(c), lane);
   RowView mine = {};
   if (wave == 0) {
     const int r = min(qbase + min(lane, TPW * 16 - 1), QR - 1) / G;
@@ -563,7 +569,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
                             sm.q.plain(i, s, lane), sc[kk]);
       } else {
         K kc;
-        kc.load(rec, lane);
+        kc.template load<ONCE>(rec, lane);
         K::score(kc.operand(), sm.q, i, lane, sc);
       }
       mask(i, tr0, pos0, sc);
@@ -590,12 +596,8 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   // its values once they are multiplied: a wave's loads cross the other half of its work.
   // A lane does not look for its largest score: a reference that is too low (or, before the
   // first, -inf) shows in the sum of the weights, and the scores are then computed again.
-  K key;
   Values<HD> val;
-  if (c < w1) {
-    key.load(record(c), lane);
-    val.load(record(c), lane);
-  }
+  if (c < w1) val.template load<ONCE>(record(c), lane);
   while (c < w1) {
     c = whole_of_round(++round);
     F8 p[TPW];
@@ -618,7 +620,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
         SCHED_FENCE();
       }
     }
-    key.load(record(c), lane);
+    key.template load<ONCE>(record(c), lane);
 #pragma unroll
     for (int i = 0; i < TPW; ++i) l_run[i] += add[i];
 #pragma unroll
@@ -627,7 +629,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
 #pragma unroll
       for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], o[i][nb]);
     }
-    val.load(record(c), lane);
+    val.template load<ONCE>(record(c), lane);
   }
 
   // Join the waves: o[i][nb][e] is head dim 16 nb + 4 lg + e of query 16 i + lr.  Wave w joins
@@ -739,7 +741,7 @@ template <typename T> constexpr int waves_per_simd(int tpw) {
 
 // A workgroup: TPW tiles of a session's kv head (or TPW - 1: the tiles are dealt evenly to nqg
 // groups) over one of nsplit shares of its blocks.
-template <typename T, int HD, int TPW>
+template <typename T, int HD, int TPW, bool ONCE>
 __global__ __launch_bounds__(NW * 64, waves_per_simd<T>(TPW)) void quant_attn_kernel(QuantAttnArgs a) {
   __shared__ __attribute__((aligned(16))) Shared<T, HD, TPW> sm;
   // The query groups and the splits of a session's kv head follow each other on one XCD: the
@@ -748,8 +750,8 @@ __global__ __launch_bounds__(NW * 64, waves_per_simd<T>(TPW)) void quant_attn_ke
   const int grp = id % a.nqg, split = id / a.nqg % a.nsplit, item = id / (a.nqg * a.nsplit);
   const int tiles = (a.H / a.Hkv * a.n1 + 15) / 16, each = tiles / a.nqg, more = tiles % a.nqg;
   const int qbase = (grp * each + min(grp, more)) * 16;
-  if (TPW == 1 || each + (grp < more) == TPW) attend<T, HD, TPW, TPW>(a, sm, item, split, qbase);
-  else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW>(a, sm, item, split, qbase);
+  if (TPW == 1 || each + (grp < more) == TPW) attend<T, HD, TPW, TPW, ONCE>(a, sm, item, split, qbase);
+  else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW, ONCE>(a, sm, item, split, qbase);
 }
 
 // Joins the splits: one thread per 4 head dims of a query row.
@@ -785,8 +787,10 @@ __global__ __launch_bounds__(256) void quant_combine_kernel(QuantAttnArgs a, int
 }
 
 template <typename T, int HD>
-void launch_tiles(int tpw, unsigned grid, hipStream_t s, const QuantAttnArgs &a) {
-  const auto kernel = tpw == 1 ? quant_attn_kernel<T, HD, 1> : quant_attn_kernel<T, HD, 2>;
+void launch_tiles(int tpw, bool once, unsigned grid, hipStream_t s, const QuantAttnArgs &a) {
+  const auto kernel = once       ? quant_attn_kernel<T, HD, 1, true>
+                      : tpw == 1 ? quant_attn_kernel<T, HD, 1, false>
+                                 : quant_attn_kernel<T, HD, 2, false>;
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(NW * 64), 0, s, a);
 }
 
@@ -826,8 +830,12 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
   const QuantAttnArgs a{q, blocks, tk, tv, meta.pos, meta.anc, parents, prefix, status, out, part_o, part_ml, B, n1, H, Hkv,
                         capacity / Q4_SLOTS, tcap, (int)nsplit, nqg, window, sinks, rows_io};
   const unsigned grid = (unsigned)(groups * nsplit);
-  if (hd == 128) launch_tiles<T, 128>(tpw, grid, s, a);
-  else launch_tiles<T, 64>(tpw, grid, s, a);
+  // One tile a session (a token, as in plain decoding), and more records than the L2s' 32 MB:
+  // they pass the caches (64 sessions x 2048 slots, 143 MB: 29.6 us against 31.8; 26 MB, which a
+  // repeated call finds in the L2: 13.9 against 12.4).
+  const bool once = tiles == 1 && items * (seen < capacity ? seen : capacity) / Q4_SLOTS * q4_bytes(hd) > (32 << 20);
+  if (hd == 128) launch_tiles<T, 128>(tpw, once, grid, s, a);
+  else launch_tiles<T, 64>(tpw, once, grid, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || nsplit == 1) return e;
   hipLaunchKernelGGL(quant_combine_kernel<T>, dim3((QR * (hd / 4) + 255) / 256, items), dim3(256), 0,

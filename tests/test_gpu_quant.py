@@ -182,10 +182,11 @@ def bound(dtype, out, mag, big, hd):
     return b + 1e-30
 
 
-def check_attention(dtype, hd, H, Hkv, lens, N, window, sinks, seed, layer=0, L=1, poison=None):
+def check_attention(dtype, hd, H, Hkv, lens, N, window, sinks, seed, layer=0, L=1, poison=None,
+                    least=64):
     r = random.Random(seed)
     B, n1 = len(lens), N + 1
-    cap = max(64, (max(lens) + 63) // 64 * 64)
+    cap = max(least, (max(lens) + 63) // 64 * 64)
     ver, cache = make(L, B, H, Hkv, hd, dtype, N, cap)
     k, v = random_cache(L, B, Hkv, cap, hd, dtype, seed, spread=0.5)
     kv = fill(ver, cache, k, v, lens, n1, seed + 1)
@@ -221,6 +222,18 @@ def check_attention(dtype, hd, H, Hkv, lens, N, window, sinks, seed, layer=0, L=
     (4, 4, [130, 63], 8), (14, 2, [257], 33), (16, 2, [64, 31], 64), (6, 2, [1000, 3], 5)])
 def test_attention_against_64_bits(dtype, hd, H, Hkv, lens, N):
     check_attention(dtype, hd, H, Hkv, lens, N, 0, 0, seed=H * 100 + N + hd)
+
+
+@pytest.mark.parametrize("dtype, hd, window", [("bf16", 128, 0), ("f32", 64, 0), ("bf16", 64, 70000),
+                                               ("f32", 128, 70000)])
+def test_one_token_over_more_records_than_the_caches_hold(dtype, hd, window):
+    """Above 32 MB a single tile's records are read past the caches; in splits too."""
+    check_attention(dtype, hd, 4, 2, [123000, 45], 0, window, 4, seed=hd, least=123392)
+
+
+def test_a_long_prefix_under_wide_trees():
+    """Enough groups of rows to fill the chip, over a prefix long enough to be split all the same."""
+    check_attention("bf16", 64, 32, 8, [12350, 5, 40], 64, 0, 0, seed=64)
 
 
 @pytest.mark.parametrize("dtype, hd", [("bf16", 128), ("f32", 64), ("bf16", 64)])
@@ -585,3 +598,11 @@ def test_a_captured_step_replays_as_it_ran():
         step(other, outs2, torch.roll(batch.tokens, 1 + i, 1))
         torch.cuda.synchronize()
     ver.close()
+
+
+def test_the_stream_handle_is_the_current_streams():
+    from paper_2609_02514_amd import acespec as A
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        assert A.Verifier._stream() == side.cuda_stream
+    assert A.Verifier._stream() == torch.cuda.current_stream().cuda_stream
