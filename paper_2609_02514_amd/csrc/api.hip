@@ -505,6 +505,9 @@ int check_quant(const acespec_model_desc &d, const acespec_kv_quant *qc, int B, 
     return fail(ACESPEC_EINVAL,
                 "tail_capacity must be a multiple of 64 that holds 31 slots and the %d tree rows "
                 "(got %d)", n1, qc->tail_capacity);
+  const size_t planes = (size_t)d.n_layers * B * d.n_kv_heads;
+  if (planes > 0x7fffff)   // of two workgroups of 256 threads, in a launch of less than 2^32
+    return fail(ACESPEC_EUNSUPPORTED, "%zu planes (layer, session, kv head) exceed one launch", planes);
   return ACESPEC_OK;
 }
 
@@ -755,18 +758,27 @@ int acespec_attention_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, int la
   const int n1 = N + 1, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
   const size_t io = (size_t)B * n1 * H * hd * ctx->esz;
   if (overlap(q, io, out, io)) return fail(ACESPEC_EINVAL, "q and out overlap");
+  const size_t tails = (size_t)d.n_layers * B * Hkv * qc->tail_capacity * hd * ctx->esz;
+  if (overlap(out, io, qc->blocks, d.n_layers * quant_layer_bytes(d, qc, B)) ||
+      overlap(out, io, qc->tail_k, tails) || overlap(out, io, qc->tail_v, tails))
+    return fail(ACESPEC_EINVAL, "out and the quantized cache overlap");
+  const size_t each = (size_t)B * sizeof(int32_t);   // (read by workgroups while one writes status)
+  if (overlap(status, each, qc->prefix_len, each) || overlap(status, each, parent_idx, each * n1))
+    return fail(ACESPEC_EINVAL, "status overlaps prefix_len or parent_idx");
   const uint8_t *blocks = (const uint8_t *)qc->blocks + layer * quant_layer_bytes(d, qc, B);
   const size_t tail = (size_t)layer * B * Hkv * qc->tail_capacity * hd;
   if (d.dtype == ACESPEC_BF16)
     RUN(K_ATTN, launch_attention_quant<bf16>(
                     q, blocks, (const bf16 *)qc->tail_k + tail, (const bf16 *)qc->tail_v + tail,
-                    TreeMeta{}, parent_idx, qc->prefix_len, status, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
-                    qc->capacity, qc->tail_capacity, sp.window, sp.sinks, 1, ctx->cus, stream));
+                    TreeMeta{}, parent_idx, qc->prefix_len, status, out, ctx->part_o, ctx->part_ml,
+                    ctx->part_cap, B, n1, H, Hkv, hd, qc->capacity, qc->tail_capacity, sp.window,
+                    sp.sinks, 1, ctx->cus, stream));
   else
     RUN(K_ATTN, launch_attention_quant<float>(
                     q, blocks, (const float *)qc->tail_k + tail, (const float *)qc->tail_v + tail,
-                    TreeMeta{}, parent_idx, qc->prefix_len, status, out, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
-                    qc->capacity, qc->tail_capacity, sp.window, sp.sinks, 1, ctx->cus, stream));
+                    TreeMeta{}, parent_idx, qc->prefix_len, status, out, ctx->part_o, ctx->part_ml,
+                    ctx->part_cap, B, n1, H, Hkv, hd, qc->capacity, qc->tail_capacity, sp.window,
+                    sp.sinks, 1, ctx->cus, stream));
   return ACESPEC_OK;
 }
 
@@ -777,7 +789,7 @@ namespace {
 // The arguments that acespec_quantize_kv and acespec_dequantize_kv share; prefix_len is the
 // source's.
 int check_convert(const acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
-                  const int32_t *prefix_len, int B) {
+                  const int32_t *prefix_len, const int32_t *first, const int32_t *status, int B) {
   if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
   const acespec_model_desc &d = ctx->d;
   if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
@@ -794,7 +806,6 @@ int check_convert(const acespec_ctx *ctx, const acespec_kv_cache *kv, const aces
   rc = check_quant(d, qc ? &c : nullptr, B, 0);
   if (rc) return rc;
   const size_t planes = (size_t)d.n_layers * B * d.n_kv_heads;
-  if (planes > 0x7fff0000u) return fail(ACESPEC_EINVAL, "%zu planes exceed one launch", planes);
   const size_t eb = d.dtype == ACESPEC_BF16 ? 2 : 4, n = planes * d.head_dim * eb;
   const void *held[3] = {qc->blocks, qc->tail_k, qc->tail_v};
   const size_t sizes[3] = {planes * (qc->capacity / kBlock) * 34 * d.head_dim,
@@ -803,6 +814,9 @@ int check_convert(const acespec_ctx *ctx, const acespec_kv_cache *kv, const aces
     if (overlap(kv->k, n * kv->capacity, held[i], sizes[i]) ||
         overlap(kv->v, n * kv->capacity, held[i], sizes[i]))
       return fail(ACESPEC_EINVAL, "the cache and the quantized cache overlap");
+  const size_t each = (size_t)B * sizeof(int32_t);   // (read by workgroups while one writes status)
+  if (status && (overlap(status, each, prefix_len, each) || (first && overlap(status, each, first, each))))
+    return fail(ACESPEC_EINVAL, "status overlaps prefix_len or first");
   return ACESPEC_OK;
 }
 
@@ -813,7 +827,7 @@ extern "C" {
 int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
                         const int32_t *first, int B, int32_t *status, hipStream_t stream) {
   g_err.clear();
-  const int rc = check_convert(ctx, kv, qc, kv ? kv->prefix_len : nullptr, B);
+  const int rc = check_convert(ctx, kv, qc, kv ? kv->prefix_len : nullptr, first, status, B);
   if (rc) return rc;
   const acespec_model_desc &d = ctx->d;
   if (d.dtype == ACESPEC_BF16)
@@ -834,7 +848,7 @@ int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const aces
 int acespec_dequantize_kv(acespec_ctx *ctx, const acespec_kv_quant *qc, const acespec_kv_cache *kv,
                           const int32_t *first, int B, int32_t *status, hipStream_t stream) {
   g_err.clear();
-  const int rc = check_convert(ctx, kv, qc, qc ? qc->prefix_len : nullptr, B);
+  const int rc = check_convert(ctx, kv, qc, qc ? qc->prefix_len : nullptr, first, status, B);
   if (rc) return rc;
   const acespec_model_desc &d = ctx->d;
   if (d.dtype == ACESPEC_BF16)
@@ -869,6 +883,10 @@ int acespec_commit_kv_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, const 
     return fail(ACESPEC_EINVAL,
                 "new_prefix_len overlaps prefix_len: give it its own buffer and copy it over "
                 "after the call");
+  if (overlap(path, (size_t)B * (N + 1) * 4, new_prefix_len, (size_t)B * 4) ||
+      overlap(path_len, (size_t)B * 4, new_prefix_len, (size_t)B * 4) ||
+      (status && overlap(status, (size_t)B * 4, new_prefix_len, (size_t)B * 4)))
+    return fail(ACESPEC_EINVAL, "new_prefix_len overlaps path, path_len or status");
   if (d.dtype == ACESPEC_BF16)
     RUN(K_COMMIT, launch_commit_quant<bf16>((uint8_t *)qc->blocks, (bf16 *)qc->tail_k,
                                             (bf16 *)qc->tail_v, qc->prefix_len, path, path_len, status,

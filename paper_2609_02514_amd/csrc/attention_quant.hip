@@ -41,7 +41,6 @@ constexpr float LAZY_LOG2 = 8.f;
 constexpr float LAZY_SUM = 8 * 256.f;   // of 8 weights none of which exceeds 2^LAZY_LOG2
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int NW = 4;     // waves of a workgroup
-constexpr int JOIN = 2;   // tiles joined at a time
 constexpr int SLOW = 3;   // what a masked block costs a wave, in blocks that every row sees whole
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -361,7 +360,7 @@ template <int HD> struct Values {
 template <typename T, int HD, int TPW> struct Shared {
   union {
     Queries<T, HD, TPW> q;
-    f32x4 part[TPW < JOIN ? TPW : JOIN][NW][(HD / 16) * (NW - 1) / NW][64];   // accumulators other waves join
+    f32x4 part[TPW][NW][(HD / 16) * (NW - 1) / NW][64];   // accumulators other waves join
   };
   RowView view[TPW * 16];
   float2 ml[NW][TPW * 16];
@@ -595,7 +594,8 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   // Whole blocks.  The next block's keys are asked for once the scores have read this one's,
   // its values once they are multiplied: a wave's loads cross the other half of its work.
   // A lane does not look for its largest score: a reference that is too low (or, before the
-  // first, -inf) shows in the sum of the weights, and the scores are then computed again.
+  // first, -inf) shows in the sum of the weights (inf, or NaN where a score is -inf itself), and
+  // the scores are then computed again.
   Values<HD> val;
   if (c < w1) val.template load<ONCE>(record(c), lane);
   while (c < w1) {
@@ -609,7 +609,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
       f32x4 sc[2];
       K::score(kop, sm.q, i, lane, sc);
       p[i] = weights(sc, mb[i], add[i]);
-      over |= add[i] > LAZY_SUM;
+      over |= !(add[i] <= LAZY_SUM);
     }
     if (__ballot(over)) {
 #pragma unroll
@@ -666,7 +666,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
     const int qi = qbase + i * 16 + lr;
 #pragma unroll
     for (int w = 0; w < NW - 1; ++w) {
-      const f32x4 v = sm.part[i % JOIN][wave][w * OWN + nb % OWN][lane];
+      const f32x4 v = sm.part[i][wave][w * OWN + nb % OWN][lane];
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] += v[e];
     }
@@ -685,21 +685,17 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
     }
   };
 #pragma unroll
-  for (int i = 0; i < TPW; ++i) {
+  for (int i = 0; i < TPW; ++i)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
       if (nb / OWN != wave)
-        sm.part[i % JOIN][nb / OWN][(wave - (wave > nb / OWN)) * OWN + nb % OWN][lane] = o[i][nb];
-    if (i % JOIN == JOIN - 1 || i + 1 == TPW) {
-      __syncthreads();
+        sm.part[i][nb / OWN][(wave - (wave > nb / OWN)) * OWN + nb % OWN][lane] = o[i][nb];
+  __syncthreads();
 #pragma unroll
-      for (int j = i / JOIN * JOIN; j <= i; ++j)
+  for (int i = 0; i < TPW; ++i)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          if (nb / OWN == wave) finish(j, nb, o[j][nb]);
-      if (i + 1 < TPW) __syncthreads();
-    }
-  }
+    for (int nb = 0; nb < NB; ++nb)
+      if (nb / OWN == wave) finish(i, nb, o[i][nb]);
   if (!any_bad) return;
   // Values that are not finite, in the masked blocks of this split (rare): added to the rows
   // that see their slots, and to no others.

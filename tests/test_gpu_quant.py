@@ -145,8 +145,8 @@ def test_what_was_appended_and_sessions_that_do_not_fit(dtype, hd):
 # --------------------------------------------------------------------------------------
 
 
-def random_parents(r, n):
-    return [-1] + [r.randint(max(0, i - 7), i - 1) for i in range(1, n + 1)]
+def random_parents(r, n, reach=7):
+    return [-1] + [r.randint(max(0, i - reach), i - 1) for i in range(1, n + 1)]
 
 
 def fill(ver, cache, k, v, lens, n1, seed):
@@ -183,7 +183,7 @@ def bound(dtype, out, mag, big, hd):
 
 
 def check_attention(dtype, hd, H, Hkv, lens, N, window, sinks, seed, layer=0, L=1, poison=None,
-                    least=64):
+                    least=64, reach=7):
     r = random.Random(seed)
     B, n1 = len(lens), N + 1
     cap = max(least, (max(lens) + 63) // 64 * 64)
@@ -191,7 +191,7 @@ def check_attention(dtype, hd, H, Hkv, lens, N, window, sinks, seed, layer=0, L=
     k, v = random_cache(L, B, Hkv, cap, hd, dtype, seed, spread=0.5)
     kv = fill(ver, cache, k, v, lens, n1, seed + 1)
     cache = cache.with_prefix(i32(lens))
-    parents = [random_parents(r, N) for _ in range(B)]
+    parents = [random_parents(r, N, reach) for _ in range(B)]
     g = torch.Generator().manual_seed(seed + 2)
     q = torch.randn(B, n1, H, hd, generator=g).to(DT[dtype]).cuda()
     if poison:
@@ -229,6 +229,13 @@ def test_attention_against_64_bits(dtype, hd, H, Hkv, lens, N):
 def test_one_token_over_more_records_than_the_caches_hold(dtype, hd, window):
     """Above 32 MB a single tile's records are read past the caches; in splits too."""
     check_attention(dtype, hd, 4, 2, [123000, 45], 0, window, 4, seed=hd, least=123392)
+
+
+@pytest.mark.parametrize("reach", [1, 2, 64])
+@pytest.mark.parametrize("window, sinks", [(0, 0), (7, 0), (40, 70), (63, 2), (65, 1)])
+def test_the_deepest_and_the_widest_trees_under_windows(reach, window, sinks):
+    """A chain of 64 (reach 1), a tree nearly as deep, and a wide one."""
+    check_attention("bf16", 64, 4, 1, [0, 69, 96, 31], 64, window, sinks, seed=reach + window, reach=reach)
 
 
 def test_a_long_prefix_under_wide_trees():
@@ -598,6 +605,25 @@ def test_a_captured_step_replays_as_it_ran():
         step(other, outs2, torch.roll(batch.tokens, 1 + i, 1))
         torch.cuda.synchronize()
     ver.close()
+
+
+def test_scores_below_fp32s_range():
+    """Keys of the largest magnitude against queries of 1e35: fp32 holds -inf, so the row sees
+    itself alone, whose weight is a power of two's rounding from 1 and cancels (three roundings)."""
+    P, hd = 320, 64
+    ver, cache = make(1, 1, 1, 1, hd, "f32", 0, P)
+    k = torch.full((1, 1, 1, P, hd), -57000.0, device="cuda")
+    v = torch.ones(1, 1, 1, hd, P, device="cuda")
+    ver.quantize_kv(k, v, P, i32([P]), cache)
+    cache.tail_k.zero_()
+    cache.tail_k[..., 0, :] = 1e-30
+    own = torch.linspace(-3, 5, hd, device="cuda")
+    cache.tail_v[..., 0] = own
+    q, out, status = torch.full((1, 1, 1, hd), 1e35, device="cuda"), torch.empty(1, 1, 1, hd, device="cuda"), i32([9])
+    ver.attention_quant(cache.with_prefix(i32([P])), 0, q, i32([[-1]]), out, status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0]
+    assert bool(((out.flatten() - own).abs() <= own.abs() * 2.0 ** -22).all())
 
 
 def test_the_stream_handle_is_the_current_streams():

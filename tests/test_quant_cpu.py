@@ -179,3 +179,35 @@ def test_a_cache_of_another_device_or_model_is_refused_by_the_binding(monkeypatc
     ver._check_quant(c, 3)
     with pytest.raises(ValueError, match="is not this model's"):
         ver._check_quant(c, 2)
+
+
+def test_arrays_that_one_workgroup_writes_while_others_read():
+    lib, ctx, qc = A.load(), Ctx(), quant()
+    far, prefix = P + (7 << 32), P + (3 << 32)
+    size = 2 * 4 * 2 * 4 * 34 * 128      # the records of two layers
+
+    def attention(status=far, parents=far + 64, out=P + (9 << 32)):
+        return lib.acespec_attention_quant(ctx.ptr, C.byref(qc), 0, None, P + (8 << 32), parents, 4, 16,
+                                           out, status, None)
+
+    for status in (prefix, prefix + 12, prefix - 12, far + 64, far + 64 + 4 * 17 * 4 - 4):
+        refused(attention(status=status), "status overlaps")
+    for out in (P, P + size - 16, P + (1 << 32), P + (2 << 32) + 256):
+        refused(attention(out=out), "out and the quantized cache")
+    kv = cache()
+    for status, first in ((P + (6 << 32), None), (far + 8, far)):
+        refused(lib.acespec_quantize_kv(ctx.ptr, C.byref(kv), C.byref(qc), first, 4, status, None),
+                "status overlaps")
+    for status, first in ((prefix + 4, None), (far + 8, far)):
+        refused(lib.acespec_dequantize_kv(ctx.ptr, C.byref(qc), C.byref(kv), first, 4, status, None),
+                "status overlaps")
+    for path, path_len, status in ((far, P, None), (far - 4 * 17 * 4 + 4, P, None), (P, far + 12, None),
+                                   (P, P, far - 12)):
+        refused(lib.acespec_commit_kv_quant(ctx.ptr, C.byref(qc), path, path_len, status, 4, 16, far,
+                                            None), "path, path_len or status")
+
+
+def test_more_planes_than_a_launch_takes():
+    for name, rc in calls(A.load(), Ctx(L=2 ** 20, Hkv=2).ptr, quant(), cache()):
+        if name != "verify":             # (its layers' weights are looked at first)
+            refused(rc, "exceed one launch", A.ACESPEC_EUNSUPPORTED)
