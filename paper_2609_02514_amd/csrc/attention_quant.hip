@@ -169,6 +169,37 @@ AS_DEVICE void store_out(const QuantAttnArgs &a, float, int row, int col, int wi
 
 AS_DEVICE bool not_finite(f16 v) { return (__builtin_bit_cast(uint16_t, v) & 0x7c00) == 0x7c00; }
 AS_DEVICE bool not_finite(float v) { return abs_bits(v) >= 0x7f800000u; }
+template <typename F8> AS_DEVICE F8 finite(F8 v) {   // 0 for what is not
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = not_finite(v[j]) ? 0.f : v[j];
+  return v;
+}
+// Whether one is not, for many at once: an exponent of ones carries into the sign's place.
+AS_DEVICE uint32_t carries(f16x8 v) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  uint32_t t = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t |= (w[i] & 0x7c007c00u) + 0x04000400u;
+  return t & 0x80008000u;
+}
+AS_DEVICE uint32_t carries(f32x8 v) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) t |= (__float_as_uint(v[j]) & 0x7f800000u) + 0x00800000u;
+  return t & 0x80000000u;
+}
+// The first n of eight (none, or all, where n is below or above that), 0 for the others.
+AS_DEVICE f16x8 first_of(f16x8 v, int n) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] &= n >= 2 * i + 2 ? ~0u : n > 2 * i ? 0xffffu : 0u;
+  return __builtin_bit_cast(f16x8, w);
+}
+AS_DEVICE f32x8 first_of(f32x8 v, int n) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;
+  return v;
+}
 
 // The queries of a workgroup's tiles as operands of the scores, in LDS.
 //
@@ -505,15 +536,6 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
 #pragma unroll
     for (int j = 0; j < 8; ++j) sc[j >> 2][j & 3] = (vis >> j) & 1u ? sc[j >> 2][j & 3] : -INFINITY;
   };
-  auto clean = [&](F8 vf, int tr0) -> F8 {   // slots behind the last row were never written
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool nf = not_finite(vf[j]), there = tr0 + j < a.n1;
-      bad |= nf && there;
-      vf[j] = nf || !there ? (E)0.f : vf[j];
-    }
-    return vf;
-  };
   if (early) {   // nothing is summed yet
     const int s0 = (m0 + wave) * Q4_SLOTS, tr0 = s0 - t + lg * 8;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -533,12 +555,22 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
       mb[i] = rows4_max(mx) * sscale;
       p[i] = weights(sc, mb[i] == -INFINITY ? 0.f : mb[i], l_run[i]);
     }
+    F8 vf[NB];
+    uint32_t nf = 0;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const F8 vf = clean(O::wide(vt[nb]), tr0);
-#pragma unroll
-      for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], zero);
+      vf[nb] = first_of(O::wide(vt[nb]), a.n1 - tr0);   // slots behind the last row were never written
+      nf |= carries(vf[nb]);
     }
+    if (__ballot(nf)) {
+      bad = true;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) vf[nb] = finite(vf[nb]);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf[nb], p[i], zero);
   } else {
 #pragma unroll
     for (int i = 0; i < TPW; ++i) {
@@ -585,7 +617,11 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
       else
         vf = O::decode(*(const uint32_t *)(rec + 16 * HD + (nb >> 2) * 1024 + lane * 16 + (nb & 3) * 4),
                        q4_scale(rec[33 * HD + lr * NB + nb]));
-      vf = clean(vf, tr0);
+      vf = first_of(vf, a.n1 - tr0);
+      if (__ballot(carries(vf))) {
+        bad = true;
+        vf = finite(vf);
+      }
 #pragma unroll
       for (int i = 0; i < TPW; ++i) o[i][nb] = O::mma(vf, p[i], o[i][nb]);
       if (nb % 2) SCHED_FENCE();
