@@ -74,6 +74,14 @@ template <> struct Ops<float> {
   }
 };
 
+// n / d by one multiplication, for 0 <= n and (n + 1) d <= 2^32: a workgroup's own indices cost
+// a chain of eight divisions otherwise (some 250 scalar instructions before its first load).
+struct Div {
+  uint32_t m;
+  explicit Div(int d) : m(0xffffffffu / (uint32_t)d) {}
+  AS_DEVICE int operator()(int n) const { return (int)__umulhi((uint32_t)n + 1u, m); }
+};
+
 struct QuantAttnArgs {
   const void *q;            // [rows][H hd]: T (rows_io) or the activation type
   const uint8_t *blocks;    // records of the layer
@@ -86,7 +94,9 @@ struct QuantAttnArgs {
   int32_t *status;
   void *out;
   float *part_o, *part_ml;
-  int B, n1, H, Hkv, nblk, tcap, nsplit, nqg, window, sinks;
+  int rows, n1, H, Hkv, G, nblk, tcap, nsplit, nqg, each, more, window, sinks;   // G = H / Hkv; a
+                            // group has each tiles, the first `more` of them one more
+  Div by_nqg, by_nsplit, by_Hkv, by_G;
   int rows_io;              // 1: q and out are row-major in T; 0: q row-major and out in the
                             // activation layout, fp16 (bf16 model; fp32: the same as 1)
 };
@@ -148,7 +158,7 @@ AS_DEVICE void store_out(const QuantAttnArgs &a, bf16, int row, int col, int wid
     *(bf16x4 *)((bf16 *)a.out + (size_t)row * width + col) =
         bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
   else
-    *(f16x4 *)((f16 *)a.out + act_off(row, col, a.B * a.n1, width)) =
+    *(f16x4 *)((f16 *)a.out + act_off(row, col, a.rows, width)) =
         f16x4{(f16)v[0], (f16)v[1], (f16)v[2], (f16)v[3]};
 }
 AS_DEVICE void add_out(const QuantAttnArgs &a, bf16, int row, int col, int width, float v) {
@@ -156,7 +166,7 @@ AS_DEVICE void add_out(const QuantAttnArgs &a, bf16, int row, int col, int width
     bf16 *p = (bf16 *)a.out + (size_t)row * width + col;
     *p = (bf16)((float)*p + v);
   } else {
-    f16 *p = (f16 *)a.out + act_off(row, col, a.B * a.n1, width);
+    f16 *p = (f16 *)a.out + act_off(row, col, a.rows, width);
     *p = (f16)((float)*p + v);
   }
 }
@@ -207,13 +217,13 @@ AS_DEVICE f32x8 first_of(f32x8 v, int n) {
 template <typename T, int HD, int TPW> struct Queries {
   float x[TPW][HD / 32][64][8];
   AS_DEVICE f32x8 plain(int i, int s, int lane) const { return *(const f32x8 *)x[i][s][lane]; }
-  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int G, int g, int row0, int tid) {
+  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
     const int width = a.H * HD;
     for (int e = tid; e < TPW * 16 * (HD / 8); e += NW * 64) {
       const int qi = e / (HD / 8), c = e % (HD / 8);     // query of the group, piece of 8 head dims
       f32x8 v{};
       if (qbase + qi < QR) {
-        const int r = (qbase + qi) / G, h = g * G + (qbase + qi - r * G);
+        const int r = a.by_G(qbase + qi), h = g * a.G + (qbase + qi - r * a.G);
         v = load_q(a, T(), (size_t)(row0 + r) * width + h * HD + c * 8);
       }
       *(f32x8 *)x[qi >> 4][c % (HD / 32)][c / (HD / 32) * 16 + (qi & 15)] = v;
@@ -236,7 +246,7 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
     const u32x4 a = x[i][p][0][lane], b = x[i][p][1][lane];
     return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
   }
-  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int G, int g, int row0, int tid) {
+  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
     const int width = a.H * HD;
 #pragma unroll
     for (int e0 = 0; e0 < TPW * 16 * (HD / 8); e0 += NW * 64) {
@@ -245,7 +255,7 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
       const int qi = e / (HD / 8), piece = e % (HD / 8), lr = qi & 15, c = piece >> 2;   // c: group
       f16x8 v = {};
       if (qbase + qi < QR) {
-        const int r = (qbase + qi) / G, h = g * G + (qbase + qi - r * G);
+        const int r = a.by_G(qbase + qi), h = g * a.G + (qbase + qi - r * a.G);
         v = load_q(a, T16(), (size_t)(row0 + r) * width + h * HD + piece * 8);
       }
       wide[qi >> 4][piece % (HD / 32)][piece / (HD / 32) * 16 + lr] = v;
@@ -406,8 +416,8 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   typedef Keys<T, HD> K;
   constexpr int NB = HD / 16, LD = HD / 4, OWN = NB / NW;   // OWN: value operands a wave joins
   Shared<T, HD, TPW> &sm = reinterpret_cast<Shared<T, HD, TPW> &>(smem_);
-  const int b = item / a.Hkv, g = item - b * a.Hkv;
-  const int G = a.H / a.Hkv, QR = G * a.n1;
+  const int b = a.by_Hkv(item), g = item - b * a.Hkv;
+  const int G = a.G, QR = G * a.n1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lg = lane >> 4;
   const int row0 = b * a.n1, width = a.H * HD;
@@ -431,7 +441,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   // counts as SLOW whole ones in the shares of the splits and of the waves.
   const int ntail = (t + a.n1 + Q4_SLOTS - 1) / Q4_SLOTS;
   const int nmask = ntail + nsink - send + wend - wlo, nwhole = send + full - wend;
-  const int per = (nmask * SLOW + nwhole + a.nsplit - 1) / a.nsplit;
+  const int per = a.by_nsplit(nmask * SLOW + nwhole + a.nsplit - 1);
   const int u0 = split * per, u1 = u0 + per;
   const int m0 = min((u0 + SLOW - 1) / SLOW, nmask), m1 = min((u1 + SLOW - 1) / SLOW, nmask);
   const int w0 = min(max(u0 - nmask * SLOW, 0), nwhole), w1 = min(max(u1 - nmask * SLOW, 0), nwhole);
@@ -472,7 +482,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
   if (c < w1) key.template load<ONCE>(record(c), lane);
   RowView mine = {};
   if (wave == 0) {
-    const int r = min(qbase + min(lane, TPW * 16 - 1), QR - 1) / G;
+    const int r = a.by_G(min(qbase + min(lane, TPW * 16 - 1), QR - 1));
     int depth;
     if (own) {
       const bool ok = __all(parent >= 0 && parent <= lane) && root == -1 && given == P;
@@ -488,7 +498,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
     mine.lo = a.window ? max(P + depth - a.window + 1, 0) : 0;
     mine.root = !a.window || depth < a.window || P < a.sinks;
   }
-  sm.q.fill(a, qbase, QR, G, g, row0, tid);
+  sm.q.fill(a, qbase, QR, g, row0, tid);
   if (tid < TPW * 16) sm.view[tid] = mine;
   __syncthreads();
 
@@ -707,7 +717,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
       for (int e = 0; e < 4; ++e) acc[e] += v[e];
     }
     if (qi < QR) {
-      const int r = qi / G, h = g * G + (qi - r * G);
+      const int r = a.by_G(qi), h = g * G + (qi - r * G);
       if (a.nsplit == 1) {
         const float inv = 1.f / sum[i];                  // every row sees itself
 #pragma unroll
@@ -759,7 +769,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
       }
     }
     if (v == 0.f) continue;
-    const int r = qi / G, h = g * G + (qi - r * G);
+    const int r = a.by_G(qi), h = g * G + (qi - r * G);
     if (a.nsplit == 1) add_out(a, T(), row0 + r, h * HD + d, width, v);
     else a.part_o[(((size_t)item * a.nsplit + split) * QR + qi) * HD + d] += v;
   }
@@ -779,18 +789,18 @@ __global__ __launch_bounds__(NW * 64, waves_per_simd<T>(TPW)) void quant_attn_ke
   // The query groups and the splits of a session's kv head follow each other on one XCD: the
   // groups read the same records.
   const int id = xcd_tile(blockIdx.x, gridDim.x);
-  const int grp = id % a.nqg, split = id / a.nqg % a.nsplit, item = id / (a.nqg * a.nsplit);
-  const int tiles = (a.H / a.Hkv * a.n1 + 15) / 16, each = tiles / a.nqg, more = tiles % a.nqg;
-  const int qbase = (grp * each + min(grp, more)) * 16;
-  if (TPW == 1 || each + (grp < more) == TPW) attend<T, HD, TPW, TPW, ONCE>(a, sm, item, split, qbase);
+  const int pair = a.by_nqg(id), grp = id - pair * a.nqg;
+  const int item = a.by_nsplit(pair), split = pair - item * a.nsplit;
+  const int qbase = (grp * a.each + min(grp, a.more)) * 16;
+  if (TPW == 1 || a.each + (grp < a.more) == TPW) attend<T, HD, TPW, TPW, ONCE>(a, sm, item, split, qbase);
   else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW, ONCE>(a, sm, item, split, qbase);
 }
 
 // Joins the splits: one thread per 4 head dims of a query row.
 template <typename T>
 __global__ __launch_bounds__(256) void quant_combine_kernel(QuantAttnArgs a, int HD) {
-  const int item = blockIdx.y, b = item / a.Hkv, g = item - b * a.Hkv;
-  const int G = a.H / a.Hkv, QR = G * a.n1, hd4 = HD >> 2;
+  const int item = blockIdx.y, b = a.by_Hkv(item), g = item - b * a.Hkv;
+  const int G = a.G, QR = G * a.n1, hd4 = HD >> 2;
   const int idx = blockIdx.x * 256 + threadIdx.x;
   if (idx >= QR * hd4) return;
   const int qi = idx / hd4, d = (idx - qi * hd4) * 4;
@@ -814,7 +824,7 @@ __global__ __launch_bounds__(256) void quant_combine_kernel(QuantAttnArgs a, int
   const float inv = 1.f / den;
 #pragma unroll
   for (int j = 0; j < 4; ++j) num[j] *= inv;
-  const int r = qi / G, h = g * G + (qi - r * G);
+  const int r = a.by_G(qi), h = g * G + (qi - r * G);
   store_out(a, T(), b * a.n1 + r, h * HD + d, a.H * HD, num);
 }
 
@@ -859,8 +869,15 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
   nsplit = nsplit < splits ? nsplit : splits;
   if (nsplit < 1) nsplit = 1;
   while (nsplit > 1 && (long long)items * nsplit * QR * hd > part_capacity) --nsplit;
-  const QuantAttnArgs a{q, blocks, tk, tv, meta.pos, meta.anc, parents, prefix, status, out, part_o, part_ml, B, n1, H, Hkv,
-                        capacity / Q4_SLOTS, tcap, (int)nsplit, nqg, window, sinks, rows_io};
+  const int G = H / Hkv, nblk = capacity / Q4_SLOTS;
+  // (what Div divides; only a long cache can bring a number of splits to the limit)
+  while (nsplit > 1 && (nblk + 128 + nsplit) * nsplit > 0x80000000LL) --nsplit;
+  if ((groups * nsplit + 1) * nqg > 0xffffffffLL || (items + 1LL) * Hkv > 0xffffffffLL ||
+      (QR + 33LL) * G > 0xffffffffLL)
+    return hipErrorInvalidValue;
+  const QuantAttnArgs a{q, blocks, tk, tv, meta.pos, meta.anc, parents, prefix, status, out, part_o, part_ml,
+                        B * n1, n1, H, Hkv, G, nblk, tcap, (int)nsplit, nqg, tiles / nqg, tiles % nqg, window,
+                        sinks, Div(nqg), Div((int)nsplit), Div(Hkv), Div(G), rows_io};
   const unsigned grid = (unsigned)(groups * nsplit);
   // One tile a session (a token, as in plain decoding), and more records than the L2s' 32 MB:
   // they pass the caches (64 sessions x 2048 slots, 143 MB: 29.6 us against 31.8; 26 MB, which a
