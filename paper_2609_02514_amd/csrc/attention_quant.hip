@@ -40,7 +40,6 @@ namespace {
 constexpr float LAZY_LOG2 = 8.f;
 constexpr float LAZY_SUM = 8 * 256.f;   // of 8 weights none of which exceeds 2^LAZY_LOG2
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int NW = 4;     // waves of a workgroup
 constexpr int SLOW = 3;   // what a masked block costs a wave, in blocks that every row sees whole
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -217,9 +216,9 @@ AS_DEVICE f32x8 first_of(f32x8 v, int n) {
 template <typename T, int HD, int TPW> struct Queries {
   float x[TPW][HD / 32][64][8];
   AS_DEVICE f32x8 plain(int i, int s, int lane) const { return *(const f32x8 *)x[i][s][lane]; }
-  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
+  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
     const int width = a.H * HD;
-    for (int e = tid; e < TPW * 16 * (HD / 8); e += NW * 64) {
+    for (int e = tid; e < TPW * 16 * (HD / 8); e += NT) {
       const int qi = e / (HD / 8), c = e % (HD / 8);     // query of the group, piece of 8 head dims
       f32x8 v{};
       if (qbase + qi < QR) {
@@ -246,12 +245,12 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
     const u32x4 a = x[i][p][0][lane], b = x[i][p][1][lane];
     return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
   }
-  AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
+  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
     const int width = a.H * HD;
 #pragma unroll
-    for (int e0 = 0; e0 < TPW * 16 * (HD / 8); e0 += NW * 64) {
+    for (int e0 = 0; e0 < TPW * 16 * (HD / 8); e0 += NT) {
       const int e = e0 + tid;
-      if (TPW * 16 * (HD / 8) % (NW * 64) && e >= TPW * 16 * (HD / 8)) break;
+      if (TPW * 16 * (HD / 8) % NT && e >= TPW * 16 * (HD / 8)) break;
       const int qi = e / (HD / 8), piece = e % (HD / 8), lr = qi & 15, c = piece >> 2;   // c: group
       f16x8 v = {};
       if (qbase + qi < QR) {
@@ -398,24 +397,26 @@ template <int HD> struct Values {
   AS_DEVICE float scale(int nb) const { return q4_scale((vs[nb >> 2] >> (8 * (nb & 3))) & 255u); }
 };
 
-template <typename T, int HD, int TPW> struct Shared {
+template <typename T, int HD, int TPW, int NW> struct Shared {
+  // value operands a wave joins (8 waves and head dim 64: only the first four do)
+  static constexpr int OWN = HD / 16 > NW ? HD / 16 / NW : 1;
   union {
     Queries<T, HD, TPW> q;
-    f32x4 part[TPW][NW][(HD / 16) * (NW - 1) / NW][64];   // accumulators other waves join
+    f32x4 part[TPW][HD / 16 / OWN][OWN * (NW - 1)][64];   // accumulators other waves join
   };
   RowView view[TPW * 16];
   float2 ml[NW][TPW * 16];
 };
 
-template <typename T, int HD, int TPW, int LDST, bool ONCE>
-AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int item, int split, int qbase) {
+template <typename T, int HD, int TPW, int LDST, int NW, bool ONCE>
+AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST, NW> &smem_, int item, int split, int qbase) {
   typedef Ops<T> O;
   typedef typename O::F8 F8;
   typedef typename O::E E;
   typedef typename O::Raw Raw;
   typedef Keys<T, HD> K;
-  constexpr int NB = HD / 16, LD = HD / 4, OWN = NB / NW;   // OWN: value operands a wave joins
-  Shared<T, HD, TPW> &sm = reinterpret_cast<Shared<T, HD, TPW> &>(smem_);
+  constexpr int NB = HD / 16, LD = HD / 4, OWN = Shared<T, HD, TPW, NW>::OWN;
+  Shared<T, HD, TPW, NW> &sm = reinterpret_cast<Shared<T, HD, TPW, NW> &>(smem_);
   const int b = a.by_Hkv(item), g = item - b * a.Hkv;
   const int G = a.G, QR = G * a.n1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -498,7 +499,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST> &smem_, int it
     mine.lo = a.window ? max(P + depth - a.window + 1, 0) : 0;
     mine.root = !a.window || depth < a.window || P < a.sinks;
   }
-  sm.q.fill(a, qbase, QR, g, row0, tid);
+  sm.q.template fill<NW * 64>(a, qbase, QR, g, row0, tid);
   if (tid < TPW * 16) sm.view[tid] = mine;
   __syncthreads();
 
@@ -783,17 +784,17 @@ template <typename T> constexpr int waves_per_simd(int tpw) {
 
 // A workgroup: TPW tiles of a session's kv head (or TPW - 1: the tiles are dealt evenly to nqg
 // groups) over one of nsplit shares of its blocks.
-template <typename T, int HD, int TPW, bool ONCE>
+template <typename T, int HD, int TPW, int NW, bool ONCE>
 __global__ __launch_bounds__(NW * 64, waves_per_simd<T>(TPW)) void quant_attn_kernel(QuantAttnArgs a) {
-  __shared__ __attribute__((aligned(16))) Shared<T, HD, TPW> sm;
+  __shared__ __attribute__((aligned(16))) Shared<T, HD, TPW, NW> sm;
   // The query groups and the splits of a session's kv head follow each other on one XCD: the
   // groups read the same records.
   const int id = xcd_tile(blockIdx.x, gridDim.x);
   const int pair = a.by_nqg(id), grp = id - pair * a.nqg;
   const int item = a.by_nsplit(pair), split = pair - item * a.nsplit;
   const int qbase = (grp * a.each + min(grp, a.more)) * 16;
-  if (TPW == 1 || a.each + (grp < a.more) == TPW) attend<T, HD, TPW, TPW, ONCE>(a, sm, item, split, qbase);
-  else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW, ONCE>(a, sm, item, split, qbase);
+  if (TPW == 1 || a.each + (grp < a.more) == TPW) attend<T, HD, TPW, TPW, NW, ONCE>(a, sm, item, split, qbase);
+  else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW, NW, ONCE>(a, sm, item, split, qbase);
 }
 
 // Joins the splits: one thread per 4 head dims of a query row.
@@ -829,11 +830,13 @@ __global__ __launch_bounds__(256) void quant_combine_kernel(QuantAttnArgs a, int
 }
 
 template <typename T, int HD>
-void launch_tiles(int tpw, bool once, unsigned grid, hipStream_t s, const QuantAttnArgs &a) {
-  const auto kernel = once       ? quant_attn_kernel<T, HD, 1, true>
-                      : tpw == 1 ? quant_attn_kernel<T, HD, 1, false>
-                                 : quant_attn_kernel<T, HD, 2, false>;
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(NW * 64), 0, s, a);
+void launch_tiles(int tpw, int waves, bool once, unsigned grid, hipStream_t s, const QuantAttnArgs &a) {
+  auto kernel = once       ? quant_attn_kernel<T, HD, 1, 4, true>
+                : tpw == 1 ? quant_attn_kernel<T, HD, 1, 4, false>
+                           : quant_attn_kernel<T, HD, 2, 4, false>;
+  if constexpr (sizeof(T) == 2)
+    if (waves == 8) kernel = quant_attn_kernel<T, HD, 1, 8, false>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(waves * 64), 0, s, a);
 }
 
 }  // namespace
@@ -850,22 +853,34 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
   const int QR = H / Hkv * n1, tiles = (QR + 15) / 16, items = B * Hkv;
   const long long seen = window ? (long long)window + n1 + sinks + 2 * Q4_SLOTS : capacity;
   const int blocks_seen = (int)((seen < capacity ? seen : capacity) / Q4_SLOTS) + 3;
-  // Splits of at least 8 blocks a wave, which pays for their joining.
-  const long long splits = blocks_seen > 8 * NW ? blocks_seen / (8 * NW) : 1;
-  // Tiles a workgroup: two share a block's decoding and its read (70b fan-out: 85 us against 106),
-  // one gives twice the workgroups, for few rows over a short prefix (one session: 15 against 19).
-  // Three were slower than two at head dim 128 (90 against 85) and mixed at 64 (36 against 33 with 5
-  // tiles, 57 against 64 with 17).
+  // Splits: of 32 blocks at least, which pays for their joining (fp32 model: of 12, as a block
+  // takes longer there; 4 sessions x 1000 slots: 22 us in two, 28 in one).
+  const int least = sizeof(T) == 2 ? 32 : 12;
+  const long long splits = blocks_seen > least ? blocks_seen / least : 1;
   const long long work = (long long)items * tiles;
-  const int most = work <= 2LL * cus && work * splits <= 4LL * cus ? 1 : 2;
+  // No more tiles than CUs: a workgroup of eight waves on each CU, one tile each (bf16; one
+  // session of 17 rows, 1500 slots: 10.2 us against 11.1 with four waves, 24 x one row, 4000
+  // slots: 21 against 27).  Below 16 blocks eight waves have nothing to share.
+  const bool few = sizeof(T) == 2 && work <= cus;
+  const int waves = few && blocks_seen >= 16 ? 8 : 4;
+  // One tile a session (a token, as in plain decoding) otherwise, and more records than half the
+  // MALL keeps: they pass the caches (64 sessions x 2048 slots, 143 MB: 29.6 us against 31.8; 26
+  // MB, which a repeated call finds there: 13.9 against 12.4).
+  const bool once = tiles == 1 && !few && items * (long long)blocks_seen * q4_bytes(hd) > (96 << 20);
+  // Tiles a workgroup otherwise: two share a block's decoding and its read (70b fan-out: 85 us
+  // against 106), one gives twice the workgroups, for few rows over a short prefix.  Three were
+  // slower than two at head dim 128 (90 against 85) and mixed at 64 (36 against 33 with 5 tiles, 57
+  // against 64 with 17).
+  const int most = few || (work <= 2LL * cus && work * splits <= 4LL * cus) ? 1 : 2;
   const int nqg = (tiles + most - 1) / most, tpw = (tiles + nqg - 1) / nqg;
-  // Splits, where a CU would have less than two workgroups: as many as it holds at once.  A prefix
-  // of 96 blocks a wave or more is read in four parts also by up to three workgroups a CU: small
-  // ones end closer together (16384 slots, 576 workgroups: 169 us against 179).
+  // Splits, where a CU would have less than two workgroups: as many as it holds at once, of eight
+  // waves one.  A prefix of 384 blocks or more is read in four parts also by up to three
+  // workgroups a CU: small ones end closer together (16384 slots, 576 workgroups: 169 us against
+  // 179).
   const long long groups = (long long)items * nqg;
   long long nsplit = 1;
-  if (groups < 2LL * cus) nsplit = (tpw == 1 ? 4LL : 3LL) * cus / groups;
-  if (groups < 3LL * cus && nsplit < 4 && blocks_seen / NW >= 96) nsplit = 4;
+  if (groups < 2LL * cus) nsplit = (waves == 8 ? 1LL : tpw == 1 ? 4LL : 3LL) * cus / groups;
+  if (waves == 4 && groups < 3LL * cus && nsplit < 4 && blocks_seen >= 384) nsplit = 4;
   nsplit = nsplit < splits ? nsplit : splits;
   if (nsplit < 1) nsplit = 1;
   while (nsplit > 1 && (long long)items * nsplit * QR * hd > part_capacity) --nsplit;
@@ -879,12 +894,8 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
                         B * n1, n1, H, Hkv, G, nblk, tcap, (int)nsplit, nqg, tiles / nqg, tiles % nqg, window,
                         sinks, Div(nqg), Div((int)nsplit), Div(Hkv), Div(G), rows_io};
   const unsigned grid = (unsigned)(groups * nsplit);
-  // One tile a session (a token, as in plain decoding), and more records than the L2s' 32 MB:
-  // they pass the caches (64 sessions x 2048 slots, 143 MB: 29.6 us against 31.8; 26 MB, which a
-  // repeated call finds in the L2: 13.9 against 12.4).
-  const bool once = tiles == 1 && items * (seen < capacity ? seen : capacity) / Q4_SLOTS * q4_bytes(hd) > (32 << 20);
-  if (hd == 128) launch_tiles<T, 128>(tpw, once, grid, s, a);
-  else launch_tiles<T, 64>(tpw, once, grid, s, a);
+  if (hd == 128) launch_tiles<T, 128>(tpw, waves, once, grid, s, a);
+  else launch_tiles<T, 64>(tpw, waves, once, grid, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || nsplit == 1) return e;
   hipLaunchKernelGGL(quant_combine_kernel<T>, dim3((QR * (hd / 4) + 255) / 256, items), dim3(256), 0,

@@ -224,11 +224,18 @@ def test_attention_against_64_bits(dtype, hd, H, Hkv, lens, N):
     check_attention(dtype, hd, H, Hkv, lens, N, 0, 0, seed=H * 100 + N + hd)
 
 
-@pytest.mark.parametrize("dtype, hd, window", [("bf16", 128, 0), ("f32", 64, 0), ("bf16", 64, 70000),
-                                               ("f32", 128, 70000)])
+@pytest.mark.parametrize("dtype, hd, window", [("bf16", 128, 0), ("f32", 64, 0), ("bf16", 64, 4700)])
 def test_one_token_over_more_records_than_the_caches_hold(dtype, hd, window):
-    """Above 32 MB a single tile's records are read past the caches; in splits too."""
-    check_attention(dtype, hd, 4, 2, [123000, 45], 0, window, 4, seed=hd, least=123392)
+    """Above 96 MB and as many tiles as CUs a single tile's records are read past the caches."""
+    check_attention(dtype, hd, 64, 64, [4600, 45, 0, 4672, 31], 0, window, 4, seed=hd, least=4672)
+
+
+@pytest.mark.parametrize("dtype, hd, H, Hkv, lens, N, window", [
+    ("bf16", 128, 32, 8, [1500], 16, 0), ("bf16", 64, 32, 8, [1500], 16, 0), ("bf16", 64, 7, 1, [480, 0, 33], 6, 200),
+    ("bf16", 128, 8, 2, [3000, 700, 31], 2, 0), ("f32", 128, 16, 4, [1000, 420], 16, 0)])
+def test_few_tiles_over_a_long_prefix(dtype, hd, H, Hkv, lens, N, window):
+    """Workgroups of eight waves, with and without splits (fp32 model: four waves, short splits)."""
+    check_attention(dtype, hd, H, Hkv, lens, N, window, 4, seed=hd + N)
 
 
 @pytest.mark.parametrize("reach", [1, 2, 64])
