@@ -8,9 +8,9 @@
 //
 // Query rows are the G query heads of the kv head times the tree rows (row = tree_row * G +
 // head) in tiles of 16.  The work is divided by slots, not by queries: a wave holds all TPW
-// tiles of its workgroup (as accumulators) and takes blocks of its own, so a block's codes are
-// read by one wave, straight into the registers that the matrix instructions read, and serve
-// all the tiles.  No barrier and no LDS traffic but the queries' fragments.
+// tiles of its workgroup (as accumulators; one or two) and takes blocks of its own, so a block's
+// codes are read by one wave, straight into the registers that the matrix instructions read, and
+// serve all the tiles.  No barrier and no LDS traffic but the queries' fragments.
 //  * S^T = K Q^T by 16x16 products: a lane holds 8 scores of ONE query, for 8 consecutive
 //    slots.  Its running reference, exp2 and the probabilities stay in the lane, and these are
 //    its B operand of O^T = V^T P^T.
@@ -29,6 +29,14 @@
 //    pipe's time on the others.
 // At the end the waves of a workgroup, and then the splits of a session, are joined by their
 // (maximum, sum) pairs.
+//
+// What bounds it: a single row, HBM (64 sessions x 2048 slots x 8 kv heads of 128: 156 MB counted
+// in 25.3 us, 6.2 TB/s); 17 rows there, vector issue (69 % busy in 61.6 us; of a block's 760
+// cycles for two tiles 300 decode the values, 176 are exponentials) and two rounds' fixed part of
+// about 10 us each (tail, queries, join); 65 rows over 16384 slots, vector issue (74 %, matrix
+// cores 50 %; 167.5 us, 140 GFLOP).  Few rows: the chain of loads, products and join, 7 to 10 us.
+// Slower as measured: keys decoded to fp16 (92 us where this took 70), records through a ring in
+// LDS (72 and 181 against 69 and 167), weights through LDS with waves taking head dims (79, 240).
 //
 // Not finite: a group of 32 marked so reads as NaN.  NaN and inf reach the rows that see them
 // and no others: where a mask applies, values that are not finite count as 0 in the products and
@@ -782,7 +790,7 @@ template <typename T> constexpr int waves_per_simd(int tpw) {
   return sizeof(T) == 4 ? 2 : tpw == 1 ? 4 : 3;
 }
 
-// A workgroup: TPW tiles of a session's kv head (or TPW - 1: the tiles are dealt evenly to nqg
+// A workgroup: TPW tiles of a session's kv head (or one less: the tiles are dealt evenly to nqg
 // groups) over one of nsplit shares of its blocks.
 template <typename T, int HD, int TPW, int NW, bool ONCE>
 __global__ __launch_bounds__(NW * 64, waves_per_simd<T>(TPW)) void quant_attn_kernel(QuantAttnArgs a) {
