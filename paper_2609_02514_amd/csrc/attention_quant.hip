@@ -43,6 +43,8 @@
 // are added at the end, to the rows that see their slots.
 #include "quant.h"
 
+#include <utility>
+
 namespace {
 
 constexpr float LAZY_LOG2 = 8.f;
@@ -150,14 +152,32 @@ AS_DEVICE TreeRow tree_row(const QuantAttnArgs &a, int lane, int P, int parent, 
   return {anc, depth};
 }
 
-// Eight consecutive elements of a query row, and four of an output row.
-AS_DEVICE f16x8 load_q(const QuantAttnArgs &a, bf16, size_t off) {
-  if (a.rows_io) return bf16x8_to_f16x8(*(const bf16x8 *)((const bf16 *)a.q + off));
-  return *(const f16x8 *)((const f16 *)a.q + off);
+// Eight consecutive elements of a query row as they are, and as operands; four of an output row.
+AS_DEVICE u32x4 load_q(const QuantAttnArgs &a, bf16, size_t off) {
+  return *(const u32x4 *)((const uint16_t *)a.q + off);
+}
+AS_DEVICE f16x8 wide_q(const QuantAttnArgs &a, u32x4 v) {
+  return a.rows_io ? bf16x8_to_f16x8(__builtin_bit_cast(bf16x8, v)) : __builtin_bit_cast(f16x8, v);
 }
 AS_DEVICE f32x8 load_q(const QuantAttnArgs &a, float, size_t off) {
   return Ops<float>::raw((const float *)a.q + off);
 }
+// What a thread of NT loads of a workgroup's queries: element e = i NT + its number is a piece of
+// 8 head dims, e % (HD / 8), of query e / (HD / 8).  Asked for first of all, as nothing else
+// need be known for it.
+template <typename T, int HD, int TPW, int NT> struct Asked {
+  static constexpr int ALL = TPW * 16 * (HD / 8), N = (ALL + NT - 1) / NT;
+  decltype(load_q(std::declval<const QuantAttnArgs &>(), T(), 0)) v[N];
+  AS_DEVICE void load(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = i * NT + tid, qi = qbase + e / (HD / 8), r = a.by_G(qi), h = g * a.G + (qi - r * a.G);
+      v[i] = {};
+      if ((ALL % NT == 0 || e < ALL) && qi < QR)
+        v[i] = load_q(a, T(), (size_t)(row0 + r) * (a.H * HD) + h * HD + e % (HD / 8) * 8);
+    }
+  }
+};
 AS_DEVICE void store_out(const QuantAttnArgs &a, bf16, int row, int col, int width, f32x4 v) {
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
   typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
@@ -224,16 +244,12 @@ AS_DEVICE f32x8 first_of(f32x8 v, int n) {
 template <typename T, int HD, int TPW> struct Queries {
   float x[TPW][HD / 32][64][8];
   AS_DEVICE f32x8 plain(int i, int s, int lane) const { return *(const f32x8 *)x[i][s][lane]; }
-  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
-    const int width = a.H * HD;
-    for (int e = tid; e < TPW * 16 * (HD / 8); e += NT) {
-      const int qi = e / (HD / 8), c = e % (HD / 8);     // query of the group, piece of 8 head dims
-      f32x8 v{};
-      if (qbase + qi < QR) {
-        const int r = a.by_G(qbase + qi), h = g * a.G + (qbase + qi - r * a.G);
-        v = load_q(a, T(), (size_t)(row0 + r) * width + h * HD + c * 8);
-      }
-      *(f32x8 *)x[qi >> 4][c % (HD / 32)][c / (HD / 32) * 16 + (qi & 15)] = v;
+  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &, const Asked<T, HD, TPW, NT> &q, int tid) {
+#pragma unroll
+    for (int i = 0; i < q.N; ++i) {
+      const int e = i * NT + tid, qi = e / (HD / 8), c = e % (HD / 8);
+      if (q.ALL % NT == 0 || e < q.ALL)
+        *(f32x8 *)x[qi >> 4][c % (HD / 32)][c / (HD / 32) * 16 + (qi & 15)] = q.v[i];
     }
   }
 };
@@ -253,18 +269,13 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
     const u32x4 a = x[i][p][0][lane], b = x[i][p][1][lane];
     return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
   }
-  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &a, int qbase, int QR, int g, int row0, int tid) {
-    const int width = a.H * HD;
+  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &a, const Asked<bf16, HD, TPW, NT> &q, int tid) {
 #pragma unroll
-    for (int e0 = 0; e0 < TPW * 16 * (HD / 8); e0 += NT) {
-      const int e = e0 + tid;
-      if (TPW * 16 * (HD / 8) % NT && e >= TPW * 16 * (HD / 8)) break;
+    for (int i = 0; i < q.N; ++i) {
+      const int e = i * NT + tid;
+      if (q.ALL % NT && e >= q.ALL) break;
       const int qi = e / (HD / 8), piece = e % (HD / 8), lr = qi & 15, c = piece >> 2;   // c: group
-      f16x8 v = {};
-      if (qbase + qi < QR) {
-        const int r = a.by_G(qbase + qi), h = g * a.G + (qbase + qi - r * a.G);
-        v = load_q(a, T16(), (size_t)(row0 + r) * width + h * HD + piece * 8);
-      }
+      const f16x8 v = wide_q(a, q.v[i]);
       wide[qi >> 4][piece % (HD / 32)][piece / (HD / 32) * 16 + lr] = v;
       float f[8];
       uint32_t top = 0;
@@ -312,7 +323,6 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
       }
     }
   }
-  typedef bf16 T16;
 };
 
 // 16 bytes of a record's codes; ONCE: past the caches, as no other workgroup reads them.
@@ -434,6 +444,8 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST, NW> &smem_, in
   const int given = own ? a.prefix[b] : a.pos[row0], most = a.nblk * Q4_SLOTS + Q4_SLOTS - 1;
   const int parent = own && wave == 0 && lane + 1 < a.n1 ? a.parents[row0 + lane + 1] : 0;
   const int root = own ? a.parents[row0] : -1;
+  Asked<T, HD, TPW, NW * 64> asked;
+  asked.load(a, qbase, QR, g, row0, tid);
   const int P = min(max(given, 0), most), t = P & (Q4_SLOTS - 1), full = P / Q4_SLOTS;
 
   // Complete blocks that some row sees: [0, nsink) and [wlo, full).  Those that every row sees
@@ -507,7 +519,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST, NW> &smem_, in
     mine.lo = a.window ? max(P + depth - a.window + 1, 0) : 0;
     mine.root = !a.window || depth < a.window || P < a.sinks;
   }
-  sm.q.template fill<NW * 64>(a, qbase, QR, g, row0, tid);
+  sm.q.template fill<NW * 64>(a, asked, tid);
   if (tid < TPW * 16) sm.view[tid] = mine;
   __syncthreads();
 
