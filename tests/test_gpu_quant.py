@@ -219,7 +219,8 @@ def check_attention(dtype, hd, H, Hkv, lens, N, window, sinks, seed, layer=0, L=
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("H, Hkv, lens, N", [
     (1, 1, [0], 0), (1, 1, [1], 0), (4, 1, [0, 31, 32, 33, 64, 95], 0), (8, 2, [5, 200, 97], 16),
-    (4, 4, [130, 63], 8), (14, 2, [257], 33), (16, 2, [64, 31], 64), (6, 2, [1000, 3], 5)])
+    (4, 4, [130, 63], 8), (14, 2, [257], 33), (16, 2, [64, 31], 64), (6, 2, [1000, 3], 5),
+    (64, 1, [70, 3], 64), (40, 40, [33] * 9, 0)])
 def test_attention_against_64_bits(dtype, hd, H, Hkv, lens, N):
     check_attention(dtype, hd, H, Hkv, lens, N, 0, 0, seed=H * 100 + N + hd)
 
@@ -612,6 +613,48 @@ def test_a_captured_step_replays_as_it_ran():
         step(other, outs2, torch.roll(batch.tokens, 1 + i, 1))
         torch.cuda.synchronize()
     ver.close()
+
+
+@pytest.mark.parametrize("dtype, lens, N", [("bf16", [5000, 40], 3), ("bf16", [300, 0], 16), ("f32", [900, 33], 3)])
+def test_captured_attention_replays_between_other_calls(dtype, lens, N):
+    """With splits and without: two graphs and an eager call of other queries share the context's
+    workspace, one after the other on a stream of their own."""
+    B, n1, H, Hkv, hd = 2, N + 1, 8, 2, 128
+    cap = (max(lens) + 63) // 64 * 64
+    ver, cache = make(1, B, H, Hkv, hd, dtype, N, cap)
+    k, v = random_cache(1, B, Hkv, cap, hd, dtype, 5)
+    fill(ver, cache, k, v, lens, n1, 6)
+    cache, r = cache.with_prefix(i32(lens)), random.Random(7)
+    parents = i32([random_parents(r, N) for _ in range(B)])
+    g = torch.Generator().manual_seed(8)
+    qs = [torch.randn(B, n1, H, hd, generator=g).to(DT[dtype]).cuda() for _ in range(3)]
+    outs, status = [torch.zeros_like(q) for q in qs], [i32([9] * B) for _ in qs]
+    windows = [0, 100, 0]
+
+    def call(i):
+        ver.attention_quant(cache, 0, qs[i], parents, outs[i], status[i], windows[i], 4)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i in range(3):
+            call(i)
+        side.synchronize()
+        want = [o.clone() for o in outs]
+        graphs = []
+        for i in range(2):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[i], stream=side):
+                call(i)
+        for _ in range(3):
+            for t in outs + status:
+                t.fill_(7)
+            graphs[1].replay()
+            call(2)
+            graphs[0].replay()
+            side.synchronize()
+            for i in range(3):
+                assert torch.equal(outs[i], want[i]) and status[i].tolist() == [0] * B, i
 
 
 def test_scores_below_fp32s_range():
