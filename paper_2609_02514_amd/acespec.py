@@ -301,10 +301,11 @@ class QuantCache:
         if blocks.dim() != 5 or tail_k.dim() != 5 or tail_k.dtype not in (torch.bfloat16, torch.float32):
             raise ValueError("blocks and tail_k must have five dimensions, tail_k in bfloat16 or float32")
         L, B, Hkv, _, hd = tail_k.shape
+        self.index = blocks.get_device() if blocks.is_cuda else None   # the GPU's number
         _check_tensors([("blocks", blocks, (L, B, Hkv, capacity // 32, 34 * hd), torch.uint8),
                         ("tail_k", tail_k, (L, B, Hkv, tail_capacity, hd), tail_k.dtype),
                         ("tail_v", tail_v, (L, B, Hkv, hd, tail_capacity), tail_k.dtype),
-                        ("prefix_len", prefix_len, (B,), torch.int32)], blocks.device)
+                        ("prefix_len", prefix_len, (B,), torch.int32)], self.index)
         self.blocks, self.tail_k, self.tail_v = blocks, tail_k, tail_v
         self.capacity, self.tail_capacity, self.prefix_len = capacity, tail_capacity, prefix_len
         self._fit = (L, B, Hkv, hd, ACESPEC_BF16 if tail_k.dtype == torch.bfloat16 else ACESPEC_F32)
@@ -326,9 +327,8 @@ class QuantCache:
 
     def with_prefix(self, prefix_len) -> "QuantCache":
         """The same cache under other lengths (a commit's new_prefix_len)."""
-        import torch
-        _check_tensors([("prefix_len", prefix_len, self.prefix_len.shape, torch.int32)],
-                       self.blocks.device)
+        _check_tensors((("prefix_len", prefix_len, self.prefix_len.shape, self.prefix_len.dtype),),
+                       self.index)
         other = QuantCache.__new__(QuantCache)
         other.__dict__.update(self.__dict__)
         other.prefix_len = prefix_len
@@ -340,14 +340,13 @@ class QuantCache:
         return self._struct
 
 
-def _check_tensors(want, device=None):
+def _check_tensors(want, index):
     """Tensors whose shape, type or stride differ from what the call says would be read out of
-    range."""
+    range.  index: the GPU's."""
     for name, t, shape, dt in want:
-        if t.shape != shape or t.dtype is not dt or not t.is_contiguous() or not t.is_cuda or (
-                device is not None and t.device != device):
-            raise ValueError(f"{name} must be a contiguous {dt} tensor {tuple(shape)} on the "
-                             f"GPU (got {t.dtype} {tuple(t.shape)} on {t.device})")
+        if t.shape != shape or t.dtype is not dt or t.get_device() != index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} tensor {tuple(shape)} on GPU {index} "
+                             f"(got {t.dtype} {tuple(t.shape)} on {t.device})")
 
 
 class Verifier:
@@ -487,34 +486,30 @@ class Verifier:
     def _check_quant(self, cache: QuantCache, B: int):
         import torch
         d = self.desc
-        if cache.blocks.device.index != torch.cuda.current_device():
-            raise ValueError(f"the cache is on {cache.blocks.device}, the current device and stream "
+        if cache.index != torch.cuda.current_device():
+            raise ValueError(f"the cache is on cuda:{cache.index}, the current device and stream "
                              f"are cuda:{torch.cuda.current_device()}'s")
         if cache._fit != (d.n_layers, B, d.n_kv_heads, d.head_dim, d.dtype):
             raise ValueError(f"a cache of (layers, sessions, kv heads, head dim, dtype) {cache._fit} "
                              f"is not this model's and batch's "
                              f"{(d.n_layers, B, d.n_kv_heads, d.head_dim, d.dtype)}")
 
-    def _torch_dtype(self):
-        import torch
-        return torch.bfloat16 if self.desc.dtype == ACESPEC_BF16 else torch.float32
-
-    def _check_kv(self, kv_k, kv_v, capacity: int, B: int, more, device):
-        import torch
-        d, dt = self.desc, self._torch_dtype()
-        lead = (d.n_layers, B, d.n_kv_heads)
-        _check_tensors([("kv_k", kv_k, lead + (capacity, d.head_dim), dt),
-                        ("kv_v", kv_v, lead + (d.head_dim, capacity), dt)]
-                       + [(n, t, (B,), torch.int32) for n, t in more if t is not None], device)
+    def _check_kv(self, kv_k, kv_v, capacity: int, cache: QuantCache, lengths):
+        """A cache in the model's type against one in 4 bits; lengths: (name, tensor or None)."""
+        L, B, Hkv, hd, _ = cache._fit
+        dt, i32 = cache.tail_k.dtype, cache.prefix_len.dtype
+        _check_tensors((("kv_k", kv_k, (L, B, Hkv, capacity, hd), dt),
+                        ("kv_v", kv_v, (L, B, Hkv, hd, capacity), dt)), cache.index)
+        _check_tensors([(n, t, (B,), i32) for n, t in lengths if t is not None], cache.index)
 
     def quantize_kv(self, kv_k, kv_v, capacity: int, prefix_len, cache: QuantCache, status=None,
                     first=None) -> int:
         """kv's slots [0, prefix_len) brought to 4 bits (acespec_quantize_kv).  The cache's own
         prefix_len is not touched."""
         B = prefix_len.shape[0]
-        self._check_kv(kv_k, kv_v, capacity, B, [("prefix_len", prefix_len), ("status", status),
-                                                 ("first", first)], cache.blocks.device)
         self._check_quant(cache, B)
+        self._check_kv(kv_k, kv_v, capacity, cache, (("prefix_len", prefix_len), ("status", status),
+                                                     ("first", first)))
         kv = KVCache(_ptr(kv_k), _ptr(kv_v), capacity, _ptr(prefix_len))
         return acespec_quantize_kv(self.ctx, kv, cache.struct(), _ptr(first), B, _ptr(status),
                                    self._stream())
@@ -523,9 +518,8 @@ class Verifier:
                       first=None) -> int:
         """Slots [first / 32 * 32, cache.prefix_len) read back into kv (acespec_dequantize_kv)."""
         B = cache.prefix_len.shape[0]
-        self._check_kv(kv_k, kv_v, capacity, B, [("status", status), ("first", first)],
-                       cache.blocks.device)
         self._check_quant(cache, B)
+        self._check_kv(kv_k, kv_v, capacity, cache, (("status", status), ("first", first)))
         kv = KVCache(_ptr(kv_k), _ptr(kv_v), capacity, None)
         return acespec_dequantize_kv(self.ctx, cache.struct(), kv, _ptr(first), B, _ptr(status),
                                      self._stream())
@@ -533,13 +527,12 @@ class Verifier:
     def attention_quant(self, cache: QuantCache, layer: int, q, parents, out, status,
                         window: int = 0, sinks: int = 0) -> int:
         """Tree attention of one layer (acespec_attention_quant): q, out [B, N+1, H, hd]."""
-        import torch
-        d, (B, n1), dt = self.desc, parents.shape, self._torch_dtype()
-        shape = (B, n1, d.n_heads, d.head_dim)
-        _check_tensors([("q", q, shape, dt), ("out", out, shape, dt),
-                        ("parents", parents, (B, n1), torch.int32),
-                        ("status", status, (B,), torch.int32)], cache.blocks.device)
+        B, n1 = parents.shape
         self._check_quant(cache, B)
+        shape = (B, n1, self.desc.n_heads, self.desc.head_dim)
+        dt, i32 = cache.tail_k.dtype, cache.prefix_len.dtype
+        _check_tensors((("q", q, shape, dt), ("out", out, shape, dt), ("parents", parents, (B, n1), i32),
+                        ("status", status, (B,), i32)), cache.index)
         return acespec_attention_quant(self.ctx, cache.struct(), layer, AttnSpan(window, sinks),
                                        _ptr(q), _ptr(parents), B, n1 - 1, _ptr(out), _ptr(status),
                                        self._stream())
@@ -557,12 +550,13 @@ class Verifier:
                                          self._stream())
 
     def commit_kv_quant(self, cache: QuantCache, path, path_len, status, new_prefix_len) -> int:
-        import torch
         B, n1 = path.shape
         self._check_quant(cache, B)
-        _check_tensors([(n, t, s, torch.int32) for n, t, s in (
-            ("path", path, (B, n1)), ("path_len", path_len, (B,)), ("status", status, (B,)),
-            ("new_prefix_len", new_prefix_len, (B,))) if t is not None], cache.blocks.device)
+        i32 = cache.prefix_len.dtype
+        _check_tensors((("path", path, (B, n1), i32), ("path_len", path_len, (B,), i32),
+                        ("new_prefix_len", new_prefix_len, (B,), i32)), cache.index)
+        if status is not None:
+            _check_tensors((("status", status, (B,), i32),), cache.index)
         return acespec_commit_kv_quant(self.ctx, cache.struct(), _ptr(path), _ptr(path_len),
                                        _ptr(status), B, n1 - 1, _ptr(new_prefix_len),
                                        self._stream())

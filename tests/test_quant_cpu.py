@@ -167,11 +167,10 @@ def test_tensors_of_another_shape_or_type_are_refused_by_the_binding():
 
 def test_a_cache_of_another_device_or_model_is_refused_by_the_binding(monkeypatch):
     import torch
-    from types import SimpleNamespace
     ver = A.Verifier.__new__(A.Verifier)
     ver.desc, ver.ctx = A.ModelDesc(2, 64, 2, 1, 64, 64, 64, 1e4, 1e-5, A.ACESPEC_F32), None
     c = A.QuantCache.__new__(A.QuantCache)
-    c.blocks, c._fit = SimpleNamespace(device=torch.device("cuda:1")), (2, 3, 1, 64, A.ACESPEC_F32)
+    c.index, c._fit = 1, (2, 3, 1, 64, A.ACESPEC_F32)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     with pytest.raises(ValueError, match="cuda:1"):
         ver._check_quant(c, 3)
