@@ -31,10 +31,10 @@
 // (maximum, sum) pairs.
 //
 // What bounds it: a single row, HBM (64 sessions x 2048 slots x 8 kv heads of 128: 156 MB counted
-// in 25.3 us, 6.2 TB/s); 17 rows there, vector issue (69 % busy in 61.6 us; of a block's 760
+// in 25.3 us, 6.2 TB/s); 17 rows there, vector issue (69 % busy in 60.2 us; of a block's 760
 // cycles for two tiles 300 decode the values, 176 are exponentials) and two rounds' fixed part of
-// about 10 us each (tail, queries, join); 65 rows over 16384 slots, vector issue (74 %, matrix
-// cores 50 %; 167.5 us, 140 GFLOP).  Few rows: the chain of loads, products and join, 7 to 10 us.
+// about 9 us each (tail, queries, join); 65 rows over 16384 slots, vector issue (74 %, matrix
+// cores 50 %; 158.6 us, 140 GFLOP).  Few rows: the chain of loads, products and join, 6 to 10 us.
 // Slower as measured: keys decoded to fp16 (92 us where this took 70), records through a ring in
 // LDS (72 and 181 against 69 and 167), weights through LDS with waves taking head dims (79, 240).
 //
