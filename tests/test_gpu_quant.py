@@ -225,7 +225,8 @@ def test_attention_against_64_bits(dtype, hd, H, Hkv, lens, N):
     check_attention(dtype, hd, H, Hkv, lens, N, 0, 0, seed=H * 100 + N + hd)
 
 
-@pytest.mark.parametrize("dtype, hd, window", [("bf16", 128, 0), ("f32", 64, 0), ("bf16", 64, 4700)])
+@pytest.mark.parametrize("dtype, hd, window", [("bf16", 128, 0), ("f32", 64, 0), ("bf16", 64, 4700),
+                                               ("f32", 128, 0)])
 def test_one_token_over_more_records_than_the_caches_hold(dtype, hd, window):
     """Above 96 MB and as many tiles as CUs a single tile's records are read past the caches."""
     check_attention(dtype, hd, 64, 64, [4600, 45, 0, 4672, 31], 0, window, 4, seed=hd, least=4672)
@@ -613,6 +614,33 @@ def test_a_captured_step_replays_as_it_ran():
         step(other, outs2, torch.roll(batch.tokens, 1 + i, 1))
         torch.cuda.synchronize()
     ver.close()
+
+
+def test_offsets_beyond_32_bits():
+    """2^24 slots of three heads: 6.8 GB of records, 12.9 of keys.  Keys are 0, so that every slot
+    weighs the same; the values' mean, of 1 and 3 in halves, tells whether all were read (weights
+    and sums are whole numbers below 2^24 a lane, hence exact; the output rounds to bf16)."""
+    P, Hkv, hd = 2 ** 24, 3, 128
+    ver, cache = make(1, 1, Hkv, Hkv, hd, "bf16", 1, P)
+    k = torch.zeros(1, 1, Hkv, P, hd, dtype=torch.bfloat16, device="cuda")
+    v = torch.ones(1, 1, Hkv, hd, P, dtype=torch.bfloat16, device="cuda")
+    v[..., P // 2:] = 3
+    status = i32([9])
+    ver.quantize_kv(k, v, P, i32([P]), cache, status)
+    cache = cache.with_prefix(i32([P]))
+    q, out = torch.ones(1, 2, Hkv, hd, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 2, Hkv, hd, dtype=torch.bfloat16, device="cuda")
+    for window, want in ((0, 2.0), (2 ** 22, 3.0), (3 * 2 ** 22, 7 / 3)):
+        ver.attention_quant(cache, 0, q, i32([[-1, 0]]), out, status, window)
+        torch.cuda.synchronize()
+        assert status.tolist() == [0]
+        assert bool(((out.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -16)).all()), (window, out)
+    k.fill_(5), v.fill_(5)
+    ver.dequantize_kv(cache, k, v, P, status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0] and not bool(k.any())
+    assert bool((v[..., :P // 2] == 1).all()) and bool((v[..., P // 2:] == 3).all())
+    del k, v, cache
+    torch.cuda.empty_cache()
 
 
 @pytest.mark.parametrize("dtype, lens, N", [("bf16", [5000, 40], 3), ("bf16", [300, 0], 16), ("f32", [900, 33], 3)])
