@@ -873,30 +873,35 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
   const int QR = H / Hkv * n1, tiles = (QR + 15) / 16, items = B * Hkv;
   const long long seen = window ? (long long)window + n1 + sinks + 2 * Q4_SLOTS : capacity;
   const int blocks_seen = (int)((seen < capacity ? seen : capacity) / Q4_SLOTS) + 3;
-  // Splits: of 32 blocks at least, which pays for their joining (fp32 model: of 12, as a block
-  // takes longer there; 4 sessions x 1000 slots: 22 us in two, 28 in one).
-  const int least = sizeof(T) == 2 ? 32 : 12;
-  const long long splits = blocks_seen > least ? blocks_seen / least : 1;
   const long long work = (long long)items * tiles;
   // No more tiles than CUs: a workgroup of eight waves on each CU, one tile each (bf16; one
   // session of 17 rows, 1500 slots: 10.2 us against 11.1 with four waves, 24 x one row, 4000
   // slots: 21 against 27).  Below 16 blocks eight waves have nothing to share.
-  const bool few = sizeof(T) == 2 && work <= cus;
-  const int waves = few && blocks_seen >= 16 ? 8 : 4;
+  const bool wide = sizeof(T) == 4, few = work <= cus;
+  const int waves = few && !wide && blocks_seen >= 16 ? 8 : 4;
   // One tile a session (a token, as in plain decoding) otherwise, and more records than half the
   // MALL keeps: they pass the caches (64 sessions x 2048 slots, 143 MB: 29.6 us against 31.8; 26
   // MB, which a repeated call finds there: 13.9 against 12.4).
   const bool once = tiles == 1 && !few && items * (long long)blocks_seen * q4_bytes(hd) > (96 << 20);
   // Tiles a workgroup otherwise: two share a block's decoding and its read (70b fan-out: 85 us
-  // against 106), one gives twice the workgroups, for few rows over a short prefix.  Three were
-  // slower than two at head dim 128 (90 against 85) and mixed at 64 (36 against 33 with 5 tiles, 57
-  // against 64 with 17).
-  const int most = few || (work <= 2LL * cus && work * splits <= 4LL * cus) ? 1 : 2;
+  // against 106), so they are taken for many tiles, for long prefixes and where they leave a CU
+  // one workgroup (8 sessions of 17 rows x 2000: 17.0 us against 19.0; x 2: 6.5 against 5.9, so
+  // not below 32 blocks); one keeps two or three on each CU and the CUs even (12 x 2000: 19.7 against 23.9; fp32 model: 3 sessions of 60 rows,
+  // 8.8 against 11.6, one workgroup a CU or not).  Three were slower than two at head
+  // dim 128 (90 against 85) and mixed at 64 (36 against 33 with 5 tiles, 57 against 64 with 17).
+  const bool even = wide ? work <= 2LL * cus
+                         : blocks_seen < 128 && work <= 3LL * cus &&
+                               (blocks_seen < 32 || items * ((tiles + 1LL) / 2) > cus);
+  const int most = few || even ? 1 : 2;
   const int nqg = (tiles + most - 1) / most, tpw = (tiles + nqg - 1) / nqg;
   // Splits, where a CU would have less than two workgroups: as many as it holds at once, of eight
-  // waves one.  A prefix of 384 blocks or more is read in four parts also by up to three
-  // workgroups a CU: small ones end closer together (16384 slots, 576 workgroups: 169 us against
-  // 179).
+  // waves one; from 128 blocks on (few tiles: from 64), of 32 at least, which pays for their
+  // joining (40 single rows x 2000: 21.5 us in two, 19.4 in one).  fp32 model: of 12, as a block
+  // takes longer there (4 sessions x 1000: 22 us in two, 28 in one).  A prefix of 384 blocks or
+  // more is read in four parts also by up to three workgroups a CU: small ones end closer
+  // together (16384 slots, 576 workgroups: 169 us against 179).
+  const int each = wide ? 12 : 32, from = wide || few ? 2 * each : 128;
+  const long long splits = blocks_seen >= from ? blocks_seen / each : 1;
   const long long groups = (long long)items * nqg;
   long long nsplit = 1;
   if (groups < 2LL * cus) nsplit = (waves == 8 ? 1LL : tpw == 1 ? 4LL : 3LL) * cus / groups;
