@@ -3,7 +3,7 @@
 //
 // All three move bytes, and HBM bounds them: 4 layers x 16 sessions x 8 kv heads of 128, up to
 // 2048 slots, 429 MB of bf16: 104 us to 4 bits (5.4 TB/s), 77 us back.  After a commit (32 layers
-// x 48 sessions x 8, 5 to 17 slots each) it is lines: a value row has a few two-byte slots in
+// x 48 sessions x 8, 1 to 9 slots each) it is lines: a value row has a few two-byte slots in
 // each 128, and 268 MB move in 74 us (commit), 424 MB in 138 (read-back).  A workgroup takes the keys, or the values, of 64
 // slots of a plane (layer, session, kv head): the unquantized side is read or written in whole
 // 128-byte lines through LDS, the records in runs of 1 KB, and each wave converts one operand
