@@ -294,7 +294,8 @@ class QuantCache:
     """The tensors of a KV cache in 4 bits (acespec_kv_quant): blocks [L, B, Hkv,
     capacity / 32, 34 hd] uint8, tail_k [L, B, Hkv, tail_capacity, hd] and tail_v [L, B, Hkv,
     hd, tail_capacity] in the model dtype, prefix_len [B] int32, all contiguous on one GPU.
-    Shapes and types are checked here, once; the tensors are the cache's from then on."""
+    Shapes and types are checked here, once.  Only prefix_len can be assigned (a commit's new
+    lengths; checked again); a call refuses tensors whose memory has moved since."""
 
     def __init__(self, blocks, tail_k, tail_v, capacity: int, tail_capacity: int, prefix_len):
         import torch
@@ -306,11 +307,25 @@ class QuantCache:
                         ("tail_k", tail_k, (L, B, Hkv, tail_capacity, hd), tail_k.dtype),
                         ("tail_v", tail_v, (L, B, Hkv, hd, tail_capacity), tail_k.dtype),
                         ("prefix_len", prefix_len, (B,), torch.int32)], self.index)
-        self.blocks, self.tail_k, self.tail_v = blocks, tail_k, tail_v
-        self.capacity, self.tail_capacity, self.prefix_len = capacity, tail_capacity, prefix_len
         self._fit = (L, B, Hkv, hd, ACESPEC_BF16 if tail_k.dtype == torch.bfloat16 else ACESPEC_F32)
-        self._struct = KVQuant(_ptr(blocks), _ptr(tail_k), _ptr(tail_v), capacity, tail_capacity,
-                               _ptr(prefix_len))
+        self._tensors = (blocks, tail_k, tail_v, prefix_len)
+        self._at = (_ptr(blocks), _ptr(tail_k), _ptr(tail_v), _ptr(prefix_len))
+        self._struct = KVQuant(*self._at[:3], capacity, tail_capacity, self._at[3])
+
+    blocks = property(lambda self: self._tensors[0])
+    tail_k = property(lambda self: self._tensors[1])
+    tail_v = property(lambda self: self._tensors[2])
+    prefix_len = property(lambda self: self._tensors[3])
+    capacity = property(lambda self: self._struct.capacity)
+    tail_capacity = property(lambda self: self._struct.tail_capacity)
+
+    @prefix_len.setter
+    def prefix_len(self, lengths):
+        _check_tensors((("prefix_len", lengths, self.prefix_len.shape, self.prefix_len.dtype),),
+                       self.index)
+        self._tensors = (*self._tensors[:3], lengths)
+        self._at = (*self._at[:3], _ptr(lengths))
+        self._struct = KVQuant(*self._at[:3], self.capacity, self.tail_capacity, self._at[3])
 
     @classmethod
     def alloc(cls, L: int, B: int, Hkv: int, hd: int, capacity: int, max_nodes: int, dtype: str,
@@ -327,16 +342,17 @@ class QuantCache:
 
     def with_prefix(self, prefix_len) -> "QuantCache":
         """The same cache under other lengths (a commit's new_prefix_len)."""
-        _check_tensors((("prefix_len", prefix_len, self.prefix_len.shape, self.prefix_len.dtype),),
-                       self.index)
         other = QuantCache.__new__(QuantCache)
         other.__dict__.update(self.__dict__)
         other.prefix_len = prefix_len
-        other._struct = KVQuant.from_buffer_copy(self._struct)
-        other._struct.prefix_len = _ptr(prefix_len)
         return other
 
     def struct(self) -> KVQuant:
+        b, k, v, p = self._tensors
+        if (b.data_ptr(), k.data_ptr(), v.data_ptr(), p.data_ptr()) != self._at:
+            moved = [n for n, t, at in zip(("blocks", "tail_k", "tail_v", "prefix_len"), self._tensors, self._at)
+                     if t.data_ptr() != at]
+            raise ValueError(f"the memory of {', '.join(moved)} moved after the cache was made (resize_ or set_)")
         return self._struct
 
 

@@ -210,3 +210,47 @@ def test_more_planes_than_a_launch_takes():
     for name, rc in calls(A.load(), Ctx(L=2 ** 20, Hkv=2).ptr, quant(), cache()):
         if name != "verify":             # (its layers' weights are looked at first)
             refused(rc, "exceed one launch", A.ACESPEC_EUNSUPPORTED)
+
+
+def cpu_cache(monkeypatch):
+    """A cache of CPU tensors (the check that they are on a GPU left out)."""
+    import torch
+    monkeypatch.setattr(A, "_check_tensors", lambda *a: None)
+    return A.QuantCache(torch.zeros(2, 3, 1, 2, 34 * 64, dtype=torch.uint8), torch.zeros(2, 3, 1, 64, 64),
+                        torch.zeros(2, 3, 1, 64, 64), 64, 64, torch.zeros(3, dtype=torch.int32))
+
+
+def test_a_cache_under_assigned_lengths_hands_those_on(monkeypatch):
+    import torch
+    c = cpu_cache(monkeypatch)
+    old, new = c.prefix_len, torch.ones(3, dtype=torch.int32)
+    other = c.with_prefix(old)
+    c.prefix_len = new
+    assert c.prefix_len is new and c.struct().prefix_len == new.data_ptr()
+    assert other.prefix_len is old and other.struct().prefix_len == old.data_ptr()
+    monkeypatch.undo()
+    with pytest.raises(ValueError, match="prefix_len"):
+        c.prefix_len = torch.ones(2, dtype=torch.int32)
+    assert c.prefix_len is new
+
+
+@pytest.mark.parametrize("name", ["blocks", "tail_k", "tail_v", "capacity", "tail_capacity"])
+def test_a_caches_tensors_and_sizes_cannot_be_replaced(monkeypatch, name):
+    c = cpu_cache(monkeypatch)
+    with pytest.raises(AttributeError):
+        setattr(c, name, getattr(c, name))
+
+
+@pytest.mark.parametrize("name", ["blocks", "tail_k", "tail_v", "prefix_len"])
+def test_a_tensor_whose_memory_moved_is_refused(monkeypatch, name):
+    import torch
+    c = cpu_cache(monkeypatch)
+    c.struct()
+    t = getattr(c, name)
+    t.set_(torch.zeros(t.shape, dtype=t.dtype))
+    with pytest.raises(ValueError, match=f"{name} moved"):
+        c.struct()
+    other = c.with_prefix(torch.zeros(3, dtype=torch.int32))   # new lengths take nothing else over
+    if name != "prefix_len":
+        with pytest.raises(ValueError, match=f"{name} moved"):
+            other.struct()
