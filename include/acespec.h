@@ -302,7 +302,8 @@ int acespec_convert_v_cache(const void *src, void *dst, int planes, int capacity
  *          [..][head_dim][tail_capacity], as in acespec_kv_cache.
  * A session of P = prefix_len[b] slots holds slots [0, P / 32 * 32) in blocks, slot
  * P / 32 * 32 + i in tail slot i (i < P % 32), and tree row r in tail slot P % 32 + r.
- * P % 32 = 0 leaves no slot in the tail, and P may be 0. */
+ * P % 32 = 0 leaves no slot in the tail, and P may be 0.  blocks, tail_k and tail_v do not
+ * overlap (ACESPEC_EINVAL from every call below). */
 typedef struct {
   void *blocks;
   void *tail_k, *tail_v;
@@ -330,9 +331,9 @@ typedef struct {
  *  status [B] DEVICE or NULL: ACESPEC_OK, or ACESPEC_EBADTREE for a session with
  *          prefix_len[b] outside [0, kv->capacity], beyond qc->capacity + 31, or first[b]
  *          outside [0, prefix_len[b]]; nothing of such a session is written.
- * kv->capacity is a multiple of 64; k, v, blocks and the tails are 16-byte aligned and do not
- * overlap.  Enqueued on stream; ACESPEC_EINVAL before anything is launched for arguments
- * outside the above. */
+ * kv->capacity is a multiple of 64; k, v, blocks and the tails are 16-byte aligned.  They do not
+ * overlap, and what the call writes overlaps nothing else that is given.  Enqueued on stream;
+ * ACESPEC_EINVAL before anything is launched for arguments outside the above. */
 int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
                         const int32_t *first, int B, int32_t *status, hipStream_t stream);
 

@@ -12,6 +12,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -491,6 +492,28 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
   return a0 < b0 + nb && b0 < a0 + na;
 }
 
+// An array of a call (NULL: not given).  What one workgroup writes no other may read or write, so
+// an array that the call writes lies apart from all its others.
+struct Array {
+  const char *name;
+  const void *p;
+  size_t bytes;
+  bool written;
+};
+int check_apart(std::initializer_list<Array> all) {
+  for (const Array *a = all.begin(); a != all.end(); ++a)
+    for (const Array *b = all.begin(); b != a; ++b)
+      if (a->p && b->p && (a->written || b->written) && overlap(a->p, a->bytes, b->p, b->bytes))
+        return fail(ACESPEC_EINVAL, "%s and %s overlap", b->name, a->name);
+  return ACESPEC_OK;
+}
+
+// Bytes of tail_k or tail_v, of all layers.
+size_t quant_tail_bytes(const acespec_model_desc &d, const acespec_kv_quant *qc, int B) {
+  return (size_t)d.n_layers * B * d.n_kv_heads * qc->tail_capacity * d.head_dim *
+         (d.dtype == ACESPEC_BF16 ? 2 : 4);
+}
+
 // A cache in 4 bits for B sessions whose tail takes n1 tree rows behind any prefix (n1 0: no
 // tree).
 int check_quant(const acespec_model_desc &d, const acespec_kv_quant *qc, int B, int n1) {
@@ -508,7 +531,10 @@ int check_quant(const acespec_model_desc &d, const acespec_kv_quant *qc, int B, 
   const size_t planes = (size_t)d.n_layers * B * d.n_kv_heads;
   if (planes > 0x7fffff)   // of two workgroups of 256 threads, in a launch of less than 2^32
     return fail(ACESPEC_EUNSUPPORTED, "%zu planes (layer, session, kv head) exceed one launch", planes);
-  return ACESPEC_OK;
+  const size_t tail = quant_tail_bytes(d, qc, B);
+  return check_apart({{"blocks", qc->blocks, d.n_layers * quant_layer_bytes(d, qc, B), true},
+                      {"tail_k", qc->tail_k, tail, true},
+                      {"tail_v", qc->tail_v, tail, true}});
 }
 
 int check_span(const acespec_attn_span *span, acespec_attn_span *out) {
@@ -789,7 +815,8 @@ namespace {
 // The arguments that acespec_quantize_kv and acespec_dequantize_kv share; prefix_len is the
 // source's.
 int check_convert(const acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
-                  const int32_t *prefix_len, const int32_t *first, const int32_t *status, int B) {
+                  const int32_t *prefix_len, const int32_t *first, const int32_t *status, int B,
+                  bool quantize) {
   if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
   const acespec_model_desc &d = ctx->d;
   if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
@@ -805,19 +832,25 @@ int check_convert(const acespec_ctx *ctx, const acespec_kv_cache *kv, const aces
   if (qc) c.prefix_len = prefix_len;
   rc = check_quant(d, qc ? &c : nullptr, B, 0);
   if (rc) return rc;
-  const size_t planes = (size_t)d.n_layers * B * d.n_kv_heads;
-  const size_t eb = d.dtype == ACESPEC_BF16 ? 2 : 4, n = planes * d.head_dim * eb;
-  const void *held[3] = {qc->blocks, qc->tail_k, qc->tail_v};
-  const size_t sizes[3] = {planes * (qc->capacity / kBlock) * 34 * d.head_dim,
-                           n * qc->tail_capacity, n * qc->tail_capacity};
+  const size_t tail = quant_tail_bytes(d, qc, B), held = tail / qc->tail_capacity * kv->capacity;
+  const size_t blocks = d.n_layers * quant_layer_bytes(d, qc, B);
+  const void *in4[3] = {qc->blocks, qc->tail_k, qc->tail_v};
+  const size_t sizes[3] = {blocks, tail, tail};
   for (int i = 0; i < 3; ++i)
-    if (overlap(kv->k, n * kv->capacity, held[i], sizes[i]) ||
-        overlap(kv->v, n * kv->capacity, held[i], sizes[i]))
+    if (overlap(kv->k, held, in4[i], sizes[i]) || overlap(kv->v, held, in4[i], sizes[i]))
       return fail(ACESPEC_EINVAL, "the cache and the quantized cache overlap");
+  if (overlap(kv->k, held, kv->v, held)) return fail(ACESPEC_EINVAL, "k and v overlap");
   const size_t each = (size_t)B * sizeof(int32_t);   // (read by workgroups while one writes status)
   if (status && (overlap(status, each, prefix_len, each) || (first && overlap(status, each, first, each))))
     return fail(ACESPEC_EINVAL, "status overlaps prefix_len or first");
-  return ACESPEC_OK;
+  return check_apart({{"k", kv->k, held, !quantize},
+                      {"v", kv->v, held, !quantize},
+                      {"blocks", qc->blocks, blocks, quantize},
+                      {"tail_k", qc->tail_k, tail, quantize},
+                      {"tail_v", qc->tail_v, tail, quantize},
+                      {"prefix_len", prefix_len, each, false},
+                      {"first", first, each, false},
+                      {"status", status, each, true}});
 }
 
 }  // namespace
@@ -827,7 +860,7 @@ extern "C" {
 int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
                         const int32_t *first, int B, int32_t *status, hipStream_t stream) {
   g_err.clear();
-  const int rc = check_convert(ctx, kv, qc, kv ? kv->prefix_len : nullptr, first, status, B);
+  const int rc = check_convert(ctx, kv, qc, kv ? kv->prefix_len : nullptr, first, status, B, true);
   if (rc) return rc;
   const acespec_model_desc &d = ctx->d;
   if (d.dtype == ACESPEC_BF16)
@@ -848,7 +881,7 @@ int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const aces
 int acespec_dequantize_kv(acespec_ctx *ctx, const acespec_kv_quant *qc, const acespec_kv_cache *kv,
                           const int32_t *first, int B, int32_t *status, hipStream_t stream) {
   g_err.clear();
-  const int rc = check_convert(ctx, kv, qc, qc ? qc->prefix_len : nullptr, first, status, B);
+  const int rc = check_convert(ctx, kv, qc, qc ? qc->prefix_len : nullptr, first, status, B, false);
   if (rc) return rc;
   const acespec_model_desc &d = ctx->d;
   if (d.dtype == ACESPEC_BF16)

@@ -254,3 +254,43 @@ def test_a_tensor_whose_memory_moved_is_refused(monkeypatch, name):
     if name != "prefix_len":
         with pytest.raises(ValueError, match=f"{name} moved"):
             other.struct()
+
+
+TAIL = 2 * 4 * 2 * 64 * 128 * 2          # bytes of tail_k or tail_v of quant(), and of k or v ..
+KV = 2 * TAIL                            # .. of cache(): 64 and 128 slots
+BLOCKS = 2 * 4 * 2 * 4 * 34 * 128
+
+
+@pytest.mark.parametrize("kw", [dict(tail_k=P), dict(tail_k=P + BLOCKS - 16), dict(blocks=P + (1 << 32) + TAIL - 16),
+                                dict(tail_v=P), dict(tail_v=P + (1 << 32)), dict(tail_v=P + (1 << 32) - TAIL + 16)])
+def test_blocks_and_tails_that_overlap_each_other_are_refused_everywhere(kw):
+    for name, rc in calls(A.load(), Ctx().ptr, quant(**kw), cache()):
+        refused(rc, "overlap")
+
+
+def test_conversions_refuse_arrays_that_overlap_what_is_written():
+    lib, ctx = A.load(), Ctx()
+    k, v, lens, far = P + (4 << 32), P + (5 << 32), P + (6 << 32), P + (7 << 32)
+
+    def both(qc, kv, first=None, status=None):
+        yield "quantize", lib.acespec_quantize_kv(ctx.ptr, C.byref(kv), C.byref(qc), first, 4, status, None)
+        yield "dequantize", lib.acespec_dequantize_kv(ctx.ptr, C.byref(qc), C.byref(kv), first, 4, status, None)
+
+    for kw in (dict(v=k), dict(v=k + KV - 16), dict(v=k - KV + 16)):
+        for name, rc in both(quant(), cache(**kw)):
+            refused(rc, "overlap")
+    cached = (k + KV - 16, v, v + KV - 4)
+    held = (P + BLOCKS - 16, P + (1 << 32), P + (1 << 32) + TAIL - 4, P + (2 << 32) + TAIL - 16)
+    for at in cached + held:             # status is written, whatever the direction
+        for name, rc in both(quant(), cache(), status=at):
+            refused(rc, "overlap")
+    for at in held:                      # quantising writes blocks and tails
+        refused(lib.acespec_quantize_kv(ctx.ptr, C.byref(cache(prefix=at)), C.byref(quant()), None, 4, None,
+                                        None), "overlap")
+        refused(lib.acespec_quantize_kv(ctx.ptr, C.byref(cache()), C.byref(quant()), at, 4, None, None),
+                "overlap")
+    for at in cached:                    # reading back writes k and v
+        refused(lib.acespec_dequantize_kv(ctx.ptr, C.byref(quant(prefix=at)), C.byref(cache()), None, 4, None,
+                                          None), "overlap")
+        refused(lib.acespec_dequantize_kv(ctx.ptr, C.byref(quant()), C.byref(cache()), at, 4, None, None),
+                "overlap")
