@@ -348,9 +348,10 @@ int acespec_dequantize_kv(acespec_ctx *ctx, const acespec_kv_quant *qc, const ac
  * prefix_len[b] + depth(r), attends to the prefix, its ancestors and itself, as far as span
  * shows them, with scale 1/sqrt(head_dim).
  *  layer   in [0, n_layers) of ctx's model,
- *  q, out  [B, N+1, n_heads, head_dim] in the model dtype, q rotated; 16-byte aligned, no
- *          overlap.  Tail slots prefix_len[b] % 32 + r hold the keys (rotated) and values of the
- *          tree's rows.  A decode of single tokens is N = 0.
+ *  q, out  [B, N+1, n_heads, head_dim] in the model dtype, q rotated; 16-byte aligned.  out and
+ *          status overlap nothing else that is given (ACESPEC_EINVAL).  Tail slots
+ *          prefix_len[b] % 32 + r hold the keys (rotated) and values of the tree's rows.  A
+ *          decode of single tokens is N = 0.
  *  parent_idx [B, N+1] as in acespec_verify_tree,
  *  status [B]: ACESPEC_OK or ACESPEC_EBADTREE (parents, or prefix_len outside
  *          [0, capacity + 31]).

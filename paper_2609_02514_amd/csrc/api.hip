@@ -783,14 +783,22 @@ int acespec_attention_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, int la
   if (rc) return rc;
   const int n1 = N + 1, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
   const size_t io = (size_t)B * n1 * H * hd * ctx->esz;
-  if (overlap(q, io, out, io)) return fail(ACESPEC_EINVAL, "q and out overlap");
-  const size_t tails = (size_t)d.n_layers * B * Hkv * qc->tail_capacity * hd * ctx->esz;
-  if (overlap(out, io, qc->blocks, d.n_layers * quant_layer_bytes(d, qc, B)) ||
-      overlap(out, io, qc->tail_k, tails) || overlap(out, io, qc->tail_v, tails))
+  const size_t held = d.n_layers * quant_layer_bytes(d, qc, B), tails = quant_tail_bytes(d, qc, B);
+  if (overlap(out, io, qc->blocks, held) || overlap(out, io, qc->tail_k, tails) ||
+      overlap(out, io, qc->tail_v, tails))
     return fail(ACESPEC_EINVAL, "out and the quantized cache overlap");
   const size_t each = (size_t)B * sizeof(int32_t);   // (read by workgroups while one writes status)
   if (overlap(status, each, qc->prefix_len, each) || overlap(status, each, parent_idx, each * n1))
     return fail(ACESPEC_EINVAL, "status overlaps prefix_len or parent_idx");
+  rc = check_apart({{"blocks", qc->blocks, held, false},
+                    {"tail_k", qc->tail_k, tails, false},
+                    {"tail_v", qc->tail_v, tails, false},
+                    {"prefix_len", qc->prefix_len, each, false},
+                    {"parent_idx", parent_idx, each * n1, false},
+                    {"q", q, io, false},
+                    {"out", out, io, true},
+                    {"status", status, each, true}});
+  if (rc) return rc;
   const uint8_t *blocks = (const uint8_t *)qc->blocks + layer * quant_layer_bytes(d, qc, B);
   const size_t tail = (size_t)layer * B * Hkv * qc->tail_capacity * hd;
   if (d.dtype == ACESPEC_BF16)

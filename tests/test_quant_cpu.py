@@ -294,3 +294,22 @@ def test_conversions_refuse_arrays_that_overlap_what_is_written():
                                           None), "overlap")
         refused(lib.acespec_dequantize_kv(ctx.ptr, C.byref(quant()), C.byref(cache()), at, 4, None, None),
                 "overlap")
+
+
+def test_attention_refuses_arrays_that_overlap_what_is_written():
+    lib, ctx = A.load(), Ctx()
+    io, rows = 4 * 17 * 4 * 128 * 2, 4 * 17 * 4
+    q, out, parents, status, prefix = (P + (i << 32) for i in (8, 9, 10, 11, 3))
+
+    def attention(q=q, out=out, parents=parents, status=status, qc=None):
+        return lib.acespec_attention_quant(ctx.ptr, C.byref(qc or quant()), 0, None, q, parents, 4, 16, out,
+                                           status, None)
+
+    for at in (out, out + io - 4, q, q + io - 4, P, P + BLOCKS - 4, P + (1 << 32), P + (2 << 32) + TAIL - 4,
+               parents, parents + rows - 4, prefix, prefix + 12):
+        refused(attention(status=at), "overlap")
+    refused(attention(out=parents), "overlap")
+    refused(attention(out=parents + rows - 16), "overlap")
+    refused(attention(parents=out + io - 4), "overlap")
+    refused(attention(qc=quant(prefix=out + io - 4)), "overlap")
+    refused(attention(out=P + (2 << 32) + TAIL - 16), "overlap")
