@@ -377,8 +377,9 @@ int acespec_verify_tree_quant(acespec_ctx *ctx, const acespec_weights *weights,
 
 /* acespec_commit_kv over a cache in 4 bits: the root and the kept rows join the tail's
  * committed slots, every 32 of which become a block; the rest move to the tail's front.  Tail
- * slots past them keep stale entries.  Arguments and new_prefix_len as in acespec_commit_kv; a
- * session is not committed (-1, nothing moved) also where its new blocks do not fit capacity. */
+ * slots past them keep stale entries.  Arguments and new_prefix_len as in acespec_commit_kv, none
+ * of them inside blocks or the tails (ACESPEC_EINVAL); a session is not committed (-1, nothing
+ * moved) also where its new blocks do not fit capacity. */
 int acespec_commit_kv_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, const int32_t *path,
                             const int32_t *path_len, const int32_t *status, int B, int N,
                             int32_t *new_prefix_len, hipStream_t stream);

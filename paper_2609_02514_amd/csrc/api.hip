@@ -928,6 +928,16 @@ int acespec_commit_kv_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, const 
       overlap(path_len, (size_t)B * 4, new_prefix_len, (size_t)B * 4) ||
       (status && overlap(status, (size_t)B * 4, new_prefix_len, (size_t)B * 4)))
     return fail(ACESPEC_EINVAL, "new_prefix_len overlaps path, path_len or status");
+  const size_t each = (size_t)B * sizeof(int32_t), tails = quant_tail_bytes(d, qc, B);
+  rc = check_apart({{"blocks", qc->blocks, d.n_layers * quant_layer_bytes(d, qc, B), true},
+                    {"tail_k", qc->tail_k, tails, true},
+                    {"tail_v", qc->tail_v, tails, true},
+                    {"prefix_len", qc->prefix_len, each, false},
+                    {"path", path, each * (N + 1), false},
+                    {"path_len", path_len, each, false},
+                    {"status", status, each, false},
+                    {"new_prefix_len", new_prefix_len, each, true}});
+  if (rc) return rc;
   if (d.dtype == ACESPEC_BF16)
     RUN(K_COMMIT, launch_commit_quant<bf16>((uint8_t *)qc->blocks, (bf16 *)qc->tail_k,
                                             (bf16 *)qc->tail_v, qc->prefix_len, path, path_len, status,

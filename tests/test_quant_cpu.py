@@ -313,3 +313,17 @@ def test_attention_refuses_arrays_that_overlap_what_is_written():
     refused(attention(parents=out + io - 4), "overlap")
     refused(attention(qc=quant(prefix=out + io - 4)), "overlap")
     refused(attention(out=P + (2 << 32) + TAIL - 16), "overlap")
+
+
+def test_the_commit_refuses_arrays_that_overlap_what_is_written():
+    lib, ctx = A.load(), Ctx()
+    path, path_len, status, new = (P + (i << 32) for i in (8, 9, 10, 11))
+    written = (P, P + BLOCKS - 4, P + (1 << 32), P + (1 << 32) + TAIL - 4, P + (2 << 32) + TAIL - 4)
+
+    def commit(path=path, path_len=path_len, status=status, new=new, qc=None):
+        return lib.acespec_commit_kv_quant(ctx.ptr, C.byref(qc or quant()), path, path_len, status, 4, 16, new,
+                                           None)
+
+    for at in written:
+        for kw in (dict(path=at), dict(path_len=at), dict(status=at), dict(new=at), dict(qc=quant(prefix=at))):
+            refused(commit(**kw), "overlap")
