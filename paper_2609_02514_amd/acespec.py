@@ -365,6 +365,14 @@ def _check_tensors(want, index):
                              f"(got {t.dtype} {tuple(t.shape)} on {t.device})")
 
 
+def _check_room(want, index):
+    """Tensors of which a call uses the first n elements."""
+    for name, t, n, dt in want:
+        if t is None or t.numel() < n or t.dtype is not dt or t.get_device() != index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} tensor of at least {n} elements on GPU {index} "
+                             f"(got {'None' if t is None else f'{t.dtype} {tuple(t.shape)} on {t.device}'})")
+
+
 class Verifier:
     """Owns a context for one model shape and turns torch tensors into ABI structs."""
 
@@ -559,11 +567,29 @@ class Verifier:
         """verify_tree over a cache in 4 bits; scalar: q is q_hat [B, N+1]."""
         B, n1 = tokens.shape
         self._check_quant(cache, B)
+        self._check_step(cache, tokens, parents, q, u, k, outs, scalar)
         return acespec_verify_tree_quant(self.ctx, wstruct, cache.struct(), AttnSpan(window, sinks),
                                          _ptr(tokens), _ptr(parents), None if scalar else _ptr(q),
                                          _ptr(q) if scalar else None, _ptr(u), B, n1 - 1,
                                          Params(T, top_p, k), self.outputs_struct(outs),
                                          self._stream())
+
+    def _check_step(self, cache: QuantCache, tokens, parents, q, u, k: int, outs: Dict, scalar: bool):
+        """A verify step's inputs and outputs (those of alloc_outputs; they may be larger)."""
+        import torch
+        B, n1 = tokens.shape
+        rows, V = B * n1, self.desc.vocab
+        i32, f32, u8 = torch.int32, torch.float32, torch.uint8
+        _check_tensors((("tokens", tokens, (B, n1), i32), ("parents", parents, (B, n1), i32)), cache.index)
+        room = [("q", q, rows if scalar else rows * V, f32), ("u", u, rows * 3, f32)]
+        for name, n, dt in (("accept", rows, u8), ("acc_prefix_len", rows, i32), ("resample_token", rows, i32),
+                            ("bonus_token", rows, i32), ("topk_ids", rows * k, i32),
+                            ("topk_probs", rows * k, f32), ("path", rows, i32), ("path_len", B, i32),
+                            ("next_token", B, i32), ("sibling_hit", B, u8), ("status", B, i32)):
+            room.append((name, outs[name], n, dt))
+        if outs["logits_out"] is not None:
+            room.append(("logits_out", outs["logits_out"], rows * V, f32))
+        _check_room(room, cache.index)
 
     def commit_kv_quant(self, cache: QuantCache, path, path_len, status, new_prefix_len) -> int:
         B, n1 = path.shape

@@ -327,3 +327,72 @@ def test_the_commit_refuses_arrays_that_overlap_what_is_written():
     for at in written:
         for kw in (dict(path=at), dict(path_len=at), dict(status=at), dict(new=at), dict(qc=quant(prefix=at))):
             refused(commit(**kw), "overlap")
+
+
+def verify_call(monkeypatch, dtype="f32"):
+    """verify_tree_quant's arguments for two sessions of three rows, on the CPU, which takes device
+    -1's place; the ABI call only counts."""
+    import torch
+    L, B, n1, V, k = 1, 2, 3, 64, 4
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    monkeypatch.setattr(A.Verifier, "_stream", staticmethod(lambda: 0))
+    made = []
+    monkeypatch.setattr(A, "acespec_verify_tree_quant", lambda *a: made.append(a) or 0)
+    ver = A.Verifier.__new__(A.Verifier)
+    ver.desc, ver.ctx, ver.V = A.ModelDesc(L, 64, 1, 1, 64, 64, V, 1e4, 1e-5, A.ACESPEC_F32), None, V
+    with monkeypatch.context() as m:
+        m.setattr(A, "_check_tensors", lambda *a: None)
+        cache = A.QuantCache(torch.zeros(L, B, 1, 2, 34 * 64, dtype=torch.uint8), torch.zeros(L, B, 1, 64, 64),
+                             torch.zeros(L, B, 1, 64, 64), 64, 64, torch.zeros(B, dtype=torch.int32))
+    cache.index = -1
+    i32 = dict(dtype=torch.int32)
+    args = dict(tokens=torch.zeros(B, n1, **i32), parents=torch.zeros(B, n1, **i32),
+                q=torch.zeros(B, n1, V), u=torch.zeros(B, n1, 3))
+    outs = ver.alloc_outputs(B * n1, B, n1, k, V, "cpu", True)
+
+    def call(scalar=False, top_k=k, drop=(), **kw):
+        a = {**args, **{n: t for n, t in kw.items() if n in args}}
+        o = {**outs, **{n: t for n, t in kw.items() if n not in args}}
+        return ver.verify_tree_quant(A.Weights(), cache, a["tokens"], a["parents"], a["q"], a["u"], 1.0, 0.9,
+                                     top_k, o, scalar=scalar)
+
+    return call, made, {**args, **outs}
+
+
+def test_the_verify_step_takes_what_it_needs_and_more(monkeypatch):
+    import torch
+    call, made, t = verify_call(monkeypatch)
+    call()
+    call(logits_out=None)
+    call(q=torch.zeros(2, 3), scalar=True)
+    call(q=t["q"].view(6, 64), u=torch.zeros(50), topk_ids=torch.zeros(9, 8, dtype=torch.int32))
+    assert len(made) == 4
+
+
+@pytest.mark.parametrize("name", ["tokens", "parents", "q", "u", "accept", "acc_prefix_len", "resample_token",
+                                  "bonus_token", "topk_ids", "topk_probs", "path", "path_len", "next_token",
+                                  "sibling_hit", "status", "logits_out"])
+def test_the_verify_step_refuses_tensors_that_it_would_leave(monkeypatch, name):
+    import torch
+    call, made, t = verify_call(monkeypatch)
+    x = t[name]
+    other = torch.int64 if x.dtype != torch.float32 else torch.float64
+    wide = torch.zeros(*x.shape, 2, dtype=x.dtype)[..., 0]         # strided
+    short = [] if name == "tokens" else [x[:-1].contiguous()]      # (tokens say how many rows there are)
+    for bad in [x.to(other), wide] + short:
+        with pytest.raises(ValueError, match=name):
+            call(**{name: bad})
+    if name not in ("tokens", "parents", "logits_out"):
+        with pytest.raises(ValueError, match=name):
+            call(**{name: None})
+    assert not made
+
+
+def test_the_verify_steps_room_goes_by_top_k_and_by_the_kind_of_draft(monkeypatch):
+    import torch
+    call, made, t = verify_call(monkeypatch)
+    with pytest.raises(ValueError, match="topk_ids"):
+        call(top_k=5)
+    with pytest.raises(ValueError, match="q must"):
+        call(q=torch.zeros(2, 3))                 # q_hat where the dense distributions are due
+    assert not made
