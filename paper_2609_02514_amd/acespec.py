@@ -376,12 +376,16 @@ def _check_room(want, index):
 class Verifier:
     """Owns a context for one model shape and turns torch tensors into ABI structs."""
 
+    index = None   # the GPU that the context's workspace is on
+
     def __init__(self, L, d, H, Hkv, hd, F, V, dtype: str, max_batch: int, max_nodes: int,
                  rope_base=10000.0, rms_eps=1e-5):
+        import torch
         self.desc = ModelDesc(L, d, H, Hkv, hd, F, V, rope_base, rms_eps,
                               ACESPEC_BF16 if dtype == "bf16" else ACESPEC_F32)
         self.V = V
         self.ctx = acespec_create(self.desc, max_batch, max_nodes)
+        self.index = torch.cuda.current_device()
         self._keep: List = []
 
     @classmethod
@@ -513,6 +517,8 @@ class Verifier:
         if cache.index != torch.cuda.current_device():
             raise ValueError(f"the cache is on cuda:{cache.index}, the current device and stream "
                              f"are cuda:{torch.cuda.current_device()}'s")
+        if self.index not in (None, cache.index):
+            raise ValueError(f"the context is on cuda:{self.index}, the cache on cuda:{cache.index}")
         if cache._fit != (d.n_layers, B, d.n_kv_heads, d.head_dim, d.dtype):
             raise ValueError(f"a cache of (layers, sessions, kv heads, head dim, dtype) {cache._fit} "
                              f"is not this model's and batch's "

@@ -396,3 +396,17 @@ def test_the_verify_steps_room_goes_by_top_k_and_by_the_kind_of_draft(monkeypatc
     with pytest.raises(ValueError, match="q must"):
         call(q=torch.zeros(2, 3))                 # q_hat where the dense distributions are due
     assert not made
+
+
+def test_a_context_of_another_device_is_refused_by_the_binding(monkeypatch):
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(A, "acespec_create", lambda *a: None)
+    ver = A.Verifier(2, 64, 2, 1, 64, 64, 64, "f32", 3, 4)
+    c = A.QuantCache.__new__(A.QuantCache)
+    c.index, c._fit = 1, (2, 3, 1, 64, A.ACESPEC_F32)
+    ver._check_quant(c, 3)
+    c.index = 0
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="context.*cuda:1"):
+        ver._check_quant(c, 3)
