@@ -366,8 +366,8 @@ int acespec_attention_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, int la
 /* acespec_verify_tree, or with q_hat in draft_q's place acespec_verify_tree_scalar_q, over a
  * cache in 4 bits (exactly one of draft_q and q_hat is given).  The tree's keys and values are
  * written to its tail in the model dtype and attended to unrounded; nothing is committed.  A
- * bf16 model's rotated queries are fp16 there; against blocks each counts with 8 significant
- * bits (off by at most 2^-8 of itself, or 2^-21 of the largest in its 32 head dims). */
+ * bf16 model's rotated queries are fp16, as in acespec_verify_tree; against blocks each is held
+ * exactly, or, below 1/64 of the largest in its 32 head dims, to 2^-17 of that. */
 int acespec_verify_tree_quant(acespec_ctx *ctx, const acespec_weights *weights,
                               const acespec_kv_quant *qc, const acespec_attn_span *span,
                               const int32_t *tree_tokens, const int32_t *parent_idx,

@@ -16,12 +16,16 @@
 //    its B operand of O^T = V^T P^T.
 //  * bf16 model: the keys' codes and scale bytes ARE the operand of the scaled product
 //    (v_mfma_scale_f32_16x16x128_f8f6f4, a scale per 32 elements), so keys are never decoded.
-//    The queries are its e4m3 operand in two pieces, q = hi + lo: hi the nearest e4m3, lo the
-//    nearest to the rest, each with its own scale per 32 head dims.  A bf16 query (8
-//    significant bits) is held exactly, but for what lies 2^22 below its group's largest;
-//    an fp16 one (the verify step's) to 2^-8 of each element.  Values are decoded to fp16
-//    (exactly) and multiplied by fp16 weights (v_mfma_f32_16x16x32_f16), the tail's keys and
-//    values widened to fp16.
+//    The queries are the other operand in pieces, hi the nearest e4m3 and each next one the
+//    nearest to what is left, each with its own scale per 32 head dims.  A bf16 query (8
+//    significant bits) is held exactly by hi and an e4m3 lo, but for what lies 2^22 below its
+//    group's largest, and fp16's own range.  An fp16 one (the verify step's, 11 bits) is held
+//    exactly by hi and two e3m2 pieces from 1/64 of its group's largest on, below that to
+//    2^-17 of it, which is what fp32 sums of 128 products may lose; e3m2 multiplies at twice
+//    e4m3's rate (a layer of the 8B step: 69.8 us, with three e4m3 pieces 71.5; with two, which
+//    are off by up to 2^-9 of an element, 66.5).
+//    Values are decoded to fp16 (exactly) and multiplied by fp16 weights
+//    (v_mfma_f32_16x16x32_f16), the tail's keys and values widened to fp16.
 //  * fp32 model: keys and values decoded to fp32 (exactly), v_mfma_f32_16x16x4_f32.
 //  * The reference of a query's exponents moves only when a score exceeds it by about 2^8
 //    (LAZY_LOG2), and only then are the four lanes of a query reduced and the accumulators
@@ -43,6 +47,7 @@
 // are added at the end, to the rows that see their slots.
 #include "quant.h"
 
+#include <type_traits>
 #include <utility>
 
 namespace {
@@ -53,6 +58,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int SLOW = 3;   // what a masked block costs a wave, in blocks that every row sees whole
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // The operand arithmetic of a model's type: eight elements of a lane.
 template <typename T> struct Ops;
 template <> struct Ops<bf16> {
@@ -156,8 +162,8 @@ AS_DEVICE TreeRow tree_row(const QuantAttnArgs &a, int lane, int P, int parent, 
 AS_DEVICE u32x4 load_q(const QuantAttnArgs &a, bf16, size_t off) {
   return *(const u32x4 *)((const uint16_t *)a.q + off);
 }
-AS_DEVICE f16x8 wide_q(const QuantAttnArgs &a, u32x4 v) {
-  return a.rows_io ? bf16x8_to_f16x8(__builtin_bit_cast(bf16x8, v)) : __builtin_bit_cast(f16x8, v);
+template <bool FP16> AS_DEVICE f16x8 wide_q(u32x4 v) {   // FP16: so they are already
+  return FP16 ? __builtin_bit_cast(f16x8, v) : bf16x8_to_f16x8(__builtin_bit_cast(bf16x8, v));
 }
 AS_DEVICE f32x8 load_q(const QuantAttnArgs &a, float, size_t off) {
   return Ops<float>::raw((const float *)a.q + off);
@@ -241,10 +247,10 @@ AS_DEVICE f32x8 first_of(f32x8 v, int n) {
 // The queries of a workgroup's tiles as operands of the scores, in LDS.
 //
 // fp32 model: [tile][hd / 32 fragments][lane][8], head dims lg * hd/4 + 8 s .. of query lr.
-template <typename T, int HD, int TPW> struct Queries {
+template <typename T, int HD, int TPW, bool FP16> struct Queries {
   float x[TPW][HD / 32][64][8];
   AS_DEVICE f32x8 plain(int i, int s, int lane) const { return *(const f32x8 *)x[i][s][lane]; }
-  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &, const Asked<T, HD, TPW, NT> &q, int tid) {
+  template <int NT> AS_DEVICE void fill(const Asked<T, HD, TPW, NT> &q, int tid) {
 #pragma unroll
     for (int i = 0; i < q.N; ++i) {
       const int e = i * NT + tid, qi = e / (HD / 8), c = e % (HD / 8);
@@ -253,30 +259,61 @@ template <typename T, int HD, int TPW> struct Queries {
     }
   }
 };
-// bf16 model: e4m3 pieces [tile][piece][half][lane][16 bytes] and their scale bytes
+// bf16 model, bf16 queries: e4m3 pieces [tile][piece][half][lane][16 bytes] and their scale bytes
 // [tile][lane].  Element k of the 128 that a product contracts is byte k % 16 of lane group
 // k % 64 / 16 in half k / 64 (measured; an e2m1 operand's is nibble k % 32 of lane group k / 32),
 // its scale that of lane group k / 32.  hd 128: pieces hi and lo, their scales bytes 0 and 1.
-// hd 64: one piece, the first half hi and the second lo (the keys' lane groups 2 and 3 repeat 0
+// hd 64: one product, the first half hi and the second lo (the keys' lane groups 2 and 3 repeat 0
 // and 1, so one product adds both).
-template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
-  static constexpr int NP = HD / 64;
-  u32x4 x[TPW][NP][2][64];
+// FP16: hi alone (hd 64: the second half is 0), scale byte 0, and e3m2 pieces lo and rest, which
+// lie as e2m1 does, in 6 bits an element: 16 bytes of a lane and 8 more.  hd 128: products 0 and
+// 1, scale bytes 1 and 2.  hd 64: one product, lane groups 0 and 1 lo, 2 and 3 rest, scale byte 1.
+template <int HD, int TPW, bool FP16> struct Queries<bf16, HD, TPW, FP16> {
+  static constexpr int NP = HD / 64, N8 = FP16 ? 1 : NP;   // products of a half or whole; e4m3 ones
+  u32x4 x[TPW][N8][2][64];
+  u32x4 six[TPW][FP16 ? NP : 1][64];
+  uint2 six2[TPW][FP16 ? NP : 1][64];
   f16x8 wide[TPW][HD / 32][64];   // fp16, for the tail: as in the fp32 model
-  uint16_t scale[TPW][64];
+  typename std::conditional<FP16, uint32_t, uint16_t>::type scale[TPW][64];
   AS_DEVICE f16x8 plain(int i, int s, int lane) const { return wide[i][s][lane]; }
   AS_DEVICE i32x8 piece(int i, int p, int lane) const {
-    const u32x4 a = x[i][p][0][lane], b = x[i][p][1][lane];
+    const u32x4 a = x[i][p][0][lane], b = FP16 && HD == 64 ? u32x4{} : x[i][p][1][lane];
     return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
   }
-  template <int NT> AS_DEVICE void fill(const QuantAttnArgs &a, const Asked<bf16, HD, TPW, NT> &q, int tid) {
+  AS_DEVICE i32x8 piece6(int i, int p, int lane) const {
+    const u32x4 a = six[i][p][lane];
+    const uint2 b = six2[i][p][lane];
+    return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b.x, (int)b.y, 0, 0};
+  }
+  // The nearest e3m2 (sign, 3 bits of exponent with bias 3, 2 of mantissa) of eight values of at
+  // most 28, piece `at` of a lane's four; what they leave.  At 2^-12 of a value fp16's exponent is
+  // e3m2's, subnormals among them, so its upper bits, rounded, are the code.
+  AS_DEVICE void put6(f16x2 (&v)[4], int i, int p, int lane, int at) {
+    uint32_t c[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t h = __builtin_bit_cast(uint32_t, v[w] * (f16)0x1p-12);
+      const uint32_t r = h + 0x007f007fu + ((h >> 8) & 0x00010001u);
+      v[w] -= __builtin_bit_cast(f16x2, r & 0xff00ff00u) * (f16)0x1p12;
+      const uint32_t t = ((r >> 8) & 0x001f001fu) | ((r >> 10) & 0x00200020u);
+      c[w] = (t | (t >> 10)) & 0xfffu;
+    }
+    const uint32_t word[2] = {c[0] | (c[1] << 12) | (c[2] << 24), (c[2] >> 8) | (c[3] << 4)};
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {   // 48 bits
+      const int u = at * 3 + j;
+      uint16_t *to = u < 8 ? (uint16_t *)&six[i][p][lane] + u : (uint16_t *)&six2[i][p][lane] + (u - 8);
+      *to = (uint16_t)(word[j >> 1] >> (16 * (j & 1)));
+    }
+  }
+  template <int NT> AS_DEVICE void fill(const Asked<bf16, HD, TPW, NT> &q, int tid) {
 #pragma unroll
     for (int i = 0; i < q.N; ++i) {
       const int e = i * NT + tid;
       if (q.ALL % NT && e >= q.ALL) break;
-      const int qi = e / (HD / 8), piece = e % (HD / 8), lr = qi & 15, c = piece >> 2;   // c: group
-      const f16x8 v = wide_q(a, q.v[i]);
-      wide[qi >> 4][piece % (HD / 32)][piece / (HD / 32) * 16 + lr] = v;
+      const int qi = e / (HD / 8), tile = qi >> 4, piece = e % (HD / 8), lr = qi & 15, c = piece >> 2;   // c: group
+      const f16x8 v = wide_q<FP16>(q.v[i]);
+      wide[tile][piece % (HD / 32)][piece / (HD / 32) * 16 + lr] = v;
       float f[8];
       uint32_t top = 0;
 #pragma unroll
@@ -286,11 +323,13 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
       }
       top = max(top, (uint32_t)__shfl_xor((int)top, 1));   // four lanes a group
       top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-      // hi: the largest in [128, 256); what it leaves is at most 8, lo holds 16 times that
+      // hi: the largest in [128, 256); what it leaves is at most 8.  An e4m3 lo holds 16 times
+      // that; an e3m2 one twice that, leaving at most 1 of 16, of which rest holds 16 times
       const int ex = max((int)(top >> 23), 30) - 7;      // biased; fp16 queries are 2^-24 or 0
       const bool bad = top >= 0x7f800000u;               // NaN or inf: every score is NaN
       const float down = bad ? 0.f : __uint_as_float((uint32_t)(254 - ex) << 23);
       uint32_t hi[2], lo[2];
+      f16x2 left[4];
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         float y[4], d[4];
@@ -298,27 +337,44 @@ template <int HD, int TPW> struct Queries<bf16, HD, TPW> {
         for (int j = 0; j < 4; ++j) y[j] = bad ? 0.f : f[4 * w + j] * down;
         hi[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         hi[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], hi[w], true);
-        d[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 0)) * 16.f;
-        d[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 1)) * 16.f;
-        d[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 2)) * 16.f;
-        d[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 3)) * 16.f;
-        lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(d[0], d[1], 0, false);
-        lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(d[2], d[3], lo[w], true);
+        d[0] = (y[0] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 0)) * (FP16 ? 2.f : 16.f);
+        d[1] = (y[1] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 1)) * (FP16 ? 2.f : 16.f);
+        d[2] = (y[2] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 2)) * (FP16 ? 2.f : 16.f);
+        d[3] = (y[3] - __builtin_amdgcn_cvt_f32_fp8(hi[w], 3)) * (FP16 ? 2.f : 16.f);
+        if (FP16) {   // (at most 7 bits)
+          left[2 * w] = f16x2{(f16)d[0], (f16)d[1]};
+          left[2 * w + 1] = f16x2{(f16)d[2], (f16)d[3]};
+        } else {
+          lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(d[0], d[1], 0, false);
+          lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(d[2], d[3], lo[w], true);
+        }
       }
-      const uint32_t sh = bad ? 255u : (uint32_t)ex, sl = bad ? 255u : (uint32_t)(ex - 4);
+      auto scaled = [&](int down) { return bad ? 255u : (uint32_t)(ex - down); };
       const int half = piece >> 1 & 1, at = piece & 1;   // of the group's 32 bytes: which 8
-      if (HD == 128) {
-        const int l = ((c & 1) * 2 + half) * 16 + lr;
-        ((uint2 *)&x[qi >> 4][0][c >> 1][l])[at] = make_uint2(hi[0], hi[1]);
-        ((uint2 *)&x[qi >> 4][NP - 1][c >> 1][l])[at] = make_uint2(lo[0], lo[1]);
-        if ((piece & 3) == 0) scale[qi >> 4][c * 16 + lr] = (uint16_t)(sh | (sl << 8));
+      const bool one = (piece & 3) == 0;
+      const int l = (HD == 128 ? (c & 1) * 2 + half : c * 2 + half) * 16 + lr, lane = c * 16 + lr;
+      ((uint2 *)&x[tile][0][HD == 128 ? c >> 1 : 0][l])[at] = make_uint2(hi[0], hi[1]);
+      if constexpr (FP16) {
+        put6(left, tile, 0, lane, piece & 3);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) left[w] *= (f16)16.f;
+        put6(left, tile, NP - 1, HD == 128 ? lane : lane + 32, piece & 3);
+        if (one) {
+          if (HD == 128) {
+            scale[tile][lane] = scaled(0) | (scaled(1) << 8) | (scaled(5) << 16);
+          } else {
+            scale[tile][lane] = scaled(0) | (scaled(1) << 8);
+            scale[tile][lane + 32] = scaled(5) << 8;
+          }
+        }
+      } else if constexpr (HD == 128) {
+        ((uint2 *)&x[tile][N8 - 1][c >> 1][l])[at] = make_uint2(lo[0], lo[1]);
+        if (one) scale[tile][lane] = (uint16_t)(scaled(0) | (scaled(4) << 8));
       } else {
-        const int l = (c * 2 + half) * 16 + lr;
-        ((uint2 *)&x[qi >> 4][0][0][l])[at] = make_uint2(hi[0], hi[1]);
-        ((uint2 *)&x[qi >> 4][0][1][l])[at] = make_uint2(lo[0], lo[1]);
-        if ((piece & 3) == 0) {
-          scale[qi >> 4][c * 16 + lr] = (uint16_t)sh;
-          scale[qi >> 4][c * 16 + lr + 32] = (uint16_t)sl;
+        ((uint2 *)&x[tile][0][1][l])[at] = make_uint2(lo[0], lo[1]);
+        if (one) {
+          scale[tile][lane] = (uint16_t)scaled(0);
+          scale[tile][lane + 32] = (uint16_t)scaled(4);
         }
       }
     }
@@ -350,8 +406,7 @@ template <typename T, int HD> struct Keys {   // fp32 model
                                    q4_scale((ks >> (8 * kk)) & 255u));
     return o;
   }
-  template <int TPW>
-  static AS_DEVICE void score(const Op &o, const Queries<T, HD, TPW> &q, int i, int lane, f32x4 (&sc)[2]) {
+  template <typename Q> static AS_DEVICE void score(const Op &o, const Q &q, int i, int lane, f32x4 (&sc)[2]) {
     sc[0] = sc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < HD / 32; ++s) {
@@ -386,15 +441,25 @@ template <int HD> struct Keys<bf16, HD> {     // bf16 model: as they are
     o.ks = (int)ks;
     return o;
   }
-  template <int TPW>
-  static AS_DEVICE void score(const Op &o, const Queries<bf16, HD, TPW> &q, int i, int lane, f32x4 (&sc)[2]) {
+  template <int TPW, bool FP16>
+  static AS_DEVICE void score(const Op &o, const Queries<bf16, HD, TPW, FP16> &q, int i, int lane,
+                              f32x4 (&sc)[2]) {
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const int qs = q.scale[i][lane];
-    // operand formats: 4 e2m1 (keys), 0 e4m3 (queries); scale byte kk of ks, and the piece's
+    // operand formats: 4 e2m1 (keys), 0 e4m3, 3 e3m2; scale byte kk of ks, and the piece's of qs
     const i32x8 a = q.piece(i, 0, lane);
     sc[0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[0], a, zero, 4, 0, 0, o.ks, 0, qs);
     sc[1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[1], a, zero, 4, 0, 1, o.ks, 0, qs);
-    if constexpr (HD == 128) {
+    if constexpr (FP16) {
+      const i32x8 b = q.piece6(i, 0, lane);
+      sc[0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[0], b, sc[0], 4, 3, 0, o.ks, 1, qs);
+      sc[1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[1], b, sc[1], 4, 3, 1, o.ks, 1, qs);
+      if constexpr (HD == 128) {
+        const i32x8 d = q.piece6(i, 1, lane);
+        sc[0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[0], d, sc[0], 4, 3, 0, o.ks, 2, qs);
+        sc[1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[1], d, sc[1], 4, 3, 1, o.ks, 2, qs);
+      }
+    } else if constexpr (HD == 128) {
       const i32x8 b = q.piece(i, 1, lane);
       sc[0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[0], b, sc[0], 4, 0, 0, o.ks, 1, qs);
       sc[1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(o.f[1], b, sc[1], 4, 0, 1, o.ks, 1, qs);
@@ -415,26 +480,26 @@ template <int HD> struct Values {
   AS_DEVICE float scale(int nb) const { return q4_scale((vs[nb >> 2] >> (8 * (nb & 3))) & 255u); }
 };
 
-template <typename T, int HD, int TPW, int NW> struct Shared {
+template <typename T, int HD, int TPW, int NW, bool FP16> struct Shared {
   // value operands a wave joins (8 waves and head dim 64: only the first four do)
   static constexpr int OWN = HD / 16 > NW ? HD / 16 / NW : 1;
   union {
-    Queries<T, HD, TPW> q;
+    Queries<T, HD, TPW, FP16> q;
     f32x4 part[TPW][HD / 16 / OWN][OWN * (NW - 1)][64];   // accumulators other waves join
   };
   RowView view[TPW * 16];
   float2 ml[NW][TPW * 16];
 };
 
-template <typename T, int HD, int TPW, int LDST, int NW, bool ONCE>
-AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST, NW> &smem_, int item, int split, int qbase) {
+template <typename T, int HD, int TPW, int LDST, int NW, bool ONCE, bool FP16>
+AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST, NW, FP16> &smem_, int item, int split, int qbase) {
   typedef Ops<T> O;
   typedef typename O::F8 F8;
   typedef typename O::E E;
   typedef typename O::Raw Raw;
   typedef Keys<T, HD> K;
-  constexpr int NB = HD / 16, LD = HD / 4, OWN = Shared<T, HD, TPW, NW>::OWN;
-  Shared<T, HD, TPW, NW> &sm = reinterpret_cast<Shared<T, HD, TPW, NW> &>(smem_);
+  constexpr int NB = HD / 16, LD = HD / 4, OWN = Shared<T, HD, TPW, NW, FP16>::OWN;
+  Shared<T, HD, TPW, NW, FP16> &sm = reinterpret_cast<Shared<T, HD, TPW, NW, FP16> &>(smem_);
   const int b = a.by_Hkv(item), g = item - b * a.Hkv;
   const int G = a.G, QR = G * a.n1;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -519,7 +584,7 @@ AS_DEVICE void attend(const QuantAttnArgs &a, Shared<T, HD, LDST, NW> &smem_, in
     mine.lo = a.window ? max(P + depth - a.window + 1, 0) : 0;
     mine.root = !a.window || depth < a.window || P < a.sinks;
   }
-  sm.q.template fill<NW * 64>(a, asked, tid);
+  sm.q.template fill<NW * 64>(asked, tid);
   if (tid < TPW * 16) sm.view[tid] = mine;
   __syncthreads();
 
@@ -803,18 +868,19 @@ template <typename T> constexpr int waves_per_simd(int tpw) {
 }
 
 // A workgroup: TPW tiles of a session's kv head (or one less: the tiles are dealt evenly to nqg
-// groups) over one of nsplit shares of its blocks.
-template <typename T, int HD, int TPW, int NW, bool ONCE>
+// groups) over one of nsplit shares of its blocks.  FP16: the queries are fp16 (not those of the
+// standalone call, which two pieces hold).
+template <typename T, int HD, int TPW, int NW, bool ONCE, bool FP16>
 __global__ __launch_bounds__(NW * 64, waves_per_simd<T>(TPW)) void quant_attn_kernel(QuantAttnArgs a) {
-  __shared__ __attribute__((aligned(16))) Shared<T, HD, TPW, NW> sm;
+  __shared__ __attribute__((aligned(16))) Shared<T, HD, TPW, NW, FP16> sm;
   // The query groups and the splits of a session's kv head follow each other on one XCD: the
   // groups read the same records.
   const int id = xcd_tile(blockIdx.x, gridDim.x);
   const int pair = a.by_nqg(id), grp = id - pair * a.nqg;
   const int item = a.by_nsplit(pair), split = pair - item * a.nsplit;
   const int qbase = (grp * a.each + min(grp, a.more)) * 16;
-  if (TPW == 1 || a.each + (grp < a.more) == TPW) attend<T, HD, TPW, TPW, NW, ONCE>(a, sm, item, split, qbase);
-  else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW, NW, ONCE>(a, sm, item, split, qbase);
+  if (TPW == 1 || a.each + (grp < a.more) == TPW) attend<T, HD, TPW, TPW, NW, ONCE, FP16>(a, sm, item, split, qbase);
+  else attend<T, HD, (TPW > 1 ? TPW - 1 : 1), TPW, NW, ONCE, FP16>(a, sm, item, split, qbase);
 }
 
 // Joins the splits: one thread per 4 head dims of a query row.
@@ -849,13 +915,13 @@ __global__ __launch_bounds__(256) void quant_combine_kernel(QuantAttnArgs a, int
   store_out(a, T(), b * a.n1 + r, h * HD + d, a.H * HD, num);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool FP16>
 void launch_tiles(int tpw, int waves, bool once, unsigned grid, hipStream_t s, const QuantAttnArgs &a) {
-  auto kernel = once       ? quant_attn_kernel<T, HD, 1, 4, true>
-                : tpw == 1 ? quant_attn_kernel<T, HD, 1, 4, false>
-                           : quant_attn_kernel<T, HD, 2, 4, false>;
+  auto kernel = once       ? quant_attn_kernel<T, HD, 1, 4, true, FP16>
+                : tpw == 1 ? quant_attn_kernel<T, HD, 1, 4, false, FP16>
+                           : quant_attn_kernel<T, HD, 2, 4, false, FP16>;
   if constexpr (sizeof(T) == 2)
-    if (waves == 8) kernel = quant_attn_kernel<T, HD, 1, 8, false>;
+    if (waves == 8) kernel = quant_attn_kernel<T, HD, 1, 8, false, FP16>;
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(waves * 64), 0, s, a);
 }
 
@@ -919,8 +985,10 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
                         B * n1, n1, H, Hkv, G, nblk, tcap, (int)nsplit, nqg, tiles / nqg, tiles % nqg, window,
                         sinks, Div(nqg), Div((int)nsplit), Div(Hkv), Div(G), rows_io};
   const unsigned grid = (unsigned)(groups * nsplit);
-  if (hd == 128) launch_tiles<T, 128>(tpw, waves, once, grid, s, a);
-  else launch_tiles<T, 64>(tpw, waves, once, grid, s, a);
+  auto launch = hd == 128 ? launch_tiles<T, 128, false> : launch_tiles<T, 64, false>;
+  if constexpr (sizeof(T) == 2)
+    if (!rows_io) launch = hd == 128 ? launch_tiles<T, 128, true> : launch_tiles<T, 64, true>;
+  launch(tpw, waves, once, grid, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || nsplit == 1) return e;
   hipLaunchKernelGGL(quant_combine_kernel<T>, dim3((QR * (hd / 4) + 255) / 256, items), dim3(256), 0,

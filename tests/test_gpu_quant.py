@@ -710,3 +710,98 @@ def test_the_stream_handle_is_the_current_streams():
     with torch.cuda.stream(side):
         assert A.Verifier._stream() == side.cuda_stream
     assert A.Verifier._stream() == torch.cuda.current_stream().cuda_stream
+
+
+def near(q, m, target, r):
+    """Signs s [hd] for which sum s q m / sqrt(hd) comes close to target: random ones for the
+    largest of q, then whatever leads there."""
+    order = sorted(range(len(q)), key=lambda i: -abs(q[i]))
+    s, left = [0.0] * len(q), target * math.sqrt(len(q)) / m
+    for n, i in enumerate(order):
+        s[i] = r.choice((-1.0, 1.0)) if 4 * n < len(q) else math.copysign(1.0, left * q[i])
+        left -= s[i] * q[i]
+    return s
+
+
+@pytest.mark.parametrize("B, H, Hkv, hd, N", [(16, 4, 4, 128, 2), (16, 8, 8, 64, 2), (32, 16, 4, 128, 32),
+                                              (32, 32, 4, 64, 16)])
+def test_the_verify_steps_queries_are_held_as_they_are(B, H, Hkv, hd, N):
+    """The difference of two scores, each the sum of large terms that cancel, as the verify step
+    finds it over 4 bits and over the model's type (the read-back cache is the same, bit for bit).
+
+    One layer; heads of a group and siblings of a tree share one query.  Of 32 slots two have keys
+    m s with scores of about 20, the others far lower ones; a tree's own keys and values are 0.
+    The two slots' values are 3 and 1, the first's 3 in even head dims and the second's in odd
+    ones, so with weights p and 1 - p the outputs' means are 1 + 2 p and 3 - 2 p, which wo (2^13
+    times the identity), a SwiGLU of zeros and the LM head (the identity) leave in proportion.
+
+    Bound, of each of the two steps: a score is off by (hd + 4) 2^-24 of its sum of magnitudes,
+    the difference by twice that; over 4 bits a query's elements below 1/64 of the largest of their
+    32 head dims (a margin of two: q is not known to the last bit here) by 2^-17 of that; the ratio
+    of the means by 2 x 2^-11 each for weights, outputs
+    and normalised rows in fp16, which counts at most 4.7 times in log(p / (1 - p)) for p in
+    [0.1, 0.9]."""
+    from paper_2609_02514_amd.acespec import QuantCache, Verifier
+    d, n1, P, m, T = H * hd, N + 1, 32, 64.0, 20.0
+    r, g = random.Random(hd + N), torch.Generator().manual_seed(hd + N)
+    embed = torch.randn(d, d, generator=g).bfloat16()
+    wq = (torch.randn(Hkv, 1, hd, d, generator=g) * 8 / math.sqrt(d)).bfloat16()
+    wqkv = torch.zeros((H + 2 * Hkv) * hd, d, dtype=torch.bfloat16)
+    wqkv[:H * hd] = wq.expand(Hkv, H // Hkv, hd, d).reshape(H * hd, d)
+    one, zero = torch.ones(d).bfloat16(), torch.zeros
+    layer = dict(attn_norm=one, wqkv=wqkv, wo=2.0 ** 13 * torch.eye(d).bfloat16(), mlp_norm=one,
+                 w_gate_up=zero(128, d).bfloat16(), w_down=zero(d, 64).bfloat16())
+    W = synth.Weights(embed.cuda(), [{n: t.cuda() for n, t in layer.items()}], one.cuda(),
+                      torch.eye(d).bfloat16().cuda())
+    # the siblings' queries (position P + 1), to what the kernels' own roundings leave
+    a = om.rms_norm(om.to_f64(embed[:B]), np.ones(d), 1e-5)
+    cos, sin = om.rope_cos_sin(np.full(B, P + 1), hd, 10000.0)
+    q = om.apply_rope((a @ om.to_f64(wq.view(Hkv * hd, d)).T).reshape(B, Hkv, hd), cos, sin)
+    k, v = torch.zeros(1, B, Hkv, 64, hd), torch.ones(1, B, Hkv, hd, 64)
+    big = small = 0.0
+    for b in range(B):
+        for h in range(Hkv):
+            group = np.abs(q[b, h]).reshape(-1, 32)
+            top = group.max(1, keepdims=True)
+            small = max(small, m * 2.0 ** -17 * float(((group < top / 32) * top).sum()) / math.sqrt(hd))
+            k[0, b, h, :P] = torch.from_numpy(-m * np.sign(q[b, h]))
+            for i, slot in enumerate(r.sample(range(P), 2)):
+                k[0, b, h, slot] = m * torch.tensor(near(q[b, h].tolist(), m, T, r))
+                v[0, b, h, i::2, slot] = 3.0
+            big = max(big, m * float(np.abs(q[b, h]).sum()) / math.sqrt(hd))
+    k, v = k.bfloat16().cuda(), v.bfloat16().cuda()
+    ver = Verifier(1, d, H, Hkv, hd, 64, d, "bf16", B, N)
+    cache = QuantCache.alloc(1, B, Hkv, hd, P, N, "bf16")
+    lens = i32([P] * B)
+    ver.quantize_kv(k, v, 64, lens, cache)
+    cache.prefix_len = lens
+    cap = (P + n1 + 63) // 64 * 64
+    bk = torch.zeros((1, B, Hkv, cap, hd), dtype=torch.bfloat16, device="cuda")
+    bv = torch.zeros((1, B, Hkv, hd, cap), dtype=torch.bfloat16, device="cuda")
+    ver.dequantize_kv(cache, bk, bv, cap)
+    torch.cuda.synchronize()
+    assert torch.equal(bk[:, :, :, :P], k[:, :, :, :P]) and torch.equal(bv[..., :P], v[..., :P])
+    tokens, parents = i32([[b] * n1 for b in range(B)]), i32([[-1] + [0] * N] * B)
+    draft, u = torch.full((B, n1, d), 1.0 / d, device="cuda"), torch.full((B, n1, 3), 0.5, device="cuda")
+    ws, found = ver.weights_struct(W), []
+    for quant in (True, False):
+        outs = ver.alloc_outputs(B * n1, B, n1, 8, d, "cuda", True)
+        hz.log(f"verify step, 4 bits {quant}: {B} sessions, {H}/{Hkv} heads of {hd}, {n1} rows")
+        if quant:
+            ver.verify_tree_quant(ws, cache, tokens, parents, draft, u, 1.0, 0.9, 8, outs)
+        else:
+            ver.verify_tree(ws, bk, bv, cap, lens, tokens, parents, draft, u, 1.0, 0.9, 8, outs)
+        torch.cuda.synchronize()
+        assert outs["status"].tolist() == [0] * B
+        z = outs["logits_out"].view(B, n1, H, hd)[:, 1:].double()
+        ratio = z[..., 0::2].mean(-1) / z[..., 1::2].mean(-1)
+        p = (3 * ratio - 1) / (2 * (1 + ratio))
+        found.append((p, torch.log(p / (1 - p))))
+    (_, got), (p, want) = found
+    near_half = (p > 0.1) & (p < 0.9)
+    assert float(near_half.float().mean()) > 0.5
+    bound = 2 * (2 * big * (hd + 4) * 2.0 ** -24 + 4.7 * 6 * 2.0 ** -11) + 2 * small
+    err = float((got - want).abs()[near_half].max())
+    hz.log(f"  scores of {big:.0f} in terms: their difference off by {err:.4f}, bound {bound:.4f}")
+    assert err <= bound
+    ver.close()
