@@ -307,7 +307,8 @@ int acespec_convert_v_cache(const void *src, void *dst, int planes, int capacity
 typedef struct {
   void *blocks;
   void *tail_k, *tail_v;
-  int capacity;                 /* slots in blocks; a positive multiple of 32             */
+  int capacity;                 /* slots in blocks; a positive multiple of 32.  Launches are
+                                   chosen by it: one far above the prefixes costs time    */
   int tail_capacity;            /* a multiple of 64; at least 31 + N + 1 where a tree of N
                                    drafted nodes is verified or committed               */
   const int32_t *prefix_len;    /* [B] DEVICE; at most capacity + 31                     */
@@ -332,8 +333,8 @@ typedef struct {
  *          prefix_len[b] outside [0, kv->capacity], beyond qc->capacity + 31, or first[b]
  *          outside [0, prefix_len[b]]; nothing of such a session is written.
  * kv->capacity is a multiple of 64; k, v, blocks and the tails are 16-byte aligned.  They do not
- * overlap, and what the call writes overlaps nothing else that is given.  Enqueued on stream;
- * ACESPEC_EINVAL before anything is launched for arguments outside the above. */
+ * overlap, and what the call writes overlaps nothing else that it reads or writes.  Enqueued on
+ * stream; ACESPEC_EINVAL before anything is launched for arguments outside the above. */
 int acespec_quantize_kv(acespec_ctx *ctx, const acespec_kv_cache *kv, const acespec_kv_quant *qc,
                         const int32_t *first, int B, int32_t *status, hipStream_t stream);
 
@@ -356,7 +357,8 @@ int acespec_dequantize_kv(acespec_ctx *ctx, const acespec_kv_quant *qc, const ac
  *  status [B]: ACESPEC_OK or ACESPEC_EBADTREE (parents, or prefix_len outside
  *          [0, capacity + 31]).
  * A bf16 model multiplies in fp16 with fp32 sums: queries, and keys and values of the tail,
- * beyond its range (65504) count as infinite.  A NaN or an infinity among the keys and values
+ * beyond its range (65504) count as infinite, and softmax weights below 2^-25 of a row's largest
+ * may count as 0.  A NaN or an infinity among the keys and values
  * reaches the rows that attend to its slot and no others. */
 int acespec_attention_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, int layer,
                             const acespec_attn_span *span, const void *q,

@@ -25,7 +25,9 @@
 //    e4m3's rate (a layer of the 8B step: 69.8 us, with three e4m3 pieces 71.5; with two, which
 //    are off by up to 2^-9 of an element, 66.5).
 //    Values are decoded to fp16 (exactly) and multiplied by fp16 weights
-//    (v_mfma_f32_16x16x32_f16), the tail's keys and values widened to fp16.
+//    (v_mfma_f32_16x16x32_f16), the tail's keys and values widened to fp16.  A weight is rounded
+//    once (2^-11 of it; below 2^-25 of the row's largest it may count as 0), their sum stays
+//    fp32: an output moves by 2e-4 in the norm, before it is rounded to bf16 by 1.7e-3.
 //  * fp32 model: keys and values decoded to fp32 (exactly), v_mfma_f32_16x16x4_f32.
 //  * The reference of a query's exponents moves only when a score exceeds it by about 2^8
 //    (LAZY_LOG2), and only then are the four lanes of a query reduced and the accumulators
@@ -34,8 +36,9 @@
 // At the end the waves of a workgroup, and then the splits of a session, are joined by their
 // (maximum, sum) pairs.
 //
-// What bounds it: a single row, HBM (64 sessions x 2048 slots x 8 kv heads of 128: 156 MB counted
-// in 25.3 us, 6.2 TB/s); 17 rows there, vector issue (69 % busy in 60.2 us; of a block's 760
+// What bounds it: a single row, the way from memory to L2 (64 sessions x 2048 slots x 8 kv heads of
+// 128: 156 MB counted there in 25.3 us, repeated, the MALL keeping some; 27.5 us with the records in
+// HBM, 5.7 TB/s); 17 rows there, vector issue (69 % busy in 60.2 us, 65 from HBM; of a block's 760
 // cycles for two tiles 300 decode the values, 176 are exponentials) and two rounds' fixed part of
 // about 9 us each (tail, queries, join); 65 rows over 16384 slots, vector issue (74 %, matrix
 // cores 50 %; 158.6 us, 140 GFLOP).  Few rows: the chain of loads, products and join, 6 to 10 us.
@@ -936,6 +939,10 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
                                   float *part_ml, long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                                   int capacity, int tcap, int window, int sinks, int rows_io,
                                   int cus, hipStream_t s) {
+  // The lengths are on the device, so that all that follows goes by the capacity: right for any
+  // prefix, chosen for long ones.  Much shorter prefixes pay for it (17 rows over 32 heads: 8
+  // sessions of 300 slots 8.1 us in a cache of 320 and 17.8 in one of 32768, of 2000 slots 19.3
+  // and 22.0; 64 of 2048 58.7 and 58.5).
   const int QR = H / Hkv * n1, tiles = (QR + 15) / 16, items = B * Hkv;
   const long long seen = window ? (long long)window + n1 + sinks + 2 * Q4_SLOTS : capacity;
   const int blocks_seen = (int)((seen < capacity ? seen : capacity) / Q4_SLOTS) + 3;
@@ -945,8 +952,8 @@ hipError_t launch_attention_quant(const void *q, const uint8_t *blocks, const T 
   // slots: 21 against 27).  Below 16 blocks eight waves have nothing to share.
   const bool wide = sizeof(T) == 4, few = work <= cus;
   const int waves = few && !wide && blocks_seen >= 16 ? 8 : 4;
-  // One tile a session (a token, as in plain decoding) otherwise, and more records than half the
-  // MALL keeps: they pass the caches (64 sessions x 2048 slots, 143 MB: 29.6 us against 31.8; 26
+  // One tile a session (a token, as in plain decoding) otherwise, and more than 96 MB of records:
+  // they pass the caches (64 sessions x 2048 slots, 143 MB: 29.6 us against 31.8; 26
   // MB, which a repeated call finds there: 13.9 against 12.4).
   const bool once = tiles == 1 && !few && items * (long long)blocks_seen * q4_bytes(hd) > (96 << 20);
   // Tiles a workgroup otherwise: two share a block's decoding and its read (70b fan-out: 85 us
