@@ -386,6 +386,95 @@ int acespec_commit_kv_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, const 
                             const int32_t *path_len, const int32_t *status, int B, int N,
                             int32_t *new_prefix_len, hipStream_t stream);
 
+/* ---- Sessions behind shared prefixes ----------------------------------------------------
+ * Prefixes that several sessions of a batch have in common (a system prompt, a document, the
+ * prompt of several samples) are held once, apart from the sessions' own caches, and attended to
+ * once for all rows of the sessions behind them.  A session behind a prefix of n slots that has P
+ * own slots in its acespec_kv_cache (prefix_len[b] = P) is at position n + P; own slot i is
+ * position n + i, and tree row r writes slot P + r.  acespec_commit_kv serves the own cache as it
+ * is.
+ *  blocks  [n_layers][prefixes][n_kv_heads][capacity / 64] records of 128 * head_dim elements, in
+ *          fp16 for a bf16 model (a value beyond its range counts as infinite, as in the verify
+ *          step) and in fp32 for an fp32 model.  A record holds 64 slots' keys and values in the
+ *          order of the attention's matrix operands; acespec_share_prefix writes it.
+ *  len     [prefixes] slots held, in [0, capacity]; what lies behind them is not read as numbers.
+ * One prefix and kv head takes less than 2 GiB (ACESPEC_EUNSUPPORTED otherwise). */
+typedef struct {
+  void *blocks;
+  int prefixes;                 /* >= 1                                                  */
+  int capacity;                 /* slots of each; a positive multiple of 64              */
+  const int32_t *len;           /* [prefixes] DEVICE                                     */
+} acespec_kv_shared;
+
+/* Gains [head_dim] in the model dtype, 16-byte aligned, of the RMSNorm (eps: the model's rms_eps)
+ * that each query head and each key head passes before its rotation; NULL: no norm there. */
+typedef struct {
+  const void *q_gain, *k_gain;
+} acespec_qk_norm;
+
+/* The calls of this section take arrays that are 16-byte aligned (the caches, blocks, q, qkv, out)
+ * and, for what one of them writes, apart from everything else that it is given (ACESPEC_EINVAL).
+ * prefix_of [B] DEVICE: the prefix that session b stands behind, or -1.  Any number of sessions may
+ * stand behind one, in any order.  status[b] is ACESPEC_EBADTREE for a malformed tree, a prefix_of
+ * outside [-1, prefixes), a len outside [0, capacity] or a prefix_len that leaves no room. */
+
+/* Takes sessions' first slots over into the store.  from [prefixes] DEVICE: the session of kv (of
+ * B) whose slots [0, count[p]) become prefix p, or -1: p is left as it is; count DEVICE, NULL: all
+ * prefix_len of them.  Behind the last slot its record is zeroed; later records are left as they
+ * were.  new_len [prefixes] DEVICE output: the slots of each prefix now (for -1 len[p]), or -1 for
+ * one that was refused (from outside [-1, B), count outside [0, prefix_len] or beyond capacity),
+ * of which nothing is written.  Copy it into len after the call. */
+int acespec_share_prefix(acespec_ctx *ctx, const acespec_kv_cache *kv, int B,
+                         const acespec_kv_shared *sh, const int32_t *from, const int32_t *count,
+                         int32_t *new_len, hipStream_t stream);
+
+/* Tree attention of one layer: row r of session b attends to its shared prefix, its own slots, its
+ * ancestors and itself, with scale 1/sqrt(head_dim).  q (rotated), out [B, N+1, n_heads, head_dim]
+ * in the model dtype; own slots prefix_len[b] + r hold the tree rows' keys and values.  A decode of
+ * single tokens is N = 0.  A bf16 model multiplies in fp16 with fp32 sums.  A NaN or an infinity
+ * among the keys and values reaches the rows that attend to its slot and no others. */
+int acespec_attention_shared(acespec_ctx *ctx, const acespec_kv_shared *sh, const int32_t *prefix_of,
+                             const acespec_kv_cache *kv, int layer, const void *q,
+                             const int32_t *parent_idx, int B, int N, void *out, int32_t *status,
+                             hipStream_t stream);
+
+/* From one layer's projection qkv [B, N+1, (n_heads + 2 n_kv_heads) head_dim] (model dtype; heads
+ * of q, k, v) in one pass: every query and key head normalised as norm says and rotated to its
+ * row's position (prefix, own slots and depth in the tree), q [B, N+1, n_heads, head_dim] written,
+ * and the keys and values into slots prefix_len[b] + r of kv's layer.  sh and prefix_of may be NULL
+ * (both): no session stands behind a prefix.  Nothing of a session with a bad status is written. */
+int acespec_qk_norm_rope(acespec_ctx *ctx, const acespec_qk_norm *norm, const acespec_kv_shared *sh,
+                         const int32_t *prefix_of, const acespec_kv_cache *kv, int layer,
+                         const void *qkv, const int32_t *parent_idx, int B, int N, void *q,
+                         int32_t *status, hipStream_t stream);
+
+/* acespec_verify_tree, or with q_hat in draft_q's place acespec_verify_tree_scalar_q, for sessions
+ * behind shared prefixes, for a decoder whose query and key heads are normalised, or for both.
+ *  norms  HOST array of n_layers entries, or NULL: no norms,
+ *  sh, prefix_of  both, or both NULL: no shared prefixes. */
+int acespec_verify_tree_shared(acespec_ctx *ctx, const acespec_weights *weights,
+                               const acespec_qk_norm *norms, const acespec_kv_shared *sh,
+                               const int32_t *prefix_of, const acespec_kv_cache *kv,
+                               const int32_t *tree_tokens, const int32_t *parent_idx,
+                               const float *draft_q, const float *q_hat, const float *uniforms,
+                               int B, int N, const acespec_params *params,
+                               const acespec_outputs *outs, hipStream_t stream);
+
+/* Sessions take over others' slots (a beam that goes on twice, samples of one session, a batch that
+ * closes its gaps, the rest of sessions whose front became a shared prefix): session b of dst gets
+ * slots [first[b], prefix_len) of session from[b] of src, as its slots from 0 on, in all layers;
+ * what lies behind them is left as it was.  from[b] = -1: session b stays as it is.  first NULL: 0.
+ *  src, dst  caches of src_batch and dst_batch sessions (each at most max_batch) that lie apart,
+ *          or one and the same (k, v, capacity and batch equal), where a session that receives
+ *          another's slots is no session's source, and one that is its own source (from[b] = b)
+ *          stays as it is.
+ *  new_prefix_len [dst_batch] DEVICE output: the session's slots now (for -1 dst's prefix_len), or
+ *          -1 for one that was refused (from, first or the lengths out of range, no room, or a
+ *          source that itself receives), of which nothing is written. */
+int acespec_fork_kv(acespec_ctx *ctx, const acespec_kv_cache *src, int src_batch,
+                    const acespec_kv_cache *dst, int dst_batch, const int32_t *from,
+                    const int32_t *first, int32_t *new_prefix_len, hipStream_t stream);
+
 /* Message for the last non-OK return on this thread ("" if none). */
 const char *acespec_last_error(void);
 

@@ -23,7 +23,9 @@ EXPORTED = ["acespec_create", "acespec_destroy", "acespec_verify_tree",
             "acespec_last_error", "acespec_timing_enable", "acespec_timing_read",
             "acespec_timing_only", "acespec_verify_tail_noalloc", "acespec_pack_weight",
             "acespec_convert_v_cache", "acespec_quantize_kv", "acespec_dequantize_kv",
-            "acespec_attention_quant", "acespec_verify_tree_quant", "acespec_commit_kv_quant"]
+            "acespec_attention_quant", "acespec_verify_tree_quant", "acespec_commit_kv_quant",
+            "acespec_share_prefix", "acespec_attention_shared", "acespec_qk_norm_rope",
+            "acespec_verify_tree_shared", "acespec_fork_kv"]
 
 
 class ModelDesc(C.Structure):
@@ -59,6 +61,15 @@ class KVQuant(C.Structure):
 
 class AttnSpan(C.Structure):
     _fields_ = [("window", C.c_int), ("sinks", C.c_int)]
+
+
+class KVShared(C.Structure):
+    _fields_ = [("blocks", C.c_void_p), ("prefixes", C.c_int), ("capacity", C.c_int),
+                ("len", C.c_void_p)]
+
+
+class QKNorm(C.Structure):
+    _fields_ = [("q_gain", C.c_void_p), ("k_gain", C.c_void_p)]
 
 
 class Params(C.Structure):
@@ -134,6 +145,28 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.acespec_commit_kv_quant.argtypes = [C.c_void_p, C.POINTER(KVQuant), C.c_void_p, C.c_void_p,
                                             C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
     lib.acespec_commit_kv_quant.restype = C.c_int
+    lib.acespec_share_prefix.argtypes = [C.c_void_p, C.POINTER(KVCache), C.c_int,
+                                         C.POINTER(KVShared), C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_void_p]
+    lib.acespec_share_prefix.restype = C.c_int
+    lib.acespec_attention_shared.argtypes = [C.c_void_p, C.POINTER(KVShared), C.c_void_p,
+                                             C.POINTER(KVCache), C.c_int, C.c_void_p, C.c_void_p,
+                                             C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.acespec_attention_shared.restype = C.c_int
+    lib.acespec_qk_norm_rope.argtypes = [C.c_void_p, C.POINTER(QKNorm), C.POINTER(KVShared),
+                                         C.c_void_p, C.POINTER(KVCache), C.c_int, C.c_void_p,
+                                         C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
+                                         C.c_void_p]
+    lib.acespec_qk_norm_rope.restype = C.c_int
+    lib.acespec_verify_tree_shared.argtypes = [C.c_void_p, C.POINTER(Weights), C.POINTER(QKNorm),
+                                               C.POINTER(KVShared), C.c_void_p, C.POINTER(KVCache),
+                                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                               C.c_void_p, C.c_int, C.c_int, C.POINTER(Params),
+                                               C.POINTER(Outputs), C.c_void_p]
+    lib.acespec_verify_tree_shared.restype = C.c_int
+    lib.acespec_fork_kv.argtypes = [C.c_void_p, C.POINTER(KVCache), C.c_int, C.POINTER(KVCache),
+                                    C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.acespec_fork_kv.restype = C.c_int
     lib.acespec_last_error.argtypes = []
     lib.acespec_last_error.restype = C.c_char_p
     lib.acespec_timing_enable.argtypes = [C.c_void_p, C.c_int]
@@ -264,6 +297,47 @@ def acespec_commit_kv_quant(ctx, qc: KVQuant, path: int, path_len: int, status: 
                                                  new_prefix_len, stream))
 
 
+def acespec_share_prefix(ctx, kv: KVCache, B: int, shared: KVShared, from_: int,
+                         count: Optional[int], new_len: int, stream: int) -> int:
+    return _check(load().acespec_share_prefix(ctx, C.byref(kv), B, C.byref(shared), from_, count,
+                                              new_len, stream))
+
+
+def acespec_attention_shared(ctx, shared: KVShared, prefix_of: int, kv: KVCache, layer: int, q: int,
+                             parent_idx: int, B: int, N: int, out: int, status: int,
+                             stream: int) -> int:
+    return _check(load().acespec_attention_shared(ctx, C.byref(shared), prefix_of, C.byref(kv), layer,
+                                                  q, parent_idx, B, N, out, status, stream))
+
+
+def acespec_qk_norm_rope(ctx, norm: QKNorm, shared: Optional[KVShared], prefix_of: Optional[int],
+                         kv: KVCache, layer: int, qkv: int, parent_idx: int, B: int, N: int, q: int,
+                         status: int, stream: int) -> int:
+    return _check(load().acespec_qk_norm_rope(ctx, C.byref(norm),
+                                              None if shared is None else C.byref(shared), prefix_of,
+                                              C.byref(kv), layer, qkv, parent_idx, B, N, q, status,
+                                              stream))
+
+
+def acespec_verify_tree_shared(ctx, weights: Weights, norms, shared: Optional[KVShared],
+                               prefix_of: Optional[int], kv: KVCache, tree_tokens: int,
+                               parent_idx: int, draft_q: Optional[int], q_hat: Optional[int],
+                               uniforms: int, B: int, N: int, params: Params, outputs: Outputs,
+                               stream: int) -> int:
+    """norms: an array of QKNorm, one a layer, or None."""
+    return _check(load().acespec_verify_tree_shared(ctx, C.byref(weights), norms,
+                                                    None if shared is None else C.byref(shared),
+                                                    prefix_of, C.byref(kv), tree_tokens, parent_idx,
+                                                    draft_q, q_hat, uniforms, B, N, C.byref(params),
+                                                    C.byref(outputs), stream))
+
+
+def acespec_fork_kv(ctx, src: KVCache, src_batch: int, dst: KVCache, dst_batch: int, from_: int,
+                    first: Optional[int], new_prefix_len: int, stream: int) -> int:
+    return _check(load().acespec_fork_kv(ctx, C.byref(src), src_batch, C.byref(dst), dst_batch, from_,
+                                         first, new_prefix_len, stream))
+
+
 def acespec_timing_enable(ctx, enable: bool) -> None:
     _check(load().acespec_timing_enable(ctx, 1 if enable else 0))
 
@@ -353,6 +427,52 @@ class QuantCache:
             moved = [n for n, t, at in zip(("blocks", "tail_k", "tail_v", "prefix_len"), self._tensors, self._at)
                      if t.data_ptr() != at]
             raise ValueError(f"the memory of {', '.join(moved)} moved after the cache was made (resize_ or set_)")
+        return self._struct
+
+
+class SharedPrefix:
+    """The tensors of a store of shared prefixes (acespec_kv_shared): blocks [L, P, Hkv,
+    capacity / 64, 128 hd] in float16 for a bf16 model and float32 for an fp32 one, len [P] int32,
+    contiguous on one GPU.  Shapes and types are checked here, once.  Only len can be assigned (what
+    share_prefix returned; checked again); a call refuses tensors whose memory has moved since."""
+
+    def __init__(self, blocks, capacity: int, lengths):
+        import torch
+        if blocks.dim() != 5 or blocks.dtype not in (torch.float16, torch.float32):
+            raise ValueError("blocks must have five dimensions, in float16 or float32")
+        L, P, Hkv, _, n = blocks.shape
+        self.index = blocks.get_device() if blocks.is_cuda else None   # the GPU's number
+        _check_tensors((("blocks", blocks, (L, P, Hkv, capacity // 64, n // 128 * 128), blocks.dtype),
+                        ("len", lengths, (P,), torch.int32)), self.index)
+        self._fit = (L, Hkv, n // 128, ACESPEC_BF16 if blocks.dtype == torch.float16 else ACESPEC_F32)
+        self._tensors = (blocks, lengths)
+        self._at = (_ptr(blocks), _ptr(lengths))
+        self._struct = KVShared(self._at[0], P, capacity, self._at[1])
+
+    blocks = property(lambda self: self._tensors[0])
+    len = property(lambda self: self._tensors[1])
+    prefixes = property(lambda self: self._struct.prefixes)
+    capacity = property(lambda self: self._struct.capacity)
+
+    @len.setter
+    def len(self, lengths):
+        _check_tensors((("len", lengths, self._tensors[1].shape, self._tensors[1].dtype),), self.index)
+        self._tensors = (self._tensors[0], lengths)
+        self._at = (self._at[0], _ptr(lengths))
+        self._struct = KVShared(self._at[0], self.prefixes, self.capacity, self._at[1])
+
+    @classmethod
+    def alloc(cls, L: int, P: int, Hkv: int, hd: int, capacity: int, dtype: str, device="cuda"):
+        """An empty store of P prefixes of up to `capacity` slots each."""
+        import torch
+        cap = (capacity + 63) // 64 * 64
+        return cls(torch.zeros((L, P, Hkv, cap // 64, 128 * hd), device=device,
+                               dtype=torch.float16 if dtype == "bf16" else torch.float32),
+                   cap, torch.zeros(P, dtype=torch.int32, device=device))
+
+    def struct(self) -> KVShared:
+        if (self._tensors[0].data_ptr(), self._tensors[1].data_ptr()) != self._at:
+            raise ValueError("the memory of blocks or len moved after the store was made (resize_ or set_)")
         return self._struct
 
 
@@ -573,20 +693,20 @@ class Verifier:
         """verify_tree over a cache in 4 bits; scalar: q is q_hat [B, N+1]."""
         B, n1 = tokens.shape
         self._check_quant(cache, B)
-        self._check_step(cache, tokens, parents, q, u, k, outs, scalar)
+        self._check_step(cache.index, tokens, parents, q, u, k, outs, scalar)
         return acespec_verify_tree_quant(self.ctx, wstruct, cache.struct(), AttnSpan(window, sinks),
                                          _ptr(tokens), _ptr(parents), None if scalar else _ptr(q),
                                          _ptr(q) if scalar else None, _ptr(u), B, n1 - 1,
                                          Params(T, top_p, k), self.outputs_struct(outs),
                                          self._stream())
 
-    def _check_step(self, cache: QuantCache, tokens, parents, q, u, k: int, outs: Dict, scalar: bool):
+    def _check_step(self, index: int, tokens, parents, q, u, k: int, outs: Dict, scalar: bool):
         """A verify step's inputs and outputs (those of alloc_outputs; they may be larger)."""
         import torch
         B, n1 = tokens.shape
         rows, V = B * n1, self.desc.vocab
         i32, f32, u8 = torch.int32, torch.float32, torch.uint8
-        _check_tensors((("tokens", tokens, (B, n1), i32), ("parents", parents, (B, n1), i32)), cache.index)
+        _check_tensors((("tokens", tokens, (B, n1), i32), ("parents", parents, (B, n1), i32)), index)
         room = [("q", q, rows if scalar else rows * V, f32), ("u", u, rows * 3, f32)]
         for name, n, dt in (("accept", rows, u8), ("acc_prefix_len", rows, i32), ("resample_token", rows, i32),
                             ("bonus_token", rows, i32), ("topk_ids", rows * k, i32),
@@ -595,7 +715,7 @@ class Verifier:
             room.append((name, outs[name], n, dt))
         if outs["logits_out"] is not None:
             room.append(("logits_out", outs["logits_out"], rows * V, f32))
-        _check_room(room, cache.index)
+        _check_room(room, index)
 
     def commit_kv_quant(self, cache: QuantCache, path, path_len, status, new_prefix_len) -> int:
         B, n1 = path.shape
@@ -608,3 +728,129 @@ class Verifier:
         return acespec_commit_kv_quant(self.ctx, cache.struct(), _ptr(path), _ptr(path_len),
                                        _ptr(status), B, n1 - 1, _ptr(new_prefix_len),
                                        self._stream())
+
+    def _here(self) -> int:
+        """The current GPU, which must be the context's."""
+        import torch
+        here = torch.cuda.current_device()
+        if self.index not in (None, here):
+            raise ValueError(f"the context is on cuda:{self.index}, the current device and stream are "
+                             f"cuda:{here}'s")
+        return here
+
+    def _types(self):
+        import torch
+        return torch.bfloat16 if self.desc.dtype == ACESPEC_BF16 else torch.float32, torch.int32
+
+    def _check_store(self, shared: SharedPrefix, index: int):
+        d = self.desc
+        if shared.index != index:
+            raise ValueError(f"the shared prefixes are on cuda:{shared.index}, the current device and "
+                             f"stream are cuda:{index}'s")
+        if shared._fit != (d.n_layers, d.n_kv_heads, d.head_dim, d.dtype):
+            raise ValueError(f"a store of (layers, kv heads, head dim, dtype) {shared._fit} is not this "
+                             f"model's {(d.n_layers, d.n_kv_heads, d.head_dim, d.dtype)}")
+
+    def _check_shared(self, shared: Optional[SharedPrefix], prefix_of, B: int, index: int):
+        if (shared is None) != (prefix_of is None):
+            raise ValueError("shared prefixes and prefix_of come together")
+        if shared is not None:
+            self._check_store(shared, index)
+            _check_tensors((("prefix_of", prefix_of, (B,), self._types()[1]),), index)
+
+    def _check_cache(self, kv_k, kv_v, capacity: int, lengths, index: int, name: str = "") -> KVCache:
+        """The tensors of a cache in the model's type, of len(lengths) sessions."""
+        d, (dt, i32) = self.desc, self._types()
+        shape = (d.n_layers, lengths.shape[0], d.n_kv_heads)
+        _check_tensors(((name + "kv_k", kv_k, (*shape, capacity, d.head_dim), dt),
+                        (name + "kv_v", kv_v, (*shape, d.head_dim, capacity), dt),
+                        (name + "prefix_len", lengths, (shape[1],), i32)), index)
+        return KVCache(_ptr(kv_k), _ptr(kv_v), capacity, _ptr(lengths))
+
+    def share_prefix(self, kv_k, kv_v, capacity: int, prefix_len, from_, shared: SharedPrefix, new_len,
+                     count=None) -> int:
+        """Sessions' first slots taken over as shared prefixes (acespec_share_prefix): from_ [P] the
+        sessions or -1, count [P] how many slots (None: all).  shared.len is not touched; new_len [P]
+        is written."""
+        index, i32 = self._here(), self._types()[1]
+        self._check_store(shared, index)
+        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
+        _check_tensors([(n, t, (shared.prefixes,), i32) for n, t in
+                        (("from_", from_), ("new_len", new_len), ("count", count)) if t is not None],
+                       index)
+        return acespec_share_prefix(self.ctx, kv, prefix_len.shape[0], shared.struct(), _ptr(from_),
+                                    _ptr(count), _ptr(new_len), self._stream())
+
+    def attention_shared(self, shared: SharedPrefix, prefix_of, kv_k, kv_v, capacity: int, prefix_len,
+                         layer: int, q, parents, out, status) -> int:
+        """Tree attention of one layer behind shared prefixes (acespec_attention_shared): q, out
+        [B, N+1, H, hd]."""
+        B, n1 = parents.shape
+        index, (dt, i32) = self._here(), self._types()
+        self._check_shared(shared, prefix_of, B, index)
+        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
+        shape = (B, n1, self.desc.n_heads, self.desc.head_dim)
+        _check_tensors((("q", q, shape, dt), ("out", out, shape, dt), ("parents", parents, (B, n1), i32),
+                        ("prefix_len", prefix_len, (B,), i32), ("status", status, (B,), i32)), index)
+        return acespec_attention_shared(self.ctx, shared.struct(), _ptr(prefix_of), kv, layer, _ptr(q),
+                                        _ptr(parents), B, n1 - 1, _ptr(out), _ptr(status),
+                                        self._stream())
+
+    def qk_norm_rope(self, qkv, q_gain, k_gain, kv_k, kv_v, capacity: int, prefix_len, layer: int,
+                     parents, q_out, status, shared: Optional[SharedPrefix] = None,
+                     prefix_of=None) -> int:
+        """One layer's projection [B, N+1, (H + 2 Hkv) hd] normalised per head (gains [hd] or None),
+        rotated and written to q_out [B, N+1, H, hd] and the cache (acespec_qk_norm_rope)."""
+        B, n1 = parents.shape
+        d, index, (dt, i32) = self.desc, self._here(), self._types()
+        self._check_shared(shared, prefix_of, B, index)
+        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
+        gains = [(n, t, (d.head_dim,), dt) for n, t in (("q_gain", q_gain), ("k_gain", k_gain))
+                 if t is not None]
+        _check_tensors([("qkv", qkv, (B, n1, (d.n_heads + 2 * d.n_kv_heads) * d.head_dim), dt),
+                        ("q_out", q_out, (B, n1, d.n_heads, d.head_dim), dt),
+                        ("parents", parents, (B, n1), i32), ("prefix_len", prefix_len, (B,), i32),
+                        ("status", status, (B,), i32)] + gains, index)
+        return acespec_qk_norm_rope(self.ctx, QKNorm(_ptr(q_gain), _ptr(k_gain)),
+                                    None if shared is None else shared.struct(), _ptr(prefix_of), kv,
+                                    layer, _ptr(qkv), _ptr(parents), B, n1 - 1, _ptr(q_out),
+                                    _ptr(status), self._stream())
+
+    def verify_tree_shared(self, wstruct: Weights, shared: Optional[SharedPrefix], prefix_of, kv_k, kv_v,
+                           capacity: int, prefix_len, tokens, parents, q, u, T: float, top_p: float,
+                           k: int, outs: Dict, norms=None, scalar: bool = False) -> int:
+        """verify_tree for sessions behind shared prefixes (or None, None); norms: a (q_gain, k_gain)
+        pair a layer, or None; scalar: q is q_hat [B, N+1]."""
+        B, n1 = tokens.shape
+        d, index, (dt, i32) = self.desc, self._here(), self._types()
+        self._check_shared(shared, prefix_of, B, index)
+        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
+        _check_tensors((("prefix_len", prefix_len, (B,), i32),), index)
+        self._check_step(index, tokens, parents, q, u, k, outs, scalar)
+        array = None
+        if norms is not None:
+            if len(norms) != d.n_layers:
+                raise ValueError(f"norms has {len(norms)} entries, the model {d.n_layers} layers")
+            _check_tensors([(f"norms[{l}]", t, (d.head_dim,), dt) for l, pair in enumerate(norms)
+                            for t in pair if t is not None], index)
+            array = (QKNorm * d.n_layers)(*[QKNorm(_ptr(a), _ptr(b)) for a, b in norms])
+        return acespec_verify_tree_shared(self.ctx, wstruct, array,
+                                          None if shared is None else shared.struct(), _ptr(prefix_of),
+                                          kv, _ptr(tokens), _ptr(parents), None if scalar else _ptr(q),
+                                          _ptr(q) if scalar else None, _ptr(u), B, n1 - 1,
+                                          Params(T, top_p, k), self.outputs_struct(outs),
+                                          self._stream())
+
+    def fork_kv(self, src_k, src_v, src_capacity: int, src_len, dst_k, dst_v, dst_capacity: int, dst_len,
+                from_, new_prefix_len, first=None) -> int:
+        """Sessions take over others' slots [first, src_len) (acespec_fork_kv): from_ [B of dst] the
+        sessions of src, or -1; src and dst may be the same tensors.  dst_len is not touched;
+        new_prefix_len is written."""
+        index, i32 = self._here(), self._types()[1]
+        src = self._check_cache(src_k, src_v, src_capacity, src_len, index, "src ")
+        dst = self._check_cache(dst_k, dst_v, dst_capacity, dst_len, index, "dst ")
+        B = dst_len.shape[0]
+        _check_tensors([(n, t, (B,), i32) for n, t in (("from_", from_), ("new_prefix_len", new_prefix_len),
+                                                       ("first", first)) if t is not None], index)
+        return acespec_fork_kv(self.ctx, src, src_len.shape[0], dst, B, _ptr(from_), _ptr(first),
+                               _ptr(new_prefix_len), self._stream())

@@ -37,13 +37,15 @@ int fail(int code, const char *fmt, ...) {
 
 enum Kind {
   K_TREE, K_EMBED, K_RMSNORM, K_GEMM_QKV, K_ROPE, K_ATTN, K_GEMM_O, K_GEMM_GATE_UP,
-  K_GEMM_DOWN, K_GEMM_LM, K_VOCAB, K_WALK, K_COMMIT, K_QUANTIZE, K_DEQUANTIZE, K_COUNT
+  K_GEMM_DOWN, K_GEMM_LM, K_VOCAB, K_WALK, K_COMMIT, K_QUANTIZE, K_DEQUANTIZE, K_QK_NORM,
+  K_SHARE, K_FORK, K_COUNT
 };
 const char *kKindNames[K_COUNT] = {"tree_prep",    "embed",       "rmsnorm",
                                    "gemm_qkv",     "rope_table",  "tree_attention",
                                    "gemm_o",       "gemm_gate_up", "gemm_down",
                                    "gemm_lm_head", "vocab_verify", "path_walk",
-                                   "commit_kv",    "quantize_kv", "dequantize_kv"};
+                                   "commit_kv",    "quantize_kv", "dequantize_kv",
+                                   "qk_norm_rope", "share_prefix", "fork_kv"};
 
 size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -71,6 +73,8 @@ struct acespec_ctx {
   size_t vsplit_bytes = 0;
   int32_t *rowflag = nullptr; // vocabulary kernel: per-row data-error code (0 = none)
   TreeMeta meta{};
+  SharedMeta shm{};           // the groups behind shared prefixes
+  float *sh_o = nullptr, *sh_ml = nullptr;  // partial results over them
   // timing
   bool timing = false;
   uint32_t timing_mask = ~0u;  // kinds timed while timing is on
@@ -173,7 +177,18 @@ struct CacheView {
   const int32_t *prefix_len;
   const acespec_kv_quant *quant;   // NULL: k and v hold the prefix too
   acespec_attn_span span;
+  const acespec_kv_shared *shared = nullptr;  // in front of the prefix, or NULL
+  const int32_t *prefix_of = nullptr;
+  const acespec_qk_norm *norms = nullptr;     // [n_layers] or NULL
 };
+
+SharedArgs shared_args(const acespec_kv_shared *sh, const int32_t *prefix_of) {
+  return sh ? SharedArgs{prefix_of, sh->len, sh->prefixes, sh->capacity} : SharedArgs{};
+}
+// Elements of one layer's records.
+size_t shared_layer_elems(const acespec_model_desc &d, const acespec_kv_shared *sh) {
+  return (size_t)sh->prefixes * d.n_kv_heads * sh->capacity * 2 * d.head_dim;
+}
 
 template <typename T>
 int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView &kv,
@@ -191,11 +206,16 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
                    w->layout == ACESPEC_LAYOUT_PACKED ? 1 : 0};
   float *logits = o->logits_out ? o->logits_out : ctx->logits;
   const TreeMeta &meta = ctx->meta;
+  const SharedArgs sh = shared_args(kv.shared, kv.prefix_of);
 
   if (kv.quant)
     RUN(K_TREE, launch_tree_prep_quant(tokens, parents, kv.prefix_len, B, n1, V,
                                        kv.quant->capacity, kv.span.window, kv.span.sinks, meta,
                                        o->status, stream));
+  else if (kv.shared)
+    RUN(K_TREE, launch_tree_prep_shared(tokens, parents, kv.prefix_len, B, n1, V, cap, sh, H / Hkv,
+                                        kSharedTile, meta, ctx->shm, o->status, nullptr, nullptr, 0,
+                                        stream));
   else
     RUN(K_TREE, launch_tree_prep(tokens, parents, kv.prefix_len, B, n1, V, cap, meta, o->status,
                                  stream));
@@ -211,7 +231,12 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
     const acespec_layer_weights &lw = w->layers[l];
     T *ck = (T *)kv.k + l * layer_stride;
     T *cv = (T *)kv.v + l * layer_stride;
-    const RopeOut<T> ro{x_q, ck, cv, ctx->rot, meta.sess_S, n1, H, Hkv, hd, cap};
+    RopeOut<T> ro{x_q, ck, cv, ctx->rot, meta.sess_S, n1, H, Hkv, hd, cap};
+    if (kv.norms) {
+      ro.q_gain = (const T *)kv.norms[l].q_gain;
+      ro.k_gain = (const T *)kv.norms[l].k_gain;
+      ro.eps = d.rms_eps;
+    }
     RUN(K_GEMM_QKV, (launch_qkv_rope<T, A>(x_a, (const T *)lw.wqkv, R, QKVN, D, ctx->qkv, ro,
                                            meta, B, aux, stream)));
     int nsplit = 1;
@@ -221,6 +246,11 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
                       ck, cv, meta, nullptr, nullptr, nullptr, x_attn, ctx->part_o, ctx->part_ml,
                       ctx->part_cap, B, n1, H, Hkv, hd, kv.quant->capacity, cap, kv.span.window, kv.span.sinks, 0, ctx->cus,
                       stream));
+    else if (kv.shared)
+      RUN(K_ATTN, launch_attention_shared<T>(
+                      x_q, (const A *)kv.shared->blocks + l * shared_layer_elems(d, kv.shared), sh,
+                      ctx->shm, ck, cv, meta, x_attn, 0, ctx->sh_o, ctx->sh_ml, ctx->part_o,
+                      ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd, cap, ctx->cus, stream));
     else
       RUN(K_ATTN, launch_attention<T>(x_q, ck, cv, meta, x_attn, ctx->part_o, ctx->part_ml,
                                       ctx->part_cap, B, n1, H, Hkv, hd, cap, ctx->cus, stream,
@@ -396,12 +426,25 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   for (int r = 1; r <= c->max_rows && r <= kVocabSplitRows; ++r)
     c->vsplit_bytes = std::max(c->vsplit_bytes, vocab_split_bytes(r, d.vocab));
   c->part_cap = layers ? ((long long)max_batch * d.n_kv_heads + 512) * QR * d.head_dim : 0;
+  {
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) == hipSuccess &&
+        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
+      c->cus = n;
+  }
+  const size_t shr = layers && d.dtype == ACESPEC_BF16   // partial rows, of all kv heads
+                         ? d.n_kv_heads * shared_part_rows((long long)(R * G), d.n_kv_heads, c->cus)
+                         : 0;
+  const size_t each = layers ? max_batch : 0;
   struct Part { size_t bytes; void **dst; };
   void *p_x = nullptr, *p_logits = nullptr, *p_po = nullptr, *p_pml = nullptr, *p_if = nullptr;
   void *p_qkv = nullptr, *p_gpart = nullptr, *p_rot = nullptr, *p_tmax = nullptr,
        *p_cand = nullptr, *p_rflag = nullptr;
   void *p_tok = nullptr, *p_par = nullptr, *p_pos = nullptr, *p_depth = nullptr,
        *p_anc = nullptr, *p_S = nullptr;
+  void *p_so = nullptr, *p_sml = nullptr, *p_slots = nullptr, *p_place = nullptr,
+       *p_first = nullptr, *p_order = nullptr, *p_units = nullptr, *p_groups = nullptr,
+       *p_total = nullptr;
   std::vector<Part> parts = {
       {R * d.d_model * 4, &p_x},
       {R * d.d_model * c->esz, &c->a},
@@ -420,7 +463,10 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
       {layers ? R * (size_t)d.head_dim / 2 * 8 : 0, &p_rot},
       {(size_t)8 * R * d.d_model * 4, &p_gpart},
       {R * 4, &p_tok}, {R * 4, &p_par}, {R * 4, &p_pos}, {R * 4, &p_depth}, {R * 8, &p_anc},
-      {(size_t)max_batch * 4, &p_S}};
+      {(size_t)max_batch * 4, &p_S},
+      {shr * d.head_dim * 4, &p_so}, {shr * 2 * 4, &p_sml},
+      {each * 4, &p_slots}, {each * 4, &p_place}, {each * 4, &p_first}, {each * 4, &p_order},
+      {each * 8, &p_units}, {each * sizeof(SharedGroup), &p_groups}, {layers ? 16u : 0u, &p_total}};
   size_t total = 0;
   for (auto &pt : parts) total += align_up(pt.bytes);
   if (hipMalloc(&c->ws, total) != hipSuccess) {
@@ -437,12 +483,6 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   c->qkv = (float *)p_qkv;
   c->gpart = (float *)p_gpart;
   c->gpart_cap = (long long)8 * R * d.d_model;
-  {
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) == hipSuccess &&
-        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
-      c->cus = n;
-  }
   c->logits = (float *)p_logits;
   c->part_o = (float *)p_po;
   c->part_ml = (float *)p_pml;
@@ -457,6 +497,11 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   c->meta.depth = (int32_t *)p_depth;
   c->meta.anc = (uint64_t *)p_anc;
   c->meta.sess_S = (int32_t *)p_S;
+  c->sh_o = (float *)p_so;
+  c->sh_ml = (float *)p_sml;
+  c->shm = SharedMeta{(int32_t *)p_slots, (int32_t *)p_place, (int32_t *)p_first,
+                      (int32_t *)p_order, (long long *)p_units, (SharedGroup *)p_groups,
+                      (long long *)p_total};
   if (layers) {
     std::vector<double> f(d.head_dim / 2);
     for (int i = 0; i < d.head_dim / 2; ++i)
@@ -537,12 +582,74 @@ int check_quant(const acespec_model_desc &d, const acespec_kv_quant *qc, int B, 
                       {"tail_v", qc->tail_v, tail, true}});
 }
 
+int check_batch(const acespec_ctx *ctx, int B, int N);
+
 int check_span(const acespec_attn_span *span, acespec_attn_span *out) {
   *out = span ? *span : acespec_attn_span{0, 0};
   if (out->window < 0 || out->sinks < 0)
     return fail(ACESPEC_EINVAL, "window and sinks must be >= 0 (got %d, %d)", out->window,
                 out->sinks);
   return ACESPEC_OK;
+}
+
+// One plane (layer, session, kv head) of an ordinary cache.
+size_t plane_bytes(const acespec_model_desc &d, int capacity) {
+  return (size_t)capacity * d.head_dim * (d.dtype == ACESPEC_BF16 ? 2 : 4);
+}
+size_t cache_bytes(const acespec_model_desc &d, int capacity, int B) {
+  return (size_t)d.n_layers * B * d.n_kv_heads * plane_bytes(d, capacity);
+}
+
+// A cache of B sessions with room for n1 tree rows (n1 0: no tree), as the calls below take it.
+int check_cache(const acespec_model_desc &d, const acespec_kv_cache *kv, int n1, const char *name) {
+  if (!kv || !kv->k || !kv->v || !kv->prefix_len)
+    return fail(ACESPEC_EINVAL, "%s or a pointer of it is NULL", name);
+  if (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15)
+    return fail(ACESPEC_EINVAL, "%s: k and v must be 16-byte aligned", name);
+  if (kv->capacity < 64 || kv->capacity % 64 != 0 || kv->capacity < n1)
+    return fail(ACESPEC_EINVAL,
+                "%s: capacity must be a positive multiple of 64 that holds the %d tree rows (got %d)",
+                name, n1, kv->capacity);
+  if (plane_bytes(d, kv->capacity) > 0xffffffffull)
+    return fail(ACESPEC_EUNSUPPORTED, "%s: more than 4 GiB of keys a session and head", name);
+  return ACESPEC_OK;
+}
+
+// A store of shared prefixes (behind which a cache of own_capacity slots stands).
+int check_shared(const acespec_model_desc &d, const acespec_kv_shared *sh, int own_capacity) {
+  if (!sh || !sh->blocks || !sh->len)
+    return fail(ACESPEC_EINVAL, "the shared prefixes or a pointer of them is NULL");
+  if ((uintptr_t)sh->blocks & 15) return fail(ACESPEC_EINVAL, "blocks must be 16-byte aligned");
+  if (sh->prefixes < 1) return fail(ACESPEC_EINVAL, "prefixes must be >= 1 (got %d)", sh->prefixes);
+  if (sh->capacity < 64 || sh->capacity % 64 != 0)
+    return fail(ACESPEC_EINVAL, "capacity must be a positive multiple of 64 (got %d)", sh->capacity);
+  if (2 * plane_bytes(d, sh->capacity) > 0x7fffffffull)   // (a kernel's offsets within a prefix)
+    return fail(ACESPEC_EUNSUPPORTED, "2 GiB or more a prefix and kv head");
+  if ((long long)sh->capacity + own_capacity > 0x7fffffff)
+    return fail(ACESPEC_EUNSUPPORTED, "positions beyond 2^31");
+  return ACESPEC_OK;
+}
+size_t shared_bytes(const acespec_model_desc &d, const acespec_kv_shared *sh) {
+  return d.n_layers * shared_layer_elems(d, sh) * (d.dtype == ACESPEC_BF16 ? 2 : 4);
+}
+
+// What a call over one layer of a cache behind shared prefixes needs (sh may be NULL with may).
+int check_layer(const acespec_ctx *ctx, const acespec_kv_shared *sh, const int32_t *prefix_of,
+                bool may, const acespec_kv_cache *kv, int layer, const int32_t *parent_idx, int B,
+                int N) {
+  if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
+  const acespec_model_desc &d = ctx->d;
+  if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
+  if (!parent_idx) return fail(ACESPEC_EINVAL, "parent_idx is NULL");
+  if (layer < 0 || layer >= d.n_layers)
+    return fail(ACESPEC_EINVAL, "layer must be in [0, %d) (got %d)", d.n_layers, layer);
+  int rc = check_batch(ctx, B, N);
+  if (!rc) rc = check_cache(d, kv, N + 1, "kv");
+  if (rc) return rc;
+  if ((sh != nullptr) != (prefix_of != nullptr))
+    return fail(ACESPEC_EINVAL, "shared prefixes and prefix_of come together (one of them is NULL)");
+  if (!sh && may) return ACESPEC_OK;
+  return check_shared(d, sh, kv->capacity);
 }
 
 int check_batch(const acespec_ctx *ctx, int B, int N) {
@@ -561,7 +668,8 @@ int verify_tree_checked(acespec_ctx *ctx, const acespec_weights *w, const acespe
                         const int32_t *tree_tokens, const int32_t *parent_idx,
                         const float *draft_q, const float *q_scalar, const float *uniforms,
                         int B, int N, const acespec_params *p, const acespec_outputs *o,
-                        hipStream_t stream) {
+                        hipStream_t stream, const acespec_qk_norm *norms = nullptr,
+                        const acespec_kv_shared *sh = nullptr, const int32_t *prefix_of = nullptr) {
   g_err.clear();
   if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
   const acespec_model_desc &d = ctx->d;
@@ -588,13 +696,15 @@ int verify_tree_checked(acespec_ctx *ctx, const acespec_weights *w, const acespe
     rc = check_quant(d, qc, B, N + 1);
     if (!rc) rc = check_span(span, &view.span);
     if (rc) return rc;
-    view = CacheView{qc->tail_k, qc->tail_v, qc->tail_capacity, qc->prefix_len, qc, view.span};
+    view = CacheView{qc->tail_k, qc->tail_v, qc->tail_capacity, qc->prefix_len, qc, view.span,
+                     nullptr, nullptr, nullptr};
   } else {
     if (kv->capacity < N + 1)
       return fail(ACESPEC_EINVAL, "kv capacity %d cannot hold the %d tree rows", kv->capacity, N + 1);
     if (kv->capacity % 64 != 0)
       return fail(ACESPEC_EINVAL, "kv capacity must be a multiple of 64 (got %d)", kv->capacity);
-    view = CacheView{kv->k, kv->v, kv->capacity, kv->prefix_len, nullptr, {0, 0}};
+    view = CacheView{kv->k, kv->v, kv->capacity, kv->prefix_len, nullptr, {0, 0}, sh, prefix_of,
+                     norms};
   }
   rc = check_params(p, d.vocab);
   if (rc) return rc;
@@ -998,6 +1108,214 @@ int acespec_timing_read(acespec_ctx *ctx, const char **names, double *total_ms, 
     ctx->launches[k] = 0;
   }
   return n;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------
+// Sessions behind shared prefixes
+// ------------------------------------------------------------------------------------
+extern "C" {
+
+int acespec_share_prefix(acespec_ctx *ctx, const acespec_kv_cache *kv, int B,
+                         const acespec_kv_shared *sh, const int32_t *from, const int32_t *count,
+                         int32_t *new_len, hipStream_t stream) {
+  g_err.clear();
+  if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
+  const acespec_model_desc &d = ctx->d;
+  if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
+  if (!from || !new_len) return fail(ACESPEC_EINVAL, "a required pointer is NULL (only count may be)");
+  int rc = check_batch(ctx, B, 0);
+  if (!rc) rc = check_cache(d, kv, 0, "kv");
+  if (!rc) rc = check_shared(d, sh, 0);
+  if (rc) return rc;
+  const size_t held = cache_bytes(d, kv->capacity, B), each = (size_t)sh->prefixes * sizeof(int32_t);
+  rc = check_apart({{"k", kv->k, held, false},
+                    {"v", kv->v, held, false},
+                    {"blocks", sh->blocks, shared_bytes(d, sh), true},
+                    {"prefix_len", kv->prefix_len, (size_t)B * sizeof(int32_t), false},
+                    {"len", sh->len, each, false},
+                    {"from", from, each, false},
+                    {"count", count, each, false},
+                    {"new_len", new_len, each, true}});
+  if (rc) return rc;
+  if ((long long)d.n_layers * d.n_kv_heads * sh->prefixes * (sh->capacity / 64) > 0xffffffLL)
+    return fail(ACESPEC_EUNSUPPORTED, "more records than one launch takes");
+  const SharedArgs sa = shared_args(sh, nullptr);
+  if (d.dtype == ACESPEC_BF16)
+    RUN(K_SHARE, launch_share_prefix<bf16>((const bf16 *)kv->k, (const bf16 *)kv->v, kv->prefix_len, B,
+                                           kv->capacity, sh->blocks, sa, from, count, new_len,
+                                           d.n_layers, d.n_kv_heads, d.head_dim, stream));
+  else
+    RUN(K_SHARE, launch_share_prefix<float>((const float *)kv->k, (const float *)kv->v, kv->prefix_len,
+                                            B, kv->capacity, sh->blocks, sa, from, count, new_len,
+                                            d.n_layers, d.n_kv_heads, d.head_dim, stream));
+  return ACESPEC_OK;
+}
+
+int acespec_attention_shared(acespec_ctx *ctx, const acespec_kv_shared *sh, const int32_t *prefix_of,
+                             const acespec_kv_cache *kv, int layer, const void *q,
+                             const int32_t *parent_idx, int B, int N, void *out, int32_t *status,
+                             hipStream_t stream) {
+  g_err.clear();
+  int rc = check_layer(ctx, sh, prefix_of, false, kv, layer, parent_idx, B, N);
+  if (rc) return rc;
+  if (!q || !out || !status) return fail(ACESPEC_EINVAL, "a required pointer is NULL");
+  if (((uintptr_t)q | (uintptr_t)out) & 15)
+    return fail(ACESPEC_EINVAL, "q and out must be 16-byte aligned");
+  const acespec_model_desc &d = ctx->d;
+  const int n1 = N + 1, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
+  const size_t io = (size_t)B * n1 * H * hd * ctx->esz, held = cache_bytes(d, kv->capacity, B);
+  const size_t each = (size_t)B * sizeof(int32_t);
+  rc = check_apart({{"blocks", sh->blocks, shared_bytes(d, sh), false},
+                    {"len", sh->len, (size_t)sh->prefixes * sizeof(int32_t), false},
+                    {"prefix_of", prefix_of, each, false},
+                    {"k", kv->k, held, false},
+                    {"v", kv->v, held, false},
+                    {"prefix_len", kv->prefix_len, each, false},
+                    {"parent_idx", parent_idx, each * n1, false},
+                    {"q", q, io, false},
+                    {"out", out, io, true},
+                    {"status", status, each, true}});
+  if (rc) return rc;
+  const SharedArgs sa = shared_args(sh, prefix_of);
+  const size_t own = (size_t)layer * B * Hkv * kv->capacity * hd;
+  const size_t rec = layer * shared_layer_elems(d, sh);
+  const bool b16 = d.dtype == ACESPEC_BF16;
+  RUN(K_TREE, launch_tree_prep_shared(nullptr, parent_idx, kv->prefix_len, B, n1, d.vocab,
+                                      kv->capacity, sa, H / Hkv, kSharedTile, ctx->meta, ctx->shm,
+                                      status, b16 ? (const bf16 *)q : nullptr, (f16 *)ctx->q, H * hd,
+                                      stream));
+  if (b16)
+    RUN(K_ATTN, launch_attention_shared<bf16>(
+                    (const f16 *)ctx->q, (const f16 *)sh->blocks + rec, sa, ctx->shm,
+                    (const bf16 *)kv->k + own, (const bf16 *)kv->v + own, ctx->meta, out, 1, ctx->sh_o,
+                    ctx->sh_ml, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
+                    kv->capacity, ctx->cus, stream));
+  else
+    RUN(K_ATTN, launch_attention_shared<float>(
+                    (const float *)q, (const float *)sh->blocks + rec, sa, ctx->shm,
+                    (const float *)kv->k + own, (const float *)kv->v + own, ctx->meta, out, 1,
+                    ctx->sh_o, ctx->sh_ml, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv,
+                    hd, kv->capacity, ctx->cus, stream));
+  return ACESPEC_OK;
+}
+
+int acespec_qk_norm_rope(acespec_ctx *ctx, const acespec_qk_norm *norm, const acespec_kv_shared *sh,
+                         const int32_t *prefix_of, const acespec_kv_cache *kv, int layer,
+                         const void *qkv, const int32_t *parent_idx, int B, int N, void *q,
+                         int32_t *status, hipStream_t stream) {
+  g_err.clear();
+  int rc = check_layer(ctx, sh, prefix_of, true, kv, layer, parent_idx, B, N);
+  if (rc) return rc;
+  if (!norm || !qkv || !q || !status) return fail(ACESPEC_EINVAL, "a required pointer is NULL");
+  if (((uintptr_t)qkv | (uintptr_t)q | (uintptr_t)norm->q_gain | (uintptr_t)norm->k_gain) & 15)
+    return fail(ACESPEC_EINVAL, "qkv, q and the gains must be 16-byte aligned");
+  if (B > 65535) return fail(ACESPEC_EUNSUPPORTED, "more than 65535 sessions");
+  const acespec_model_desc &d = ctx->d;
+  const int n1 = N + 1, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
+  const size_t row = (size_t)B * n1 * hd * ctx->esz, held = cache_bytes(d, kv->capacity, B);
+  const size_t each = (size_t)B * sizeof(int32_t), gain = hd * ctx->esz;
+  rc = check_apart({{"q_gain", norm->q_gain, gain, false},
+                    {"k_gain", norm->k_gain, gain, false},
+                    {"len", sh ? sh->len : nullptr, sh ? (size_t)sh->prefixes * sizeof(int32_t) : 0, false},
+                    {"prefix_of", prefix_of, each, false},
+                    {"k", kv->k, held, true},
+                    {"v", kv->v, held, true},
+                    {"prefix_len", kv->prefix_len, each, false},
+                    {"qkv", qkv, row * (H + 2 * Hkv), false},
+                    {"parent_idx", parent_idx, each * n1, false},
+                    {"q", q, row * H, true},
+                    {"status", status, each, true}});
+  if (rc) return rc;
+  const SharedArgs sa = shared_args(sh, prefix_of);
+  const size_t own = (size_t)layer * B * Hkv * kv->capacity * hd;
+  if (d.dtype == ACESPEC_BF16)
+    RUN(K_QK_NORM, (launch_qk_norm_rope<bf16, bf16, bf16>(
+                       (const bf16 *)qkv, 1, (const bf16 *)norm->q_gain, (const bf16 *)norm->k_gain,
+                       d.rms_eps, ctx->inv_freq, TreeMeta{}, parent_idx, kv->prefix_len, sa, status,
+                       (bf16 *)q, (bf16 *)kv->k + own, (bf16 *)kv->v + own, nullptr, B, n1, H, Hkv, hd,
+                       kv->capacity, stream)));
+  else
+    RUN(K_QK_NORM, (launch_qk_norm_rope<float, float, float>(
+                       (const float *)qkv, 1, (const float *)norm->q_gain, (const float *)norm->k_gain,
+                       d.rms_eps, ctx->inv_freq, TreeMeta{}, parent_idx, kv->prefix_len, sa, status,
+                       (float *)q, (float *)kv->k + own, (float *)kv->v + own, nullptr, B, n1, H, Hkv,
+                       hd, kv->capacity, stream)));
+  return ACESPEC_OK;
+}
+
+int acespec_verify_tree_shared(acespec_ctx *ctx, const acespec_weights *w,
+                               const acespec_qk_norm *norms, const acespec_kv_shared *sh,
+                               const int32_t *prefix_of, const acespec_kv_cache *kv,
+                               const int32_t *tree_tokens, const int32_t *parent_idx,
+                               const float *draft_q, const float *q_hat, const float *uniforms, int B,
+                               int N, const acespec_params *p, const acespec_outputs *o,
+                               hipStream_t stream) {
+  g_err.clear();
+  if ((draft_q != nullptr) == (q_hat != nullptr))
+    return fail(ACESPEC_EINVAL, "exactly one of draft_q and q_hat must be given");
+  const int rc = check_layer(ctx, sh, prefix_of, true, kv, 0, parent_idx, B, N);
+  if (rc) return rc;
+  const acespec_model_desc &d = ctx->d;
+  const size_t held = cache_bytes(d, kv->capacity, B);
+  for (int l = 0; norms && l < d.n_layers; ++l)
+    if (((uintptr_t)norms[l].q_gain | (uintptr_t)norms[l].k_gain) & 15)
+      return fail(ACESPEC_EINVAL, "the gains must be 16-byte aligned (layer %d)", l);
+  if (norms && B > 65535) return fail(ACESPEC_EUNSUPPORTED, "more than 65535 sessions");
+  if (sh) {
+    const int apart = check_apart({{"blocks", sh->blocks, shared_bytes(d, sh), false},
+                                   {"k", kv->k, held, true},
+                                   {"v", kv->v, held, true}});
+    if (apart) return apart;
+  }
+  return verify_tree_checked(ctx, w, kv, nullptr, nullptr, tree_tokens, parent_idx, draft_q, q_hat,
+                             uniforms, B, N, p, o, stream, norms, sh, prefix_of);
+}
+
+int acespec_fork_kv(acespec_ctx *ctx, const acespec_kv_cache *src, int src_batch,
+                    const acespec_kv_cache *dst, int dst_batch, const int32_t *from,
+                    const int32_t *first, int32_t *new_prefix_len, hipStream_t stream) {
+  g_err.clear();
+  if (!ctx) return fail(ACESPEC_EINVAL, "ctx is NULL");
+  const acespec_model_desc &d = ctx->d;
+  if (d.n_layers < 1) return fail(ACESPEC_EINVAL, "the model has no layers (no KV cache)");
+  if (!from || !new_prefix_len)
+    return fail(ACESPEC_EINVAL, "a required pointer is NULL (only first may be)");
+  int rc = check_batch(ctx, src_batch, 0);
+  if (!rc) rc = check_batch(ctx, dst_batch, 0);
+  if (!rc) rc = check_cache(d, src, 0, "src");
+  if (!rc) rc = check_cache(d, dst, 0, "dst");
+  if (rc) return rc;
+  const size_t sb = cache_bytes(d, src->capacity, src_batch), db = cache_bytes(d, dst->capacity, dst_batch);
+  const size_t each = (size_t)dst_batch * sizeof(int32_t), have = (size_t)src_batch * sizeof(int32_t);
+  // the same cache on both sides, or two that lie apart
+  const bool same = src->k == dst->k && src->v == dst->v && src_batch == dst_batch &&
+                    src->capacity == dst->capacity;
+  rc = check_apart({{"src k", same ? nullptr : src->k, sb, false},
+                    {"src v", same ? nullptr : src->v, sb, false},
+                    {"dst k", dst->k, db, true},
+                    {"dst v", dst->v, db, true},
+                    {"src prefix_len", src->prefix_len, have, false},
+                    {"dst prefix_len", dst->prefix_len, each, false},
+                    {"from", from, each, false},
+                    {"first", first, each, false},
+                    {"new_prefix_len", new_prefix_len, each, true}});
+  if (rc) return rc;
+  const int least = src->capacity < dst->capacity ? src->capacity : dst->capacity;
+  if ((long long)d.n_layers * d.n_kv_heads * dst_batch * ((least + 255) / 256) > 0xffffffLL)
+    return fail(ACESPEC_EUNSUPPORTED, "more slots than one launch takes");
+  if (d.dtype == ACESPEC_BF16)
+    RUN(K_FORK, launch_fork_kv<bf16>((const bf16 *)src->k, (const bf16 *)src->v, src->prefix_len,
+                                     src_batch, src->capacity, (bf16 *)dst->k, (bf16 *)dst->v,
+                                     dst->prefix_len, dst_batch, dst->capacity, from, first,
+                                     new_prefix_len, d.n_layers, d.n_kv_heads, d.head_dim, stream));
+  else
+    RUN(K_FORK, launch_fork_kv<float>((const float *)src->k, (const float *)src->v, src->prefix_len,
+                                      src_batch, src->capacity, (float *)dst->k, (float *)dst->v,
+                                      dst->prefix_len, dst_batch, dst->capacity, from, first,
+                                      new_prefix_len, d.n_layers, d.n_kv_heads, d.head_dim, stream));
+  return ACESPEC_OK;
 }
 
 }  // extern "C"

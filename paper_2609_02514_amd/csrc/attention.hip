@@ -144,8 +144,11 @@ AS_DEVICE void issue_chunk(uint16_t *stage, __amdgpu_buffer_rsrc_t kr,
 
 // bf16 -> fp16 in place for pieces t, t + stride, ... of a stage (t: the thread's index
 // among the widening threads); value slots >= total are zeroed.
-template <int HD>
-AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int total) {
+// PART: values that are not finite are zeroed in the tree's slots (>= S) too, and the slots
+// marked in bad (two words); add_marked brings them to the rows that see them.
+template <int HD, bool PART = false>
+AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int total, int S = 0,
+                           uint32_t *bad = nullptr) {
   constexpr int KPIECES = KC * HD / 8;
   const bool tail = key0 + KC > total;
   for (int pc = t; pc < 2 * KPIECES; pc += stride) {
@@ -158,11 +161,39 @@ AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int tot
       for (int e = 0; e < 8; ++e)
         if (s0 + e >= total) h[e] = (f16)0.f;
     }
+    if (PART && key0 + KC > S && pc >= KPIECES) {
+      const int vp = pc - KPIECES, row = vp >> 3;
+      const int i0 = ((vp & 7) ^ vsw(row)) << 3;   // slot within the chunk
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (key0 + i0 + e >= S && !(fabsf((float)h[e]) <= 65504.f)) {
+          h[e] = (f16)0.f;
+          atomicOr(bad + ((i0 + e) >> 5), 1u << ((i0 + e) & 31));
+        }
+    }
     *(f16x8 *)p = h;
   }
 }
 
-template <int HD, int NW, int UPW, int NST>
+// The values that widen_chunk took out of a tree chunk, added to o for a row that sees their
+// slots: an infinity or a NaN stays one whatever weight it has.  dim(i): head dim of o's i-th
+// element.
+template <int N, typename F>
+AS_DEVICE void add_marked(float (&o)[N], F dim, const uint32_t *bad, const bf16 *vb, int capacity,
+                          int key0, int S, uint64_t anc) {
+  for (int w = 0; w < 2; ++w)
+    for (uint32_t rest = bad[w]; rest; rest &= rest - 1) {
+      const int slot = key0 + w * 32 + __builtin_ctz(rest), j = slot - S;   // (a tree row, marked)
+      if (j > 0 && !((anc >> (j - 1)) & 1ull)) continue;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float v = (float)(f16)(float)vb[(size_t)dim(i) * capacity + slot];
+        if (!(fabsf(v) <= 65504.f)) o[i] += v;
+      }
+    }
+}
+
+template <int HD, int NW, int UPW, int NST, bool PART = false>
 __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     const f16 *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
@@ -172,6 +203,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
   constexpr int L_DMA = HD / 4 / NW;     // DMA instructions per wave per chunk
   static_assert(NST >= 3, "the widening runs one stage ahead of the MFMAs");
   __shared__ __attribute__((aligned(1024))) uint16_t smem[NST * STAGE];
+  __shared__ uint32_t s_bad[PART ? 2 * NST : 1];   // a stage's marked slots (widen_chunk)
 
   const int g = blockIdx.y, b = blockIdx.z;
   const int G = H / Hkv, QR = G * n1;
@@ -236,8 +268,10 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     for (int nb = 0; nb < NB; ++nb) o[t][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   wait_vmcnt<0>();   // the loop's vmcnt accounting covers the DMA only
+  if (PART && tid < 2 * NST) s_bad[tid] = 0;   // (before the prologue's barrier)
 
   auto stage_of = [&](int c) { return smem + ((c - c0) % NST) * STAGE; };
+  auto bad_of = [&](int c) { return PART ? s_bad + ((c - c0) % NST) * 2 : nullptr; };
   // The widening goes to the waves without a tile when there are any (one SIMD then
   // holds no more than its share of tile work plus widening), else to every wave.
   const int wbeg = ntiles < NW ? ntiles : 0;
@@ -251,7 +285,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
   if (c0 < c1) {
     if (c0 + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
     lds_barrier();
-    if (widener) widen_chunk<HD>(stage_of(c0), wt, wstride, c0 * KC, total);
+    if (widener) widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad_of(c0));
   }
 
   // Fragment offsets: the swizzles depend on the lane only, so the read of K block kk at
@@ -274,7 +308,8 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     chunk_barrier();
     if (c + NST - 1 < c1)
       issue_chunk<HD, NW>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity, wave, lane);
-    if (c + 1 < c1 && widener) widen_chunk<HD>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total);
+    if (c + 1 < c1 && widener)
+      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad_of(c + 1));
 
     const uint16_t *st = stage_of(c);
     const f16 *sk = (const f16 *)st;
@@ -346,6 +381,15 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
           const f16x8 va = *(const f16x8 *)(sv + voff[ks] + nb * 16 * KC);
           o[t][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[ks], o[t][nb], 0, 0, 0);
         }
+      if (PART && tree_chunk && (bad_of(c)[0] | bad_of(c)[1])) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          float ob[4] = {o[t][nb][0], o[t][nb][1], o[t][nb][2], o[t][nb][3]};
+          add_marked(ob, [&](int e) { return nb * 16 + lg * 4 + e; }, bad_of(c), vb, capacity, key0,
+                     S, anc[t]);
+          o[t][nb] = f32x4{ob[0], ob[1], ob[2], ob[3]};
+        }
+      }
     }
     if (quarter) {
       // One 16-key block (key block qk of the chunk) of the split tile: 4 scores a lane.
@@ -444,7 +488,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += wj[j] * v[e];
           }
-          if (nsplit == 1) {
+          if (!PART && nsplit == 1) {
             const float inv = L > 0.f ? 1.0f / L : 0.f;
             f16x4 v;
 #pragma unroll
@@ -455,7 +499,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
             *(f32x4 *)(part_o + (item * QR + qi) * HD + nb * 16 + lg * 4) = acc;
           }
         }
-        if (nsplit > 1 && qk == 0 && lg == 0) {
+        if ((PART || nsplit > 1) && qk == 0 && lg == 0) {
           const size_t item = ((size_t)b * Hkv + g) * nsplit + split;
           part_ml[(item * QR + qi) * 2 + 0] = M;
           part_ml[(item * QR + qi) * 2 + 1] = L;
@@ -473,7 +517,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     const int qi = (tbase + tile) * 16 + lr;
     if (qi >= QR) continue;
     const int r = qi / G, h = g * G + (qi - r * G);
-    if (nsplit == 1) {
+    if (!PART && nsplit == 1) {
       const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -532,7 +576,7 @@ AS_DEVICE float halves_sum(float v) {
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
-template <int HD, int NST>
+template <int HD, int NST, bool PART = false>
 __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     const f16 *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
@@ -546,6 +590,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   constexpr int L_DMA = HD / 4 / NW;
   static_assert(NST >= 3, "the widening runs one stage ahead of the MFMAs");
   __shared__ __attribute__((aligned(1024))) uint16_t smem[NST * STAGE];
+  __shared__ uint32_t s_bad[PART ? 2 * NST : 1];   // a stage's marked slots (widen_chunk)
 
   const int g = blockIdx.y, b = blockIdx.z;
   const int G = H / Hkv, QR = G * n1;
@@ -622,8 +667,10 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     for (int nb = 0; nb < NB16; ++nb) oq[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   wait_vmcnt<0>();   // the loop's vmcnt accounting covers the DMA only
+  if (PART && tid < 2 * NST) s_bad[tid] = 0;   // (before the prologue's barrier)
 
   auto stage_of = [&](int c) { return smem + ((c - c0) % NST) * STAGE; };
+  auto bad_of = [&](int c) { return PART ? s_bad + ((c - c0) % NST) * 2 : nullptr; };
   const int wt = tid, wstride = NW * 64;   // every wave widens its share
 
   // Prologue: chunks c0 .. c0+NST-2 in flight, chunk c0 widened.
@@ -634,7 +681,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   if (c0 < c1) {
     if (c0 + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
     lds_barrier();
-    widen_chunk<HD>(stage_of(c0), wt, wstride, c0 * KC, total);
+    widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad_of(c0));
   }
 
   // Fragment offsets (lane registers; blocks add compile-time constants): K row p32(lq)
@@ -662,7 +709,8 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     if (c + NST - 1 < c1)
       issue_chunk<HD, NW, true>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity,
                                 wave, lane);
-    if (c + 1 < c1) widen_chunk<HD>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total);
+    if (c + 1 < c1)
+      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad_of(c + 1));
 
     const uint16_t *st = stage_of(c);
     const f16 *sk = (const f16 *)st;
@@ -736,6 +784,17 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
           }
       }
       SCHED_FENCE();
+      if (PART && tree_chunk && (bad_of(c)[0] | bad_of(c)[1])) {
+#pragma unroll
+        for (int i = 0; i < 4 * NDB; ++i) {
+          const int db = i >> 2, j = i & 3;
+          float ob[4] = {o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
+          add_marked(ob, [&](int e) { return 32 * db + 8 * j + 4 * hh + e; }, bad_of(c), vb, capacity,
+                     key0, S, anc);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[db][4 * j + e] = ob[e];
+        }
+      }
     }
     if (quarter) {
       // key block qk of the chunk for the remainder tile: 4 scores a lane
@@ -781,6 +840,15 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
       for (int nb = 0; nb < NB16; ++nb) {
         const f16x4 va = *(const f16x4 *)(sv + qvoff + nb * 16 * KC);
         oq[nb] = __builtin_amdgcn_mfma_f32_16x16x16f16(va, pq, oq[nb], 0, 0, 0);
+      }
+      if (PART && tree_chunk && qk == 0 && (bad_of(c)[0] | bad_of(c)[1])) {   // (once a tile)
+#pragma unroll
+        for (int nb = 0; nb < NB16; ++nb) {
+          float ob[4] = {oq[nb][0], oq[nb][1], oq[nb][2], oq[nb][3]};
+          add_marked(ob, [&](int e) { return nb * 16 + lg * 4 + e; }, bad_of(c), vb, capacity, key0,
+                     S, ancq);
+          oq[nb] = f32x4{ob[0], ob[1], ob[2], ob[3]};
+        }
       }
     }
   }
@@ -830,7 +898,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += wj[j] * v[e];
           }
-          if (nsplit == 1) {
+          if (!PART && nsplit == 1) {
             const float inv = L > 0.f ? 1.0f / L : 0.f;
             f16x4 v;
 #pragma unroll
@@ -840,7 +908,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
             *(f32x4 *)(part_o + (item * QR + qi) * HD + nb * 16 + lg * 4) = acc;
           }
         }
-        if (nsplit > 1 && qk == 0 && lg == 0) {
+        if ((PART || nsplit > 1) && qk == 0 && lg == 0) {
           part_ml[(item * QR + qi) * 2 + 0] = M;
           part_ml[(item * QR + qi) * 2 + 1] = L;
         }
@@ -854,7 +922,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     const int qi = rlo + wave * 32 + lq;
     if (qi < rlo + rows) {
       const int r = qi / G, h = g * G + (qi - r * G);
-      if (nsplit == 1) {
+      if (!PART && nsplit == 1) {
         const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
@@ -1012,25 +1080,21 @@ __global__ __launch_bounds__(256) void tree_attn_f32_kernel(
 // Ring depth: 4 stages of 32 KB (head_dim 128) or 16 KB (head_dim 64).
 template <int HD> struct AttnCfg { static constexpr int NST = 4; };
 
-template <int HD, int NW, int UPW>
+template <int HD, int NW, int UPW, bool PART>
 void launch_mfma(dim3 grid, hipStream_t s, const f16 *q, const bf16 *ck, const bf16 *cv,
                  const TreeMeta &meta, f16 *out, float *po, float *pml, int n1, int H, int Hkv,
                  int capacity, int nsplit, int tpg) {
-  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, AttnCfg<HD>::NST>), grid,
+  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, AttnCfg<HD>::NST, PART>), grid,
                      dim3(NW * 64), 0, s, q, ck, cv, meta, out, po, pml, n1, H, Hkv,
                      capacity, nsplit, tpg);
 }
 
-}  // namespace
-
-namespace acespec {
-
-template <>
-hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
-                                  const TreeMeta &meta, f16 *out, float *part_o,
-                                  float *part_ml, long long part_capacity, int B, int n1, int H,
-                                  int Hkv, int hd, int capacity, int cus, hipStream_t s,
-                                  int *nsplit_used) {
+// The kernels of one layer, without the merge of their splits.
+template <bool PART>
+hipError_t launch_tree_attn(const f16 *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
+                            f16 *out, float *part_o, float *part_ml, long long part_capacity, int B,
+                            int n1, int H, int Hkv, int hd, int capacity, int cus, hipStream_t s,
+                            int *nsplit_used) {
   const int G = H / Hkv, QR = G * n1;
   const int all_tiles = (QR + 15) / 16;
   if (capacity % KC != 0) return hipErrorInvalidValue;
@@ -1062,26 +1126,49 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
   const dim3 grid(nsplit * nqg, Hkv, B);
   if (t32) {
     if (hd == 128)
-      hipLaunchKernelGGL((tree_attn_t32_kernel<128, AttnCfg<128>::NST>), grid, dim3(512), 0, s,
+      hipLaunchKernelGGL((tree_attn_t32_kernel<128, AttnCfg<128>::NST, PART>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
                          rpg);
     else
-      hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST>), grid, dim3(512), 0, s,
+      hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, PART>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
                          rpg);
   } else if (hd == 128) {
-    launch_mfma<128, 16, 1>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+    launch_mfma<128, 16, 1, PART>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
                             capacity, nsplit, all_tiles);
   } else {
-    launch_mfma<64, 16, 1>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+    launch_mfma<64, 16, 1, PART>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
                            capacity, nsplit, all_tiles);
   }
-  hipError_t e = hipGetLastError();
+  return hipGetLastError();
+}
+
+}  // namespace
+
+namespace acespec {
+
+template <>
+hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
+                                  const TreeMeta &meta, f16 *out, float *part_o,
+                                  float *part_ml, long long part_capacity, int B, int n1, int H,
+                                  int Hkv, int hd, int capacity, int cus, hipStream_t s,
+                                  int *nsplit_used) {
+  const hipError_t e = launch_tree_attn<false>(q, ck, cv, meta, out, part_o, part_ml, part_capacity, B,
+                                               n1, H, Hkv, hd, capacity, cus, s, nsplit_used);
+  const int nsplit = *nsplit_used;
   if (e != hipSuccess || nsplit == 1) return e;
-  const int cblocks = (QR * (hd / 4) + 255) / 256;
+  const int QR = H / Hkv * n1, cblocks = (QR * (hd / 4) + 255) / 256;
   hipLaunchKernelGGL(attn_combine_kernel, dim3(cblocks, Hkv, B), dim3(256), 0, s, part_o,
                      part_ml, out, n1, H, Hkv, hd, nsplit);
   return hipGetLastError();
+}
+
+hipError_t launch_attention_part(const f16 *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
+                                 float *part_o, float *part_ml, long long part_capacity, int B,
+                                 int n1, int H, int Hkv, int hd, int capacity, int cus,
+                                 hipStream_t s, int *nsplit) {
+  return launch_tree_attn<true>(q, ck, cv, meta, nullptr, part_o, part_ml, part_capacity, B, n1, H,
+                                Hkv, hd, capacity, cus, s, nsplit);
 }
 
 template <>

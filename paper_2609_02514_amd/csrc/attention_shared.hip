@@ -1,0 +1,421 @@
+// Tree attention for sessions that stand behind shared prefixes.
+//
+// A row's keys are its session's shared prefix, the session's own slots, and its ancestors in the
+// tree: with scores z and base-2 exponents, o = sum 2^(z - m) v / sum 2^(z - m) over all of them.
+// The sum over the shared slots is the same product for every session of a group, so it is
+// computed for all their query rows at once: the group's members * G * (N + 1) rows of a kv head
+// against the prefix's records, a matrix product with a softmax between, where a session alone
+// would stream the prefix for G * (N + 1) rows.  The own slots are the tree attention's work
+// (attention.hip); both leave partial (sum, max, outputs) and one pass joins them.
+#include "common.h"
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LAZY_LOG2 = 8.f;   // the exponent's reference moves once a weight passes 2^8
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int TM = acespec::kSharedTile;
+
+AS_DEVICE float halves_max(float v) {
+  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+AS_DEVICE float halves_sum(float v) {
+  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+AS_DEVICE void block_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Units of work (a record for a tile of TM rows) lie on a line: group after group, tile after
+// tile, record after record.  Workgroup w of `wgs` takes [w U / wgs, (w + 1) U / wgs) of a kv
+// head's line, so that all finish together whatever the lengths; a tile that is cut leaves
+// several partial results.  At least `least` units a workgroup, and no more workgroups than units.
+AS_DEVICE int working(long long units, int wgs) {
+  constexpr int least = 4;
+  const long long n = (units + least - 1) / least;
+  return (int)(n < wgs ? n : wgs);
+}
+AS_DEVICE long long line_begin(int w, long long units, int wgs) { return w * units / wgs; }
+// the workgroup that takes unit u
+AS_DEVICE int worker_of(long long u, long long units, int wgs) {
+  return (int)(((u + 1) * wgs - 1) / units);
+}
+// Where the partial rows of (a group's first member, tile, workgroup) begin, of one kv head: rows
+// and workgroups both only grow along the line, so no two meet.
+AS_DEVICE long long part_base(int first, int QR, long long tile, int w) {
+  return (long long)first * QR + (tile + w) * TM;
+}
+
+// Eight waves, 32 query rows each, over one record after the other.  A record is 1 KB operands of
+// v_mfma_f32_32x32x16_f16 in the order in which they are multiplied: keys (rows are slots, in an
+// order that makes a lane's scores 8 neighbouring slots) for S^T = K Q^T, then values (rows are
+// head dims) for O^T = V^T P^T.  A lane's scores, as fp16 weights, are its operand of the second
+// product, so they never leave its registers.  Records come by DMA into a ring of NST stages.
+template <int HD, int NST>
+__global__ __launch_bounds__(512) void shared_attn_kernel(
+    const f16 *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
+    float *__restrict__ part_o, float *__restrict__ part_ml, int n1, int H, int Hkv, int cap,
+    int wgs, long long rows_total) {
+  constexpr int KS = HD / 16, NDB = HD / 32;
+  constexpr int REC = 128 * HD;                 // elements of a record
+  constexpr int L_DMA = REC * 2 / 1024 / 8;     // 1 KB pieces a wave
+  __shared__ __attribute__((aligned(1024))) f16 smem[NST * REC];
+  const int t = xcd_tile(blockIdx.x, gridDim.x), g = t / wgs, w = t - g * wgs;
+  const long long units = sm.total[0];
+  const int groups = (int)sm.total[1], wk = working(units, wgs);
+  if (w >= wk) return;
+  long long u = line_begin(w, units, wk);
+  const long long uend = line_begin(w + 1, units, wk);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lq = lane & 31, hh = lane >> 5;
+  const int G = H / Hkv, QR = G * n1;
+  const float sscale = LOG2E / sqrtf((float)HD), lazy = LAZY_LOG2 / sscale;
+  int gi = 0;
+  while (gi + 1 < groups && sm.groups[gi + 1].units <= u) ++gi;
+
+  while (u < uend) {
+    while (gi + 1 < groups && sm.groups[gi + 1].units <= u) ++gi;
+    const SharedGroup grp = sm.groups[gi];
+    const int nblk = (grp.slots + 63) >> 6, rows = grp.members * QR;
+    const int tile = (int)((u - grp.units) / nblk), c0 = (int)(u - grp.units - (long long)tile * nblk);
+    const int c1 = (int)min((long long)nblk, c0 + (uend - u));
+    u += c1 - c0;
+    const int row = tile * TM + wave * 32 + lq;   // of the group
+    const bool any = tile * TM + wave * 32 < rows;
+    const f16 *kv = blocks + (((size_t)grp.prefix * Hkv + g) * (cap >> 6) + c0) * REC;
+    const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(kv, (uint32_t)(c1 - c0) * (REC * 2));
+    auto issue = [&](int c) {
+      const int i = c - c0;
+#pragma unroll
+      for (int j = 0; j < L_DMA; ++j) {
+        const int piece = j * 8 + wave;
+        buf_dma16(rsrc, (lds_ptr_t)(smem + (i % NST) * REC + piece * 512), lane * 16,
+                  i * (REC * 2) + piece * 1024);
+      }
+    };
+    // queries: rows of padding multiply zeros
+    f16x8 qf[KS];
+    {
+      const int rr = min(row, rows - 1), m = rr / QR, rem = rr - m * QR, r = rem / G;
+      const f16 *qp = q + ((size_t)sm.order[grp.first + m] * n1 + r) * H * HD +
+                      (g * G + rem - r * G) * HD + hh * 8;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const f16x8 v = *(const f16x8 *)(qp + s * 16);
+        qf[s] = row < rows ? v : f16x8{};
+      }
+    }
+    float m_run = -INFINITY, l_run = 0.f;
+    f32x16 o[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+    block_barrier();      // the last tile's stages are free
+    wait_vmcnt<0>();      // the loop's count covers the DMA only
+#pragma unroll
+    for (int i = 0; i < NST - 1; ++i)
+      if (c0 + i < c1) issue(c0 + i);
+
+    for (int c = c0; c < c1; ++c) {
+      if (c + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
+      block_barrier();    // record c is there, record c - 1 is used up, for every wave
+      if (c + NST - 1 < c1) issue(c + NST - 1);
+      if (!any) continue;
+      const f16 *sk = smem + ((c - c0) % NST) * REC + lane * 8, *sv = sk + REC / 2;
+      const int valid = grp.slots - c * 64;
+      f32x16 sc[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8 *)(sk + (kb * KS + s) * 512),
+                                                          qf[s], sc[kb], 0, 0, 0);
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        // score i of this lane: slot 32 kb + 16 (i / 8) + 8 hh + i % 8
+        if (valid < 64) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (kb * 32 + (i >> 3) * 16 + hh * 8 + (i & 7) >= valid) sc[kb][i] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kb][i]);
+        mx = halves_max(mx);
+        const float m_new = mx > m_run + lazy ? mx : m_run;
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f((m_run - m_use) * sscale);
+        m_run = m_new;
+        const float mb = m_use * sscale;
+        f16x8 p[2];
+        float rs = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], sscale, -mb));
+          rs += e;
+          p[i >> 3][i & 7] = (f16)e;
+        }
+        l_run = l_run * alpha + rs;
+        if (__ballot(alpha < 1.f)) {
+#pragma unroll
+          for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+        }
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            f16x8 v = *(const f16x8 *)(sv + ((kb * 2 + k2) * NDB + db) * 512);
+            if (valid < 64) {   // what lies behind the prefix may be no number at all
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (kb * 32 + k2 * 16 + hh * 8 + e >= valid) v[e] = (f16)0.f;
+            }
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k2], o[db], 0, 0, 0);
+          }
+      }
+    }
+    const float l = halves_sum(l_run);
+    if (row < rows) {
+      const long long at =
+          g * rows_total + part_base(grp.first, QR, tile, w) + wave * 32 + lq;
+      float *po = part_o + at * HD + hh * 4;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *(f32x4 *)(po + db * 32 + j * 8) =
+              f32x4{o[db][j * 4], o[db][j * 4 + 1], o[db][j * 4 + 2], o[db][j * 4 + 3]};
+      if (hh == 0) {
+        part_ml[at * 2] = m_run == -INFINITY ? -INFINITY : m_run * sscale;
+        part_ml[at * 2 + 1] = l;
+      }
+    }
+  }
+}
+
+// A row's partial results joined: of its tile over the shared prefix, and of its session's own
+// slots.  One thread per four head dims.  ROWS: out is row-major bf16, else in the activation
+// layout.  (A part without slots has weight 2^-inf = 0 and zero sums.)
+template <int HD, bool ROWS>
+__global__ __launch_bounds__(256) void shared_combine_kernel(
+    const float *__restrict__ sh_o, const float *__restrict__ sh_ml,
+    const float *__restrict__ part_o, const float *__restrict__ part_ml, SharedMeta sm,
+    void *__restrict__ out, int rows, int n1, int H, int Hkv, int nsplit, int wgs,
+    long long rows_total) {
+  const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int d = (int)(idx % (HD / 4)) * 4;
+  const long long rh = idx / (HD / 4);
+  const int row = (int)(rh / H), h = (int)(rh - (long long)row * H);
+  if (row >= rows) return;
+  const int b = row / n1, r = row - b * n1, G = H / Hkv, g = h / G, QR = G * n1;
+  const int qi = r * G + h - g * G;
+  const size_t item0 = ((size_t)b * Hkv + g) * nsplit * QR + qi;
+  const float2 *ml = (const float2 *)part_ml + item0;
+  const float *po = part_o + item0 * HD + d;
+  const int place = sm.place[b], slots = sm.slots[b];
+  const float2 *sml = nullptr;
+  const float *spo = nullptr;
+  int parts = 0;
+  if (place >= 0) {
+    const int first = sm.first[b];
+    const long long units = sm.total[0];
+    const int wk = working(units, wgs), nblk = (slots + 63) >> 6;
+    const long long local = (long long)(place - first) * QR + qi, tile = local / TM;
+    const long long u0 = sm.units[first] + tile * nblk;
+    const int w0 = worker_of(u0, units, wk);
+    parts = worker_of(u0 + nblk - 1, units, wk) - w0 + 1;
+    const long long at = g * rows_total + part_base(first, QR, tile, w0) + (local - tile * TM);
+    sml = (const float2 *)sh_ml + at;
+    spo = sh_o + at * HD + d;
+  }
+  float M = -INFINITY;
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s) M = fmaxf(M, sml[(size_t)s * TM].x);
+#pragma unroll 4
+  for (int s = 0; s < nsplit; ++s) M = fmaxf(M, ml[(size_t)s * QR].x);
+  if (M == -INFINITY) M = 0.f;
+  float num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+  auto add = [&](float2 e, float4 v) {
+    const float x = __builtin_amdgcn_exp2f(e.x - M);
+    den += x * e.y;
+    num[0] += x * v.x;
+    num[1] += x * v.y;
+    num[2] += x * v.z;
+    num[3] += x * v.w;
+  };
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s)
+    add(sml[(size_t)s * TM], *(const float4 *)(spo + (size_t)s * TM * HD));
+#pragma unroll 4
+  for (int s = 0; s < nsplit; ++s)
+    add(ml[(size_t)s * QR], *(const float4 *)(po + (size_t)s * QR * HD));
+  const float inv = 1.f / den;   // (a row sees itself)
+  if (ROWS) {
+    typedef bf16 b4 __attribute__((ext_vector_type(4)));
+    *(b4 *)((bf16 *)out + (size_t)row * H * HD + h * HD + d) =
+        b4{(bf16)(num[0] * inv), (bf16)(num[1] * inv), (bf16)(num[2] * inv), (bf16)(num[3] * inv)};
+  } else {
+    *(f16x4 *)((f16 *)out + act_off(row, h * HD + d, rows, H * HD)) =
+        f16x4{(f16)(num[0] * inv), (f16)(num[1] * inv), (f16)(num[2] * inv), (f16)(num[3] * inv)};
+  }
+}
+
+// fp32 models: one workgroup per (tree row, query head), over the prefix's records and then the
+// session's own slots, 256 slots at a time: scores with HD / 4 lanes a slot, a softmax step over
+// the block, then the values, 16 lanes x 4 slots of a head dim.
+template <int HD>
+__global__ __launch_bounds__(256) void shared_attn_f32_kernel(
+    const float *__restrict__ qin, const float *__restrict__ blocks, SharedArgs sh,
+    const int32_t *__restrict__ session_slots, const float *__restrict__ ck,
+    const float *__restrict__ cv, TreeMeta meta, float *__restrict__ out, int n1, int H, int Hkv,
+    int capacity) {
+  constexpr int LPS = HD / 4, SPW = 64 / LPS;   // lanes a slot, slots a wave and load
+  constexpr int NCH = 256, STEPS = NCH / 4 / SPW;
+  constexpr int DJ = HD / 16;                   // head dims a lane sums
+  constexpr int REC = 128 * HD;
+  __shared__ __attribute__((aligned(16))) float p[NCH];
+  __shared__ float red[8];
+  const int h = blockIdx.x, row = blockIdx.y;
+  const int b = row / n1;
+  const int G = H / Hkv, g = h / G, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int S = meta.sess_S[b], own = S + n1, front = session_slots[b];
+  const uint64_t anc = meta.anc[row];
+  const int prefix = front > 0 ? sh.of[b] : 0;
+  const float *rec = blocks + ((size_t)prefix * Hkv + g) * (sh.cap >> 6) * REC;
+  const float *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
+  const float *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;   // [HD][capacity]
+  const float4 q4 = *(const float4 *)(qin + (size_t)row * H * HD + h * HD + lane % LPS * 4);
+  const float scale = 1.0f / sqrtf((float)HD);
+  float m = -INFINITY, l = 0.f, o[DJ];
+#pragma unroll
+  for (int j = 0; j < DJ; ++j) o[j] = 0.f;
+  for (int part = 0; part < 2; ++part) {
+    const int total = part == 0 ? front : own;
+    for (int c0 = 0; c0 < total; c0 += NCH) {
+      float4 kv[STEPS];
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int slot = min(c0 + wave * 64 + i * SPW + lane / LPS, total - 1);
+        const float *k = part == 0 ? rec + (size_t)(slot >> 6) * REC + (slot & 63) * HD
+                                   : kb + (size_t)slot * HD;
+        kv[i] = *(const float4 *)(k + lane % LPS * 4);
+      }
+      auto visible = [&](int slot) {
+        if (part == 0 || slot < S) return slot < total;
+        const int j = slot - S;
+        return j < n1 && (j == 0 || (bool)((anc >> (j - 1)) & 1ull));
+      };
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int ls = wave * 64 + i * SPW + lane / LPS;
+        float d = q4.x * kv[i].x + q4.y * kv[i].y + q4.z * kv[i].z + q4.w * kv[i].w;
+#pragma unroll
+        for (int x = 1; x < LPS; x <<= 1) d += __shfl_xor(d, x);
+        if (lane % LPS == 0) p[ls] = visible(c0 + ls) ? d * scale : -INFINITY;
+      }
+      __syncthreads();
+      const float s = p[tid];
+      float mx = wave_max(s);
+      if (lane == 0) red[wave] = mx;
+      __syncthreads();
+      mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+      const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
+      const bool vis = visible(c0 + tid);
+      const float e = vis ? expf(s - mu) : 0.f, a = expf(m - mu);
+      m = mn;
+      p[tid] = vis ? e : -1.f;            // (a hidden slot's value is left out, not times 0)
+      const float ls = wave_sum(e);
+      if (lane == 0) red[4 + wave] = ls;
+      __syncthreads();
+      l = l * a + ((red[4] + red[5]) + (red[6] + red[7]));
+#pragma unroll
+      for (int j = 0; j < DJ; ++j) o[j] *= a;
+      // values: lane % 16 takes slots 4 (lane % 16) + 64 i, for head dims wave * 4 + lane / 16
+      // + 16 j (rows of 64 slots or of the capacity, a multiple of 64: reads stay in them)
+      for (int i = 0; i < NCH / 64 && c0 + i * 64 < total; ++i) {
+        const int ls4 = i * 64 + lane % 16 * 4, slot = c0 + ls4;
+        const float4 pw = *(const float4 *)(p + ls4);
+#pragma unroll
+        for (int j = 0; j < DJ; ++j) {
+          const int dim = wave * 4 + lane / 16 + 16 * j;
+          const float *vr = part == 0 ? rec + (size_t)(slot >> 6) * REC + REC / 2 + dim * 64 + (slot & 63)
+                                      : vb + (size_t)dim * capacity + slot;
+          const float4 v = *(const float4 *)vr;
+          if (pw.x >= 0.f) o[j] += pw.x * v.x;
+          if (pw.y >= 0.f) o[j] += pw.y * v.y;
+          if (pw.z >= 0.f) o[j] += pw.z * v.z;
+          if (pw.w >= 0.f) o[j] += pw.w * v.w;
+        }
+      }
+      __syncthreads();
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < DJ; ++j) {
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) o[j] += __shfl_xor(o[j], x);
+    if (lane % 16 == 0)
+      out[(size_t)row * (H * HD) + h * HD + wave * 4 + lane / 16 + 16 * j] = o[j] / l;
+  }
+}
+
+template <int HD>
+hipError_t launch_hd(const f16 *q, const f16 *blocks, const SharedArgs &sh, const SharedMeta &sm,
+                     void *out, int rows_out, float *sh_o, float *sh_ml, const float *part_o,
+                     const float *part_ml, int rows, int n1, int H, int Hkv, int cus, int nsplit,
+                     hipStream_t s) {
+  const int wgs = acespec::shared_wgs(Hkv, cus);
+  const long long rows_total = acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus);
+  hipLaunchKernelGGL((shared_attn_kernel<HD, 4>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
+                     sh_o, sh_ml, n1, H, Hkv, sh.cap, wgs, rows_total);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const long long wg = ((long long)rows * H * (HD / 4) + 255) / 256;
+  if (wg > 0x7fffffffLL / 256) return hipErrorInvalidValue;
+  auto kernel = rows_out ? shared_combine_kernel<HD, true> : shared_combine_kernel<HD, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(256), 0, s, sh_o, sh_ml, part_o, part_ml, sm,
+                     out, rows, n1, H, Hkv, nsplit, wgs, rows_total);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+namespace acespec {
+
+template <>
+hipError_t launch_attention_shared<bf16>(const f16 *q, const f16 *blocks, const SharedArgs &sh,
+                                         const SharedMeta &sm, const bf16 *ck, const bf16 *cv,
+                                         const TreeMeta &meta, void *out, int rows_out, float *sh_o,
+                                         float *sh_ml, float *part_o, float *part_ml,
+                                         long long part_capacity, int B, int n1, int H, int Hkv,
+                                         int hd, int capacity, int cus, hipStream_t s) {
+  int nsplit = 1;
+  const hipError_t e = launch_attention_part(q, ck, cv, meta, part_o, part_ml, part_capacity, B, n1,
+                                             H, Hkv, hd, capacity, cus, s, &nsplit);
+  if (e != hipSuccess) return e;
+  auto launch = hd == 128 ? launch_hd<128> : launch_hd<64>;
+  return launch(q, blocks, sh, sm, out, rows_out, sh_o, sh_ml, part_o, part_ml, B * n1, n1, H, Hkv,
+                cus, nsplit, s);
+}
+
+template <>
+hipError_t launch_attention_shared<float>(const float *q, const float *blocks, const SharedArgs &sh,
+                                          const SharedMeta &sm, const float *ck, const float *cv,
+                                          const TreeMeta &meta, void *out, int, float *, float *,
+                                          float *, float *, long long, int B, int n1, int H,
+                                          int Hkv, int hd, int capacity, int, hipStream_t s) {
+  auto kernel = hd == 64 ? shared_attn_f32_kernel<64> : shared_attn_f32_kernel<128>;
+  hipLaunchKernelGGL(kernel, dim3(H, B * n1), dim3(256), 0, s, q, blocks, sh, sm.slots, ck, cv, meta,
+                     (float *)out, n1, H, Hkv, capacity);
+  return hipGetLastError();
+}
+
+}  // namespace acespec

@@ -197,6 +197,28 @@ struct TreeMeta {
   int32_t *sess_S;   // [B] prefix length, clamped so that S + N + 1 <= capacity
 };
 
+// Prefixes that several sessions share: len [P] slots each, of at most cap; of [B] the sessions'
+// prefixes (-1: none).
+struct SharedArgs {
+  const int32_t *of, *len;
+  int P, cap;
+};
+// Sessions grouped by the shared prefix that they stand behind (one entry per session; groups
+// in the order of their prefixes, members in the order of their rows).
+struct SharedGroup {
+  int32_t prefix, first, members, slots;  // first: its members' place in `order`
+  long long units;                        // work units of the groups before it
+};
+struct SharedMeta {
+  int32_t *slots;        // [B] slots of the session's shared prefix, 0 for a session without one
+  int32_t *place;        // [B] place in `order` (-1: none), and
+  int32_t *first;        // [B] its group's first place there
+  int32_t *order;        // [B] sessions
+  long long *units;      // [B] by a group's first place: units of the groups before it
+  SharedGroup *groups;   // [B]
+  long long *total;      // [2] units of all groups; number of groups
+};
+
 // Fixed-point scale for deterministic mass sums in the vocabulary kernel.
 #define AS_FX_SCALE 1099511627776.0f  /* 2^40 */
 
@@ -214,6 +236,15 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
                                   const int32_t *prefix_len, int B, int n1, int V, int capacity,
                                   int window, int sinks, TreeMeta meta, int32_t *status,
                                   hipStream_t s);
+
+// The same for sessions behind shared prefixes (positions start behind them), and their groups;
+// a unit of work is a 64-slot record for tile_rows query rows.  tokens may be NULL (meta.tok is
+// then not written).  q [rows][width] bf16 or NULL: brought to fp16 at q16 on the way.
+hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
+                                   const int32_t *prefix_len, int B, int n1, int V, int capacity,
+                                   const SharedArgs &sh, int G, int tile_rows, TreeMeta meta,
+                                   const SharedMeta &sm, int32_t *status, const bf16 *q, f16 *q16,
+                                   int width, hipStream_t s);
 
 template <typename TW>
 hipError_t launch_embed(const TW *embed, const int32_t *tok, float *x, int rows, int d,
@@ -265,6 +296,10 @@ template <typename TW> struct RopeOut {
   const float2 *rot;
   const int32_t *sess_S;
   int n1, H, Hkv, hd, capacity;
+  // norms of each head before the rotation (gains [hd], or NULL: none), which take the
+  // projection out of the epilogue
+  const TW *q_gain = nullptr, *k_gain = nullptr;
+  float eps = 0.f;
 };
 // The QKV projection with RoPE and the cache write fused into its epilogue when the
 // product is not sliced along K; otherwise the fp32 projection goes to qkv and the RoPE
@@ -310,6 +345,57 @@ hipError_t launch_attention(const typename ActOf<TW>::type *q, const TW *cache_k
                             typename ActOf<TW>::type *out, float *part_o, float *part_ml,
                             long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                             int capacity, int cus, hipStream_t s, int *nsplit_used);
+
+// The same over the own slots alone of sessions behind shared prefixes: always as partial sums,
+// of *nsplit parts a session; a value that is not finite reaches only rows that see its slot.
+hipError_t launch_attention_part(const f16 *q, const bf16 *cache_k, const bf16 *cache_v,
+                                 const TreeMeta &meta, float *part_o, float *part_ml,
+                                 long long part_capacity, int B, int n1, int H, int Hkv, int hd,
+                                 int capacity, int cus, hipStream_t s, int *nsplit);
+
+// One layer's tree attention behind shared prefixes: blocks [P][Hkv][cap / 64] records, own slots
+// ck, cv as in launch_attention.  q is row-major [rows][H hd] in the activation type; out is in
+// the activation layout, or row-major in TW with rows_out.  sh_o, sh_ml: partial results of the
+// shared slots, shared_part_rows(..) rows a kv head.
+constexpr int kSharedTile = 256;   // query rows of a workgroup over a shared prefix
+inline int shared_wgs(int Hkv, int cus) { return cus > Hkv ? cus / Hkv : 1; }  // a kv head
+inline long long shared_part_rows(long long rows, int Hkv, int cus) {
+  return rows + (long long)kSharedTile * shared_wgs(Hkv, cus);
+}
+template <typename TW>
+hipError_t launch_attention_shared(const typename ActOf<TW>::type *q,
+                                   const typename ActOf<TW>::type *blocks, const SharedArgs &sh,
+                                   const SharedMeta &sm, const TW *ck, const TW *cv,
+                                   const TreeMeta &meta, void *out, int rows_out, float *sh_o,
+                                   float *sh_ml, float *part_o, float *part_ml,
+                                   long long part_capacity, int B, int n1, int H, int Hkv, int hd,
+                                   int capacity, int cus, hipStream_t s);
+
+// Queries and keys of a projection qkv (nsl k-slices [rows, (H + 2 Hkv) hd], summed in order)
+// normalised per head (where a gain [hd] is given) and rotated, the tree rows' keys and values
+// written to the cache.  meta.pos gives the positions, or with parents given [rows] they follow
+// from these, the prefixes and sh (of may be NULL), and status [B] is written.
+template <typename TW, typename TIN, typename TQ>
+hipError_t launch_qk_norm_rope(const TIN *qkv, int nsl, const TW *q_gain, const TW *k_gain,
+                               float eps, const double *inv_freq, const TreeMeta &meta,
+                               const int32_t *parents, const int32_t *prefix_len,
+                               const SharedArgs &sh, int32_t *status, TQ *q_out, TW *ck, TW *cv,
+                               const float2 *rot, int B, int n1, int H, int Hkv, int hd,
+                               int capacity, hipStream_t s);
+
+// Slots [0, count[p]) (count NULL: all) of session from[p] brought into the records of shared
+// prefix p; new_len[p] slots are then held (-1: refused, nothing written).
+template <typename T>
+hipError_t launch_share_prefix(const T *k, const T *v, const int32_t *prefix_len, int B, int cap,
+                               void *blocks, const SharedArgs &sh, const int32_t *from,
+                               const int32_t *count, int32_t *new_len, int L, int Hkv, int hd,
+                               hipStream_t s);
+// Slots [first[b], len of from[b]) of another session, written to session b's from 0 on.
+template <typename T>
+hipError_t launch_fork_kv(const T *sk, const T *sv, const int32_t *src_len, int Bs, int scap, T *dk,
+                          T *dv, const int32_t *dst_len, int Bd, int dcap, const int32_t *from,
+                          const int32_t *first, int32_t *new_len, int L, int Hkv, int hd,
+                          hipStream_t s);
 
 // One layer's tree attention over the cache in 4 bits: blocks [B][Hkv][capacity / 32] records,
 // the tail tk [B][Hkv][tcap][hd] and tv [B][Hkv][hd][tcap].  window (0: none) and sinks as in

@@ -1432,6 +1432,18 @@ hipError_t launch_gemm_resid_norm<float, float>(const float *A, const float *W, 
   return launch_rmsnorm<float, float>(x, gain, out, M, N, eps, s);
 }
 
+// The rotation after a projection that went to fp32 (nsl slices), with the heads' norms if any.
+template <typename TW>
+static hipError_t launch_rotation(const float *qkv, int nsl, const RopeOut<TW> &ro,
+                                  const TreeMeta &meta, int B, hipStream_t s) {
+  if (ro.q_gain || ro.k_gain)
+    return launch_qk_norm_rope<TW, float, typename ActOf<TW>::type>(
+        qkv, nsl, ro.q_gain, ro.k_gain, ro.eps, nullptr, meta, nullptr, nullptr, SharedArgs{},
+        nullptr, ro.q, ro.ck, ro.cv, ro.rot, B, ro.n1, ro.H, ro.Hkv, ro.hd, ro.capacity, s);
+  return launch_rope_kv<TW>(qkv, nsl, ro.q, meta, ro.ck, ro.cv, B, ro.n1, ro.H, ro.Hkv, ro.hd,
+                            ro.capacity, ro.rot, s);
+}
+
 template <>
 hipError_t launch_qkv_rope<bf16, f16>(const f16 *A, const bf16 *W, int M, int N, int K,
                                       float *qkv, const RopeOut<bf16> &ro, const TreeMeta &meta,
@@ -1439,15 +1451,14 @@ hipError_t launch_qkv_rope<bf16, f16>(const f16 *A, const bf16 *W, int M, int N,
   // packed weights: 128 x 256 tiles kept whole when they fill most CUs, so the RoPE and
   // cache write stay in the epilogue (measured level with the separate RoPE kernel after
   // a split product, and with eight 64 x 64 waves a tile)
-  const bool fusable = N == (ro.H + 2 * ro.Hkv) * ro.hd;
+  const bool fusable = N == (ro.H + 2 * ro.Hkv) * ro.hd && !ro.q_gain && !ro.k_gain;
   if (rows_ok(EPI_F32, M, N, K, aux.packed)) {
     const RowsPlan mp = plan_rows(EPI_F32, M, N, K, aux.cus, aux.part_cap);
     float *dst = mp.nsl > 1 ? aux.part : qkv;
     const hipError_t e =
         launch_rows<EPI_F32>(s, A, W, M, N, K, (f16 *)nullptr, dst, mp, aux.packed);
     if (e != hipSuccess) return e;
-    return launch_rope_kv<bf16>(dst, mp.nsl, ro.q, meta, ro.ck, ro.cv, B, ro.n1, ro.H, ro.Hkv,
-                                ro.hd, ro.capacity, ro.rot, s);
+    return launch_rotation<bf16>(dst, mp.nsl, ro, meta, B, s);
   }
   if (aux.packed && M > 384 && fusable && 128 % ro.hd == 0) {
     // tiles kept whole, each with two wave groups splitting its k-steps (two waves a SIMD
@@ -1474,8 +1485,7 @@ hipError_t launch_qkv_rope<bf16, f16>(const f16 *A, const bf16 *W, int M, int N,
   const hipError_t e = launch_f16w_variant<bf16>(var, EPI_F32, A, W, M, N, K, nullptr, qkv,
                                            aux.part, aux.part_cap, aux.cus, s, aux.packed);
   if (e != hipSuccess) return e;
-  return launch_rope_kv<bf16>(qkv, 1, ro.q, meta, ro.ck, ro.cv, B, ro.n1, ro.H, ro.Hkv, ro.hd,
-                              ro.capacity, ro.rot, s);
+  return launch_rotation<bf16>(qkv, 1, ro, meta, B, s);
 }
 
 template <>
@@ -1487,8 +1497,7 @@ hipError_t launch_qkv_rope<float, float>(const float *A, const float *W, int M, 
   float *dst = p.nsl > 1 ? aux.part : qkv;
   const hipError_t e = launch_rows<EPI_F32>(s, A, W, M, N, K, (float *)nullptr, dst, p, 0);
   if (e != hipSuccess) return e;
-  return launch_rope_kv<float>(dst, p.nsl, ro.q, meta, ro.ck, ro.cv, B, ro.n1, ro.H, ro.Hkv,
-                               ro.hd, ro.capacity, ro.rot, s);
+  return launch_rotation<float>(dst, p.nsl, ro, meta, B, s);
 }
 
 template <>

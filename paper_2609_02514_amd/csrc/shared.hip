@@ -1,0 +1,187 @@
+// Moves between caches: a session's first slots into the store of shared prefixes, and sessions
+// that take over another session's slots.
+//
+// Both are copies, bound by memory.  The store keeps records of 64 slots in the order in which the
+// attention over them multiplies (fp16 for a bf16 model: the values that the products take anyway),
+// so that a prefix is brought into that order once and read by every step from then on.
+#include "common.h"
+
+namespace {
+
+constexpr int ST = 256;   // threads
+
+// One workgroup a record.  grid: records x prefixes x (layer, kv head), records fastest.
+template <typename T, int HD>
+__global__ __launch_bounds__(ST) void share_kernel(const T *__restrict__ k, const T *__restrict__ v,
+                                                   const int32_t *__restrict__ prefix_len, int B,
+                                                   int cap, void *__restrict__ blocks, SharedArgs sh,
+                                                   const int32_t *__restrict__ from,
+                                                   const int32_t *__restrict__ count,
+                                                   int32_t *__restrict__ new_len, int Hkv) {
+  constexpr int REC = 128 * HD;
+  const int nblk = sh.cap >> 6;
+  const long long item = blockIdx.x / nblk;
+  const int c = (int)(blockIdx.x - item * nblk), p = (int)(item % sh.P), lg = (int)(item / sh.P);
+  const int l = lg / Hkv, g = lg - l * Hkv, tid = threadIdx.x;
+  const int src = from[p];
+  int n = -1;
+  if (src >= 0 && src < B) {
+    const int len = prefix_len[src];
+    n = count ? count[p] : len;
+    if (len < 0 || len > cap || n < 0 || n > len || n > sh.cap) n = -1;
+  }
+  if (lg == 0 && c == 0 && tid == 0) new_len[p] = src == -1 ? sh.len[p] : n;
+  if (c * 64 >= n) return;
+  const size_t plane = ((size_t)l * B + src) * Hkv + g;
+  const T *kp = k + (plane * cap + c * 64) * HD, *vp = v + plane * HD * cap + c * 64;
+  const size_t rec = (((size_t)l * sh.P + p) * Hkv + g) * nblk + c;
+  const int valid = min(64, n - c * 64);
+  constexpr int PE = 16 / sizeof(T);
+  typedef T piece __attribute__((ext_vector_type(PE)));
+  if constexpr (sizeof(T) == 4) {
+    float *dst = (float *)blocks + rec * REC;
+    for (int e = tid; e < 64 * HD / PE; e += ST) {
+      const int slot = e / (HD / PE);
+      piece x{};
+      if (slot < valid) x = *(const piece *)(kp + (size_t)e * PE);
+      *(piece *)(dst + e * PE) = x;
+    }
+    for (int e = tid; e < 64 * HD / PE; e += ST) {
+      const int d = e / (64 / PE), s0 = e % (64 / PE) * PE;
+      piece x{};
+      if (s0 < valid) x = *(const piece *)(vp + (size_t)d * cap + s0);
+#pragma unroll
+      for (int i = 0; i < PE; ++i)
+        if (s0 + i >= valid) x[i] = 0.f;
+      *(piece *)(dst + REC / 2 + e * PE) = x;
+    }
+  } else {
+    // read in the cache's order, whole rows at a time; written as runs of 64 and 128 bytes
+    f16 *dst = (f16 *)blocks + rec * REC;
+#pragma unroll 4
+    for (int e = tid; e < 64 * HD / 8; e += ST) {
+      const int slot = e / (HD / 8), d8 = e % (HD / 8);
+      f16x8 x{};
+      if (slot < valid) x = bf16x8_to_f16x8(*(const bf16x8 *)(kp + (size_t)e * 8));
+      // row r of a 32 x 32 operand holds slot 16 r4 + 8 r2 + 4 r3 + r10 of its half
+      const int lane = (d8 & 1) * 32 + (slot & 16) + ((slot >> 3) & 1) * 4 + ((slot >> 2) & 1) * 8 + (slot & 3);
+      *(f16x8 *)(dst + (((slot >> 5) * (HD / 16) + (d8 >> 1)) * 64 + lane) * 8) = x;
+    }
+#pragma unroll 4
+    for (int e = tid; e < 64 * HD / 8; e += ST) {
+      const int d = e >> 3, s8 = e & 7;
+      f16x8 x{};
+      if (s8 * 8 < valid) x = bf16x8_to_f16x8(*(const bf16x8 *)(vp + (size_t)d * cap + s8 * 8));
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (s8 * 8 + i >= valid) x[i] = (f16)0.f;
+      const int lane = (s8 & 1) * 32 + (d & 31);
+      *(f16x8 *)(dst + REC / 2 + (((s8 >> 1) * (HD / 32) + (d >> 5)) * 64 + lane) * 8) = x;
+    }
+  }
+}
+
+// 16 bytes at any element's address
+template <typename T> AS_DEVICE u32x4 load_any(const T *p) {
+  struct __attribute__((packed, aligned(sizeof(T)))) U { u32x4 x; };
+  return ((const U *)p)->x;
+}
+
+// One workgroup takes FCH slots of one plane (layer, kv head, session).  Neighbouring workgroups
+// take the same slots of the sessions that may have them from one source, so that a source read by
+// several is read from memory once.
+constexpr int FCH = 256;
+template <typename T, int HD>
+__global__ __launch_bounds__(ST) void fork_kernel(const T *__restrict__ sk, const T *__restrict__ sv,
+                                                  const int32_t *__restrict__ src_len, int Bs,
+                                                  int scap, T *dk, T *dv,
+                                                  const int32_t *__restrict__ dst_len, int Bd,
+                                                  int dcap, const int32_t *__restrict__ from,
+                                                  const int32_t *__restrict__ first,
+                                                  int32_t *__restrict__ new_len, int Hkv,
+                                                  int chunks, int same) {
+  constexpr int PE = 16 / sizeof(T);
+  const int b = blockIdx.x % Bd, rest = blockIdx.x / Bd;
+  const int c = rest % chunks, lg = rest / chunks, l = lg / Hkv, g = lg - l * Hkv;
+  const int tid = threadIdx.x;
+  const int src = from[b];
+  int n = -1, x0 = 0;
+  if (src >= 0 && src < Bs) {
+    const int len = src_len[src];
+    x0 = first ? first[b] : 0;
+    if (len >= 0 && len <= scap && x0 >= 0 && x0 <= len && len - x0 <= dcap) n = len - x0;
+    if (same) {   // a session that receives slots itself is no source
+      if (src == b && x0 != 0) n = -1;
+      const int f = from[src];
+      if (src != b && f != -1 && f != src) n = -1;
+    }
+  }
+  if (lg == 0 && c == 0 && tid == 0) new_len[b] = src == -1 ? dst_len[b] : n;
+  if (c * FCH >= n || (same && src == b)) return;
+  const size_t sp = ((size_t)l * Bs + src) * Hkv + g, dp = ((size_t)l * Bd + b) * Hkv + g;
+  const int lo = c * FCH, m = min(FCH, n - lo);   // slots of this workgroup
+  const T *ks = sk + (sp * scap + x0 + lo) * HD, *vs = sv + sp * HD * scap + x0 + lo;
+  T *kd = dk + (dp * dcap + lo) * HD, *vd = dv + dp * HD * dcap + lo;
+#pragma unroll 4
+  for (int e = tid; e < m * (HD / PE); e += ST) ((u32x4 *)kd)[e] = ((const u32x4 *)ks)[e];
+  // values: m columns of each head dim, from any column on
+  const int pieces = (m + PE - 1) / PE, full = m / PE;
+#pragma unroll 4
+  for (int e = tid; e < HD * (FCH / PE); e += ST) {
+    const int d = e / (FCH / PE), i = e % (FCH / PE);
+    if (i >= pieces) continue;
+    const T *s = vs + (size_t)d * scap + i * PE;
+    T *t = vd + (size_t)d * dcap + i * PE;
+    if (i < full) {
+      *(u32x4 *)t = load_any(s);
+    } else {
+      for (int j = 0; j < m - full * PE; ++j) t[j] = s[j];
+    }
+  }
+}
+
+}  // namespace
+
+namespace acespec {
+
+template <typename T>
+hipError_t launch_share_prefix(const T *k, const T *v, const int32_t *prefix_len, int B, int cap,
+                               void *blocks, const SharedArgs &sh, const int32_t *from,
+                               const int32_t *count, int32_t *new_len, int L, int Hkv, int hd,
+                               hipStream_t s) {
+  const long long wgs = (long long)L * Hkv * sh.P * (sh.cap / 64);
+  if ((hd != 64 && hd != 128) || wgs > 0xffffffffLL / ST) return hipErrorInvalidValue;
+  auto kernel = hd == 64 ? share_kernel<T, 64> : share_kernel<T, 128>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(ST), 0, s, k, v, prefix_len, B, cap, blocks, sh,
+                     from, count, new_len, Hkv);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_fork_kv(const T *sk, const T *sv, const int32_t *src_len, int Bs, int scap, T *dk,
+                          T *dv, const int32_t *dst_len, int Bd, int dcap, const int32_t *from,
+                          const int32_t *first, int32_t *new_len, int L, int Hkv, int hd,
+                          hipStream_t s) {
+  const int chunks = ((scap < dcap ? scap : dcap) + FCH - 1) / FCH;
+  const long long wgs = (long long)L * Hkv * Bd * chunks;
+  if ((hd != 64 && hd != 128) || wgs > 0xffffffffLL / ST) return hipErrorInvalidValue;
+  const int same = sk == dk && sv == dv;
+  auto kernel = hd == 64 ? fork_kernel<T, 64> : fork_kernel<T, 128>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(ST), 0, s, sk, sv, src_len, Bs, scap, dk, dv,
+                     dst_len, Bd, dcap, from, first, new_len, Hkv, chunks, same);
+  return hipGetLastError();
+}
+
+#define MOVES(T)                                                                                   \
+  template hipError_t launch_share_prefix<T>(const T *, const T *, const int32_t *, int, int,      \
+                                             void *, const SharedArgs &, const int32_t *,          \
+                                             const int32_t *, int32_t *, int, int, int,            \
+                                             hipStream_t);                                         \
+  template hipError_t launch_fork_kv<T>(const T *, const T *, const int32_t *, int, int, T *, T *, \
+                                        const int32_t *, int, int, const int32_t *,                \
+                                        const int32_t *, int32_t *, int, int, int, hipStream_t);
+MOVES(bf16)
+MOVES(float)
+#undef MOVES
+
+}  // namespace acespec

@@ -5,6 +5,7 @@
 // the drafted rows (the root, row 0, is every row's ancestor and is always visible).
 // Positions: siblings share a position, prefix_len + depth; keys/values of row r live
 // in cache slot prefix_len + r.
+// Behind a shared prefix positions start at its end; the sessions of a prefix become a group.
 // Over a cache in 4 bits the tree's rows go behind the prefix_len % 32 slots of the tail, and a
 // sliding window takes ancestors that are too far back out of a row's set.
 #include "common.h"
@@ -17,23 +18,26 @@ constexpr int TP_THREADS = 128;  // one thread per tree row (at most 65 rows)
 // (the root carries none); it is built by pointer jumping, every row doubling the span of
 // ancestors it has folded in per round (7 rounds cover 65 rows), and the row's depth is
 // the mask's population count.
+// tokens may be NULL.  front: positions before the prefix (-1: a shared prefix that is not one).
 template <bool QUANT>
-__global__ __launch_bounds__(TP_THREADS) void tree_prep_kernel(
-    const int32_t *__restrict__ tokens, const int32_t *__restrict__ parents,
-    const int32_t *__restrict__ prefix_len, int B, int n1, int V, int capacity, int window,
-    int sinks, TreeMeta meta, int32_t *__restrict__ status) {
+AS_DEVICE void prepare_tree(int b, const int32_t *__restrict__ tokens,
+                            const int32_t *__restrict__ parents,
+                            const int32_t *__restrict__ prefix_len, int n1, int V, int capacity,
+                            int window, int sinks, int front, const TreeMeta &meta,
+                            int32_t *__restrict__ status) {
   __shared__ int s_jump[TP_THREADS];
   __shared__ uint64_t s_anc[TP_THREADS];
-  const int b = blockIdx.x, r = threadIdx.x;
+  const int r = threadIdx.x;
   const size_t base = (size_t)b * n1;
   const bool in = r < n1;
   const int pr = in ? parents[base + r] : 0;
-  const int tk = in ? tokens[base + r] : 0;
+  const int tk = in && tokens ? tokens[base + r] : 0;
   int S = prefix_len[b];
   const bool row_ok = !in || (((r == 0) ? (pr == -1) : (pr >= 0 && pr < r)) && tk >= 0 && tk < V);
   // largest prefix: with QUANT full blocks and a full tail behind them
   const long long most = QUANT ? (long long)capacity + 31 : (long long)capacity - n1;
-  const bool ok = __syncthreads_and(row_ok) && S >= 0 && S <= most;
+  const bool ok = __syncthreads_and(row_ok) && S >= 0 && S <= most && front >= 0;
+  if (front < 0) front = 0;
   if (S < 0) S = 0;
   if (S > most) S = (int)most;
   const int p = !in || r == 0 ? -1 : (ok ? pr : r - 1);  // malformed trees become a chain
@@ -60,11 +64,119 @@ __global__ __launch_bounds__(TP_THREADS) void tree_prep_kernel(
       const int j = __builtin_ctzll(rest) + 1, dj = __popcll(s_anc[j]);
       if (depth - dj >= window && S + dj >= sinks) anc &= ~(1ull << (j - 1));
     }
-  meta.tok[base + r] = tk < 0 ? 0 : (tk >= V ? V - 1 : tk);
+  if (tokens) meta.tok[base + r] = tk < 0 ? 0 : (tk >= V ? V - 1 : tk);
   meta.par[base + r] = p;
   meta.depth[base + r] = depth;
   meta.anc[base + r] = anc;
-  meta.pos[base + r] = S + depth;
+  meta.pos[base + r] = front + S + depth;
+}
+
+template <bool QUANT>
+__global__ __launch_bounds__(TP_THREADS) void tree_prep_kernel(
+    const int32_t *__restrict__ tokens, const int32_t *__restrict__ parents,
+    const int32_t *__restrict__ prefix_len, int B, int n1, int V, int capacity, int window,
+    int sinks, TreeMeta meta, int32_t *__restrict__ status) {
+  prepare_tree<QUANT>(blockIdx.x, tokens, parents, prefix_len, n1, V, capacity, window, sinks, 0,
+                      meta, status);
+}
+
+// Session b's shared prefix, -1 where it has none (or an empty or malformed one); *slots its
+// length, -1 where malformed.
+AS_DEVICE int shared_prefix(const SharedArgs &sh, int b, int *slots) {
+  const int p = sh.of[b];
+  *slots = p == -1 ? 0 : -1;
+  if (p < 0 || p >= sh.P) return -1;
+  const int n = sh.len[p];
+  if (n < 0 || n > sh.cap) return -1;
+  *slots = n;
+  return n > 0 ? p : -1;
+}
+
+// The groups, by one workgroup: a session's place follows from counts over all the sessions (64
+// sessions: 64 reads from LDS a thread; B^2 / 128 of them at most).
+constexpr int GROUP_TILE = 1024;   // sessions in LDS at a time
+AS_DEVICE void group_sessions(int B, int QR, const SharedArgs &sh, int tile_rows,
+                              const SharedMeta &sm) {
+  __shared__ int s_p[GROUP_TILE];
+  const int tid = threadIdx.x;
+  int grouped = 0;
+  for (int b0 = 0; b0 < B; b0 += TP_THREADS) {
+    const int b = b0 + tid;
+    int slots = 0, before = 0, rank = 0, members = 0;
+    const int p = b < B ? shared_prefix(sh, b, &slots) : -1;
+    grouped = 0;
+    for (int t0 = 0; t0 < B; t0 += GROUP_TILE) {
+      const int n = min(GROUP_TILE, B - t0);
+      int unused;
+      __syncthreads();
+      for (int i = tid; i < n; i += TP_THREADS) s_p[i] = shared_prefix(sh, t0 + i, &unused);
+      __syncthreads();
+      for (int i = 0; i < n; ++i) {
+        const int o = s_p[i];
+        grouped += o >= 0;
+        before += o >= 0 && o < p;
+        members += o == p;
+        rank += o == p && t0 + i < b;
+      }
+    }
+    if (b >= B) continue;
+    sm.slots[b] = max(slots, 0);
+    sm.place[b] = p < 0 ? -1 : before + rank;
+    sm.first[b] = before;
+    if (p < 0) continue;
+    sm.order[before + rank] = b;
+    // a group's entry waits at its first place until the ones before it are known
+    sm.groups[before + rank] = SharedGroup{p, before, rank == 0 ? members : 0, slots, 0};
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  // one wave closes the gaps, and sums the units
+  int count = 0;
+  long long units = 0;
+  for (int x0 = 0; x0 < grouped; x0 += 64) {
+    const int x = x0 + tid;
+    SharedGroup g = x < grouped ? sm.groups[x] : SharedGroup{0, 0, 0, 0, 0};
+    const bool lead = g.members > 0;
+    const long long mine =
+        lead ? ((long long)g.members * QR + tile_rows - 1) / tile_rows * ((g.slots + 63) / 64) : 0;
+    long long sum = mine;   // of this lane's and the ones' before
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long v = __shfl_up(sum, o);
+      if (tid >= o) sum += v;
+    }
+    const uint64_t leads = __ballot(lead);
+    g.units = units + sum - mine;
+    if (lead) {
+      sm.units[x] = g.units;
+      sm.groups[count + __popcll(leads & ((1ull << tid) - 1))] = g;   // (at most x: read already)
+    }
+    count += __popcll(leads);
+    units += __shfl(sum, 63);
+  }
+  if (tid == 0) {
+    sm.total[0] = units;
+    sm.total[1] = count;
+  }
+}
+
+// Workgroups: the groups, then a session each, then 8 query elements a thread.
+__global__ __launch_bounds__(TP_THREADS) void tree_prep_shared_kernel(
+    const int32_t *__restrict__ tokens, const int32_t *__restrict__ parents,
+    const int32_t *__restrict__ prefix_len, int B, int n1, int V, int capacity, SharedArgs sh,
+    int QR, int tile_rows, TreeMeta meta, SharedMeta sm, int32_t *__restrict__ status,
+    const bf16 *__restrict__ q, f16 *__restrict__ q16, long long pieces) {
+  const int w = blockIdx.x;
+  if (w == 0) {
+    group_sessions(B, QR, sh, tile_rows, sm);
+  } else if (w <= B) {
+    int slots;
+    shared_prefix(sh, w - 1, &slots);
+    prepare_tree<false>(w - 1, tokens, parents, prefix_len, n1, V, capacity, 0, 0, slots, meta,
+                        status);
+  } else {
+    const long long i = (long long)(w - 1 - B) * TP_THREADS + threadIdx.x;
+    if (i < pieces) ((f16x8 *)q16)[i] = bf16x8_to_f16x8(((const bf16x8 *)q)[i]);
+  }
 }
 
 }  // namespace
@@ -87,6 +199,21 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
   if (n1 > TP_THREADS) return hipErrorInvalidValue;
   hipLaunchKernelGGL(tree_prep_kernel<true>, dim3(B), dim3(TP_THREADS), 0, s, tokens, parents,
                      prefix_len, B, n1, V, capacity, window, sinks, meta, status);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
+                                   const int32_t *prefix_len, int B, int n1, int V, int capacity,
+                                   const SharedArgs &sh, int G, int tile_rows, TreeMeta meta,
+                                   const SharedMeta &sm, int32_t *status, const bf16 *q, f16 *q16,
+                                   int width, hipStream_t s) {
+  if (n1 > TP_THREADS || width % 8 != 0) return hipErrorInvalidValue;
+  const long long pieces = q ? (long long)B * n1 * (width / 8) : 0;
+  const long long wgs = 1 + B + (pieces + TP_THREADS - 1) / TP_THREADS;
+  if (wgs > 0x7fffffffLL / TP_THREADS) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(tree_prep_shared_kernel, dim3((unsigned)wgs), dim3(TP_THREADS), 0, s, tokens,
+                     parents, prefix_len, B, n1, V, capacity, sh, G * n1, tile_rows, meta, sm,
+                     status, q, q16, pieces);
   return hipGetLastError();
 }
 
