@@ -214,7 +214,7 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
                                        o->status, stream));
   else if (kv.shared)
     RUN(K_TREE, launch_tree_prep_shared(tokens, parents, kv.prefix_len, B, n1, V, cap, sh, H / Hkv,
-                                        kSharedTile, meta, ctx->shm, o->status, nullptr, nullptr, 0,
+                                        Hkv, kSharedTile, meta, ctx->shm, o->status, nullptr, nullptr, 0,
                                         stream));
   else
     RUN(K_TREE, launch_tree_prep(tokens, parents, kv.prefix_len, B, n1, V, cap, meta, o->status,
@@ -444,7 +444,7 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
        *p_anc = nullptr, *p_S = nullptr;
   void *p_so = nullptr, *p_sml = nullptr, *p_slots = nullptr, *p_place = nullptr,
        *p_first = nullptr, *p_order = nullptr, *p_units = nullptr, *p_groups = nullptr,
-       *p_total = nullptr;
+       *p_total = nullptr, *p_bad = nullptr;
   std::vector<Part> parts = {
       {R * d.d_model * 4, &p_x},
       {R * d.d_model * c->esz, &c->a},
@@ -466,7 +466,8 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
       {(size_t)max_batch * 4, &p_S},
       {shr * d.head_dim * 4, &p_so}, {shr * 2 * 4, &p_sml},
       {each * 4, &p_slots}, {each * 4, &p_place}, {each * 4, &p_first}, {each * 4, &p_order},
-      {each * 8, &p_units}, {each * sizeof(SharedGroup), &p_groups}, {layers ? 16u : 0u, &p_total}};
+      {each * 8, &p_units}, {each * sizeof(SharedGroup), &p_groups}, {layers ? 16u : 0u, &p_total},
+      {layers ? each * d.n_kv_heads * 12 : 0, &p_bad}};
   size_t total = 0;
   for (auto &pt : parts) total += align_up(pt.bytes);
   if (hipMalloc(&c->ws, total) != hipSuccess) {
@@ -501,7 +502,7 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   c->sh_ml = (float *)p_sml;
   c->shm = SharedMeta{(int32_t *)p_slots, (int32_t *)p_place, (int32_t *)p_first,
                       (int32_t *)p_order, (long long *)p_units, (SharedGroup *)p_groups,
-                      (long long *)p_total};
+                      (long long *)p_total, (uint32_t *)p_bad};
   if (layers) {
     std::vector<double> f(d.head_dim / 2);
     for (int i = 0; i < d.head_dim / 2; ++i)
@@ -1183,7 +1184,7 @@ int acespec_attention_shared(acespec_ctx *ctx, const acespec_kv_shared *sh, cons
   const size_t rec = layer * shared_layer_elems(d, sh);
   const bool b16 = d.dtype == ACESPEC_BF16;
   RUN(K_TREE, launch_tree_prep_shared(nullptr, parent_idx, kv->prefix_len, B, n1, d.vocab,
-                                      kv->capacity, sa, H / Hkv, kSharedTile, ctx->meta, ctx->shm,
+                                      kv->capacity, sa, H / Hkv, Hkv, kSharedTile, ctx->meta, ctx->shm,
                                       status, b16 ? (const bf16 *)q : nullptr, (f16 *)ctx->q, H * hd,
                                       stream));
   if (b16)

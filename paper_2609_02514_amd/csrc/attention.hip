@@ -142,10 +142,13 @@ AS_DEVICE void issue_chunk(uint16_t *stage, __amdgpu_buffer_rsrc_t kr,
   }
 }
 
+// Tree rows whose values are not all finite: three words a session and kv head.
+AS_DEVICE void mark_row(uint32_t *bad, int row) { atomicOr(bad + (row >> 5), 1u << (row & 31)); }
+
 // bf16 -> fp16 in place for pieces t, t + stride, ... of a stage (t: the thread's index
 // among the widening threads); value slots >= total are zeroed.
-// PART: values that are not finite are zeroed in the tree's slots (>= S) too, and the slots
-// marked in bad (two words); add_marked brings them to the rows that see them.
+// PART: values that are not finite are zeroed in the tree's slots (>= S) too, and their rows
+// marked in bad; the join of the parts brings them to the rows that see them.
 template <int HD, bool PART = false>
 AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int total, int S = 0,
                            uint32_t *bad = nullptr) {
@@ -163,47 +166,29 @@ AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int tot
     }
     if (PART && key0 + KC > S && pc >= KPIECES) {
       const int vp = pc - KPIECES, row = vp >> 3;
-      const int i0 = ((vp & 7) ^ vsw(row)) << 3;   // slot within the chunk
+      const int j0 = key0 + (((vp & 7) ^ vsw(row)) << 3) - S;   // the piece's first tree row
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (key0 + i0 + e >= S && !(fabsf((float)h[e]) <= 65504.f)) {
+        if (j0 + e >= 0 && !(fabsf((float)h[e]) <= 65504.f)) {
           h[e] = (f16)0.f;
-          atomicOr(bad + ((i0 + e) >> 5), 1u << ((i0 + e) & 31));
+          mark_row(bad, j0 + e);
         }
     }
     *(f16x8 *)p = h;
   }
 }
 
-// The values that widen_chunk took out of a tree chunk, added to o for a row that sees their
-// slots: an infinity or a NaN stays one whatever weight it has.  dim(i): head dim of o's i-th
-// element.
-template <int N, typename F>
-AS_DEVICE void add_marked(float (&o)[N], F dim, const uint32_t *bad, const bf16 *vb, int capacity,
-                          int key0, int S, uint64_t anc) {
-  for (int w = 0; w < 2; ++w)
-    for (uint32_t rest = bad[w]; rest; rest &= rest - 1) {
-      const int slot = key0 + w * 32 + __builtin_ctz(rest), j = slot - S;   // (a tree row, marked)
-      if (j > 0 && !((anc >> (j - 1)) & 1ull)) continue;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float v = (float)(f16)(float)vb[(size_t)dim(i) * capacity + slot];
-        if (!(fabsf(v) <= 65504.f)) o[i] += v;
-      }
-    }
-}
-
 template <int HD, int NW, int UPW, int NST, bool PART = false>
 __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     const f16 *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
-    float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int tpg) {
+    float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int tpg,
+    uint32_t *bad_rows) {
   constexpr int KSTEPS = HD / 32, NB = HD / 16;
   constexpr int STAGE = 2 * KC * HD;     // elements: K [KC][HD], then V^T [HD][KC]
   constexpr int L_DMA = HD / 4 / NW;     // DMA instructions per wave per chunk
   static_assert(NST >= 3, "the widening runs one stage ahead of the MFMAs");
   __shared__ __attribute__((aligned(1024))) uint16_t smem[NST * STAGE];
-  __shared__ uint32_t s_bad[PART ? 2 * NST : 1];   // a stage's marked slots (widen_chunk)
 
   const int g = blockIdx.y, b = blockIdx.z;
   const int G = H / Hkv, QR = G * n1;
@@ -231,6 +216,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
   const int cps = (nchunks + nsplit - 1) / nsplit;
   const int c0 = split * cps;
   const int c1 = min(nchunks, c0 + cps);
+  uint32_t *bad = PART ? bad_rows + ((size_t)b * Hkv + g) * 3 : nullptr;
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -268,10 +254,8 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     for (int nb = 0; nb < NB; ++nb) o[t][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   wait_vmcnt<0>();   // the loop's vmcnt accounting covers the DMA only
-  if (PART && tid < 2 * NST) s_bad[tid] = 0;   // (before the prologue's barrier)
 
   auto stage_of = [&](int c) { return smem + ((c - c0) % NST) * STAGE; };
-  auto bad_of = [&](int c) { return PART ? s_bad + ((c - c0) % NST) * 2 : nullptr; };
   // The widening goes to the waves without a tile when there are any (one SIMD then
   // holds no more than its share of tile work plus widening), else to every wave.
   const int wbeg = ntiles < NW ? ntiles : 0;
@@ -285,7 +269,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
   if (c0 < c1) {
     if (c0 + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
     lds_barrier();
-    if (widener) widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad_of(c0));
+    if (widener) widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad);
   }
 
   // Fragment offsets: the swizzles depend on the lane only, so the read of K block kk at
@@ -309,7 +293,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     if (c + NST - 1 < c1)
       issue_chunk<HD, NW>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity, wave, lane);
     if (c + 1 < c1 && widener)
-      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad_of(c + 1));
+      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad);
 
     const uint16_t *st = stage_of(c);
     const f16 *sk = (const f16 *)st;
@@ -381,15 +365,6 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
           const f16x8 va = *(const f16x8 *)(sv + voff[ks] + nb * 16 * KC);
           o[t][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[ks], o[t][nb], 0, 0, 0);
         }
-      if (PART && tree_chunk && (bad_of(c)[0] | bad_of(c)[1])) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          float ob[4] = {o[t][nb][0], o[t][nb][1], o[t][nb][2], o[t][nb][3]};
-          add_marked(ob, [&](int e) { return nb * 16 + lg * 4 + e; }, bad_of(c), vb, capacity, key0,
-                     S, anc[t]);
-          o[t][nb] = f32x4{ob[0], ob[1], ob[2], ob[3]};
-        }
-      }
     }
     if (quarter) {
       // One 16-key block (key block qk of the chunk) of the split tile: 4 scores a lane.
@@ -580,7 +555,8 @@ template <int HD, int NST, bool PART = false>
 __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     const f16 *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
-    float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int rpg) {
+    float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int rpg,
+    uint32_t *bad_rows) {
   constexpr int NW = 8;
   constexpr int KS16 = HD / 16;   // 16-dim k-steps of a 32-row tile's S^T
   constexpr int NDB = HD / 32;    // 32-dim blocks of its O^T
@@ -590,7 +566,6 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   constexpr int L_DMA = HD / 4 / NW;
   static_assert(NST >= 3, "the widening runs one stage ahead of the MFMAs");
   __shared__ __attribute__((aligned(1024))) uint16_t smem[NST * STAGE];
-  __shared__ uint32_t s_bad[PART ? 2 * NST : 1];   // a stage's marked slots (widen_chunk)
 
   const int g = blockIdx.y, b = blockIdx.z;
   const int G = H / Hkv, QR = G * n1;
@@ -614,6 +589,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   const int cps = (nchunks + nsplit - 1) / nsplit;
   const int c0 = split * cps;
   const int c1 = min(nchunks, c0 + cps);
+  uint32_t *bad = PART ? bad_rows + ((size_t)b * Hkv + g) * 3 : nullptr;
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -667,10 +643,8 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     for (int nb = 0; nb < NB16; ++nb) oq[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   wait_vmcnt<0>();   // the loop's vmcnt accounting covers the DMA only
-  if (PART && tid < 2 * NST) s_bad[tid] = 0;   // (before the prologue's barrier)
 
   auto stage_of = [&](int c) { return smem + ((c - c0) % NST) * STAGE; };
-  auto bad_of = [&](int c) { return PART ? s_bad + ((c - c0) % NST) * 2 : nullptr; };
   const int wt = tid, wstride = NW * 64;   // every wave widens its share
 
   // Prologue: chunks c0 .. c0+NST-2 in flight, chunk c0 widened.
@@ -681,7 +655,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   if (c0 < c1) {
     if (c0 + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
     lds_barrier();
-    widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad_of(c0));
+    widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad);
   }
 
   // Fragment offsets (lane registers; blocks add compile-time constants): K row p32(lq)
@@ -710,7 +684,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
       issue_chunk<HD, NW, true>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity,
                                 wave, lane);
     if (c + 1 < c1)
-      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad_of(c + 1));
+      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad);
 
     const uint16_t *st = stage_of(c);
     const f16 *sk = (const f16 *)st;
@@ -784,17 +758,6 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
           }
       }
       SCHED_FENCE();
-      if (PART && tree_chunk && (bad_of(c)[0] | bad_of(c)[1])) {
-#pragma unroll
-        for (int i = 0; i < 4 * NDB; ++i) {
-          const int db = i >> 2, j = i & 3;
-          float ob[4] = {o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
-          add_marked(ob, [&](int e) { return 32 * db + 8 * j + 4 * hh + e; }, bad_of(c), vb, capacity,
-                     key0, S, anc);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[db][4 * j + e] = ob[e];
-        }
-      }
     }
     if (quarter) {
       // key block qk of the chunk for the remainder tile: 4 scores a lane
@@ -840,15 +803,6 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
       for (int nb = 0; nb < NB16; ++nb) {
         const f16x4 va = *(const f16x4 *)(sv + qvoff + nb * 16 * KC);
         oq[nb] = __builtin_amdgcn_mfma_f32_16x16x16f16(va, pq, oq[nb], 0, 0, 0);
-      }
-      if (PART && tree_chunk && qk == 0 && (bad_of(c)[0] | bad_of(c)[1])) {   // (once a tile)
-#pragma unroll
-        for (int nb = 0; nb < NB16; ++nb) {
-          float ob[4] = {oq[nb][0], oq[nb][1], oq[nb][2], oq[nb][3]};
-          add_marked(ob, [&](int e) { return nb * 16 + lg * 4 + e; }, bad_of(c), vb, capacity, key0,
-                     S, ancq);
-          oq[nb] = f32x4{ob[0], ob[1], ob[2], ob[3]};
-        }
       }
     }
   }
@@ -1083,10 +1037,10 @@ template <int HD> struct AttnCfg { static constexpr int NST = 4; };
 template <int HD, int NW, int UPW, bool PART>
 void launch_mfma(dim3 grid, hipStream_t s, const f16 *q, const bf16 *ck, const bf16 *cv,
                  const TreeMeta &meta, f16 *out, float *po, float *pml, int n1, int H, int Hkv,
-                 int capacity, int nsplit, int tpg) {
+                 int capacity, int nsplit, int tpg, uint32_t *bad) {
   hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, AttnCfg<HD>::NST, PART>), grid,
                      dim3(NW * 64), 0, s, q, ck, cv, meta, out, po, pml, n1, H, Hkv,
-                     capacity, nsplit, tpg);
+                     capacity, nsplit, tpg, bad);
 }
 
 // The kernels of one layer, without the merge of their splits.
@@ -1094,7 +1048,7 @@ template <bool PART>
 hipError_t launch_tree_attn(const f16 *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
                             f16 *out, float *part_o, float *part_ml, long long part_capacity, int B,
                             int n1, int H, int Hkv, int hd, int capacity, int cus, hipStream_t s,
-                            int *nsplit_used) {
+                            int *nsplit_used, uint32_t *bad) {
   const int G = H / Hkv, QR = G * n1;
   const int all_tiles = (QR + 15) / 16;
   if (capacity % KC != 0) return hipErrorInvalidValue;
@@ -1128,17 +1082,17 @@ hipError_t launch_tree_attn(const f16 *q, const bf16 *ck, const bf16 *cv, const 
     if (hd == 128)
       hipLaunchKernelGGL((tree_attn_t32_kernel<128, AttnCfg<128>::NST, PART>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
-                         rpg);
+                         rpg, bad);
     else
       hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, PART>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
-                         rpg);
+                         rpg, bad);
   } else if (hd == 128) {
     launch_mfma<128, 16, 1, PART>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                            capacity, nsplit, all_tiles);
+                            capacity, nsplit, all_tiles, bad);
   } else {
     launch_mfma<64, 16, 1, PART>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                           capacity, nsplit, all_tiles);
+                           capacity, nsplit, all_tiles, bad);
   }
   return hipGetLastError();
 }
@@ -1154,7 +1108,7 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
                                   int Hkv, int hd, int capacity, int cus, hipStream_t s,
                                   int *nsplit_used) {
   const hipError_t e = launch_tree_attn<false>(q, ck, cv, meta, out, part_o, part_ml, part_capacity, B,
-                                               n1, H, Hkv, hd, capacity, cus, s, nsplit_used);
+                                               n1, H, Hkv, hd, capacity, cus, s, nsplit_used, nullptr);
   const int nsplit = *nsplit_used;
   if (e != hipSuccess || nsplit == 1) return e;
   const int QR = H / Hkv * n1, cblocks = (QR * (hd / 4) + 255) / 256;
@@ -1166,9 +1120,9 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
 hipError_t launch_attention_part(const f16 *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
                                  float *part_o, float *part_ml, long long part_capacity, int B,
                                  int n1, int H, int Hkv, int hd, int capacity, int cus,
-                                 hipStream_t s, int *nsplit) {
+                                 hipStream_t s, int *nsplit, uint32_t *bad) {
   return launch_tree_attn<true>(q, ck, cv, meta, nullptr, part_o, part_ml, part_capacity, B, n1, H,
-                                Hkv, hd, capacity, cus, s, nsplit);
+                                Hkv, hd, capacity, cus, s, nsplit, bad);
 }
 
 template <>

@@ -208,7 +208,7 @@ template <int HD, bool ROWS>
 __global__ __launch_bounds__(256) void shared_combine_kernel(
     const float *__restrict__ sh_o, const float *__restrict__ sh_ml,
     const float *__restrict__ part_o, const float *__restrict__ part_ml, SharedMeta sm,
-    void *__restrict__ out, int rows, int n1, int H, int Hkv, int nsplit, int wgs,
+    const bf16 *__restrict__ cv, int capacity, TreeMeta meta, void *__restrict__ out, int rows, int n1, int H, int Hkv, int nsplit, int wgs,
     long long rows_total) {
   const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
   const int d = (int)(idx % (HD / 4)) * 4;
@@ -258,6 +258,20 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(
   for (int s = 0; s < nsplit; ++s)
     add(ml[(size_t)s * QR], *(const float4 *)(po + (size_t)s * QR * HD));
   const float inv = 1.f / den;   // (a row sees itself)
+  // values of the tree that are not finite were left out: whatever weight such a value has, an
+  // infinity or a NaN comes of it in the rows that see its slot
+  const uint32_t *bad = sm.bad + ((size_t)b * Hkv + g) * 3;
+  if (bad[0] | bad[1] | bad[2]) {
+    const bf16 *vb = cv + (((size_t)b * Hkv + g) * HD + d) * capacity + meta.sess_S[b];
+    for (int j = 0; j < n1; ++j) {
+      if (!((bad[j >> 5] >> (j & 31)) & 1u) || (j > 0 && !((meta.anc[row] >> (j - 1)) & 1ull))) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float v = (float)(f16)(float)vb[(size_t)i * capacity + j];
+        if (!(fabsf(v) <= 65504.f)) num[i] += v;
+      }
+    }
+  }
   if (ROWS) {
     typedef bf16 b4 __attribute__((ext_vector_type(4)));
     *(b4 *)((bf16 *)out + (size_t)row * H * HD + h * HD + d) =
@@ -369,8 +383,8 @@ __global__ __launch_bounds__(256) void shared_attn_f32_kernel(
 
 template <int HD>
 hipError_t launch_hd(const f16 *q, const f16 *blocks, const SharedArgs &sh, const SharedMeta &sm,
-                     void *out, int rows_out, float *sh_o, float *sh_ml, const float *part_o,
-                     const float *part_ml, int rows, int n1, int H, int Hkv, int cus, int nsplit,
+                     const bf16 *cv, int capacity, const TreeMeta &meta, void *out, int rows_out,
+                     float *sh_o, float *sh_ml, const float *part_o, const float *part_ml, int rows, int n1, int H, int Hkv, int cus, int nsplit,
                      hipStream_t s) {
   const int wgs = acespec::shared_wgs(Hkv, cus);
   const long long rows_total = acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus);
@@ -382,7 +396,7 @@ hipError_t launch_hd(const f16 *q, const f16 *blocks, const SharedArgs &sh, cons
   if (wg > 0x7fffffffLL / 256) return hipErrorInvalidValue;
   auto kernel = rows_out ? shared_combine_kernel<HD, true> : shared_combine_kernel<HD, false>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(256), 0, s, sh_o, sh_ml, part_o, part_ml, sm,
-                     out, rows, n1, H, Hkv, nsplit, wgs, rows_total);
+                     cv, capacity, meta, out, rows, n1, H, Hkv, nsplit, wgs, rows_total);
   return hipGetLastError();
 }
 
@@ -399,10 +413,10 @@ hipError_t launch_attention_shared<bf16>(const f16 *q, const f16 *blocks, const 
                                          int hd, int capacity, int cus, hipStream_t s) {
   int nsplit = 1;
   const hipError_t e = launch_attention_part(q, ck, cv, meta, part_o, part_ml, part_capacity, B, n1,
-                                             H, Hkv, hd, capacity, cus, s, &nsplit);
+                                             H, Hkv, hd, capacity, cus, s, &nsplit, sm.bad);
   if (e != hipSuccess) return e;
   auto launch = hd == 128 ? launch_hd<128> : launch_hd<64>;
-  return launch(q, blocks, sh, sm, out, rows_out, sh_o, sh_ml, part_o, part_ml, B * n1, n1, H, Hkv,
+  return launch(q, blocks, sh, sm, cv, capacity, meta, out, rows_out, sh_o, sh_ml, part_o, part_ml, B * n1, n1, H, Hkv,
                 cus, nsplit, s);
 }
 

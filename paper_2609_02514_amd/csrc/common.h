@@ -217,6 +217,7 @@ struct SharedMeta {
   long long *units;      // [B] by a group's first place: units of the groups before it
   SharedGroup *groups;   // [B]
   long long *total;      // [2] units of all groups; number of groups
+  uint32_t *bad;         // [B][kv heads][3] tree rows with values that are not finite
 };
 
 // Fixed-point scale for deterministic mass sums in the vocabulary kernel.
@@ -242,7 +243,7 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
 // then not written).  q [rows][width] bf16 or NULL: brought to fp16 at q16 on the way.
 hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
                                    const int32_t *prefix_len, int B, int n1, int V, int capacity,
-                                   const SharedArgs &sh, int G, int tile_rows, TreeMeta meta,
+                                   const SharedArgs &sh, int G, int Hkv, int tile_rows, TreeMeta meta,
                                    const SharedMeta &sm, int32_t *status, const bf16 *q, f16 *q16,
                                    int width, hipStream_t s);
 
@@ -347,11 +348,12 @@ hipError_t launch_attention(const typename ActOf<TW>::type *q, const TW *cache_k
                             int capacity, int cus, hipStream_t s, int *nsplit_used);
 
 // The same over the own slots alone of sessions behind shared prefixes: always as partial sums,
-// of *nsplit parts a session; a value that is not finite reaches only rows that see its slot.
+// of *nsplit parts a session.  Tree rows with values that are not finite are marked in bad (three
+// words a session and kv head, cleared by launch_tree_prep_shared) and these values left out.
 hipError_t launch_attention_part(const f16 *q, const bf16 *cache_k, const bf16 *cache_v,
                                  const TreeMeta &meta, float *part_o, float *part_ml,
                                  long long part_capacity, int B, int n1, int H, int Hkv, int hd,
-                                 int capacity, int cus, hipStream_t s, int *nsplit);
+                                 int capacity, int cus, hipStream_t s, int *nsplit, uint32_t *bad);
 
 // One layer's tree attention behind shared prefixes: blocks [P][Hkv][cap / 64] records, own slots
 // ck, cv as in launch_attention.  q is row-major [rows][H hd] in the activation type; out is in

@@ -163,12 +163,13 @@ AS_DEVICE void group_sessions(int B, int QR, const SharedArgs &sh, int tile_rows
 __global__ __launch_bounds__(TP_THREADS) void tree_prep_shared_kernel(
     const int32_t *__restrict__ tokens, const int32_t *__restrict__ parents,
     const int32_t *__restrict__ prefix_len, int B, int n1, int V, int capacity, SharedArgs sh,
-    int QR, int tile_rows, TreeMeta meta, SharedMeta sm, int32_t *__restrict__ status,
+    int QR, int Hkv, int tile_rows, TreeMeta meta, SharedMeta sm, int32_t *__restrict__ status,
     const bf16 *__restrict__ q, f16 *__restrict__ q16, long long pieces) {
   const int w = blockIdx.x;
   if (w == 0) {
     group_sessions(B, QR, sh, tile_rows, sm);
   } else if (w <= B) {
+    for (int i = threadIdx.x; i < 3 * Hkv; i += TP_THREADS) sm.bad[(size_t)(w - 1) * 3 * Hkv + i] = 0;
     int slots;
     shared_prefix(sh, w - 1, &slots);
     prepare_tree<false>(w - 1, tokens, parents, prefix_len, n1, V, capacity, 0, 0, slots, meta,
@@ -204,7 +205,7 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
 
 hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
                                    const int32_t *prefix_len, int B, int n1, int V, int capacity,
-                                   const SharedArgs &sh, int G, int tile_rows, TreeMeta meta,
+                                   const SharedArgs &sh, int G, int Hkv, int tile_rows, TreeMeta meta,
                                    const SharedMeta &sm, int32_t *status, const bf16 *q, f16 *q16,
                                    int width, hipStream_t s) {
   if (n1 > TP_THREADS || width % 8 != 0) return hipErrorInvalidValue;
@@ -212,7 +213,7 @@ hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents
   const long long wgs = 1 + B + (pieces + TP_THREADS - 1) / TP_THREADS;
   if (wgs > 0x7fffffffLL / TP_THREADS) return hipErrorInvalidValue;
   hipLaunchKernelGGL(tree_prep_shared_kernel, dim3((unsigned)wgs), dim3(TP_THREADS), 0, s, tokens,
-                     parents, prefix_len, B, n1, V, capacity, sh, G * n1, tile_rows, meta, sm,
+                     parents, prefix_len, B, n1, V, capacity, sh, G * n1, Hkv, tile_rows, meta, sm,
                      status, q, q16, pieces);
   return hipGetLastError();
 }
