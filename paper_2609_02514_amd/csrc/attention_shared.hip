@@ -27,6 +27,15 @@ AS_DEVICE float halves_sum(float v) {
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
+// An empty volatile asm keeps a seldom taken branch one (it is not if-converted into selects).
+#define MASK_BRANCH() __asm__ volatile("")
+
+// A value is computed where this stands, not where it is used.
+#define PIN(x) __asm__ volatile("" : "+v"(x))
+
+AS_DEVICE f16x8 load_f16x8(const f16 *p) { return *(const f16x8 *)p; }
+AS_DEVICE f16x8 load_f16x8(const bf16 *p) { return bf16x8_to_f16x8(*(const bf16x8 *)p); }
+
 AS_DEVICE void block_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Units of work (a record for a tile of TM rows) lie on a line: group after group, tile after
@@ -54,14 +63,21 @@ AS_DEVICE long long part_base(int first, int QR, long long tile, int w) {
 // order that makes a lane's scores 8 neighbouring slots) for S^T = K Q^T, then values (rows are
 // head dims) for O^T = V^T P^T.  A lane's scores, as fp16 weights, are its operand of the second
 // product, so they never leave its registers.  Records come by DMA into a ring of NST stages.
-template <int HD, int NST>
+//
+// What bounds it: a half record (32 slots) takes a wave 512 cycles of its SIMD's matrix core and
+// about 430 of its vector unit (16 exponentials of 16 cycles, their scaling, sums, rounding), and
+// two waves share a SIMD.  The halves are therefore pipelined: while the weights of one half are
+// computed, the scores of the next and the product with the values of the one before run, which
+// depend on none of it.
+template <int HD, int NST, typename QT>
 __global__ __launch_bounds__(512) void shared_attn_kernel(
-    const f16 *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
+    const QT *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
     float *__restrict__ part_o, float *__restrict__ part_ml, int n1, int H, int Hkv, int cap,
     int wgs, long long rows_total) {
   constexpr int KS = HD / 16, NDB = HD / 32;
   constexpr int REC = 128 * HD;                 // elements of a record
   constexpr int L_DMA = REC * 2 / 1024 / 8;     // 1 KB pieces a wave
+  static_assert(NST == 4, "the loop holds two records and has one in flight beside the next");
   __shared__ __attribute__((aligned(1024))) f16 smem[NST * REC];
   const int t = xcd_tile(blockIdx.x, gridDim.x), g = t / wgs, w = t - g * wgs;
   const long long units = sm.total[0];
@@ -99,11 +115,11 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     f16x8 qf[KS];
     {
       const int rr = min(row, rows - 1), m = rr / QR, rem = rr - m * QR, r = rem / G;
-      const f16 *qp = q + ((size_t)sm.order[grp.first + m] * n1 + r) * H * HD +
-                      (g * G + rem - r * G) * HD + hh * 8;
+      const QT *qp = q + ((size_t)sm.order[grp.first + m] * n1 + r) * H * HD +
+                     (g * G + rem - r * G) * HD + hh * 8;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const f16x8 v = *(const f16x8 *)(qp + s * 16);
+        const f16x8 v = load_f16x8(qp + s * 16);
         qf[s] = row < rows ? v : f16x8{};
       }
     }
@@ -113,74 +129,170 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+
+    auto stage_of = [&](int c) { return smem + ((c - c0) % NST) * REC + lane * 8; };
+    // S^T of half kb of a stage
+    auto scores = [&](const f16 *st, int kb, f32x16 &z) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8 *)(st + (kb * KS + s) * 512), qf[s], z,
+                                                   0, 0, 0);
+    };
+    // O^T += V^T P^T of half kb; valid: slots of the record (what lies behind the prefix may be no
+    // number at all)
+    auto values = [&](const f16 *st, int kb, const f16x8 (&p)[2], int valid) {
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          f16x8 v = *(const f16x8 *)(st + REC / 2 + ((kb * 2 + k2) * NDB + db) * 512);
+          if (valid < 64) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (kb * 32 + k2 * 16 + hh * 8 + e >= valid) v[e] = (f16)0.f;
+          }
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k2], o[db], 0, 0, 0);
+        }
+    };
+    // score i of a lane in half kb: slot 32 kb + 16 (i / 8) + 8 hh + i % 8
+    auto mask = [&](f32x16 &z, int kb, int valid) {
+      if (valid < 64) {
+        MASK_BRANCH();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (kb * 32 + (i >> 3) * 16 + hh * 8 + (i & 7) >= valid) z[i] = -INFINITY;
+      }
+    };
+    auto top = [&](const f32x16 &z) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, z[i]);
+      return halves_max(mx);
+    };
+    auto weights = [&](const f32x16 &z, f16x8 (&p)[2]) {
+      const float mb = m_run == -INFINITY ? 0.f : m_run * sscale;
+      float rs = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(z[i], sscale, -mb));
+        rs += e;
+        p[i >> 3][i & 7] = (f16)e;
+      }
+      l_run += rs;
+    };
+    // Moves the reference of the exponents where a score exceeds it by too much (seldom).  The
+    // product that is pending is in the old reference: settle() follows it.
+    float alpha = 1.f;
+    auto raise = [&](const f32x16 &z) {
+      const float mx = top(z);
+      const bool moved = __ballot(mx > m_run + lazy) != 0;
+      if (moved) {
+        MASK_BRANCH();
+        const float mn = mx > m_run + lazy ? mx : m_run;
+        alpha = __builtin_amdgcn_exp2f((m_run - (mn == -INFINITY ? 0.f : mn)) * sscale);
+        m_run = mn;
+        l_run *= alpha;
+      }
+      return moved;
+    };
+    auto settle = [&](bool moved) {
+      if (moved) {
+        MASK_BRANCH();
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+      }
+    };
+    // One half: the weights pc of scores zc, beside them the scores zn of half kn of stage sn and the
+    // product with half kv of stage sv that was pending (weights pp).  The products' operands are
+    // read two ahead, and each product is followed by the weights' share of its time.
+    auto half = [&](const f32x16 &zc, f16x8 (&pc)[2], f32x16 &zn, const f16 *sn, int kn,
+                    const f16x8 (&pp)[2], const f16 *sv, int kv) {
+      constexpr int SPP = 16 / KS;   // scores a pair of products
+      const f16 *kp = sn + kn * KS * 512, *vp = sv + REC / 2 + kv * KS * 512;
+      f16x8 kf[KS], vf[KS];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        kf[i] = *(const f16x8 *)(kp + i * 512);
+        vf[i] = *(const f16x8 *)(vp + i * 512);
+      }
+      const bool moved = raise(zc);
+      const float mb = m_run == -INFINITY ? 0.f : m_run * sscale;
+      float e[16], rs = 0.f;
+      auto sum = [&](int x0) {
+#pragma unroll
+        for (int x = x0; x < x0 + SPP; ++x) {
+          rs += e[x];
+          pc[x >> 3][x & 7] = (f16)e[x];
+        }
+        PIN(rs);
+      };
+#pragma unroll
+      for (int i = 0; i < 16; ++i) zn[i] = 0.f;
+      SCHED_FENCE();
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        zn = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], qf[i], zn, 0, 0, 0);
+        if (i + 2 < KS) kf[i + 2] = *(const f16x8 *)(kp + (i + 2) * 512);
+#pragma unroll
+        for (int x = i * SPP; x < (i + 1) * SPP; ++x) {
+          e[x] = __builtin_amdgcn_exp2f(fmaf(zc[x], sscale, -mb));
+          PIN(e[x]);
+        }
+        SCHED_FENCE();
+        o[i % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i], pp[i / NDB], o[i % NDB], 0, 0, 0);
+        if (i + 2 < KS) vf[i + 2] = *(const f16x8 *)(vp + (i + 2) * 512);
+        if (i > 0) sum((i - 1) * SPP);
+        SCHED_FENCE();
+      }
+      sum((KS - 1) * SPP);
+      l_run += rs;
+      PIN(pc[0]);
+      PIN(pc[1]);
+      settle(moved);
+    };
+
+
     block_barrier();      // the last tile's stages are free
-    wait_vmcnt<0>();      // the loop's count covers the DMA only
 #pragma unroll
     for (int i = 0; i < NST - 1; ++i)
       if (c0 + i < c1) issue(c0 + i);
-
-    for (int c = c0; c < c1; ++c) {
-      if (c + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
-      block_barrier();    // record c is there, record c - 1 is used up, for every wave
-      if (c + NST - 1 < c1) issue(c + NST - 1);
+    if (c0 + 2 < c1) wait_vmcnt<2 * L_DMA>(); else wait_vmcnt<0>();
+    block_barrier();      // record c0 is there
+    f32x16 za, zb;        // scores of the record's halves
+    f16x8 pa[2], pb[2];
+    if (any) {
+      const int valid = grp.slots - c0 * 64;
+      scores(stage_of(c0), 0, za);
+      mask(za, 0, valid);
+      m_run = top(za);
+      scores(stage_of(c0), 1, zb);
+      weights(za, pa);
+      mask(zb, 1, valid);
+    }
+    for (int c = c0; c + 1 < c1; ++c) {
+      if (c + 2 < c1) wait_vmcnt<L_DMA>(); else wait_vmcnt<0>();
+      block_barrier();    // record c + 1 is there, record c - 1 is used up, for every wave
+      if (c + 3 < c1) issue(c + 3);
       if (!any) continue;
-      const f16 *sk = smem + ((c - c0) % NST) * REC + lane * 8, *sv = sk + REC / 2;
-      const int valid = grp.slots - c * 64;
-      f32x16 sc[2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-          sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8 *)(sk + (kb * KS + s) * 512),
-                                                          qf[s], sc[kb], 0, 0, 0);
-      }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        // score i of this lane: slot 32 kb + 16 (i / 8) + 8 hh + i % 8
-        if (valid < 64) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (kb * 32 + (i >> 3) * 16 + hh * 8 + (i & 7) >= valid) sc[kb][i] = -INFINITY;
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kb][i]);
-        mx = halves_max(mx);
-        const float m_new = mx > m_run + lazy ? mx : m_run;
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f((m_run - m_use) * sscale);
-        m_run = m_new;
-        const float mb = m_use * sscale;
-        f16x8 p[2];
-        float rs = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], sscale, -mb));
-          rs += e;
-          p[i >> 3][i & 7] = (f16)e;
-        }
-        l_run = l_run * alpha + rs;
-        if (__ballot(alpha < 1.f)) {
-#pragma unroll
-          for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-        }
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) {
-            f16x8 v = *(const f16x8 *)(sv + ((kb * 2 + k2) * NDB + db) * 512);
-            if (valid < 64) {   // what lies behind the prefix may be no number at all
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (kb * 32 + k2 * 16 + hh * 8 + e >= valid) v[e] = (f16)0.f;
-            }
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k2], o[db], 0, 0, 0);
-          }
-      }
+      const f16 *st = stage_of(c), *next = stage_of(c + 1);
+      half(zb, pb, za, next, 0, pa, st, 0);
+      const int valid = grp.slots - (c + 1) * 64;
+      mask(za, 0, valid);
+      half(za, pa, zb, next, 1, pb, st, 1);
+      mask(zb, 1, valid);
+    }
+    if (any) {
+      const f16 *st = stage_of(c1 - 1);
+      const int valid = grp.slots - (c1 - 1) * 64;
+      const bool moved = raise(zb);
+      weights(zb, pb);
+      values(st, 0, pa, valid);
+      settle(moved);
+      values(st, 1, pb, valid);
     }
     const float l = halves_sum(l_run);
     if (row < rows) {
@@ -388,7 +500,7 @@ hipError_t launch_hd(const f16 *q, const f16 *blocks, const SharedArgs &sh, cons
                      hipStream_t s) {
   const int wgs = acespec::shared_wgs(Hkv, cus);
   const long long rows_total = acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus);
-  hipLaunchKernelGGL((shared_attn_kernel<HD, 4>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
+  hipLaunchKernelGGL((shared_attn_kernel<HD, 4, f16>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
                      sh_o, sh_ml, n1, H, Hkv, sh.cap, wgs, rows_total);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
