@@ -12,7 +12,9 @@
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LAZY_LOG2 = 8.f;   // the exponent's reference moves once a weight passes 2^8
+constexpr float RAISE = 1024.f;    // sum of 16 weights from which on their reference moves
+constexpr int AHEAD = 2;           // products whose operands are on their way from LDS
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -25,6 +27,13 @@ AS_DEVICE float halves_max(float v) {
 AS_DEVICE float halves_sum(float v) {
   auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// A value that all lanes hold alike, in a scalar register: what depends on it stays there too (loop
+// counts, addresses, branches), where a loaded value would make vector work of all of it.
+AS_DEVICE int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+AS_DEVICE long long uniform(long long v) {
+  return ((long long)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v);
 }
 
 // An empty volatile asm keeps a seldom taken branch one (it is not if-converted into selects).
@@ -80,27 +89,28 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
   static_assert(NST == 4, "the loop holds two records and has one in flight beside the next");
   __shared__ __attribute__((aligned(1024))) f16 smem[NST * REC];
   const int t = xcd_tile(blockIdx.x, gridDim.x), g = t / wgs, w = t - g * wgs;
-  const long long units = sm.total[0];
-  const int groups = (int)sm.total[1], wk = working(units, wgs);
+  const long long units = uniform(sm.total[0]);
+  const int groups = (int)uniform(sm.total[1]), wk = working(units, wgs);
   if (w >= wk) return;
   long long u = line_begin(w, units, wk);
   const long long uend = line_begin(w + 1, units, wk);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lq = lane & 31, hh = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), lq = lane & 31, hh = lane >> 5;
   const int G = H / Hkv, QR = G * n1;
-  const float sscale = LOG2E / sqrtf((float)HD), lazy = LAZY_LOG2 / sscale;
+  const float sscale = LOG2E / sqrtf((float)HD);
   int gi = 0;
-  while (gi + 1 < groups && sm.groups[gi + 1].units <= u) ++gi;
 
   while (u < uend) {
-    while (gi + 1 < groups && sm.groups[gi + 1].units <= u) ++gi;
-    const SharedGroup grp = sm.groups[gi];
-    const int nblk = (grp.slots + 63) >> 6, rows = grp.members * QR;
-    const int tile = (int)((u - grp.units) / nblk), c0 = (int)(u - grp.units - (long long)tile * nblk);
+    while (gi + 1 < groups && uniform(sm.groups[gi + 1].units) <= u) ++gi;
+    const SharedGroup *gp = sm.groups + gi;
+    const int first = uniform(gp->first), slots = uniform(gp->slots);
+    const long long before = uniform(gp->units);
+    const int nblk = (slots + 63) >> 6, rows = uniform(gp->members) * QR;
+    const int tile = (int)((u - before) / nblk), c0 = (int)(u - before - (long long)tile * nblk);
     const int c1 = (int)min((long long)nblk, c0 + (uend - u));
     u += c1 - c0;
     const int row = tile * TM + wave * 32 + lq;   // of the group
     const bool any = tile * TM + wave * 32 < rows;
-    const f16 *kv = blocks + (((size_t)grp.prefix * Hkv + g) * (cap >> 6) + c0) * REC;
+    const f16 *kv = blocks + (((size_t)uniform(gp->prefix) * Hkv + g) * (cap >> 6) + c0) * REC;
     const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(kv, (uint32_t)(c1 - c0) * (REC * 2));
     auto issue = [&](int c) {
       const int i = c - c0;
@@ -115,7 +125,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     f16x8 qf[KS];
     {
       const int rr = min(row, rows - 1), m = rr / QR, rem = rr - m * QR, r = rem / G;
-      const QT *qp = q + ((size_t)sm.order[grp.first + m] * n1 + r) * H * HD +
+      const QT *qp = q + ((size_t)sm.order[first + m] * n1 + r) * H * HD +
                      (g * G + rem - r * G) * HD + hh * 8;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -149,9 +159,11 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
         for (int db = 0; db < NDB; ++db) {
           f16x8 v = *(const f16x8 *)(st + REC / 2 + ((kb * 2 + k2) * NDB + db) * 512);
           if (valid < 64) {
+            MASK_BRANCH();
+            const int lim = valid - hh * 8 - kb * 32 - k2 * 16;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (kb * 32 + k2 * 16 + hh * 8 + e >= valid) v[e] = (f16)0.f;
+              if (e >= lim) v[e] = (f16)0.f;
           }
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k2], o[db], 0, 0, 0);
         }
@@ -160,9 +172,10 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     auto mask = [&](f32x16 &z, int kb, int valid) {
       if (valid < 64) {
         MASK_BRANCH();
+        const int lim = valid - hh * 8 - kb * 32;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (kb * 32 + (i >> 3) * 16 + hh * 8 + (i & 7) >= valid) z[i] = -INFINITY;
+          if ((i >> 3) * 16 + (i & 7) >= lim) z[i] = -INFINITY;
       }
     };
     auto top = [&](const f32x16 &z) {
@@ -171,8 +184,10 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, z[i]);
       return halves_max(mx);
     };
+    // The weights of scores z in the reference m_run; their sum.
+    auto reference = [&] { return m_run == -INFINITY ? 0.f : m_run * sscale; };
     auto weights = [&](const f32x16 &z, f16x8 (&p)[2]) {
-      const float mb = m_run == -INFINITY ? 0.f : m_run * sscale;
+      const float mb = reference();
       float rs = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -180,31 +195,26 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
         rs += e;
         p[i >> 3][i & 7] = (f16)e;
       }
-      l_run += rs;
+      return rs;
     };
-    // Moves the reference of the exponents where a score exceeds it by too much (seldom).  The
-    // product that is pending is in the old reference: settle() follows it.
-    float alpha = 1.f;
-    auto raise = [&](const f32x16 &z) {
-      const float mx = top(z);
-      const bool moved = __ballot(mx > m_run + lazy) != 0;
-      if (moved) {
+    // Takes up the sum rs of weights p of scores z.  The reference of the exponents is not looked
+    // for beforehand: it holds until a lane's weights add up to more than RAISE (each is then still
+    // far inside fp16), when it moves to the largest score and they are computed again.  o holds no
+    // product of p yet.
+    auto take = [&](const f32x16 &z, f16x8 (&p)[2], float rs) {
+      if (__ballot(rs > RAISE || m_run == -INFINITY)) {
         MASK_BRANCH();
-        const float mn = mx > m_run + lazy ? mx : m_run;
-        alpha = __builtin_amdgcn_exp2f((m_run - (mn == -INFINITY ? 0.f : mn)) * sscale);
+        const float mn = fmaxf(m_run, top(z));
+        const float alpha = __builtin_amdgcn_exp2f((m_run - (mn == -INFINITY ? 0.f : mn)) * sscale);
         m_run = mn;
         l_run *= alpha;
-      }
-      return moved;
-    };
-    auto settle = [&](bool moved) {
-      if (moved) {
-        MASK_BRANCH();
+        rs = weights(z, p);
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
       }
+      l_run += rs;
     };
     // One half: the weights pc of scores zc, beside them the scores zn of half kn of stage sn and the
     // product with half kv of stage sv that was pending (weights pp).  The products' operands are
@@ -215,18 +225,21 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
       const f16 *kp = sn + kn * KS * 512, *vp = sv + REC / 2 + kv * KS * 512;
       f16x8 kf[KS], vf[KS];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < AHEAD; ++i) {
         kf[i] = *(const f16x8 *)(kp + i * 512);
         vf[i] = *(const f16x8 *)(vp + i * 512);
       }
-      const bool moved = raise(zc);
-      const float mb = m_run == -INFINITY ? 0.f : m_run * sscale;
+      const float mb = reference();
       float e[16], rs = 0.f;
       auto sum = [&](int x0) {
 #pragma unroll
-        for (int x = x0; x < x0 + SPP; ++x) {
+        for (int x = x0; x < x0 + SPP; x += 2) {
           rs += e[x];
-          pc[x >> 3][x & 7] = (f16)e[x];
+          rs += e[x + 1];
+          f16x2 two = {(f16)e[x], (f16)e[x + 1]};
+          PIN(two);
+          pc[x >> 3][x & 7] = two[0];
+          pc[x >> 3][(x & 7) + 1] = two[1];
         }
         PIN(rs);
       };
@@ -236,7 +249,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
         zn = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[i], qf[i], zn, 0, 0, 0);
-        if (i + 2 < KS) kf[i + 2] = *(const f16x8 *)(kp + (i + 2) * 512);
+        if (i + AHEAD < KS) kf[i + AHEAD] = *(const f16x8 *)(kp + (i + AHEAD) * 512);
 #pragma unroll
         for (int x = i * SPP; x < (i + 1) * SPP; ++x) {
           e[x] = __builtin_amdgcn_exp2f(fmaf(zc[x], sscale, -mb));
@@ -244,17 +257,13 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
         }
         SCHED_FENCE();
         o[i % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i], pp[i / NDB], o[i % NDB], 0, 0, 0);
-        if (i + 2 < KS) vf[i + 2] = *(const f16x8 *)(vp + (i + 2) * 512);
+        if (i + AHEAD < KS) vf[i + AHEAD] = *(const f16x8 *)(vp + (i + AHEAD) * 512);
         if (i > 0) sum((i - 1) * SPP);
         SCHED_FENCE();
       }
       sum((KS - 1) * SPP);
-      l_run += rs;
-      PIN(pc[0]);
-      PIN(pc[1]);
-      settle(moved);
+      take(zc, pc, rs);
     };
-
 
     block_barrier();      // the last tile's stages are free
 #pragma unroll
@@ -265,12 +274,12 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     f32x16 za, zb;        // scores of the record's halves
     f16x8 pa[2], pb[2];
     if (any) {
-      const int valid = grp.slots - c0 * 64;
+      const int valid = slots - c0 * 64;
       scores(stage_of(c0), 0, za);
       mask(za, 0, valid);
       m_run = top(za);
       scores(stage_of(c0), 1, zb);
-      weights(za, pa);
+      l_run = weights(za, pa);
       mask(zb, 1, valid);
     }
     for (int c = c0; c + 1 < c1; ++c) {
@@ -280,24 +289,23 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
       if (!any) continue;
       const f16 *st = stage_of(c), *next = stage_of(c + 1);
       half(zb, pb, za, next, 0, pa, st, 0);
-      const int valid = grp.slots - (c + 1) * 64;
+      const int valid = slots - (c + 1) * 64;
       mask(za, 0, valid);
       half(za, pa, zb, next, 1, pb, st, 1);
       mask(zb, 1, valid);
     }
     if (any) {
       const f16 *st = stage_of(c1 - 1);
-      const int valid = grp.slots - (c1 - 1) * 64;
-      const bool moved = raise(zb);
-      weights(zb, pb);
+      const int valid = slots - (c1 - 1) * 64;
+      const float rs = weights(zb, pb);
       values(st, 0, pa, valid);
-      settle(moved);
+      take(zb, pb, rs);
       values(st, 1, pb, valid);
     }
     const float l = halves_sum(l_run);
     if (row < rows) {
       const long long at =
-          g * rows_total + part_base(grp.first, QR, tile, w) + wave * 32 + lq;
+          g * rows_total + part_base(first, QR, tile, w) + wave * 32 + lq;
       float *po = part_o + at * HD + hh * 4;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
