@@ -214,8 +214,7 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
                                        o->status, stream));
   else if (kv.shared)
     RUN(K_TREE, launch_tree_prep_shared(tokens, parents, kv.prefix_len, B, n1, V, cap, sh, H / Hkv,
-                                        Hkv, kSharedTile, meta, ctx->shm, o->status, nullptr, nullptr, 0,
-                                        stream));
+                                        Hkv, kSharedTile, meta, ctx->shm, o->status, stream));
   else
     RUN(K_TREE, launch_tree_prep(tokens, parents, kv.prefix_len, B, n1, V, cap, meta, o->status,
                                  stream));
@@ -466,7 +465,7 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
       {(size_t)max_batch * 4, &p_S},
       {shr * d.head_dim * 4, &p_so}, {shr * 2 * 4, &p_sml},
       {each * 4, &p_slots}, {each * 4, &p_place}, {each * 4, &p_first}, {each * 4, &p_order},
-      {each * 8, &p_units}, {each * sizeof(SharedGroup), &p_groups}, {layers ? 16u : 0u, &p_total},
+      {each * 4, &p_units}, {each * sizeof(SharedGroup), &p_groups}, {layers ? 8u : 0u, &p_total},
       {layers ? each * d.n_kv_heads * 12 : 0, &p_bad}};
   size_t total = 0;
   for (auto &pt : parts) total += align_up(pt.bytes);
@@ -501,8 +500,8 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   c->sh_o = (float *)p_so;
   c->sh_ml = (float *)p_sml;
   c->shm = SharedMeta{(int32_t *)p_slots, (int32_t *)p_place, (int32_t *)p_first,
-                      (int32_t *)p_order, (long long *)p_units, (SharedGroup *)p_groups,
-                      (long long *)p_total, (uint32_t *)p_bad};
+                      (int32_t *)p_order, (int32_t *)p_units, (SharedGroup *)p_groups,
+                      (int2 *)p_total, (uint32_t *)p_bad};
   if (layers) {
     std::vector<double> f(d.head_dim / 2);
     for (int i = 0; i < d.head_dim / 2; ++i)
@@ -634,6 +633,15 @@ size_t shared_bytes(const acespec_model_desc &d, const acespec_kv_shared *sh) {
   return d.n_layers * shared_layer_elems(d, sh) * (d.dtype == ACESPEC_BF16 ? 2 : 4);
 }
 
+// Units of work over shared prefixes (records times tiles of query rows) are counted in 32 bits.
+int check_units(const acespec_model_desc &d, const acespec_kv_shared *sh, int B, int N) {
+  const long long rows = (long long)B * (N + 1) * (d.n_heads / d.n_kv_heads);
+  const long long tiles = rows / kSharedTile + std::min(B, sh->prefixes) + 1;
+  if (tiles * (sh->capacity / 64) > 0x7fffffff)
+    return fail(ACESPEC_EUNSUPPORTED, "%lld query rows over prefixes of up to %d slots", rows, sh->capacity);
+  return ACESPEC_OK;
+}
+
 // What a call over one layer of a cache behind shared prefixes needs (sh may be NULL with may).
 int check_layer(const acespec_ctx *ctx, const acespec_kv_shared *sh, const int32_t *prefix_of,
                 bool may, const acespec_kv_cache *kv, int layer, const int32_t *parent_idx, int B,
@@ -650,7 +658,8 @@ int check_layer(const acespec_ctx *ctx, const acespec_kv_shared *sh, const int32
   if ((sh != nullptr) != (prefix_of != nullptr))
     return fail(ACESPEC_EINVAL, "shared prefixes and prefix_of come together (one of them is NULL)");
   if (!sh && may) return ACESPEC_OK;
-  return check_shared(d, sh, kv->capacity);
+  rc = check_shared(d, sh, kv->capacity);
+  return rc ? rc : check_units(d, sh, B, N);
 }
 
 int check_batch(const acespec_ctx *ctx, int B, int N) {
@@ -1182,20 +1191,18 @@ int acespec_attention_shared(acespec_ctx *ctx, const acespec_kv_shared *sh, cons
   const SharedArgs sa = shared_args(sh, prefix_of);
   const size_t own = (size_t)layer * B * Hkv * kv->capacity * hd;
   const size_t rec = layer * shared_layer_elems(d, sh);
-  const bool b16 = d.dtype == ACESPEC_BF16;
   RUN(K_TREE, launch_tree_prep_shared(nullptr, parent_idx, kv->prefix_len, B, n1, d.vocab,
                                       kv->capacity, sa, H / Hkv, Hkv, kSharedTile, ctx->meta, ctx->shm,
-                                      status, b16 ? (const bf16 *)q : nullptr, (f16 *)ctx->q, H * hd,
-                                      stream));
-  if (b16)
+                                      status, stream));
+  if (d.dtype == ACESPEC_BF16)
     RUN(K_ATTN, launch_attention_shared<bf16>(
-                    (const f16 *)ctx->q, (const f16 *)sh->blocks + rec, sa, ctx->shm,
+                    q, (const f16 *)sh->blocks + rec, sa, ctx->shm,
                     (const bf16 *)kv->k + own, (const bf16 *)kv->v + own, ctx->meta, out, 1, ctx->sh_o,
                     ctx->sh_ml, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
                     kv->capacity, ctx->cus, stream));
   else
     RUN(K_ATTN, launch_attention_shared<float>(
-                    (const float *)q, (const float *)sh->blocks + rec, sa, ctx->shm,
+                    q, (const float *)sh->blocks + rec, sa, ctx->shm,
                     (const float *)kv->k + own, (const float *)kv->v + own, ctx->meta, out, 1,
                     ctx->sh_o, ctx->sh_ml, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv,
                     hd, kv->capacity, ctx->cus, stream));

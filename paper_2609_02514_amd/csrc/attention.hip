@@ -42,7 +42,7 @@
 //  a small combine kernel.
 //
 // fp32 kernel (small models): one workgroup per (tree row, query head).
-#include "common.h"
+#include "shared.h"
 
 namespace {
 
@@ -142,13 +142,13 @@ AS_DEVICE void issue_chunk(uint16_t *stage, __amdgpu_buffer_rsrc_t kr,
   }
 }
 
-// Tree rows whose values are not all finite: three words a session and kv head.
+// Tree rows whose values are not all finite: three words.
 AS_DEVICE void mark_row(uint32_t *bad, int row) { atomicOr(bad + (row >> 5), 1u << (row & 31)); }
 
 // bf16 -> fp16 in place for pieces t, t + stride, ... of a stage (t: the thread's index
 // among the widening threads); value slots >= total are zeroed.
 // PART: values that are not finite are zeroed in the tree's slots (>= S) too, and their rows
-// marked in bad; the join of the parts brings them to the rows that see them.
+// marked in bad (in LDS); the join of the parts brings them to the rows that see them.
 template <int HD, bool PART = false>
 AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int total, int S = 0,
                            uint32_t *bad = nullptr) {
@@ -178,12 +178,12 @@ AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int tot
   }
 }
 
-template <int HD, int NW, int UPW, int NST, bool PART = false>
+template <int HD, int NW, int UPW, int NST, bool PART = false, typename TQ = f16>
 __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
-    const f16 *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
+    const TQ *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
     float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int tpg,
-    uint32_t *bad_rows) {
+    SharedJoin join) {
   constexpr int KSTEPS = HD / 32, NB = HD / 16;
   constexpr int STAGE = 2 * KC * HD;     // elements: K [KC][HD], then V^T [HD][KC]
   constexpr int L_DMA = HD / 4 / NW;     // DMA instructions per wave per chunk
@@ -216,7 +216,8 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
   const int cps = (nchunks + nsplit - 1) / nsplit;
   const int c0 = split * cps;
   const int c1 = min(nchunks, c0 + cps);
-  uint32_t *bad = PART ? bad_rows + ((size_t)b * Hkv + g) * 3 : nullptr;
+  __shared__ uint32_t bad[PART ? 3 : 1];   // tree rows with values that are not finite
+  if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -238,13 +239,13 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     int qi = (tbase + tile) * 16 + lr;   // (slot QS of a wave without a quarter unit: unused)
     qi = qi < 0 ? 0 : (qi < QR ? qi : QR - 1);
     const int r = qi / G, h = g * G + (qi - r * G);
-    const f16 *qp = qin + (row0 + r) * q_stride + h * HD;
+    const TQ *qp = qin + (row0 + r) * q_stride + h * HD;
     // padding rows of the last tile multiply zeros (their outputs are dropped; zero
     // operands keep the MFMA's switching, and so its power draw, down)
     const bool pad = (tbase + tile) * 16 + lr >= QR;
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) {
-      const f16x8 v = *(const f16x8 *)(qp + s * 32 + lg * 8);
+      const f16x8 v = load_f16x8(qp + s * 32 + lg * 8);
       qf[t][s] = pad ? f16x8{} : v;
     }
     anc[t] = meta.anc[row0 + r];
@@ -416,6 +417,11 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     }
   }
   wait_vmcnt<0>();
+  if (PART) {
+    __syncthreads();   // the marks are complete
+    if (!join.here && tid < 3 && bad[tid]) atomicOr(join.sm.bad + ((size_t)b * Hkv + g) * 3 + tid, bad[tid]);
+  }
+  const bf16 *vtree = vb + S;   // the tree's values
 
   if (split_last) {
     // Merge the quarter units of each split tile (the ring is free once every wave is
@@ -463,7 +469,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += wj[j] * v[e];
           }
-          if (!PART && nsplit == 1) {
+          if (nsplit == 1) {
             const float inv = L > 0.f ? 1.0f / L : 0.f;
             f16x4 v;
 #pragma unroll
@@ -474,7 +480,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
             *(f32x4 *)(part_o + (item * QR + qi) * HD + nb * 16 + lg * 4) = acc;
           }
         }
-        if ((PART || nsplit > 1) && qk == 0 && lg == 0) {
+        if (nsplit > 1 && qk == 0 && lg == 0) {
           const size_t item = ((size_t)b * Hkv + g) * nsplit + split;
           part_ml[(item * QR + qi) * 2 + 0] = M;
           part_ml[(item * QR + qi) * 2 + 1] = L;
@@ -492,7 +498,11 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
     const int qi = (tbase + tile) * 16 + lr;
     if (qi >= QR) continue;
     const int r = qi / G, h = g * G + (qi - r * G);
-    if (!PART && nsplit == 1) {
+    if (PART && join.here) {
+      shared_finish<HD>(join, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
+                        m_run[t] == -INFINITY ? -INFINITY : m_run[t] * sscale, l, o[t],
+                        [&](int nb) { return nb * 16 + lg * 4; });
+    } else if (!PART && nsplit == 1) {
       const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -551,12 +561,12 @@ AS_DEVICE float halves_sum(float v) {
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
-template <int HD, int NST, bool PART = false>
+template <int HD, int NST, bool PART = false, typename TQ = f16>
 __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
-    const f16 *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
+    const TQ *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
     float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int rpg,
-    uint32_t *bad_rows) {
+    SharedJoin join) {
   constexpr int NW = 8;
   constexpr int KS16 = HD / 16;   // 16-dim k-steps of a 32-row tile's S^T
   constexpr int NDB = HD / 32;    // 32-dim blocks of its O^T
@@ -589,7 +599,8 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   const int cps = (nchunks + nsplit - 1) / nsplit;
   const int c0 = split * cps;
   const int c1 = min(nchunks, c0 + cps);
-  uint32_t *bad = PART ? bad_rows + ((size_t)b * Hkv + g) * 3 : nullptr;
+  __shared__ uint32_t bad[PART ? 3 : 1];   // tree rows with values that are not finite
+  if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -610,10 +621,10 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     const bool pad = !t32 || qv >= rlo + rows;
     const int qi = min(qv, QR - 1);
     const int r = qi / G, h = g * G + (qi - r * G);
-    const f16 *qp = qin + (row0 + r) * q_stride + h * HD;
+    const TQ *qp = qin + (row0 + r) * q_stride + h * HD;
 #pragma unroll
     for (int s = 0; s < KS16; ++s) {
-      const f16x8 v = *(const f16x8 *)(qp + s * 16 + hh * 8);
+      const f16x8 v = load_f16x8(qp + s * 16 + hh * 8);
       qf[s] = pad ? f16x8{} : v;
     }
     anc = meta.anc[row0 + r];
@@ -632,10 +643,10 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     const bool pad = !quarter || lr >= rem;
     const int qi = min(qv, QR - 1);
     const int r = qi / G, h = g * G + (qi - r * G);
-    const f16 *qp = qin + (row0 + r) * q_stride + h * HD;
+    const TQ *qp = qin + (row0 + r) * q_stride + h * HD;
 #pragma unroll
     for (int s = 0; s < KS32; ++s) {
-      const f16x8 v = *(const f16x8 *)(qp + s * 32 + lg * 8);
+      const f16x8 v = load_f16x8(qp + s * 32 + lg * 8);
       qq[s] = pad ? f16x8{} : v;
     }
     ancq = meta.anc[row0 + r];
@@ -807,6 +818,11 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     }
   }
   wait_vmcnt<0>();
+  if (PART) {
+    __syncthreads();   // the marks are complete
+    if (!join.here && tid < 3 && bad[tid]) atomicOr(join.sm.bad + ((size_t)b * Hkv + g) * 3 + tid, bad[tid]);
+  }
+  const bf16 *vtree = vb + S;   // the tree's values
 
   if (rem > 0) {
     // Merge the remainder tile's four quarter units (the ring is free once every wave is
@@ -842,6 +858,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
       if (lr < rem) {
         const int r = qi / G, h = g * G + (qi - r * G);
         const size_t item = ((size_t)b * Hkv + g) * nsplit + split;
+        f32x4 all[NB16 / 4];
 #pragma unroll
         for (int i = 0; i < NB16 / 4; ++i) {
           const int nb = qk * (NB16 / 4) + i;
@@ -852,6 +869,8 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += wj[j] * v[e];
           }
+          all[i] = acc;
+          if (PART && join.here) continue;
           if (!PART && nsplit == 1) {
             const float inv = L > 0.f ? 1.0f / L : 0.f;
             f16x4 v;
@@ -862,7 +881,10 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
             *(f32x4 *)(part_o + (item * QR + qi) * HD + nb * 16 + lg * 4) = acc;
           }
         }
-        if ((PART || nsplit > 1) && qk == 0 && lg == 0) {
+        if (PART && join.here)
+          shared_finish<HD>(join, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all, M, L, all,
+                            [&](int i) { return (qk * (NB16 / 4) + i) * 16 + lg * 4; });
+        if ((PART ? !join.here : nsplit > 1) && qk == 0 && lg == 0) {
           part_ml[(item * QR + qi) * 2 + 0] = M;
           part_ml[(item * QR + qi) * 2 + 1] = L;
         }
@@ -876,7 +898,16 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     const int qi = rlo + wave * 32 + lq;
     if (qi < rlo + rows) {
       const int r = qi / G, h = g * G + (qi - r * G);
-      if (!PART && nsplit == 1) {
+      if (PART && join.here) {
+        f32x4 all[4 * NDB];
+#pragma unroll
+        for (int i = 0; i < 4 * NDB; ++i)
+          all[i] = f32x4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2],
+                         o[i >> 2][4 * (i & 3) + 3]};
+        shared_finish<HD>(join, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
+                          m_run == -INFINITY ? -INFINITY : m_run * sscale, l, all,
+                          [&](int i) { return 8 * i + 4 * hh; });
+      } else if (!PART && nsplit == 1) {
         const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
@@ -1034,21 +1065,21 @@ __global__ __launch_bounds__(256) void tree_attn_f32_kernel(
 // Ring depth: 4 stages of 32 KB (head_dim 128) or 16 KB (head_dim 64).
 template <int HD> struct AttnCfg { static constexpr int NST = 4; };
 
-template <int HD, int NW, int UPW, bool PART>
-void launch_mfma(dim3 grid, hipStream_t s, const f16 *q, const bf16 *ck, const bf16 *cv,
+template <int HD, int NW, int UPW, bool PART, typename TQ>
+void launch_mfma(dim3 grid, hipStream_t s, const TQ *q, const bf16 *ck, const bf16 *cv,
                  const TreeMeta &meta, f16 *out, float *po, float *pml, int n1, int H, int Hkv,
-                 int capacity, int nsplit, int tpg, uint32_t *bad) {
-  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, AttnCfg<HD>::NST, PART>), grid,
+                 int capacity, int nsplit, int tpg, const SharedJoin &join) {
+  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, AttnCfg<HD>::NST, PART, TQ>), grid,
                      dim3(NW * 64), 0, s, q, ck, cv, meta, out, po, pml, n1, H, Hkv,
-                     capacity, nsplit, tpg, bad);
+                     capacity, nsplit, tpg, join);
 }
 
 // The kernels of one layer, without the merge of their splits.
-template <bool PART>
-hipError_t launch_tree_attn(const f16 *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
+template <bool PART, typename TQ>
+hipError_t launch_tree_attn(const TQ *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
                             f16 *out, float *part_o, float *part_ml, long long part_capacity, int B,
                             int n1, int H, int Hkv, int hd, int capacity, int cus, hipStream_t s,
-                            int *nsplit_used, uint32_t *bad) {
+                            int *nsplit_used, SharedJoin join) {
   const int G = H / Hkv, QR = G * n1;
   const int all_tiles = (QR + 15) / 16;
   if (capacity % KC != 0) return hipErrorInvalidValue;
@@ -1077,22 +1108,23 @@ hipError_t launch_tree_attn(const f16 *q, const bf16 *ck, const bf16 *cv, const 
   if (nsplit < 1) nsplit = 1;
   while (nsplit > 1 && (long long)B * Hkv * nsplit * QR * hd > part_capacity) --nsplit;
   *nsplit_used = nsplit;
+  if (PART && nsplit > 1) join.here = 0;
   const dim3 grid(nsplit * nqg, Hkv, B);
   if (t32) {
     if (hd == 128)
-      hipLaunchKernelGGL((tree_attn_t32_kernel<128, AttnCfg<128>::NST, PART>), grid, dim3(512), 0, s,
+      hipLaunchKernelGGL((tree_attn_t32_kernel<128, AttnCfg<128>::NST, PART, TQ>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
-                         rpg, bad);
+                         rpg, join);
     else
-      hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, PART>), grid, dim3(512), 0, s,
+      hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, PART, TQ>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
-                         rpg, bad);
+                         rpg, join);
   } else if (hd == 128) {
-    launch_mfma<128, 16, 1, PART>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                            capacity, nsplit, all_tiles, bad);
+    launch_mfma<128, 16, 1, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+                            capacity, nsplit, all_tiles, join);
   } else {
-    launch_mfma<64, 16, 1, PART>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                           capacity, nsplit, all_tiles, bad);
+    launch_mfma<64, 16, 1, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+                           capacity, nsplit, all_tiles, join);
   }
   return hipGetLastError();
 }
@@ -1107,8 +1139,8 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
                                   float *part_ml, long long part_capacity, int B, int n1, int H,
                                   int Hkv, int hd, int capacity, int cus, hipStream_t s,
                                   int *nsplit_used) {
-  const hipError_t e = launch_tree_attn<false>(q, ck, cv, meta, out, part_o, part_ml, part_capacity, B,
-                                               n1, H, Hkv, hd, capacity, cus, s, nsplit_used, nullptr);
+  const hipError_t e = launch_tree_attn<false, f16>(q, ck, cv, meta, out, part_o, part_ml, part_capacity, B,
+                                               n1, H, Hkv, hd, capacity, cus, s, nsplit_used, SharedJoin{});
   const int nsplit = *nsplit_used;
   if (e != hipSuccess || nsplit == 1) return e;
   const int QR = H / Hkv * n1, cblocks = (QR * (hd / 4) + 255) / 256;
@@ -1117,13 +1149,22 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
   return hipGetLastError();
 }
 
-hipError_t launch_attention_part(const f16 *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
-                                 float *part_o, float *part_ml, long long part_capacity, int B,
-                                 int n1, int H, int Hkv, int hd, int capacity, int cus,
-                                 hipStream_t s, int *nsplit, uint32_t *bad) {
-  return launch_tree_attn<true>(q, ck, cv, meta, nullptr, part_o, part_ml, part_capacity, B, n1, H,
-                                Hkv, hd, capacity, cus, s, nsplit, bad);
+template <typename TQ>
+hipError_t launch_attention_own(const TQ *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
+                                const SharedJoin &j, float *part_o, float *part_ml,
+                                long long part_capacity, int B, int n1, int H, int Hkv, int hd,
+                                int capacity, int cus, hipStream_t s, int *nsplit) {
+  return launch_tree_attn<true, TQ>(q, ck, cv, meta, nullptr, part_o, part_ml, part_capacity, B, n1, H,
+                                    Hkv, hd, capacity, cus, s, nsplit, j);
 }
+template hipError_t launch_attention_own<f16>(const f16 *, const bf16 *, const bf16 *,
+                                              const TreeMeta &, const SharedJoin &, float *, float *,
+                                              long long, int, int, int, int, int, int, int,
+                                              hipStream_t, int *);
+template hipError_t launch_attention_own<bf16>(const bf16 *, const bf16 *, const bf16 *,
+                                               const TreeMeta &, const SharedJoin &, float *,
+                                               float *, long long, int, int, int, int, int, int, int,
+                                               hipStream_t, int *);
 
 template <>
 hipError_t launch_attention<float>(const float *q, const float *ck, const float *cv,

@@ -7,7 +7,7 @@
 // against the prefix's records, a matrix product with a softmax between, where a session alone
 // would stream the prefix for G * (N + 1) rows.  The own slots are the tree attention's work
 // (attention.hip); both leave partial (sum, max, outputs) and one pass joins them.
-#include "common.h"
+#include "shared.h"
 
 namespace {
 
@@ -32,9 +32,6 @@ AS_DEVICE float halves_sum(float v) {
 // A value that all lanes hold alike, in a scalar register: what depends on it stays there too (loop
 // counts, addresses, branches), where a loaded value would make vector work of all of it.
 AS_DEVICE int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-AS_DEVICE long long uniform(long long v) {
-  return ((long long)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v);
-}
 
 // An empty volatile asm keeps a seldom taken branch one (it is not if-converted into selects).
 #define MASK_BRANCH() __asm__ volatile("")
@@ -42,30 +39,7 @@ AS_DEVICE long long uniform(long long v) {
 // A value is computed where this stands, not where it is used.
 #define PIN(x) __asm__ volatile("" : "+v"(x))
 
-AS_DEVICE f16x8 load_f16x8(const f16 *p) { return *(const f16x8 *)p; }
-AS_DEVICE f16x8 load_f16x8(const bf16 *p) { return bf16x8_to_f16x8(*(const bf16x8 *)p); }
-
 AS_DEVICE void block_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// Units of work (a record for a tile of TM rows) lie on a line: group after group, tile after
-// tile, record after record.  Workgroup w of `wgs` takes [w U / wgs, (w + 1) U / wgs) of a kv
-// head's line, so that all finish together whatever the lengths; a tile that is cut leaves
-// several partial results.  At least `least` units a workgroup, and no more workgroups than units.
-AS_DEVICE int working(long long units, int wgs) {
-  constexpr int least = 4;
-  const long long n = (units + least - 1) / least;
-  return (int)(n < wgs ? n : wgs);
-}
-AS_DEVICE long long line_begin(int w, long long units, int wgs) { return w * units / wgs; }
-// the workgroup that takes unit u
-AS_DEVICE int worker_of(long long u, long long units, int wgs) {
-  return (int)(((u + 1) * wgs - 1) / units);
-}
-// Where the partial rows of (a group's first member, tile, workgroup) begin, of one kv head: rows
-// and workgroups both only grow along the line, so no two meet.
-AS_DEVICE long long part_base(int first, int QR, long long tile, int w) {
-  return (long long)first * QR + (tile + w) * TM;
-}
 
 // Eight waves, 32 query rows each, over one record after the other.  A record is 1 KB operands of
 // v_mfma_f32_32x32x16_f16 in the order in which they are multiplied: keys (rows are slots, in an
@@ -81,7 +55,7 @@ AS_DEVICE long long part_base(int first, int QR, long long tile, int w) {
 template <int HD, int NST, typename QT>
 __global__ __launch_bounds__(512) void shared_attn_kernel(
     const QT *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
-    float *__restrict__ part_o, float *__restrict__ part_ml, int n1, int H, int Hkv, int cap,
+    float *__restrict__ part_o, float *__restrict__ part_ml, int B, int n1, int H, int Hkv, int cap,
     int wgs, long long rows_total) {
   constexpr int KS = HD / 16, NDB = HD / 32;
   constexpr int REC = 128 * HD;                 // elements of a record
@@ -89,28 +63,35 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
   static_assert(NST == 4, "the loop holds two records and has one in flight beside the next");
   __shared__ __attribute__((aligned(1024))) f16 smem[NST * REC];
   const int t = xcd_tile(blockIdx.x, gridDim.x), g = t / wgs, w = t - g * wgs;
-  const long long units = uniform(sm.total[0]);
-  const int groups = (int)uniform(sm.total[1]), wk = working(units, wgs);
-  if (w >= wk) return;
-  long long u = line_begin(w, units, wk);
-  const long long uend = line_begin(w + 1, units, wk);
+  // (the groups are asked for, 64 at a time, before it is known how many there are)
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), lq = lane & 31, hh = lane >> 5;
+  SharedGroup mine = sm.groups[min(lane, B - 1)];
+  const int2 total = *sm.total;
+  const int groups = uniform(total.y);
+  const SharedLine line(uniform(total.x), wgs);
+  if (w >= line.n) return;
+  int u = line.begin(w), at = 0;   // `mine` is group at + lane
+  const int uend = line.begin(w + 1);
   const int G = H / Hkv, QR = G * n1;
   const float sscale = LOG2E / sqrtf((float)HD);
-  int gi = 0;
 
   while (u < uend) {
-    while (gi + 1 < groups && uniform(sm.groups[gi + 1].units) <= u) ++gi;
-    const SharedGroup *gp = sm.groups + gi;
-    const int first = uniform(gp->first), slots = uniform(gp->slots);
-    const long long before = uniform(gp->units);
-    const int nblk = (slots + 63) >> 6, rows = uniform(gp->members) * QR;
-    const int tile = (int)((u - before) / nblk), c0 = (int)(u - before - (long long)tile * nblk);
-    const int c1 = (int)min((long long)nblk, c0 + (uend - u));
+    int before;   // groups of the 64 that begin at u or before
+    while ((before = __popcll(__ballot(at + lane < groups && mine.units <= u))) == 64 && at + 64 < groups &&
+           uniform(sm.groups[at + 64].units) <= u) {
+      at += 64;
+      mine = sm.groups[min(at + lane, B - 1)];
+    }
+    const int gi = before - 1;
+    const int first = __builtin_amdgcn_readlane(mine.first, gi), slots = __builtin_amdgcn_readlane(mine.slots, gi);
+    const int prefix = __builtin_amdgcn_readlane(mine.prefix, gi);
+    const int rows = __builtin_amdgcn_readlane(mine.members, gi) * QR, nblk = (slots + 63) >> 6;
+    const int in = u - __builtin_amdgcn_readlane(mine.units, gi), tile = in / nblk, c0 = in - tile * nblk;
+    const int c1 = min(nblk, c0 + (uend - u));
     u += c1 - c0;
     const int row = tile * TM + wave * 32 + lq;   // of the group
     const bool any = tile * TM + wave * 32 < rows;
-    const f16 *kv = blocks + (((size_t)uniform(gp->prefix) * Hkv + g) * (cap >> 6) + c0) * REC;
+    const f16 *kv = blocks + (((size_t)prefix * Hkv + g) * (cap >> 6) + c0) * REC;
     const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(kv, (uint32_t)(c1 - c0) * (REC * 2));
     auto issue = [&](int c) {
       const int i = c - c0;
@@ -304,9 +285,8 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     }
     const float l = halves_sum(l_run);
     if (row < rows) {
-      const long long at =
-          g * rows_total + part_base(first, QR, tile, w) + wave * 32 + lq;
-      float *po = part_o + at * HD + hh * 4;
+      const long long to = g * rows_total + shared_rows_at(first, QR, tile, w) + wave * 32 + lq;
+      float *po = part_o + to * HD + hh * 4;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -314,22 +294,22 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
           *(f32x4 *)(po + db * 32 + j * 8) =
               f32x4{o[db][j * 4], o[db][j * 4 + 1], o[db][j * 4 + 2], o[db][j * 4 + 3]};
       if (hh == 0) {
-        part_ml[at * 2] = m_run == -INFINITY ? -INFINITY : m_run * sscale;
-        part_ml[at * 2 + 1] = l;
+        part_ml[to * 2] = m_run == -INFINITY ? -INFINITY : m_run * sscale;
+        part_ml[to * 2 + 1] = l;
       }
     }
   }
 }
 
-// A row's partial results joined: of its tile over the shared prefix, and of its session's own
-// slots.  One thread per four head dims.  ROWS: out is row-major bf16, else in the activation
-// layout.  (A part without slots has weight 2^-inf = 0 and zero sums.)
-template <int HD, bool ROWS>
-__global__ __launch_bounds__(256) void shared_combine_kernel(
-    const float *__restrict__ sh_o, const float *__restrict__ sh_ml,
-    const float *__restrict__ part_o, const float *__restrict__ part_ml, SharedMeta sm,
-    const bf16 *__restrict__ cv, int capacity, TreeMeta meta, void *__restrict__ out, int rows, int n1, int H, int Hkv, int nsplit, int wgs,
-    long long rows_total) {
+// A row's partial results joined where its session was split: of its tile over the shared prefix,
+// and of the parts of its own slots.  One thread per four head dims.
+template <int HD>
+__global__ __launch_bounds__(256) void shared_combine_kernel(const float *__restrict__ part_o,
+                                                             const float *__restrict__ part_ml,
+                                                             SharedJoin j, TreeMeta meta,
+                                                             const bf16 *__restrict__ cv,
+                                                             int capacity, int rows, int n1, int H,
+                                                             int Hkv, int nsplit) {
   const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
   const int d = (int)(idx % (HD / 4)) * 4;
   const long long rh = idx / (HD / 4);
@@ -340,66 +320,22 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(
   const size_t item0 = ((size_t)b * Hkv + g) * nsplit * QR + qi;
   const float2 *ml = (const float2 *)part_ml + item0;
   const float *po = part_o + item0 * HD + d;
-  const int place = sm.place[b], slots = sm.slots[b];
-  const float2 *sml = nullptr;
-  const float *spo = nullptr;
-  int parts = 0;
-  if (place >= 0) {
-    const int first = sm.first[b];
-    const long long units = sm.total[0];
-    const int wk = working(units, wgs), nblk = (slots + 63) >> 6;
-    const long long local = (long long)(place - first) * QR + qi, tile = local / TM;
-    const long long u0 = sm.units[first] + tile * nblk;
-    const int w0 = worker_of(u0, units, wk);
-    parts = worker_of(u0 + nblk - 1, units, wk) - w0 + 1;
-    const long long at = g * rows_total + part_base(first, QR, tile, w0) + (local - tile * TM);
-    sml = (const float2 *)sh_ml + at;
-    spo = sh_o + at * HD + d;
-  }
   float M = -INFINITY;
 #pragma unroll 4
-  for (int s = 0; s < parts; ++s) M = fmaxf(M, sml[(size_t)s * TM].x);
-#pragma unroll 4
   for (int s = 0; s < nsplit; ++s) M = fmaxf(M, ml[(size_t)s * QR].x);
-  if (M == -INFINITY) M = 0.f;
-  float num[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
-  auto add = [&](float2 e, float4 v) {
-    const float x = __builtin_amdgcn_exp2f(e.x - M);
-    den += x * e.y;
-    num[0] += x * v.x;
-    num[1] += x * v.y;
-    num[2] += x * v.z;
-    num[3] += x * v.w;
-  };
+  const float top = M == -INFINITY ? 0.f : M;
+  f32x4 o[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
+  float l = 0.f;
 #pragma unroll 4
-  for (int s = 0; s < parts; ++s)
-    add(sml[(size_t)s * TM], *(const float4 *)(spo + (size_t)s * TM * HD));
-#pragma unroll 4
-  for (int s = 0; s < nsplit; ++s)
-    add(ml[(size_t)s * QR], *(const float4 *)(po + (size_t)s * QR * HD));
-  const float inv = 1.f / den;   // (a row sees itself)
-  // values of the tree that are not finite were left out: whatever weight such a value has, an
-  // infinity or a NaN comes of it in the rows that see its slot
-  const uint32_t *bad = sm.bad + ((size_t)b * Hkv + g) * 3;
-  if (bad[0] | bad[1] | bad[2]) {
-    const bf16 *vb = cv + (((size_t)b * Hkv + g) * HD + d) * capacity + meta.sess_S[b];
-    for (int j = 0; j < n1; ++j) {
-      if (!((bad[j >> 5] >> (j & 31)) & 1u) || (j > 0 && !((meta.anc[row] >> (j - 1)) & 1ull))) continue;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float v = (float)(f16)(float)vb[(size_t)i * capacity + j];
-        if (!(fabsf(v) <= 65504.f)) num[i] += v;
-      }
-    }
+  for (int s = 0; s < nsplit; ++s) {
+    const float2 e = ml[(size_t)s * QR];   // (a part without slots: weight 2^-inf, zero sums)
+    const float x = __builtin_amdgcn_exp2f(e.x - top);
+    l += x * e.y;
+    o[0] += x * *(const f32x4 *)(po + (size_t)s * QR * HD);
   }
-  if (ROWS) {
-    typedef bf16 b4 __attribute__((ext_vector_type(4)));
-    *(b4 *)((bf16 *)out + (size_t)row * H * HD + h * HD + d) =
-        b4{(bf16)(num[0] * inv), (bf16)(num[1] * inv), (bf16)(num[2] * inv), (bf16)(num[3] * inv)};
-  } else {
-    *(f16x4 *)((f16 *)out + act_off(row, h * HD + d, rows, H * HD)) =
-        f16x4{(f16)(num[0] * inv), (f16)(num[1] * inv), (f16)(num[2] * inv), (f16)(num[3] * inv)};
-  }
+  const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity + meta.sess_S[b];
+  shared_finish<HD>(j, meta, vb, capacity, j.sm.bad + ((size_t)b * Hkv + g) * 3, b, g, qi, n1, H, Hkv,
+                    rows, M, l, o, [&](int) { return d; });
 }
 
 // fp32 models: one workgroup per (tree row, query head), over the prefix's records and then the
@@ -501,22 +437,30 @@ __global__ __launch_bounds__(256) void shared_attn_f32_kernel(
   }
 }
 
-template <int HD>
-hipError_t launch_hd(const f16 *q, const f16 *blocks, const SharedArgs &sh, const SharedMeta &sm,
-                     const bf16 *cv, int capacity, const TreeMeta &meta, void *out, int rows_out,
-                     float *sh_o, float *sh_ml, const float *part_o, const float *part_ml, int rows, int n1, int H, int Hkv, int cus, int nsplit,
-                     hipStream_t s) {
-  const int wgs = acespec::shared_wgs(Hkv, cus);
-  const long long rows_total = acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus);
-  hipLaunchKernelGGL((shared_attn_kernel<HD, 4, f16>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
-                     sh_o, sh_ml, n1, H, Hkv, sh.cap, wgs, rows_total);
+template <int HD, typename TQ>
+hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const SharedMeta &sm,
+                     const bf16 *ck, const bf16 *cv, const TreeMeta &meta, void *out, int rows_out,
+                     float *sh_o, float *sh_ml, float *part_o, float *part_ml, long long part_cap,
+                     int B, int n1, int H, int Hkv, int capacity, int cus, hipStream_t s) {
+  const int rows = B * n1, wgs = acespec::shared_wgs(Hkv, cus);
+  // Few tiles are cut into many parts, which a kernel of its own joins faster, with a thread for four
+  // head dims, than the waves over the own slots do (64 single tokens, one tile in 32 parts: 30 + 10
+  // us against 88; the 8B batch, 17 tiles in up to three: 45 + 18 against 57).
+  const int here = 3LL * rows * (H / Hkv) >= (long long)wgs * TM;
+  const SharedJoin j{sh_o, sh_ml, sm, wgs,
+                     acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus), out, rows_out, here};
+  hipLaunchKernelGGL((shared_attn_kernel<HD, 4, TQ>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
+                     sh_o, sh_ml, B, n1, H, Hkv, sh.cap, wgs, j.rows_total);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  int nsplit = 1;
+  e = acespec::launch_attention_own(q, ck, cv, meta, j, part_o, part_ml, part_cap, B, n1, H, Hkv, HD,
+                                    capacity, cus, s, &nsplit);
+  if (e != hipSuccess || (here && nsplit == 1)) return e;
   const long long wg = ((long long)rows * H * (HD / 4) + 255) / 256;
-  if (wg > 0x7fffffffLL / 256) return hipErrorInvalidValue;
-  auto kernel = rows_out ? shared_combine_kernel<HD, true> : shared_combine_kernel<HD, false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(256), 0, s, sh_o, sh_ml, part_o, part_ml, sm,
-                     cv, capacity, meta, out, rows, n1, H, Hkv, nsplit, wgs, rows_total);
+  if (wg > 0xffffffffLL / 256) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(shared_combine_kernel<HD>, dim3((unsigned)wg), dim3(256), 0, s, part_o, part_ml, j,
+                     meta, cv, capacity, rows, n1, H, Hkv, nsplit);
   return hipGetLastError();
 }
 
@@ -525,29 +469,29 @@ hipError_t launch_hd(const f16 *q, const f16 *blocks, const SharedArgs &sh, cons
 namespace acespec {
 
 template <>
-hipError_t launch_attention_shared<bf16>(const f16 *q, const f16 *blocks, const SharedArgs &sh,
+hipError_t launch_attention_shared<bf16>(const void *q, const f16 *blocks, const SharedArgs &sh,
                                          const SharedMeta &sm, const bf16 *ck, const bf16 *cv,
-                                         const TreeMeta &meta, void *out, int rows_out, float *sh_o,
+                                         const TreeMeta &meta, void *out, int rows_io, float *sh_o,
                                          float *sh_ml, float *part_o, float *part_ml,
                                          long long part_capacity, int B, int n1, int H, int Hkv,
                                          int hd, int capacity, int cus, hipStream_t s) {
-  int nsplit = 1;
-  const hipError_t e = launch_attention_part(q, ck, cv, meta, part_o, part_ml, part_capacity, B, n1,
-                                             H, Hkv, hd, capacity, cus, s, &nsplit, sm.bad);
-  if (e != hipSuccess) return e;
-  auto launch = hd == 128 ? launch_hd<128> : launch_hd<64>;
-  return launch(q, blocks, sh, sm, cv, capacity, meta, out, rows_out, sh_o, sh_ml, part_o, part_ml, B * n1, n1, H, Hkv,
-                cus, nsplit, s);
+  auto run = [&](auto launch, auto *queries) {
+    return launch(queries, blocks, sh, sm, ck, cv, meta, out, rows_io, sh_o, sh_ml, part_o, part_ml,
+                  part_capacity, B, n1, H, Hkv, capacity, cus, s);
+  };
+  if (rows_io)
+    return hd == 128 ? run(launch_hd<128, bf16>, (const bf16 *)q) : run(launch_hd<64, bf16>, (const bf16 *)q);
+  return hd == 128 ? run(launch_hd<128, f16>, (const f16 *)q) : run(launch_hd<64, f16>, (const f16 *)q);
 }
 
 template <>
-hipError_t launch_attention_shared<float>(const float *q, const float *blocks, const SharedArgs &sh,
+hipError_t launch_attention_shared<float>(const void *q, const float *blocks, const SharedArgs &sh,
                                           const SharedMeta &sm, const float *ck, const float *cv,
                                           const TreeMeta &meta, void *out, int, float *, float *,
                                           float *, float *, long long, int B, int n1, int H,
                                           int Hkv, int hd, int capacity, int, hipStream_t s) {
   auto kernel = hd == 64 ? shared_attn_f32_kernel<64> : shared_attn_f32_kernel<128>;
-  hipLaunchKernelGGL(kernel, dim3(H, B * n1), dim3(256), 0, s, q, blocks, sh, sm.slots, ck, cv, meta,
+  hipLaunchKernelGGL(kernel, dim3(H, B * n1), dim3(256), 0, s, (const float *)q, blocks, sh, sm.slots, ck, cv, meta,
                      (float *)out, n1, H, Hkv, capacity);
   return hipGetLastError();
 }

@@ -38,6 +38,8 @@ AS_DEVICE f16x8 bf16x8_to_f16x8(bf16x8 v) {
   for (int i = 0; i < 8; ++i) r[i] = (f16)(float)v[i];
   return r;
 }
+AS_DEVICE f16x8 load_f16x8(const f16 *p) { return *(const f16x8 *)p; }
+AS_DEVICE f16x8 load_f16x8(const bf16 *p) { return bf16x8_to_f16x8(*(const bf16x8 *)p); }
 
 // Order-preserving map of an fp32 value to uint32 (larger float -> larger key).
 AS_DEVICE uint32_t f32_key(float f) {
@@ -203,21 +205,33 @@ struct SharedArgs {
   const int32_t *of, *len;
   int P, cap;
 };
-// Sessions grouped by the shared prefix that they stand behind (one entry per session; groups
-// in the order of their prefixes, members in the order of their rows).
-struct SharedGroup {
+// Sessions grouped by the shared prefix that they stand behind (one entry per session; members in
+// the order of their rows).
+struct alignas(32) SharedGroup {
   int32_t prefix, first, members, slots;  // first: its members' place in `order`
-  long long units;                        // work units of the groups before it
+  int32_t units;                          // work units of the groups before it
 };
 struct SharedMeta {
   int32_t *slots;        // [B] slots of the session's shared prefix, 0 for a session without one
   int32_t *place;        // [B] place in `order` (-1: none), and
   int32_t *first;        // [B] its group's first place there
   int32_t *order;        // [B] sessions
-  long long *units;      // [B] by a group's first place: units of the groups before it
+  int32_t *units;        // [B] by a group's first place: units of the groups before it
   SharedGroup *groups;   // [B]
-  long long *total;      // [2] units of all groups; number of groups
+  int2 *total;           // units of all groups; number of groups
   uint32_t *bad;         // [B][kv heads][3] tree rows with values that are not finite
+};
+
+// The partial results over shared prefixes, and where the rows go once they are joined with those
+// of the own slots.
+struct SharedJoin {
+  const float *o, *ml;   // rows_total rows a kv head (shared.h)
+  SharedMeta sm;
+  int wgs;               // workgroups a kv head
+  long long rows_total;
+  void *out;             // fp16 in the activation layout, or with rows_out bf16, row-major
+  int rows_out;
+  int here;              // 1: the kernel over the own slots joins them, unless these are split
 };
 
 // Fixed-point scale for deterministic mass sums in the vocabulary kernel.
@@ -240,12 +254,11 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
 
 // The same for sessions behind shared prefixes (positions start behind them), and their groups;
 // a unit of work is a 64-slot record for tile_rows query rows.  tokens may be NULL (meta.tok is
-// then not written).  q [rows][width] bf16 or NULL: brought to fp16 at q16 on the way.
+// then not written).
 hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
                                    const int32_t *prefix_len, int B, int n1, int V, int capacity,
                                    const SharedArgs &sh, int G, int Hkv, int tile_rows, TreeMeta meta,
-                                   const SharedMeta &sm, int32_t *status, const bf16 *q, f16 *q16,
-                                   int width, hipStream_t s);
+                                   const SharedMeta &sm, int32_t *status, hipStream_t s);
 
 template <typename TW>
 hipError_t launch_embed(const TW *embed, const int32_t *tok, float *x, int rows, int d,
@@ -347,17 +360,21 @@ hipError_t launch_attention(const typename ActOf<TW>::type *q, const TW *cache_k
                             long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                             int capacity, int cus, hipStream_t s, int *nsplit_used);
 
-// The same over the own slots alone of sessions behind shared prefixes: always as partial sums,
-// of *nsplit parts a session.  Tree rows with values that are not finite are marked in bad (three
-// words a session and kv head, cleared by launch_tree_prep_shared) and these values left out.
-hipError_t launch_attention_part(const f16 *q, const bf16 *cache_k, const bf16 *cache_v,
-                                 const TreeMeta &meta, float *part_o, float *part_ml,
-                                 long long part_capacity, int B, int n1, int H, int Hkv, int hd,
-                                 int capacity, int cus, hipStream_t s, int *nsplit, uint32_t *bad);
+// The same over the own slots alone of sessions behind shared prefixes: joined with j's partial
+// results and written to j's out, if j.here and the sessions are not split (*nsplit 1), or else as
+// partial sums.
+// Values of tree rows that are not finite reach only rows that see them: where they are not joined
+// here they are left out, and their rows marked in j.sm.bad (three words a session and kv head,
+// cleared by launch_tree_prep_shared).  TQ: q's type, [rows][H hd].
+template <typename TQ>
+hipError_t launch_attention_own(const TQ *q, const bf16 *cache_k, const bf16 *cache_v,
+                                const TreeMeta &meta, const SharedJoin &j, float *part_o,
+                                float *part_ml, long long part_capacity, int B, int n1, int H,
+                                int Hkv, int hd, int capacity, int cus, hipStream_t s, int *nsplit);
 
 // One layer's tree attention behind shared prefixes: blocks [P][Hkv][cap / 64] records, own slots
-// ck, cv as in launch_attention.  q is row-major [rows][H hd] in the activation type; out is in
-// the activation layout, or row-major in TW with rows_out.  sh_o, sh_ml: partial results of the
+// ck, cv as in launch_attention.  q is row-major [rows][H hd] in the activation type, out in the
+// activation layout; or, with rows_io, both row-major in TW.  sh_o, sh_ml: partial results of the
 // shared slots, shared_part_rows(..) rows a kv head.
 constexpr int kSharedTile = 256;   // query rows of a workgroup over a shared prefix
 inline int shared_wgs(int Hkv, int cus) { return cus > Hkv ? cus / Hkv : 1; }  // a kv head
@@ -365,10 +382,10 @@ inline long long shared_part_rows(long long rows, int Hkv, int cus) {
   return rows + (long long)kSharedTile * shared_wgs(Hkv, cus);
 }
 template <typename TW>
-hipError_t launch_attention_shared(const typename ActOf<TW>::type *q,
-                                   const typename ActOf<TW>::type *blocks, const SharedArgs &sh,
-                                   const SharedMeta &sm, const TW *ck, const TW *cv,
-                                   const TreeMeta &meta, void *out, int rows_out, float *sh_o,
+hipError_t launch_attention_shared(const void *q, const typename ActOf<TW>::type *blocks,
+                                   const SharedArgs &sh, const SharedMeta &sm, const TW *ck,
+                                   const TW *cv, const TreeMeta &meta, void *out, int rows_io,
+                                   float *sh_o,
                                    float *sh_ml, float *part_o, float *part_ml,
                                    long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                                    int capacity, int cus, hipStream_t s);

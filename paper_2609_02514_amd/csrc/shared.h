@@ -1,0 +1,112 @@
+// How the work over shared prefixes is dealt out, and how its partial results are joined with those
+// of a session's own slots.
+#pragma once
+#include "common.h"
+
+// Units of work (a 64-slot record for a tile of kSharedTile rows) lie on a line: group after group,
+// tile after tile, record after record.  The n workgroups of a kv head take pieces of the line that
+// differ by a unit at most, so that all finish together whatever the lengths; a tile that is cut
+// leaves several partial results.
+struct SharedLine {
+  int n, each, more;   // workgroups; units of each, and one more for the first `more`
+  // at least `least` units a workgroup
+  AS_DEVICE SharedLine(int units, int wgs) {
+    constexpr int least = 4;
+    const int most = (units + least - 1) / least;
+    n = most < wgs ? most : wgs;
+    each = n > 0 ? units / n : 0;
+    more = units - n * each;
+  }
+  AS_DEVICE int begin(int w) const { return w * each + (w < more ? w : more); }
+  // the workgroup that takes unit u
+  AS_DEVICE int worker(int u) const {
+    const int front = more * (each + 1);
+    return u < front ? u / (each + 1) : more + (u - front) / each;
+  }
+};
+// Where the partial rows of (a group's first member, tile, workgroup) begin, of one kv head: rows
+// and workgroups both only grow along the line, so no two meet.
+AS_DEVICE long long shared_rows_at(int first, int QR, int tile, int w) {
+  return (long long)first * QR + (long long)(tile + w) * acespec::kSharedTile;
+}
+
+// The shared partial results of a row: `parts` of them, the first at ml (largest exponent, sum) and
+// o, the next ones a tile's rows on.
+struct SharedParts {
+  const float2 *ml;
+  const float *o;
+  int parts;
+};
+template <int HD>
+AS_DEVICE SharedParts shared_parts(const SharedJoin &j, int b, int g, int qi, int QR) {
+  SharedParts p{nullptr, nullptr, 0};
+  const int place = j.sm.place[b];
+  if (place < 0) return p;
+  const int first = j.sm.first[b], nblk = (j.sm.slots[b] + 63) >> 6;
+  const int local = (place - first) * QR + qi, tile = local / acespec::kSharedTile;
+  const int u0 = j.sm.units[first] + tile * nblk;
+  const SharedLine line(j.sm.total->x, j.wgs);
+  const int w0 = line.worker(u0);
+  const long long at = g * j.rows_total + shared_rows_at(first, QR, tile, w0) +
+                       (local - tile * acespec::kSharedTile);
+  p.parts = line.worker(u0 + nblk - 1) - w0 + 1;
+  p.ml = (const float2 *)j.ml + at;
+  p.o = j.o + at * HD;
+  return p;
+}
+
+// A row's own partial result (largest exponent M in base 2, sum l, outputs o of four head dims from
+// dim(i) on) joined with the shared ones, and written.  bad: tree rows with values that are not
+// finite, which were left out: whatever weight such a value has, an infinity or a NaN comes of it
+// in the rows that see its slot.  vb: the tree's values, [head dim][capacity].
+template <int HD, int N, typename F>
+AS_DEVICE void shared_finish(const SharedJoin &j, const TreeMeta &meta, const bf16 *vb, int capacity,
+                             const uint32_t *bad, int b, int g, int qi, int n1, int H, int Hkv,
+                             int rows, float M, float l, f32x4 (&o)[N], F dim) {
+  typedef bf16 b4 __attribute__((ext_vector_type(4)));
+  typedef f16 h4 __attribute__((ext_vector_type(4)));
+  const int G = H / Hkv, r = qi / G, h = g * G + qi - r * G;
+  const SharedParts p = shared_parts<HD>(j, b, g, qi, G * n1);
+  float top = M;
+#pragma unroll 4
+  for (int s = 0; s < p.parts; ++s) top = fmaxf(top, p.ml[(size_t)s * acespec::kSharedTile].x);
+  if (top == -INFINITY) top = 0.f;
+  const float w = __builtin_amdgcn_exp2f(M - top);
+  l *= w;
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] *= w;
+#pragma unroll 2
+  for (int s = 0; s < p.parts; ++s) {
+    const float2 e = p.ml[(size_t)s * acespec::kSharedTile];
+    const float x = __builtin_amdgcn_exp2f(e.x - top);
+    l += x * e.y;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] += x * *(const f32x4 *)(p.o + (size_t)s * acespec::kSharedTile * HD + dim(i));
+  }
+  if (bad[0] | bad[1] | bad[2]) {
+    __asm__ volatile("");   // (seldom: a branch)
+    const uint64_t anc = meta.anc[(size_t)b * n1 + r];
+    for (int t = 0; t < n1; ++t) {
+      if (!((bad[t >> 5] >> (t & 31)) & 1u) || (t > 0 && !((anc >> (t - 1)) & 1ull))) continue;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = (float)(f16)(float)vb[(size_t)(dim(i) + e) * capacity + t];
+          if (!(fabsf(v) <= 65504.f)) o[i][e] += v;
+        }
+    }
+  }
+  const float inv = 1.f / l;   // (a row sees itself)
+  const int row = b * n1 + r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const f32x4 y = o[i] * inv;
+    if (j.rows_out)
+      *(b4 *)((bf16 *)j.out + (size_t)row * H * HD + h * HD + dim(i)) =
+          b4{(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+    else
+      *(h4 *)((f16 *)j.out + act_off(row, h * HD + dim(i), rows, H * HD)) =
+          h4{(f16)y[0], (f16)y[1], (f16)y[2], (f16)y[3]};
+  }
+}

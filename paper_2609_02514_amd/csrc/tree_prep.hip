@@ -92,11 +92,46 @@ AS_DEVICE int shared_prefix(const SharedArgs &sh, int b, int *slots) {
   return n > 0 ? p : -1;
 }
 
-// The groups, by one workgroup: a session's place follows from counts over all the sessions (64
-// sessions: 64 reads from LDS a thread; B^2 / 128 of them at most).
+AS_DEVICE int group_units(int members, int QR, int tile_rows, int slots) {
+  return (members * QR + tile_rows - 1) / tile_rows * ((slots + 63) / 64);
+}
+
+// The groups of at most 64 sessions, a lane each of one wave: in the order of their first members.
+AS_DEVICE void group_few(int B, int QR, const SharedArgs &sh, int tile_rows, const SharedMeta &sm) {
+  const int b = threadIdx.x;
+  if (b >= 64) return;
+  int slots = 0, place = -1, first = 0, groups = 0, units = 0, grouped = 0;
+  const int p = b < B ? shared_prefix(sh, b, &slots) : -1;
+  for (uint64_t rest = __ballot(p >= 0); rest;) {
+    const int lead = __builtin_ctzll(rest);
+    const uint64_t with = __ballot(p == __builtin_amdgcn_readlane(p, lead));
+    const int members = __popcll(with), n = __builtin_amdgcn_readlane(slots, lead);
+    if ((with >> b) & 1) {
+      first = grouped;
+      place = grouped + __popcll(with & ((1ull << b) - 1));
+      if (b == lead) {
+        sm.units[grouped] = units;
+        sm.groups[groups] = SharedGroup{p, grouped, members, n, units};
+      }
+    }
+    ++groups;
+    grouped += members;
+    units += group_units(members, QR, tile_rows, n);
+    rest &= ~with;
+  }
+  if (b < B) {
+    sm.slots[b] = max(slots, 0);
+    sm.place[b] = place;
+    sm.first[b] = first;
+    if (place >= 0) sm.order[place] = b;
+  }
+  if (b == 0) *sm.total = make_int2(units, groups);
+}
+
+// The groups of any number of sessions, by one workgroup, in the order of their prefixes: a
+// session's place follows from counts over all the sessions (B^2 / 128 reads from LDS a thread).
 constexpr int GROUP_TILE = 1024;   // sessions in LDS at a time
-AS_DEVICE void group_sessions(int B, int QR, const SharedArgs &sh, int tile_rows,
-                              const SharedMeta &sm) {
+AS_DEVICE void group_many(int B, int QR, const SharedArgs &sh, int tile_rows, const SharedMeta &sm) {
   __shared__ int s_p[GROUP_TILE];
   const int tid = threadIdx.x;
   int grouped = 0;
@@ -111,6 +146,7 @@ AS_DEVICE void group_sessions(int B, int QR, const SharedArgs &sh, int tile_rows
       __syncthreads();
       for (int i = tid; i < n; i += TP_THREADS) s_p[i] = shared_prefix(sh, t0 + i, &unused);
       __syncthreads();
+#pragma unroll 8
       for (int i = 0; i < n; ++i) {
         const int o = s_p[i];
         grouped += o >= 0;
@@ -131,17 +167,15 @@ AS_DEVICE void group_sessions(int B, int QR, const SharedArgs &sh, int tile_rows
   __syncthreads();
   if (tid >= 64) return;
   // one wave closes the gaps, and sums the units
-  int count = 0;
-  long long units = 0;
+  int count = 0, units = 0;
   for (int x0 = 0; x0 < grouped; x0 += 64) {
     const int x = x0 + tid;
     SharedGroup g = x < grouped ? sm.groups[x] : SharedGroup{0, 0, 0, 0, 0};
     const bool lead = g.members > 0;
-    const long long mine =
-        lead ? ((long long)g.members * QR + tile_rows - 1) / tile_rows * ((g.slots + 63) / 64) : 0;
-    long long sum = mine;   // of this lane's and the ones' before
+    const int mine = lead ? group_units(g.members, QR, tile_rows, g.slots) : 0;
+    int sum = mine;   // of this lane's and the ones' before
     for (int o = 1; o < 64; o <<= 1) {
-      const long long v = __shfl_up(sum, o);
+      const int v = __shfl_up(sum, o);
       if (tid >= o) sum += v;
     }
     const uint64_t leads = __ballot(lead);
@@ -153,30 +187,27 @@ AS_DEVICE void group_sessions(int B, int QR, const SharedArgs &sh, int tile_rows
     count += __popcll(leads);
     units += __shfl(sum, 63);
   }
-  if (tid == 0) {
-    sm.total[0] = units;
-    sm.total[1] = count;
-  }
+  if (tid == 0) *sm.total = make_int2(units, count);
 }
 
-// Workgroups: the groups, then a session each, then 8 query elements a thread.
+// Workgroups: the groups, then a session each.
 __global__ __launch_bounds__(TP_THREADS) void tree_prep_shared_kernel(
     const int32_t *__restrict__ tokens, const int32_t *__restrict__ parents,
     const int32_t *__restrict__ prefix_len, int B, int n1, int V, int capacity, SharedArgs sh,
-    int QR, int Hkv, int tile_rows, TreeMeta meta, SharedMeta sm, int32_t *__restrict__ status,
-    const bf16 *__restrict__ q, f16 *__restrict__ q16, long long pieces) {
+    int QR, int Hkv, int tile_rows, TreeMeta meta, SharedMeta sm,
+    int32_t *__restrict__ status) {
   const int w = blockIdx.x;
   if (w == 0) {
-    group_sessions(B, QR, sh, tile_rows, sm);
-  } else if (w <= B) {
+    if (B <= 64)
+      group_few(B, QR, sh, tile_rows, sm);
+    else
+      group_many(B, QR, sh, tile_rows, sm);
+  } else {
     for (int i = threadIdx.x; i < 3 * Hkv; i += TP_THREADS) sm.bad[(size_t)(w - 1) * 3 * Hkv + i] = 0;
     int slots;
     shared_prefix(sh, w - 1, &slots);
     prepare_tree<false>(w - 1, tokens, parents, prefix_len, n1, V, capacity, 0, 0, slots, meta,
                         status);
-  } else {
-    const long long i = (long long)(w - 1 - B) * TP_THREADS + threadIdx.x;
-    if (i < pieces) ((f16x8 *)q16)[i] = bf16x8_to_f16x8(((const bf16x8 *)q)[i]);
   }
 }
 
@@ -206,15 +237,10 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
 hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
                                    const int32_t *prefix_len, int B, int n1, int V, int capacity,
                                    const SharedArgs &sh, int G, int Hkv, int tile_rows, TreeMeta meta,
-                                   const SharedMeta &sm, int32_t *status, const bf16 *q, f16 *q16,
-                                   int width, hipStream_t s) {
-  if (n1 > TP_THREADS || width % 8 != 0) return hipErrorInvalidValue;
-  const long long pieces = q ? (long long)B * n1 * (width / 8) : 0;
-  const long long wgs = 1 + B + (pieces + TP_THREADS - 1) / TP_THREADS;
-  if (wgs > 0x7fffffffLL / TP_THREADS) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(tree_prep_shared_kernel, dim3((unsigned)wgs), dim3(TP_THREADS), 0, s, tokens,
-                     parents, prefix_len, B, n1, V, capacity, sh, G * n1, Hkv, tile_rows, meta, sm,
-                     status, q, q16, pieces);
+                                   const SharedMeta &sm, int32_t *status, hipStream_t s) {
+  if (n1 > TP_THREADS) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(tree_prep_shared_kernel, dim3(1 + B), dim3(TP_THREADS), 0, s, tokens, parents,
+                     prefix_len, B, n1, V, capacity, sh, G * n1, Hkv, tile_rows, meta, sm, status);
   return hipGetLastError();
 }
 
