@@ -179,7 +179,7 @@ AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int tot
 }
 
 template <int HD, int NW, int UPW, int NST, bool PART = false, typename TQ = f16>
-__global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
+__global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
     const TQ *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
     float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int tpg,
@@ -187,7 +187,10 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
   constexpr int KSTEPS = HD / 32, NB = HD / 16;
   constexpr int STAGE = 2 * KC * HD;     // elements: K [KC][HD], then V^T [HD][KC]
   constexpr int L_DMA = HD / 4 / NW;     // DMA instructions per wave per chunk
-  static_assert(NST >= 3, "the widening runs one stage ahead of the MFMAs");
+  // Two stages: a chunk is widened once it is there, between two barriers, with the next one in
+  // flight; the shorter ring leaves room for a second workgroup on the CU, whose loads and products
+  // fill these gaps.  Otherwise the widening runs one stage ahead of the MFMAs.
+  constexpr bool SYNC = NST == 2;
   __shared__ __attribute__((aligned(1024))) uint16_t smem[NST * STAGE];
 
   const int g = blockIdx.y, b = blockIdx.z;
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
 #pragma unroll
   for (int i = 0; i < NST - 1; ++i)
     if (c0 + i < c1) issue_chunk<HD, NW>(stage_of(c0 + i), kr, vr, (c0 + i) * KC, capacity, wave, lane);
-  if (c0 < c1) {
+  if (!SYNC && c0 < c1) {
     if (c0 + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
     lds_barrier();
     if (widener) widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad);
@@ -287,14 +290,23 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_mfma_kernel(
   const int qvoff = (qk & 2 ? voff[1] : voff[0]) + (qk & 1) * 4;  // and its V^T half-piece
 
   for (int c = c0; c < c1; ++c) {
-    if (c + 1 < c1) {
-      if (c + NST - 2 < c1) wait_vmcnt<(NST - 3) * L_DMA>(); else wait_vmcnt<0>();
+    if constexpr (SYNC) {
+      wait_vmcnt<0>();
+      chunk_barrier();
+      if (c + 1 < c1)
+        issue_chunk<HD, NW>(stage_of(c + 1), kr, vr, (c + 1) * KC, capacity, wave, lane);
+      widen_chunk<HD, PART>(stage_of(c), tid, NW * 64, c * KC, total, S, bad);
+      chunk_barrier();
+    } else {
+      if (c + 1 < c1) {
+        if (c + NST - 2 < c1) wait_vmcnt<(NST > 3 ? NST - 3 : 0) * L_DMA>(); else wait_vmcnt<0>();
+      }
+      chunk_barrier();
+      if (c + NST - 1 < c1)
+        issue_chunk<HD, NW>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity, wave, lane);
+      if (c + 1 < c1 && widener)
+        widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad);
     }
-    chunk_barrier();
-    if (c + NST - 1 < c1)
-      issue_chunk<HD, NW>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity, wave, lane);
-    if (c + 1 < c1 && widener)
-      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad);
 
     const uint16_t *st = stage_of(c);
     const f16 *sk = (const f16 *)st;
@@ -1065,11 +1077,11 @@ __global__ __launch_bounds__(256) void tree_attn_f32_kernel(
 // Ring depth: 4 stages of 32 KB (head_dim 128) or 16 KB (head_dim 64).
 template <int HD> struct AttnCfg { static constexpr int NST = 4; };
 
-template <int HD, int NW, int UPW, bool PART, typename TQ>
+template <int HD, int NW, int UPW, int NST, bool PART, typename TQ>
 void launch_mfma(dim3 grid, hipStream_t s, const TQ *q, const bf16 *ck, const bf16 *cv,
                  const TreeMeta &meta, f16 *out, float *po, float *pml, int n1, int H, int Hkv,
                  int capacity, int nsplit, int tpg, const SharedJoin &join) {
-  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, AttnCfg<HD>::NST, PART, TQ>), grid,
+  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, NST, PART, TQ>), grid,
                      dim3(NW * 64), 0, s, q, ck, cv, meta, out, po, pml, n1, H, Hkv,
                      capacity, nsplit, tpg, join);
 }
@@ -1119,12 +1131,19 @@ hipError_t launch_tree_attn(const TQ *q, const bf16 *ck, const bf16 *cv, const T
       hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, PART, TQ>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
                          rpg, join);
+  } else if (PART && all_tiles <= 8) {
+    if (hd == 128)
+      launch_mfma<128, 8, 1, 2, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+                                          capacity, nsplit, all_tiles, join);
+    else
+      launch_mfma<64, 8, 1, 4, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+                                         capacity, nsplit, all_tiles, join);
   } else if (hd == 128) {
-    launch_mfma<128, 16, 1, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                            capacity, nsplit, all_tiles, join);
+    launch_mfma<128, 16, 1, 4, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+                                         capacity, nsplit, all_tiles, join);
   } else {
-    launch_mfma<64, 16, 1, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                           capacity, nsplit, all_tiles, join);
+    launch_mfma<64, 16, 1, 4, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+                                        capacity, nsplit, all_tiles, join);
   }
   return hipGetLastError();
 }

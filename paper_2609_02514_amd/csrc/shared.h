@@ -75,26 +75,33 @@ AS_DEVICE void shared_finish(const SharedJoin &j, const TreeMeta &meta, const bf
   l *= w;
 #pragma unroll
   for (int i = 0; i < N; ++i) o[i] *= w;
-#pragma unroll 2
+#pragma unroll 1
   for (int s = 0; s < p.parts; ++s) {
     const float2 e = p.ml[(size_t)s * acespec::kSharedTile];
     const float x = __builtin_amdgcn_exp2f(e.x - top);
     l += x * e.y;
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[i] += x * *(const f32x4 *)(p.o + (size_t)s * acespec::kSharedTile * HD + dim(i));
+    for (int i = 0; i < N; ++i) {
+      o[i] += x * *(const f32x4 *)(p.o + (size_t)s * acespec::kSharedTile * HD + dim(i));
+      if (i % 8 == 7) SCHED_FENCE();   // (no more loads at a time than there are registers)
+    }
   }
   if (bad[0] | bad[1] | bad[2]) {
     __asm__ volatile("");   // (seldom: a branch)
     const uint64_t anc = meta.anc[(size_t)b * n1 + r];
-    for (int t = 0; t < n1; ++t) {
-      if (!((bad[t >> 5] >> (t & 31)) & 1u) || (t > 0 && !((anc >> (t - 1)) & 1ull))) continue;
 #pragma unroll
-      for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
+#pragma unroll 1
+      for (int t = 0; t < n1; ++t) {
+        if (!((bad[t >> 5] >> (t & 31)) & 1u) || (t > 0 && !((anc >> (t - 1)) & 1ull))) continue;
+        const bf16 *v = vb + (size_t)dim(i) * capacity + t;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float v = (float)(f16)(float)vb[(size_t)(dim(i) + e) * capacity + t];
-          if (!(fabsf(v) <= 65504.f)) o[i][e] += v;
+          const float x = (float)(f16)(float)v[(size_t)e * capacity];
+          if (!(fabsf(x) <= 65504.f)) o[i][e] += x;
         }
+      }
+      SCHED_FENCE();   // (few registers: the loops' addresses are not kept side by side)
     }
   }
   const float inv = 1.f / l;   // (a row sees itself)
