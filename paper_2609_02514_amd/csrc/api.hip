@@ -441,9 +441,8 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
        *p_cand = nullptr, *p_rflag = nullptr;
   void *p_tok = nullptr, *p_par = nullptr, *p_pos = nullptr, *p_depth = nullptr,
        *p_anc = nullptr, *p_S = nullptr;
-  void *p_so = nullptr, *p_sml = nullptr, *p_slots = nullptr, *p_place = nullptr,
-       *p_first = nullptr, *p_order = nullptr, *p_units = nullptr, *p_groups = nullptr,
-       *p_total = nullptr, *p_bad = nullptr;
+  void *p_so = nullptr, *p_sml = nullptr, *p_sess = nullptr, *p_order = nullptr,
+       *p_groups = nullptr, *p_total = nullptr, *p_bad = nullptr;
   std::vector<Part> parts = {
       {R * d.d_model * 4, &p_x},
       {R * d.d_model * c->esz, &c->a},
@@ -464,8 +463,8 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
       {R * 4, &p_tok}, {R * 4, &p_par}, {R * 4, &p_pos}, {R * 4, &p_depth}, {R * 8, &p_anc},
       {(size_t)max_batch * 4, &p_S},
       {shr * d.head_dim * 4, &p_so}, {shr * 2 * 4, &p_sml},
-      {each * 4, &p_slots}, {each * 4, &p_place}, {each * 4, &p_first}, {each * 4, &p_order},
-      {each * 4, &p_units}, {each * sizeof(SharedGroup), &p_groups}, {layers ? 8u : 0u, &p_total},
+      {each * sizeof(SharedSession), &p_sess}, {each * 4, &p_order}, {each * sizeof(SharedGroup), &p_groups},
+      {layers ? 16u : 0u, &p_total},
       {layers ? each * d.n_kv_heads * 12 : 0, &p_bad}};
   size_t total = 0;
   for (auto &pt : parts) total += align_up(pt.bytes);
@@ -499,9 +498,8 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   c->meta.sess_S = (int32_t *)p_S;
   c->sh_o = (float *)p_so;
   c->sh_ml = (float *)p_sml;
-  c->shm = SharedMeta{(int32_t *)p_slots, (int32_t *)p_place, (int32_t *)p_first,
-                      (int32_t *)p_order, (int32_t *)p_units, (SharedGroup *)p_groups,
-                      (int2 *)p_total, (uint32_t *)p_bad};
+  c->shm = SharedMeta{(SharedSession *)p_sess, (int32_t *)p_order, (SharedGroup *)p_groups,
+                      (int4 *)p_total, (uint32_t *)p_bad};
   if (layers) {
     std::vector<double> f(d.head_dim / 2);
     for (int i = 0; i < d.head_dim / 2; ++i)

@@ -221,6 +221,12 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   const int c1 = min(nchunks, c0 + cps);
   __shared__ uint32_t bad[PART ? 3 : 1];   // tree rows with values that are not finite
   if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
+  SharedSession me{};          // (asked for here, well before the join needs it)
+  int4 total_units{};
+  if (PART && join.here) {
+    me = join.sm.sessions[b];
+    total_units = *join.sm.total;
+  }
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -511,7 +517,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
     if (qi >= QR) continue;
     const int r = qi / G, h = g * G + (qi - r * G);
     if (PART && join.here) {
-      shared_finish<HD>(join, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
+      shared_finish<HD>(join, me, total_units, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
                         m_run[t] == -INFINITY ? -INFINITY : m_run[t] * sscale, l, o[t],
                         [&](int nb) { return nb * 16 + lg * 4; });
     } else if (!PART && nsplit == 1) {
@@ -613,6 +619,12 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   const int c1 = min(nchunks, c0 + cps);
   __shared__ uint32_t bad[PART ? 3 : 1];   // tree rows with values that are not finite
   if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
+  SharedSession me{};          // (asked for here, well before the join needs it)
+  int4 total_units{};
+  if (PART && join.here) {
+    me = join.sm.sessions[b];
+    total_units = *join.sm.total;
+  }
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -894,7 +906,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
           }
         }
         if (PART && join.here)
-          shared_finish<HD>(join, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all, M, L, all,
+          shared_finish<HD>(join, me, total_units, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all, M, L, all,
                             [&](int i) { return (qk * (NB16 / 4) + i) * 16 + lg * 4; });
         if ((PART ? !join.here : nsplit > 1) && qk == 0 && lg == 0) {
           part_ml[(item * QR + qi) * 2 + 0] = M;
@@ -916,7 +928,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
         for (int i = 0; i < 4 * NDB; ++i)
           all[i] = f32x4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2],
                          o[i >> 2][4 * (i & 3) + 3]};
-        shared_finish<HD>(join, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
+        shared_finish<HD>(join, me, total_units, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
                           m_run == -INFINITY ? -INFINITY : m_run * sscale, l, all,
                           [&](int i) { return 8 * i + 4 * hh; });
       } else if (!PART && nsplit == 1) {

@@ -66,23 +66,38 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
   // (the groups are asked for, 64 at a time, before it is known how many there are)
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), lq = lane & 31, hh = lane >> 5;
   SharedGroup mine = sm.groups[min(lane, B - 1)];
-  const int2 total = *sm.total;
-  const int groups = uniform(total.y);
-  const SharedLine line(uniform(total.x), wgs);
+  int4 total = *sm.total;
+  total = make_int4(uniform(total.x), uniform(total.y), uniform(total.z), uniform(total.w));
+  const int groups = total.y;
+  const SharedLine line(total, wgs);
   if (w >= line.n) return;
   int u = line.begin(w), at = 0;   // `mine` is group at + lane
-  const int uend = line.begin(w + 1);
+  int uend = line.begin(w + 1);
   const int G = H / Hkv, QR = G * n1;
   const float sscale = LOG2E / sqrtf((float)HD);
-
-  while (u < uend) {
-    int before;   // groups of the 64 that begin at u or before
-    while ((before = __popcll(__ballot(at + lane < groups && mine.units <= u))) == 64 && at + 64 < groups &&
-           uniform(sm.groups[at + 64].units) <= u) {
+  // the group of unit x, or of tile x
+  auto group_of = [&](int x, bool tiles) {
+    auto begins = [&](const SharedGroup &s) { return tiles ? s.tiles : s.units; };
+    int before;   // groups of the 64 that begin at x or before
+    while ((before = __popcll(__ballot(at + lane < groups && begins(mine) <= x))) == 64 && at + 64 < groups &&
+           uniform(begins(sm.groups[at + 64])) <= x) {
       at += 64;
       mine = sm.groups[min(at + lane, B - 1)];
     }
-    const int gi = before - 1;
+    return before - 1;
+  };
+  if (line.pieces) {   // a piece of one tile
+    const int tile = w / line.pieces, gi = group_of(tile, true);
+    const int nblk = (__builtin_amdgcn_readlane(mine.slots, gi) + 63) >> 6, piece = line.piece(nblk);
+    const int u0 = __builtin_amdgcn_readlane(mine.units, gi) +
+                   (tile - __builtin_amdgcn_readlane(mine.tiles, gi)) * nblk;
+    const int c = (w - tile * line.pieces) * piece;
+    u = u0 + min(c, nblk);
+    uend = u0 + min(c + piece, nblk);
+  }
+
+  while (u < uend) {
+    const int gi = group_of(u, false);
     const int first = __builtin_amdgcn_readlane(mine.first, gi), slots = __builtin_amdgcn_readlane(mine.slots, gi);
     const int prefix = __builtin_amdgcn_readlane(mine.prefix, gi);
     const int rows = __builtin_amdgcn_readlane(mine.members, gi) * QR, nblk = (slots + 63) >> 6;
@@ -317,6 +332,8 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
   if (row >= rows) return;
   const int b = row / n1, r = row - b * n1, G = H / Hkv, g = h / G, QR = G * n1;
   const int qi = r * G + h - g * G;
+  const SharedSession me = j.sm.sessions[b];
+  const int4 total = *j.sm.total;
   const size_t item0 = ((size_t)b * Hkv + g) * nsplit * QR + qi;
   const float2 *ml = (const float2 *)part_ml + item0;
   const float *po = part_o + item0 * HD + d;
@@ -334,7 +351,7 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
     o[0] += x * *(const f32x4 *)(po + (size_t)s * QR * HD);
   }
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity + meta.sess_S[b];
-  shared_finish<HD>(j, meta, vb, capacity, j.sm.bad + ((size_t)b * Hkv + g) * 3, b, g, qi, n1, H, Hkv,
+  shared_finish<HD>(j, me, total, meta, vb, capacity, j.sm.bad + ((size_t)b * Hkv + g) * 3, b, g, qi, n1, H, Hkv,
                     rows, M, l, o, [&](int) { return d; });
 }
 
@@ -344,7 +361,7 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
 template <int HD>
 __global__ __launch_bounds__(256) void shared_attn_f32_kernel(
     const float *__restrict__ qin, const float *__restrict__ blocks, SharedArgs sh,
-    const int32_t *__restrict__ session_slots, const float *__restrict__ ck,
+    const SharedSession *__restrict__ sessions, const float *__restrict__ ck,
     const float *__restrict__ cv, TreeMeta meta, float *__restrict__ out, int n1, int H, int Hkv,
     int capacity) {
   constexpr int LPS = HD / 4, SPW = 64 / LPS;   // lanes a slot, slots a wave and load
@@ -356,7 +373,7 @@ __global__ __launch_bounds__(256) void shared_attn_f32_kernel(
   const int h = blockIdx.x, row = blockIdx.y;
   const int b = row / n1;
   const int G = H / Hkv, g = h / G, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int S = meta.sess_S[b], own = S + n1, front = session_slots[b];
+  const int S = meta.sess_S[b], own = S + n1, front = sessions[b].slots;
   const uint64_t anc = meta.anc[row];
   const int prefix = front > 0 ? sh.of[b] : 0;
   const float *rec = blocks + ((size_t)prefix * Hkv + g) * (sh.cap >> 6) * REC;
@@ -491,7 +508,7 @@ hipError_t launch_attention_shared<float>(const void *q, const float *blocks, co
                                           float *, float *, long long, int B, int n1, int H,
                                           int Hkv, int hd, int capacity, int, hipStream_t s) {
   auto kernel = hd == 64 ? shared_attn_f32_kernel<64> : shared_attn_f32_kernel<128>;
-  hipLaunchKernelGGL(kernel, dim3(H, B * n1), dim3(256), 0, s, (const float *)q, blocks, sh, sm.slots, ck, cv, meta,
+  hipLaunchKernelGGL(kernel, dim3(H, B * n1), dim3(256), 0, s, (const float *)q, blocks, sh, sm.sessions, ck, cv, meta,
                      (float *)out, n1, H, Hkv, capacity);
   return hipGetLastError();
 }

@@ -209,17 +209,20 @@ struct SharedArgs {
 // the order of their rows).
 struct alignas(32) SharedGroup {
   int32_t prefix, first, members, slots;  // first: its members' place in `order`
-  int32_t units;                          // work units of the groups before it
+  int32_t units, tiles;                   // work units and query tiles of the groups before it
+};
+// What a session's rows need to find their partial results.
+struct alignas(32) SharedSession {
+  int32_t slots;          // of its shared prefix, 0 for a session without one
+  int32_t place, first;   // in `order` (-1: none), and its group's first place there
+  int32_t units, tiles;   // of the groups before its own
 };
 struct SharedMeta {
-  int32_t *slots;        // [B] slots of the session's shared prefix, 0 for a session without one
-  int32_t *place;        // [B] place in `order` (-1: none), and
-  int32_t *first;        // [B] its group's first place there
-  int32_t *order;        // [B] sessions
-  int32_t *units;        // [B] by a group's first place: units of the groups before it
-  SharedGroup *groups;   // [B]
-  int2 *total;           // units of all groups; number of groups
-  uint32_t *bad;         // [B][kv heads][3] tree rows with values that are not finite
+  SharedSession *sessions;  // [B]
+  int32_t *order;           // [B]
+  SharedGroup *groups;      // [B]
+  int4 *total;              // of all groups: units, number of groups, tiles, most records of one
+  uint32_t *bad;            // [B][kv heads][3] tree rows with values that are not finite
 };
 
 // The partial results over shared prefixes, and where the rows go once they are joined with those

@@ -4,21 +4,44 @@
 #include "common.h"
 
 // Units of work (a 64-slot record for a tile of kSharedTile rows) lie on a line: group after group,
-// tile after tile, record after record.  The n workgroups of a kv head take pieces of the line that
-// differ by a unit at most, so that all finish together whatever the lengths; a tile that is cut
-// leaves several partial results.
+// tile after tile, record after record, and the workgroups of a kv head take it in pieces, of which
+// each leaves a partial result a tile.  The line is cut in one of two ways:
+//  * evenly, so that all workgroups finish together whatever the lengths; a piece may then reach
+//    over tiles, and each of them costs its queries' way in and its results' way out;
+//  * every tile into the same number of pieces, which is taken where the longest of these is
+//    shorter than an even piece and the price of a second tile in it (six records: eight sessions of
+//    17 rows behind 2000 slots, three tiles, 44 us evenly cut and 37 tile by tile).
+// A piece has two records at least.
 struct SharedLine {
-  int n, each, more;   // workgroups; units of each, and one more for the first `more`
-  // at least `least` units a workgroup
-  AS_DEVICE SharedLine(int units, int wgs) {
-    constexpr int least = 4;
-    const int most = (units + least - 1) / least;
-    n = most < wgs ? most : wgs;
+  int n, each, more;   // workgroups; evenly: records of each, and one more for the first `more`
+  int pieces;          // of a tile, or 0: evenly
+  // total: units, -, tiles, most records of a tile
+  AS_DEVICE SharedLine(int4 total, int wgs) {
+    const int units = total.x, tiles = total.z;
+    n = min(max((units + 1) / 2, tiles), wgs);
     each = n > 0 ? units / n : 0;
     more = units - n * each;
+    pieces = tiles > 0 && tiles <= wgs ? min(wgs / tiles, (total.w + 1) / 2) : 0;
+    if (pieces && (total.w + pieces - 1) / pieces <= each + 6)
+      n = tiles * pieces;
+    else
+      pieces = 0;
   }
   AS_DEVICE int begin(int w) const { return w * each + (w < more ? w : more); }
-  // the workgroup that takes unit u
+  // records of a piece of a tile of nblk
+  AS_DEVICE int piece(int nblk) const { return (nblk + pieces - 1) / pieces; }
+  // The workgroups of a tile (the tiles-th, from unit u0 on): the first, and how many.
+  AS_DEVICE void workers(int tiles, int u0, int nblk, int *first, int *count) const {
+    if (pieces) {
+      *first = tiles * pieces;
+      *count = (nblk + piece(nblk) - 1) / piece(nblk);
+    } else {
+      *first = worker(u0);
+      *count = worker(u0 + nblk - 1) - *first + 1;
+    }
+  }
+
+ private:
   AS_DEVICE int worker(int u) const {
     const int front = more * (each + 1);
     return u < front ? u / (each + 1) : more + (u - front) / each;
@@ -38,35 +61,34 @@ struct SharedParts {
   int parts;
 };
 template <int HD>
-AS_DEVICE SharedParts shared_parts(const SharedJoin &j, int b, int g, int qi, int QR) {
+AS_DEVICE SharedParts shared_parts(const SharedJoin &j, const SharedSession &me, int4 total, int g,
+                                   int qi, int QR) {
   SharedParts p{nullptr, nullptr, 0};
-  const int place = j.sm.place[b];
-  if (place < 0) return p;
-  const int first = j.sm.first[b], nblk = (j.sm.slots[b] + 63) >> 6;
-  const int local = (place - first) * QR + qi, tile = local / acespec::kSharedTile;
-  const int u0 = j.sm.units[first] + tile * nblk;
-  const SharedLine line(j.sm.total->x, j.wgs);
-  const int w0 = line.worker(u0);
-  const long long at = g * j.rows_total + shared_rows_at(first, QR, tile, w0) +
+  if (me.place < 0) return p;
+  const int nblk = (me.slots + 63) >> 6;
+  const int local = (me.place - me.first) * QR + qi, tile = local / acespec::kSharedTile;
+  const SharedLine line(total, j.wgs);
+  int w0;
+  line.workers(me.tiles + tile, me.units + tile * nblk, nblk, &w0, &p.parts);
+  const long long at = g * j.rows_total + shared_rows_at(me.first, QR, tile, w0) +
                        (local - tile * acespec::kSharedTile);
-  p.parts = line.worker(u0 + nblk - 1) - w0 + 1;
   p.ml = (const float2 *)j.ml + at;
   p.o = j.o + at * HD;
   return p;
 }
 
 // A row's own partial result (largest exponent M in base 2, sum l, outputs o of four head dims from
-// dim(i) on) joined with the shared ones, and written.  bad: tree rows with values that are not
+// dim(i) on) joined with the shared ones, and written.  me, total: j.sm's, asked for in time.  bad: tree rows with values that are not
 // finite, which were left out: whatever weight such a value has, an infinity or a NaN comes of it
 // in the rows that see its slot.  vb: the tree's values, [head dim][capacity].
 template <int HD, int N, typename F>
-AS_DEVICE void shared_finish(const SharedJoin &j, const TreeMeta &meta, const bf16 *vb, int capacity,
+AS_DEVICE void shared_finish(const SharedJoin &j, const SharedSession &me, int4 total, const TreeMeta &meta, const bf16 *vb, int capacity,
                              const uint32_t *bad, int b, int g, int qi, int n1, int H, int Hkv,
                              int rows, float M, float l, f32x4 (&o)[N], F dim) {
   typedef bf16 b4 __attribute__((ext_vector_type(4)));
   typedef f16 h4 __attribute__((ext_vector_type(4)));
   const int G = H / Hkv, r = qi / G, h = g * G + qi - r * G;
-  const SharedParts p = shared_parts<HD>(j, b, g, qi, G * n1);
+  const SharedParts p = shared_parts<HD>(j, me, total, g, qi, G * n1);
   float top = M;
 #pragma unroll 4
   for (int s = 0; s < p.parts; ++s) top = fmaxf(top, p.ml[(size_t)s * acespec::kSharedTile].x);
@@ -75,7 +97,8 @@ AS_DEVICE void shared_finish(const SharedJoin &j, const TreeMeta &meta, const bf
   l *= w;
 #pragma unroll
   for (int i = 0; i < N; ++i) o[i] *= w;
-#pragma unroll 1
+  constexpr int UNROLL = N == 1 ? 8 : 1;
+#pragma unroll UNROLL
   for (int s = 0; s < p.parts; ++s) {
     const float2 e = p.ml[(size_t)s * acespec::kSharedTile];
     const float x = __builtin_amdgcn_exp2f(e.x - top);

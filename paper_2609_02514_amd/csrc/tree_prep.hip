@@ -92,40 +92,37 @@ AS_DEVICE int shared_prefix(const SharedArgs &sh, int b, int *slots) {
   return n > 0 ? p : -1;
 }
 
-AS_DEVICE int group_units(int members, int QR, int tile_rows, int slots) {
-  return (members * QR + tile_rows - 1) / tile_rows * ((slots + 63) / 64);
+AS_DEVICE int group_tiles(int members, int QR, int tile_rows) {
+  return (members * QR + tile_rows - 1) / tile_rows;
 }
 
 // The groups of at most 64 sessions, a lane each of one wave: in the order of their first members.
 AS_DEVICE void group_few(int B, int QR, const SharedArgs &sh, int tile_rows, const SharedMeta &sm) {
   const int b = threadIdx.x;
   if (b >= 64) return;
-  int slots = 0, place = -1, first = 0, groups = 0, units = 0, grouped = 0;
+  int slots = 0, groups = 0, units = 0, tiles = 0, most = 0, grouped = 0;
   const int p = b < B ? shared_prefix(sh, b, &slots) : -1;
+  SharedSession mine{max(slots, 0), -1, 0, 0, 0};
   for (uint64_t rest = __ballot(p >= 0); rest;) {
     const int lead = __builtin_ctzll(rest);
     const uint64_t with = __ballot(p == __builtin_amdgcn_readlane(p, lead));
     const int members = __popcll(with), n = __builtin_amdgcn_readlane(slots, lead);
     if ((with >> b) & 1) {
-      first = grouped;
-      place = grouped + __popcll(with & ((1ull << b) - 1));
-      if (b == lead) {
-        sm.units[grouped] = units;
-        sm.groups[groups] = SharedGroup{p, grouped, members, n, units};
-      }
+      mine = SharedSession{slots, grouped + (int)__popcll(with & ((1ull << b) - 1)), grouped, units, tiles};
+      if (b == lead) sm.groups[groups] = SharedGroup{p, grouped, members, n, units, tiles};
     }
     ++groups;
     grouped += members;
-    units += group_units(members, QR, tile_rows, n);
+    units += group_tiles(members, QR, tile_rows) * ((n + 63) / 64);
+    tiles += group_tiles(members, QR, tile_rows);
+    most = max(most, (n + 63) / 64);
     rest &= ~with;
   }
   if (b < B) {
-    sm.slots[b] = max(slots, 0);
-    sm.place[b] = place;
-    sm.first[b] = first;
-    if (place >= 0) sm.order[place] = b;
+    sm.sessions[b] = mine;
+    if (mine.place >= 0) sm.order[mine.place] = b;
   }
-  if (b == 0) *sm.total = make_int2(units, groups);
+  if (b == 0) *sm.total = make_int4(units, groups, tiles, most);
 }
 
 // The groups of any number of sessions, by one workgroup, in the order of their prefixes: a
@@ -156,38 +153,54 @@ AS_DEVICE void group_many(int B, int QR, const SharedArgs &sh, int tile_rows, co
       }
     }
     if (b >= B) continue;
-    sm.slots[b] = max(slots, 0);
-    sm.place[b] = p < 0 ? -1 : before + rank;
-    sm.first[b] = before;
+    sm.sessions[b] = SharedSession{max(slots, 0), p < 0 ? -1 : before + rank, before, 0, 0};
     if (p < 0) continue;
     sm.order[before + rank] = b;
     // a group's entry waits at its first place until the ones before it are known
-    sm.groups[before + rank] = SharedGroup{p, before, rank == 0 ? members : 0, slots, 0};
+    sm.groups[before + rank] = SharedGroup{p, before, rank == 0 ? members : 0, slots, 0, 0};
   }
   __syncthreads();
-  if (tid >= 64) return;
   // one wave closes the gaps, and sums the units
-  int count = 0, units = 0;
-  for (int x0 = 0; x0 < grouped; x0 += 64) {
-    const int x = x0 + tid;
-    SharedGroup g = x < grouped ? sm.groups[x] : SharedGroup{0, 0, 0, 0, 0};
-    const bool lead = g.members > 0;
-    const int mine = lead ? group_units(g.members, QR, tile_rows, g.slots) : 0;
-    int sum = mine;   // of this lane's and the ones' before
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(sum, o);
-      if (tid >= o) sum += v;
+  if (tid < 64) {
+    int count = 0, units = 0, tiles = 0, most = 0;
+    for (int x0 = 0; x0 < grouped; x0 += 64) {
+      const int x = x0 + tid;
+      SharedGroup g = x < grouped ? sm.groups[x] : SharedGroup{0, 0, 0, 0, 0, 0};
+      const bool lead = g.members > 0;
+      const int t = lead ? group_tiles(g.members, QR, tile_rows) : 0, mine = t * ((g.slots + 63) / 64);
+      int sum = mine, sum_t = t;   // of this lane's and the ones' before
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(sum, o), vt = __shfl_up(sum_t, o);
+        if (tid >= o) {
+          sum += v;
+          sum_t += vt;
+        }
+      }
+      const uint64_t leads = __ballot(lead);
+      g.units = units + sum - mine;
+      g.tiles = tiles + sum_t - t;
+      if (lead) {
+        most = max(most, (g.slots + 63) / 64);
+        sm.groups[count + __popcll(leads & ((1ull << tid) - 1))] = g;   // (at most x: read already)
+      }
+      count += __popcll(leads);
+      units += __shfl(sum, 63);
+      tiles += __shfl(sum_t, 63);
     }
-    const uint64_t leads = __ballot(lead);
-    g.units = units + sum - mine;
-    if (lead) {
-      sm.units[x] = g.units;
-      sm.groups[count + __popcll(leads & ((1ull << tid) - 1))] = g;   // (at most x: read already)
+    for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
+    if (tid == 0) *sm.total = make_int4(units, count, tiles, most);
+    // and its members learn what lies before their group
+    for (int x = tid; x < grouped; x += 64) {
+      int lo = 0, hi = count - 1;   // the last group that begins at place x or before
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (sm.groups[mid].first <= x) lo = mid; else hi = mid - 1;
+      }
+      SharedSession &m = sm.sessions[sm.order[x]];
+      m.units = sm.groups[lo].units;
+      m.tiles = sm.groups[lo].tiles;
     }
-    count += __popcll(leads);
-    units += __shfl(sum, 63);
   }
-  if (tid == 0) *sm.total = make_int2(units, count);
 }
 
 // Workgroups: the groups, then a session each.
