@@ -476,6 +476,18 @@ class SharedPrefix:
         return self._struct
 
 
+def _stream_of(index: int) -> int:
+    """The current stream's handle on that GPU (the Stream object around it costs 2.5 us more)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _fits(t, shape, dt, index) -> bool:
+    """What _check_tensors asks of one tensor."""
+    return (t is not None and t.shape == shape and t.dtype is dt and t.get_device() == index and
+            t.is_contiguous())
+
+
 def _check_tensors(want, index):
     """Tensors whose shape, type or stride differ from what the call says would be read out of
     range.  index: the GPU's."""
@@ -506,6 +518,7 @@ class Verifier:
         self.V = V
         self.ctx = acespec_create(self.desc, max_batch, max_nodes)
         self.index = torch.cuda.current_device()
+        self._kv = (L, Hkv, hd, torch.bfloat16 if dtype == "bf16" else torch.float32, torch.int32)
         self._keep: List = []
 
     @classmethod
@@ -733,14 +746,10 @@ class Verifier:
         """The current GPU, which must be the context's."""
         import torch
         here = torch.cuda.current_device()
-        if self.index not in (None, here):
+        if self.index is not None and self.index != here:
             raise ValueError(f"the context is on cuda:{self.index}, the current device and stream are "
                              f"cuda:{here}'s")
         return here
-
-    def _types(self):
-        import torch
-        return torch.bfloat16 if self.desc.dtype == ACESPEC_BF16 else torch.float32, torch.int32
 
     def _check_store(self, shared: SharedPrefix, index: int):
         d = self.desc
@@ -756,45 +765,52 @@ class Verifier:
             raise ValueError("shared prefixes and prefix_of come together")
         if shared is not None:
             self._check_store(shared, index)
-            _check_tensors((("prefix_of", prefix_of, (B,), self._types()[1]),), index)
+            i32 = self._kv[4]
+            if not _fits(prefix_of, (B,), i32, index):
+                _check_tensors((("prefix_of", prefix_of, (B,), i32),), index)
 
-    def _check_cache(self, kv_k, kv_v, capacity: int, lengths, index: int, name: str = "") -> KVCache:
-        """The tensors of a cache in the model's type, of len(lengths) sessions."""
-        d, (dt, i32) = self.desc, self._types()
-        shape = (d.n_layers, lengths.shape[0], d.n_kv_heads)
-        _check_tensors(((name + "kv_k", kv_k, (*shape, capacity, d.head_dim), dt),
-                        (name + "kv_v", kv_v, (*shape, d.head_dim, capacity), dt),
-                        (name + "prefix_len", lengths, (shape[1],), i32)), index)
-        return KVCache(_ptr(kv_k), _ptr(kv_v), capacity, _ptr(lengths))
+    def _check_cache(self, kv_k, kv_v, capacity: int, lengths, index: int, B: Optional[int] = None,
+                     name: str = "") -> KVCache:
+        """The tensors of a cache in the model's type, of B (None: len(lengths)) sessions."""
+        B = lengths.shape[0] if B is None else B
+        L, Hkv, hd, dt, i32 = self._kv
+        k, v = (L, B, Hkv, capacity, hd), (L, B, Hkv, hd, capacity)
+        if not (_fits(kv_k, k, dt, index) and _fits(kv_v, v, dt, index) and _fits(lengths, (B,), i32, index)):
+            _check_tensors(((name + "kv_k", kv_k, k, dt), (name + "kv_v", kv_v, v, dt),
+                            (name + "prefix_len", lengths, (B,), i32)), index)
+        return KVCache(kv_k.data_ptr(), kv_v.data_ptr(), capacity, lengths.data_ptr())
 
     def share_prefix(self, kv_k, kv_v, capacity: int, prefix_len, from_, shared: SharedPrefix, new_len,
                      count=None) -> int:
         """Sessions' first slots taken over as shared prefixes (acespec_share_prefix): from_ [P] the
         sessions or -1, count [P] how many slots (None: all).  shared.len is not touched; new_len [P]
         is written."""
-        index, i32 = self._here(), self._types()[1]
+        index, P, i32 = self._here(), (shared.prefixes,), self._kv[4]
         self._check_store(shared, index)
         kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
-        _check_tensors([(n, t, (shared.prefixes,), i32) for n, t in
-                        (("from_", from_), ("new_len", new_len), ("count", count)) if t is not None],
-                       index)
-        return acespec_share_prefix(self.ctx, kv, prefix_len.shape[0], shared.struct(), _ptr(from_),
-                                    _ptr(count), _ptr(new_len), self._stream())
+        if not (_fits(from_, P, i32, index) and _fits(new_len, P, i32, index) and
+                (count is None or _fits(count, P, i32, index))):
+            _check_tensors([(n, t, P, i32) for n, t in (("from_", from_), ("new_len", new_len), ("count", count))
+                            if n != "count" or t is not None], index)
+        return acespec_share_prefix(self.ctx, kv, prefix_len.shape[0], shared.struct(), from_.data_ptr(),
+                                    _ptr(count), new_len.data_ptr(), _stream_of(index))
 
     def attention_shared(self, shared: SharedPrefix, prefix_of, kv_k, kv_v, capacity: int, prefix_len,
                          layer: int, q, parents, out, status) -> int:
         """Tree attention of one layer behind shared prefixes (acespec_attention_shared): q, out
         [B, N+1, H, hd]."""
         B, n1 = parents.shape
-        index, (dt, i32) = self._here(), self._types()
+        index, dt, i32 = self._here(), self._kv[3], self._kv[4]
         self._check_shared(shared, prefix_of, B, index)
-        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
+        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
         shape = (B, n1, self.desc.n_heads, self.desc.head_dim)
-        _check_tensors((("q", q, shape, dt), ("out", out, shape, dt), ("parents", parents, (B, n1), i32),
-                        ("prefix_len", prefix_len, (B,), i32), ("status", status, (B,), i32)), index)
-        return acespec_attention_shared(self.ctx, shared.struct(), _ptr(prefix_of), kv, layer, _ptr(q),
-                                        _ptr(parents), B, n1 - 1, _ptr(out), _ptr(status),
-                                        self._stream())
+        if not (_fits(q, shape, dt, index) and _fits(out, shape, dt, index) and
+                _fits(parents, (B, n1), i32, index) and _fits(status, (B,), i32, index)):
+            _check_tensors((("q", q, shape, dt), ("out", out, shape, dt), ("parents", parents, (B, n1), i32),
+                            ("status", status, (B,), i32)), index)
+        return acespec_attention_shared(self.ctx, shared.struct(), prefix_of.data_ptr(), kv, layer,
+                                        q.data_ptr(), parents.data_ptr(), B, n1 - 1, out.data_ptr(),
+                                        status.data_ptr(), _stream_of(index))
 
     def qk_norm_rope(self, qkv, q_gain, k_gain, kv_k, kv_v, capacity: int, prefix_len, layer: int,
                      parents, q_out, status, shared: Optional[SharedPrefix] = None,
@@ -802,19 +818,23 @@ class Verifier:
         """One layer's projection [B, N+1, (H + 2 Hkv) hd] normalised per head (gains [hd] or None),
         rotated and written to q_out [B, N+1, H, hd] and the cache (acespec_qk_norm_rope)."""
         B, n1 = parents.shape
-        d, index, (dt, i32) = self.desc, self._here(), self._types()
+        d, index, dt, i32 = self.desc, self._here(), self._kv[3], self._kv[4]
         self._check_shared(shared, prefix_of, B, index)
-        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
-        gains = [(n, t, (d.head_dim,), dt) for n, t in (("q_gain", q_gain), ("k_gain", k_gain))
-                 if t is not None]
-        _check_tensors([("qkv", qkv, (B, n1, (d.n_heads + 2 * d.n_kv_heads) * d.head_dim), dt),
-                        ("q_out", q_out, (B, n1, d.n_heads, d.head_dim), dt),
-                        ("parents", parents, (B, n1), i32), ("prefix_len", prefix_len, (B,), i32),
-                        ("status", status, (B,), i32)] + gains, index)
+        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
+        H, hd = d.n_heads, d.head_dim
+        wide, rows = (B, n1, (H + 2 * d.n_kv_heads) * hd), (B, n1, H, hd)
+        if not (_fits(qkv, wide, dt, index) and _fits(q_out, rows, dt, index) and
+                _fits(parents, (B, n1), i32, index) and _fits(status, (B,), i32, index) and
+                (q_gain is None or _fits(q_gain, (hd,), dt, index)) and
+                (k_gain is None or _fits(k_gain, (hd,), dt, index))):
+            _check_tensors([("qkv", qkv, wide, dt), ("q_out", q_out, rows, dt),
+                            ("parents", parents, (B, n1), i32), ("status", status, (B,), i32)] +
+                           [(n, t, (hd,), dt) for n, t in (("q_gain", q_gain), ("k_gain", k_gain))
+                            if t is not None], index)
         return acespec_qk_norm_rope(self.ctx, QKNorm(_ptr(q_gain), _ptr(k_gain)),
                                     None if shared is None else shared.struct(), _ptr(prefix_of), kv,
-                                    layer, _ptr(qkv), _ptr(parents), B, n1 - 1, _ptr(q_out),
-                                    _ptr(status), self._stream())
+                                    layer, qkv.data_ptr(), parents.data_ptr(), B, n1 - 1,
+                                    q_out.data_ptr(), status.data_ptr(), _stream_of(index))
 
     def verify_tree_shared(self, wstruct: Weights, shared: Optional[SharedPrefix], prefix_of, kv_k, kv_v,
                            capacity: int, prefix_len, tokens, parents, q, u, T: float, top_p: float,
@@ -822,10 +842,9 @@ class Verifier:
         """verify_tree for sessions behind shared prefixes (or None, None); norms: a (q_gain, k_gain)
         pair a layer, or None; scalar: q is q_hat [B, N+1]."""
         B, n1 = tokens.shape
-        d, index, (dt, i32) = self.desc, self._here(), self._types()
+        d, index, dt, i32 = self.desc, self._here(), self._kv[3], self._kv[4]
         self._check_shared(shared, prefix_of, B, index)
-        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
-        _check_tensors((("prefix_len", prefix_len, (B,), i32),), index)
+        kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
         self._check_step(index, tokens, parents, q, u, k, outs, scalar)
         array = None
         if norms is not None:
@@ -846,11 +865,13 @@ class Verifier:
         """Sessions take over others' slots [first, src_len) (acespec_fork_kv): from_ [B of dst] the
         sessions of src, or -1; src and dst may be the same tensors.  dst_len is not touched;
         new_prefix_len is written."""
-        index, i32 = self._here(), self._types()[1]
-        src = self._check_cache(src_k, src_v, src_capacity, src_len, index, "src ")
-        dst = self._check_cache(dst_k, dst_v, dst_capacity, dst_len, index, "dst ")
-        B = dst_len.shape[0]
-        _check_tensors([(n, t, (B,), i32) for n, t in (("from_", from_), ("new_prefix_len", new_prefix_len),
-                                                       ("first", first)) if t is not None], index)
-        return acespec_fork_kv(self.ctx, src, src_len.shape[0], dst, B, _ptr(from_), _ptr(first),
-                               _ptr(new_prefix_len), self._stream())
+        index, n, i32 = self._here(), dst_len.shape, self._kv[4]
+        src = self._check_cache(src_k, src_v, src_capacity, src_len, index, None, "src ")
+        dst = self._check_cache(dst_k, dst_v, dst_capacity, dst_len, index, None, "dst ")
+        if not (_fits(from_, n, i32, index) and _fits(new_prefix_len, n, i32, index) and
+                (first is None or _fits(first, n, i32, index))):
+            _check_tensors([(x, t, n, i32) for x, t in
+                            (("from_", from_), ("new_prefix_len", new_prefix_len), ("first", first))
+                            if x != "first" or t is not None], index)
+        return acespec_fork_kv(self.ctx, src, src_len.shape[0], dst, n[0], from_.data_ptr(), _ptr(first),
+                               new_prefix_len.data_ptr(), _stream_of(index))

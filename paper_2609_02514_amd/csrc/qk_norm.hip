@@ -5,9 +5,8 @@
 // Memory bound (the projection read once, rotated queries, keys and values written once); with few
 // rows the chain of loads.  A lane holds 8 dims of a head's lower half and their partners in the
 // upper half, so that a pair never crosses lanes and the sum of squares is 3 lane swaps (2 for
-// head dim 64).  A workgroup takes some rows of a session and some of the heads: angles are
-// evaluated in 64 bits once a row and frequency, kept in LDS and used for all its heads (a row's
-// hd / 2 sines in double cost as much as some 10 heads' loads).
+// head dim 64).  A workgroup takes some rows of a session and some query and key heads, whose loads
+// are under way while it evaluates the rows' angles; or one value head of a session.
 #include "common.h"
 
 namespace {
@@ -39,8 +38,23 @@ template <typename T> AS_DEVICE void load_slices(float (&x)[8], const T *p, int 
   }
 }
 
-// grid: (groups of hpw heads out of H + 2 Hkv, chunks of rpw rows, sessions).  META: positions,
-// slots and angles are there (meta, rot); else they follow from the parents.
+// cos and sin of pos * freq: the product and its distance from a multiple of 2 pi in 64 bits (a
+// position times a frequency of 1 loses 2 pi's fraction in 32), the functions in 32 on that
+// distance's upper part, its lower one to first order.  Off by 2^-23; sines in double took as long
+// as ten heads' loads.
+AS_DEVICE float2 cos_sin(int pos, double freq) {
+  constexpr double TWO_PI = 6.283185307179586, TWO_PI_LOW = 2.4492935982947064e-16;
+  const double x = (double)pos * freq, n = rint(x * (1 / TWO_PI));
+  const double r = fma(-n, TWO_PI_LOW, fma(-n, TWO_PI, x));
+  const float hi = (float)r, lo = (float)(r - (double)hi);
+  float s, c;
+  sincosf(hi, &s, &c);
+  return make_float2(fmaf(-lo, s, c), fmaf(lo, c, s));
+}
+
+// grid: (groups of hpw heads out of H + Hkv for each of `chunks` chunks of rpw rows, then the value
+// heads; sessions).  META: positions, slots and angles are there (meta, rot); else they follow from
+// the parents.
 template <typename TW, typename TIN, typename TQ, int HD, bool META>
 __global__ __launch_bounds__(QT) void qk_norm_rope_kernel(
     const TIN *__restrict__ qkv, int nsl, const TW *__restrict__ q_gain,
@@ -48,19 +62,37 @@ __global__ __launch_bounds__(QT) void qk_norm_rope_kernel(
     const int32_t *__restrict__ parents, const int32_t *__restrict__ prefix_len, SharedArgs sh,
     int32_t *__restrict__ status, TQ *__restrict__ q_out, TW *__restrict__ ck,
     TW *__restrict__ cv, const float2 *__restrict__ rot, int n1, int H, int Hkv, int capacity,
-    int hpw, int rpw) {
+    int hpw, int rpw, int chunks, int groups) {
   constexpr int HALF = HD / 2, LPH = HD / 16;   // lanes a head
-  __shared__ float2 s_rot[QROWS][HALF];
+  __shared__ float2 s_rot[QROWS][HALF + 1];
   __shared__ int s_par[128];
-  const int b = blockIdx.z, r0 = blockIdx.y * rpw, nr = min(rpw, n1 - r0), tid = threadIdx.x;
-  const int h0 = blockIdx.x * hpw, h1 = min(h0 + hpw, H + 2 * Hkv);
+  const int b = blockIdx.y, x = blockIdx.x, tid = threadIdx.x;
+  const bool values = x >= groups * chunks;
+  const int chunk = values ? 0 : x / groups;
+  const int r0 = chunk * rpw, nr = values ? n1 : min(rpw, n1 - r0);
+  const int h0 = (x - chunk * groups) * hpw, hq = values ? 0 : min(hpw, H + Hkv - h0);
   const size_t row0 = (size_t)b * n1 + r0, W = (size_t)(H + 2 * Hkv) * HD;
-  const size_t slice = W * n1 * gridDim.z;
+  const size_t slice = W * n1 * gridDim.y;
+  const TIN *rows = qkv + row0 * W;
+
+  // queries and keys: LPH lanes a (row, head), heads next to each other; the first ones' loads go
+  // out before anything else is known
+  const int l8 = tid % LPH * 8, e0 = tid / LPH, tasks = nr * hq;
+  float a[8], c[8];
+  auto load = [&](int e) {
+    const int r = e / hq, h = h0 + e - r * hq;
+    const TIN *src = rows + r * W + (size_t)h * HD + l8;
+    load_slices(a, src, nsl, slice);
+    load_slices(c, src + HALF, nsl, slice);
+  };
+  if (e0 < tasks) load(e0);
+
   int S;
   if (META) {
     S = meta.sess_S[b];
-    for (int e = tid; e < nr * HALF; e += QT)
-      s_rot[e / HALF][e % HALF] = rot[(row0 + e / HALF) * HALF + e % HALF];
+    if (!values)
+      for (int e = tid; e < nr * HALF; e += QT)
+        s_rot[e / HALF][e % HALF] = rot[(row0 + e / HALF) * HALF + e % HALF];
   } else {
     S = prefix_len[b];
     int front = 0;
@@ -70,40 +102,45 @@ __global__ __launch_bounds__(QT) void qk_norm_rope_kernel(
       const bool in = p >= 0 && p < sh.P;
       if (in) front = sh.len[p];
       ok = ok && (in || p == -1) && front >= 0 && front <= sh.cap;
-      front = min(max(front, 0), sh.cap);
     }
     const int pr = tid < n1 ? parents[(size_t)b * n1 + tid] : 0;
     if (tid < n1) s_par[tid] = pr;
     ok = __syncthreads_and(ok && (tid >= n1 || (tid == 0 ? pr == -1 : pr >= 0 && pr < tid)));
-    if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0)
-      status[b] = ok ? ACESPEC_OK : ACESPEC_EBADTREE;
+    if (x == 0 && tid == 0) status[b] = ok ? ACESPEC_OK : ACESPEC_EBADTREE;
     if (!ok) return;   // nothing of the session is written
-    for (int e = tid; e < nr * HALF; e += QT) {
-      const int r = e / HALF, i = e % HALF;
-      int depth = 0;
-      for (int j = r0 + r; j > 0; j = s_par[j]) ++depth;
-      double sd, cd;
-      sincos((double)(front + S + depth) * inv_freq[i], &sd, &cd);
-      s_rot[r][i] = make_float2((float)cd, (float)sd);
+    if (!values)
+      for (int e = tid; e < nr * HALF; e += QT) {
+        const int r = e / HALF, i = e % HALF;
+        int depth = 0;
+        for (int j = r0 + r; j > 0; j = s_par[j]) ++depth;
+        s_rot[r][i] = cos_sin(front + S + depth, inv_freq[i]);
+      }
+  }
+  if (values) {
+    // rows next to each other, so that a wave's two-byte stores are runs of slots
+    const int g = x - groups * chunks;
+    const TIN *src = rows + (size_t)(H + Hkv + g) * HD;
+    TW *dst = cv + ((size_t)b * Hkv + g) * HD * capacity + S;
+#pragma unroll 2
+    for (int e = tid; e < n1 * (HD / 8); e += QT) {
+      const int p = e / n1, r = e - p * n1;
+      float v[8];
+      load_slices(v, src + r * W + p * 8, nsl, slice);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dst[(size_t)(p * 8 + i) * capacity + r] = from_f32<TW>(v[i]);
     }
+    return;
   }
   __syncthreads();
-  // queries and keys: LPH lanes a (row, head), heads next to each other
-  const int hq = min(h1, H + Hkv) - h0;
-  const int l8 = tid % LPH * 8;
-  for (int e = tid / LPH; e < nr * hq; e += QT / LPH) {   // (whole groups of LPH lanes)
+  for (int e = e0; e < tasks;) {   // (whole groups of LPH lanes)
     const int r = e / hq, h = h0 + e - r * hq;
-    const TIN *src = qkv + (row0 + r) * W + (size_t)h * HD + l8;
-    float a[8], c[8];
-    load_slices(a, src, nsl, slice);
-    load_slices(c, src + HALF, nsl, slice);
     const TW *gain = h < H ? q_gain : k_gain;
     if (gain) {
       float ss = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + c[i] * c[i];
 #pragma unroll
-      for (int x = 1; x < LPH; x <<= 1) ss += __shfl_xor(ss, x);
+      for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o);
       const float inv = 1.0f / sqrtf(ss / (float)HD + eps);
       float ga[8], gc[8];
       load8(ga, gain + l8);
@@ -121,6 +158,8 @@ __global__ __launch_bounds__(QT) void qk_norm_rope_kernel(
       y1[i] = a[i] * cs.x - c[i] * cs.y;
       y2[i] = c[i] * cs.x + a[i] * cs.y;
     }
+    e += QT / LPH;
+    if (e < tasks) load(e);
     if (h < H) {
       TQ *dst = q_out + ((row0 + r) * H + h) * HD + l8;
       store8(dst, y1);
@@ -130,18 +169,6 @@ __global__ __launch_bounds__(QT) void qk_norm_rope_kernel(
       store8(dst, y1);
       store8(dst + HALF, y2);
     }
-  }
-  // values: rows next to each other, so that a wave's two-byte stores are runs of slots
-  const int v0 = max(h0, H + Hkv), hv = h1 - v0;
-  const int pr2 = nr > 8 ? 16 : nr > 4 ? 8 : nr > 2 ? 4 : nr > 1 ? 2 : 1;   // lanes a column of rows
-  for (int e = tid; e < hv * (HD / 8) * pr2; e += QT) {
-    const int r = e % pr2, x = e / pr2, d = x % (HD / 8) * 8, h = v0 + x / (HD / 8);
-    if (r >= nr) continue;
-    float v[8];
-    load_slices(v, qkv + (row0 + r) * W + (size_t)h * HD + d, nsl, slice);
-    TW *dst = cv + (((size_t)b * Hkv + h - H - Hkv) * HD + d) * capacity + S + r0 + r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dst[(size_t)i * capacity] = from_f32<TW>(v[i]);
   }
 }
 
@@ -158,15 +185,15 @@ hipError_t launch_qk_norm_rope(const TIN *qkv, int nsl, const TW *q_gain, const 
                                int capacity, hipStream_t s) {
   if ((hd != 64 && hd != 128) || H % Hkv || n1 > 65 || B > 65535) return hipErrorInvalidValue;
   const int chunks = (n1 + QROWS - 1) / QROWS, rpw = (n1 + chunks - 1) / chunks;
-  const int heads = H + 2 * Hkv, groups = (heads + 11) / 12, hpw = (heads + groups - 1) / groups;
-  const dim3 grid((heads + hpw - 1) / hpw, chunks, B);
+  const int heads = H + Hkv, hpw = heads < 8 ? heads : 8, groups = (heads + hpw - 1) / hpw;
+  const dim3 grid(groups * chunks + Hkv, B);
   auto kernel = parents ? (hd == 64 ? qk_norm_rope_kernel<TW, TIN, TQ, 64, false>
                                     : qk_norm_rope_kernel<TW, TIN, TQ, 128, false>)
                         : (hd == 64 ? qk_norm_rope_kernel<TW, TIN, TQ, 64, true>
                                     : qk_norm_rope_kernel<TW, TIN, TQ, 128, true>);
   hipLaunchKernelGGL(kernel, grid, dim3(QT), 0, s, qkv, nsl, q_gain, k_gain, eps, inv_freq, meta,
                      parents, prefix_len, sh, status, q_out, ck, cv, rot, n1, H, Hkv, capacity, hpw,
-                     rpw);
+                     rpw, chunks, groups);
   return hipGetLastError();
 }
 

@@ -87,9 +87,9 @@ template <typename T> AS_DEVICE u32x4 load_any(const T *p) {
   return ((const U *)p)->x;
 }
 
-// One workgroup takes FCH slots of one plane (layer, kv head, session).  Neighbouring workgroups
-// take the same slots of the sessions that may have them from one source, so that a source read by
-// several is read from memory once.
+// One workgroup takes FCH slots of one plane (layer, kv head, session).  Workgroups that take the
+// same slots of the sessions follow each other on one XCD: what several have from one source its L2
+// reads from memory once.
 constexpr int FCH = 256;
 template <typename T, int HD>
 __global__ __launch_bounds__(ST) void fork_kernel(const T *__restrict__ sk, const T *__restrict__ sv,
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(ST) void fork_kernel(const T *__restrict__ sk, cons
                                                   int32_t *__restrict__ new_len, int Hkv,
                                                   int chunks, int same) {
   constexpr int PE = 16 / sizeof(T);
-  const int b = blockIdx.x % Bd, rest = blockIdx.x / Bd;
+  const int id = xcd_tile(blockIdx.x, gridDim.x), b = id % Bd, rest = id / Bd;
   const int c = rest % chunks, lg = rest / chunks, l = lg / Hkv, g = lg - l * Hkv;
   const int tid = threadIdx.x;
   const int src = from[b];
