@@ -355,9 +355,11 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
                     rows, M, l, o, [&](int) { return d; });
 }
 
-// fp32 models: one workgroup per (tree row, query head), over the prefix's records and then the
-// session's own slots, 256 slots at a time: scores with HD / 4 lanes a slot, a softmax step over
-// the block, then the values, 16 lanes x 4 slots of a head dim.
+// fp32 models: one workgroup per (tree row, query head), over the prefix's records and behind them
+// the session's own slots as one line of slots, 256 at a time (their latencies bound it: the two
+// one after the other took 18 us where this takes 13, two sessions of 128 and 40 slots): scores with
+// HD / 4 lanes a slot, a softmax step over the block, then the values, 16 lanes x 4 slots of a head
+// dim.
 template <int HD>
 __global__ __launch_bounds__(256) void shared_attn_f32_kernel(
     const float *__restrict__ qin, const float *__restrict__ blocks, SharedArgs sh,
@@ -373,77 +375,73 @@ __global__ __launch_bounds__(256) void shared_attn_f32_kernel(
   const int h = blockIdx.x, row = blockIdx.y;
   const int b = row / n1;
   const int G = H / Hkv, g = h / G, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int S = meta.sess_S[b], own = S + n1, front = sessions[b].slots;
+  const int S = meta.sess_S[b], front = sessions[b].slots, prefix = max(sh.of[b], 0);
   const uint64_t anc = meta.anc[row];
-  const int prefix = front > 0 ? sh.of[b] : 0;
-  const float *rec = blocks + ((size_t)prefix * Hkv + g) * (sh.cap >> 6) * REC;
+  const int start = (front + 63) & ~63, total = start + S + n1;   // own slots begin at `start`
+  const float *rec = blocks + ((size_t)(front > 0 ? prefix : 0) * Hkv + g) * (sh.cap >> 6) * REC;
   const float *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const float *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;   // [HD][capacity]
   const float4 q4 = *(const float4 *)(qin + (size_t)row * H * HD + h * HD + lane % LPS * 4);
   const float scale = 1.0f / sqrtf((float)HD);
+  auto visible = [&](int slot) {
+    const int j = slot - start - S;
+    return slot < start ? slot < front : j <= 0 || (j < n1 && (bool)((anc >> (j - 1)) & 1ull));
+  };
   float m = -INFINITY, l = 0.f, o[DJ];
 #pragma unroll
   for (int j = 0; j < DJ; ++j) o[j] = 0.f;
-  for (int part = 0; part < 2; ++part) {
-    const int total = part == 0 ? front : own;
-    for (int c0 = 0; c0 < total; c0 += NCH) {
-      float4 kv[STEPS];
+  for (int c0 = 0; c0 < total; c0 += NCH) {
+    float4 kv[STEPS];
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int slot = min(c0 + wave * 64 + i * SPW + lane / LPS, total - 1);
-        const float *k = part == 0 ? rec + (size_t)(slot >> 6) * REC + (slot & 63) * HD
-                                   : kb + (size_t)slot * HD;
-        kv[i] = *(const float4 *)(k + lane % LPS * 4);
-      }
-      auto visible = [&](int slot) {
-        if (part == 0 || slot < S) return slot < total;
-        const int j = slot - S;
-        return j < n1 && (j == 0 || (bool)((anc >> (j - 1)) & 1ull));
-      };
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int ls = wave * 64 + i * SPW + lane / LPS;
-        float d = q4.x * kv[i].x + q4.y * kv[i].y + q4.z * kv[i].z + q4.w * kv[i].w;
-#pragma unroll
-        for (int x = 1; x < LPS; x <<= 1) d += __shfl_xor(d, x);
-        if (lane % LPS == 0) p[ls] = visible(c0 + ls) ? d * scale : -INFINITY;
-      }
-      __syncthreads();
-      const float s = p[tid];
-      float mx = wave_max(s);
-      if (lane == 0) red[wave] = mx;
-      __syncthreads();
-      mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-      const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
-      const bool vis = visible(c0 + tid);
-      const float e = vis ? expf(s - mu) : 0.f, a = expf(m - mu);
-      m = mn;
-      p[tid] = vis ? e : -1.f;            // (a hidden slot's value is left out, not times 0)
-      const float ls = wave_sum(e);
-      if (lane == 0) red[4 + wave] = ls;
-      __syncthreads();
-      l = l * a + ((red[4] + red[5]) + (red[6] + red[7]));
-#pragma unroll
-      for (int j = 0; j < DJ; ++j) o[j] *= a;
-      // values: lane % 16 takes slots 4 (lane % 16) + 64 i, for head dims wave * 4 + lane / 16
-      // + 16 j (rows of 64 slots or of the capacity, a multiple of 64: reads stay in them)
-      for (int i = 0; i < NCH / 64 && c0 + i * 64 < total; ++i) {
-        const int ls4 = i * 64 + lane % 16 * 4, slot = c0 + ls4;
-        const float4 pw = *(const float4 *)(p + ls4);
-#pragma unroll
-        for (int j = 0; j < DJ; ++j) {
-          const int dim = wave * 4 + lane / 16 + 16 * j;
-          const float *vr = part == 0 ? rec + (size_t)(slot >> 6) * REC + REC / 2 + dim * 64 + (slot & 63)
-                                      : vb + (size_t)dim * capacity + slot;
-          const float4 v = *(const float4 *)vr;
-          if (pw.x >= 0.f) o[j] += pw.x * v.x;
-          if (pw.y >= 0.f) o[j] += pw.y * v.y;
-          if (pw.z >= 0.f) o[j] += pw.z * v.z;
-          if (pw.w >= 0.f) o[j] += pw.w * v.w;
-        }
-      }
-      __syncthreads();
+    for (int i = 0; i < STEPS; ++i) {
+      const int slot = min(c0 + wave * 64 + i * SPW + lane / LPS, total - 1);
+      const float *k = slot < start ? rec + (size_t)(slot >> 6) * REC + (slot & 63) * HD
+                                    : kb + (size_t)(slot - start) * HD;
+      kv[i] = *(const float4 *)(k + lane % LPS * 4);
     }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int ls = wave * 64 + i * SPW + lane / LPS;
+      float d = q4.x * kv[i].x + q4.y * kv[i].y + q4.z * kv[i].z + q4.w * kv[i].w;
+#pragma unroll
+      for (int x = 1; x < LPS; x <<= 1) d += __shfl_xor(d, x);
+      if (lane % LPS == 0) p[ls] = visible(c0 + ls) ? d * scale : -INFINITY;
+    }
+    __syncthreads();
+    const float s = p[tid];
+    float mx = wave_max(s);
+    if (lane == 0) red[wave] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
+    const bool vis = visible(c0 + tid);
+    const float e = vis ? expf(s - mu) : 0.f, a = expf(m - mu);
+    m = mn;
+    p[tid] = vis ? e : -1.f;            // (a hidden slot's value is left out, not times 0)
+    const float ls = wave_sum(e);
+    if (lane == 0) red[4 + wave] = ls;
+    __syncthreads();
+    l = l * a + ((red[4] + red[5]) + (red[6] + red[7]));
+#pragma unroll
+    for (int j = 0; j < DJ; ++j) o[j] *= a;
+    // values: lane % 16 takes slots 4 (lane % 16) + 64 i, for head dims wave * 4 + lane / 16 + 16 j
+    // (rows of 64 slots or of the capacity, a multiple of 64: reads stay in them)
+    for (int i = 0; i < NCH / 64 && c0 + i * 64 < total; ++i) {
+      const int ls4 = i * 64 + lane % 16 * 4, slot = c0 + ls4;
+      const float4 pw = *(const float4 *)(p + ls4);
+#pragma unroll
+      for (int j = 0; j < DJ; ++j) {
+        const int dim = wave * 4 + lane / 16 + 16 * j;
+        const float *vr = slot < start ? rec + (size_t)(slot >> 6) * REC + REC / 2 + dim * 64 + (slot & 63)
+                                       : vb + (size_t)dim * capacity + slot - start;
+        const float4 v = *(const float4 *)vr;
+        if (pw.x >= 0.f) o[j] += pw.x * v.x;
+        if (pw.y >= 0.f) o[j] += pw.y * v.y;
+        if (pw.z >= 0.f) o[j] += pw.z * v.z;
+        if (pw.w >= 0.f) o[j] += pw.w * v.w;
+      }
+    }
+    __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < DJ; ++j) {
