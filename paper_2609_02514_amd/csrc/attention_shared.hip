@@ -355,100 +355,146 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
                     rows, M, l, o, [&](int) { return d; });
 }
 
-// fp32 models: one workgroup per (tree row, query head), over the prefix's records and behind them
-// the session's own slots as one line of slots, 256 at a time (their latencies bound it: the two
-// one after the other took 18 us where this takes 13, two sessions of 128 and 40 slots): scores with
-// HD / 4 lanes a slot, a softmax step over the block, then the values, 16 lanes x 4 slots of a head
-// dim.
+// fp32 models: one workgroup per 16 query rows of a (session, kv head), over the prefix's records
+// and behind them the session's own slots as one line of slots, whose blocks of 16 go round its
+// eight waves.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x4_f32: lane (x, y) of 16 x 4
+// holds key row x and head dims y HD/4 .. of it (the products' steps may take the dims in any order
+// that the queries share), hence scores of slots 4 y .. 4 y + 3 for query x, which are as they stand
+// its operand of the second product: step e takes slot 4 y + e.  No LDS before the join, and no
+// rounding to fewer bits anywhere.  Bound by latency in small batches and by the reads of keys and
+// values (L2) in large ones, 16 rows a read: a workgroup a row and head took 332 us for 4 sessions
+// of 25 rows and 4 heads a kv head over 1200 slots where this takes 50.
 template <int HD>
-__global__ __launch_bounds__(256) void shared_attn_f32_kernel(
+__global__ __launch_bounds__(512) void shared_attn_f32_kernel(
     const float *__restrict__ qin, const float *__restrict__ blocks, SharedArgs sh,
     const SharedSession *__restrict__ sessions, const float *__restrict__ ck,
     const float *__restrict__ cv, TreeMeta meta, float *__restrict__ out, int n1, int H, int Hkv,
     int capacity) {
-  constexpr int LPS = HD / 4, SPW = 64 / LPS;   // lanes a slot, slots a wave and load
-  constexpr int NCH = 256, STEPS = NCH / 4 / SPW;
-  constexpr int DJ = HD / 16;                   // head dims a lane sums
-  constexpr int REC = 128 * HD;
-  __shared__ __attribute__((aligned(16))) float p[NCH];
-  __shared__ float red[8];
-  const int h = blockIdx.x, row = blockIdx.y;
-  const int b = row / n1;
-  const int G = H / Hkv, g = h / G, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int S = meta.sess_S[b], front = sessions[b].slots, prefix = max(sh.of[b], 0);
-  const uint64_t anc = meta.anc[row];
+  constexpr int NW = 8, NK = HD / 16, ND = HD / 16, REC = 128 * HD;
+  __shared__ __attribute__((aligned(16))) float so[NW][16][HD + 4];
+  __shared__ float sml[NW][16][2];
+  __shared__ int s_bad;   // a tree row has a value that is not finite
+  const int tile = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lx = lane & 15, ly = lane >> 4;
+  const int G = H / Hkv, QR = G * n1, qi = min(tile * 16 + lx, QR - 1), r = qi / G;
+  const int S = meta.sess_S[b], front = sessions[b].slots, prefix = front > 0 ? sh.of[b] : 0;
   const int start = (front + 63) & ~63, total = start + S + n1;   // own slots begin at `start`
-  const float *rec = blocks + ((size_t)(front > 0 ? prefix : 0) * Hkv + g) * (sh.cap >> 6) * REC;
+  const uint64_t anc = meta.anc[(size_t)b * n1 + r];
+  const float *rec = blocks + ((size_t)prefix * Hkv + g) * (sh.cap >> 6) * REC;
   const float *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const float *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;   // [HD][capacity]
-  const float4 q4 = *(const float4 *)(qin + (size_t)row * H * HD + h * HD + lane % LPS * 4);
   const float scale = 1.0f / sqrtf((float)HD);
-  auto visible = [&](int slot) {
-    const int j = slot - start - S;
-    return slot < start ? slot < front : j <= 0 || (j < n1 && (bool)((anc >> (j - 1)) & 1ull));
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  f32x4 qf[NK];
+  const float *qp = qin + ((size_t)b * n1 + r) * H * HD + (g * G + qi - r * G) * HD + ly * (HD / 4);
+#pragma unroll
+  for (int i = 0; i < NK; ++i) qf[i] = *(const f32x4 *)(qp + i * 4);
+  const int nblk = (total + 15) >> 4;
+  f32x4 kx[NK], vx[ND];
+  auto load = [&](int c) {   // (a record's or the capacity's 64 slots hold all of a block)
+    const int slot = c * 16, in = slot & 63;
+    const float *rp = rec + (size_t)(slot >> 6) * REC;
+    const float *kp = slot < start ? rp + in * HD : kb + (size_t)(slot - start) * HD;
+    const float *vp = slot < start ? rp + REC / 2 + in : vb + slot - start;
+    const int stride = slot < start ? 64 : capacity;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) kx[i] = *(const f32x4 *)(kp + lx * HD + ly * (HD / 4) + i * 4);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) vx[d] = *(const f32x4 *)(vp + (size_t)(d * 16 + lx) * stride + ly * 4);
   };
-  float m = -INFINITY, l = 0.f, o[DJ];
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[ND];
 #pragma unroll
-  for (int j = 0; j < DJ; ++j) o[j] = 0.f;
-  for (int c0 = 0; c0 < total; c0 += NCH) {
-    float4 kv[STEPS];
+  for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (wave < nblk) load(wave);
+  for (int c = wave; c < nblk; c += NW) {
+    const int slot0 = c * 16 + ly * 4;   // of this lane's four
+    f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-      const int slot = min(c0 + wave * 64 + i * SPW + lane / LPS, total - 1);
-      const float *k = slot < start ? rec + (size_t)(slot >> 6) * REC + (slot & 63) * HD
-                                    : kb + (size_t)(slot - start) * HD;
-      kv[i] = *(const float4 *)(k + lane % LPS * 4);
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[i][e], qf[i][e], z, 0, 0, 0);
+    f32x4 v[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) v[d] = vx[d];
+    if (c + NW < nblk) load(c + NW);
+    z *= scale;
+    if (c * 16 + 16 > front && (c * 16 < start || c * 16 + 16 > start + S)) {
+      // the prefix's end, or the tree: hidden slots, and values there that are no numbers
+      // (bitwise, so that these are selects)
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int slot = slot0 + e, j = slot - start - S, sh = min(max(j - 1, 0), 63);
+        const bool front_part = slot < start;
+        const bool there = slot < (front_part ? front : total);
+        const bool seen = there & (front_part | (j <= 0) | (bool)((anc >> sh) & 1ull));
+        const bool tree = !front_part & (j >= 0) & there;
+        z[e] = seen ? z[e] : -INFINITY;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const bool number = fabsf(v[d][e]) <= 3.402823466e38f;
+          odd |= tree & !number;
+          v[d][e] = there & (number | !tree) ? v[d][e] : 0.f;
+        }
+      }
+      if (__ballot(odd)) s_bad = 1;
     }
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-      const int ls = wave * 64 + i * SPW + lane / LPS;
-      float d = q4.x * kv[i].x + q4.y * kv[i].y + q4.z * kv[i].z + q4.w * kv[i].w;
-#pragma unroll
-      for (int x = 1; x < LPS; x <<= 1) d += __shfl_xor(d, x);
-      if (lane % LPS == 0) p[ls] = visible(c0 + ls) ? d * scale : -INFINITY;
-    }
-    __syncthreads();
-    const float s = p[tid];
-    float mx = wave_max(s);
-    if (lane == 0) red[wave] = mx;
-    __syncthreads();
-    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
-    const bool vis = visible(c0 + tid);
-    const float e = vis ? expf(s - mu) : 0.f, a = expf(m - mu);
+    const float mn = fmaxf(m, rows4_max(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]))));
+    const float mu = mn == -INFINITY ? 0.f : mn, alpha = expf(m - mu);
     m = mn;
-    p[tid] = vis ? e : -1.f;            // (a hidden slot's value is left out, not times 0)
-    const float ls = wave_sum(e);
-    if (lane == 0) red[4 + wave] = ls;
-    __syncthreads();
-    l = l * a + ((red[4] + red[5]) + (red[6] + red[7]));
+    f32x4 p;
 #pragma unroll
-    for (int j = 0; j < DJ; ++j) o[j] *= a;
-    // values: lane % 16 takes slots 4 (lane % 16) + 64 i, for head dims wave * 4 + lane / 16 + 16 j
-    // (rows of 64 slots or of the capacity, a multiple of 64: reads stay in them)
-    for (int i = 0; i < NCH / 64 && c0 + i * 64 < total; ++i) {
-      const int ls4 = i * 64 + lane % 16 * 4, slot = c0 + ls4;
-      const float4 pw = *(const float4 *)(p + ls4);
+    for (int e = 0; e < 4; ++e) p[e] = expf(z[e] - mu);
+    l = l * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
+    if (__ballot(alpha < 1.f)) {
 #pragma unroll
-      for (int j = 0; j < DJ; ++j) {
-        const int dim = wave * 4 + lane / 16 + 16 * j;
-        const float *vr = slot < start ? rec + (size_t)(slot >> 6) * REC + REC / 2 + dim * 64 + (slot & 63)
-                                       : vb + (size_t)dim * capacity + slot - start;
-        const float4 v = *(const float4 *)vr;
-        if (pw.x >= 0.f) o[j] += pw.x * v.x;
-        if (pw.y >= 0.f) o[j] += pw.y * v.y;
-        if (pw.z >= 0.f) o[j] += pw.z * v.z;
-        if (pw.w >= 0.f) o[j] += pw.w * v.w;
+      for (int d = 0; d < ND; ++d) o[d] *= alpha;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[d][e], p[e], o[d], 0, 0, 0);
+  }
+  // o[d][e] is head dim 16 d + 4 ly + e of query lx: the waves' parts join in LDS
+  l = rows4_sum(l);
+#pragma unroll
+  for (int d = 0; d < ND; ++d) *(f32x4 *)(&so[wave][lx][d * 16 + ly * 4]) = o[d];
+  if (ly == 0) {
+    sml[wave][lx][0] = m;
+    sml[wave][lx][1] = l;
+  }
+  __syncthreads();
+  for (int e = tid; e < 16 * HD / 4; e += 512) {
+    const int x = e / (HD / 4), d = e % (HD / 4) * 4, qx = tile * 16 + x;
+    if (qx >= QR) continue;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, sml[w][x][0]);
+    if (M == -INFINITY) M = 0.f;
+    f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+    float den = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float y = expf(sml[w][x][0] - M);
+      den += y * sml[w][x][1];
+      sum += y * *(const f32x4 *)(&so[w][x][d]);
+    }
+    const int rx = qx / G, h = g * G + qx - rx * G, row = b * n1 + rx;
+    if (s_bad) {   // an infinity or a NaN comes of such a value in the rows that see it
+      const uint64_t ax = meta.anc[row];
+      for (int t = 0; t < n1; ++t) {
+        if (t > 0 && !((ax >> (t - 1)) & 1ull)) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = vb[(size_t)(d + i) * capacity + S + t];
+          if (!(fabsf(v) <= 3.402823466e38f)) sum[i] += v;
+        }
       }
     }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int j = 0; j < DJ; ++j) {
-#pragma unroll
-    for (int x = 1; x < 16; x <<= 1) o[j] += __shfl_xor(o[j], x);
-    if (lane % 16 == 0)
-      out[(size_t)row * (H * HD) + h * HD + wave * 4 + lane / 16 + 16 * j] = o[j] / l;
+    *(f32x4 *)(out + (size_t)row * H * HD + h * HD + d) = sum / den;
   }
 }
 
@@ -506,7 +552,8 @@ hipError_t launch_attention_shared<float>(const void *q, const float *blocks, co
                                           float *, float *, long long, int B, int n1, int H,
                                           int Hkv, int hd, int capacity, int, hipStream_t s) {
   auto kernel = hd == 64 ? shared_attn_f32_kernel<64> : shared_attn_f32_kernel<128>;
-  hipLaunchKernelGGL(kernel, dim3(H, B * n1), dim3(256), 0, s, (const float *)q, blocks, sh, sm.sessions, ck, cv, meta,
+  if (Hkv > 65535 || B > 65535) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(kernel, dim3((H / Hkv * n1 + 15) / 16, Hkv, B), dim3(512), 0, s, (const float *)q, blocks, sh, sm.sessions, ck, cv, meta,
                      (float *)out, n1, H, Hkv, capacity);
   return hipGetLastError();
 }
