@@ -142,6 +142,39 @@ AS_DEVICE void issue_chunk(uint16_t *stage, __amdgpu_buffer_rsrc_t kr,
   }
 }
 
+// The same of a record of a shared prefix (fp16, pieces in the order of 32 x 32 operands) at byte
+// `at` of its plane.
+template <int HD, int NW, bool T32 = false>
+AS_DEVICE void issue_record(uint16_t *stage, __amdgpu_buffer_rsrc_t rr, int at, int wave, int lane) {
+  constexpr int BLOCKS = HD / 8;
+#pragma unroll
+  for (int j = 0; j < 2 * BLOCKS / NW; ++j) {
+    const int blk = wave + NW * j;
+    int from;   // the piece
+    if (blk < BLOCKS) {
+      const int e = blk * 512 + lane * 8, key = e / HD, d8 = ((e % HD) >> 3) ^ kswz<HD, T32>(key);
+      const int row = (key & 16) + ((key >> 3) & 1) * 4 + ((key >> 2) & 1) * 8 + (key & 3);
+      from = ((key >> 5) * (HD / 16) + (d8 >> 1)) * 64 + (d8 & 1) * 32 + row;
+    } else {
+      const int row = (blk - BLOCKS) * 8 + (lane >> 3), s8 = (lane & 7) ^ vsw(row);
+      from = KC * HD / 8 + ((s8 >> 1) * (HD / 32) + (row >> 5)) * 64 + (s8 & 1) * 32 + (row & 31);
+    }
+    buf_dma16(rr, (lds_ptr_t)(stage + blk * 512), (uint32_t)from * 16, at);
+  }
+}
+
+// Zeroes the values of a record's slots >= valid in a stage.
+template <int HD>
+AS_DEVICE void cut_record(uint16_t *stage, int t, int stride, int valid) {
+  for (int vp = t; vp < KC * HD / 8; vp += stride) {
+    uint16_t *p = stage + KC * HD + vp * 8;
+    const int s0 = ((vp & 7) ^ vsw(vp >> 3)) << 3;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (s0 + e >= valid) p[e] = 0;
+  }
+}
+
 // Tree rows whose values are not all finite: three words.
 AS_DEVICE void mark_row(uint32_t *bad, int row) { atomicOr(bad + (row >> 5), 1u << (row & 31)); }
 
@@ -178,12 +211,15 @@ AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int tot
   }
 }
 
-template <int HD, int NW, int UPW, int NST, bool PART = false, typename TQ = f16>
+template <int HD, int NW, int UPW, int NST, int MODE = 0, typename TQ = f16>
 __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
     const TQ *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
     float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int tpg,
     SharedJoin join) {
+  // MODE 0: the verify pass; 1: own slots behind a shared prefix, joined with its partial results or
+  // left as some; 2: its records first, then the own slots
+  constexpr bool PART = MODE > 0, RECORDS = MODE == 2;
   constexpr int KSTEPS = HD / 32, NB = HD / 16;
   constexpr int STAGE = 2 * KC * HD;     // elements: K [KC][HD], then V^T [HD][KC]
   constexpr int L_DMA = HD / 4 / NW;     // DMA instructions per wave per chunk
@@ -213,20 +249,28 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   const int qbase = NW - 4 * rlast;  // first wave holding a quarter unit
   const bool quarter = split_last && wave >= qbase;
   const int qk = (wave - qbase) & 3;  // a quarter unit's key block within each chunk
-  const int S = meta.sess_S[b];
-  const int total = S + n1;
-  const int nchunks = (total + KC - 1) / KC;
-  const int cps = (nchunks + nsplit - 1) / nsplit;
-  const int c0 = split * cps;
-  const int c1 = min(nchunks, c0 + cps);
   __shared__ uint32_t bad[PART ? 3 : 1];   // tree rows with values that are not finite
   if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
   SharedSession me{};          // (asked for here, well before the join needs it)
   int4 total_units{};
-  if (PART && join.here) {
+  if (PART && (RECORDS || join.here)) {
     me = join.sm.sessions[b];
     total_units = *join.sm.total;
   }
+  // chunks of the session's shared prefix, in front of its own, if they are taken here
+  const int front = RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
+  const int fc = RECORDS ? (front + KC - 1) / KC : 0;
+  const size_t plane = RECORDS && fc > 0 ? (size_t)join.sh.cap * 2 * HD : 0;
+  const int prefix = RECORDS && fc > 0 ? __builtin_amdgcn_readfirstlane(join.sh.of[b]) : 0;
+  const __amdgpu_buffer_rsrc_t rr = make_rsrc(join.blocks + ((size_t)prefix * Hkv + g) * plane,
+                                              (uint32_t)(plane * 2));
+  if (RECORDS) me.place = -1;   // nothing to join
+  const int S = meta.sess_S[b];
+  const int total = S + n1;
+  const int nchunks = fc + (total + KC - 1) / KC;
+  const int cps = (nchunks + nsplit - 1) / nsplit;
+  const int c0 = split * cps;
+  const int c1 = min(nchunks, c0 + cps);
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -266,6 +310,18 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   wait_vmcnt<0>();   // the loop's vmcnt accounting covers the DMA only
 
   auto stage_of = [&](int c) { return smem + ((c - c0) % NST) * STAGE; };
+  auto issue = [&](int c) {
+    if (RECORDS && c < fc)
+      issue_record<HD, NW>(stage_of(c), rr, c * (STAGE * 2), wave, lane);
+    else
+      issue_chunk<HD, NW>(stage_of(c), kr, vr, (c - fc) * KC, capacity, wave, lane);
+  };
+  auto widen = [&](int c, int t, int stride) {
+    if (!RECORDS || c >= fc)
+      widen_chunk<HD, PART>(stage_of(c), t, stride, (c - fc) * KC, total, S, bad);
+    else if (front - c * KC < KC)
+      cut_record<HD>(stage_of(c), t, stride, front - c * KC);
+  };
   // The widening goes to the waves without a tile when there are any (one SIMD then
   // holds no more than its share of tile work plus widening), else to every wave.
   const int wbeg = ntiles < NW ? ntiles : 0;
@@ -275,11 +331,11 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   // Prologue: chunks c0 .. c0+NST-2 in flight, chunk c0 widened.
 #pragma unroll
   for (int i = 0; i < NST - 1; ++i)
-    if (c0 + i < c1) issue_chunk<HD, NW>(stage_of(c0 + i), kr, vr, (c0 + i) * KC, capacity, wave, lane);
+    if (c0 + i < c1) issue(c0 + i);
   if (!SYNC && c0 < c1) {
     if (c0 + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
     lds_barrier();
-    if (widener) widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad);
+    if (widener) widen(c0, wt, wstride);
   }
 
   // Fragment offsets: the swizzles depend on the lane only, so the read of K block kk at
@@ -300,8 +356,8 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
       wait_vmcnt<0>();
       chunk_barrier();
       if (c + 1 < c1)
-        issue_chunk<HD, NW>(stage_of(c + 1), kr, vr, (c + 1) * KC, capacity, wave, lane);
-      widen_chunk<HD, PART>(stage_of(c), tid, NW * 64, c * KC, total, S, bad);
+        issue(c + 1);
+      widen(c, tid, NW * 64);
       chunk_barrier();
     } else {
       if (c + 1 < c1) {
@@ -309,16 +365,18 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
       }
       chunk_barrier();
       if (c + NST - 1 < c1)
-        issue_chunk<HD, NW>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity, wave, lane);
+        issue(c + NST - 1);
       if (c + 1 < c1 && widener)
-        widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad);
+        widen(c + 1, wt, wstride);
     }
 
     const uint16_t *st = stage_of(c);
     const f16 *sk = (const f16 *)st;
     const f16 *sv = (const f16 *)(st + KC * HD);
-    const int key0 = c * KC;
-    const bool tree_chunk = key0 + KC > S;
+    // (a record's slots in front of the prefix's end are seen by all, those behind it by none)
+    const bool record = RECORDS && c < fc;
+    const int key0 = record ? 0 : (c - fc) * KC, Sc = record ? front - c * KC : S, n1c = record ? 0 : n1;
+    const bool tree_chunk = key0 + KC > Sc;
 #pragma unroll
     for (int t = 0; t < UPW; ++t) {
       if (wave + NW * t >= ntiles || (split_last && t == QS)) break;
@@ -341,9 +399,9 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             // the slot is tree row j (a prefix slot if j < 0)
-            const int j = key0 + key_of_score(kk, lg, e) - S;
+            const int j = key0 + key_of_score(kk, lg, e) - Sc;
             const int sh = min(max(j - 1, 0), 63);
-            const bool vis = (j < 0) | ((j < n1) & ((j == 0) | (bool)((anc[t] >> sh) & 1ull)));
+            const bool vis = (j < 0) | ((j < n1c) & ((j == 0) | (bool)((anc[t] >> sh) & 1ull)));
             sc[kk][e] = vis ? sc[kk][e] : -INFINITY;
           }
       }
@@ -397,9 +455,9 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
         MASK_BRANCH();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int j = key0 + key_of_score(qk, lg, e) - S;
+          const int j = key0 + key_of_score(qk, lg, e) - Sc;
           const int sh = min(max(j - 1, 0), 63);
-          const bool vis = (j < 0) | ((j < n1) & ((j == 0) | (bool)((anc[QS] >> sh) & 1ull)));
+          const bool vis = (j < 0) | ((j < n1c) & ((j == 0) | (bool)((anc[QS] >> sh) & 1ull)));
           sq[e] = vis ? sq[e] : -INFINITY;
         }
       }
@@ -579,12 +637,13 @@ AS_DEVICE float halves_sum(float v) {
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
-template <int HD, int NST, bool PART = false, typename TQ = f16>
+template <int HD, int NST, int MODE = 0, typename TQ = f16>
 __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     const TQ *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
     float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int rpg,
     SharedJoin join) {
+  constexpr bool PART = MODE > 0, RECORDS = MODE == 2;
   constexpr int NW = 8;
   constexpr int KS16 = HD / 16;   // 16-dim k-steps of a 32-row tile's S^T
   constexpr int NDB = HD / 32;    // 32-dim blocks of its O^T
@@ -611,20 +670,28 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   const bool t32 = wave < n32;
   const bool quarter = rem > 0 && wave >= NW - 4;
   const int qk = wave & 3;                    // a quarter unit's key block in each chunk
-  const int S = meta.sess_S[b];
-  const int total = S + n1;
-  const int nchunks = (total + KC - 1) / KC;
-  const int cps = (nchunks + nsplit - 1) / nsplit;
-  const int c0 = split * cps;
-  const int c1 = min(nchunks, c0 + cps);
   __shared__ uint32_t bad[PART ? 3 : 1];   // tree rows with values that are not finite
   if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
   SharedSession me{};          // (asked for here, well before the join needs it)
   int4 total_units{};
-  if (PART && join.here) {
+  if (PART && (RECORDS || join.here)) {
     me = join.sm.sessions[b];
     total_units = *join.sm.total;
   }
+  // chunks of the session's shared prefix, in front of its own, if they are taken here
+  const int front = RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
+  const int fc = RECORDS ? (front + KC - 1) / KC : 0;
+  const size_t plane = RECORDS && fc > 0 ? (size_t)join.sh.cap * 2 * HD : 0;
+  const int prefix = RECORDS && fc > 0 ? __builtin_amdgcn_readfirstlane(join.sh.of[b]) : 0;
+  const __amdgpu_buffer_rsrc_t rr = make_rsrc(join.blocks + ((size_t)prefix * Hkv + g) * plane,
+                                              (uint32_t)(plane * 2));
+  if (RECORDS) me.place = -1;   // nothing to join
+  const int S = meta.sess_S[b];
+  const int total = S + n1;
+  const int nchunks = fc + (total + KC - 1) / KC;
+  const int cps = (nchunks + nsplit - 1) / nsplit;
+  const int c0 = split * cps;
+  const int c1 = min(nchunks, c0 + cps);
   const bf16 *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(kb, (uint32_t)((size_t)capacity * HD * 2));
@@ -680,17 +747,29 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   wait_vmcnt<0>();   // the loop's vmcnt accounting covers the DMA only
 
   auto stage_of = [&](int c) { return smem + ((c - c0) % NST) * STAGE; };
+  auto issue = [&](int c) {
+    if (RECORDS && c < fc)
+      issue_record<HD, NW, true>(stage_of(c), rr, c * (STAGE * 2), wave, lane);
+    else
+      issue_chunk<HD, NW, true>(stage_of(c), kr, vr, (c - fc) * KC, capacity, wave, lane);
+  };
+  auto widen = [&](int c, int t, int stride) {
+    if (!RECORDS || c >= fc)
+      widen_chunk<HD, PART>(stage_of(c), t, stride, (c - fc) * KC, total, S, bad);
+    else if (front - c * KC < KC)
+      cut_record<HD>(stage_of(c), t, stride, front - c * KC);
+  };
   const int wt = tid, wstride = NW * 64;   // every wave widens its share
 
   // Prologue: chunks c0 .. c0+NST-2 in flight, chunk c0 widened.
 #pragma unroll
   for (int i = 0; i < NST - 1; ++i)
     if (c0 + i < c1)
-      issue_chunk<HD, NW, true>(stage_of(c0 + i), kr, vr, (c0 + i) * KC, capacity, wave, lane);
+      issue(c0 + i);
   if (c0 < c1) {
     if (c0 + NST - 2 < c1) wait_vmcnt<(NST - 2) * L_DMA>(); else wait_vmcnt<0>();
     lds_barrier();
-    widen_chunk<HD, PART>(stage_of(c0), wt, wstride, c0 * KC, total, S, bad);
+    widen(c0, wt, wstride);
   }
 
   // Fragment offsets (lane registers; blocks add compile-time constants): K row p32(lq)
@@ -716,16 +795,17 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     }
     chunk_barrier();
     if (c + NST - 1 < c1)
-      issue_chunk<HD, NW, true>(stage_of(c + NST - 1), kr, vr, (c + NST - 1) * KC, capacity,
-                                wave, lane);
+      issue(c + NST - 1);
     if (c + 1 < c1)
-      widen_chunk<HD, PART>(stage_of(c + 1), wt, wstride, (c + 1) * KC, total, S, bad);
+      widen(c + 1, wt, wstride);
 
     const uint16_t *st = stage_of(c);
     const f16 *sk = (const f16 *)st;
     const f16 *sv = (const f16 *)(st + KC * HD);
-    const int key0 = c * KC;
-    const bool tree_chunk = key0 + KC > S;
+    // (a record's slots in front of the prefix's end are seen by all, those behind it by none)
+    const bool record = RECORDS && c < fc;
+    const int key0 = record ? 0 : (c - fc) * KC, Sc = record ? front - c * KC : S, n1c = record ? 0 : n1;
+    const bool tree_chunk = key0 + KC > Sc;
     if (t32) {
       // S^T for the chunk's two 32-key blocks: sc[kb][i] is the score of slot
       // key0 + 32 kb + key32_of_score(i, hh) against this lane's query.  Both blocks are
@@ -751,9 +831,9 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
           MASK_BRANCH();
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int j = key0 + kb2 * 32 + key32_of_score(i, hh) - S;  // tree row, or < 0
+            const int j = key0 + kb2 * 32 + key32_of_score(i, hh) - Sc;  // tree row, or < 0
             const int sh = min(max(j - 1, 0), 63);
-            const bool vis = (j < 0) | ((j < n1) & ((j == 0) | (bool)((anc >> sh) & 1ull)));
+            const bool vis = (j < 0) | ((j < n1c) & ((j == 0) | (bool)((anc >> sh) & 1ull)));
             z[i] = vis ? z[i] : -INFINITY;
           }
         }
@@ -806,9 +886,9 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
         MASK_BRANCH();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int j = key0 + key_of_score(qk, lg, e) - S;
+          const int j = key0 + key_of_score(qk, lg, e) - Sc;
           const int sh = min(max(j - 1, 0), 63);
-          const bool vis = (j < 0) | ((j < n1) & ((j == 0) | (bool)((ancq >> sh) & 1ull)));
+          const bool vis = (j < 0) | ((j < n1c) & ((j == 0) | (bool)((ancq >> sh) & 1ull)));
           sq[e] = vis ? sq[e] : -INFINITY;
         }
       }
@@ -1089,21 +1169,44 @@ __global__ __launch_bounds__(256) void tree_attn_f32_kernel(
 // Ring depth: 4 stages of 32 KB (head_dim 128) or 16 KB (head_dim 64).
 template <int HD> struct AttnCfg { static constexpr int NST = 4; };
 
-template <int HD, int NW, int UPW, int NST, bool PART, typename TQ>
+template <int HD, int NW, int UPW, int NST, int MODE, typename TQ>
 void launch_mfma(dim3 grid, hipStream_t s, const TQ *q, const bf16 *ck, const bf16 *cv,
                  const TreeMeta &meta, f16 *out, float *po, float *pml, int n1, int H, int Hkv,
                  int capacity, int nsplit, int tpg, const SharedJoin &join) {
-  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, NST, PART, TQ>), grid,
+  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, NST, MODE, TQ>), grid,
                      dim3(NW * 64), 0, s, q, ck, cv, meta, out, po, pml, n1, H, Hkv,
                      capacity, nsplit, tpg, join);
 }
 
+// Key splits: as many as the CUs hold at once, rounded down, for a second round of a few
+// workgroups costs what the first does (6 sessions of 8 kv heads: six splits, 288
+// workgroups, took 29.2 us, five 24.6; where the items do not divide the CUs some idle).
+// A split is at least 4 chunks, as the merge's launch and its fp32 partials cost about as
+// much as three (16 sessions of 8 kv heads, 300 slots, two splits 27.3 us, whole 21.0),
+// but 2 for up to 32 items, whose few partials cost little, if the chunks' query tiles add
+// up to some work (one session of 1500 slots: 16.2 us against 17.3 at 4 chunks; 65 rows of
+// 8 query heads over 300 slots: 26 against 33 whole).
+int attn_items(int B, int n1, int H, int Hkv) {
+  const int QR = H / Hkv * n1;
+  return B * Hkv * (QR > 256 ? (QR + 271) / 272 : 1);   // (the query groups of launch_tree_attn)
+}
+int attn_splits(int B, int n1, int H, int Hkv, int hd, int nchunks, int cus, long long part_capacity) {
+  const int QR = H / Hkv * n1, all_tiles = (QR + 15) / 16, items = attn_items(B, n1, H, Hkv);
+  int nsplit = cus / items;
+  const int least = items <= 32 && nchunks * all_tiles >= 48 ? 2 : 4;
+  nsplit = nsplit < nchunks / least ? nsplit : nchunks / least;
+  if (nsplit < 1) nsplit = 1;
+  while (nsplit > 1 && (long long)B * Hkv * nsplit * QR * hd > part_capacity) --nsplit;
+  return nsplit;
+}
+
 // The kernels of one layer, without the merge of their splits.
-template <bool PART, typename TQ>
+template <int MODE, typename TQ>
 hipError_t launch_tree_attn(const TQ *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
                             f16 *out, float *part_o, float *part_ml, long long part_capacity, int B,
                             int n1, int H, int Hkv, int hd, int capacity, int cus, hipStream_t s,
                             int *nsplit_used, SharedJoin join) {
+  constexpr bool PART = MODE > 0;
   const int G = H / Hkv, QR = G * n1;
   const int all_tiles = (QR + 15) / 16;
   if (capacity % KC != 0) return hipErrorInvalidValue;
@@ -1115,46 +1218,33 @@ hipError_t launch_tree_attn(const TQ *q, const bf16 *ck, const bf16 *cv, const T
   const bool t32 = all_tiles > 16;
   const int nqg = t32 ? (QR + 271) / 272 : 1;
   const int rpg = (QR + nqg - 1) / nqg;
-  // Key splits: as many as the CUs hold at once, rounded down, for a second round of a few
-  // workgroups costs what the first does (6 sessions of 8 kv heads: six splits, 288
-  // workgroups, took 29.2 us, five 24.6; where the items do not divide the CUs some idle).
-  // A split is at least 4 chunks, as the merge's launch and its fp32 partials cost about as
-  // much as three (16 sessions of 8 kv heads, 300 slots, two splits 27.3 us, whole 21.0),
-  // but 2 for up to 32 items, whose few partials cost little, if the chunks' query tiles add
-  // up to some work (one session of 1500 slots: 16.2 us against 17.3 at 4 chunks; 65 rows of
-  // 8 query heads over 300 slots: 26 against 33 whole).
-  const int slots = cus;
-  const int items = B * Hkv * nqg;
-  const int nchunks = capacity / KC;
-  int nsplit = slots / items;
-  const int least = items <= 32 && nchunks * all_tiles >= 48 ? 2 : 4;
-  nsplit = nsplit < nchunks / least ? nsplit : nchunks / least;
-  if (nsplit < 1) nsplit = 1;
-  while (nsplit > 1 && (long long)B * Hkv * nsplit * QR * hd > part_capacity) --nsplit;
+  const int nsplit = attn_splits(B, n1, H, Hkv, hd,
+                                 capacity / KC + (MODE == 2 ? join.sh.cap / KC : 0), cus,
+                                 part_capacity);
   *nsplit_used = nsplit;
   if (PART && nsplit > 1) join.here = 0;
   const dim3 grid(nsplit * nqg, Hkv, B);
   if (t32) {
     if (hd == 128)
-      hipLaunchKernelGGL((tree_attn_t32_kernel<128, AttnCfg<128>::NST, PART, TQ>), grid, dim3(512), 0, s,
+      hipLaunchKernelGGL((tree_attn_t32_kernel<128, AttnCfg<128>::NST, MODE, TQ>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
                          rpg, join);
     else
-      hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, PART, TQ>), grid, dim3(512), 0, s,
+      hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, MODE, TQ>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
                          rpg, join);
   } else if (PART && all_tiles <= 8) {
     if (hd == 128)
-      launch_mfma<128, 8, 1, 2, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+      launch_mfma<128, 8, 1, 2, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
                                           capacity, nsplit, all_tiles, join);
     else
-      launch_mfma<64, 8, 1, 4, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+      launch_mfma<64, 8, 1, 4, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
                                          capacity, nsplit, all_tiles, join);
   } else if (hd == 128) {
-    launch_mfma<128, 16, 1, 4, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+    launch_mfma<128, 16, 1, 4, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
                                          capacity, nsplit, all_tiles, join);
   } else {
-    launch_mfma<64, 16, 1, 4, PART, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
+    launch_mfma<64, 16, 1, 4, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
                                         capacity, nsplit, all_tiles, join);
   }
   return hipGetLastError();
@@ -1170,7 +1260,7 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
                                   float *part_ml, long long part_capacity, int B, int n1, int H,
                                   int Hkv, int hd, int capacity, int cus, hipStream_t s,
                                   int *nsplit_used) {
-  const hipError_t e = launch_tree_attn<false, f16>(q, ck, cv, meta, out, part_o, part_ml, part_capacity, B,
+  const hipError_t e = launch_tree_attn<0, f16>(q, ck, cv, meta, out, part_o, part_ml, part_capacity, B,
                                                n1, H, Hkv, hd, capacity, cus, s, nsplit_used, SharedJoin{});
   const int nsplit = *nsplit_used;
   if (e != hipSuccess || nsplit == 1) return e;
@@ -1180,13 +1270,21 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
   return hipGetLastError();
 }
 
+int attention_chunks_in_turn(int B, int n1, int H, int Hkv, int hd, int nchunks, int cus,
+                             long long part_capacity) {
+  const int nsplit = attn_splits(B, n1, H, Hkv, hd, nchunks, cus, part_capacity);
+  const int rounds = (attn_items(B, n1, H, Hkv) * nsplit + 2 * cus - 1) / (2 * cus);
+  return rounds * ((nchunks + nsplit - 1) / nsplit);
+}
+
 template <typename TQ>
 hipError_t launch_attention_own(const TQ *q, const bf16 *ck, const bf16 *cv, const TreeMeta &meta,
                                 const SharedJoin &j, float *part_o, float *part_ml,
                                 long long part_capacity, int B, int n1, int H, int Hkv, int hd,
                                 int capacity, int cus, hipStream_t s, int *nsplit) {
-  return launch_tree_attn<true, TQ>(q, ck, cv, meta, nullptr, part_o, part_ml, part_capacity, B, n1, H,
-                                    Hkv, hd, capacity, cus, s, nsplit, j);
+  auto launch = j.blocks ? launch_tree_attn<2, TQ> : launch_tree_attn<1, TQ>;
+  return launch(q, ck, cv, meta, nullptr, part_o, part_ml, part_capacity, B, n1, H, Hkv, hd, capacity, cus,
+                s, nsplit, j);
 }
 template hipError_t launch_attention_own<f16>(const f16 *, const bf16 *, const bf16 *,
                                               const TreeMeta &, const SharedJoin &, float *, float *,

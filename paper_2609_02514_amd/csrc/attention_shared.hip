@@ -19,6 +19,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int TM = acespec::kSharedTile;
+constexpr int DIRECT = 12;
 
 AS_DEVICE float halves_max(float v) {
   auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -332,7 +333,8 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
   if (row >= rows) return;
   const int b = row / n1, r = row - b * n1, G = H / Hkv, g = h / G, QR = G * n1;
   const int qi = r * G + h - g * G;
-  const SharedSession me = j.sm.sessions[b];
+  SharedSession me = j.sm.sessions[b];
+  if (j.blocks) me.place = -1;   // (the parts hold the shared slots too)
   const int4 total = *j.sm.total;
   const size_t item0 = ((size_t)b * Hkv + g) * nsplit * QR + qi;
   const float2 *ml = (const float2 *)part_ml + item0;
@@ -508,16 +510,26 @@ hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const
   // head dims, than the waves over the own slots do (64 single tokens, one tile in 32 parts: 30 + 10
   // us against 88; the 8B batch, 17 tiles in up to three: 45 + 18 against 57).
   const int here = 3LL * rows * (H / Hkv) >= (long long)wgs * TM;
+  // Small batches over short prefixes: the kernel over the own slots takes the records first, each
+  // session for itself, which leaves the tiles' way in and out of memory away.  Up to DIRECT chunks
+  // in turn (8 kv heads of 17 rows each; chunks, so taken, by tiles: 8 sessions behind 2048 slots 9,
+  // 33 us, 39; 64 behind 512 9, 39, 46; 16 behind 2048 17, 51, 44; 32 behind 2048 33, 79, 55).
+  const bool direct = acespec::attention_chunks_in_turn(B, n1, H, Hkv, HD, (sh.cap + capacity) / 64, cus,
+                                                        part_cap) <= DIRECT;
   const SharedJoin j{sh_o, sh_ml, sm, wgs,
-                     acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus), out, rows_out, here};
-  hipLaunchKernelGGL((shared_attn_kernel<HD, 4, TQ>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
-                     sh_o, sh_ml, B, n1, H, Hkv, sh.cap, wgs, j.rows_total);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+                     acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus), out, rows_out,
+                     direct || here, direct ? blocks : nullptr, sh};
+  hipError_t e = hipSuccess;
+  if (!direct) {
+    hipLaunchKernelGGL((shared_attn_kernel<HD, 4, TQ>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
+                       sh_o, sh_ml, B, n1, H, Hkv, sh.cap, wgs, j.rows_total);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   int nsplit = 1;
   e = acespec::launch_attention_own(q, ck, cv, meta, j, part_o, part_ml, part_cap, B, n1, H, Hkv, HD,
                                     capacity, cus, s, &nsplit);
-  if (e != hipSuccess || (here && nsplit == 1)) return e;
+  if (e != hipSuccess || (j.here && nsplit == 1)) return e;
   const long long wg = ((long long)rows * H * (HD / 4) + 255) / 256;
   if (wg > 0xffffffffLL / 256) return hipErrorInvalidValue;
   hipLaunchKernelGGL(shared_combine_kernel<HD>, dim3((unsigned)wg), dim3(256), 0, s, part_o, part_ml, j,

@@ -235,6 +235,8 @@ struct SharedJoin {
   void *out;             // fp16 in the activation layout, or with rows_out bf16, row-major
   int rows_out;
   int here;              // 1: the kernel over the own slots joins them, unless these are split
+  const f16 *blocks;     // this layer's records, if the kernel over the own slots is to go over the
+  SharedArgs sh;         // shared ones too (there are no partial results then), or NULL
 };
 
 // Fixed-point scale for deterministic mass sums in the vocabulary kernel.
@@ -374,6 +376,10 @@ hipError_t launch_attention_own(const TQ *q, const bf16 *cache_k, const bf16 *ca
                                 const TreeMeta &meta, const SharedJoin &j, float *part_o,
                                 float *part_ml, long long part_capacity, int B, int n1, int H,
                                 int Hkv, int hd, int capacity, int cus, hipStream_t s, int *nsplit);
+
+// The 64-slot chunks that launch_attention_own's workgroups, two a CU, go over one after the other.
+int attention_chunks_in_turn(int B, int n1, int H, int Hkv, int hd, int nchunks, int cus,
+                             long long part_capacity);
 
 // One layer's tree attention behind shared prefixes: blocks [P][Hkv][cap / 64] records, own slots
 // ck, cv as in launch_attention.  q is row-major [rows][H hd] in the activation type, out in the

@@ -42,16 +42,19 @@ def random_parents(r, n, reach=7):
     return [-1] + [r.randint(max(0, i - reach), i - 1) for i in range(1, n + 1)]
 
 
-def store(L, held, Hkv, hd, dtype, seed):
+def store(L, held, Hkv, hd, dtype, seed, cap=0):
     """A store of len(held) prefixes, their keys and values [L, P, Hkv, cap, hd] / [.., hd, cap].
-    Behind a prefix's end there is a NaN."""
+    Behind a prefix's end there is a NaN, as in the records of a larger capacity behind all."""
     from paper_2609_02514_amd.acespec import SharedPrefix
-    cap = up64(max(held))
+    more, cap = cap // 64, up64(max(held))
     k, v = random_cache(L, len(held), Hkv, cap, hd, dtype, seed)
     pk, pv = k.clone(), v.clone()
     for p, n in enumerate(held):
         pk[:, p, :, n:], pv[:, p, :, :, n:] = math.nan, math.nan
-    return SharedPrefix(sr.records(pk, pv, F16[dtype]), cap, i32(held)), k, v
+    rec = sr.records(pk, pv, F16[dtype])
+    if more > rec.shape[3]:
+        rec = torch.cat([rec, rec.new_full((*rec.shape[:3], more - rec.shape[3], 128 * hd), math.nan)], 3)
+    return SharedPrefix(rec, rec.shape[3] * 64, i32(held)), k, v
 
 
 # ---- the store ------------------------------------------------------------------------------
@@ -116,6 +119,9 @@ def test_take_overs_that_are_refused_on_the_device_write_nothing(lens, take, cou
             assert bool((shared.blocks[:, p] == 3).all())
 
 
+LARGE = 13 * 64 * 256   # slots: more than 12 chunks in turn for a workgroup on each of 256 CUs
+
+
 # ---- the attention --------------------------------------------------------------------------
 
 
@@ -134,10 +140,11 @@ def bound(dtype, out, mag, big, hd):
     return b + 1e-30
 
 
-def check_attention(dtype, hd, H, Hkv, held, of, mine, N, seed, L=1, layer=0, poison=None, reach=7, cap=None):
+def check_attention(dtype, hd, H, Hkv, held, of, mine, N, seed, L=1, layer=0, poison=None, reach=7, cap=None,
+                    scap=0):
     r, B, n1, P = random.Random(seed), len(of), N + 1, len(held)
     cap = cap or up64(max(mine) + n1)
-    shared, sk, sv = store(L, held, Hkv, hd, dtype, seed)
+    shared, sk, sv = store(L, held, Hkv, hd, dtype, seed, scap)
     k, v = random_cache(L, B, Hkv, cap, hd, dtype, seed + 1)
     ver = verifier(L, B, H, Hkv, hd, dtype, N)
     parents = [random_parents(r, N, reach) for _ in range(B)]
@@ -178,8 +185,12 @@ def check_attention(dtype, hd, H, Hkv, held, of, mine, N, seed, L=1, layer=0, po
     (7, 1, [300, 17], [1, 0, 1, 0, 0, -1], [3, 0, 90, 1, 2, 4], 5),
     (6, 3, [700], [0, 0, 0, 0, 0, 0, 0, 0, 0], [0] * 9, 33),       # nothing of their own
     (2, 2, [5], [-1, -1], [70, 0], 3)])                            # nobody behind the prefix
-def test_attention_against_64_bits(dtype, hd, H, Hkv, held, of, mine, N):
-    check_attention(dtype, hd, H, Hkv, held, of, mine, N, seed=H + N)
+@pytest.mark.parametrize("tiles", [False, True])
+def test_attention_against_64_bits(dtype, hd, H, Hkv, held, of, mine, N, tiles):
+    """tiles: in a store so large that a session's own way over its prefix would take too long."""
+    if tiles and dtype == "f32":
+        pytest.skip("fp32 goes one way")
+    check_attention(dtype, hd, H, Hkv, held, of, mine, N, seed=H + N, scap=LARGE if tiles else 0)
 
 
 @pytest.mark.parametrize("dtype, hd, H, Hkv, held, B, N", [
@@ -198,12 +209,14 @@ def test_attention_of_batches(dtype, hd, H, Hkv, held, B, N):
 
 def test_one_layer_of_several_and_a_larger_cache():
     check_attention("bf16", 128, 8, 2, [100, 70], [1, 0, 1], [10, 20, 30], 4, seed=5, L=3, layer=1, cap=512)
+    check_attention("bf16", 64, 4, 1, [100, 70], [1, 0, 1], [10, 20, 30], 4, seed=5, L=2, layer=1, cap=512, scap=LARGE)
     check_attention("f32", 64, 8, 2, [100, 70], [1, 0, 1], [10, 20, 30], 4, seed=6, L=3, layer=2, cap=320)
 
 
 @pytest.mark.parametrize("reach", [1, 64])
 def test_the_deepest_and_the_widest_trees(reach):
     check_attention("bf16", 128, 8, 2, [333], [0, 0], [100, 64], 64, seed=reach, reach=reach)
+    check_attention("bf16", 128, 8, 2, [333], [0, 0], [100, 64], 64, seed=reach, reach=reach, scap=LARGE)
 
 
 @pytest.mark.parametrize("dtype, hd, H, N", [("bf16", 128, 8, 16), ("bf16", 64, 8, 64), ("f32", 64, 4, 16),
@@ -220,8 +233,11 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, hd, H, N):
         sv[0, 1, 0, 9, 20] = -math.inf              # a shared slot of prefix 1 (sessions 2 and 3)
         pk, pv = sk.clone(), sv.clone()
         pk[:, 1, :, 70:], pv[:, 1, :, :, 70:] = math.nan, math.nan
-        shared.blocks[:, 1] = sr.records(pk, pv, F16[dtype])[:, 1]
-    check_attention(dtype, hd, H, 2, [130, 70], [0, 0, 1, 1, -1], [50, 7, 12, 0, 3], N, seed=9, poison=poison)
+        rec = sr.records(pk, pv, F16[dtype])[:, 1]
+        shared.blocks[:, 1, :, :rec.shape[2]] = rec
+    for scap in (0, LARGE):
+        check_attention(dtype, hd, H, 2, [130, 70], [0, 0, 1, 1, -1], [50, 7, 12, 0, 3], N, seed=9, poison=poison,
+                        scap=scap)
 
 
 def test_malformed_sessions_are_flagged_and_the_others_unharmed():
@@ -261,10 +277,12 @@ def test_large_scores_and_far_apart_references():
 
     def poison(shared, sk, sv, k, v, parents):
         sk *= torch.linspace(-3, 3, sk.shape[3], device="cuda").view(1, 1, 1, -1, 1).to(sk.dtype) * 8
-        shared.blocks.copy_(sr.records(sk, sv, True))
+        rec = sr.records(sk, sv, True)
+        shared.blocks[:, :, :, :rec.shape[3]] = rec
         k[:, 0] *= 30
         k[:, 1] *= 0.01
-    check_attention("bf16", hd, H, Hkv, [n], [0, 0, 0], [10, 64, 0], N, seed=21, poison=poison, reach=1)
+    for scap in (0, LARGE):
+        check_attention("bf16", hd, H, Hkv, [n], [0, 0, 0], [10, 64, 0], N, seed=21, poison=poison, reach=1, scap=scap)
 
 
 def test_offsets_beyond_32_bits():
@@ -653,9 +671,9 @@ def test_a_captured_run_replays_between_other_calls():
 
 
 def test_a_call_repeats_bit_for_bit():
-    a = check_attention("bf16", 128, 16, 2, [1000, 300], [0, 1, 0, 0, 1, 0, 0], [5, 9, 100, 3, 0, 7, 64], 16, seed=2)
-    b = check_attention("bf16", 128, 16, 2, [1000, 300], [0, 1, 0, 0, 1, 0, 0], [5, 9, 100, 3, 0, 7, 64], 16, seed=2)
-    assert torch.equal(a, b)
+    for scap in (0, LARGE):
+        args = ("bf16", 128, 16, 2, [1000, 300], [0, 1, 0, 0, 1, 0, 0], [5, 9, 100, 3, 0, 7, 64], 16)
+        assert torch.equal(check_attention(*args, seed=2, scap=scap), check_attention(*args, seed=2, scap=scap))
 
 
 def test_wrong_tensors_are_refused():
