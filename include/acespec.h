@@ -413,7 +413,8 @@ typedef struct {
 } acespec_qk_norm;
 
 /* The calls of this section take arrays that are 16-byte aligned (the caches, blocks, q, qkv, out)
- * and, for what one of them writes, apart from everything else that it is given (ACESPEC_EINVAL).
+ * and, for what one of them writes, apart from everything else that it is given (ACESPEC_EINVAL;
+ * weights aside), for at most 65535 sessions with trees.
  * prefix_of [B] DEVICE: the prefix that session b stands behind, or -1.  Any number of sessions may
  * stand behind one, in any order.  status[b] is ACESPEC_EBADTREE for a malformed tree, a prefix_of
  * outside [-1, prefixes), a len outside [0, capacity] or a prefix_len that leaves no room. */

@@ -653,6 +653,8 @@ int check_layer(const acespec_ctx *ctx, const acespec_kv_shared *sh, const int32
   int rc = check_batch(ctx, B, N);
   if (!rc) rc = check_cache(d, kv, N + 1, "kv");
   if (rc) return rc;
+  if (B > 65535 || d.n_kv_heads > 65535)   // (a dimension of the grids)
+    return fail(ACESPEC_EUNSUPPORTED, "more than 65535 sessions or kv heads");
   if ((sh != nullptr) != (prefix_of != nullptr))
     return fail(ACESPEC_EINVAL, "shared prefixes and prefix_of come together (one of them is NULL)");
   if (!sh && may) return ACESPEC_OK;
@@ -1217,13 +1219,13 @@ int acespec_qk_norm_rope(acespec_ctx *ctx, const acespec_qk_norm *norm, const ac
   if (!norm || !qkv || !q || !status) return fail(ACESPEC_EINVAL, "a required pointer is NULL");
   if (((uintptr_t)qkv | (uintptr_t)q | (uintptr_t)norm->q_gain | (uintptr_t)norm->k_gain) & 15)
     return fail(ACESPEC_EINVAL, "qkv, q and the gains must be 16-byte aligned");
-  if (B > 65535) return fail(ACESPEC_EUNSUPPORTED, "more than 65535 sessions");
   const acespec_model_desc &d = ctx->d;
   const int n1 = N + 1, H = d.n_heads, Hkv = d.n_kv_heads, hd = d.head_dim;
   const size_t row = (size_t)B * n1 * hd * ctx->esz, held = cache_bytes(d, kv->capacity, B);
   const size_t each = (size_t)B * sizeof(int32_t), gain = hd * ctx->esz;
   rc = check_apart({{"q_gain", norm->q_gain, gain, false},
                     {"k_gain", norm->k_gain, gain, false},
+                    {"blocks", sh ? sh->blocks : nullptr, sh ? shared_bytes(d, sh) : 0, false},
                     {"len", sh ? sh->len : nullptr, sh ? (size_t)sh->prefixes * sizeof(int32_t) : 0, false},
                     {"prefix_of", prefix_of, each, false},
                     {"k", kv->k, held, true},
@@ -1268,12 +1270,43 @@ int acespec_verify_tree_shared(acespec_ctx *ctx, const acespec_weights *w,
   for (int l = 0; norms && l < d.n_layers; ++l)
     if (((uintptr_t)norms[l].q_gain | (uintptr_t)norms[l].k_gain) & 15)
       return fail(ACESPEC_EINVAL, "the gains must be 16-byte aligned (layer %d)", l);
-  if (norms && B > 65535) return fail(ACESPEC_EUNSUPPORTED, "more than 65535 sessions");
-  if (sh) {
-    const int apart = check_apart({{"blocks", sh->blocks, shared_bytes(d, sh), false},
-                                   {"k", kv->k, held, true},
-                                   {"v", kv->v, held, true}});
-    if (apart) return apart;
+  if (w && p && o) {   // (their absence is refused below)
+    const size_t rows = (size_t)B * (N + 1), each = (size_t)B * 4, top = rows * 4 * (p->top_k > 0 ? p->top_k : 0);
+    const Array written[] = {{"k", kv->k, held, true},
+                             {"v", kv->v, held, true},
+                             {"accept", o->accept, rows, true},
+                             {"acc_prefix_len", o->acc_prefix_len, rows * 4, true},
+                             {"resample_token", o->resample_token, rows * 4, true},
+                             {"bonus_token", o->bonus_token, rows * 4, true},
+                             {"topk_ids", o->topk_ids, top, true},
+                             {"topk_probs", o->topk_probs, top, true},
+                             {"path", o->path, rows * 4, true},
+                             {"path_len", o->path_len, each, true},
+                             {"next_token", o->next_token, each, true},
+                             {"sibling_hit", o->sibling_hit, (size_t)B, true},
+                             {"status", o->status, each, true},
+                             {"logits_out", o->logits_out, rows * d.vocab * 4, true}};
+    const Array read[] = {{"blocks", sh ? sh->blocks : nullptr, sh ? shared_bytes(d, sh) : 0, false},
+                          {"len", sh ? sh->len : nullptr, sh ? (size_t)sh->prefixes * 4 : 0, false},
+                          {"prefix_of", prefix_of, each, false},
+                          {"prefix_len", kv->prefix_len, each, false},
+                          {"tree_tokens", tree_tokens, rows * 4, false},
+                          {"parent_idx", parent_idx, rows * 4, false},
+                          {"draft_q", draft_q, rows * d.vocab * 4, false},
+                          {"q_hat", q_hat, rows * 4, false},
+                          {"uniforms", uniforms, rows * 12, false}};
+    const size_t gain = d.head_dim * ctx->esz;
+    for (const Array *a = written; a != std::end(written); ++a) {
+      int apart = ACESPEC_OK;
+      for (const Array &b : read)
+        if (!apart) apart = check_apart({*a, b});
+      for (const Array *b = written; b != a && !apart; ++b) apart = check_apart({*b, *a});
+      for (int l = 0; norms && l < d.n_layers && !apart; ++l) {
+        apart = check_apart({*a, {"a q_gain", norms[l].q_gain, gain, false}});
+        if (!apart) apart = check_apart({*a, {"a k_gain", norms[l].k_gain, gain, false}});
+      }
+      if (apart) return apart;
+    }
   }
   return verify_tree_checked(ctx, w, kv, nullptr, nullptr, tree_tokens, parent_idx, draft_q, q_hat,
                              uniforms, B, N, p, o, stream, norms, sh, prefix_of);

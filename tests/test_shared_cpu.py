@@ -168,3 +168,42 @@ def test_what_a_call_writes_lies_apart():
     refused(fork(ctx, src=cache(), dst=cache(capacity=64)), "overlap")
     refused(fork(ctx, src=cache(), dst=cache(), Bd=3), "overlap")
     refused(fork(ctx, src=cache(), dst=cache(v=far[1])), "overlap")
+
+
+def step(ctx, outs=None, norms=None, sh=None, **at):
+    """The whole step with every array in a place of its own but those that `at` and `outs` name."""
+    places = dict(of=FAR + 2 * G, tokens=FAR + 30 * G, parents=FAR + 31 * G, q=FAR + 32 * G, uniforms=FAR + 40 * G)
+    places.update(at)
+    where = [FAR + (50 + i) * G for i in range(11)] + [None]
+    for i, p in (outs or {}).items():
+        where[i] = p
+    layers = (A.LayerWeights * 2)(*[A.LayerWeights(P, P, P, P, P, P)] * 2)
+    return A.load().acespec_verify_tree_shared(
+        ctx, C.byref(A.Weights(P, layers, P, P, 0)), norms, ref(shared() if sh is None else sh), places["of"], ref(cache()),
+        places["tokens"], places["parents"], places["q"], None, places["uniforms"], 4, 16, C.byref(A.Params(0.8, 0.9, 8)),
+        C.byref(A.Outputs(*where)), None)
+
+
+@pytest.mark.parametrize("field", range(12))
+def test_what_a_step_writes_lies_apart(field):
+    ctx, kv, sh = Ctx().ptr, cache(), shared()
+    norms = (A.QKNorm * 2)(A.QKNorm(FAR + 70 * G, None), A.QKNorm(None, FAR + 71 * G))
+    for at in (sh.blocks, sh.len, FAR + 2 * G, kv.k, kv.v, kv.prefix_len, FAR + 30 * G, FAR + 31 * G, FAR + 32 * G,
+               FAR + 40 * G, FAR + 70 * G, FAR + 71 * G, FAR + (50 + (field + 1) % 11) * G):
+        refused(step(ctx, {field: at}, norms), "overlap")
+
+
+def test_the_caches_of_a_step_lie_apart():
+    ctx, kv = Ctx().ptr, cache()
+    for at in (kv.k, kv.v):
+        for name in ("of", "tokens", "parents", "q", "uniforms"):
+            refused(step(ctx, **{name: at}), "overlap")
+        refused(step(ctx, sh=shared(length=at)), "overlap")
+        refused(step(ctx, norms=(A.QKNorm * 2)(A.QKNorm(None, None), A.QKNorm(at, None))), "overlap")
+        refused(rotate(ctx, sh=shared(blocks=at)), "overlap")
+
+
+def test_more_sessions_than_a_grid_takes():
+    ctx = Ctx(max_batch=70000).ptr
+    for call in (attention, rotate, verify):
+        refused(call(ctx, B=65536), "65535", A.ACESPEC_EUNSUPPORTED)
