@@ -189,6 +189,7 @@ AS_DEVICE void group_many(int B, int QR, const SharedArgs &sh, int tile_rows, co
     }
     for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
     if (tid == 0) *sm.total = make_int4(units, count, tiles, most);
+    __threadfence_block();   // (the entries were moved by other lanes)
     // and its members learn what lies before their group
     for (int x = tid; x < grouped; x += 64) {
       int lo = 0, hi = count - 1;   // the last group that begins at place x or before
