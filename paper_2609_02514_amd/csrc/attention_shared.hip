@@ -40,6 +40,9 @@ AS_DEVICE int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // A value is computed where this stands, not where it is used.
 #define PIN(x) __asm__ volatile("" : "+v"(x))
 
+AS_DEVICE f16x8 to_f16x8(f16x8 v) { return v; }
+AS_DEVICE f16x8 to_f16x8(bf16x8 v) { return bf16x8_to_f16x8(v); }
+
 AS_DEVICE void block_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Eight waves, 32 query rows each, over one record after the other.  A record is 1 KB operands of
@@ -53,9 +56,9 @@ AS_DEVICE void block_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_bar
 // two waves share a SIMD.  The halves are therefore pipelined: while the weights of one half are
 // computed, the scores of the next and the product with the values of the one before run, which
 // depend on none of it.
-template <int HD, int NST, typename QT>
+template <int HD, int NST, typename TQ>
 __global__ __launch_bounds__(512) void shared_attn_kernel(
-    const QT *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
+    const TQ *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
     float *__restrict__ part_o, float *__restrict__ part_ml, int B, int n1, int H, int Hkv, int cap,
     int wgs, long long rows_total) {
   constexpr int KS = HD / 16, NDB = HD / 32;
@@ -118,15 +121,25 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
                   i * (REC * 2) + piece * 1024);
       }
     };
+    // the first record is on its way while the queries are looked up
+    block_barrier();      // (the last tile's stages are free)
+    issue(c0);
     // queries: rows of padding multiply zeros
     f16x8 qf[KS];
     {
       const int rr = min(row, rows - 1), m = rr / QR, rem = rr - m * QR, r = rem / G;
-      const QT *qp = q + ((size_t)sm.order[first + m] * n1 + r) * H * HD +
+      const TQ *qp = q + ((size_t)sm.order[first + m] * n1 + r) * H * HD +
                      (g * G + rem - r * G) * HD + hh * 8;
+      typedef TQ q8 __attribute__((ext_vector_type(8)));
+      q8 raw[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) raw[s] = *(const q8 *)(qp + s * 16);
+#pragma unroll
+      for (int i = 1; i < NST - 1; ++i)
+        if (c0 + i < c1) issue(c0 + i);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const f16x8 v = load_f16x8(qp + s * 16);
+        const f16x8 v = to_f16x8(raw[s]);
         qf[s] = row < rows ? v : f16x8{};
       }
     }
@@ -262,10 +275,6 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
       take(zc, pc, rs);
     };
 
-    block_barrier();      // the last tile's stages are free
-#pragma unroll
-    for (int i = 0; i < NST - 1; ++i)
-      if (c0 + i < c1) issue(c0 + i);
     if (c0 + 2 < c1) wait_vmcnt<2 * L_DMA>(); else wait_vmcnt<0>();
     block_barrier();      // record c0 is there
     f32x16 za, zb;        // scores of the record's halves
