@@ -327,40 +327,66 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
 }
 
 // A row's partial results joined where its session was split: of its tile over the shared prefix,
-// and of the parts of its own slots.  One thread per four head dims.
-template <int HD>
+// and of the parts of its own slots.  A thread takes four head dims of every JOIN-th part: few rows
+// have many parts, and one thread for all of them leaves too few loads under way (4: one token behind
+// 8192 slots 25.2 -> 21.1 us, 32 behind 2048 36.2 -> 34.3, 64 behind 8192 61.6 -> 60.8), which many
+// rows do by themselves (8 sessions of 17 rows 28.2 -> 29.7, 256 single tokens 136 -> 143; so from
+// 256 threads a CU on JOIN is 1).
+template <int HD, int JOIN>
 __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__restrict__ part_o,
                                                              const float *__restrict__ part_ml,
                                                              SharedJoin j, TreeMeta meta,
                                                              const bf16 *__restrict__ cv,
                                                              int capacity, int rows, int n1, int H,
                                                              int Hkv, int nsplit) {
-  const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int d = (int)(idx % (HD / 4)) * 4;
-  const long long rh = idx / (HD / 4);
+  constexpr int TD = HD / 4, RPW = 256 / (TD * JOIN);   // threads of a part, rows of a workgroup
+  __shared__ f32x4 s_o[RPW][JOIN][TD];
+  __shared__ float2 s_ml[RPW][JOIN];
+  const int piece = threadIdx.x % TD, d = piece * 4, k = threadIdx.x / TD % JOIN, x = threadIdx.x / (TD * JOIN);
+  const long long rh = min((long long)blockIdx.x * RPW + x, (long long)rows * H - 1);
   const int row = (int)(rh / H), h = (int)(rh - (long long)row * H);
-  if (row >= rows) return;
   const int b = row / n1, r = row - b * n1, G = H / Hkv, g = h / G, QR = G * n1;
   const int qi = r * G + h - g * G;
   SharedSession me = j.sm.sessions[b];
   if (j.blocks) me.place = -1;   // (the parts hold the shared slots too)
   const int4 total = *j.sm.total;
+  const SharedParts p = shared_parts<HD>(j, me, total, g, qi, QR);
   const size_t item0 = ((size_t)b * Hkv + g) * nsplit * QR + qi;
   const float2 *ml = (const float2 *)part_ml + item0;
   const float *po = part_o + item0 * HD + d;
+  constexpr size_t ON = acespec::kSharedTile;
   float M = -INFINITY;
 #pragma unroll 4
-  for (int s = 0; s < nsplit; ++s) M = fmaxf(M, ml[(size_t)s * QR].x);
-  const float top = M == -INFINITY ? 0.f : M;
+  for (int s = k; s < nsplit; s += JOIN) M = fmaxf(M, ml[(size_t)s * QR].x);
+#pragma unroll 8
+  for (int s = k; s < p.parts; s += JOIN) M = fmaxf(M, p.ml[s * ON].x);
+  float top = M == -INFINITY ? 0.f : M;
   f32x4 o[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
   float l = 0.f;
+  auto add = [&](float2 e, f32x4 v) {   // (a part without slots: weight 2^-inf, zero sums)
+    const float w = __builtin_amdgcn_exp2f(e.x - top);
+    l += w * e.y;
+    o[0] += w * v;
+  };
 #pragma unroll 4
-  for (int s = 0; s < nsplit; ++s) {
-    const float2 e = ml[(size_t)s * QR];   // (a part without slots: weight 2^-inf, zero sums)
-    const float x = __builtin_amdgcn_exp2f(e.x - top);
-    l += x * e.y;
-    o[0] += x * *(const f32x4 *)(po + (size_t)s * QR * HD);
+  for (int s = k; s < nsplit; s += JOIN) add(ml[(size_t)s * QR], *(const f32x4 *)(po + (size_t)s * QR * HD));
+#pragma unroll 8
+  for (int s = k; s < p.parts; s += JOIN) add(p.ml[s * ON], *(const f32x4 *)(p.o + s * ON * HD + d));
+  if constexpr (JOIN > 1) {
+    s_o[x][k][piece] = o[0];
+    if (piece == 0) s_ml[x][k] = make_float2(M, l);
+    __syncthreads();
+    M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < JOIN; ++i) M = fmaxf(M, s_ml[x][i].x);
+    top = M == -INFINITY ? 0.f : M;
+    o[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < JOIN; ++i) add(s_ml[x][i], s_o[x][i][piece]);
   }
+  if (k > 0 || (long long)blockIdx.x * RPW + x > rh) return;
+  me.place = -1;   // (its parts are in)
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity + meta.sess_S[b];
   shared_finish<HD>(j, me, total, meta, vb, capacity, j.sm.bad + ((size_t)b * Hkv + g) * 3, b, g, qi, n1, H, Hkv,
                     rows, M, l, o, [&](int) { return d; });
@@ -539,10 +565,13 @@ hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const
   e = acespec::launch_attention_own(q, ck, cv, meta, j, part_o, part_ml, part_cap, B, n1, H, Hkv, HD,
                                     capacity, cus, s, &nsplit);
   if (e != hipSuccess || (j.here && nsplit == 1)) return e;
-  const long long wg = ((long long)rows * H * (HD / 4) + 255) / 256;
+  const long long threads = (long long)rows * H * (HD / 4);
+  const bool few = threads <= 256LL * cus;
+  const long long wg = (threads * (few ? 4 : 1) + 255) / 256;
   if (wg > 0xffffffffLL / 256) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(shared_combine_kernel<HD>, dim3((unsigned)wg), dim3(256), 0, s, part_o, part_ml, j,
-                     meta, cv, capacity, rows, n1, H, Hkv, nsplit);
+  auto kernel = few ? shared_combine_kernel<HD, 4> : shared_combine_kernel<HD, 1>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wg), dim3(256), 0, s, part_o, part_ml, j, meta, cv, capacity, rows, n1,
+                     H, Hkv, nsplit);
   return hipGetLastError();
 }
 

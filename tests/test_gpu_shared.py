@@ -207,6 +207,40 @@ def test_attention_of_batches(dtype, hd, H, Hkv, held, B, N):
     check_attention(dtype, hd, H, Hkv, held, of, [r.randint(0, 200) for _ in range(B)], N, seed=B + N)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("G, N", [(1, 0), (2, 0), (3, 0), (4, 0), (5, 0), (7, 0), (8, 0), (9, 0), (1, 7), (4, 1), (3, 1),
+                                  (2, 3), (2, 2), (1, 8)])
+@pytest.mark.parametrize("scap", [0, LARGE])
+def test_few_rows(hd, G, N, scap):
+    """Up to 8 query rows a kv head and the first sizes beyond, with own slots that one workgroup goes
+    over and with ones that several share, behind prefixes of every length within a record."""
+    check_attention("bf16", hd, 2 * G, 2, [200, 33, 63], [0, 1, 2, -1, 0, 1], [0, 31, 32, 33, 600, 1], N, seed=G + N, scap=scap)
+    check_attention("bf16", hd, G, 1, [97], [0], [500], N, seed=G + N, scap=scap)
+    r = random.Random(G + N)
+    check_attention("bf16", hd, 4 * G, 4, [1030], [0] * 70, [r.randint(0, 100) for _ in range(70)], N, seed=G + N, scap=scap)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("cap", [128, 4096])
+@pytest.mark.parametrize("scap", [0, LARGE])
+def test_what_few_rows_do_not_see_does_not_reach_them(hd, cap, scap):
+    """As below, with 8 rows a kv head; cap 4096: own slots shared by several workgroups."""
+    def poison(shared, sk, sv, k, v, parents):
+        parents[0][:] = [-1, 0, 1, 1]
+        parents[1][:] = [-1, 0, 0, 2]
+        v[0, 0, 0, 3, 53] = math.nan                # row 3: nobody's ancestor
+        v[0, 0, 1, 5, 51] = math.inf                # row 1: of rows 2 and 3
+        k[0, 1, 0, 7 + 2, 2] = math.nan             # row 2: of row 3
+        v[0, 2, 1, 1, 4] = math.inf                 # an own slot, seen by all rows of session 2
+        sv[0, 1, 0, 9, 20] = -math.inf              # a shared slot of prefix 1 (sessions 2 and 3)
+        pk, pv = sk.clone(), sv.clone()
+        pk[:, 1, :, 70:], pv[:, 1, :, :, 70:] = math.nan, math.nan
+        rec = sr.records(pk, pv, True)[:, 1]
+        shared.blocks[:, 1, :, :rec.shape[2]] = rec
+    check_attention("bf16", hd, 4, 2, [130, 70], [0, 0, 1, 1, -1], [50, 7, 12, 0, 3], 3, seed=9, poison=poison, cap=cap,
+                    scap=scap)
+
+
 def test_one_layer_of_several_and_a_larger_cache():
     check_attention("bf16", 128, 8, 2, [100, 70], [1, 0, 1], [10, 20, 30], 4, seed=5, L=3, layer=1, cap=512)
     check_attention("bf16", 64, 4, 1, [100, 70], [1, 0, 1], [10, 20, 30], 4, seed=5, L=2, layer=1, cap=512, scap=LARGE)
