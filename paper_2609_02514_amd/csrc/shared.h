@@ -11,17 +11,20 @@
 //  * every tile into the same number of pieces, which is taken where the longest of these is
 //    shorter than an even piece and the price of a second tile in it (six records: eight sessions of
 //    17 rows behind 2000 slots, three tiles, 44 us evenly cut and 37 tile by tile).
-// A piece has two records at least.
+// A piece has LEAST records at least, fewer only where an even cut leaves a tile's end: short pieces
+// finish sooner, but each leaves its rows' results to be written and read (64 single tokens behind
+// 8192 slots: 61.0 us at two records, 58.1 at four, 59.6 at eight; 32 behind 2048 34.9, 35.3 and 38.0).
 struct SharedLine {
+  static constexpr int LEAST = 4;
   int n, each, more;   // workgroups; evenly: records of each, and one more for the first `more`
   int pieces;          // of a tile, or 0: evenly
   // total: units, -, tiles, most records of a tile
   AS_DEVICE SharedLine(int4 total, int wgs) {
     const int units = total.x, tiles = total.z;
-    n = min(max((units + 1) / 2, tiles), wgs);
+    n = min(max((units + LEAST - 1) / LEAST, tiles), wgs);
     each = n > 0 ? units / n : 0;
     more = units - n * each;
-    pieces = tiles > 0 && tiles <= wgs ? min(wgs / tiles, (total.w + 1) / 2) : 0;
+    pieces = tiles > 0 && tiles <= wgs ? min(wgs / tiles, (total.w + LEAST - 1) / LEAST) : 0;
     if (pieces && (total.w + pieces - 1) / pieces <= each + 6)
       n = tiles * pieces;
     else

@@ -16,8 +16,8 @@ constexpr int TP_THREADS = 128;  // one thread per tree row (at most 65 rows)
 
 // One workgroup per session.  A row's ancestor mask is its own bit and its ancestors'
 // (the root carries none); it is built by pointer jumping, every row doubling the span of
-// ancestors it has folded in per round (7 rounds cover 65 rows), and the row's depth is
-// the mask's population count.
+// ancestors it has folded in per round until the span covers n1 rows (7 rounds for 65), and the
+// row's depth is the mask's population count.
 // tokens may be NULL.  front: positions before the prefix (-1: a shared prefix that is not one).
 template <bool QUANT>
 AS_DEVICE void prepare_tree(int b, const int32_t *__restrict__ tokens,
@@ -43,7 +43,7 @@ AS_DEVICE void prepare_tree(int b, const int32_t *__restrict__ tokens,
   const int p = !in || r == 0 ? -1 : (ok ? pr : r - 1);  // malformed trees become a chain
   s_jump[r] = p < 0 ? 0 : p;
   s_anc[r] = (in && r > 0) ? (1ull << (r - 1)) : 0ull;
-  for (int round = 0; round < 7; ++round) {
+  for (int span = 1; span < n1; span *= 2) {
     __syncthreads();
     const int jr = s_jump[r];
     const uint64_t a = s_anc[r] | s_anc[jr];
@@ -56,9 +56,10 @@ AS_DEVICE void prepare_tree(int b, const int32_t *__restrict__ tokens,
     meta.sess_S[b] = QUANT ? S & 31 : S;
     status[b] = ok ? ACESPEC_OK : ACESPEC_EBADTREE;
   }
-  if (!in) return;
   uint64_t anc = s_anc[r];
   const int depth = __popcll(anc);
+  if (QUANT) __syncthreads();   // (other rows' sets are read)
+  if (!in) return;
   if (QUANT && window > 0)
     for (uint64_t rest = anc; rest; rest &= rest - 1) {
       const int j = __builtin_ctzll(rest) + 1, dj = __popcll(s_anc[j]);
