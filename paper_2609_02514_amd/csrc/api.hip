@@ -214,7 +214,7 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
                                        o->status, stream));
   else if (kv.shared)
     RUN(K_TREE, launch_tree_prep_shared(tokens, parents, kv.prefix_len, B, n1, V, cap, sh, H / Hkv,
-                                        Hkv, kSharedTile, meta, ctx->shm, o->status, stream));
+                                        kSharedTile, meta, ctx->shm, o->status, stream));
   else
     RUN(K_TREE, launch_tree_prep(tokens, parents, kv.prefix_len, B, n1, V, cap, meta, o->status,
                                  stream));
@@ -248,7 +248,7 @@ int verify_tree_impl(acespec_ctx *ctx, const acespec_weights *w, const CacheView
     else if (kv.shared)
       RUN(K_ATTN, launch_attention_shared<T>(
                       x_q, (const A *)kv.shared->blocks + l * shared_layer_elems(d, kv.shared), sh,
-                      ctx->shm, ck, cv, meta, x_attn, 0, ctx->sh_o, ctx->sh_ml, ctx->part_o,
+                      ctx->shm, TreeArgs{}, ck, cv, meta, x_attn, 0, ctx->sh_o, ctx->sh_ml, ctx->part_o,
                       ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd, cap, ctx->cus, stream));
     else
       RUN(K_ATTN, launch_attention<T>(x_q, ck, cv, meta, x_attn, ctx->part_o, ctx->part_ml,
@@ -465,7 +465,7 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
       {shr * d.head_dim * 4, &p_so}, {shr * 2 * 4, &p_sml},
       {each * sizeof(SharedSession), &p_sess}, {each * 4, &p_order}, {each * sizeof(SharedGroup), &p_groups},
       {layers ? 16u : 0u, &p_total},
-      {layers ? each * d.n_kv_heads * 12 : 0, &p_bad}};
+      {layers ? (each * d.n_kv_heads + c->cus) * 12 : 0, &p_bad}};
   size_t total = 0;
   for (auto &pt : parts) total += align_up(pt.bytes);
   if (hipMalloc(&c->ws, total) != hipSuccess) {
@@ -1191,18 +1191,16 @@ int acespec_attention_shared(acespec_ctx *ctx, const acespec_kv_shared *sh, cons
   const SharedArgs sa = shared_args(sh, prefix_of);
   const size_t own = (size_t)layer * B * Hkv * kv->capacity * hd;
   const size_t rec = layer * shared_layer_elems(d, sh);
-  RUN(K_TREE, launch_tree_prep_shared(nullptr, parent_idx, kv->prefix_len, B, n1, d.vocab,
-                                      kv->capacity, sa, H / Hkv, Hkv, kSharedTile, ctx->meta, ctx->shm,
-                                      status, stream));
+  const TreeArgs trees{parent_idx, kv->prefix_len, status};
   if (d.dtype == ACESPEC_BF16)
     RUN(K_ATTN, launch_attention_shared<bf16>(
-                    q, (const f16 *)sh->blocks + rec, sa, ctx->shm,
+                    q, (const f16 *)sh->blocks + rec, sa, ctx->shm, trees,
                     (const bf16 *)kv->k + own, (const bf16 *)kv->v + own, ctx->meta, out, 1, ctx->sh_o,
                     ctx->sh_ml, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv, hd,
                     kv->capacity, ctx->cus, stream));
   else
     RUN(K_ATTN, launch_attention_shared<float>(
-                    q, (const float *)sh->blocks + rec, sa, ctx->shm,
+                    q, (const float *)sh->blocks + rec, sa, ctx->shm, trees,
                     (const float *)kv->k + own, (const float *)kv->v + own, ctx->meta, out, 1,
                     ctx->sh_o, ctx->sh_ml, ctx->part_o, ctx->part_ml, ctx->part_cap, B, n1, H, Hkv,
                     hd, kv->capacity, ctx->cus, stream));

@@ -220,6 +220,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   // MODE 0: the verify pass; 1: own slots behind a shared prefix, joined with its partial results or
   // left as some; 2: its records first, then the own slots
   constexpr bool PART = MODE > 0, RECORDS = MODE == 2;
+  constexpr bool TREES = RECORDS && std::is_same<TQ, bf16>::value;   // (a call of the attention alone)
   constexpr int KSTEPS = HD / 32, NB = HD / 16;
   constexpr int STAGE = 2 * KC * HD;     // elements: K [KC][HD], then V^T [HD][KC]
   constexpr int L_DMA = HD / 4 / NW;     // DMA instructions per wave per chunk
@@ -253,19 +254,24 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
   SharedSession me{};          // (asked for here, well before the join needs it)
   int4 total_units{};
-  if (PART && (RECORDS || join.here)) {
+  if (PART && !TREES && (RECORDS || join.here)) {
     me = join.sm.sessions[b];
     total_units = *join.sm.total;
   }
+  __shared__ TreeSets sets[1];
+  TreeSession session{};
+  if constexpr (TREES)
+    session = tree_session(sets[0], join.trees, join.sh, b, n1, capacity, blockIdx.x == 0 && g == 0, meta);
   // chunks of the session's shared prefix, in front of its own, if they are taken here
-  const int front = RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
+  const int front = TREES ? session.front : RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
   const int fc = RECORDS ? (front + KC - 1) / KC : 0;
   const size_t plane = RECORDS && fc > 0 ? (size_t)join.sh.cap * 2 * HD : 0;
-  const int prefix = RECORDS && fc > 0 ? __builtin_amdgcn_readfirstlane(join.sh.of[b]) : 0;
+  const int prefix = TREES ? session.prefix : RECORDS && fc > 0 ? __builtin_amdgcn_readfirstlane(join.sh.of[b]) : 0;
   const __amdgpu_buffer_rsrc_t rr = make_rsrc(join.blocks + ((size_t)prefix * Hkv + g) * plane,
                                               (uint32_t)(plane * 2));
   if (RECORDS) me.place = -1;   // nothing to join
-  const int S = meta.sess_S[b];
+  const int S = TREES ? session.S : meta.sess_S[b];
+  const uint64_t *ancs = TREES ? sets[0].anc : meta.anc + (size_t)b * n1;
   const int total = S + n1;
   const int nchunks = fc + (total + KC - 1) / KC;
   const int cps = (nchunks + nsplit - 1) / nsplit;
@@ -301,7 +307,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
       const f16x8 v = load_f16x8(qp + s * 32 + lg * 8);
       qf[t][s] = pad ? f16x8{} : v;
     }
-    anc[t] = meta.anc[row0 + r];
+    anc[t] = ancs[r];
     m_run[t] = -INFINITY;
     l_run[t] = 0.f;
 #pragma unroll
@@ -495,7 +501,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   wait_vmcnt<0>();
   if (PART) {
     __syncthreads();   // the marks are complete
-    if (!join.here && tid < 3 && bad[tid]) atomicOr(join.sm.bad + ((size_t)b * Hkv + g) * 3 + tid, bad[tid]);
+    if (!join.here && tid < 3) join.sm.bad[(((size_t)b * Hkv + g) * nsplit + split) * 3 + tid] = bad[tid];
   }
   const bf16 *vtree = vb + S;   // the tree's values
 
@@ -575,7 +581,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
     if (qi >= QR) continue;
     const int r = qi / G, h = g * G + (qi - r * G);
     if (PART && join.here) {
-      shared_finish<HD>(join, me, total_units, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
+      shared_finish<HD>(join, me, total_units, ancs, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
                         m_run[t] == -INFINITY ? -INFINITY : m_run[t] * sscale, l, o[t],
                         [&](int nb) { return nb * 16 + lg * 4; });
     } else if (!PART && nsplit == 1) {
@@ -644,6 +650,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
     float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int rpg,
     SharedJoin join) {
   constexpr bool PART = MODE > 0, RECORDS = MODE == 2;
+  constexpr bool TREES = RECORDS && std::is_same<TQ, bf16>::value;   // (a call of the attention alone)
   constexpr int NW = 8;
   constexpr int KS16 = HD / 16;   // 16-dim k-steps of a 32-row tile's S^T
   constexpr int NDB = HD / 32;    // 32-dim blocks of its O^T
@@ -674,19 +681,24 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
   SharedSession me{};          // (asked for here, well before the join needs it)
   int4 total_units{};
-  if (PART && (RECORDS || join.here)) {
+  if (PART && !TREES && (RECORDS || join.here)) {
     me = join.sm.sessions[b];
     total_units = *join.sm.total;
   }
+  __shared__ TreeSets sets[1];
+  TreeSession session{};
+  if constexpr (TREES)
+    session = tree_session(sets[0], join.trees, join.sh, b, n1, capacity, blockIdx.x == 0 && g == 0, meta);
   // chunks of the session's shared prefix, in front of its own, if they are taken here
-  const int front = RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
+  const int front = TREES ? session.front : RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
   const int fc = RECORDS ? (front + KC - 1) / KC : 0;
   const size_t plane = RECORDS && fc > 0 ? (size_t)join.sh.cap * 2 * HD : 0;
-  const int prefix = RECORDS && fc > 0 ? __builtin_amdgcn_readfirstlane(join.sh.of[b]) : 0;
+  const int prefix = TREES ? session.prefix : RECORDS && fc > 0 ? __builtin_amdgcn_readfirstlane(join.sh.of[b]) : 0;
   const __amdgpu_buffer_rsrc_t rr = make_rsrc(join.blocks + ((size_t)prefix * Hkv + g) * plane,
                                               (uint32_t)(plane * 2));
   if (RECORDS) me.place = -1;   // nothing to join
-  const int S = meta.sess_S[b];
+  const int S = TREES ? session.S : meta.sess_S[b];
+  const uint64_t *ancs = TREES ? sets[0].anc : meta.anc + (size_t)b * n1;
   const int total = S + n1;
   const int nchunks = fc + (total + KC - 1) / KC;
   const int cps = (nchunks + nsplit - 1) / nsplit;
@@ -718,7 +730,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
       const f16x8 v = load_f16x8(qp + s * 16 + hh * 8);
       qf[s] = pad ? f16x8{} : v;
     }
-    anc = meta.anc[row0 + r];
+    anc = ancs[r];
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -740,7 +752,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
       const f16x8 v = load_f16x8(qp + s * 32 + lg * 8);
       qq[s] = pad ? f16x8{} : v;
     }
-    ancq = meta.anc[row0 + r];
+    ancq = ancs[r];
 #pragma unroll
     for (int nb = 0; nb < NB16; ++nb) oq[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -924,7 +936,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   wait_vmcnt<0>();
   if (PART) {
     __syncthreads();   // the marks are complete
-    if (!join.here && tid < 3 && bad[tid]) atomicOr(join.sm.bad + ((size_t)b * Hkv + g) * 3 + tid, bad[tid]);
+    if (!join.here && tid < 3) join.sm.bad[(((size_t)b * Hkv + g) * nsplit + split) * 3 + tid] = bad[tid];
   }
   const bf16 *vtree = vb + S;   // the tree's values
 
@@ -986,7 +998,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
           }
         }
         if (PART && join.here)
-          shared_finish<HD>(join, me, total_units, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all, M, L, all,
+          shared_finish<HD>(join, me, total_units, ancs, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all, M, L, all,
                             [&](int i) { return (qk * (NB16 / 4) + i) * 16 + lg * 4; });
         if ((PART ? !join.here : nsplit > 1) && qk == 0 && lg == 0) {
           part_ml[(item * QR + qi) * 2 + 0] = M;
@@ -1008,7 +1020,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
         for (int i = 0; i < 4 * NDB; ++i)
           all[i] = f32x4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2],
                          o[i >> 2][4 * (i & 3) + 3]};
-        shared_finish<HD>(join, me, total_units, meta, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
+        shared_finish<HD>(join, me, total_units, ancs, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
                           m_run == -INFINITY ? -INFINITY : m_run * sscale, l, all,
                           [&](int i) { return 8 * i + 4 * hh; });
       } else if (!PART && nsplit == 1) {

@@ -342,22 +342,32 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
   constexpr int TD = HD / 4, RPW = 256 / (TD * JOIN);   // threads of a part, rows of a workgroup
   __shared__ f32x4 s_o[RPW][JOIN][TD];
   __shared__ float2 s_ml[RPW][JOIN];
+  __shared__ uint32_t s_bad[RPW][JOIN][3];
   const int piece = threadIdx.x % TD, d = piece * 4, k = threadIdx.x / TD % JOIN, x = threadIdx.x / (TD * JOIN);
   const long long rh = min((long long)blockIdx.x * RPW + x, (long long)rows * H - 1);
   const int row = (int)(rh / H), h = (int)(rh - (long long)row * H);
   const int b = row / n1, r = row - b * n1, G = H / Hkv, g = h / G, QR = G * n1;
   const int qi = r * G + h - g * G;
-  SharedSession me = j.sm.sessions[b];
-  if (j.blocks) me.place = -1;   // (the parts hold the shared slots too)
-  const int4 total = *j.sm.total;
+  SharedSession me{0, -1, 0, 0, 0};   // (with blocks the parts hold the shared slots too)
+  int4 total{};
+  if (!j.blocks) {
+    me = j.sm.sessions[b];
+    total = *j.sm.total;
+  }
   const SharedParts p = shared_parts<HD>(j, me, total, g, qi, QR);
   const size_t item0 = ((size_t)b * Hkv + g) * nsplit * QR + qi;
   const float2 *ml = (const float2 *)part_ml + item0;
   const float *po = part_o + item0 * HD + d;
   constexpr size_t ON = acespec::kSharedTile;
   float M = -INFINITY;
+  const uint32_t *marks = j.sm.bad + ((size_t)b * Hkv + g) * nsplit * 3;
+  uint32_t bad[3] = {0, 0, 0};
 #pragma unroll 4
-  for (int s = k; s < nsplit; s += JOIN) M = fmaxf(M, ml[(size_t)s * QR].x);
+  for (int s = k; s < nsplit; s += JOIN) {
+    M = fmaxf(M, ml[(size_t)s * QR].x);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) bad[i] |= marks[s * 3 + i];
+  }
 #pragma unroll 8
   for (int s = k; s < p.parts; s += JOIN) M = fmaxf(M, p.ml[s * ON].x);
   float top = M == -INFINITY ? 0.f : M;
@@ -374,7 +384,11 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
   for (int s = k; s < p.parts; s += JOIN) add(p.ml[s * ON], *(const f32x4 *)(p.o + s * ON * HD + d));
   if constexpr (JOIN > 1) {
     s_o[x][k][piece] = o[0];
-    if (piece == 0) s_ml[x][k] = make_float2(M, l);
+    if (piece == 0) {
+      s_ml[x][k] = make_float2(M, l);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) s_bad[x][k][i] = bad[i];
+    }
     __syncthreads();
     M = -INFINITY;
 #pragma unroll
@@ -383,13 +397,17 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
     o[0] = f32x4{0.f, 0.f, 0.f, 0.f};
     l = 0.f;
 #pragma unroll
-    for (int i = 0; i < JOIN; ++i) add(s_ml[x][i], s_o[x][i][piece]);
+    for (int i = 0; i < JOIN; ++i) {
+      add(s_ml[x][i], s_o[x][i][piece]);
+#pragma unroll
+      for (int w = 0; w < 3; ++w) bad[w] |= s_bad[x][i][w];
+    }
   }
   if (k > 0 || (long long)blockIdx.x * RPW + x > rh) return;
   me.place = -1;   // (its parts are in)
   const bf16 *vb = cv + ((size_t)b * Hkv + g) * HD * capacity + meta.sess_S[b];
-  shared_finish<HD>(j, me, total, meta, vb, capacity, j.sm.bad + ((size_t)b * Hkv + g) * 3, b, g, qi, n1, H, Hkv,
-                    rows, M, l, o, [&](int) { return d; });
+  shared_finish<HD>(j, me, total, meta.anc + (size_t)b * n1, vb, capacity, bad, b, g, qi, n1, H, Hkv, rows, M, l, o,
+                    [&](int) { return d; });
 }
 
 // fp32 models: one workgroup per 16 query rows of a (session, kv head), over the prefix's records
@@ -401,12 +419,12 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(const float *__rest
 // rounding to fewer bits anywhere.  Bound by latency in small batches and by the reads of keys and
 // values (L2) in large ones, 16 rows a read: a workgroup a row and head took 332 us for 4 sessions
 // of 25 rows and 4 heads a kv head over 1200 slots where this takes 50.
-template <int HD>
+template <int HD, bool TREES>
 __global__ __launch_bounds__(512) void shared_attn_f32_kernel(
     const float *__restrict__ qin, const float *__restrict__ blocks, SharedArgs sh,
     const SharedSession *__restrict__ sessions, const float *__restrict__ ck,
-    const float *__restrict__ cv, TreeMeta meta, float *__restrict__ out, int n1, int H, int Hkv,
-    int capacity) {
+    const float *__restrict__ cv, TreeMeta meta, TreeArgs trees, float *__restrict__ out, int n1, int H,
+    int Hkv, int capacity) {
   constexpr int NW = 8, NK = HD / 16, ND = HD / 16, REC = 128 * HD;
   __shared__ __attribute__((aligned(16))) float so[NW][16][HD + 4];
   __shared__ float sml[NW][16][2];
@@ -414,9 +432,15 @@ __global__ __launch_bounds__(512) void shared_attn_f32_kernel(
   const int tile = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lx = lane & 15, ly = lane >> 4;
   const int G = H / Hkv, QR = G * n1, qi = min(tile * 16 + lx, QR - 1), r = qi / G;
-  const int S = meta.sess_S[b], front = sessions[b].slots, prefix = front > 0 ? sh.of[b] : 0;
+  __shared__ TreeSets sets[1];
+  TreeSession session{};
+  if constexpr (TREES)
+    session = tree_session(sets[0], trees, sh, b, n1, capacity, tile == 0 && g == 0, TreeMeta{});
+  const uint64_t *ancs = TREES ? sets[0].anc : meta.anc + (size_t)b * n1;
+  const int S = TREES ? session.S : meta.sess_S[b], front = TREES ? session.front : sessions[b].slots;
+  const int prefix = TREES ? session.prefix : front > 0 ? sh.of[b] : 0;
   const int start = (front + 63) & ~63, total = start + S + n1;   // own slots begin at `start`
-  const uint64_t anc = meta.anc[(size_t)b * n1 + r];
+  const uint64_t anc = ancs[r];
   const float *rec = blocks + ((size_t)prefix * Hkv + g) * (sh.cap >> 6) * REC;
   const float *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const float *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;   // [HD][capacity]
@@ -521,7 +545,7 @@ __global__ __launch_bounds__(512) void shared_attn_f32_kernel(
     }
     const int rx = qx / G, h = g * G + qx - rx * G, row = b * n1 + rx;
     if (s_bad) {   // an infinity or a NaN comes of such a value in the rows that see it
-      const uint64_t ax = meta.anc[row];
+      const uint64_t ax = ancs[rx];
       for (int t = 0; t < n1; ++t) {
         if (t > 0 && !((ax >> (t - 1)) & 1ull)) continue;
 #pragma unroll
@@ -537,7 +561,7 @@ __global__ __launch_bounds__(512) void shared_attn_f32_kernel(
 
 template <int HD, typename TQ>
 hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const SharedMeta &sm,
-                     const bf16 *ck, const bf16 *cv, const TreeMeta &meta, void *out, int rows_out,
+                     const TreeArgs &trees, const bf16 *ck, const bf16 *cv, const TreeMeta &meta, void *out, int rows_out,
                      float *sh_o, float *sh_ml, float *part_o, float *part_ml, long long part_cap,
                      int B, int n1, int H, int Hkv, int capacity, int cus, hipStream_t s) {
   const int rows = B * n1, wgs = acespec::shared_wgs(Hkv, cus);
@@ -553,8 +577,13 @@ hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const
                                                         part_cap) <= DIRECT;
   const SharedJoin j{sh_o, sh_ml, sm, wgs,
                      acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus), out, rows_out,
-                     direct || here, direct ? blocks : nullptr, sh};
+                     direct || here, direct ? blocks : nullptr, sh, trees};
   hipError_t e = hipSuccess;
+  if (trees.parents && !direct) {
+    e = acespec::launch_tree_prep_shared(nullptr, trees.parents, trees.prefix_len, B, n1, 1, capacity, sh,
+                                         H / Hkv, TM, meta, sm, trees.status, s);
+    if (e != hipSuccess) return e;
+  }
   if (!direct) {
     hipLaunchKernelGGL((shared_attn_kernel<HD, 4, TQ>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
                        sh_o, sh_ml, B, n1, H, Hkv, sh.cap, wgs, j.rows_total);
@@ -581,13 +610,13 @@ namespace acespec {
 
 template <>
 hipError_t launch_attention_shared<bf16>(const void *q, const f16 *blocks, const SharedArgs &sh,
-                                         const SharedMeta &sm, const bf16 *ck, const bf16 *cv,
-                                         const TreeMeta &meta, void *out, int rows_io, float *sh_o,
+                                         const SharedMeta &sm, const TreeArgs &trees, const bf16 *ck,
+                                         const bf16 *cv, const TreeMeta &meta, void *out, int rows_io, float *sh_o,
                                          float *sh_ml, float *part_o, float *part_ml,
                                          long long part_capacity, int B, int n1, int H, int Hkv,
                                          int hd, int capacity, int cus, hipStream_t s) {
   auto run = [&](auto launch, auto *queries) {
-    return launch(queries, blocks, sh, sm, ck, cv, meta, out, rows_io, sh_o, sh_ml, part_o, part_ml,
+    return launch(queries, blocks, sh, sm, trees, ck, cv, meta, out, rows_io, sh_o, sh_ml, part_o, part_ml,
                   part_capacity, B, n1, H, Hkv, capacity, cus, s);
   };
   if (rows_io)
@@ -597,14 +626,16 @@ hipError_t launch_attention_shared<bf16>(const void *q, const f16 *blocks, const
 
 template <>
 hipError_t launch_attention_shared<float>(const void *q, const float *blocks, const SharedArgs &sh,
-                                          const SharedMeta &sm, const float *ck, const float *cv,
+                                          const SharedMeta &sm, const TreeArgs &trees, const float *ck,
+                                          const float *cv,
                                           const TreeMeta &meta, void *out, int, float *, float *,
                                           float *, float *, long long, int B, int n1, int H,
                                           int Hkv, int hd, int capacity, int, hipStream_t s) {
-  auto kernel = hd == 64 ? shared_attn_f32_kernel<64> : shared_attn_f32_kernel<128>;
   if (Hkv > 65535 || B > 65535) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kernel, dim3((H / Hkv * n1 + 15) / 16, Hkv, B), dim3(512), 0, s, (const float *)q, blocks, sh, sm.sessions, ck, cv, meta,
-                     (float *)out, n1, H, Hkv, capacity);
+  auto kernel = trees.parents ? (hd == 64 ? shared_attn_f32_kernel<64, true> : shared_attn_f32_kernel<128, true>)
+                              : (hd == 64 ? shared_attn_f32_kernel<64, false> : shared_attn_f32_kernel<128, false>);
+  hipLaunchKernelGGL(kernel, dim3((H / Hkv * n1 + 15) / 16, Hkv, B), dim3(512), 0, s, (const float *)q, blocks, sh,
+                     sm.sessions, ck, cv, meta, trees, (float *)out, n1, H, Hkv, capacity);
   return hipGetLastError();
 }
 

@@ -222,7 +222,13 @@ struct SharedMeta {
   int32_t *order;           // [B]
   SharedGroup *groups;      // [B]
   int4 *total;              // of all groups: units, number of groups, tiles, most records of one
-  uint32_t *bad;            // [B][kv heads][3] tree rows with values that are not finite
+  uint32_t *bad;            // [B][kv heads][splits][3] tree rows with values that are not finite
+};
+
+// Trees that the attention is to prepare itself.
+struct TreeArgs {
+  const int32_t *parents, *prefix_len;
+  int32_t *status;
 };
 
 // The partial results over shared prefixes, and where the rows go once they are joined with those
@@ -237,6 +243,7 @@ struct SharedJoin {
   int here;              // 1: the kernel over the own slots joins them, unless these are split
   const f16 *blocks;     // this layer's records, if the kernel over the own slots is to go over the
   SharedArgs sh;         // shared ones too (there are no partial results then), or NULL
+  TreeArgs trees;        // with blocks and queries in bf16: the trees, which are then prepared there
 };
 
 // Fixed-point scale for deterministic mass sums in the vocabulary kernel.
@@ -262,7 +269,7 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
 // then not written).
 hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
                                    const int32_t *prefix_len, int B, int n1, int V, int capacity,
-                                   const SharedArgs &sh, int G, int Hkv, int tile_rows, TreeMeta meta,
+                                   const SharedArgs &sh, int G, int tile_rows, TreeMeta meta,
                                    const SharedMeta &sm, int32_t *status, hipStream_t s);
 
 template <typename TW>
@@ -369,8 +376,8 @@ hipError_t launch_attention(const typename ActOf<TW>::type *q, const TW *cache_k
 // results and written to j's out, if j.here and the sessions are not split (*nsplit 1), or else as
 // partial sums.
 // Values of tree rows that are not finite reach only rows that see them: where they are not joined
-// here they are left out, and their rows marked in j.sm.bad (three words a session and kv head,
-// cleared by launch_tree_prep_shared).  TQ: q's type, [rows][H hd].
+// here they are left out, and their rows marked in j.sm.bad (three words a session, kv head and
+// split).  TQ: q's type, [rows][H hd].
 template <typename TQ>
 hipError_t launch_attention_own(const TQ *q, const bf16 *cache_k, const bf16 *cache_v,
                                 const TreeMeta &meta, const SharedJoin &j, float *part_o,
@@ -392,8 +399,8 @@ inline long long shared_part_rows(long long rows, int Hkv, int cus) {
 }
 template <typename TW>
 hipError_t launch_attention_shared(const void *q, const typename ActOf<TW>::type *blocks,
-                                   const SharedArgs &sh, const SharedMeta &sm, const TW *ck,
-                                   const TW *cv, const TreeMeta &meta, void *out, int rows_io,
+                                   const SharedArgs &sh, const SharedMeta &sm, const TreeArgs &trees,
+                                   const TW *ck, const TW *cv, const TreeMeta &meta, void *out, int rows_io,
                                    float *sh_o,
                                    float *sh_ml, float *part_o, float *part_ml,
                                    long long part_capacity, int B, int n1, int H, int Hkv, int hd,

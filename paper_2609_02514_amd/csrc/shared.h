@@ -1,7 +1,7 @@
 // How the work over shared prefixes is dealt out, and how its partial results are joined with those
 // of a session's own slots.
 #pragma once
-#include "common.h"
+#include "tree.h"
 
 // Units of work (a 64-slot record for a tile of kSharedTile rows) lie on a line: group after group,
 // tile after tile, record after record, and the workgroups of a kv head take it in pieces, of which
@@ -81,11 +81,13 @@ AS_DEVICE SharedParts shared_parts(const SharedJoin &j, const SharedSession &me,
 }
 
 // A row's own partial result (largest exponent M in base 2, sum l, outputs o of four head dims from
-// dim(i) on) joined with the shared ones, and written.  me, total: j.sm's, asked for in time.  bad: tree rows with values that are not
-// finite, which were left out: whatever weight such a value has, an infinity or a NaN comes of it
-// in the rows that see its slot.  vb: the tree's values, [head dim][capacity].
+// dim(i) on) joined with the shared ones, and written.  me, total: j.sm's, asked for in time.  bad:
+// tree rows with values that are not finite, which were left out: whatever weight such a value has,
+// an infinity or a NaN comes of it in the rows that see its slot.  sets: the session's ancestor sets;
+// vb: the tree's values, [head dim][capacity].
 template <int HD, int N, typename F>
-AS_DEVICE void shared_finish(const SharedJoin &j, const SharedSession &me, int4 total, const TreeMeta &meta, const bf16 *vb, int capacity,
+AS_DEVICE void shared_finish(const SharedJoin &j, const SharedSession &me, int4 total,
+                             const uint64_t *sets, const bf16 *vb, int capacity,
                              const uint32_t *bad, int b, int g, int qi, int n1, int H, int Hkv,
                              int rows, float M, float l, f32x4 (&o)[N], F dim) {
   typedef bf16 b4 __attribute__((ext_vector_type(4)));
@@ -114,7 +116,7 @@ AS_DEVICE void shared_finish(const SharedJoin &j, const SharedSession &me, int4 
   }
   if (bad[0] | bad[1] | bad[2]) {
     __asm__ volatile("");   // (seldom: a branch)
-    const uint64_t anc = meta.anc[(size_t)b * n1 + r];
+    const uint64_t anc = sets[r];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
 #pragma unroll 1

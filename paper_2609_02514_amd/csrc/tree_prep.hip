@@ -8,16 +8,13 @@
 // Behind a shared prefix positions start at its end; the sessions of a prefix become a group.
 // Over a cache in 4 bits the tree's rows go behind the prefix_len % 32 slots of the tail, and a
 // sliding window takes ancestors that are too far back out of a row's set.
-#include "common.h"
+#include "tree.h"
 
 namespace {
 
-constexpr int TP_THREADS = 128;  // one thread per tree row (at most 65 rows)
+constexpr int TP_THREADS = TREE_ROWS;  // one thread per tree row (at most 65 rows)
 
-// One workgroup per session.  A row's ancestor mask is its own bit and its ancestors'
-// (the root carries none); it is built by pointer jumping, every row doubling the span of
-// ancestors it has folded in per round until the span covers n1 rows (7 rounds for 65), and the
-// row's depth is the mask's population count.
+// One workgroup per session.  A row's depth is its set's population count.
 // tokens may be NULL.  front: positions before the prefix (-1: a shared prefix that is not one).
 template <bool QUANT>
 AS_DEVICE void prepare_tree(int b, const int32_t *__restrict__ tokens,
@@ -25,44 +22,30 @@ AS_DEVICE void prepare_tree(int b, const int32_t *__restrict__ tokens,
                             const int32_t *__restrict__ prefix_len, int n1, int V, int capacity,
                             int window, int sinks, int front, const TreeMeta &meta,
                             int32_t *__restrict__ status) {
-  __shared__ int s_jump[TP_THREADS];
-  __shared__ uint64_t s_anc[TP_THREADS];
+  __shared__ TreeSets sets;
   const int r = threadIdx.x;
   const size_t base = (size_t)b * n1;
   const bool in = r < n1;
   const int pr = in ? parents[base + r] : 0;
   const int tk = in && tokens ? tokens[base + r] : 0;
-  int S = prefix_len[b];
-  const bool row_ok = !in || (((r == 0) ? (pr == -1) : (pr >= 0 && pr < r)) && tk >= 0 && tk < V);
+  int S = prefix_len[b], p;
   // largest prefix: with QUANT full blocks and a full tail behind them
   const long long most = QUANT ? (long long)capacity + 31 : (long long)capacity - n1;
-  const bool ok = __syncthreads_and(row_ok) && S >= 0 && S <= most && front >= 0;
+  const bool ok = tree_sets(sets, n1, pr, tk >= 0 && tk < V && S >= 0 && S <= most && front >= 0, &p);
   if (front < 0) front = 0;
   if (S < 0) S = 0;
   if (S > most) S = (int)most;
-  const int p = !in || r == 0 ? -1 : (ok ? pr : r - 1);  // malformed trees become a chain
-  s_jump[r] = p < 0 ? 0 : p;
-  s_anc[r] = (in && r > 0) ? (1ull << (r - 1)) : 0ull;
-  for (int span = 1; span < n1; span *= 2) {
-    __syncthreads();
-    const int jr = s_jump[r];
-    const uint64_t a = s_anc[r] | s_anc[jr];
-    const int jj = s_jump[jr];
-    __syncthreads();
-    s_anc[r] = a;
-    s_jump[r] = jj;
-  }
   if (r == 0) {
     meta.sess_S[b] = QUANT ? S & 31 : S;
     status[b] = ok ? ACESPEC_OK : ACESPEC_EBADTREE;
   }
-  uint64_t anc = s_anc[r];
+  uint64_t anc = sets.anc[r];
   const int depth = __popcll(anc);
   if (QUANT) __syncthreads();   // (other rows' sets are read)
   if (!in) return;
   if (QUANT && window > 0)
     for (uint64_t rest = anc; rest; rest &= rest - 1) {
-      const int j = __builtin_ctzll(rest) + 1, dj = __popcll(s_anc[j]);
+      const int j = __builtin_ctzll(rest) + 1, dj = __popcll(sets.anc[j]);
       if (depth - dj >= window && S + dj >= sinks) anc &= ~(1ull << (j - 1));
     }
   if (tokens) meta.tok[base + r] = tk < 0 ? 0 : (tk >= V ? V - 1 : tk);
@@ -79,18 +62,6 @@ __global__ __launch_bounds__(TP_THREADS) void tree_prep_kernel(
     int sinks, TreeMeta meta, int32_t *__restrict__ status) {
   prepare_tree<QUANT>(blockIdx.x, tokens, parents, prefix_len, n1, V, capacity, window, sinks, 0,
                       meta, status);
-}
-
-// Session b's shared prefix, -1 where it has none (or an empty or malformed one); *slots its
-// length, -1 where malformed.
-AS_DEVICE int shared_prefix(const SharedArgs &sh, int b, int *slots) {
-  const int p = sh.of[b];
-  *slots = p == -1 ? 0 : -1;
-  if (p < 0 || p >= sh.P) return -1;
-  const int n = sh.len[p];
-  if (n < 0 || n > sh.cap) return -1;
-  *slots = n;
-  return n > 0 ? p : -1;
 }
 
 AS_DEVICE int group_tiles(int members, int QR, int tile_rows) {
@@ -209,7 +180,7 @@ AS_DEVICE void group_many(int B, int QR, const SharedArgs &sh, int tile_rows, co
 __global__ __launch_bounds__(TP_THREADS) void tree_prep_shared_kernel(
     const int32_t *__restrict__ tokens, const int32_t *__restrict__ parents,
     const int32_t *__restrict__ prefix_len, int B, int n1, int V, int capacity, SharedArgs sh,
-    int QR, int Hkv, int tile_rows, TreeMeta meta, SharedMeta sm,
+    int QR, int tile_rows, TreeMeta meta, SharedMeta sm,
     int32_t *__restrict__ status) {
   const int w = blockIdx.x;
   if (w == 0) {
@@ -218,7 +189,6 @@ __global__ __launch_bounds__(TP_THREADS) void tree_prep_shared_kernel(
     else
       group_many(B, QR, sh, tile_rows, sm);
   } else {
-    for (int i = threadIdx.x; i < 3 * Hkv; i += TP_THREADS) sm.bad[(size_t)(w - 1) * 3 * Hkv + i] = 0;
     int slots;
     shared_prefix(sh, w - 1, &slots);
     prepare_tree<false>(w - 1, tokens, parents, prefix_len, n1, V, capacity, 0, 0, slots, meta,
@@ -251,11 +221,11 @@ hipError_t launch_tree_prep_quant(const int32_t *tokens, const int32_t *parents,
 
 hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents,
                                    const int32_t *prefix_len, int B, int n1, int V, int capacity,
-                                   const SharedArgs &sh, int G, int Hkv, int tile_rows, TreeMeta meta,
+                                   const SharedArgs &sh, int G, int tile_rows, TreeMeta meta,
                                    const SharedMeta &sm, int32_t *status, hipStream_t s) {
   if (n1 > TP_THREADS) return hipErrorInvalidValue;
   hipLaunchKernelGGL(tree_prep_shared_kernel, dim3(1 + B), dim3(TP_THREADS), 0, s, tokens, parents,
-                     prefix_len, B, n1, V, capacity, sh, G * n1, Hkv, tile_rows, meta, sm, status);
+                     prefix_len, B, n1, V, capacity, sh, G * n1, tile_rows, meta, sm, status);
   return hipGetLastError();
 }
 
