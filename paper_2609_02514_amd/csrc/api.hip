@@ -465,7 +465,7 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
       {shr * d.head_dim * 4, &p_so}, {shr * 2 * 4, &p_sml},
       {each * sizeof(SharedSession), &p_sess}, {each * 4, &p_order}, {each * sizeof(SharedGroup), &p_groups},
       {layers ? 16u : 0u, &p_total},
-      {layers ? (each * d.n_kv_heads + c->cus) * 12 : 0, &p_bad}};
+      {layers ? (each * d.n_kv_heads + 2 * c->cus) * 12 : 0, &p_bad}};
   size_t total = 0;
   for (auto &pt : parts) total += align_up(pt.bytes);
   if (hipMalloc(&c->ws, total) != hipSuccess) {

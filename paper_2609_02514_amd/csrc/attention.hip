@@ -42,6 +42,8 @@
 //  a small combine kernel.
 //
 // fp32 kernel (small models): one workgroup per (tree row, query head).
+#include <algorithm>
+
 #include "shared.h"
 
 namespace {
@@ -1198,15 +1200,23 @@ void launch_mfma(dim3 grid, hipStream_t s, const TQ *q, const bf16 *ck, const bf
 // but 2 for up to 32 items, whose few partials cost little, if the chunks' query tiles add
 // up to some work (one session of 1500 slots: 16.2 us against 17.3 at 4 chunks; 65 rows of
 // 8 query heads over 300 slots: 26 against 33 whole).
+int workgroups_a_cu(int all_tiles) { return all_tiles <= 8 ? 2 : 1; }   // behind shared prefixes
 int attn_items(int B, int n1, int H, int Hkv) {
   const int QR = H / Hkv * n1;
   return B * Hkv * (QR > 256 ? (QR + 271) / 272 : 1);   // (the query groups of launch_tree_attn)
 }
-int attn_splits(int B, int n1, int H, int Hkv, int hd, int nchunks, int cus, long long part_capacity) {
+int attn_splits(int B, int n1, int H, int Hkv, int hd, int nchunks, int cus, long long part_capacity,
+                bool part) {
   const int QR = H / Hkv * n1, all_tiles = (QR + 15) / 16, items = attn_items(B, n1, H, Hkv);
   int nsplit = cus / items;
   const int least = items <= 32 && nchunks * all_tiles >= 48 ? 2 : 4;
   nsplit = nsplit < nchunks / least ? nsplit : nchunks / least;
+  // Behind shared prefixes two workgroups share a CU up to 8 tiles: items that are split already are
+  // split for both where five chunks are left of each (17 rows, 8 kv heads: 8 sessions of 4096 slots
+  // 39.0 -> 35.2 us, 12 of 2048 40.9 -> 34.4; 8 of 2048, four chunks, 27.5 -> 28.6, two chunks 22.3 ->
+  // 26.7, and items that were whole 37.4 -> 41.0).
+  if (part && nsplit > 1 && workgroups_a_cu(all_tiles) == 2 && nchunks / 5 >= 2 * cus / items)
+    nsplit = std::max(nsplit, 2 * cus / items);
   if (nsplit < 1) nsplit = 1;
   while (nsplit > 1 && (long long)B * Hkv * nsplit * QR * hd > part_capacity) --nsplit;
   return nsplit;
@@ -1232,7 +1242,7 @@ hipError_t launch_tree_attn(const TQ *q, const bf16 *ck, const bf16 *cv, const T
   const int rpg = (QR + nqg - 1) / nqg;
   const int nsplit = attn_splits(B, n1, H, Hkv, hd,
                                  capacity / KC + (MODE == 2 ? join.sh.cap / KC : 0), cus,
-                                 part_capacity);
+                                 part_capacity, PART);
   *nsplit_used = nsplit;
   if (PART && nsplit > 1) join.here = 0;
   const dim3 grid(nsplit * nqg, Hkv, B);
@@ -1245,7 +1255,7 @@ hipError_t launch_tree_attn(const TQ *q, const bf16 *ck, const bf16 *cv, const T
       hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, MODE, TQ>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
                          rpg, join);
-  } else if (PART && all_tiles <= 8) {
+  } else if (PART && workgroups_a_cu(all_tiles) == 2) {
     if (hd == 128)
       launch_mfma<128, 8, 1, 2, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
                                           capacity, nsplit, all_tiles, join);
@@ -1284,8 +1294,9 @@ hipError_t launch_attention<bf16>(const f16 *q, const bf16 *ck, const bf16 *cv,
 
 int attention_chunks_in_turn(int B, int n1, int H, int Hkv, int hd, int nchunks, int cus,
                              long long part_capacity) {
-  const int nsplit = attn_splits(B, n1, H, Hkv, hd, nchunks, cus, part_capacity);
-  const int rounds = (attn_items(B, n1, H, Hkv) * nsplit + 2 * cus - 1) / (2 * cus);
+  const int nsplit = attn_splits(B, n1, H, Hkv, hd, nchunks, cus, part_capacity, true);
+  const int at_once = cus * workgroups_a_cu((H / Hkv * n1 + 15) / 16);
+  const int rounds = (attn_items(B, n1, H, Hkv) * nsplit + at_once - 1) / at_once;
   return rounds * ((nchunks + nsplit - 1) / nsplit);
 }
 

@@ -19,7 +19,6 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int TM = acespec::kSharedTile;
-constexpr int DIRECT = 12;
 
 AS_DEVICE float halves_max(float v) {
   auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -570,11 +569,14 @@ hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const
   // us against 88; the 8B batch, 17 tiles in up to three: 45 + 18 against 57).
   const int here = 3LL * rows * (H / Hkv) >= (long long)wgs * TM;
   // Small batches over short prefixes: the kernel over the own slots takes the records first, each
-  // session for itself, which leaves the tiles' way in and out of memory away.  Up to DIRECT chunks
-  // in turn (8 kv heads of 17 rows each; chunks, so taken, by tiles: 8 sessions behind 2048 slots 9,
-  // 33 us, 39; 64 behind 512 9, 39, 46; 16 behind 2048 17, 51, 44; 32 behind 2048 33, 79, 55).
-  const bool direct = acespec::attention_chunks_in_turn(B, n1, H, Hkv, HD, (sh.cap + capacity) / 64, cus,
-                                                        part_cap) <= DIRECT;
+  // session for itself, which leaves the tiles' way in and out of memory, and a launch, away.  It is
+  // taken up to 18 chunks in turn of head dim 128 or 36 of 64 (17 rows, 8 kv heads; so taken, by
+  // tiles: 8 sessions behind 2048 slots, 9 chunks, 27.5 us, 39.3; 16 behind 2048, 9, 35.6, 47.7; 64
+  // behind 1024, 18, 51, 62; 16 behind 4096, 17, 51, 55; 24 behind 2048, 34, 79, 55), single tokens
+  // up to 16, as they leave the tiles little to do (8 behind 8192, 17, 39.6, 33.1; 16 behind 1024, 6,
+  // 23.8, 31.5).
+  const int chunks = acespec::attention_chunks_in_turn(B, n1, H, Hkv, HD, (sh.cap + capacity) / 64, cus, part_cap);
+  const bool direct = (long long)chunks * HD <= (H / Hkv * n1 <= 16 ? 16 : 18) * 128;
   const SharedJoin j{sh_o, sh_ml, sm, wgs,
                      acespec::shared_part_rows((long long)rows * (H / Hkv), Hkv, cus), out, rows_out,
                      direct || here, direct ? blocks : nullptr, sh, trees};

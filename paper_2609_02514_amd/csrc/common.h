@@ -384,7 +384,7 @@ hipError_t launch_attention_own(const TQ *q, const bf16 *cache_k, const bf16 *ca
                                 float *part_ml, long long part_capacity, int B, int n1, int H,
                                 int Hkv, int hd, int capacity, int cus, hipStream_t s, int *nsplit);
 
-// The 64-slot chunks that launch_attention_own's workgroups, two a CU, go over one after the other.
+// The 64-slot chunks that launch_attention_own's workgroups go over one after the other.
 int attention_chunks_in_turn(int B, int n1, int H, int Hkv, int hd, int nchunks, int cus,
                              long long part_capacity);
 
