@@ -41,6 +41,13 @@
 //  With several splits, unnormalised partial outputs and (max, sum) pairs are merged by
 //  a small combine kernel.
 //
+// Behind shared prefixes (attention_shared.hip) the same kernels go over the sessions' own slots and
+// join the prefix's partial results (MODE 1), or over the prefix's records and then the own slots
+// (MODE 2: records come in the order of 32 x 32 operands and in fp16, so the DMA's source addresses
+// undo that order, and nothing of them is widened).  Up to 8 tiles they take 8 waves and two stages, two
+// workgroups a CU: 64 sessions of 17 rows over up to 512 own slots 47 us, 20 of it their stream at
+// 5 TB/s, 7 the prefix's parts; 64 single tokens 27.
+//
 // fp32 kernel (small models): one workgroup per (tree row, query head).
 #include <algorithm>
 

@@ -54,7 +54,10 @@ AS_DEVICE void block_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_bar
 // about 430 of its vector unit (16 exponentials of 16 cycles, their scaling, sums, rounding), and
 // two waves share a SIMD.  The halves are therefore pipelined: while the weights of one half are
 // computed, the scores of the next and the product with the values of the one before run, which
-// depend on none of it.
+// depend on none of it.  Measured: 32 sessions of 264 rows behind up to 16384 slots 0.98 to 1.05
+// PFLOP/s (475 to 525 us), the matrix cores 56 % busy at the 1.73 GHz that the card's power leaves; 64
+// sessions of 68 rows behind up to 8192 slots 105 to 123 us, 42 % busy at 2.0 GHz, as a workgroup goes
+// through one and a half tiles there.
 template <int HD, int NST, typename TQ>
 __global__ __launch_bounds__(512) void shared_attn_kernel(
     const TQ *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
@@ -564,9 +567,9 @@ hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const
                      float *sh_o, float *sh_ml, float *part_o, float *part_ml, long long part_cap,
                      int B, int n1, int H, int Hkv, int capacity, int cus, hipStream_t s) {
   const int rows = B * n1, wgs = acespec::shared_wgs(Hkv, cus);
-  // Few tiles are cut into many parts, which a kernel of its own joins faster, with a thread for four
-  // head dims, than the waves over the own slots do (64 single tokens, one tile in 32 parts: 30 + 10
-  // us against 88; the 8B batch, 17 tiles in up to three: 45 + 18 against 57).
+  // Few tiles are cut into many parts, which a kernel of its own joins faster, with a thread or more
+  // for four head dims, than the waves over the own slots do (64 single tokens, one tile in 32 parts:
+  // 27 + 9 us against 88; the 8B batch, 17 tiles in up to three: 45 + 18 against 49).
   const int here = 3LL * rows * (H / Hkv) >= (long long)wgs * TM;
   // Small batches over short prefixes: the kernel over the own slots takes the records first, each
   // session for itself, which leaves the tiles' way in and out of memory, and a launch, away.  It is
