@@ -492,9 +492,9 @@ def _check_tensors(want, index):
     """Tensors whose shape, type or stride differ from what the call says would be read out of
     range.  index: the GPU's."""
     for name, t, shape, dt in want:
-        if t.shape != shape or t.dtype is not dt or t.get_device() != index or not t.is_contiguous():
+        if t is None or t.shape != shape or t.dtype is not dt or t.get_device() != index or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dt} tensor {tuple(shape)} on GPU {index} "
-                             f"(got {t.dtype} {tuple(t.shape)} on {t.device})")
+                             f"(got {'None' if t is None else f'{t.dtype} {tuple(t.shape)} on {t.device}'})")
 
 
 def _check_room(want, index):

@@ -119,7 +119,7 @@ def test_take_overs_that_are_refused_on_the_device_write_nothing(lens, take, cou
             assert bool((shared.blocks[:, p] == 3).all())
 
 
-LARGE = 13 * 64 * 256   # slots: more than 12 chunks in turn for a workgroup on each of 256 CUs
+LARGE = 37 * 64 * 512   # slots: more chunks in turn than a session goes over by itself, with two workgroups on each of 256 CUs
 
 
 # ---- the attention --------------------------------------------------------------------------
@@ -239,6 +239,15 @@ def test_what_few_rows_do_not_see_does_not_reach_them(hd, cap, scap):
         shared.blocks[:, 1, :, :rec.shape[2]] = rec
     check_attention("bf16", hd, 4, 2, [130, 70], [0, 0, 1, 1, -1], [50, 7, 12, 0, 3], 3, seed=9, poison=poison, cap=cap,
                     scap=scap)
+
+
+def test_many_groups_of_many_sessions():
+    """More sessions than a wave, dealt to tiles of 70 prefixes; some stand alone, some behind none."""
+    r = random.Random(3)
+    held = [r.choice([1, 64, r.randint(1, 2400), 2400]) for _ in range(70)]
+    of = [r.randint(-1, 69) for _ in range(60)] + [r.randint(0, 4) for _ in range(70)]
+    check_attention("bf16", 64, 2, 1, held, of, [r.randint(0, 40) for _ in of], 2, seed=3)
+    check_attention("bf16", 64, 8, 1, held, of, [r.randint(0, 40) for _ in of], 9, seed=4)
 
 
 def test_one_layer_of_several_and_a_larger_cache():
@@ -634,6 +643,36 @@ def test_one_layers_calls_are_the_steps():
         ver.close()
 
 
+def test_a_step_by_tiles_decides_as_one_session_by_session():
+    """The same step behind a store so large that prefixes are read in tiles: logits differ by the
+    rounding of weights and outputs to fp16, through two layers."""
+    for kw in (dict(H=8, Hkv=2, hd=128, d=512), dict(H=4, Hkv=2, hd=64, tree="chain_sib", depth=8, sib=7)):
+        w = workload("bf16", **kw)
+        W = synth.make_weights(w, "cuda")
+        logits = []
+        for cap in (0, LARGE):
+            batch, ver, shared, of, k, v, ocap, own = start(w, [100, 40, 0, 70])
+            if cap:
+                from paper_2609_02514_amd.acespec import SharedPrefix
+                wide = SharedPrefix.alloc(w.L, shared.prefixes, w.Hkv, w.hd, cap, "bf16")
+                wide.blocks[:, :, :, :shared.blocks.shape[3]] = shared.blocks
+                wide.len = shared.len
+                shared = wide
+            n1 = batch.tokens.shape[1]
+            outs = ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True)
+            ver.verify_tree_shared(ver.weights_struct(W), shared, of, k, v, ocap, own, batch.tokens, batch.parents, batch.q,
+                                   batch.u, w.T, w.top_p, w.top_k, outs)
+            torch.cuda.synchronize()
+            assert outs["status"].tolist() == [0] * w.B
+            logits.append(outs["logits_out"].double())
+            ver.close()
+        # an activation of a layer is off by a few roundings to fp16 (2^-11 each), of which a logit's
+        # sum of d products keeps its share of their root sum of squares
+        err = (logits[0] - logits[1]).norm() / logits[0].norm()
+        hz.log(f"tiles against session by session: {float(err):.2e}")
+        assert 0 < err < 8 * 2.0 ** -11
+
+
 def test_a_nonfinite_shared_value_flags_the_sessions_behind_it():
     from paper_2609_02514_amd import acespec as A
     w = workload("bf16")
@@ -704,6 +743,45 @@ def test_a_captured_run_replays_between_other_calls():
     ver.close()
 
 
+@pytest.mark.parametrize("hd, N", [(128, 16), (128, 0), (64, 3)])
+def test_captured_attention_by_tiles_and_session_by_session(hd, N):
+    """Two graphs on one context, whose workspace they share, replayed in both orders between eager calls."""
+    B, H, Hkv, L = 3, 8, 2, 1
+    small, _, _ = store(L, [200, 70], Hkv, hd, "bf16", 1)
+    wide, _, _ = store(L, [150, 33], Hkv, hd, "bf16", 2, LARGE)
+    k, v = random_cache(L, B, Hkv, 128, hd, "bf16", 3)
+    ver, of, mine = verifier(L, B, H, Hkv, hd, "bf16", N), i32([1, 0, 1]), i32([5, 64, 0])
+    r, g = random.Random(5), torch.Generator().manual_seed(6)
+    par = i32([random_parents(r, N) for _ in range(B)])
+    q = torch.randn(B, N + 1, H, hd, generator=g).to(torch.bfloat16).cuda()
+    outs, status = [torch.zeros_like(q) for _ in range(2)], [i32([9] * B) for _ in range(2)]
+
+    def call(i):
+        ver.attention_shared((small, wide)[i], of, k, v, 128, mine, 0, q, par, outs[i], status[i])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i in range(2):
+            call(i)
+        side.synchronize()
+        want, graphs = [o.clone() for o in outs], [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+        for i in range(2):
+            with torch.cuda.graph(graphs[i], stream=side):
+                call(i)
+        for order in ((0, 1), (1, 0), (1, 1, 0), (0, 0, 1)):
+            for t in outs + status:
+                t.fill_(9)
+            for i in order:
+                graphs[i].replay()
+            side.synchronize()
+            assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+            assert status[0].tolist() == status[1].tolist() == [0] * B
+            call(order[0])
+    torch.cuda.synchronize()
+    ver.close()
+
+
 def test_a_call_repeats_bit_for_bit():
     for scap in (0, LARGE):
         args = ("bf16", 128, 16, 2, [1000, 300], [0, 1, 0, 0, 1, 0, 0], [5, 9, 100, 3, 0, 7, 64], 16)
@@ -726,7 +804,8 @@ def test_wrong_tensors_are_refused():
     for bad in (dict(shared=other), dict(shared=f32), dict(prefix_of=of.long()), dict(prefix_of=i32([0])),
                 dict(prefix_of=None), dict(kv_k=v), dict(kv_v=k), dict(capacity=64), dict(prefix_len=i32([1, 2, 3])),
                 dict(prefix_len=own.cpu()), dict(q=q.float()), dict(q=q.transpose(1, 2)), dict(out=q[:1]),
-                dict(parents=par.long()), dict(status=i32([0])), dict(kv_k=k[:1])):
+                dict(parents=par.long()), dict(status=i32([0])), dict(kv_k=k[:1]), dict(q=None), dict(out=None),
+                dict(status=None), dict(kv_v=None)):
         with pytest.raises(ValueError):
             ver.attention_shared(**dict(good, **bad))
     with pytest.raises(ValueError, match="moved"):
