@@ -478,8 +478,19 @@ class SharedPrefix:
 
 def _stream_of(index: int) -> int:
     """The current stream's handle on that GPU (the Stream object around it costs 2.5 us more)."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(index)
+    return _torch_c()._cuda_getCurrentRawStream(index)
+
+
+_torch_bindings = None
+
+
+def _torch_c():
+    """torch._C, looked up once (an import statement in every call costs as much as a tensor's checks)."""
+    global _torch_bindings
+    if _torch_bindings is None:
+        import torch
+        _torch_bindings = torch._C
+    return _torch_bindings
 
 
 def _fits(t, shape, dt, index) -> bool:
@@ -519,6 +530,8 @@ class Verifier:
         self.ctx = acespec_create(self.desc, max_batch, max_nodes)
         self.index = torch.cuda.current_device()
         self._kv = (L, Hkv, hd, torch.bfloat16 if dtype == "bf16" else torch.float32, torch.int32)
+        self._store = (L, Hkv, hd, self.desc.dtype)   # (a struct's fields cost a lookup each in every call)
+        self._heads = (H, (H + 2 * Hkv) * hd, hd)     # query heads, a projection's width, head dim
         self._keep: List = []
 
     @classmethod
@@ -744,21 +757,19 @@ class Verifier:
 
     def _here(self) -> int:
         """The current GPU, which must be the context's."""
-        import torch
-        here = torch.cuda.current_device()
+        here = _torch_c()._cuda_getDevice()   # (the context is there, and so is the GPU)
         if self.index is not None and self.index != here:
             raise ValueError(f"the context is on cuda:{self.index}, the current device and stream are "
                              f"cuda:{here}'s")
         return here
 
     def _check_store(self, shared: SharedPrefix, index: int):
-        d = self.desc
         if shared.index != index:
             raise ValueError(f"the shared prefixes are on cuda:{shared.index}, the current device and "
                              f"stream are cuda:{index}'s")
-        if shared._fit != (d.n_layers, d.n_kv_heads, d.head_dim, d.dtype):
+        if shared._fit != self._store:
             raise ValueError(f"a store of (layers, kv heads, head dim, dtype) {shared._fit} is not this "
-                             f"model's {(d.n_layers, d.n_kv_heads, d.head_dim, d.dtype)}")
+                             f"model's {self._store}")
 
     def _check_shared(self, shared: Optional[SharedPrefix], prefix_of, B: int, index: int):
         if (shared is None) != (prefix_of is None):
@@ -803,7 +814,7 @@ class Verifier:
         index, dt, i32 = self._here(), self._kv[3], self._kv[4]
         self._check_shared(shared, prefix_of, B, index)
         kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
-        shape = (B, n1, self.desc.n_heads, self.desc.head_dim)
+        shape = (B, n1, self._heads[0], self._heads[2])
         if not (_fits(q, shape, dt, index) and _fits(out, shape, dt, index) and
                 _fits(parents, (B, n1), i32, index) and _fits(status, (B,), i32, index)):
             _check_tensors((("q", q, shape, dt), ("out", out, shape, dt), ("parents", parents, (B, n1), i32),
@@ -818,11 +829,11 @@ class Verifier:
         """One layer's projection [B, N+1, (H + 2 Hkv) hd] normalised per head (gains [hd] or None),
         rotated and written to q_out [B, N+1, H, hd] and the cache (acespec_qk_norm_rope)."""
         B, n1 = parents.shape
-        d, index, dt, i32 = self.desc, self._here(), self._kv[3], self._kv[4]
+        index, dt, i32 = self._here(), self._kv[3], self._kv[4]
         self._check_shared(shared, prefix_of, B, index)
         kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
-        H, hd = d.n_heads, d.head_dim
-        wide, rows = (B, n1, (H + 2 * d.n_kv_heads) * hd), (B, n1, H, hd)
+        H, width, hd = self._heads
+        wide, rows = (B, n1, width), (B, n1, H, hd)
         if not (_fits(qkv, wide, dt, index) and _fits(q_out, rows, dt, index) and
                 _fits(parents, (B, n1), i32, index) and _fits(status, (B,), i32, index) and
                 (q_gain is None or _fits(q_gain, (hd,), dt, index)) and
