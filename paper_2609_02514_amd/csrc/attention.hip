@@ -270,7 +270,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   __shared__ TreeSets sets[1];
   TreeSession session{};
   if constexpr (TREES)
-    session = tree_session(sets[0], join.trees, join.sh, b, n1, capacity, blockIdx.x == 0 && g == 0, meta);
+    session = tree_session(sets[0], join.trees, tree_ask(join.trees, join.sh, b, n1), b, n1, capacity, blockIdx.x == 0 && g == 0, meta);
   // chunks of the session's shared prefix, in front of its own, if they are taken here
   const int front = TREES ? session.front : RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
   const int fc = RECORDS ? (front + KC - 1) / KC : 0;
@@ -697,7 +697,7 @@ __global__ __launch_bounds__(512) void tree_attn_t32_kernel(
   __shared__ TreeSets sets[1];
   TreeSession session{};
   if constexpr (TREES)
-    session = tree_session(sets[0], join.trees, join.sh, b, n1, capacity, blockIdx.x == 0 && g == 0, meta);
+    session = tree_session(sets[0], join.trees, tree_ask(join.trees, join.sh, b, n1), b, n1, capacity, blockIdx.x == 0 && g == 0, meta);
   // chunks of the session's shared prefix, in front of its own, if they are taken here
   const int front = TREES ? session.front : RECORDS ? __builtin_amdgcn_readfirstlane(me.slots) : 0;
   const int fc = RECORDS ? (front + KC - 1) / KC : 0;

@@ -435,25 +435,21 @@ __global__ __launch_bounds__(512) void shared_attn_f32_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lx = lane & 15, ly = lane >> 4;
   const int G = H / Hkv, QR = G * n1, qi = min(tile * 16 + lx, QR - 1), r = qi / G;
   __shared__ TreeSets sets[1];
-  TreeSession session{};
-  if constexpr (TREES)
-    session = tree_session(sets[0], trees, sh, b, n1, capacity, tile == 0 && g == 0, TreeMeta{});
-  const uint64_t *ancs = TREES ? sets[0].anc : meta.anc + (size_t)b * n1;
-  const int S = TREES ? session.S : meta.sess_S[b], front = TREES ? session.front : sessions[b].slots;
-  const int prefix = TREES ? session.prefix : front > 0 ? sh.of[b] : 0;
-  const int start = (front + 63) & ~63, total = start + S + n1;   // own slots begin at `start`
-  const uint64_t anc = ancs[r];
+  // queries, and the first keys and values, are on their way before the tree is known
+  f32x4 qf[NK];
+  const float *qp = qin + ((size_t)b * n1 + r) * H * HD + (g * G + qi - r * G) * HD + ly * (HD / 4);
+#pragma unroll
+  for (int i = 0; i < NK; ++i) qf[i] = *(const f32x4 *)(qp + i * 4);
+  TreeAsked asked{};
+  if constexpr (TREES) asked = tree_ask(trees, sh, b, n1);
+  const int front = TREES ? __builtin_amdgcn_readfirstlane(max(asked.slots, 0)) : sessions[b].slots;
+  const int prefix = TREES ? __builtin_amdgcn_readfirstlane(max(asked.prefix, 0)) : front > 0 ? sh.of[b] : 0;
+  const int start = (front + 63) & ~63;   // own slots begin here
   const float *rec = blocks + ((size_t)prefix * Hkv + g) * (sh.cap >> 6) * REC;
   const float *kb = ck + ((size_t)b * Hkv + g) * capacity * HD;
   const float *vb = cv + ((size_t)b * Hkv + g) * HD * capacity;   // [HD][capacity]
   const float scale = 1.0f / sqrtf((float)HD);
   if (tid == 0) s_bad = 0;
-  __syncthreads();
-  f32x4 qf[NK];
-  const float *qp = qin + ((size_t)b * n1 + r) * H * HD + (g * G + qi - r * G) * HD + ly * (HD / 4);
-#pragma unroll
-  for (int i = 0; i < NK; ++i) qf[i] = *(const f32x4 *)(qp + i * 4);
-  const int nblk = (total + 15) >> 4;
   f32x4 kx[NK], vx[ND];
   auto load = [&](int c) {   // (a record's or the capacity's 64 slots hold all of a block)
     const int slot = c * 16, in = slot & 63;
@@ -470,7 +466,16 @@ __global__ __launch_bounds__(512) void shared_attn_f32_kernel(
   f32x4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (wave < nblk) load(wave);
+  if (wave * 16 < start + capacity) load(wave);
+  int S;
+  if constexpr (TREES)
+    S = tree_session(sets[0], trees, asked, b, n1, capacity, tile == 0 && g == 0, TreeMeta{}).S;
+  else
+    S = meta.sess_S[b];
+  __syncthreads();   // (s_bad is clear)
+  const uint64_t *ancs = TREES ? sets[0].anc : meta.anc + (size_t)b * n1;
+  const uint64_t anc = ancs[r];
+  const int total = start + S + n1, nblk = (total + 15) >> 4;
   for (int c = wave; c < nblk; c += NW) {
     const int slot0 = c * 16 + ly * 4;   // of this lane's four
     f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};

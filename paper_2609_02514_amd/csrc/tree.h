@@ -50,20 +50,29 @@ AS_DEVICE int shared_prefix(const SharedArgs &sh, int b, int *slots) {
   return n > 0 ? p : -1;
 }
 
-// Session b of a call that prepares its trees in the attention itself: the sets, its own slots S, its
-// shared prefix and the slots of it.  writes: this workgroup leaves the status (and, with meta.anc
-// given, what joins parts of the session later) for all of the session's.
+// A call that prepares its trees in the attention itself asks for what session b is, in time,
+struct TreeAsked {
+  int parent, S, prefix, slots;   // (of this thread's row), own slots, shared prefix and its slots, as they are given
+};
+AS_DEVICE TreeAsked tree_ask(const TreeArgs &a, const SharedArgs &sh, int b, int n1) {
+  TreeAsked x;
+  x.parent = (int)threadIdx.x < n1 ? a.parents[(size_t)b * n1 + threadIdx.x] : 0;
+  x.S = a.prefix_len[b];
+  x.prefix = shared_prefix(sh, b, &x.slots);
+  return x;
+}
+// and makes of it the sets and the session's own slots S, its shared prefix and the slots of it.
+// writes: this workgroup leaves the status (and, with meta.anc given, what joins parts of the session
+// later) for all of the session's.
 struct TreeSession {
   int S, prefix, front;
 };
-AS_DEVICE TreeSession tree_session(TreeSets &t, const TreeArgs &a, const SharedArgs &sh, int b, int n1,
+AS_DEVICE TreeSession tree_session(TreeSets &t, const TreeArgs &a, const TreeAsked &x, int b, int n1,
                                    int capacity, bool writes, const TreeMeta &meta) {
   const int r = threadIdx.x, most = capacity - n1;
-  const int parent = r < n1 ? a.parents[(size_t)b * n1 + r] : 0;
-  int S = a.prefix_len[b], slots, up;
-  const int prefix = shared_prefix(sh, b, &slots);
-  const bool ok = tree_sets(t, n1, parent, S >= 0 && S <= most && slots >= 0, &up);
-  S = min(max(S, 0), most);
+  int up;
+  const bool ok = tree_sets(t, n1, x.parent, x.S >= 0 && x.S <= most && x.slots >= 0, &up);
+  const int S = min(max(x.S, 0), most);
   if (writes) {
     if (r == 0) {
       a.status[b] = ok ? ACESPEC_OK : ACESPEC_EBADTREE;
@@ -72,6 +81,6 @@ AS_DEVICE TreeSession tree_session(TreeSets &t, const TreeArgs &a, const SharedA
     if (r < n1 && meta.anc) meta.anc[(size_t)b * n1 + r] = t.anc[r];
   }
   __syncthreads();
-  return TreeSession{__builtin_amdgcn_readfirstlane(S), __builtin_amdgcn_readfirstlane(max(prefix, 0)),
-                     __builtin_amdgcn_readfirstlane(max(slots, 0))};
+  return TreeSession{__builtin_amdgcn_readfirstlane(S), __builtin_amdgcn_readfirstlane(max(x.prefix, 0)),
+                     __builtin_amdgcn_readfirstlane(max(x.slots, 0))};
 }
