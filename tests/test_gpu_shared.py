@@ -673,6 +673,36 @@ def test_a_step_by_tiles_decides_as_one_session_by_session():
         assert 0 < err < 8 * 2.0 ** -11
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norms_alone_and_the_scalar_uplink(dtype):
+    """Norms without any prefix decide as norms with a store that nobody stands behind, up to the
+    rounding of another attention kernel; q_hat in q's place changes nothing of the forward pass."""
+    w = workload(dtype, H=8, Hkv=2, hd=128, d=512)
+    W, norms = synth.make_weights(w, "cuda"), gains(w)
+    batch, ver, shared, of, k, v, cap, own = start(w, [0, 0, 0, 0])
+    behind = start(w, [100, 40, 0, 70])
+    n1, ws = batch.tokens.shape[1], ver.weights_struct(W)
+    head = (batch.tokens, batch.parents, batch.q, batch.u, w.T, w.top_p, w.top_k)
+    q_hat = torch.rand(w.B, n1, generator=torch.Generator().manual_seed(1)).cuda()
+    outs = [ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True) for _ in range(4)]
+    ver.verify_tree_shared(ws, None, None, k, v, cap, own, *head, outs[0], norms)
+    ver.verify_tree_shared(ws, shared, i32([-1] * w.B), k, v, cap, own, *head, outs[1], norms)
+    for o, scalar, q in ((outs[2], False, batch.q), (outs[3], True, q_hat)):
+        behind[1].verify_tree_shared(ws, *behind[2:], *head[:2], q, *head[3:], o, norms, scalar=scalar)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert o["status"].tolist() == [0] * w.B
+    a, b = (o["logits_out"].double() for o in outs[:2])
+    err = float((a - b).norm() / a.norm())
+    hz.log(f"norms alone {dtype}: {err:.2e}")
+    assert err < (8 * 2.0 ** -11 if dtype == "bf16" else 512 * 2.0 ** -24)
+    for key in ("logits_out", "topk_ids", "topk_probs"):
+        assert torch.equal(outs[2][key], outs[3][key]), key
+    assert outs[3]["next_token"].tolist() == [-1] * w.B and bool((outs[3]["resample_token"] == -1).all())
+    ver.close()
+    behind[1].close()
+
+
 def test_a_nonfinite_shared_value_flags_the_sessions_behind_it():
     from paper_2609_02514_amd import acespec as A
     w = workload("bf16")
