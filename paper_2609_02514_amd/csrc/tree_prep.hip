@@ -97,83 +97,95 @@ AS_DEVICE void group_few(int B, int QR, const SharedArgs &sh, int tile_rows, con
   if (b == 0) *sm.total = make_int4(units, groups, tiles, most);
 }
 
-// The groups of any number of sessions, by one workgroup, in the order of their prefixes: a
-// session's place follows from counts over all the sessions (B^2 / 128 reads from LDS a thread).
-constexpr int GROUP_TILE = 1024;   // sessions in LDS at a time
-AS_DEVICE void group_many(int B, int QR, const SharedArgs &sh, int tile_rows, const SharedMeta &sm) {
-  __shared__ int s_p[GROUP_TILE];
-  const int tid = threadIdx.x;
-  int grouped = 0;
-  for (int b0 = 0; b0 < B; b0 += TP_THREADS) {
-    const int b = b0 + tid;
-    int slots = 0, before = 0, rank = 0, members = 0;
-    const int p = b < B ? shared_prefix(sh, b, &slots) : -1;
-    grouped = 0;
-    for (int t0 = 0; t0 < B; t0 += GROUP_TILE) {
-      const int n = min(GROUP_TILE, B - t0);
-      int unused;
-      __syncthreads();
-      for (int i = tid; i < n; i += TP_THREADS) s_p[i] = shared_prefix(sh, t0 + i, &unused);
-      __syncthreads();
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) {
-        const int o = s_p[i];
-        grouped += o >= 0;
-        before += o >= 0 && o < p;
-        members += o == p;
-        rank += o == p && t0 + i < b;
-      }
-    }
-    if (b >= B) continue;
-    sm.sessions[b] = SharedSession{max(slots, 0), p < 0 ? -1 : before + rank, before, 0, 0};
-    if (p < 0) continue;
-    sm.order[before + rank] = b;
-    // a group's entry waits at its first place until the ones before it are known
-    sm.groups[before + rank] = SharedGroup{p, before, rank == 0 ? members : 0, slots, 0, 0};
+// More sessions: in the order of their prefixes.  Each session's workgroup counts the sessions before
+// its own (one pass over prefix_of), and a launch behind it puts the groups together.  (One workgroup
+// for all of it took 324 us for 1024 sessions, this 5 and 6.)
+AS_DEVICE void group_one(int b, int B, const SharedArgs &sh, const SharedMeta &sm) {
+  __shared__ int s_count[4][TP_THREADS / 64];
+  const int tid = threadIdx.x, mine = sh.of[b];
+  int slots, count[4] = {0, 0, 0, 0};   // of lower prefixes, of this before b, of this, of any
+  shared_prefix(sh, b, &slots);
+#pragma unroll 4
+  for (int i = tid; i < B; i += TP_THREADS) {
+    const int o = sh.of[i];
+    const bool in = o >= 0 && o < sh.P;
+    count[0] += in && o < mine;
+    count[1] += o == mine && i < b;
+    count[2] += o == mine;
+    count[3] += in;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int c = wave_sum_i32(count[k]);
+    if (tid % 64 == 0) s_count[k][tid / 64] = c;
   }
   __syncthreads();
-  // one wave closes the gaps, and sums the units
-  if (tid < 64) {
-    int count = 0, units = 0, tiles = 0, most = 0;
-    for (int x0 = 0; x0 < grouped; x0 += 64) {
-      const int x = x0 + tid;
-      SharedGroup g = x < grouped ? sm.groups[x] : SharedGroup{0, 0, 0, 0, 0, 0};
-      const bool lead = g.members > 0;
-      const int t = lead ? group_tiles(g.members, QR, tile_rows) : 0, mine = t * ((g.slots + 63) / 64);
-      int sum = mine, sum_t = t;   // of this lane's and the ones' before
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(sum, o), vt = __shfl_up(sum_t, o);
-        if (tid >= o) {
-          sum += v;
-          sum_t += vt;
-        }
-      }
-      const uint64_t leads = __ballot(lead);
-      g.units = units + sum - mine;
-      g.tiles = tiles + sum_t - t;
-      if (lead) {
-        most = max(most, (g.slots + 63) / 64);
-        sm.groups[count + __popcll(leads & ((1ull << tid) - 1))] = g;   // (at most x: read already)
-      }
-      count += __popcll(leads);
-      units += __shfl(sum, 63);
-      tiles += __shfl(sum_t, 63);
-    }
-    for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
-    if (tid == 0) *sm.total = make_int4(units, count, tiles, most);
-    __threadfence_block();   // (the entries were moved by other lanes)
-    // and its members learn what lies before their group
-    for (int x = tid; x < grouped; x += 64) {
-      int lo = 0, hi = count - 1;   // the last group that begins at place x or before
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (sm.groups[mid].first <= x) lo = mid; else hi = mid - 1;
-      }
-      SharedSession &m = sm.sessions[sm.order[x]];
-      m.units = sm.groups[lo].units;
-      m.tiles = sm.groups[lo].tiles;
-    }
+  if (tid > 0) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    count[k] = 0;
+    for (int w = 0; w < TP_THREADS / 64; ++w) count[k] += s_count[k][w];
   }
+  // (a prefix that is empty or malformed keeps its places, and has no group)
+  const bool in = mine >= 0 && mine < sh.P;
+  sm.sessions[b] = SharedSession{max(slots, 0), -1, count[0], count[2], 0};
+  if (in) sm.order[count[0] + count[1]] = b;
+  if (b == 0) *sm.total = make_int4(count[3], 0, 0, 0);
+}
+
+// A place a thread: sums over the groups before follow from a scan in which a group counts at its
+// first place.
+constexpr int GT = 1024;
+__global__ __launch_bounds__(GT) void group_kernel(int QR, int tile_rows, SharedArgs sh, SharedMeta sm) {
+  __shared__ int s_sum[4][GT / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int places = sm.total->x;
+  int units = 0, tiles = 0, groups = 0, most = 0;   // of the groups so far
+  for (int x0 = 0; x0 < places; x0 += GT) {
+    const int x = x0 + tid, b = x < places ? sm.order[x] : 0;
+    SharedSession me = x < places ? sm.sessions[b] : SharedSession{0, -1, 0, 0, 0};
+    const bool live = me.slots > 0, lead = live && me.first == x;
+    const int members = me.units, nblk = (me.slots + 63) / 64, t = live ? group_tiles(members, QR, tile_rows) : 0;
+    int sum[3] = {lead ? t * nblk : 0, lead ? t : 0, lead ? 1 : 0};   // with the lanes' before
+    for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const int v = __shfl_up(sum[k], o);
+        if (lane >= o) sum[k] += v;
+      }
+    int top = nblk;
+    for (int o = 1; o < 64; o <<= 1) top = max(top, __shfl_xor(top, o));
+    __syncthreads();
+    if (lane == 63) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) s_sum[k][wave] = sum[k];
+      s_sum[3][wave] = top;
+    }
+    __syncthreads();
+    int all[3] = {0, 0, 0};
+    for (int w = 0; w < GT / 64; ++w) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const int v = s_sum[k][w];
+        all[k] += v;
+        if (w < wave) sum[k] += v;
+      }
+      most = max(most, s_sum[3][w]);
+    }
+    if (live) {
+      me.place = x;
+      me.units = units + sum[0] - t * nblk;
+      me.tiles = tiles + sum[1] - t;
+      sm.sessions[b] = me;
+      if (lead)
+        sm.groups[groups + sum[2] - 1] = SharedGroup{sh.of[b], x, members, me.slots, me.units, me.tiles};
+    }
+    units += all[0];
+    tiles += all[1];
+    groups += all[2];
+  }
+  __syncthreads();   // (all have read how many places there are)
+  if (tid == 0) *sm.total = make_int4(units, groups, tiles, most);
 }
 
 // Workgroups: the groups, then a session each.
@@ -184,15 +196,13 @@ __global__ __launch_bounds__(TP_THREADS) void tree_prep_shared_kernel(
     int32_t *__restrict__ status) {
   const int w = blockIdx.x;
   if (w == 0) {
-    if (B <= 64)
-      group_few(B, QR, sh, tile_rows, sm);
-    else
-      group_many(B, QR, sh, tile_rows, sm);
+    if (B <= 64) group_few(B, QR, sh, tile_rows, sm);
   } else {
     int slots;
     shared_prefix(sh, w - 1, &slots);
     prepare_tree<false>(w - 1, tokens, parents, prefix_len, n1, V, capacity, 0, 0, slots, meta,
                         status);
+    if (B > 64) group_one(w - 1, B, sh, sm);
   }
 }
 
@@ -226,6 +236,11 @@ hipError_t launch_tree_prep_shared(const int32_t *tokens, const int32_t *parents
   if (n1 > TP_THREADS) return hipErrorInvalidValue;
   hipLaunchKernelGGL(tree_prep_shared_kernel, dim3(1 + B), dim3(TP_THREADS), 0, s, tokens, parents,
                      prefix_len, B, n1, V, capacity, sh, G * n1, tile_rows, meta, sm, status);
+  if (B > 64) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(group_kernel, dim3(1), dim3(GT), 0, s, G * n1, tile_rows, sh, sm);
+  }
   return hipGetLastError();
 }
 

@@ -248,6 +248,8 @@ def test_many_groups_of_many_sessions():
     of = [r.randint(-1, 69) for _ in range(60)] + [r.randint(0, 4) for _ in range(70)]
     check_attention("bf16", 64, 2, 1, held, of, [r.randint(0, 40) for _ in of], 2, seed=3)
     check_attention("bf16", 64, 8, 1, held, of, [r.randint(0, 40) for _ in of], 9, seed=4)
+    of = [r.randint(-1, 9) for _ in range(1500)]      # more places than a workgroup has threads
+    check_attention("bf16", 64, 1, 1, [2400, 1, 64, 65, 100, 0, 300, 2300, 5, 700], of, [b % 3 for b in range(1500)], 0, seed=5)
 
 
 def test_one_layer_of_several_and_a_larger_cache():
@@ -311,6 +313,37 @@ def test_malformed_sessions_are_flagged_and_the_others_unharmed():
                   A.ACESPEC_EBADTREE, A.ACESPEC_EBADTREE]
     for b in (0, 5):
         assert torch.equal(good[b], bad[b])
+
+
+def test_malformed_sessions_among_many():
+    """More than 64 sessions, some behind prefixes that are none or whose length is wrong: flagged, and
+    the others as they are without them."""
+    from paper_2609_02514_amd import acespec as A
+    B, N, H, Hkv, hd = 90, 1, 4, 1, 64
+    shared, _, _ = store(1, [100, 2400, 64, 2300], Hkv, hd, "bf16", 1)
+    k, v = random_cache(1, B, Hkv, 64, hd, "bf16", 2)
+    q = torch.randn(B, N + 1, H, hd, device="cuda").to(torch.bfloat16)
+    of = [b % 4 for b in range(B)]
+    ver, parents, mine = verifier(1, B, H, Hkv, hd, "bf16", N), i32([[-1, 0]] * B), i32([b % 7 for b in range(B)])
+
+    def call(of, lens):
+        shared.len = i32(lens)
+        out, status = torch.zeros_like(q), i32([9] * B)
+        ver.attention_shared(shared, i32(of), k, v, 64, mine, 0, q, parents, out, status)
+        torch.cuda.synchronize()
+        return out, status.tolist()
+
+    good, st = call(of, [100, 2400, 64, 2300])
+    assert st == [0] * B
+    odd = list(of)
+    odd[3], odd[5], odd[40] = 4, -2, 7
+    bad, st = call(odd, [100, 2400, 3000, 2300])      # prefix 2 longer than the store
+    for b in range(B):
+        wrong = odd[b] == 2 or odd[b] not in range(4)
+        assert st[b] == (A.ACESPEC_EBADTREE if wrong else 0)
+    worst = max(float((good[b].float() - bad[b].float()).abs().max()) for b in range(B) if st[b] == 0)
+    assert worst <= 2.0 ** -7 * float(good.float().abs().max())   # (cut elsewhere: parts round apart)
+    ver.close()
 
 
 def test_large_scores_and_far_apart_references():
