@@ -390,8 +390,9 @@ int attention_chunks_in_turn(int B, int n1, int H, int Hkv, int hd, int nchunks,
 
 // One layer's tree attention behind shared prefixes: blocks [P][Hkv][cap / 64] records, own slots
 // ck, cv as in launch_attention.  q is row-major [rows][H hd] in the activation type, out in the
-// activation layout; or, with rows_io, both row-major in TW.  sh_o, sh_ml: partial results of the
-// shared slots, shared_part_rows(..) rows a kv head.
+// activation layout; or, with rows_io, both row-major in TW.  trees: what the trees are prepared from,
+// here (with rows_io), or nothing: meta and sm are there.  sh_o, sh_ml: partial results of the shared
+// slots, shared_part_rows(..) rows a kv head.
 constexpr int kSharedTile = 256;   // query rows of a workgroup over a shared prefix
 inline int shared_wgs(int Hkv, int cus) { return cus > Hkv ? cus / Hkv : 1; }  // a kv head
 inline long long shared_part_rows(long long rows, int Hkv, int cus) {
