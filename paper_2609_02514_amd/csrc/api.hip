@@ -1339,8 +1339,7 @@ int acespec_fork_kv(acespec_ctx *ctx, const acespec_kv_cache *src, int src_batch
                     {"first", first, each, false},
                     {"new_prefix_len", new_prefix_len, each, true}});
   if (rc) return rc;
-  const int least = src->capacity < dst->capacity ? src->capacity : dst->capacity;
-  if ((long long)d.n_layers * d.n_kv_heads * dst_batch * ((least + 255) / 256) > 0xffffffLL)
+  if (fork_workgroups(d.n_layers, d.n_kv_heads, dst_batch, src->capacity, dst->capacity) > 0xffffffLL)
     return fail(ACESPEC_EUNSUPPORTED, "more slots than one launch takes");
   if (d.dtype == ACESPEC_BF16)
     RUN(K_FORK, launch_fork_kv<bf16>((const bf16 *)src->k, (const bf16 *)src->v, src->prefix_len,

@@ -426,7 +426,13 @@ hipError_t launch_share_prefix(const T *k, const T *v, const int32_t *prefix_len
                                void *blocks, const SharedArgs &sh, const int32_t *from,
                                const int32_t *count, int32_t *new_len, int L, int Hkv, int hd,
                                hipStream_t s);
-// Slots [first[b], len of from[b]) of another session, written to session b's from 0 on.
+// Slots [first[b], len of from[b]) of another session, written to session b's from 0 on; a launch has
+// fork_workgroups(..) workgroups, fewer than 2^24.
+constexpr int kForkSlots = 64;   // slots of a workgroup
+inline long long fork_workgroups(int L, int Hkv, int B, int src_capacity, int dst_capacity) {
+  const int least = src_capacity < dst_capacity ? src_capacity : dst_capacity;
+  return (long long)L * Hkv * B * ((least + kForkSlots - 1) / kForkSlots);
+}
 template <typename T>
 hipError_t launch_fork_kv(const T *sk, const T *sv, const int32_t *src_len, int Bs, int scap, T *dk,
                           T *dv, const int32_t *dst_len, int Bd, int dcap, const int32_t *from,

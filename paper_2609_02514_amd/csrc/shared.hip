@@ -99,7 +99,7 @@ template <typename T> AS_DEVICE u32x4 load_any(const T *p) {
 // the sessions that take over from it (16 rows from 4 sources, 0.78 GB written: a workgroup a session
 // 232 us, the source read again through L2, this 213).  The first of these sessions' workgroup does
 // it, the others leave.
-constexpr int FCH = 64;
+constexpr int FCH = acespec::kForkSlots;
 template <typename T, int HD>
 __global__ __launch_bounds__(ST) void fork_kernel(const T *__restrict__ sk, const T *__restrict__ sv,
                                                   const int32_t *__restrict__ src_len, int Bs,
@@ -192,7 +192,7 @@ hipError_t launch_fork_kv(const T *sk, const T *sv, const int32_t *src_len, int 
                           const int32_t *first, int32_t *new_len, int L, int Hkv, int hd,
                           hipStream_t s) {
   const int chunks = ((scap < dcap ? scap : dcap) + FCH - 1) / FCH;
-  const long long wgs = (long long)L * Hkv * Bd * chunks;
+  const long long wgs = fork_workgroups(L, Hkv, Bd, scap, dcap);
   if ((hd != 64 && hd != 128) || wgs > 0xffffffffLL / ST) return hipErrorInvalidValue;
   const int same = sk == dk && sv == dv;
   auto kernel = hd == 64 ? fork_kernel<T, 64> : fork_kernel<T, 128>;

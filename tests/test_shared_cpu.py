@@ -207,3 +207,10 @@ def test_more_sessions_than_a_grid_takes():
     ctx = Ctx(max_batch=70000).ptr
     for call in (attention, rotate, verify):
         refused(call(ctx, B=65536), "65535", A.ACESPEC_EUNSUPPORTED)
+
+
+@pytest.mark.parametrize("cap", [2 ** 24 - 64, 2 ** 23])   # 2 x 16 x 4 planes in chunks of 64 slots: 2^25 - 128, 2^24
+def test_more_slots_than_a_forks_launch_takes(cap):
+    ctx, T = Ctx(H=16, Hkv=16).ptr, 1 << 42   # (the caches take up to 2^39 bytes)
+    src, dst = cache(T, 2 * T, cap, P), cache(3 * T, 4 * T, cap, P + 64)
+    refused(fork(ctx, src, dst, frm=P + 128, first=P + 192, new=P + 256), "one launch", A.ACESPEC_EUNSUPPORTED)
