@@ -508,6 +508,14 @@ def _check_tensors(want, index):
                              f"(got {'None' if t is None else f'{t.dtype} {tuple(t.shape)} on {t.device}'})")
 
 
+def _sized(name, t, dims: int):
+    """The shape of a tensor that says how large a call is."""
+    if t is None or t.dim() != dims:
+        raise ValueError(f"{name} must be a tensor of {dims} dimension{'s' * (dims > 1)} "
+                         f"(got {'None' if t is None else tuple(t.shape)})")
+    return t.shape
+
+
 def _check_room(want, index):
     """Tensors of which a call uses the first n elements."""
     for name, t, n, dt in want:
@@ -764,6 +772,8 @@ class Verifier:
         return here
 
     def _check_store(self, shared: SharedPrefix, index: int):
+        if shared is None:
+            raise ValueError("shared must be a SharedPrefix (got None)")
         if shared.index != index:
             raise ValueError(f"the shared prefixes are on cuda:{shared.index}, the current device and "
                              f"stream are cuda:{index}'s")
@@ -783,7 +793,7 @@ class Verifier:
     def _check_cache(self, kv_k, kv_v, capacity: int, lengths, index: int, B: Optional[int] = None,
                      name: str = "") -> KVCache:
         """The tensors of a cache in the model's type, of B (None: len(lengths)) sessions."""
-        B = lengths.shape[0] if B is None else B
+        B = _sized(name + "prefix_len", lengths, 1)[0] if B is None else B
         L, Hkv, hd, dt, i32 = self._kv
         k, v = (L, B, Hkv, capacity, hd), (L, B, Hkv, hd, capacity)
         if not (_fits(kv_k, k, dt, index) and _fits(kv_v, v, dt, index) and _fits(lengths, (B,), i32, index)):
@@ -796,8 +806,9 @@ class Verifier:
         """Sessions' first slots taken over as shared prefixes (acespec_share_prefix): from_ [P] the
         sessions or -1, count [P] how many slots (None: all).  shared.len is not touched; new_len [P]
         is written."""
-        index, P, i32 = self._here(), (shared.prefixes,), self._kv[4]
+        index, i32 = self._here(), self._kv[4]
         self._check_store(shared, index)
+        P = (shared.prefixes,)
         kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index)
         if not (_fits(from_, P, i32, index) and _fits(new_len, P, i32, index) and
                 (count is None or _fits(count, P, i32, index))):
@@ -810,8 +821,10 @@ class Verifier:
                          layer: int, q, parents, out, status) -> int:
         """Tree attention of one layer behind shared prefixes (acespec_attention_shared): q, out
         [B, N+1, H, hd]."""
-        B, n1 = parents.shape
+        B, n1 = _sized("parents", parents, 2)
         index, dt, i32 = self._here(), self._kv[3], self._kv[4]
+        if shared is None:
+            self._check_store(shared, index)   # (refused: only calls that can do without take None)
         self._check_shared(shared, prefix_of, B, index)
         kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
         shape = (B, n1, self._heads[0], self._heads[2])
@@ -828,7 +841,7 @@ class Verifier:
                      prefix_of=None) -> int:
         """One layer's projection [B, N+1, (H + 2 Hkv) hd] normalised per head (gains [hd] or None),
         rotated and written to q_out [B, N+1, H, hd] and the cache (acespec_qk_norm_rope)."""
-        B, n1 = parents.shape
+        B, n1 = _sized("parents", parents, 2)
         index, dt, i32 = self._here(), self._kv[3], self._kv[4]
         self._check_shared(shared, prefix_of, B, index)
         kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
@@ -852,7 +865,7 @@ class Verifier:
                            k: int, outs: Dict, norms=None, scalar: bool = False) -> int:
         """verify_tree for sessions behind shared prefixes (or None, None); norms: a (q_gain, k_gain)
         pair a layer, or None; scalar: q is q_hat [B, N+1]."""
-        B, n1 = tokens.shape
+        B, n1 = _sized("tokens", tokens, 2)
         d, index, dt, i32 = self.desc, self._here(), self._kv[3], self._kv[4]
         self._check_shared(shared, prefix_of, B, index)
         kv = self._check_cache(kv_k, kv_v, capacity, prefix_len, index, B)
@@ -876,9 +889,10 @@ class Verifier:
         """Sessions take over others' slots [first, src_len) (acespec_fork_kv): from_ [B of dst] the
         sessions of src, or -1; src and dst may be the same tensors.  dst_len is not touched;
         new_prefix_len is written."""
-        index, n, i32 = self._here(), dst_len.shape, self._kv[4]
+        index, i32 = self._here(), self._kv[4]
         src = self._check_cache(src_k, src_v, src_capacity, src_len, index, None, "src ")
         dst = self._check_cache(dst_k, dst_v, dst_capacity, dst_len, index, None, "dst ")
+        n = dst_len.shape
         if not (_fits(from_, n, i32, index) and _fits(new_prefix_len, n, i32, index) and
                 (first is None or _fits(first, n, i32, index))):
             _check_tensors([(x, t, n, i32) for x, t in
