@@ -74,7 +74,7 @@ struct acespec_ctx {
   int32_t *rowflag = nullptr; // vocabulary kernel: per-row data-error code (0 = none)
   TreeMeta meta{};
   SharedMeta shm{};           // the groups behind shared prefixes
-  float *sh_o = nullptr, *sh_ml = nullptr;  // partial results over them
+  float *sh_o = nullptr, *sh_ml = nullptr;  // partial results over them, in gpart
   // timing
   bool timing = false;
   uint32_t timing_mask = ~0u;  // kinds timed while timing is on
@@ -434,6 +434,11 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   const size_t shr = layers && d.dtype == ACESPEC_BF16   // partial rows, of all kv heads
                          ? d.n_kv_heads * shared_part_rows((long long)(R * G), d.n_kv_heads, c->cus)
                          : 0;
+  // They lie where the GEMMs leave theirs, which are used up when an attention starts and not begun
+  // when it ends: memory of their own was 51 MB for 64 sessions of 17 rows of 32 heads and 2.2 GB for
+  // 1024 of 65 rows of 64, shared prefixes or not.
+  const size_t sh_o_bytes = align_up(shr * d.head_dim * 4);
+  const size_t gpart_bytes = std::max((size_t)8 * R * d.d_model * 4, sh_o_bytes + shr * 2 * 4);
   const size_t each = layers ? max_batch : 0;
   struct Part { size_t bytes; void **dst; };
   void *p_x = nullptr, *p_logits = nullptr, *p_po = nullptr, *p_pml = nullptr, *p_if = nullptr;
@@ -441,7 +446,7 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
        *p_cand = nullptr, *p_rflag = nullptr;
   void *p_tok = nullptr, *p_par = nullptr, *p_pos = nullptr, *p_depth = nullptr,
        *p_anc = nullptr, *p_S = nullptr;
-  void *p_so = nullptr, *p_sml = nullptr, *p_sess = nullptr, *p_order = nullptr,
+  void *p_sess = nullptr, *p_order = nullptr,
        *p_groups = nullptr, *p_total = nullptr, *p_bad = nullptr;
   std::vector<Part> parts = {
       {R * d.d_model * 4, &p_x},
@@ -459,10 +464,9 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
       {(size_t)c->part_cap / (layers ? d.head_dim : 1) * 2 * 4, &p_pml},
       {layers ? (size_t)d.head_dim / 2 * 8 : 0, &p_if},
       {layers ? R * (size_t)d.head_dim / 2 * 8 : 0, &p_rot},
-      {(size_t)8 * R * d.d_model * 4, &p_gpart},
+      {gpart_bytes, &p_gpart},
       {R * 4, &p_tok}, {R * 4, &p_par}, {R * 4, &p_pos}, {R * 4, &p_depth}, {R * 8, &p_anc},
       {(size_t)max_batch * 4, &p_S},
-      {shr * d.head_dim * 4, &p_so}, {shr * 2 * 4, &p_sml},
       {each * sizeof(SharedSession), &p_sess}, {each * 4, &p_order}, {each * sizeof(SharedGroup), &p_groups},
       {layers ? 16u : 0u, &p_total},
       {layers ? (each * d.n_kv_heads + 2 * c->cus) * 12 : 0, &p_bad}};
@@ -496,8 +500,8 @@ int acespec_create(const acespec_model_desc *desc, int max_batch, int max_nodes,
   c->meta.depth = (int32_t *)p_depth;
   c->meta.anc = (uint64_t *)p_anc;
   c->meta.sess_S = (int32_t *)p_S;
-  c->sh_o = (float *)p_so;
-  c->sh_ml = (float *)p_sml;
+  c->sh_o = (float *)p_gpart;
+  c->sh_ml = (float *)((char *)p_gpart + sh_o_bytes);
   c->shm = SharedMeta{(SharedSession *)p_sess, (int32_t *)p_order, (SharedGroup *)p_groups,
                       (int4 *)p_total, (uint32_t *)p_bad};
   if (layers) {
