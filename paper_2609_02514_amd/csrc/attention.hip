@@ -56,16 +56,6 @@
 namespace {
 
 constexpr int KC = 64;            // slots per chunk
-// Opens the tree-mask branch of a chunk loop: an empty volatile asm cannot be executed
-// speculatively, so the mask stays a branch taken only by the chunks that hold tree
-// slots instead of being if-converted into selects that every chunk pays for.
-#define MASK_BRANCH() __asm__ volatile("")
-
-// The chunk barrier: this wave's LDS accesses (the widening's stores, the fragment reads)
-// complete, then every wave of the workgroup arrives.  The DMA is not waited for here:
-// each stage's DMA is waited for explicitly, NST - 2 chunks ahead.  (Written out rather
-// than as an LDS release fence, with which the compiler drains every outstanding load,
-// the DMA of the chunks in flight included, at every barrier of some of these kernels.)
 // Online softmax with a lazy reference: the exponent's reference m moves to a new block
 // maximum only when that maximum exceeds m by more than LAZY_LOG2 in base 2 (or m is
 // unset), so the accumulators are rescaled a few times per query instead of at most
@@ -74,9 +64,6 @@ constexpr int KC = 64;            // slots per chunk
 constexpr float LAZY_LOG2 = 8.f;
 AS_DEVICE float lazy_ref(float m, float mx, float lazy) { return mx > m + lazy ? mx : m; }
 
-AS_DEVICE void chunk_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-constexpr float LOG2E = 1.4426950408889634f;
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 AS_DEVICE bool tree_visible(int slot, int S, int n1, uint64_t anc) {
   if (slot < S) return true;
@@ -632,8 +619,6 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
 //    B operand, which is exactly what p32 put in its scores; the matching V^T fragment is
 //    one contiguous 16-byte read of a head-dim row.
 // ------------------------------------------------------------------------------------
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
 // key (within a 32-key block) held by A row r of a 32 x 32 score block
 AS_DEVICE int p32(int r) {
   return ((r >> 4) & 1) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
@@ -642,14 +627,6 @@ AS_DEVICE int p32(int r) {
 AS_DEVICE int key32_of_score(int i, int h) {
   const int j = i >> 2, e = i & 3;
   return (j >> 1) * 16 + h * 8 + (j & 1) * 4 + e;
-}
-AS_DEVICE float halves_max(float v) {
-  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-AS_DEVICE float halves_sum(float v) {
-  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
 template <int HD, int NST, int MODE = 0, typename TQ = f16>

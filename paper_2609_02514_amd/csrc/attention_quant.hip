@@ -57,11 +57,9 @@ namespace {
 
 constexpr float LAZY_LOG2 = 8.f;
 constexpr float LAZY_SUM = 8 * 256.f;   // of 8 weights none of which exceeds 2^LAZY_LOG2
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr int SLOW = 3;   // what a masked block costs a wave, in blocks that every row sees whole
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // The operand arithmetic of a model's type: eight elements of a lane.
 template <typename T> struct Ops;
 template <> struct Ops<bf16> {

@@ -11,38 +11,20 @@
 
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 1024.f;    // sum of 16 weights from which on their reference moves
 constexpr int AHEAD = 2;           // products whose operands are on their way from LDS
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int TM = acespec::kSharedTile;
-
-AS_DEVICE float halves_max(float v) {
-  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-AS_DEVICE float halves_sum(float v) {
-  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
-}
 
 // A value that all lanes hold alike, in a scalar register: what depends on it stays there too (loop
 // counts, addresses, branches), where a loaded value would make vector work of all of it.
 AS_DEVICE int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// An empty volatile asm keeps a seldom taken branch one (it is not if-converted into selects).
-#define MASK_BRANCH() __asm__ volatile("")
 
 // A value is computed where this stands, not where it is used.
 #define PIN(x) __asm__ volatile("" : "+v"(x))
 
 AS_DEVICE f16x8 to_f16x8(f16x8 v) { return v; }
 AS_DEVICE f16x8 to_f16x8(bf16x8 v) { return bf16x8_to_f16x8(v); }
-
-AS_DEVICE void block_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Eight waves, 32 query rows each, over one record after the other.  A record is 1 KB operands of
 // v_mfma_f32_32x32x16_f16 in the order in which they are multiplied: keys (rows are slots, in an
@@ -124,7 +106,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
       }
     };
     // the first record is on its way while the queries are looked up
-    block_barrier();      // (the last tile's stages are free)
+    chunk_barrier();      // (the last tile's stages are free)
     issue(c0);
     // queries: rows of padding multiply zeros
     f16x8 qf[KS];
@@ -278,7 +260,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     };
 
     if (c0 + 2 < c1) wait_vmcnt<2 * L_DMA>(); else wait_vmcnt<0>();
-    block_barrier();      // record c0 is there
+    chunk_barrier();      // record c0 is there
     f32x16 za, zb;        // scores of the record's halves
     f16x8 pa[2], pb[2];
     if (any) {
@@ -292,7 +274,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
     }
     for (int c = c0; c + 1 < c1; ++c) {
       if (c + 2 < c1) wait_vmcnt<L_DMA>(); else wait_vmcnt<0>();
-      block_barrier();    // record c + 1 is there, record c - 1 is used up, for every wave
+      chunk_barrier();    // record c + 1 is there, record c - 1 is used up, for every wave
       if (c + 3 < c1) issue(c + 3);
       if (!any) continue;
       const f16 *st = stage_of(c), *next = stage_of(c + 1);

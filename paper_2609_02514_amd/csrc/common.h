@@ -9,7 +9,10 @@ typedef __bf16 bf16;
 typedef _Float16 f16;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Storage of a bf16 model: weights and KV cache in bf16; activations handed from one
@@ -71,6 +74,16 @@ AS_DEVICE float rows4_max(float v) {
 AS_DEVICE float rows4_sum(float v) {
   auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// The same over the two lanes l, l^32.
+AS_DEVICE float halves_max(float v) {
+  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+AS_DEVICE float halves_sum(float v) {
   auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
@@ -161,6 +174,18 @@ AS_DEVICE void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
+
+// The barrier of a loop over chunks: this wave's LDS accesses complete, then every wave of the workgroup
+// arrives.  The DMA is not waited for here: each stage's is waited for explicitly, some chunks ahead.
+// (Written out rather than as lds_barrier's release fence, with which the compiler drains every
+// outstanding load, the DMA of the chunks in flight included, at every barrier of some kernels.)
+AS_DEVICE void chunk_barrier() { __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Opens a branch that few iterations take, such as a chunk loop's mask: an empty volatile asm cannot be
+// executed speculatively, so the branch is not if-converted into selects that all of them pay for.
+#define MASK_BRANCH() __asm__ volatile("")
+
+constexpr float LOG2E = 1.4426950408889634f;
 
 // Where element (row, col) of a bf16 model's activation matrix [M, K] (K % 32 == 0) lives:
 // 16-row blocks, each holding its K / 8 eight-column pieces in turn, a piece's rows (16, or
