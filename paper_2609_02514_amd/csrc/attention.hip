@@ -8,10 +8,8 @@
 //
 // bf16 model.  One workgroup of 16 waves (8 with more than 16 tiles) per (key split, kv
 // head, session).  Query rows are the G query heads of the kv head times the N+1 tree rows
-// (row = tree_row * G + head), in 16-row tiles dealt round-robin to the waves; with several
-// tiles per wave, a last round of at most NW/4 tiles is split into quarter units (one
-// 16-key block of every chunk each) on the waves that would otherwise idle, merged at the
-// end through LDS.  The key range of the split streams through LDS in chunks of 64 slots:
+// (row = tree_row * G + head), in tiles of 16 rows, one a wave (more than 16 tiles: the
+// 32-row kernel below).  The key range of the split streams through LDS in chunks of 64 slots:
 //  * HBM -> LDS by direct DMA (buffer loads to LDS, 16 bytes a lane, nontemporal: the
 //    cache is read once per step, and streaming it past L2 and the MALL measured 15 %
 //    faster at the 8B shape) into a ring of NST stages.  The buffer form rather than the
@@ -207,12 +205,11 @@ AS_DEVICE void widen_chunk(uint16_t *stage, int t, int stride, int key0, int tot
   }
 }
 
-template <int HD, int NW, int UPW, int NST, int MODE = 0, typename TQ = f16>
+template <int HD, int NW, int NST, int MODE = 0, typename TQ = f16>
 __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
     const TQ *__restrict__ qin, const bf16 *__restrict__ ck, const bf16 *__restrict__ cv,
     TreeMeta meta, f16 *__restrict__ out, float *__restrict__ part_o,
-    float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, int tpg,
-    SharedJoin join) {
+    float *__restrict__ part_ml, int n1, int H, int Hkv, int capacity, int nsplit, SharedJoin join) {
   // MODE 0: the verify pass; 1: own slots behind a shared prefix, joined with its partial results or
   // left as some; 2: its records first, then the own slots
   constexpr bool PART = MODE > 0, RECORDS = MODE == 2;
@@ -227,25 +224,9 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   __shared__ __attribute__((aligned(1024))) uint16_t smem[NST * STAGE];
 
   const int g = blockIdx.y, b = blockIdx.z;
-  const int G = H / Hkv, QR = G * n1;
-  // Query groups: when the query rows of a kv head need more tiles than one workgroup
-  // holds, consecutive groups of tpg tiles go to separate workgroups (each streams the
-  // key range once); tbase is this group's first tile.
-  const int all_tiles = (QR + 15) / 16, nqg = (all_tiles + tpg - 1) / tpg;
-  const int split = blockIdx.x / nqg, tbase = (blockIdx.x - split * nqg) * tpg;
-  const int ntiles = min(tpg, all_tiles - tbase);
+  const int G = H / Hkv, QR = G * n1, ntiles = (QR + 15) / 16, split = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int lr = lane & 15, lg = lane >> 4;
-  // With several tiles per wave, a last round of only a few tiles would leave the waves
-  // that hold one waiting at every chunk barrier for the waves that hold one more; each of
-  // those last rlast tiles is then split into 4 quarter units (one 16-key block of every
-  // chunk each), run in slot QS by the last 4 * rlast waves and merged through LDS.
-  constexpr int QS = UPW - 1;
-  const int rlast = ntiles - NW * QS;
-  const bool split_last = UPW > 1 && rlast >= 1 && 4 * rlast <= NW;
-  const int qbase = NW - 4 * rlast;  // first wave holding a quarter unit
-  const bool quarter = split_last && wave >= qbase;
-  const int qk = (wave - qbase) & 3;  // a quarter unit's key block within each chunk
   __shared__ uint32_t bad[PART ? 3 : 1];   // tree rows with values that are not finite
   if (PART && threadIdx.x < 3) bad[threadIdx.x] = 0;   // (before the prologue's barrier)
   SharedSession me{};          // (asked for here, well before the join needs it)
@@ -282,32 +263,27 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   const float sscale = LOG2E / sqrtf((float)HD);   // scores -> base-2 exponent
   const float lazy = LAZY_LOG2 / sscale;           // reference threshold in score units
 
-  // Query tile t of this wave: wave + NW t.  Per tile: query fragments (B operand of
-  // S^T = K Q^T), ancestor mask, running softmax state.
-  f16x8 qf[UPW][KSTEPS];
-  uint64_t anc[UPW];
-  float m_run[UPW], l_run[UPW];
-  f32x4 o[UPW][NB];
-#pragma unroll
-  for (int t = 0; t < UPW; ++t) {
-    const int tile = (split_last && t == QS) ? NW * QS + ((wave - qbase) >> 2) : wave + NW * t;
-    int qi = (tbase + tile) * 16 + lr;   // (slot QS of a wave without a quarter unit: unused)
-    qi = qi < 0 ? 0 : (qi < QR ? qi : QR - 1);
+  // Query tile `wave`: query fragments (B operand of S^T = K Q^T), ancestor mask, running
+  // softmax state.
+  f16x8 qf[KSTEPS];
+  uint64_t anc;
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4 o[NB];
+  {
+    const int qi = min(wave * 16 + lr, QR - 1);
     const int r = qi / G, h = g * G + (qi - r * G);
     const TQ *qp = qin + (row0 + r) * q_stride + h * HD;
     // padding rows of the last tile multiply zeros (their outputs are dropped; zero
     // operands keep the MFMA's switching, and so its power draw, down)
-    const bool pad = (tbase + tile) * 16 + lr >= QR;
+    const bool pad = wave * 16 + lr >= QR;
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) {
       const f16x8 v = load_f16x8(qp + s * 32 + lg * 8);
-      qf[t][s] = pad ? f16x8{} : v;
+      qf[s] = pad ? f16x8{} : v;
     }
-    anc[t] = ancs[r];
-    m_run[t] = -INFINITY;
-    l_run[t] = 0.f;
+    anc = ancs[r];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) o[t][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int nb = 0; nb < NB; ++nb) o[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   wait_vmcnt<0>();   // the loop's vmcnt accounting covers the DMA only
 
@@ -350,8 +326,6 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
     koff[s] = key_of_row(0, lr) * HD + (((s * 4 + lg) ^ ksw_l) << 3);
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) voff[ks] = v_off(lr, ks * 4 + lg);
-  const int qkoff = key_of_row(qk, 0) * HD;                   // quarter: its key block
-  const int qvoff = (qk & 2 ? voff[1] : voff[0]) + (qk & 1) * 4;  // and its V^T half-piece
 
   for (int c = c0; c < c1; ++c) {
     if constexpr (SYNC) {
@@ -379,9 +353,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
     const bool record = RECORDS && c < fc;
     const int key0 = record ? 0 : (c - fc) * KC, Sc = record ? front - c * KC : S, n1c = record ? 0 : n1;
     const bool tree_chunk = key0 + KC > Sc;
-#pragma unroll
-    for (int t = 0; t < UPW; ++t) {
-      if (wave + NW * t >= ntiles || (split_last && t == QS)) break;
+    if (wave < ntiles) {
       // S^T for 4 blocks of 16 keys: sc[kk][e] is the score of slot
       // key0 + key_of_score(kk, lg, e) against this lane's query.
       f32x4 sc[4];
@@ -392,7 +364,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
           const f16x8 kf = *(const f16x8 *)(sk + koff[s] + key_of_row(kk, 0) * HD);
-          sc[kk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][s], sc[kk], 0, 0, 0);
+          sc[kk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[s], sc[kk], 0, 0, 0);
         }
       if (tree_chunk) {
         MASK_BRANCH();
@@ -403,7 +375,7 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
             // the slot is tree row j (a prefix slot if j < 0)
             const int j = key0 + key_of_score(kk, lg, e) - Sc;
             const int sh = min(max(j - 1, 0), 63);
-            const bool vis = (j < 0) | ((j < n1c) & ((j == 0) | (bool)((anc[t] >> sh) & 1ull)));
+            const bool vis = (j < 0) | ((j < n1c) & ((j == 0) | (bool)((anc >> sh) & 1ull)));
             sc[kk][e] = vis ? sc[kk][e] : -INFINITY;
           }
       }
@@ -413,11 +385,11 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[kk][e]);
       mx = rows4_max(mx);
-      const float m_new = lazy_ref(m_run[t], mx, lazy);
+      const float m_new = lazy_ref(m_run, mx, lazy);
       const float m_use = m_new == -INFINITY ? 0.f : m_new;
       // raw v_exp_f32: results below 2^-126 flush to zero, which a softmax weight can spare
-      const float alpha = __builtin_amdgcn_exp2f((m_run[t] - m_use) * sscale);
-      m_run[t] = m_new;
+      const float alpha = __builtin_amdgcn_exp2f((m_run - m_use) * sscale);
+      m_run = m_new;
       const float mb = m_use * sscale;
       f16x8 pb[2];
       float rs = 0.f;
@@ -429,12 +401,12 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
           rs += p;
           pb[kk >> 1][(kk & 1) * 4 + e] = (f16)p;
         }
-      l_run[t] = l_run[t] * alpha + rs;
+      l_run = l_run * alpha + rs;
       if (__ballot(alpha < 1.f)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[t][nb][e] *= alpha;
+          for (int e = 0; e < 4; ++e) o[nb][e] *= alpha;
       }
       // O^T += V^T P^T over two k-steps of 32 keys.
 #pragma unroll
@@ -442,56 +414,8 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const f16x8 va = *(const f16x8 *)(sv + voff[ks] + nb * 16 * KC);
-          o[t][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[ks], o[t][nb], 0, 0, 0);
+          o[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[ks], o[nb], 0, 0, 0);
         }
-    }
-    if (quarter) {
-      // One 16-key block (key block qk of the chunk) of the split tile: 4 scores a lane.
-      f32x4 sq = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) {
-        const f16x8 kf = *(const f16x8 *)(sk + koff[s] + qkoff);
-        sq = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[QS][s], sq, 0, 0, 0);
-      }
-      if (tree_chunk) {
-        MASK_BRANCH();
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int j = key0 + key_of_score(qk, lg, e) - Sc;
-          const int sh = min(max(j - 1, 0), 63);
-          const bool vis = (j < 0) | ((j < n1c) & ((j == 0) | (bool)((anc[QS] >> sh) & 1ull)));
-          sq[e] = vis ? sq[e] : -INFINITY;
-        }
-      }
-      float mx = fmaxf(fmaxf(sq[0], sq[1]), fmaxf(sq[2], sq[3]));
-      mx = rows4_max(mx);
-      const float m_new = lazy_ref(m_run[QS], mx, lazy);
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f((m_run[QS] - m_use) * sscale);
-      m_run[QS] = m_new;
-      const float mb = m_use * sscale;
-      f16x4 pq;
-      float rs = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sq[e], sscale, -mb));
-        rs += p;
-        pq[e] = (f16)p;
-      }
-      l_run[QS] = l_run[QS] * alpha + rs;
-      if (__ballot(alpha < 1.f)) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[QS][nb][e] *= alpha;
-      }
-      // O^T += V^T P^T over the block's 16 keys: the lane's 4 probabilities are keys
-      // (qk/2)*32 + lg*8 + (qk%2)*4 + 0..3, half of one 16-byte V^T piece.
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const f16x4 va = *(const f16x4 *)(sv + qvoff + nb * 16 * KC);
-        o[QS][nb] = __builtin_amdgcn_mfma_f32_16x16x16f16(va, pq, o[QS][nb], 0, 0, 0);
-      }
     }
   }
   wait_vmcnt<0>();
@@ -501,84 +425,15 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
   }
   const bf16 *vtree = vb + S;   // the tree's values
 
-  if (split_last) {
-    // Merge the quarter units of each split tile (the ring is free once every wave is
-    // past its last chunk); each of a tile's 4 quarter waves finalises NB/4 head-dim blocks.
-    __syncthreads();
-    const int nquart = 4 * rlast;
-    f32x4 *mo = (f32x4 *)smem;                                  // [quarter][NB][64 lanes]
-    float *mml = (float *)smem + (size_t)nquart * NB * 64 * 4;  // [quarter][16 queries][2]
-    const int qu = wave - qbase;
-    if (quarter) {
-      const float l = rows4_sum(l_run[QS]);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) mo[(qu * NB + nb) * 64 + lane] = o[QS][nb];
-      if (lg == 0) {
-        mml[(qu * 16 + lr) * 2 + 0] = m_run[QS] == -INFINITY ? -INFINITY : m_run[QS] * sscale;
-        mml[(qu * 16 + lr) * 2 + 1] = l;
-      }
-    }
-    __syncthreads();
-    if (quarter) {
-      const int q0 = qu & ~3, tile = NW * QS + (qu >> 2);
-      float mj[4], wj[4];
-      float M = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        mj[j] = mml[((q0 + j) * 16 + lr) * 2];
-        M = fmaxf(M, mj[j]);
-      }
-      float L = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        wj[j] = mj[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj[j] - M);
-        L += wj[j] * mml[((q0 + j) * 16 + lr) * 2 + 1];
-      }
-      const int qi = (tbase + tile) * 16 + lr;
-      if (qi < QR) {
-        const int r = qi / G, h = g * G + (qi - r * G);
-#pragma unroll
-        for (int i = 0; i < NB / 4; ++i) {
-          const int nb = qk * (NB / 4) + i;
-          f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x4 v = mo[((q0 + j) * NB + nb) * 64 + lane];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += wj[j] * v[e];
-          }
-          if (nsplit == 1) {
-            const float inv = L > 0.f ? 1.0f / L : 0.f;
-            f16x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (f16)(acc[e] * inv);
-            *(f16x4 *)(out + act_off((int)row0 + r, h * HD + nb * 16 + lg * 4, rows_all, q_stride)) = v;
-          } else {
-            const size_t item = ((size_t)b * Hkv + g) * nsplit + split;
-            *(f32x4 *)(part_o + (item * QR + qi) * HD + nb * 16 + lg * 4) = acc;
-          }
-        }
-        if (nsplit > 1 && qk == 0 && lg == 0) {
-          const size_t item = ((size_t)b * Hkv + g) * nsplit + split;
-          part_ml[(item * QR + qi) * 2 + 0] = M;
-          part_ml[(item * QR + qi) * 2 + 1] = L;
-        }
-      }
-    }
-  }
-
-  // o[t][nb][e] is head dim nb*16 + lg*4 + e of query tile*16 + lr.
-#pragma unroll
-  for (int t = 0; t < UPW; ++t) {
-    const int tile = wave + NW * t;
-    if (tile >= ntiles || (split_last && t == QS)) break;
-    const float l = rows4_sum(l_run[t]);
-    const int qi = (tbase + tile) * 16 + lr;
-    if (qi >= QR) continue;
+  // o[nb][e] is head dim nb*16 + lg*4 + e of query wave*16 + lr.
+  if (wave < ntiles) {
+    const float l = rows4_sum(l_run);
+    const int qi = wave * 16 + lr;
+    if (qi >= QR) return;
     const int r = qi / G, h = g * G + (qi - r * G);
     if (PART && join.here) {
       shared_finish<HD>(join, me, total_units, ancs, vtree, capacity, bad, b, g, qi, n1, H, Hkv, rows_all,
-                        m_run[t] == -INFINITY ? -INFINITY : m_run[t] * sscale, l, o[t],
+                        m_run == -INFINITY ? -INFINITY : m_run * sscale, l, o,
                         [&](int nb) { return nb * 16 + lg * 4; });
     } else if (!PART && nsplit == 1) {
       const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -586,16 +441,16 @@ __global__ __launch_bounds__(NW * 64, 4) void tree_attn_mfma_kernel(
       for (int nb = 0; nb < NB; ++nb) {
         f16x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (f16)(o[t][nb][e] * inv);
+        for (int e = 0; e < 4; ++e) v[e] = (f16)(o[nb][e] * inv);
         *(f16x4 *)(out + act_off((int)row0 + r, h * HD + nb * 16 + lg * 4, rows_all, q_stride)) = v;
       }
     } else {
       const size_t item = ((size_t)b * Hkv + g) * nsplit + split;
       float *po = part_o + (item * QR + qi) * HD + lg * 4;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(po + nb * 16) = o[t][nb];
+      for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(po + nb * 16) = o[nb];
       if (lg == 0) {
-        part_ml[(item * QR + qi) * 2 + 0] = m_run[t] == -INFINITY ? -INFINITY : m_run[t] * sscale;
+        part_ml[(item * QR + qi) * 2 + 0] = m_run == -INFINITY ? -INFINITY : m_run * sscale;
         part_ml[(item * QR + qi) * 2 + 1] = l;
       }
     }
@@ -1167,13 +1022,13 @@ __global__ __launch_bounds__(256) void tree_attn_f32_kernel(
 // Ring depth: 4 stages of 32 KB (head_dim 128) or 16 KB (head_dim 64).
 template <int HD> struct AttnCfg { static constexpr int NST = 4; };
 
-template <int HD, int NW, int UPW, int NST, int MODE, typename TQ>
+template <int HD, int NW, int NST, int MODE, typename TQ>
 void launch_mfma(dim3 grid, hipStream_t s, const TQ *q, const bf16 *ck, const bf16 *cv,
                  const TreeMeta &meta, f16 *out, float *po, float *pml, int n1, int H, int Hkv,
-                 int capacity, int nsplit, int tpg, const SharedJoin &join) {
-  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, UPW, NST, MODE, TQ>), grid,
+                 int capacity, int nsplit, const SharedJoin &join) {
+  hipLaunchKernelGGL((tree_attn_mfma_kernel<HD, NW, NST, MODE, TQ>), grid,
                      dim3(NW * 64), 0, s, q, ck, cv, meta, out, po, pml, n1, H, Hkv,
-                     capacity, nsplit, tpg, join);
+                     capacity, nsplit, join);
 }
 
 // Key splits: as many as the CUs hold at once, rounded down, for a second round of a few
@@ -1239,19 +1094,12 @@ hipError_t launch_tree_attn(const TQ *q, const bf16 *ck, const bf16 *cv, const T
       hipLaunchKernelGGL((tree_attn_t32_kernel<64, AttnCfg<64>::NST, MODE, TQ>), grid, dim3(512), 0, s,
                          q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit,
                          rpg, join);
-  } else if (PART && workgroups_a_cu(all_tiles) == 2) {
-    if (hd == 128)
-      launch_mfma<128, 8, 1, 2, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                                          capacity, nsplit, all_tiles, join);
-    else
-      launch_mfma<64, 8, 1, 4, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                                         capacity, nsplit, all_tiles, join);
-  } else if (hd == 128) {
-    launch_mfma<128, 16, 1, 4, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                                         capacity, nsplit, all_tiles, join);
   } else {
-    launch_mfma<64, 16, 1, 4, MODE, TQ>(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv,
-                                        capacity, nsplit, all_tiles, join);
+    auto launch = hd == 128 ? launch_mfma<128, 16, 4, MODE, TQ> : launch_mfma<64, 16, 4, MODE, TQ>;
+    if constexpr (PART)
+      if (workgroups_a_cu(all_tiles) == 2)
+        launch = hd == 128 ? launch_mfma<128, 8, 2, MODE, TQ> : launch_mfma<64, 8, 4, MODE, TQ>;
+    launch(grid, s, q, ck, cv, meta, out, part_o, part_ml, n1, H, Hkv, capacity, nsplit, join);
   }
   return hipGetLastError();
 }

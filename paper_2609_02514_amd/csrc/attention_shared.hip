@@ -40,7 +40,7 @@ AS_DEVICE f16x8 to_f16x8(bf16x8 v) { return bf16x8_to_f16x8(v); }
 // PFLOP/s (475 to 525 us), the matrix cores 56 % busy at the 1.73 GHz that the card's power leaves; 64
 // sessions of 68 rows behind up to 8192 slots 105 to 123 us, 42 % busy at 2.0 GHz, as a workgroup goes
 // through one and a half tiles there.
-template <int HD, int NST, typename TQ>
+template <int HD, typename TQ>
 __global__ __launch_bounds__(512) void shared_attn_kernel(
     const TQ *__restrict__ q, const f16 *__restrict__ blocks, SharedMeta sm,
     float *__restrict__ part_o, float *__restrict__ part_ml, int B, int n1, int H, int Hkv, int cap,
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(512) void shared_attn_kernel(
   constexpr int KS = HD / 16, NDB = HD / 32;
   constexpr int REC = 128 * HD;                 // elements of a record
   constexpr int L_DMA = REC * 2 / 1024 / 8;     // 1 KB pieces a wave
-  static_assert(NST == 4, "the loop holds two records and has one in flight beside the next");
+  constexpr int NST = 4;   // stages: the loop holds two records and has one in flight beside the next
   __shared__ __attribute__((aligned(1024))) f16 smem[NST * REC];
   const int t = xcd_tile(blockIdx.x, gridDim.x), g = t / wgs, w = t - g * wgs;
   // (the groups are asked for, 64 at a time, before it is known how many there are)
@@ -577,7 +577,7 @@ hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const
     if (e != hipSuccess) return e;
   }
   if (!direct) {
-    hipLaunchKernelGGL((shared_attn_kernel<HD, 4, TQ>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
+    hipLaunchKernelGGL((shared_attn_kernel<HD, TQ>), dim3(wgs * Hkv), dim3(512), 0, s, q, blocks, sm,
                        sh_o, sh_ml, B, n1, H, Hkv, sh.cap, wgs, j.rows_total);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
