@@ -388,14 +388,17 @@ int acespec_commit_kv_quant(acespec_ctx *ctx, const acespec_kv_quant *qc, const 
 
 /* ---- Sessions behind shared prefixes ----------------------------------------------------
  * Prefixes that several sessions of a batch have in common (a system prompt, a document, the
- * prompt of several samples) are held once, apart from the sessions' own caches, and attended to
- * once for all rows of the sessions behind them.  A session behind a prefix of n slots that has P
+ * prompt of several samples) are held once, apart from the sessions' own caches.  A bf16 model's
+ * larger batches attend to them once for all rows of the sessions behind them; where that takes
+ * longer (few rows or few slots, by the capacities of store and cache), and in an fp32 model, each
+ * session reads its prefix for itself.  Caches in 4 bits (above) stand behind no shared prefix and
+ * take no norms.  A session behind a prefix of n slots that has P
  * own slots in its acespec_kv_cache (prefix_len[b] = P) is at position n + P; own slot i is
  * position n + i, and tree row r writes slot P + r.  acespec_commit_kv serves the own cache as it
  * is.
  *  blocks  [n_layers][prefixes][n_kv_heads][capacity / 64] records of 128 * head_dim elements, in
- *          fp16 for a bf16 model (a value beyond its range counts as infinite, as in the verify
- *          step) and in fp32 for an fp32 model.  A record holds 64 slots' keys and values in the
+ *          fp16 for a bf16 model (as in the verify step a value beyond its range counts as
+ *          infinite, and one below 2^-14 keeps multiples of 2^-24 only) and in fp32 for an fp32 model.  A record holds 64 slots' keys and values in the
  *          order of the attention's matrix operands; acespec_share_prefix writes it.
  *  len     [prefixes] slots held, in [0, capacity]; what lies behind them is not read as numbers.
  * One prefix and kv head takes less than 2 GiB (ACESPEC_EUNSUPPORTED otherwise). */
@@ -442,7 +445,9 @@ int acespec_attention_shared(acespec_ctx *ctx, const acespec_kv_shared *sh, cons
 /* From one layer's projection qkv [B, N+1, (n_heads + 2 n_kv_heads) head_dim] (model dtype; heads
  * of q, k, v) in one pass: every query and key head normalised as norm says and rotated to its
  * row's position (prefix, own slots and depth in the tree), q [B, N+1, n_heads, head_dim] written,
- * and the keys and values into slots prefix_len[b] + r of kv's layer.  sh and prefix_of may be NULL
+ * and the keys and values into slots prefix_len[b] + r of kv's layer.  Sines and cosines are
+ * evaluated in 32 bits of an angle that is reduced in 64 (off by 2^-23; the verify step's are
+ * rounded from 64 bits, so that the two may differ in a last bit).  sh and prefix_of may be NULL
  * (both): no session stands behind a prefix.  Nothing of a session with a bad status is written. */
 int acespec_qk_norm_rope(acespec_ctx *ctx, const acespec_qk_norm *norm, const acespec_kv_shared *sh,
                          const int32_t *prefix_of, const acespec_kv_cache *kv, int layer,

@@ -560,11 +560,20 @@ hipError_t launch_hd(const TQ *q, const f16 *blocks, const SharedArgs &sh, const
   const int here = 3LL * rows * (H / Hkv) >= (long long)wgs * TM;
   // Small batches over short prefixes: the kernel over the own slots takes the records first, each
   // session for itself, which leaves the tiles' way in and out of memory, and a launch, away.  It is
-  // taken up to 18 chunks in turn of head dim 128 or 36 of 64 (17 rows, 8 kv heads; so taken, by
-  // tiles: 8 sessions behind 2048 slots, 9 chunks, 27.5 us, 39.3; 16 behind 2048, 9, 35.6, 47.7; 64
-  // behind 1024, 18, 51, 62; 16 behind 4096, 17, 51, 55; 24 behind 2048, 34, 79, 55), single tokens
-  // up to 16, as they leave the tiles little to do (8 behind 8192, 17, 39.6, 33.1; 16 behind 1024, 6,
-  // 23.8, 31.5).
+  // taken up to 18 chunks in turn of head dim 128 or 36 of 64, single tokens up to 16 or 32, as they
+  // leave the tiles little to do.  Both sides in us (so taken, by tiles), 64 own slots, captured:
+  //   17 rows, 4 heads a kv head, head dim 128: 8 sessions behind 2048 slots (9 chunks) 28.5, 44.9;
+  //   8 behind 8192 (17) 48.3, 52.8; 64 behind 1024 (18) 47.6, 59.1; 32 behind 2048 (34) 59.3, 59.8;
+  //   16 behind 8192 (33) 76.0, 69.5; of 64: 16 behind 8192 (33) 50.8, 56.4; 64 behind 2048 (34) 47.8,
+  //   51.7; 64 behind 4096 (66) 80.1, 70.9.
+  //   Single tokens, 128: 8 behind 4096 (9) 26.9, 28.2; 8 behind 8192 (17) 40.8, 28.0; of 64: 64 behind
+  //   1024 (18) 24.0, 26.2, but 16 behind 4096 (17) 24.8, 22.1; 32 behind 2048 (34) 27.7, 22.5.
+  //   More than 8 tiles, one workgroup a CU, 8 heads a kv head, 128: 17 rows, 16 behind 2048 (17)
+  //   48.6, 58.9; 64 behind 512 (20) 55.9, 73.7; 32 behind 2048 (34) 61.7, 74.2; 33 rows, 8 behind 4096
+  //   (17) 66.1, 81.0; 16 behind 4096 (33) 107, 113; 64 behind 1024 (36) 121, 143; of 64: 17 rows, 32
+  //   behind 2048 (34) 52.0, 50.7; 16 behind 8192 (65) 96.0, 76.3.
+  // (With more than 8 tiles of head dim 128 sessions could go further for themselves, with single
+  // tokens of 64 less far; of the sizes measured none loses more than a third of the other way's time by it.)
   const int chunks = acespec::attention_chunks_in_turn(B, n1, H, Hkv, HD, (sh.cap + capacity) / 64, cus, part_cap);
   const bool direct = (long long)chunks * HD <= (H / Hkv * n1 <= 16 ? 16 : 18) * 128;
   const SharedJoin j{sh_o, sh_ml, sm, wgs,

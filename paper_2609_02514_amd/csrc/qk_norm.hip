@@ -2,9 +2,10 @@
 // values written into the cache: y = x / sqrt(mean(x^2) + eps) * gain over a head's dims, then the
 // rotation of (y_i, y_{i + hd/2}) by position * base^(-2i/hd), in one pass over the projection.
 //
-// Memory bound (the projection read once, rotated queries, keys and values written once: 64 sessions of
-// 17 rows, 32 query and 8 kv heads of 128 dims 11 us, where the bytes alone take 4); with few rows
-// the chain of loads (one row 4.2).  A lane holds 8 dims of a head's lower half and their partners in the
+// Bound by the chain of loads (the projection read once, rotated queries, keys and values written once:
+// 64 sessions of 17 rows, 32 query and 8 kv heads of 128 dims 11 us, where the bytes alone take 4: 9
+// rows of 8 heads are 576 lanes' work for a workgroup of 256, three rounds of which each asks for its
+// loads when the one before is computed; one row 4.2).  A lane holds 8 dims of a head's lower half and their partners in the
 // upper half, so that a pair never crosses lanes and the sum of squares is 3 lane swaps (2 for
 // head dim 64).  A workgroup takes some rows of a session and some query and key heads, whose loads
 // are under way while it evaluates the rows' angles; or one value head of a session.

@@ -165,6 +165,54 @@ def test_parts_join_apart_one_session_short():
               sample=random.Random(N).sample(range(B), 8))
 
 
+# ---- what fp16 keeps --------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("N", [0, 16, 64])
+def test_values_below_fp16s_normal_range_keep_multiples_of_its_least(hd, tiles, N):
+    """Keys and values that are multiples of 2^-24 below 2^-14, as the store and the products hold them.
+    Keys: queries of some 2^14 make scores that weights show.  Values: the
+    same 3 * 2^-24 in every slot, whose mean is itself."""
+    from paper_2609_02514_amd.acespec import SharedPrefix
+    H, Hkv, held, mine, B, n1 = 8, 2, 200, [0, 70, 33], 3, N + 1
+    cap = up64(max(mine) + n1)
+    g = torch.Generator().manual_seed(hd + N)
+
+    def least(*shape):
+        return (torch.randint(-255, 256, shape, generator=g) * 2.0 ** -24).to(torch.bfloat16).cuda()
+    k, v = least(1, B, Hkv, cap, hd), torch.randn(1, B, Hkv, hd, cap, generator=g).to(torch.bfloat16).cuda()
+    sk, sv = least(1, 1, Hkv, up64(held), hd), torch.randn(1, 1, Hkv, hd, up64(held), generator=g).to(torch.bfloat16).cuda()
+    q = (torch.randn(B, n1, H, hd, generator=g) * 2.0 ** 14).to(torch.bfloat16).clamp(-60000, 60000).cuda()
+    ver, r = verifier(1, B, H, Hkv, hd, "bf16", N), random.Random(N)
+    parents = [random_parents(r, N) for _ in range(B)]
+    shared = SharedPrefix.alloc(1, 1, Hkv, hd, large() if tiles else held, "bf16")
+    for same in (False, True):
+        new = i32([0])
+        if same:
+            v.fill_(3 * 2.0 ** -24)
+            sv.fill_(3 * 2.0 ** -24)
+        ver.share_prefix(sk, sv, up64(held), i32([held]), i32([0]), shared, new)
+        shared.len = new
+        out, status = torch.full_like(q, -77.0), i32([9] * B)
+        ver.attention_shared(shared, i32([0] * B), k, v, cap, i32(mine), 0, q, i32(parents), out, status)
+        torch.cuda.synchronize()
+        assert status.tolist() == [0] * B
+        for b, m in enumerate(mine):
+            want, mag, big = sr.attend(q[b], (sk[0, 0, :, :held], sv[0, 0, :, :, :held].transpose(1, 2)),
+                                       k[0, b, :, :m + n1], v[0, b, :, :, :m + n1], m, parents[b])
+            if same:   # weights off by 2^-11 and the output by 2^-8, of which the mean keeps both
+                tol = want.abs() * (2.0 ** -11 + 2.0 ** -8 + 2.0 ** -18)
+            else:
+                tol = bound("bf16", want, mag, big, hd)
+                flat, _, _ = sr.attend(q[b], (0 * sk[0, 0, :, :held], sv[0, 0, :, :, :held].transpose(1, 2)),
+                                       0 * k[0, b, :, :m + n1], v[0, b, :, :, :m + n1], m, parents[b])
+                assert float(((flat - want).abs() / tol).max()) > 4   # (keys taken for zeros would show)
+            assert bool(((out[b].double() - want).abs() <= tol).all()), (same, b)
+    ver.close()
+
+
 # ---- malformed sessions -----------------------------------------------------------------------
 
 
