@@ -11,11 +11,11 @@
 //  * every tile into the same number of pieces, which is taken where the longest of these is
 //    shorter than an even piece and the price of a second tile in it (six records: eight sessions of
 //    17 rows behind 2000 slots, three tiles, 44 us evenly cut and 37 tile by tile).
-// There are no more pieces than of LEAST records each (evenly: of all records; tile by tile: of the
-// longest tile's, so that a shorter tile beside it is cut into shorter ones, ten of one record where
-// the longest is cut into ten of four): short pieces finish sooner, but each leaves its rows' results
-// to be written and read (64 single tokens behind
-// 8192 slots: 61.0 us at two records, 58.1 at four, 59.6 at eight; 32 behind 2048 34.9, 35.3 and 38.0).
+// An even piece has LEAST records at least, unless there are more tiles than such pieces; tile by tile
+// the longest tile's pieces follow from LEAST, and a shorter tile beside it is cut into as many (ten of
+// one record where the longest has ten of four).  Short pieces finish sooner, but each leaves its rows'
+// results to be written and read (64 single tokens behind 8192 slots: 61.0 us at two records, 58.1 at
+// four, 59.6 at eight; 32 behind 2048 34.9, 35.3 and 38.0).
 struct SharedLine {
   static constexpr int LEAST = 4;
   int n, each, more;   // workgroups; evenly: records of each, and one more for the first `more`
