@@ -12,7 +12,7 @@ import synth
 from oracle import model as om
 from tests import harness as hz
 from tests import shared_ref as sr
-from tests.test_gpu_shared import DT, bound, gains, i32, random_cache, random_parents, store, up64, verifier, workload
+from tests.test_gpu_shared import DT, bound, gains, i32, random_cache, random_parents, start, store, up64, verifier, workload
 
 pytestmark = pytest.mark.gpu
 
@@ -295,15 +295,69 @@ def test_steps_with_packed_weights_behind_one_prefix(kw, shared_slots, packed, n
     F64, dims, parents = om.F64Weights(W), om.dims_of(w), batch.parents.tolist()
     n64 = [tuple(om.to_f64(x) for x in pair) for pair in norms] if normed else None
     for b in [0, w.B - 1] if joined else range(w.B):
-        at = [0] * shared_slots + [b] * (lens[b] - shared_slots)
+        at = torch.tensor([0] * shared_slots + [b] * (lens[b] - shared_slots), device="cuda")
         slots = torch.arange(lens[b], device="cuda")
-        kpre = [om.to_f64(batch.kv_k[l][torch.tensor(at, device="cuda"), :, slots]).transpose(1, 0, 2) for l in range(w.L)]
-        vpre = [om.to_f64(batch.kv_v[l][torch.tensor(at, device="cuda"), :, :, slots]).transpose(1, 0, 2) for l in range(w.L)]
+        kpre = [om.to_f64(batch.kv_k[l][at, :, slots]).transpose(1, 0, 2) for l in range(w.L)]
+        vpre = [om.to_f64(batch.kv_v[l][at, :, :, slots]).transpose(1, 0, 2) for l in range(w.L)]
         z, _ = sr.forward(F64, dims, kpre, vpre, batch.tokens[b].tolist(), parents[b], lens[b], n64)
         got = outs[0]["logits_out"].view(w.B, n1, w.V)[b].double().cpu().numpy()
         err = abs(got - z).max() / abs(z).max()
         hz.log(f"  session {b}: logits off by {err:.2e} of the largest")
         assert err < 2e-2
+    ver.close()
+
+
+@pytest.mark.parametrize("dtype, tiles", [("bf16", False), ("bf16", True), ("f32", False)])
+def test_malformed_sessions_of_a_step(dtype, tiles):
+    """A step in which four of six sessions are malformed, each in its way: flagged, nothing of the others'
+    caches touched, and the others decide as without them (by tiles, where the prefixes are cut
+    elsewhere then, up to a few roundings to fp16 of each layer's activations, 2^-11 each)."""
+    from paper_2609_02514_amd.acespec import ACESPEC_EBADTREE, SharedPrefix
+    w = workload(dtype, B=6, H=8, Hkv=2, hd=128, d=512)
+    W, norms = synth.make_weights(w, "cuda"), gains(w)
+    batch, ver, shared, of, k, v, cap, own = start(w, [60, 40, 0, 70, 30, 20])
+    if tiles:
+        wide = SharedPrefix.alloc(w.L, shared.prefixes, w.Hkv, w.hd, large(), dtype)
+        wide.blocks[:, :, :, :shared.blocks.shape[3]] = shared.blocks
+        wide.len = shared.len
+        shared = wide
+    n1, ws, held = batch.tokens.shape[1], ver.weights_struct(W), shared.len.tolist()
+    k0, v0 = k.clone(), v.clone()
+
+    def step(of, lens, own, parents):
+        outs = ver.alloc_outputs(w.B * n1, w.B, n1, w.top_k, w.V, "cuda", True)
+        shared.len = i32(lens)
+        k.copy_(k0)
+        v.copy_(v0)
+        ver.verify_tree_shared(ws, shared, of, k, v, cap, own, batch.tokens, parents, batch.q, batch.u, w.T, w.top_p,
+                               w.top_k, outs, norms)
+        torch.cuda.synchronize()
+        return outs
+    good = step(of, held, own, batch.parents)
+    assert good["status"].tolist() == [0] * w.B
+    gk, gv = k.clone(), v.clone()
+    of2, own2, parents, lens = of.clone(), own.clone(), batch.parents.clone(), list(held)
+    of2[1] = shared.prefixes
+    lens[of.tolist()[3]] = shared.capacity + 1
+    own2[4] = cap - n1 + 1
+    parents[5, 3] = 3
+    hz.log(f"verify_tree_shared {dtype} tiles={tiles} with malformed sessions")
+    bad = step(of2, lens, own2, parents)
+    assert bad["status"].tolist() == [0, ACESPEC_EBADTREE, 0, ACESPEC_EBADTREE, ACESPEC_EBADTREE, ACESPEC_EBADTREE]
+    for b in (0, 2):
+        rows = slice(b * n1, (b + 1) * n1)
+        if tiles:
+            x, y = good["logits_out"][rows].double(), bad["logits_out"][rows].double()
+            assert float((x - y).norm() / x.norm()) < 8 * 2.0 ** -11
+            continue
+        assert torch.equal(gk[:, b], k[:, b]) and torch.equal(gv[:, b], v[:, b])
+        for name, t in good.items():
+            at = slice(b, b + 1) if t.shape[0] == w.B else rows
+            assert torch.equal(t[at], bad[name][at]), (name, b)
+    for b, m in enumerate(own.tolist()):   # beside the tree's slots (where the call takes them to be) nothing changes
+        at = min(max(own2.tolist()[b], 0), cap - n1)
+        for new, was in ((k[:, b], k0[:, b]), (v[:, b].transpose(2, 3), v0[:, b].transpose(2, 3))):
+            assert torch.equal(new[:, :, :at], was[:, :, :at]) and torch.equal(new[:, :, at + n1:], was[:, :, at + n1:])
     ver.close()
 
 
@@ -316,8 +370,8 @@ def test_normed_rotation_refuses_each_wrong_tensor_by_its_name():
     shared, _, _ = store(L, [70], Hkv, hd, "bf16", 1)
     k, v = random_cache(L, B, Hkv, 128, hd, "bf16", 2)
     bf = dict(dtype=torch.bfloat16, device="cuda")
-    good = dict(qkv=torch.zeros(B, N + 1, (H + 2 * Hkv) * hd, **bf), q_gain=torch.ones(hd, **bf), k_gain=torch.ones(hd, **bf),
-                kv_k=k, kv_v=v, capacity=128, prefix_len=i32([1, 2]), layer=0, parents=i32([[-1, 0, 1, 2]] * B),
+    good = dict(qkv=torch.zeros(B, N + 1, (H + 2 * Hkv) * hd, **bf), q_gain=torch.ones(hd, **bf),
+                k_gain=torch.ones(hd, **bf), kv_k=k, kv_v=v, capacity=128, prefix_len=i32([1, 2]), layer=0, parents=i32([[-1, 0, 1, 2]] * B),
                 q_out=torch.zeros(B, N + 1, H, hd, **bf), status=i32([9] * B), shared=shared, prefix_of=i32([0, 0]))
     ver.qk_norm_rope(**good)
     torch.cuda.synchronize()
